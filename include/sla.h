@@ -76,8 +76,10 @@ typedef enum {
     SLA_ERR_WORKSPACE = -3,      /* the handle's workspace is too small for this call             */
     SLA_ERR_CUDA = -4,           /* a CUDA runtime call failed (see sla_last_error)               */
     SLA_ERR_DEVICE_TIMEOUT = -5, /* a bounded device-side wait expired                            */
-    SLA_ERR_DEVICE_INDEX = -6,   /* a kernel met an anchor outside [0, i] and skipped it          */
-    SLA_ERR_DEVICE_OVERRUN = -7  /* debug canaries: a kernel wrote outside its scratch region      */
+    SLA_ERR_DEVICE_INDEX = -6,   /* a kernel met an anchor outside [0, i], or a slot, length or page
+                                    outside a paged cache, and skipped it                          */
+    SLA_ERR_DEVICE_OVERRUN = -7, /* debug canaries: a kernel wrote outside its scratch region      */
+    SLA_ERR_CACHE_FULL = -8      /* a sequence was refused pages: none free, or its table row full */
 } sla_status_t;
 
 typedef enum { SLA_F32 = 0, SLA_BF16 = 1 } sla_dtype_t;
@@ -140,7 +142,7 @@ const char *sla_status_string(sla_status_t status); /* static string, never NULL
 const char *sla_last_error(sla_handle_t handle);    /* text of the last failure on this handle     */
 
 /* Waits for `stream` and reads the device status word: SLA_OK, SLA_ERR_DEVICE_OVERRUN,
- * SLA_ERR_DEVICE_TIMEOUT or SLA_ERR_DEVICE_INDEX; the word is cleared. */
+ * SLA_ERR_DEVICE_TIMEOUT, SLA_ERR_DEVICE_INDEX or SLA_ERR_CACHE_FULL; the word is cleared. */
 sla_status_t sla_poll_status(sla_handle_t handle, void *stream);
 
 /* Number of kernels this handle has launched since sla_create (a diagnostic for benchmarks; the
@@ -348,6 +350,121 @@ sla_status_t sla_prefill_host(sla_handle_t handle, const void *q_s_host, const v
                               const void *k_host, const void *v_host, int64_t L,
                               const sla_layout_t *layout, const sla_params_t *params, void *out_host,
                               float *lse_host, int32_t *anchor_host, float *score_host, void *stream);
+
+/* ---- paged key/value cache ---------------------------------------------------------------------
+ *
+ * (The paper has no counterpart: its cache is one contiguous sequence.  A serving program holds many
+ * sequences of different lengths that grow, share their beginnings and end.)  The cache is a pool of pages of page_tokens tokens, a table that says which page holds which
+ * part of which sequence, and counts:
+ *
+ *   k, v      [n_pages, n_kv_heads, page_tokens, head_dim]  strides stride_{page,h,t}, head_dim contiguous
+ *   table     int32 [n_slots, table_width]  page of positions [c * page_tokens, (c+1) * page_tokens) of the
+ *             sequence in this slot; -1 = none
+ *   n_tokens  int32 [n_slots]  tokens of the sequence in this slot; 0 = the slot is empty
+ *   ref       int32 [n_pages]  table entries that name this page; 0 = the page is free
+ *
+ * All of it is the caller's device memory; a new cache is table = -1, n_tokens = 0, ref = 0 (k and v need
+ * no initial value: what lies in a page beyond its sequence's last token never reaches a result, NaN
+ * included).  Lengths live on the device: no call waits for them, and all can be captured into a graph.
+ * Models of several layers share table, n_tokens and ref and have k and v per layer: extend, release, fork
+ * and compact then run once with any layer's k and v, sla_cache_copy with the pairs that fork and compact
+ * return for each other layer, append and attention for every layer.
+ *
+ * Sharing: sla_cache_fork lets sequences share full pages; a partly filled page belongs to one sequence
+ * only, so that appending never writes into another's tokens.  Pages are handed out in ascending order of
+ * their index, in the order of the call's sequences: results do not depend on timing.
+ *
+ * What the device finds wrong -- a slot outside [0, n_slots), a table entry outside [0, n_pages) where
+ * the sequence has tokens, lengths that do not fit the table -- sets the status word
+ * (SLA_ERR_DEVICE_INDEX at the next sla_poll_status); nothing outside the cache is read or written. */
+typedef struct {
+    int32_t n_pages, page_tokens;   /* page_tokens: a power of two, 16 .. 256                     */
+    int32_t n_kv_heads, head_dim;   /* head_dim 64 or 128                                          */
+    int32_t dtype, reserved;        /* sla_dtype_t of k and v; reserved must be 0                   */
+    int32_t n_slots, table_width;
+    int64_t stride_page, stride_h, stride_t; /* of k and v, in elements                            */
+    void *k, *v;
+    int32_t *table, *n_tokens, *ref;
+} sla_cache_t;
+
+/* The sequences of one call.  n_new tokens in all: those of sequence x are rows cu_new[x] .. cu_new[x+1]-1 of
+ * the call's [n_new, heads, head_dim] tensors. */
+typedef struct {
+    int32_t n_seqs;
+    int32_t n_new;            /* rows of the tensors: cu_new[n_seqs]                                  */
+    int32_t max_new;          /* no sequence has more new tokens than this                           */
+    int32_t reserved;         /* must be 0                                                           */
+    const int32_t *seq;       /* device [n_seqs]: slots, all different; NULL = 0 .. n_seqs-1         */
+    const int32_t *cu_new;    /* device [n_seqs + 1], ascending from 0; NULL = one token a sequence   */
+} sla_batch_t;
+
+/* Workspace bytes that every call below needs at most, for batches of up to n_seqs sequences and n_new
+ * tokens and n_q_heads query heads.  params: of sla_paged_decode_step, NULL when it is not called.  0 when the
+ * arguments are invalid.  Host-only. */
+size_t sla_paged_workspace_bytes(const sla_cache_t *cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_new,
+                                 const sla_params_t *params);
+
+/* Makes room for the new tokens of every sequence of the batch: takes free pages, writes them into the
+ * table and adds the new tokens to n_tokens.  first [n_seqs] int32, device, out: the position of the
+ * sequence's first new token, or -1 for a sequence that was refused and left as it was -- fewer free pages
+ * than it and the sequences before it need, or a table row that is too short (SLA_ERR_CACHE_FULL at the next
+ * sla_poll_status). */
+sla_status_t sla_cache_extend(sla_handle_t handle, const sla_cache_t *cache, const sla_batch_t *batch,
+                              int32_t *first, void *stream);
+
+/* Writes the new tokens' keys and values: row r of sequence x goes to position first[x] + r.  k_new, v_new
+ * [n_new, n_kv_heads, head_dim], strides new_stride_{t,h} in elements.  Sequences with first < 0 are left out. */
+sla_status_t sla_cache_append(sla_handle_t handle, const sla_cache_t *cache, const sla_batch_t *batch,
+                              const int32_t *first, const void *k_new, const void *v_new, int64_t new_stride_t,
+                              int64_t new_stride_h, void *stream);
+
+/* Ends the sequences in the n slots seq (device): their pages lose a reference each, and the slots are empty. */
+sla_status_t sla_cache_release(sla_handle_t handle, const sla_cache_t *cache, const int32_t *seq, int32_t n,
+                               void *stream);
+
+/* Makes the n empty slots dst (all different) copies of the sequences in the slots src (any of them several
+ * times; none of them in dst).  Full pages are shared, a partly filled last page is copied into a page of its
+ * own.  pairs [2, n] int32, device, out: the page that was copied and the page it was copied to, -1 where
+ * nothing was.  A slot that is not empty (SLA_ERR_DEVICE_INDEX) or for which no page is left
+ * (SLA_ERR_CACHE_FULL) is left as it was. */
+sla_status_t sla_cache_fork(sla_handle_t handle, const sla_cache_t *cache, const int32_t *src,
+                            const int32_t *dst, int32_t n, int32_t *pairs, void *stream);
+
+/* Moves every page in use to the front of the pool, so that the pages in use are 0 .. m-1: those of index m
+ * and above go, in ascending order, to the free ones below m in ascending order; table and ref follow.
+ * pairs [2, n_pages] int32, device, out: from and to which page, -1 after the last move. */
+sla_status_t sla_cache_compact(sla_handle_t handle, const sla_cache_t *cache, int32_t *pairs, void *stream);
+
+/* Copies page pairs[0][j] of k and v to page pairs[1][j], j < n (device); pairs with a negative entry are
+ * skipped.  No page may be written by one pair and read or written by another. */
+sla_status_t sla_cache_copy(sla_handle_t handle, const sla_cache_t *cache, const int32_t *pairs, int32_t n,
+                            void *stream);
+
+/* Dense causal attention of the new tokens over the cache, which already holds them: row r of sequence x
+ * is position i = n_tokens - (its new tokens) + r and attends to positions [0, i], or with a local window w
+ * (the W of Algorithm 1) to [max(0, i-w+1), i].  The form for contexts too short for spans to pay (the paper
+ * puts that at about 60K tokens), for chunks of a prefill and single tokens alike.
+ *   q     in   [n_new, n_q_heads, head_dim]  strides q_stride_{t,h}, cache dtype; group size <= 16
+ *   out   out  as q;  lse out [n_new, n_q_heads] fp32 contiguous (natural log); a row without keys (a
+ *              sequence that is shorter than its new tokens) is 0 and -inf
+ * bf16 runs on the tensor cores with fp32 sums (weights are rounded to bf16 before they meet the values),
+ * fp32 in fp32. */
+sla_status_t sla_paged_attention(sla_handle_t handle, const void *q, const sla_cache_t *cache,
+                                 const sla_batch_t *batch, int32_t n_q_heads, int64_t q_stride_t,
+                                 int64_t q_stride_h, int32_t window, float softmax_scale, void *out, float *lse,
+                                 void *stream);
+
+/* sla_decode_step (Section "Kernel design", "Decoding path") for the sequences of a paged cache, each at its
+ * own length: query position i = n_tokens - 1 of the slot.  batch->cu_new and max_new are not read and may be
+ * NULL and 0; max_tokens is a bound of the lengths (it sizes the grids; a longer sequence is refused with
+ * SLA_ERR_DEVICE_INDEX, output 0, lse -inf, no anchors, as an empty one without the status).
+ *   q_s, q     in   [n_seqs, n_q_heads, head_dim]  strides q_stride_{b,h}
+ *   out, lse, out_anchor, out_score  as for sla_decode_step with B = n_seqs; anchors are positions of the
+ *                   sequence */
+sla_status_t sla_paged_decode_step(sla_handle_t handle, const void *q_s, const void *q, const sla_cache_t *cache,
+                                   const sla_batch_t *batch, int64_t max_tokens, int32_t n_q_heads,
+                                   int64_t q_stride_b, int64_t q_stride_h, const sla_params_t *params, void *out,
+                                   float *lse, int32_t *out_anchor, float *out_score, void *stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,10 @@ SLA_OK = 0
 SLA_F32, SLA_BF16 = 0, 1
 SLA_UNION, SLA_PER_SPAN = 0, 1
 SLA_ERR_INVALID_ARG = -1
+SLA_ERR_UNSUPPORTED = -2
+SLA_ERR_WORKSPACE = -3
+SLA_ERR_DEVICE_INDEX = -6
+SLA_ERR_CACHE_FULL = -8
 
 EXPORTS = [
     "sla_create", "sla_destroy", "sla_workspace_bytes", "sla_status_string", "sla_last_error",
@@ -29,6 +33,8 @@ EXPORTS = [
     "sla_decode_shard_search", "sla_decode_shard_attend", "sla_decode_shard_merge",
     "sla_pattern_offsets", "sla_pattern_len_steps", "sla_probe_l2_read", "sla_selftest_wait_expiry",
     "sla_set_debug_canaries", "sla_selftest_canary_trip", "sla_attention_tile_stats",
+    "sla_paged_workspace_bytes", "sla_cache_extend", "sla_cache_append", "sla_cache_release", "sla_cache_fork",
+    "sla_cache_compact", "sla_cache_copy", "sla_paged_attention", "sla_paged_decode_step",
 ]
 
 
@@ -43,6 +49,19 @@ class sla_layout_t(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32),
                 ("q_stride_b", C.c_int64), ("q_stride_h", C.c_int64), ("q_stride_t", C.c_int64),
                 ("kv_stride_b", C.c_int64), ("kv_stride_h", C.c_int64), ("kv_stride_t", C.c_int64)]
+
+
+class sla_cache_t(C.Structure):
+    """Pools, page table and counts of a paged cache; keeps the tensors it points to (see :func:`make_cache`)."""
+    _fields_ = [("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("reserved", C.c_int32), ("n_slots", C.c_int32), ("table_width", C.c_int32),
+                ("stride_page", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("n_tokens", C.c_void_p), ("ref", C.c_void_p)]
+
+
+class sla_batch_t(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_new", C.c_int32), ("max_new", C.c_int32), ("reserved", C.c_int32),
+                ("seq", C.c_void_p), ("cu_new", C.c_void_p)]
 
 
 class sla_params_t(C.Structure):
@@ -115,6 +134,25 @@ def load_library():
     lib.sla_probe_l2_read.argtypes = [vp, vp, sz, C.c_int32, vp, vp]
     lib.sla_selftest_wait_expiry.restype = i32
     lib.sla_selftest_wait_expiry.argtypes = [vp, C.c_int32, vp, vp]
+    CP, BP, f32 = C.POINTER(sla_cache_t), C.POINTER(sla_batch_t), C.c_float
+    lib.sla_paged_workspace_bytes.restype = sz
+    lib.sla_paged_workspace_bytes.argtypes = [CP, i32, i32, i32, PP]
+    lib.sla_cache_extend.restype = i32
+    lib.sla_cache_extend.argtypes = [vp, CP, BP, vp, vp]
+    lib.sla_cache_append.restype = i32
+    lib.sla_cache_append.argtypes = [vp, CP, BP, vp, vp, vp, i64, i64, vp]
+    lib.sla_cache_release.restype = i32
+    lib.sla_cache_release.argtypes = [vp, CP, vp, i32, vp]
+    lib.sla_cache_fork.restype = i32
+    lib.sla_cache_fork.argtypes = [vp, CP, vp, vp, i32, vp, vp]
+    lib.sla_cache_compact.restype = i32
+    lib.sla_cache_compact.argtypes = [vp, CP, vp, vp]
+    lib.sla_cache_copy.restype = i32
+    lib.sla_cache_copy.argtypes = [vp, CP, vp, i32, vp]
+    lib.sla_paged_attention.restype = i32
+    lib.sla_paged_attention.argtypes = [vp, vp, CP, BP, i32, i64, i64, i32, f32, vp, vp, vp]
+    lib.sla_paged_decode_step.restype = i32
+    lib.sla_paged_decode_step.argtypes = [vp, vp, vp, CP, BP, i64, i32, i64, i64, PP, vp, vp, vp, vp, vp]
     lib.sla_pattern_offsets.restype = C.c_int32
     lib.sla_pattern_offsets.argtypes = [C.c_double, i64, vp, C.c_int32]
     lib.sla_pattern_len_steps.restype = C.c_int32
@@ -442,3 +480,171 @@ def sla_decode_shard_merge(handle: Handle, all_partial: torch.Tensor, q_like: to
                                             out.data_ptr(), lse.data_ptr(), _stream_ptr(stream))
     handle.check(rc, "sla_decode_shard_merge")
     return out, lse
+
+
+# ---- paged cache ---------------------------------------------------------------------------------------
+
+
+def _int32(t: torch.Tensor, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor")
+    return t
+
+
+def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: torch.Tensor, ref: torch.Tensor) -> sla_cache_t:
+    """A paged cache from its tensors: k, v [n_pages, Hkv, page_tokens, D] (any strides with D contiguous; the two share them),
+    table int32 [n_slots, table_width], n_tokens int32 [n_slots], ref int32 [n_pages], all on one device."""
+    if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+        raise ValueError("k and v must be [n_pages, Hkv, page_tokens, D] and share their shape, strides and dtype")
+    if k.stride(-1) != 1:
+        raise ValueError("head_dim axis must be contiguous")
+    _int32(table, "table"), _int32(n_tokens, "n_tokens"), _int32(ref, "ref")
+    if table.dim() != 2 or n_tokens.shape != table.shape[:1] or ref.shape != k.shape[:1]:
+        raise ValueError("table must be [n_slots, table_width], n_tokens [n_slots] and ref [n_pages]")
+    if len({t.device for t in (k, v, table, n_tokens, ref)}) != 1:
+        raise ValueError("the tensors of a cache must be on one device")
+    n_pages, hkv, page, d = k.shape
+    c = sla_cache_t(n_pages, page, hkv, d, _dtype_code(k), 0, table.shape[0], table.shape[1], k.stride(0), k.stride(1),
+                    k.stride(2), k.data_ptr(), v.data_ptr(), table.data_ptr(), n_tokens.data_ptr(), ref.data_ptr())
+    c.tensors = (k, v, table, n_tokens, ref)
+    return c
+
+
+def _batch(cu_new: Optional[torch.Tensor], n_new: int, max_new: Optional[int], seq: Optional[torch.Tensor]) -> sla_batch_t:
+    if cu_new is None:
+        n, max_new = n_new, 1
+    else:
+        n = _int32(cu_new, "cu_new").numel() - 1
+        max_new = n_new if max_new is None else int(max_new)
+    if seq is not None and _int32(seq, "seq").numel() != n:
+        raise ValueError("seq must name one slot per sequence")
+    return sla_batch_t(n, n_new, max_new, 0, None if seq is None else seq.data_ptr(), None if cu_new is None else cu_new.data_ptr())
+
+
+def _slots(cache: sla_cache_t, cu_new: Optional[torch.Tensor], seq: Optional[torch.Tensor]) -> int:
+    return cu_new.numel() - 1 if cu_new is not None else seq.numel() if seq is not None else cache.n_slots
+
+
+def _device_of(cache: sla_cache_t) -> torch.device:
+    return cache.tensors[2].device
+
+
+def sla_paged_workspace_bytes(cache: sla_cache_t, n_q_heads: int, n_seqs: int, n_new: int,
+                              params: Optional[sla_params_t] = None) -> int:
+    """Workspace that the paged calls need for batches of up to n_seqs sequences and n_new tokens; params: of
+    sla_paged_decode_step, None when it is not called."""
+    return int(load_library().sla_paged_workspace_bytes(C.byref(cache), int(n_q_heads), int(n_seqs), int(n_new),
+                                                        None if params is None else C.byref(params)))
+
+
+def sla_cache_extend(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.Tensor] = None, *,
+                     seq: Optional[torch.Tensor] = None, n_new: Optional[int] = None, first=None, stream=None):
+    """Room for cu_new[x+1] - cu_new[x] tokens (None: one) of every sequence -> first int32 [n_seqs], the position of its
+    first new token, -1 where it was refused.  n_new: rows of the call, when cu_new's last entry does not bound them yet."""
+    n = _slots(cache, cu_new, seq)
+    if first is None:
+        first = torch.empty(n, dtype=torch.int32, device=_device_of(cache))
+    rows = n if cu_new is None or n == 0 else 0x7FFFFFFF if n_new is None else int(n_new)
+    b = sla_batch_t(n, rows, 1 if cu_new is None else rows, 0, None if seq is None else _int32(seq, "seq").data_ptr(),
+                    None if cu_new is None else _int32(cu_new, "cu_new").data_ptr())
+    handle.check(handle._lib.sla_cache_extend(handle.ptr, C.byref(cache), C.byref(b), first.data_ptr(), _stream_ptr(stream)),
+                 "sla_cache_extend")
+    return first
+
+
+def sla_cache_append(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.Tensor], first: torch.Tensor,
+                     k_new: torch.Tensor, v_new: torch.Tensor, *, seq: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k_new, v_new [n_new, Hkv, D] to the positions first[x] + r of their sequences."""
+    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.dtype != v_new.dtype or k_new.stride(-1) != 1:
+        raise ValueError("k_new and v_new must share shape, strides and dtype, head_dim contiguous")
+    if k_new.shape[1:] != (cache.n_kv_heads, cache.head_dim) or _dtype_code(k_new) != cache.dtype:
+        raise ValueError("k_new must be [n_new, Hkv, D] in the cache's dtype")
+    b = _batch(cu_new, k_new.shape[0], None, seq)
+    if _int32(first, "first").numel() != b.n_seqs:
+        raise ValueError("first must have one entry per sequence")
+    handle.check(handle._lib.sla_cache_append(handle.ptr, C.byref(cache), C.byref(b), first.data_ptr(), k_new.data_ptr(),
+                                              v_new.data_ptr(), k_new.stride(0), k_new.stride(1), _stream_ptr(stream)),
+                 "sla_cache_append")
+
+
+def sla_cache_release(handle: Handle, cache: sla_cache_t, seq: torch.Tensor, *, stream=None) -> None:
+    """Ends the sequences in the slots `seq` (int32, device)."""
+    handle.check(handle._lib.sla_cache_release(handle.ptr, C.byref(cache), _int32(seq, "seq").data_ptr(), seq.numel(),
+                                               _stream_ptr(stream)), "sla_cache_release")
+
+
+def sla_cache_fork(handle: Handle, cache: sla_cache_t, src: torch.Tensor, dst: torch.Tensor, *, pairs=None, stream=None):
+    """The empty slots dst become copies of the sequences src -> pairs int32 [2, n] of the pages that were copied."""
+    n = _int32(src, "src").numel()
+    if _int32(dst, "dst").numel() != n:
+        raise ValueError("src and dst must have the same length")
+    if pairs is None:
+        pairs = torch.empty(2, n, dtype=torch.int32, device=_device_of(cache))
+    handle.check(handle._lib.sla_cache_fork(handle.ptr, C.byref(cache), src.data_ptr(), dst.data_ptr(), n, pairs.data_ptr(),
+                                            _stream_ptr(stream)), "sla_cache_fork")
+    return pairs
+
+
+def sla_cache_compact(handle: Handle, cache: sla_cache_t, *, pairs=None, stream=None):
+    """Moves the pages in use to the front of the pool -> pairs int32 [2, n_pages] of the moves, then -1."""
+    if pairs is None:
+        pairs = torch.empty(2, cache.n_pages, dtype=torch.int32, device=_device_of(cache))
+    handle.check(handle._lib.sla_cache_compact(handle.ptr, C.byref(cache), pairs.data_ptr(), _stream_ptr(stream)),
+                 "sla_cache_compact")
+    return pairs
+
+
+def sla_cache_copy(handle: Handle, cache: sla_cache_t, pairs: torch.Tensor, *, stream=None) -> None:
+    """Copies pages pairs[0] to pages pairs[1] (int32 [2, n]; pairs with a negative entry are skipped)."""
+    if _int32(pairs, "pairs").dim() != 2 or pairs.shape[0] != 2:
+        raise ValueError("pairs must be [2, n]")
+    handle.check(handle._lib.sla_cache_copy(handle.ptr, C.byref(cache), pairs.data_ptr(), pairs.shape[1], _stream_ptr(stream)),
+                 "sla_cache_copy")
+
+
+def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_new: Optional[torch.Tensor] = None, *,
+                        seq: Optional[torch.Tensor] = None, max_new: Optional[int] = None, window: int = 0,
+                        softmax_scale: Optional[float] = None, out=None, lse=None, stream=None):
+    """q [n_new, Hq, D], the new tokens of the sequences (cu_new None: one each) -> out (q's dtype and strides), lse fp32
+    [n_new, Hq].  max_new: the longest chunk (default n_new); it decides the tiles."""
+    T, Hq, D = q.shape
+    if q.stride(-1) != 1 or D != cache.head_dim or _dtype_code(q) != cache.dtype:
+        raise ValueError("q must be [n_new, Hq, D] in the cache's dtype and head_dim, head_dim contiguous")
+    if out is None:
+        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device)
+    elif out.stride() != q.stride() or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must have q's shape, strides and dtype")
+    if lse is None:
+        lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
+    b = _batch(cu_new, T, max_new, seq)
+    rc = handle._lib.sla_paged_attention(handle.ptr, q.data_ptr(), C.byref(cache), C.byref(b), Hq, q.stride(0), q.stride(1),
+                                         int(window), 1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale,
+                                         out.data_ptr(), lse.data_ptr(), _stream_ptr(stream))
+    if rc != SLA_OK:
+        handle.check(rc, "sla_paged_attention")
+    return out, lse
+
+
+def sla_paged_decode_step(handle: Handle, q_s: torch.Tensor, q: torch.Tensor, cache: sla_cache_t, params: sla_params_t, *,
+                          seq: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None, out=None, lse=None,
+                          out_anchor=None, out_score=None, stream=None):
+    """sla_decode_step over the paged cache: q_s, q [n_seqs, Hq, D], the last token of every sequence -> out, lse, anchors
+    (positions), scores.  max_tokens: a bound of the lengths (default: what the table can hold); it sizes the grids."""
+    B, Hq, D = q.shape
+    if q_s.stride() != q.stride() or q.stride(-1) != 1 or q_s.shape != q.shape:
+        raise ValueError("q_s and q must share shape and strides, head_dim contiguous")
+    if D != cache.head_dim or _dtype_code(q) != cache.dtype or _dtype_code(q_s) != cache.dtype:
+        raise ValueError("q_s and q must have the cache's dtype and head_dim")
+    dev = q.device
+    out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev) if out is None else out
+    lse = torch.empty(B, Hq, dtype=torch.float32, device=dev) if lse is None else lse
+    out_anchor = torch.empty(B, Hq, params.top_k, dtype=torch.int32, device=dev) if out_anchor is None else out_anchor
+    out_score = torch.empty(B, Hq, params.top_k, dtype=torch.float32, device=dev) if out_score is None else out_score
+    b = _batch(None, B, 1, seq)
+    most = cache.table_width * cache.page_tokens if max_tokens is None else int(max_tokens)
+    rc = handle._lib.sla_paged_decode_step(handle.ptr, q_s.data_ptr(), q.data_ptr(), C.byref(cache), C.byref(b), most, Hq,
+                                           q.stride(0), q.stride(1), C.byref(params), out.data_ptr(), lse.data_ptr(),
+                                           out_anchor.data_ptr(), out_score.data_ptr(), _stream_ptr(stream))
+    if rc != SLA_OK:
+        handle.check(rc, "sla_paged_decode_step")
+    return out, lse, out_anchor, out_score

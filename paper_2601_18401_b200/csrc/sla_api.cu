@@ -5,10 +5,12 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <new>
 #include <vector>
 
 #include "sla_kernels.h"
+#include "sla_paged_attn.h"
 
 struct sla_handle_s {
     int device = 0;
@@ -239,6 +241,7 @@ const char *sla_status_string(sla_status_t s) {
         case SLA_ERR_DEVICE_TIMEOUT: return "SLA_ERR_DEVICE_TIMEOUT";
         case SLA_ERR_DEVICE_INDEX: return "SLA_ERR_DEVICE_INDEX";
         case SLA_ERR_DEVICE_OVERRUN: return "SLA_ERR_DEVICE_OVERRUN";
+        case SLA_ERR_CACHE_FULL: return "SLA_ERR_CACHE_FULL";
     }
     return "SLA_ERR_UNKNOWN";
 }
@@ -433,7 +436,8 @@ sla_status_t sla_poll_status(sla_handle_t h, void *stream) {
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_poll_status");
     if (word & sla::kStatusOverrun) return fail(h, SLA_ERR_DEVICE_OVERRUN, "a kernel wrote outside its scratch region%s");
     if (word & sla::kStatusTimeout) return fail(h, SLA_ERR_DEVICE_TIMEOUT, "a bounded device-side wait expired%s");
-    if (word & sla::kStatusBadIndex) return fail(h, SLA_ERR_DEVICE_INDEX, "an anchor outside [0, i] was skipped%s");
+    if (word & sla::kStatusBadIndex) return fail(h, SLA_ERR_DEVICE_INDEX, "an anchor outside [0, i], or a slot, length or page outside a paged cache, was skipped%s");
+    if (word & sla::kStatusCacheFull) return fail(h, SLA_ERR_CACHE_FULL, "a sequence was refused pages%s");
     return SLA_OK;
 }
 
@@ -787,6 +791,234 @@ sla_status_t sla_prefill_host(sla_handle_t h, const void *q_s_host, const void *
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (s != SLA_OK) return s;
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_prefill_host (copy out)");
+    return SLA_OK;
+}
+
+
+// ---- paged cache ------------------------------------------------------------------------------------
+namespace {
+
+const char *check_cache(const sla_cache_t *c) {
+    if (!c) return "cache is NULL";
+    if (c->n_pages <= 0 || c->n_kv_heads <= 0 || c->n_slots <= 0 || c->table_width <= 0) return "n_pages, n_kv_heads, n_slots and table_width must be positive";
+    if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens must be a power of two in 16..256";
+    if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+    if (c->n_kv_heads > 65536) return "n_kv_heads above 65536";
+    if (c->dtype != SLA_F32 && c->dtype != SLA_BF16) return "dtype must be SLA_F32 or SLA_BF16";
+    if (c->reserved != 0) return "reserved must be 0";
+    for (int64_t s : {c->stride_page, c->stride_h, c->stride_t})
+        if (s < 0 || s % 8 || s > ((int64_t)1 << 40)) return "cache strides must be non-negative multiples of 8 elements";
+    if (c->stride_t < c->head_dim || (c->n_kv_heads > 1 && c->stride_h < c->head_dim) || (c->n_pages > 1 && c->stride_page < c->head_dim))
+        return "a cache stride is below head_dim";
+    if (!c->k || !c->v || !c->table || !c->n_tokens || !c->ref) return "NULL pointer in the cache";
+    if (!aligned16(c->k) || !aligned16(c->v)) return "k and v must be 16-byte aligned";
+    return nullptr;
+}
+
+const char *check_batch(const sla_batch_t *b) {
+    if (!b) return "batch is NULL";
+    if (b->n_seqs < 0 || b->n_new < 0 || b->max_new < 0) return "n_seqs, n_new and max_new must be >= 0";
+    if (b->reserved != 0) return "reserved must be 0";
+    if (!b->cu_new && (b->n_new != b->n_seqs || (b->n_seqs > 0 && b->max_new != 1))) return "without cu_new every sequence has one new token";
+    if (b->n_new > 0 && b->max_new < 1) return "max_new must be positive";
+    if ((int64_t)b->n_seqs * b->max_new < b->n_new) return "n_new exceeds n_seqs * max_new";
+    return nullptr;
+}
+
+sla::Pages make_pages(sla_handle_t h, const sla_cache_t *c) {
+    sla::Pages p;
+    p.k = static_cast<char *>(c->k); p.v = static_cast<char *>(c->v);
+    p.table = c->table; p.n_tokens = c->n_tokens; p.ref = c->ref;
+    p.n_pages = c->n_pages; p.P = c->page_tokens;
+    p.shift = 0;
+    while ((1 << p.shift) < p.P) ++p.shift;
+    p.Hkv = c->n_kv_heads; p.D = c->head_dim; p.es = (int)elem_size(c->dtype);
+    p.n_slots = c->n_slots; p.width = c->table_width;
+    p.s_page = c->stride_page; p.s_h = c->stride_h; p.s_t = c->stride_t;
+    p.status = h ? reinterpret_cast<int *>(h->ws) : nullptr;
+    return p;
+}
+
+sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, b->seq, b->cu_new}; }
+
+// The handle, the cache and the scratch a bookkeeping call needs.  SLA_OK when the call may go on.
+sla_status_t cache_call(sla_handle_t h, const sla_cache_t *c, size_t n_seqs) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (const char *why = check_cache(c)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (const char *why = check_device(h)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (sla::cache_scratch_bytes(make_pages(h, c), (int)n_seqs) > h->scratch_avail)
+        return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this cache: ask sla_paged_workspace_bytes%s");
+    return SLA_OK;
+}
+
+sla_layout_t layout_of(const sla_cache_t *c, int32_t n_q_heads, int32_t n_seqs, int64_t q_sb, int64_t q_sh) {
+    sla_layout_t l = {n_seqs, n_q_heads, c->n_kv_heads, c->head_dim, c->dtype, 0, q_sb, q_sh, 0, 0, c->stride_h, c->stride_t};
+    return l;
+}
+
+}  // namespace
+
+size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_t n_seqs, int32_t n_new, const sla_params_t *p) {
+    if (check_cache(c) || n_q_heads <= 0 || n_q_heads % c->n_kv_heads || n_q_heads / c->n_kv_heads > sla::kMaxGroup || n_seqs < 0 || n_new < 0)
+        return 0;
+    size_t need = sla::cache_scratch_bytes(make_pages(nullptr, c), n_seqs > c->n_slots ? n_seqs : c->n_slots);
+    sla::PagedCall a = {};
+    a.c = make_pages(nullptr, c);
+    a.Hq = n_q_heads;
+    a.G = n_q_heads / c->n_kv_heads;
+    for (int32_t most : {1, n_new}) {   // the tiles go by the longest chunk
+        a.b = {n_seqs, n_new, most, nullptr, nullptr};
+        const size_t bytes = sla::plan_paged(a, c->dtype, 160).bytes;
+        if (bytes > need) need = bytes;
+    }
+    if (p && n_seqs > 0) {
+        const sla_layout_t l = layout_of(c, n_q_heads, n_seqs, c->head_dim * (int64_t)n_q_heads, c->head_dim);
+        const int64_t most = std::min<int64_t>((int64_t)c->table_width * c->page_tokens, 2147483647);
+        const size_t bytes = sla_workspace_bytes(&l, p, 1, most);
+        if (bytes == 0) return 0;
+        if (bytes > need) need = bytes;
+    }
+    return need + 4096 + (sla::Canaries::kMax + 1) * sla::Canaries::kBytes;
+}
+
+sla_status_t sla_cache_extend(sla_handle_t h, const sla_cache_t *c, const sla_batch_t *b, int32_t *first, void *stream) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (const char *why = check_batch(b)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (sla_status_t s = cache_call(h, c, b->n_seqs)) return s;
+    if (b->n_seqs == 0) return SLA_OK;
+    if (!first) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
+    cudaError_t e = sla::launch_cache_extend(make_pages(h, c), make_batch(b), first, reinterpret_cast<int *>(h->ws + kHeaderBytes), static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_extend");
+    h->launches += 1;
+    return SLA_OK;
+}
+
+sla_status_t sla_cache_append(sla_handle_t h, const sla_cache_t *c, const sla_batch_t *b, const int32_t *first, const void *k_new,
+                              const void *v_new, int64_t new_stride_t, int64_t new_stride_h, void *stream) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (const char *why = check_batch(b)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (sla_status_t s = cache_call(h, c, 0)) return s;
+    if (b->n_new == 0) return SLA_OK;
+    if (!first || !k_new || !v_new) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
+    if (!aligned16(k_new) || !aligned16(v_new)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");
+    if (new_stride_t < 0 || new_stride_t % 8 || new_stride_h < 0 || new_stride_h % 8)
+        return fail(h, SLA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements%s");
+    cudaError_t e = sla::launch_cache_append(make_pages(h, c), make_batch(b), first, k_new, v_new, new_stride_t, new_stride_h, h->sm_count,
+                                             static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_append");
+    h->launches += 1;
+    return SLA_OK;
+}
+
+sla_status_t sla_cache_release(sla_handle_t h, const sla_cache_t *c, const int32_t *seq, int32_t n, void *stream) {
+    if (sla_status_t s = cache_call(h, c, 0)) return s;
+    if (n < 0 || (n > 0 && !seq)) return fail(h, SLA_ERR_INVALID_ARG, "n must be >= 0 and seq not NULL%s");
+    if (n == 0) return SLA_OK;
+    cudaError_t e = sla::launch_cache_release(make_pages(h, c), seq, n, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_release");
+    h->launches += 1;
+    return SLA_OK;
+}
+
+sla_status_t sla_cache_fork(sla_handle_t h, const sla_cache_t *c, const int32_t *src, const int32_t *dst, int32_t n, int32_t *pairs,
+                            void *stream) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (n < 0 || (n > 0 && (!src || !dst || !pairs))) return fail(h, SLA_ERR_INVALID_ARG, "n must be >= 0 and src, dst and pairs not NULL%s");
+    if (sla_status_t s = cache_call(h, c, n)) return s;
+    if (n == 0) return SLA_OK;
+    cudaError_t e = sla::launch_cache_fork(make_pages(h, c), src, dst, n, pairs, reinterpret_cast<int *>(h->ws + kHeaderBytes), static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_fork");
+    h->launches += 2;
+    return SLA_OK;
+}
+
+sla_status_t sla_cache_compact(sla_handle_t h, const sla_cache_t *c, int32_t *pairs, void *stream) {
+    if (sla_status_t s = cache_call(h, c, 0)) return s;
+    if (!pairs) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
+    cudaError_t e = sla::launch_cache_compact(make_pages(h, c), pairs, reinterpret_cast<int *>(h->ws + kHeaderBytes), h->sm_count, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_compact");
+    h->launches += 3;
+    return SLA_OK;
+}
+
+sla_status_t sla_cache_copy(sla_handle_t h, const sla_cache_t *c, const int32_t *pairs, int32_t n, void *stream) {
+    if (sla_status_t s = cache_call(h, c, 0)) return s;
+    if (n < 0 || (n > 0 && !pairs)) return fail(h, SLA_ERR_INVALID_ARG, "n must be >= 0 and pairs not NULL%s");
+    if (n == 0) return SLA_OK;
+    cudaError_t e = sla::launch_cache_copy(make_pages(h, c), pairs, n, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_copy");
+    h->launches += 1;
+    return SLA_OK;
+}
+
+sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_t *c, const sla_batch_t *b, int32_t n_q_heads,
+                                 int64_t q_stride_t, int64_t q_stride_h, int32_t window, float softmax_scale, void *out, float *lse,
+                                 void *stream) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (const char *why = check_cache(c)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (const char *why = check_batch(b)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (const char *why = check_device(h)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (n_q_heads <= 0 || n_q_heads % c->n_kv_heads) return fail(h, SLA_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of n_kv_heads%s");
+    if (n_q_heads / c->n_kv_heads > sla::kMaxGroup) return fail(h, SLA_ERR_INVALID_ARG, "group size above 16%s");
+    if (window < 0) return fail(h, SLA_ERR_INVALID_ARG, "window must be >= 0%s");
+    if (!(softmax_scale == softmax_scale)) return fail(h, SLA_ERR_INVALID_ARG, "scale is NaN%s");
+    if (b->n_new == 0) return SLA_OK;
+    if (!q || !out || !lse) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
+    if (!aligned16(q) || !aligned16(out)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");
+    if (q_stride_t < 0 || q_stride_t % 8 || q_stride_h < 0 || q_stride_h % 8)
+        return fail(h, SLA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements%s");
+    if ((b->n_new > 1 && q_stride_t < c->head_dim) || (n_q_heads > 1 && q_stride_h < c->head_dim))
+        return fail(h, SLA_ERR_INVALID_ARG, "token or head stride below head_dim%s");
+    sla::PagedCall a;
+    a.c = make_pages(h, c);
+    a.b = make_batch(b);
+    a.Hq = n_q_heads;
+    a.G = n_q_heads / c->n_kv_heads;
+    a.window = window;
+    a.q_st = q_stride_t;
+    a.q_sh = q_stride_h;
+    a.scale = softmax_scale;
+    const sla::PagedPlan plan = sla::plan_paged(a, c->dtype, h->sm_count);
+    if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
+    cudaError_t e = sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, out, lse, static_cast<cudaStream_t>(stream), &h->launches);
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_paged_attention");
+    return SLA_OK;
+}
+
+sla_status_t sla_paged_decode_step(sla_handle_t h, const void *q_s, const void *q, const sla_cache_t *c, const sla_batch_t *b,
+                                   int64_t max_tokens, int32_t n_q_heads, int64_t q_stride_b, int64_t q_stride_h, const sla_params_t *p,
+                                   void *out, float *lse, int32_t *out_anchor, float *out_score, void *stream) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (const char *why = check_cache(c)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (!b || b->n_seqs < 0 || b->reserved != 0) return fail(h, SLA_ERR_INVALID_ARG, "batch is NULL, or n_seqs < 0, or reserved not 0%s");
+    if (b->n_seqs == 0) return SLA_OK;
+    if (n_q_heads <= 0 || n_q_heads % c->n_kv_heads) return fail(h, SLA_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of n_kv_heads%s");
+    const sla_layout_t l = layout_of(c, n_q_heads, b->n_seqs, q_stride_b, q_stride_h);
+    if (const char *why = check_layout_params(&l, p, true)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (max_tokens <= 0 || max_tokens > 2147483647LL) return fail(h, SLA_ERR_INVALID_ARG, "max_tokens must be in 1..2^31-1%s");
+    if (const char *why = check_device(h)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (!q_s || !q || !out || !lse || !out_anchor || !out_score) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
+    if (!aligned16(q_s) || !aligned16(q) || !aligned16(out)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (sla_status_t ps = prepare_pattern(h, p, max_tokens, st)) return ps;
+    const sla::Call call = make_call(h, &l, p, 1, max_tokens - 1, max_tokens);
+    const sla::DecodePlan plan = sla::plan_decode(call, max_tokens, h->sm_count * sla::decode_attn_blocks_per_sm(c->dtype, c->head_dim),
+                                                  h->canaries ? sla::Canaries::kBytes : 0);
+    if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
+    if ((size_t)plan.n_anchor * sizeof(float) * 8 > 180 * 1024) return fail(h, SLA_ERR_UNSUPPORTED, "context too long for the decode top-k stage%s");
+    const size_t units = p->mode == SLA_PER_SPAN ? (size_t)p->top_k : 1;
+    if ((size_t)b->n_seqs * (c->n_kv_heads + n_q_heads * (units + 1)) * sizeof(int) > kCounterEnd - kCounterOffset ||
+        (size_t)b->n_seqs * n_q_heads * units > 65535)
+        return fail(h, SLA_ERR_UNSUPPORTED, "too many (sequence, head) pairs for the decode step%s");
+    sla::Batch batch = {b->n_seqs, b->n_seqs, 1, b->seq, nullptr};
+    cudaError_t e = sla::launch_canary_fill(h->ws + kHeaderBytes, plan.canaries, st);
+    if (e == cudaSuccess)
+        e = sla::launch_paged_decode(q_s, q, make_pages(h, c), batch, call, c->dtype, plan, h->ws + kHeaderBytes,
+                                     reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, out_anchor, out_score, st);
+    if (e == cudaSuccess) e = sla::launch_canary_check(h->ws + kHeaderBytes, plan.canaries, call.status, st);
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_paged_decode_step");
+    h->launches += plan.score_first ? 2 : 1;
+    if (plan.canaries.n) { h->last_canaries = plan.canaries; h->last_canary_base = h->ws + kHeaderBytes; }
     return SLA_OK;
 }
 

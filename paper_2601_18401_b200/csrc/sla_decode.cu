@@ -24,6 +24,7 @@
 #include <math_constants.h>
 
 #include "sla_kernels.h"
+#include "sla_paged.cuh"
 #include "sla_topk.cuh"
 
 namespace sla {
@@ -42,11 +43,42 @@ template <int LPR> __device__ inline float reduce_sub(float x) {
 }
 
 // ------------------------------------------------------------------------------------------------
-template <typename T, int D, int GT>
+// Where a sequence's tokens lie.  FlatCache: one after another, all sequences n_ctx long.  PagedCache: found through a page table,
+// every sequence at its own length, read on the device (c.Lkv bounds it, c.kv_sb = 0).
+struct FlatCache {
+    static constexpr bool kPaged = false;
+};
+struct PagedCache {
+    static constexpr bool kPaged = true;
+    Pages pages;
+    Batch batch;
+    // query position of sequence x, -1 when it has no tokens (or a slot or length out of bounds, which is flagged)
+    __device__ __forceinline__ long long position(int x, long long most, const int *&row) const {
+        const int s = slot_of(pages, batch, x);
+        row = pages.table + (long long)max(s, 0) * pages.width;
+        if (s >= 0) {
+            const int n = tokens_of(pages, s);
+            if (n <= most) return n - 1;
+        }
+        atomicOr(pages.status, kStatusBadIndex);
+        return -1;
+    }
+};
+// Offset of the row of position `pos` from the first row of its KV head, in elements.
+template <class Cache> __device__ __forceinline__ long long row_at(const Cache &cache, const Call &c, const int *row, long long pos) {
+    if constexpr (Cache::kPaged) {
+        const int page = valid_page(cache.pages, __ldg(row + (pos >> cache.pages.shift)));
+        return page * cache.pages.s_page + (pos & (cache.pages.P - 1)) * c.kv_st;
+    } else {
+        return pos * c.kv_st;
+    }
+}
+
+template <typename T, int D, int GT, class Cache = FlatCache>
 __global__ void __launch_bounds__(kScoreThreads)
 decode_score(const T *__restrict__ q_s, const T *__restrict__ k, Call c, long long n_ctx, int n, int s_min,
              float *__restrict__ scores, int *__restrict__ done,
-             int32_t *__restrict__ out_anchor, float *__restrict__ out_score) {
+             int32_t *__restrict__ out_anchor, float *__restrict__ out_score, Cache cache) {
     extern __shared__ float dsm[];
     __shared__ int s_last;
     constexpr int E = Vec16<T>::kElems;
@@ -58,13 +90,19 @@ decode_score(const T *__restrict__ q_s, const T *__restrict__ k, Call c, long lo
     const int sub = lane % LPR, rsel = lane / LPR;
     const int g = blockIdx.y % c.Hkv, b = blockIdx.y / c.Hkv;
     const int h0 = g * c.G + blockIdx.z * GT;
-    const long long i = n_ctx - 1;
+    long long i = n_ctx - 1;
     const T *kbase = k + b * c.kv_sb + g * c.kv_sh;
 
     // the attention kernel of this step may be scheduled now; it waits for this grid to finish before it reads scores.
     // This grid itself may have been launched beside the tail of the kernel before it.
     chain_release();
     chain_wait();
+    int n_own = n;   // candidates of this sequence
+    const int *row = nullptr;
+    if constexpr (Cache::kPaged) {
+        i = cache.position(b, n_ctx, row);
+        n_own = min(max(n_strides(c, i) - s_min, 0), n);
+    }
     float qv[GT][E];
 #pragma unroll
     for (int t = 0; t < GT; ++t) Vec16<T>::load(q_s + b * c.q_sb + (long long)(h0 + t) * c.q_sh + sub * E, qv[t]);
@@ -76,11 +114,11 @@ decode_score(const T *__restrict__ q_s, const T *__restrict__ k, Call c, long lo
         const int s = s_base + (u * kWarps + warp) * RPI + rsel;
 #pragma unroll
         for (int t = 0; t < GT; ++t) part[u][t] = 0.f;
-        if (s < n) {
+        if (s < n_own) {
             // candidate x is stride s_min + x: the first s_min strides land inside the local window
             const long long tpos = i + 1 - stride_offset(c, s_min + s);
             float kv[E];
-            Vec16<T>::load(kbase + tpos * c.kv_st + sub * E, kv);
+            Vec16<T>::load(kbase + row_at(cache, c, row, tpos) + sub * E, kv);
 #pragma unroll
             for (int t = 0; t < GT; ++t)
 #pragma unroll
@@ -93,7 +131,7 @@ decode_score(const T *__restrict__ q_s, const T *__restrict__ k, Call c, long lo
 #pragma unroll
         for (int t = 0; t < GT; ++t) {
             const float tot = reduce_sub<LPR>(part[u][t]);
-            if (sub == 0 && s < n)
+            if (sub == 0 && s < n_own)
                 scores[((long long)b * c.Hq + h0 + t) * n + s] = tot * c.search_scale;
         }
     }
@@ -372,13 +410,13 @@ template <typename T> __device__ __forceinline__ void unpack16(const uint4 &v, f
 //   3. the cluster's first CTA merges the partial results of the others through distributed shared memory; when a
 //      unit has several clusters, the one that finishes last merges theirs (through `partial` and the counter `done`).
 // One launch or two: see the figures at plan_decode.
-template <typename T, int D>
+template <typename T, int D, class Cache = FlatCache>
 __global__ void __launch_bounds__(kAttnThreads, 2)
 decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, Call c,
             const int *__restrict__ spans, const float *__restrict__ scores, int n_cand, int s_min, int ell, float *__restrict__ partial, int *__restrict__ done,
             float *__restrict__ unit_out, int *__restrict__ done_head, int32_t *__restrict__ sel_anchor,
             float *__restrict__ sel_score, T *__restrict__ out, float *__restrict__ lse,
-            float *__restrict__ shard_out) {
+            float *__restrict__ shard_out, Cache cache) {
     extern __shared__ float s_scores[];   // [n_cand] (unsharded step)
     __shared__ int s_last;
     constexpr int E = Vec16<T>::kElems;
@@ -419,11 +457,18 @@ decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restr
     // whose results are read from here on
     chain_wait();
     int cnt;
+    const int *row = nullptr;
+    long long i = c.Lkv - 1;
+    const int n_scores = n_cand;   // scores of a head in `scores`
+    if constexpr (Cache::kPaged) {
+        i = cache.position(b, c.Lkv, row);
+        n_cand = min(max(n_strides(c, i) - s_min, 0), n_cand);
+        ell = (int)base_len(c, i);
+    }
     if (!spans) {
-        const long long i = c.Lkv - 1;
         const int per = (n_cand + csize - 1) / csize, x_lo = min(rank * per, n_cand), n_loc = min(per, n_cand - x_lo);
         if (scores) {
-            for (int x = tid; x < n_cand; x += kAttnThreads) s_scores[x] = __ldcg(scores + bh * n_cand + x);
+            for (int x = tid; x < n_cand; x += kAttnThreads) s_scores[x] = __ldcg(scores + bh * n_scores + x);
         } else {
             // scores of this CTA's share of the anchors
             constexpr int LS = D / E, RS = 32 / LS, US = 4;
@@ -438,7 +483,7 @@ decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restr
                     const int x = x0 + (u * kWarps + warp) * RS + srow;
                     // candidate y is stride s_min + y: the first s_min strides land inside the local window
                     const long long t = x < n_loc ? i + 1 - stride_offset(c, s_min + x_lo + x) : i;
-                    raw[u] = __ldg(reinterpret_cast<const uint4 *>(kbase + t * c.kv_st + ssub * E));
+                    raw[u] = __ldg(reinterpret_cast<const uint4 *>(kbase + row_at(cache, c, row, t) + ssub * E));
                 }
                 float qv[E];
                 unpack16<T>(q_raw, qv);
@@ -504,11 +549,11 @@ decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restr
             ok[u] = f < f_end;
             if (ok[u]) {
                 while (f >= s_cum[piece + 1]) ++piece;
-                const long long pos = s_start[piece] + (f - s_cum[piece]);
+                const long long at = row_at(cache, c, row, s_start[piece] + (f - s_cum[piece]));
 #pragma unroll
                 for (int ch = 0; ch < C; ++ch) {
-                    kraw[u][ch] = __ldg(reinterpret_cast<const uint4 *>(kbase + pos * c.kv_st + (ch * LPR + sub) * E));
-                    vraw[u][ch] = __ldg(reinterpret_cast<const uint4 *>(vbase + pos * c.kv_st + (ch * LPR + sub) * E));
+                    kraw[u][ch] = __ldg(reinterpret_cast<const uint4 *>(kbase + at + (ch * LPR + sub) * E));
+                    vraw[u][ch] = __ldg(reinterpret_cast<const uint4 *>(vbase + at + (ch * LPR + sub) * E));
                 }
             } else {
 #pragma unroll
@@ -725,11 +770,11 @@ cudaError_t allow_score_smem(size_t smem) {
     return e;
 }
 
-template <typename T, int D>
+template <typename T, int D, class Cache = FlatCache>
 cudaError_t attn_launch(const T *q_s, const T *q, const T *k, const T *v, const Call &c, const int *spans, const float *scores,
                         int n_cand, int s_min, const DecodePlan &p, int units, float *partial, int *done, float *unit_out,
                         int *done_head, int32_t *out_anchor, float *out_score, T *out, float *lse, float *shard_out,
-                        cudaStream_t st) {
+                        cudaStream_t st, const Cache &cache = Cache()) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.n_splits, c.B * c.Hq * units);
     cfg.blockDim = dim3(kAttnThreads);
@@ -750,15 +795,15 @@ cudaError_t attn_launch(const T *q_s, const T *q, const T *k, const T *v, const 
         ++cfg.numAttrs;
     }
     cfg.attrs = attr;
-    return cudaLaunchKernelEx(&cfg, decode_attn<T, D>, q_s, q, k, v, c, spans, scores, n_cand, s_min,
+    return cudaLaunchKernelEx(&cfg, decode_attn<T, D, Cache>, q_s, q, k, v, c, spans, scores, n_cand, s_min,
                               (int)base_len(c, c.Lkv - 1), partial, done, unit_out,
-                              done_head, out_anchor, out_score, out, lse, shard_out);
+                              done_head, out_anchor, out_score, out, lse, shard_out, cache);
 }
 
-template <typename T, int D>
+template <typename T, int D, class Cache = FlatCache>
 cudaError_t decode_launch(const void *q_s, const void *q, const void *k, const void *v, const Call &c,
                           long long n_ctx, const DecodePlan &p, void *scratch, int *counters, void *out, float *lse,
-                          int32_t *out_anchor, float *out_score, cudaStream_t st) {
+                          int32_t *out_anchor, float *out_score, cudaStream_t st, const Cache &cache = Cache()) {
     constexpr int E = Vec16<T>::kElems;
     constexpr int RPI = 32 / (D / E);
     char *base = (char *)scratch;
@@ -776,8 +821,8 @@ cudaError_t decode_launch(const void *q_s, const void *q, const void *k, const v
         // scores only (no completion counter, no shared memory)
         cudaError_t e;
 #define SLA_LAUNCH_SCORE(GT) \
-    e = launch_chained(decode_score<T, D, GT>, gs, dim3(kScoreThreads), 0, st, qs, kk, c, n_ctx, n, s_min, scores, (int *)nullptr, \
-                       out_anchor, out_score)
+    e = launch_chained(decode_score<T, D, GT, Cache>, gs, dim3(kScoreThreads), 0, st, qs, kk, c, n_ctx, n, s_min, scores, (int *)nullptr, \
+                       out_anchor, out_score, cache)
         switch (gt) {
             case 8: SLA_LAUNCH_SCORE(8); break;
             case 4: SLA_LAUNCH_SCORE(4); break;
@@ -787,9 +832,9 @@ cudaError_t decode_launch(const void *q_s, const void *q, const void *k, const v
 #undef SLA_LAUNCH_SCORE
         if (e != cudaSuccess) return e;
     }
-    return attn_launch<T, D>(qs, (const T *)q, kk, (const T *)v, c, nullptr, scores, n, s_min, p, units,
-                             (float *)(base + p.off_partial), done_unit, (float *)(base + p.off_unit_out), done_head, out_anchor,
-                             out_score, (T *)out, lse, nullptr, st);
+    return attn_launch<T, D, Cache>(qs, (const T *)q, kk, (const T *)v, c, nullptr, scores, n, s_min, p, units,
+                                    (float *)(base + p.off_partial), done_unit, (float *)(base + p.off_unit_out), done_head,
+                                    out_anchor, out_score, (T *)out, lse, nullptr, st, cache);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -924,7 +969,7 @@ cudaError_t shard_search_launch(const void *q_s, const void *k_local, const Call
         e = allow_score_smem<kern>(smem);                                                                            \
         if (e == cudaSuccess)                                                                                        \
             kern<<<gs, kScoreThreads, smem, st>>>(qs, kk, c, n_ctx, n, s_first, scores, counters, cand_anchor,       \
-                                                  cand_score);                                                      \
+                                                  cand_score, FlatCache());                                         \
     } while (0)
     switch (gt) {
         case 8: SLA_LAUNCH_SCORE(8); break;
@@ -1073,6 +1118,21 @@ cudaError_t launch_decode(const void *q_s, const void *q, const void *k, const v
     }
     return c.D == 64 ? decode_launch<__nv_bfloat16, 64>(q_s, q, k, v, c, n_ctx, plan, scratch, counters, out, lse, out_anchor, out_score, st)
                      : decode_launch<__nv_bfloat16, 128>(q_s, q, k, v, c, n_ctx, plan, scratch, counters, out, lse, out_anchor, out_score, st);
+}
+
+// The step for the sequences of a paged cache (c: B = sequences, Lkv = the bound of their lengths, kv strides those of a page).
+cudaError_t launch_paged_decode(const void *q_s, const void *q, const Pages &pages, const Batch &batch, const Call &c, int dtype,
+                                const DecodePlan &plan, void *scratch, int *counters, void *out, float *lse, int32_t *out_anchor,
+                                float *out_score, cudaStream_t st) {
+    const PagedCache cache{pages, batch};
+    const void *k = pages.k, *v = pages.v;
+    const long long n = c.Lkv;
+    if (dtype == SLA_F32) {
+        return c.D == 64 ? decode_launch<float, 64>(q_s, q, k, v, c, n, plan, scratch, counters, out, lse, out_anchor, out_score, st, cache)
+                         : decode_launch<float, 128>(q_s, q, k, v, c, n, plan, scratch, counters, out, lse, out_anchor, out_score, st, cache);
+    }
+    return c.D == 64 ? decode_launch<__nv_bfloat16, 64>(q_s, q, k, v, c, n, plan, scratch, counters, out, lse, out_anchor, out_score, st, cache)
+                     : decode_launch<__nv_bfloat16, 128>(q_s, q, k, v, c, n, plan, scratch, counters, out, lse, out_anchor, out_score, st, cache);
 }
 
 // ------------------------------------------------------------------------------------------------

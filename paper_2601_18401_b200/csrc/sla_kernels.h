@@ -103,6 +103,12 @@ cudaError_t launch_decode(const void *q_s, const void *q, const void *k, const v
                           int dtype, long long n_ctx, const DecodePlan &plan, void *scratch, int *counters,
                           void *out, float *lse, int32_t *out_anchor, float *out_score, cudaStream_t st);
 
+struct Pages;   // sla_paged.cuh
+struct Batch;
+cudaError_t launch_paged_decode(const void *q_s, const void *q, const Pages &pages, const Batch &batch, const Call &c, int dtype,
+                                const DecodePlan &plan, void *scratch, int *counters, void *out, float *lse, int32_t *out_anchor,
+                                float *out_score, cudaStream_t st);
+
 // Sequence-sharded decode step (sla_decode.cu): local candidates of one rank, global selection +
 // attention over this rank's part of the spans, merge of the ranks' partial results.
 cudaError_t launch_decode_shard_search(const void *q_s, const void *k_local, const Call &c, int dtype,

@@ -1,0 +1,313 @@
+// Paged key/value cache: what its kernels share (internal; the public interface is include/sla.h).
+#pragma once
+
+#include "sla_common.cuh"
+
+namespace sla {
+
+// A cache by value, as the kernels take it.
+struct Pages {
+    char *k, *v;
+    int *table, *n_tokens, *ref;
+    int n_pages, P, shift;          // page_tokens = P = 1 << shift
+    int Hkv, D, es;                 // es: bytes of an element
+    int n_slots, width;
+    long long s_page, s_h, s_t;     // in elements
+    int *status;
+};
+
+// The sequences of a call.
+struct Batch {
+    int n_seqs, n_new, max_new;
+    const int *seq, *cu;            // either may be NULL (slots 0 .. n_seqs-1; one token a sequence)
+};
+
+// Rows [lo, hi) of sequence x in the call's tensors, kept inside them whatever cu_new holds.
+__device__ __forceinline__ void new_rows(const Batch &b, int x, int &lo, int &hi) {
+    lo = b.cu ? min(max(b.cu[x], 0), b.n_new) : min(x, b.n_new);
+    hi = b.cu ? min(max(b.cu[x + 1], lo), b.n_new) : min(x + 1, b.n_new);
+}
+// The slot of sequence x, or -1 (the caller flags it).
+__device__ __forceinline__ int slot_of(const Pages &p, const Batch &b, int x) {
+    const int s = b.seq ? b.seq[x] : x;
+    return (unsigned)s < (unsigned)p.n_slots ? s : -1;
+}
+// Tokens of a slot, kept inside its table row.
+__device__ __forceinline__ int tokens_of(const Pages &p, int slot) {
+    const int n = p.n_tokens[slot], most = (int)min((long long)p.width << p.shift, 2147483647ll);
+    if (n < 0 || n > most) {
+        atomicOr(p.status, kStatusBadIndex);
+        return n < 0 ? 0 : most;
+    }
+    return n;
+}
+// A page number from the table: one outside the pool is flagged and read as page 0, so that no address leaves it.
+__device__ __forceinline__ int valid_page(const Pages &p, int page) {
+    if ((unsigned)page < (unsigned)p.n_pages) return page;
+    atomicOr(p.status, kStatusBadIndex);
+    return 0;
+}
+
+// ---- launchers (sla_cache.cu)
+cudaError_t launch_cache_extend(const Pages &p, const Batch &b, int *first, int *scratch, cudaStream_t st);
+cudaError_t launch_cache_append(const Pages &p, const Batch &b, const int *first, const void *k_new, const void *v_new,
+                                long long s_t, long long s_h, int sm_count, cudaStream_t st);
+cudaError_t launch_cache_release(const Pages &p, const int *seq, int n, cudaStream_t st);
+cudaError_t launch_cache_fork(const Pages &p, const int *src, const int *dst, int n, int *pairs, int *scratch, cudaStream_t st);
+cudaError_t launch_cache_compact(const Pages &p, int *pairs, int *scratch, int sm_count, cudaStream_t st);
+cudaError_t launch_cache_copy(const Pages &p, const int *pairs, int n, cudaStream_t st);
+size_t cache_scratch_bytes(const Pages &p, int n_seqs);   // of extend, fork and compact
+
+// ---- attention over the cache ---------------------------------------------------------------------
+// One call of sla_paged_attention.
+struct PagedCall {
+    Pages c;
+    Batch b;
+    int Hq, G, window;
+    long long q_st, q_sh;      // strides of q and out, in elements
+    float scale;
+};
+
+// The work of a call is a list of units -- (sequence, KV head, TQ consecutive new tokens with all G heads of the group) -- each
+// with the tiles of KT keys that its tokens see, written down as a running sum of weights (tiles + kUnitWeight, what a unit costs
+// beyond its tiles).  The list is cut into n_ranges equal ranges, wherever that falls: every CTA gets the same share of
+// the keys whatever the lengths are.  A unit that is cut leaves partial results, joined by paged_merge.
+struct Plan {
+    long long *seq_at;    // [n_seqs + 1] weight before sequence x
+    int *unit_at;         // [n_seqs + 1] units of one head before sequence x
+    long long *unit_end;  // [units] weight up to and with the unit, from the start of its (sequence, head)
+    int *n_ranges;
+    int max_units;        // room in unit_end
+};
+constexpr int kUnitWeight = 2;
+
+// Keys of the new tokens [t0, t1) of a sequence of n tokens, q of them new: tiles [lo, hi) of KT keys.
+__device__ __forceinline__ void unit_tiles(int n, int q, int t0, int t1, int window, int kt_shift, int &lo, int &hi) {
+    const int p0 = n - q + t0, end = n - q + t1;   // first position, one past the last
+    const int first = window > 0 && p0 - window + 1 > 0 ? p0 - window + 1 : 0;
+    lo = first >> kt_shift;
+    hi = end > 0 ? (end + (1 << kt_shift) - 1) >> kt_shift : lo;
+    if (hi < lo) hi = lo;
+}
+
+// A CTA builds the plan (all threads call it; the arrays are visible to the CTA on return).  TQ: tokens of a unit.
+// `groups`: the ranges are a multiple of n_ctas when the list is long, so that CTAs work on neighbouring units at any time
+// and share what they read in L2.
+template <int kThreads>
+__device__ inline void build_plan(const PagedCall &a, int TQ, int kt_shift, int n_ctas, int max_groups, int min_weight, const Plan &plan,
+                                  long long *s_sum) {
+    constexpr int kWarps = kThreads / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned full = 0xffffffffu;
+    // units of every sequence (a cu_new that does not ascend could name more than there is room for: those are left out)
+    if (warp == 0) {
+        int at = 0;
+        for (int x0 = 0; x0 < a.b.n_seqs; x0 += 32) {
+            const int x = x0 + lane;
+            int units = 0;
+            if (x < a.b.n_seqs) {
+                int lo, hi;
+                new_rows(a.b, x, lo, hi);
+                units = (hi - lo + TQ - 1) / TQ;
+            }
+            long long all = units;
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) all += __shfl_xor_sync(full, all, off);
+            if (at + all > plan.max_units) {
+                if (lane == 0) atomicOr(a.c.status, kStatusBadIndex);
+                units = 0;
+            }
+            int v = units;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int y = __shfl_up_sync(full, v, off);
+                if (lane >= off) v += y;
+            }
+            if (x < a.b.n_seqs) plan.unit_at[x] = at + v - units;
+            at += __shfl_sync(full, v, 31);
+        }
+        if (lane == 0) plan.unit_at[a.b.n_seqs] = at;
+    }
+    __syncthreads();
+    // weights of a sequence's units: by a lane where one unit is all there is, else by a warp
+    long long reread = 0;   // bytes of keys and values that several units read
+    for (int x0 = warp * 32; x0 < a.b.n_seqs; x0 += kWarps * 32) {
+        const int x = x0 + lane;
+        int units = 0, q = 0, n = 0;
+        if (x < a.b.n_seqs) {
+            int r0, r1;
+            new_rows(a.b, x, r0, r1);
+            q = r1 - r0;
+            units = plan.unit_at[x + 1] - plan.unit_at[x];
+            const int slot = slot_of(a.c, a.b, x);
+            if (slot < 0) atomicOr(a.c.status, kStatusBadIndex);
+            else n = tokens_of(a.c, slot);
+        }
+        long long total = 0;
+        if (units == 1) {
+            int lo, hi;
+            unit_tiles(n, q, 0, q, a.window, kt_shift, lo, hi);
+            total = hi - lo + kUnitWeight;
+            plan.unit_end[plan.unit_at[x]] = total;
+        }
+        for (unsigned many = __ballot_sync(full, units > 1); many; many &= many - 1) {
+            const int src = __ffs(many) - 1;
+            const int u_n = __shfl_sync(full, units, src), qs = __shfl_sync(full, q, src), ns = __shfl_sync(full, n, src);
+            const int base = plan.unit_at[x0 + src];
+            long long sum = 0;
+            for (int u0 = 0; u0 < u_n; u0 += 32) {
+                const int u = u0 + lane;
+                int lo, hi;
+                unit_tiles(ns, qs, u * TQ, min((u + 1) * TQ, qs), a.window, kt_shift, lo, hi);
+                long long v = u < u_n ? hi - lo + kUnitWeight : 0;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const long long y = __shfl_up_sync(full, v, off);
+                    if (lane >= off) v += y;
+                }
+                if (u < u_n) plan.unit_end[base + u] = sum + v;
+                sum += __shfl_sync(full, v, 31);
+            }
+            if (lane == src) {
+                total = sum;
+                reread += (long long)n * a.c.Hkv * a.c.D * a.c.es * 2;
+            }
+        }
+        if (x < a.b.n_seqs) plan.seq_at[x + 1] = total * a.c.Hkv;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        long long at = 0;
+        for (int x0 = 0; x0 < a.b.n_seqs; x0 += 32) {
+            const int x = x0 + lane;
+            long long v = x < a.b.n_seqs ? plan.seq_at[x + 1] : 0;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const long long y = __shfl_up_sync(full, v, off);
+                if (lane >= off) v += y;
+            }
+            if (x < a.b.n_seqs) plan.seq_at[x + 1] = at + v;
+            at += __shfl_sync(full, v, 31);
+        }
+        if (lane == 0) plan.seq_at[0] = 0;
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) reread += __shfl_xor_sync(full, reread, off);
+    if (lane == 0) s_sum[warp] = reread;
+    __syncthreads();
+    if (tid == 0) {
+        long long bytes = 0;
+        for (int w = 0; w < kWarps; ++w) bytes += s_sum[w];
+        const long long total = plan.seq_at[a.b.n_seqs];
+        long long groups = (bytes + (48ll << 20) - 1) / (48ll << 20);
+        groups = groups < 1 ? 1 : groups > max_groups ? max_groups : groups;
+        long long n = groups * n_ctas;
+        if (n > total / min_weight) n = total / min_weight;   // a range of a few tiles at least
+        if (n < 1) n = total > 0 ? 1 : 0;
+        *plan.n_ranges = (int)n;
+    }
+    __syncthreads();
+}
+
+// Index of the last entry of the ascending a[0 .. n) that is <= v (a[0] <= v); a converged warp, 32 ways a step.
+__device__ __forceinline__ int warp_last_le(const long long *a, int n, long long v) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 31) / 32;
+        const bool le = lane * step < n && a[lo + lane * step] <= v;
+        const int at = 31 - __clz(__ballot_sync(0xffffffffu, le));
+        lo += at * step;
+        n = min(step, n - at * step);
+    }
+    return lo;
+}
+
+__device__ __forceinline__ long long range_at(long long total, int n_ranges, int r) { return total * r / n_ranges; }
+
+// What one CTA does of one unit.
+struct Segment {
+    int x, head, unit;        // sequence, KV head, unit within the (sequence, head)
+    int slot, n, q;           // cache slot (-1: none), tokens, new tokens
+    int t0, t1, row0;         // new tokens of the unit; row of the sequence's first new token
+    int lo, hi;               // tiles to attend to
+    int part;                 // -1: the whole unit; else the partial result's number
+};
+
+// Goes through the segments of range r.  All warps that need a segment run a cursor of their own, converged, and see the same.
+struct Cursor {
+    long long w, end, total;
+    int x, head, unit, units, r, n_ranges;
+    bool first;
+
+    __device__ __forceinline__ bool start(const PagedCall &a, const Plan &plan, int range) {
+        n_ranges = *plan.n_ranges;
+        r = range;
+        if (r >= n_ranges) return false;
+        total = plan.seq_at[a.b.n_seqs];
+        w = range_at(total, n_ranges, r);
+        end = range_at(total, n_ranges, r + 1);
+        x = warp_last_le(plan.seq_at, a.b.n_seqs, w);
+        units = plan.unit_at[x + 1] - plan.unit_at[x];
+        const long long *ue = plan.unit_end + plan.unit_at[x];
+        const long long rem = w - plan.seq_at[x], per_head = ue[units - 1];
+        head = (int)(rem / per_head);
+        const long long in = rem - head * per_head;
+        unit = ue[0] > in ? 0 : warp_last_le(ue, units, in) + 1;
+        first = true;
+        return w < end;
+    }
+    // the segment at the cursor; false when the range is done.  *last_range: for a unit that starts in this range and does not
+    // end in it, the range it ends in, else -1.
+    __device__ __forceinline__ bool next(const PagedCall &a, const Plan &plan, int TQ, int kt_shift, Segment &s, int &last_range) {
+        last_range = -1;
+        if (w >= end) return false;
+        if (unit == units) {
+            unit = 0;
+            if (++head == a.c.Hkv) {
+                head = 0;
+                do ++x; while (plan.unit_at[x + 1] == plan.unit_at[x]);
+                units = plan.unit_at[x + 1] - plan.unit_at[x];
+            }
+        }
+        const long long *ue = plan.unit_end + plan.unit_at[x];
+        const long long u1 = ue[unit], u0 = unit ? ue[unit - 1] : 0;
+        const long long start = plan.seq_at[x] + head * ue[units - 1] + u0, stop = start + (u1 - u0);
+        s.x = x;
+        s.head = head;
+        s.unit = unit;
+        s.slot = slot_of(a.c, a.b, x);
+        s.n = s.slot < 0 ? 0 : tokens_of(a.c, s.slot);
+        int r1;
+        new_rows(a.b, x, s.row0, r1);
+        s.q = r1 - s.row0;
+        s.t0 = unit * TQ;
+        s.t1 = min(s.t0 + TQ, s.q);
+        int lo, hi;
+        unit_tiles(s.n, s.q, s.t0, s.t1, a.window, kt_shift, lo, hi);
+        const int from = (int)(w - start), to = (int)((end < stop ? end : stop) - start);   // weights of the unit in this range
+        s.lo = lo + max(from - kUnitWeight, 0);
+        s.hi = lo + max(to - kUnitWeight, 0);
+        const bool begins = from == 0, ends = end >= stop;
+        s.part = begins && ends ? -1 : begins ? 2 * r + 1 : 2 * r;
+        if (begins && !ends) {
+            int z = (int)(((double)stop * n_ranges) / (double)total);
+            z = min(max(z, r), n_ranges - 1);
+            while (z > r && range_at(total, n_ranges, z) >= stop) --z;
+            while (range_at(total, n_ranges, z + 1) < stop) ++z;
+            last_range = z;
+        }
+        w = end < stop ? end : stop;
+        ++unit;
+        return true;
+    }
+};
+
+// Partial results: part p of a unit of R rows has its normalised sums at o + p * R * D and its log2-sum-exp at lse2 + p * R (-inf: no
+// keys; the sums are then not written).  cut[r]: the unit that starts in range r and ends in range cut[r].w, -1 where none does.
+struct Parts {
+    float *o, *lse2;
+    int4 *cut;            // {sequence, head, unit, last range}
+};
+
+}  // namespace sla

@@ -1,0 +1,32 @@
+// Internal launcher declarations of the attention over a paged cache.
+#pragma once
+
+#include "sla_paged.cuh"
+
+namespace sla {
+
+// Tiles and scratch layout of one call (offsets in bytes from the scratch base).
+struct PagedPlan {
+    enum Kind { kRows } kind;
+    int R, RS, TS, TQ;      // rows of a unit, rows and tokens of its sub-tiles, tokens of the unit
+    int kt_shift;           // log2 of the keys of a tile
+    int n_ctas, max_groups, min_weight, max_units;
+    size_t off_seq_at, off_unit_at, off_unit_end, off_n_ranges, off_cut, off_lse2, off_o, bytes;
+};
+
+inline Plan plan_at(const PagedPlan &p, char *scratch) {
+    return {reinterpret_cast<long long *>(scratch + p.off_seq_at), reinterpret_cast<int *>(scratch + p.off_unit_at),
+            reinterpret_cast<long long *>(scratch + p.off_unit_end), reinterpret_cast<int *>(scratch + p.off_n_ranges), p.max_units};
+}
+inline Parts parts_at(const PagedPlan &p, char *scratch) {
+    return {reinterpret_cast<float *>(scratch + p.off_o), reinterpret_cast<float *>(scratch + p.off_lse2),
+            reinterpret_cast<int4 *>(scratch + p.off_cut)};
+}
+
+PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count);
+cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scratch, cudaStream_t st);
+cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st);
+cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse,
+                                   cudaStream_t st, long long *launches);
+
+}  // namespace sla

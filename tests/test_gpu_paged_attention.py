@@ -1,0 +1,259 @@
+"""Attention of new tokens over a paged cache against 64 bits: types, groups, pages, strides, windows, lengths from none to many."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sla():
+    import paper_2601_18401_b200 as sla_pkg
+    return sla_pkg
+
+
+@pytest.fixture(scope="module")
+def handle(sla):
+    h = sla.Handle(0, 1 << 30)
+    yield h
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    h.close()
+
+
+def build(sla, n, new, *, hkv=2, G=4, d=128, dtype=torch.bfloat16, page=16, token_major=False, gap=0, seed=3, spare=3):
+    """A cache of sequences of n tokens, their pages scattered; what no sequence owns is NaN."""
+    rs = np.random.RandomState(seed)
+    held = [-(-int(x) // page) for x in n]
+    n_pages = sum(held) + spare
+    k, v = U.make_pools(n_pages, hkv, page, d, dtype, token_major, gap, seed)
+    order = rs.permutation(n_pages)
+    width = max(held + [1]) + 1
+    table = np.full((len(n), width), -1, dtype=np.int32)
+    at = 0
+    for x, c in enumerate(held):
+        table[x, :c] = order[at:at + c]
+        at += c
+        if c and n[x] % page:
+            k[int(table[x, c - 1]), :, n[x] % page:] = math.nan
+            v[int(table[x, c - 1]), :, n[x] % page:] = math.nan
+    for p in order[at:]:
+        k[int(p)] = math.nan
+        v[int(p)] = math.nan
+    ref = np.bincount(table[table >= 0], minlength=n_pages)
+    tensors = [U.device_ints(table), U.device_ints(n), U.device_ints(ref)]
+    cache = sla.make_cache(k, v, *tensors)
+    cu = U.device_ints(np.concatenate([[0], np.cumsum(new)]))
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(seed + 1)
+    q = torch.empty(int(sum(new)), hkv * G, d, dtype=dtype, device="cuda:0").normal_(generator=g)
+    return cache, k, v, table, q, cu
+
+
+def run(sla, handle, n, new, window=0, scale=None, max_new=None, prep=None, **kw):
+    cache, k, v, table, q, cu = build(sla, n, new, **kw)
+    if prep:
+        prep(k, v, table, q)
+    out, lse = sla.sla_paged_attention(handle, q, cache, cu, window=window, softmax_scale=scale, max_new=max(new) if max_new is None else max_new)
+    torch.cuda.synchronize()
+    s = 1 / math.sqrt(q.shape[-1]) if scale is None else scale
+    ref = U.attention_reference(q, k, v, table, n, new, kw.get("G", 4), window, s, kw.get("page", 16))
+    U.check_attention(out, lse, ref, q.dtype)
+    return out, lse, ref
+
+
+BF16, F32 = torch.bfloat16, torch.float32
+SINGLE = ([1, 2, 15, 16, 17, 0, 63, 64, 65, 700], [1] * 10)       # one token each, an empty sequence among them
+CHUNKS = ([40, 5, 0, 129, 300, 64, 513], [40, 0, 0, 1, 77, 64, 200])   # whole prompts, ends of prompts, nothing new
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("lens", [SINGLE, CHUNKS], ids=["single", "chunks"])
+def test_types(sla, handle, dtype, d, lens):
+    run(sla, handle, *lens, dtype=dtype, d=d)
+
+
+@pytest.mark.parametrize("hkv,G", [(1, 1), (3, 2), (2, 3), (1, 5), (2, 7), (1, 8), (1, 12), (2, 16)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_groups(sla, handle, hkv, G, dtype):
+    run(sla, handle, *SINGLE, hkv=hkv, G=G, dtype=dtype)
+    run(sla, handle, *CHUNKS, hkv=hkv, G=G, dtype=dtype)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("token_major,gap", [(False, 0), (True, 0), (False, 64), (True, 8)])
+def test_pages_and_strides(sla, handle, page, token_major, gap):
+    run(sla, handle, *SINGLE, page=page, token_major=token_major, gap=gap)
+    run(sla, handle, *CHUNKS, page=page, token_major=token_major, gap=gap, hkv=3)
+
+
+@pytest.mark.parametrize("window", [1, 2, 16, 63, 64, 129, 400, 5000])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_window(sla, handle, window, dtype):
+    run(sla, handle, *SINGLE, window=window, dtype=dtype)
+    run(sla, handle, *CHUNKS, window=window, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_without_keys(sla, handle, dtype):
+    """Sequences shorter than their new tokens: the first rows see nothing."""
+    out, lse, _ = run(sla, handle, [3, 0, 20, 1], [5, 4, 20, 3], dtype=dtype)
+    assert (out[:2] == 0).all() and (out[5:9] == 0).all()
+    run(sla, handle, [0, 0], [1, 1], dtype=dtype)
+    run(sla, handle, [0, 7], [1, 0], dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("G", [4, 16])
+def test_long_sequences_are_cut_and_joined(sla, handle, dtype, G):
+    """Few rows over long contexts: every CTA takes a part, a second kernel joins them."""
+    run(sla, handle, [20000, 33, 9001], [1, 1, 1], G=G, dtype=dtype, page=64)
+    run(sla, handle, [20000, 33, 9001], [3, 2, 1], G=G, dtype=dtype, page=64)
+    run(sla, handle, [6000], [70], G=G, dtype=dtype, page=64)
+    run(sla, handle, [6000, 4000], [70, 130], G=G, dtype=dtype, page=32, window=900)
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, 1), (BF16, 2), (BF16, 150), (F32, 1), (F32, 150)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(sla, handle, dtype, new, bad):
+    """A NaN or an infinity in a key or value is seen by the rows at and after it (inside the window), and by no other."""
+    n = [400, 300]
+    new = [new, new]
+    at = 399 if new[0] == 1 else 398 if new[0] == 2 else 330
+
+    def one(which):
+        def prep(k, v, table, q):
+            t = (k, v)[which]
+            t[int(table[0, at // 16]), 1, at % 16, 5] = bad
+        return prep
+    run(sla, handle, n, new, dtype=dtype, prep=one(1))
+    run(sla, handle, n, new, dtype=dtype, prep=one(1), window=20)
+
+    # keys: a row that sees it is NaN, or has an infinite weight; the others are what they were
+    cache, k, v, table, q, cu = build(sla, n, new, dtype=dtype)
+    clean, clean_lse = sla.sla_paged_attention(handle, q, cache, cu, max_new=new[0])
+    one(0)(k, v, table, q)
+    out, lse = sla.sla_paged_attention(handle, q, cache, cu, max_new=new[0])
+    sees = n[0] - new[0] + torch.arange(new[0], device=out.device) >= at
+    assert torch.equal(out[:new[0]][~sees], clean[:new[0]][~sees]) and torch.equal(out[new[0]:], clean[new[0]:])
+    assert torch.equal(lse[:new[0]][~sees], clean_lse[:new[0]][~sees])
+    assert torch.equal(out[:, :4], clean[:, :4])   # the other KV head
+    if math.isnan(bad):
+        assert torch.isnan(out[:new[0]][sees][:, 4:]).all() and torch.isnan(lse[:new[0]][sees][:, 4:]).all()
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, [1, 1]), (BF16, [60, 1]), (F32, [60, 1])])
+def test_large_logits_and_scales(sla, handle, dtype, new):
+    run(sla, handle, [500, 31], new, dtype=dtype, scale=3.0)
+    run(sla, handle, [500, 31], new, dtype=dtype, scale=0.0)
+    run(sla, handle, [500, 31], new, dtype=dtype, scale=-0.5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_strided_queries_slots_and_shared_pages(sla, handle, dtype):
+    """Queries inside a larger tensor, sequences named by slot in any order, two sequences on the same pages."""
+    n, new = [100, 64, 250], [3, 1, 40]
+    cache, k, v, table, q, cu = build(sla, n, new, dtype=dtype)
+    table[1] = table[2]                     # slot 1 shares slot 2's first pages
+    cache.tensors[2].copy_(U.device_ints(table))
+    big = torch.zeros(44, 3, 8, 128, dtype=dtype, device="cuda:0")
+    big[:, 1] = q
+    order = [2, 0, 1]
+    cu2 = U.device_ints(np.concatenate([[0], np.cumsum([new[s] for s in order])]))
+    out = torch.full_like(big, 7.0)
+    o, lse = sla.sla_paged_attention(handle, big[:, 1], cache, cu2, seq=U.device_ints(order), max_new=40, out=out[:, 1])
+    ref = U.attention_reference(q, k, v, table[order], [n[s] for s in order], [new[s] for s in order], 4, 0, 128 ** -0.5, 16)
+    U.check_attention(o, lse, ref, dtype)
+    assert (out[:, 0] == 7).all() and (out[:, 2] == 7).all()
+
+
+def test_chunk_bound_may_be_loose(sla, handle):
+    """max_new is a bound: single tokens with a bound of many give the same results."""
+    a, la, _ = run(sla, handle, *SINGLE)
+    b, lb, _ = run(sla, handle, *SINGLE, max_new=500)
+    assert (a.float() - b.float()).abs().max() < 0.05
+
+
+def test_no_new_token_and_one_token_without_offsets(sla, handle):
+    cache, k, v, table, q, cu = build(sla, [30, 50], [1, 1])
+    a = sla.sla_paged_attention(handle, q, cache)            # one token per slot
+    b = sla.sla_paged_attention(handle, q, cache, cu, max_new=1)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    zero = torch.zeros(3, dtype=torch.int32, device="cuda:0")
+    o, l = sla.sla_paged_attention(handle, q[:0], cache, zero)
+    assert o.shape == (0, 8, 128) and l.shape == (0, 8)
+
+
+def test_same_result_every_time(sla, handle):
+    """The order of sums does not depend on timing."""
+    cache, k, v, table, q, cu = build(sla, [9000, 100, 4000], [1, 50, 300], page=64)
+    a = sla.sla_paged_attention(handle, q, cache, cu, max_new=300)
+    for _ in range(3):
+        b = sla.sla_paged_attention(handle, q, cache, cu, max_new=300)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_other_stream(sla, handle):
+    cache, k, v, table, q, cu = build(sla, *CHUNKS)
+    a = sla.sla_paged_attention(handle, q, cache, cu, max_new=200)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        b = sla.sla_paged_attention(handle, q, cache, cu, max_new=200)
+    st.synchronize()
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_what_is_out_of_range_is_flagged_and_not_followed(sla):
+    """Slots and pages outside the cache, lengths beyond the table, offsets that do not ascend: the status word, no fault."""
+    h = sla.Handle(0, 1 << 28)
+    for new in ([1, 1], [40, 33]):
+        cache, k, v, table, q, cu = build(sla, [100, 60], new)
+        sla.sla_paged_attention(h, q, cache, cu, max_new=max(new), seq=U.device_ints([0, 9]))
+        assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+        bad = table.copy()
+        bad[0, 1] = 10 ** 6
+        cache.tensors[2].copy_(U.device_ints(bad))
+        sla.sla_paged_attention(h, q, cache, cu, max_new=max(new))
+        assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+        bad[0, 1] = -1
+        cache.tensors[2].copy_(U.device_ints(bad))
+        sla.sla_paged_attention(h, q, cache, cu, max_new=max(new))
+        assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+        cache.tensors[2].copy_(U.device_ints(np.where(table < 0, 0, table)))
+        cache.tensors[3].copy_(U.device_ints([10 ** 6, 60]))
+        sla.sla_paged_attention(h, q, cache, cu, max_new=max(new))
+        assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+        cache.tensors[3].copy_(U.device_ints([100, 60]))
+        sla.sla_paged_attention(h, q, cache, U.device_ints([0, 10 ** 6, -5]), max_new=max(new))
+        torch.cuda.synchronize()
+        sla.sla_poll_status(h)
+    h.close()
+
+
+def test_refusals(sla, handle):
+    cache, k, v, table, q, cu = build(sla, [30, 50], [1, 1])
+    with pytest.raises(sla.SlaError):
+        sla.sla_paged_attention(handle, q, cache, cu, window=-1)
+    with pytest.raises(sla.SlaError):
+        sla.sla_paged_attention(handle, q, cache, cu, softmax_scale=math.nan)
+    with pytest.raises(sla.SlaError):
+        sla.sla_paged_attention(handle, q[:, :7], cache, cu)         # not a multiple of the KV heads
+    with pytest.raises(sla.SlaError):
+        sla.sla_paged_attention(handle, torch.zeros(2, 40, 128, dtype=q.dtype, device=q.device), cache, cu)   # groups of 20
+    with pytest.raises(sla.SlaError):
+        sla.sla_paged_attention(handle, q, cache, cu, max_new=0)
+    with pytest.raises(ValueError):
+        sla.sla_paged_attention(handle, q[..., :64], cache, cu)
+    with pytest.raises(TypeError):
+        sla.sla_paged_attention(handle, q.half(), cache, cu)
+    with pytest.raises(ValueError):
+        sla.sla_paged_attention(handle, q, cache, cu, out=torch.empty(2, 8, 256, dtype=q.dtype, device=q.device)[..., ::2])
+    small = sla.Handle(0, 4096)
+    with pytest.raises(sla.SlaError) as e:
+        sla.sla_paged_attention(small, q, cache, cu)
+    assert e.value.status == -3
+    small.close()

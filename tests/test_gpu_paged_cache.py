@@ -1,0 +1,305 @@
+"""Bookkeeping of the paged cache -- extend, append, fork, release, compact, copy -- against a model in plain Python: every table
+entry, length, count and every page's contents equal."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sla():
+    import paper_2601_18401_b200 as sla_pkg
+    return sla_pkg
+
+
+@pytest.fixture(scope="module")
+def handle(sla):
+    h = sla.Handle(0, 1 << 28)
+    yield h
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    h.close()
+
+
+class Pair:
+    """A cache on the device and its model; the model's tokens are a list of rows per slot."""
+
+    def __init__(self, sla, h, n_pages=40, page=16, n_slots=8, width=12, hkv=2, d=64, dtype=torch.bfloat16, token_major=False, gap=0):
+        self.sla, self.h, self.page = sla, h, page
+        self.m = U.Model(n_pages, page, n_slots, width)
+        self.k, self.v = U.make_pools(n_pages, hkv, page, d, dtype, token_major, gap)
+        self.dev = [U.device_ints(a) for a in (self.m.table, self.m.n, self.m.ref)]
+        self.cache = sla.make_cache(self.k, self.v, *self.dev)
+        self.rows = {s: [] for s in range(n_slots)}   # (k, v) rows [hkv, d] by position
+        self.gen = torch.Generator(device="cuda:0")
+
+    def same(self):
+        torch.cuda.synchronize()
+        for a, b in zip(self.dev, (self.m.table, self.m.n, self.m.ref)):
+            assert np.array_equal(a.cpu().numpy(), b)
+        for s, rows in self.rows.items():
+            assert len(rows) == self.m.n[s]
+            for p, (k, v) in enumerate(rows):
+                page = int(self.m.table[s, p // self.page])
+                assert torch.equal(self.k[page, :, p % self.page], k), (s, p)
+                assert torch.equal(self.v[page, :, p % self.page], v), (s, p)
+
+    def add(self, seq, new, strided=False):
+        hkv, d = self.k.shape[1], self.k.shape[3]
+        T = int(sum(new))
+        x = torch.empty(2, max(T, 1), hkv + (1 if strided else 0), d, dtype=self.k.dtype, device="cuda:0").normal_(generator=self.gen)
+        k_new, v_new = x[0, :T, :hkv], x[1, :T, :hkv]
+        cu = U.device_ints(np.concatenate([[0], np.cumsum(new)]))
+        first = self.sla.sla_cache_extend(self.h, self.cache, cu, seq=U.device_ints(seq))
+        want = self.m.extend(seq, new)
+        assert np.array_equal(first.cpu().numpy(), want)
+        self.sla.sla_cache_append(self.h, self.cache, cu, first, k_new, v_new, seq=U.device_ints(seq))
+        at = 0
+        for s, c, f in zip(seq, new, want):
+            if f >= 0:
+                self.rows[s] += [(k_new[at + r], v_new[at + r]) for r in range(c)]
+            at += c
+        self.same()
+        return want
+
+    def fork(self, src, dst):
+        pairs = self.sla.sla_cache_fork(self.h, self.cache, U.device_ints(src), U.device_ints(dst))
+        want = self.m.fork(src, dst)
+        assert np.array_equal(pairs.cpu().numpy(), want)
+        for s, d in zip(src, dst):
+            if self.m.n[d]:
+                self.rows[d] = list(self.rows[s])
+        self.same()
+        return pairs
+
+    def release(self, seq):
+        self.sla.sla_cache_release(self.h, self.cache, U.device_ints(seq))
+        self.m.release(seq)
+        for s in seq:
+            self.rows[s] = []
+        self.same()
+
+    def compact(self):
+        pairs = self.sla.sla_cache_compact(self.h, self.cache)
+        assert np.array_equal(pairs.cpu().numpy(), self.m.compact())
+        self.same()
+        live = int((self.m.ref > 0).sum())
+        assert (self.m.ref[:live] > 0).all()
+        return pairs
+
+
+@pytest.mark.parametrize("dtype,d,hkv", [(torch.bfloat16, 64, 2), (torch.bfloat16, 128, 8), (torch.float32, 128, 3), (torch.float32, 64, 1)])
+@pytest.mark.parametrize("token_major,gap", [(False, 0), (True, 0), (True, 24)])
+def test_a_life_of_a_cache(sla, handle, dtype, d, hkv, token_major, gap):
+    """Prompts, steps of one token, forks, ends, compaction, and on."""
+    c = Pair(sla, handle, dtype=dtype, d=d, hkv=hkv, token_major=token_major, gap=gap)
+    c.add([0, 2, 5], [40, 0, 33])
+    c.add([5, 0], [1, 15])
+    c.fork([0, 5, 0, 2], [1, 3, 4, 6])       # a partly filled page, another of the same parent, an empty parent
+    for _ in range(3):
+        c.add([4, 3, 1, 0], [1, 1, 1, 1])
+    c.release([0, 5])
+    c.add([7], [50], strided=True)
+    c.compact()
+    c.compact()                                # nothing left to move
+    c.add([1, 3, 4, 7], [17, 16, 1, 2])
+    c.release([1, 3, 4, 7, 2, 6])
+    assert (c.m.ref == 0).all()
+    c.compact()
+    c.add([0], [100])
+
+
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_page_edges(sla, handle, page):
+    c = Pair(sla, handle, page=page, n_pages=20, width=5)
+    c.add([0, 1, 2], [page, page - 1, 1])
+    c.add([0, 1, 2], [0, 1, page - 1])
+    c.fork([0, 1], [3, 4])                     # only full pages: nothing is copied
+    c.add([0, 1, 2, 3], [1, page, page + 1, 1])
+    c.fork([0], [5])
+    c.release([0])
+    c.compact()
+
+
+def test_refused_sequences_stay_as_they_were(sla):
+    h = sla.Handle(0, 1 << 26)
+    c = Pair(sla, h, n_pages=6, width=4)
+    assert list(c.add([0, 1], [40, 20])) == [0, 0]
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    # one page is left: 1 wants one and gets it, 2 wants two and 0 one more than there are, 3 wants none
+    assert list(c.add([1, 2, 0, 3], [13, 17, 9, 0])) == [20, -1, -1, 0]
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_CACHE_FULL
+    assert list(c.add([0, 1], [8, 100])) == [40, -1]        # fits the last page; a table row of four pages is too short
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_CACHE_FULL
+    # no page for the copy of a partly filled one
+    pairs = sla.sla_cache_fork(h, c.cache, U.device_ints([1, 0]), U.device_ints([4, 5]))
+    assert np.array_equal(pairs.cpu().numpy(), c.m.fork([1, 0], [4, 5]))
+    assert c.m.n[4] == 0 and c.m.n[5] == 48
+    c.rows[5] = list(c.rows[0])
+    c.same()
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_CACHE_FULL
+    # a slot that is not empty
+    sla.sla_cache_fork(h, c.cache, U.device_ints([0]), U.device_ints([1]))
+    c.same()
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    # slots outside the cache
+    first = sla.sla_cache_extend(h, c.cache, U.device_ints([0, 1, 2]), seq=U.device_ints([-1, 8]))
+    assert list(first.cpu()) == [-1, -1] and sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    sla.sla_cache_release(h, c.cache, U.device_ints([99]))
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    sla.sla_cache_copy(h, c.cache, U.device_ints([[0], [6]]))
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    c.same()
+    # released twice in one call: every reference goes once
+    sla.sla_cache_release(h, c.cache, U.device_ints([0, 0]))
+    c.m.release([0])
+    c.rows[0] = []
+    c.same()
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    h.close()
+
+
+def test_copy_follows_the_pairs_of_another_layer(sla, handle):
+    """fork and compact run on one layer; a second layer's pools follow by the pairs they return."""
+    c = Pair(sla, handle)
+    k2, v2 = U.make_pools(40, 2, 16, 64, torch.bfloat16, seed=9)
+    other = sla.make_cache(k2, v2, *c.dev)
+    c.add([0, 1], [40, 20])
+    before = [k2[int(c.m.table[0, p // 16]), :, p % 16].clone() for p in range(40)]
+    pairs = c.fork([0, 0], [2, 3])
+    sla.sla_cache_copy(handle, other, pairs)
+    c.release([0, 1])
+    sla.sla_cache_copy(handle, other, c.compact())
+    for s in (2, 3):
+        for p in range(40):
+            assert torch.equal(k2[int(c.m.table[s, p // 16]), :, p % 16], before[p])
+
+
+@pytest.mark.parametrize("n_pages", [5000, 70000])
+def test_many_pages_and_sequences(sla, n_pages):
+    """Pools of several chunks, more sequences than a warp or a CTA has threads."""
+    h = sla.Handle(0, 1 << 26)
+    rs = np.random.RandomState(n_pages)
+    slots = 1500
+    m = U.Model(n_pages, 16, slots, 40)
+    k, v = U.make_pools(n_pages, 1, 16, 64, torch.bfloat16)
+    dev = [U.device_ints(a) for a in (m.table, m.n, m.ref)]
+    cache = sla.make_cache(k, v, *dev)
+    for _ in range(3):
+        seq = rs.permutation(slots)
+        new = rs.randint(0, 40, slots)
+        first = sla.sla_cache_extend(h, cache, U.device_ints(np.concatenate([[0], np.cumsum(new)])), seq=U.device_ints(seq))
+        assert np.array_equal(first.cpu().numpy(), m.extend(seq, new))
+    gone = rs.permutation(slots)[:700]
+    sla.sla_cache_release(h, cache, U.device_ints(gone))
+    m.release(gone)
+    kids, parents = gone[:300], rs.permutation(np.setdiff1d(np.arange(slots), gone))[:300]
+    pairs = sla.sla_cache_fork(h, cache, U.device_ints(parents), U.device_ints(kids))
+    assert np.array_equal(pairs.cpu().numpy(), m.fork(parents, kids))
+    old_k, old_table = k.clone(), m.table.copy()
+    pairs = sla.sla_cache_compact(h, cache)
+    assert np.array_equal(pairs.cpu().numpy(), m.compact())
+    for a, b in zip(dev, (m.table, m.n, m.ref)):
+        assert np.array_equal(a.cpu().numpy(), b)
+    on = old_table >= 0
+    assert torch.equal(k[torch.from_numpy(m.table[on].astype(np.int64)).cuda()], old_k[torch.from_numpy(old_table[on].astype(np.int64)).cuda()])
+    sla.sla_poll_status(h)
+    h.close()
+
+
+def test_refusals(sla, handle):
+    c = Pair(sla, handle)
+    k = torch.zeros(4, 2, 24, 64, dtype=torch.bfloat16, device="cuda:0")
+    t, n, r = U.device_ints([[0, 1]]), U.device_ints([0]), U.device_ints([0] * 4)
+    odd = sla.make_cache(k, k.clone(), t, n, r)                      # 24 tokens a page
+    with pytest.raises(sla.SlaError):
+        sla.sla_cache_extend(handle, odd, U.device_ints([0, 1]))
+    assert sla.sla_paged_workspace_bytes(odd, 2, 1, 1) == 0
+    assert sla.sla_paged_workspace_bytes(c.cache, 3, 1, 1) == 0 and sla.sla_paged_workspace_bytes(c.cache, 2, 1, 1) > 0
+    for bad in (lambda: sla.make_cache(k, k[:3], t, n, r), lambda: sla.make_cache(k, k.clone(), t.long(), n, r),
+                lambda: sla.make_cache(k, k.clone(), t, n, r[:2]), lambda: sla.make_cache(k, k.transpose(2, 3), t, n, r)):
+        with pytest.raises(ValueError):
+            bad()
+    cu, first = U.device_ints([0, 2]), U.device_ints([0])
+    new = torch.zeros(2, 2, 64, dtype=torch.bfloat16, device="cuda:0")
+    with pytest.raises(ValueError):
+        sla.sla_cache_append(handle, c.cache, cu, first, new[:, :1], new[:, :1])
+    with pytest.raises(ValueError):
+        sla.sla_cache_append(handle, c.cache, cu, first, new.float(), new.float())
+    with pytest.raises(ValueError):
+        sla.sla_cache_append(handle, c.cache, cu, U.device_ints([0, 0]), new, new)
+    with pytest.raises(ValueError):
+        sla.sla_cache_fork(handle, c.cache, U.device_ints([0, 1]), U.device_ints([2]))
+    small = sla.Handle(0, 256)
+    with pytest.raises(sla.SlaError) as e:
+        sla.sla_cache_compact(small, c.cache)
+    assert e.value.status == -3
+    small.close()
+
+
+# ---- the span decode step over the cache -----------------------------------------------------------------
+
+
+def contiguous(k, table, n, page):
+    pages = torch.from_numpy(table[: -(-n // page)].astype(np.int64)).cuda()
+    return k[pages].transpose(0, 1).reshape(1, k.shape[1], -1, k.shape[3])[:, :, :n].contiguous()
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("mode", ["union", "window", "gated", "exponents"])
+def test_span_step_equals_the_step_over_each_sequence_alone(sla, dtype, d, mode):
+    """Every sequence's step is the one of sla_decode_step on a contiguous copy of it: the same anchors and scores, outputs within
+    rounding."""
+    import test_gpu_paged_attention as A
+    h = sla.Handle(0, 1 << 28)
+    n = [1, 2, 100, 1031, 0, 5000, 777]
+    cache, k, v, table, _, _ = A.build(sla, n, [0] * len(n), dtype=dtype, d=d, page=32, G=4)
+    kw = {"union": {}, "window": dict(window=33), "gated": dict(window=35, mode=sla.SLA_PER_SPAN),
+          "exponents": dict(search_exponent=0.4, span_exponent=0.6)}[mode]
+    params = sla.make_params(4, 0, fwd_factor=1, head_dim=d, **kw)
+    g = torch.Generator(device="cuda:0")
+    q_s, q = (torch.empty(len(n), 8, d, dtype=dtype, device="cuda:0").normal_(generator=g) for _ in range(2))
+    need = sla.sla_paged_workspace_bytes(cache, 8, len(n), len(n), params=params)
+    assert need <= 1 << 28
+    order = [6, 0, 5, 4, 3, 2, 1]
+    out, lse, anchor, score = sla.sla_paged_decode_step(h, q_s, q, cache, params, seq=U.device_ints(order), max_tokens=6000)
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    for x, s in enumerate(order):
+        if n[s] == 0:
+            assert (out[x] == 0).all() and (lse[x] == -math.inf).all() and (anchor[x] == -1).all() and (score[x] == -math.inf).all()
+            continue
+        one = sla.sla_decode_step(h, q_s[x:x + 1], q[x:x + 1], contiguous(k, table[s], n[s], 32), contiguous(v, table[s], n[s], 32), n[s], params)
+        assert torch.equal(one[2][0], anchor[x]) and torch.equal(one[3][0], score[x])
+        # the two differ in how a head's tokens are shared out: fp32 sums of at most n terms in another order, one rounding of the result
+        big = v.float().nan_to_num().abs().max()
+        tol = 2.0 ** -8 * one[0][0].float().abs() + 1e-6 * big if dtype == torch.bfloat16 else 2e-6 * big
+        assert ((one[0][0].float() - out[x].float()).abs() <= tol).all()
+        a, b = one[1][0], lse[x]
+        assert torch.equal(torch.isfinite(a), torch.isfinite(b)) and ((a - b).abs().nan_to_num() <= 4e-6 * (1 + a.abs().nan_to_num(posinf=0, neginf=0))).all()
+    h.close()
+
+
+def test_span_step_refusals(sla):
+    import test_gpu_paged_attention as A
+    h = sla.Handle(0, 1 << 26)
+    cache, k, v, table, _, _ = A.build(sla, [100, 60], [0, 0])
+    params = sla.make_params(4, 0)
+    q = torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda:0")
+    # longer than the bound, or a slot outside the cache: flagged, no result
+    out, lse, anchor, _ = sla.sla_paged_decode_step(h, q, q, cache, params, max_tokens=80)
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    assert (out[0] == 0).all() and (anchor[0] == -1).all() and (anchor[1] >= 0).all()
+    sla.sla_paged_decode_step(h, q, q, cache, params, seq=U.device_ints([5, -1]))
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    for bad in (lambda: sla.sla_paged_decode_step(h, q, q, cache, sla.make_params(65, 0)),
+                lambda: sla.sla_paged_decode_step(h, q, q, cache, params, max_tokens=0),
+                lambda: sla.sla_paged_decode_step(h, q[:, :7], q[:, :7], cache, params)):
+        with pytest.raises(sla.SlaError):
+            bad()
+    with pytest.raises(ValueError):
+        sla.sla_paged_decode_step(h, q.float(), q, cache, params)
+    h.close()
