@@ -381,7 +381,7 @@ typedef struct {
     int32_t n_pages, page_tokens;   /* page_tokens: a power of two, 16 .. 256                     */
     int32_t n_kv_heads, head_dim;   /* head_dim 64 or 128                                          */
     int32_t dtype, reserved;        /* sla_dtype_t of k and v; reserved must be 0                   */
-    int32_t n_slots, table_width;
+    int32_t n_slots, table_width;   /* table_width * page_tokens at most 2^31 - 1025                */
     int64_t stride_page, stride_h, stride_t; /* of k and v, in elements                            */
     void *k, *v;
     int32_t *table, *n_tokens, *ref;

@@ -5,7 +5,6 @@
 #include <stdlib.h>
 #include <string.h>
 
-#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -804,6 +803,7 @@ const char *check_cache(const sla_cache_t *c) {
     if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens must be a power of two in 16..256";
     if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
     if (c->n_kv_heads > 65536) return "n_kv_heads above 65536";
+    if ((int64_t)c->table_width * c->page_tokens > 2147483647LL - 1024) return "table_width * page_tokens above 2^31 - 1025";
     if (c->dtype != SLA_F32 && c->dtype != SLA_BF16) return "dtype must be SLA_F32 or SLA_BF16";
     if (c->reserved != 0) return "reserved must be 0";
     for (int64_t s : {c->stride_page, c->stride_h, c->stride_t})
@@ -873,8 +873,7 @@ size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_
     }
     if (p && n_seqs > 0) {
         const sla_layout_t l = layout_of(c, n_q_heads, n_seqs, c->head_dim * (int64_t)n_q_heads, c->head_dim);
-        const int64_t most = std::min<int64_t>((int64_t)c->table_width * c->page_tokens, 2147483647);
-        const size_t bytes = sla_workspace_bytes(&l, p, 1, most);
+        const size_t bytes = sla_workspace_bytes(&l, p, 1, (int64_t)c->table_width * c->page_tokens);
         if (bytes == 0) return 0;
         if (bytes > need) need = bytes;
     }
@@ -980,7 +979,7 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     a.scale = softmax_scale;
     const sla::PagedPlan plan = sla::plan_paged(a, c->dtype, h->sm_count);
     if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
-    cudaError_t e = sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, out, lse, static_cast<cudaStream_t>(stream), &h->launches);
+    cudaError_t e = sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, static_cast<cudaStream_t>(stream), &h->launches);
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_paged_attention");
     return SLA_OK;
 }

@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_extend(Pages p, Batch b, i
             } else {
                 const long long n = p.n_tokens[s], want = n + (hi - lo);
                 if (n < 0 || n > (long long)p.width << p.shift) atomicOr(p.status, kStatusBadIndex);
-                else if (want > (long long)p.width << p.shift || want > 2147483647ll) atomicOr(p.status, kStatusCacheFull);
+                else if (want > (long long)p.width << p.shift) atomicOr(p.status, kStatusCacheFull);
                 else {
                     need = pages_for(p, want) - pages_for(p, n);
                     at = (int)n;

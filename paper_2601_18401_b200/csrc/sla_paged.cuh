@@ -34,7 +34,7 @@ __device__ __forceinline__ int slot_of(const Pages &p, const Batch &b, int x) {
 }
 // Tokens of a slot, kept inside its table row.
 __device__ __forceinline__ int tokens_of(const Pages &p, int slot) {
-    const int n = p.n_tokens[slot], most = (int)min((long long)p.width << p.shift, 2147483647ll);
+    const int n = p.n_tokens[slot], most = p.width << p.shift;
     if (n < 0 || n > most) {
         atomicOr(p.status, kStatusBadIndex);
         return n < 0 ? 0 : most;

@@ -347,6 +347,10 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.n_ctas = 2 * sm_count;
     p.max_groups = 1;
     p.min_weight = 4;
+    if (paged_decode_supported(a, dtype)) {
+        p.kind = PagedPlan::kDecode;
+        plan_paged_decode(a, p, sm_count);
+    }
     const size_t ranges = (size_t)p.n_ctas * p.max_groups, units = (size_t)(a.b.n_new / p.TQ) + a.b.n_seqs + 1;
     p.max_units = (int)units;
     size_t off = 0;
@@ -366,8 +370,9 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     return p;
 }
 
-cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse,
-                                   cudaStream_t st, long long *launches) {
+cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
+                                   float *lse, cudaStream_t st, long long *launches) {
+    if (p.kind == PagedPlan::kDecode) return launch_paged_decode_attention(q, a, p, scratch, counters, out, lse, st, launches);
     cudaError_t e = launch_paged_plan(a, p, scratch, st);
     if (e == cudaSuccess) {
         if (dtype == SLA_F32) {

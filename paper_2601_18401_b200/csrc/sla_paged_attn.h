@@ -7,7 +7,7 @@ namespace sla {
 
 // Tiles and scratch layout of one call (offsets in bytes from the scratch base).
 struct PagedPlan {
-    enum Kind { kRows } kind;
+    enum Kind { kRows, kDecode } kind;
     int R, RS, TS, TQ;      // rows of a unit, rows and tokens of its sub-tiles, tokens of the unit
     int kt_shift;           // log2 of the keys of a tile
     int n_ctas, max_groups, min_weight, max_units;
@@ -26,7 +26,14 @@ inline Parts parts_at(const PagedPlan &p, char *scratch) {
 PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count);
 cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scratch, cudaStream_t st);
 cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st);
-cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse,
-                                   cudaStream_t st, long long *launches);
+// counters: p.n_ctas ints, zero on entry and again on exit
+cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
+                                   float *lse, cudaStream_t st, long long *launches);
+
+// ---- one new token a sequence, bf16 (sla_paged_decode.cu)
+bool paged_decode_supported(const PagedCall &a, int dtype);
+void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count);
+cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out,
+                                          float *lse, cudaStream_t st, long long *launches);
 
 }  // namespace sla
