@@ -866,11 +866,15 @@ size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_
     a.c = make_pages(nullptr, c);
     a.Hq = n_q_heads;
     a.G = n_q_heads / c->n_kv_heads;
-    for (int32_t most : {1, n_new}) {   // the tiles go by the longest chunk
-        a.b = {n_seqs, n_new, most, nullptr, nullptr};
-        const size_t bytes = sla::plan_paged(a, c->dtype, 160).bytes;
-        if (bytes > need) need = bytes;
-    }
+    a.q_sh = c->head_dim;
+    a.q_st = (int64_t)n_q_heads * c->head_dim;
+    for (int32_t most : {1, n_new})         // the tiles go by the longest chunk,
+        for (float scale : {1.f, -1.f}) {   // and by the sign of the scale
+            a.b = {n_seqs, n_new, most, nullptr, nullptr};
+            a.scale = scale;
+            const size_t bytes = sla::plan_paged(a, c->dtype, 160).bytes;
+            if (bytes > need) need = bytes;
+        }
     if (p && n_seqs > 0) {
         const sla_layout_t l = layout_of(c, n_q_heads, n_seqs, c->head_dim * (int64_t)n_q_heads, c->head_dim);
         const size_t bytes = sla_workspace_bytes(&l, p, 1, (int64_t)c->table_width * c->page_tokens);

@@ -80,6 +80,7 @@ struct Plan {
     int max_units;        // room in unit_end
 };
 constexpr int kUnitWeight = 2;
+constexpr long long kGroupBytes = 48ll << 20;   // of keys and values that the CTAs go through at one time
 
 // Keys of the new tokens [t0, t1) of a sequence of n tokens, q of them new: tiles [lo, hi) of KT keys.
 __device__ __forceinline__ void unit_tiles(int n, int q, int t0, int t1, int window, int kt_shift, int &lo, int &hi) {
@@ -199,7 +200,7 @@ __device__ inline void build_plan(const PagedCall &a, int TQ, int kt_shift, int 
         long long bytes = 0;
         for (int w = 0; w < kWarps; ++w) bytes += s_sum[w];
         const long long total = plan.seq_at[a.b.n_seqs];
-        long long groups = (bytes + (48ll << 20) - 1) / (48ll << 20);
+        long long groups = (bytes + kGroupBytes - 1) / kGroupBytes;
         groups = groups < 1 ? 1 : groups > max_groups ? max_groups : groups;
         long long n = groups * n_ctas;
         if (n > total / min_weight) n = total / min_weight;   // a range of a few tiles at least

@@ -350,6 +350,9 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     if (paged_decode_supported(a, dtype)) {
         p.kind = PagedPlan::kDecode;
         plan_paged_decode(a, p, sm_count);
+    } else if (paged_tiles_supported(a, dtype)) {
+        p.kind = PagedPlan::kTiles;
+        plan_paged_tiles(a, p, sm_count);
     }
     const size_t ranges = (size_t)p.n_ctas * p.max_groups, units = (size_t)(a.b.n_new / p.TQ) + a.b.n_seqs + 1;
     p.max_units = (int)units;
@@ -374,7 +377,9 @@ cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype,
                                    float *lse, cudaStream_t st, long long *launches) {
     if (p.kind == PagedPlan::kDecode) return launch_paged_decode_attention(q, a, p, scratch, counters, out, lse, st, launches);
     cudaError_t e = launch_paged_plan(a, p, scratch, st);
-    if (e == cudaSuccess) {
+    if (e == cudaSuccess && p.kind == PagedPlan::kTiles) {
+        e = launch_paged_tiles(q, a, p, scratch, out, lse, st);
+    } else if (e == cudaSuccess) {
         if (dtype == SLA_F32) {
             if (a.c.D == 64) e = p.R == 16 ? run_rows<float, 64, 16>(q, a, p, scratch, out, lse, st) : run_rows<float, 64, 64>(q, a, p, scratch, out, lse, st);
             else e = p.R == 16 ? run_rows<float, 128, 16>(q, a, p, scratch, out, lse, st) : run_rows<float, 128, 64>(q, a, p, scratch, out, lse, st);

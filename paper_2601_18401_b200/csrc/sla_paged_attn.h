@@ -7,7 +7,7 @@ namespace sla {
 
 // Tiles and scratch layout of one call (offsets in bytes from the scratch base).
 struct PagedPlan {
-    enum Kind { kRows, kDecode } kind;
+    enum Kind { kRows, kDecode, kTiles } kind;
     int R, RS, TS, TQ;      // rows of a unit, rows and tokens of its sub-tiles, tokens of the unit
     int kt_shift;           // log2 of the keys of a tile
     int n_ctas, max_groups, min_weight, max_units;
@@ -35,5 +35,10 @@ bool paged_decode_supported(const PagedCall &a, int dtype);
 void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count);
 cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches);
+
+// ---- chunks of new tokens, bf16 (sla_paged_tiles.cu)
+bool paged_tiles_supported(const PagedCall &a, int dtype);
+void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count);
+cudaError_t launch_paged_tiles(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st);
 
 }  // namespace sla

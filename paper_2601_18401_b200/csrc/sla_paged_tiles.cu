@@ -1,0 +1,798 @@
+// Attention of chunks of new tokens over a paged cache, bf16: tcgen05 MMA with TMEM accumulators, pages by TMA.
+//
+// A unit is up to 256 rows of one (sequence, KV head): 256 / G neighbouring new tokens with all G heads of the group, as two
+// streams of 128 rows.  Per tile of 128 keys and stream
+//     S = Q K^T (smem x smem -> TMEM),   P = 2^(scale S - m) in registers, as bf16 back over S,   O += P V (TMEM x smem -> TMEM),
+// with a reference maximum m per row that moves only when a logit passes it by 2^8 (then O and the sum are rescaled); sums in
+// fp32.  While the row warps of one stream work on their S, the tensor pipe does the other's products.
+//
+// CTA of 512 threads, one per SM: warps 0-3 and 4-7 are the rows of the streams (a thread a row), 8-11 write results, 12 and 13
+// issue a stream's MMAs, 14 fetches K and V (a box per page into a ring shared by both streams), 15 goes through the
+// CTA's ranges of the plan (sla_paged.cuh), hands the segments on through a ring in shared memory and fetches their Q.
+// Shared memory: Q 2 x 32 KB, ring 5 x 32 KB (K and V tiles in turn).  TMEM: O of the streams in columns 0 and 128, S in 256 and 384.
+//
+// Values in masked places: a masked weight is 0, and 0 times NaN is NaN, so a value that some row must not see may not enter the
+// product unless it is finite.  Only the tiles at the edges of the mask hold such keys; there the row warps clear the values
+// beyond the sequence's end (a page's stale rest) and look at the others, and if one is not finite all rows of the segment are
+// computed again by themselves, each over the keys it sees (redo_row).
+//
+// Every wait on an mbarrier is bounded; when one runs out the CTA sets a status bit, drains and leaves.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <math_constants.h>
+#include <stddef.h>
+
+#include "sla_paged_attn.h"
+#include "sla_tc_ptx.cuh"
+
+namespace sla {
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kThreads = 512;
+constexpr int kRows = 128;          // of a stream
+constexpr int kKeys = 128;          // of a tile
+constexpr int kTileShift = 7;
+constexpr int kTmemCols = 512;
+constexpr uint32_t kColO = 0, kColS = 256;   // + 128 per stream
+constexpr int kSegs = 2;            // entries of the ring of segments
+constexpr float kRescaleThreshold = 8.f;     // log2 units
+constexpr int kRegsRow = 184, kRegsRest = 72;
+static_assert(2 * kRegsRow + 2 * kRegsRest <= 4 * 128, "more registers than the block is launched with");
+
+template <int D> struct Layout {
+    static constexpr int kHalves = D / 64;                  // 64-column halves of a tile, 128 rows x 128 B each
+    static constexpr int kTileBytes = kKeys * D * 2, kHalfBytes = kKeys * 128;
+    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int kOffQ = 0, kOffKV = 2 * kTileBytes, kOffMeta = kOffKV + kStages * kTileBytes;
+    static constexpr int kSmem = kOffMeta + 3072;
+};
+
+// What a segment is to the warps of the CTA.
+struct Seg {
+    int lo, hi, n, q;                 // tiles; tokens and new tokens of the sequence
+    int lo_x[2], hi_x[2];             // tiles of the streams
+    int t0, t1, row0, head;
+    int part, slot, valid, pad;
+};
+static_assert(sizeof(Seg) == 64, "four 16-byte words");
+
+struct Meta {
+    unsigned long long q_full[2], q_empty[2], kv_full[10], kv_empty[2][10], s_full[2], p_ready[2][2], l_full[2], o_full[2], o_empty[2],
+        seg_full[kSegs], seg_empty[kSegs], checked[2];
+    uint32_t tmem_base;
+    int abort_flag;
+    // [stream][segment & 7]: the segment (counted from 1) if it has a value that is not finite.  Whoever finds one says so to both
+    // streams before it clears the value; the ring of ten stages at most (a tile of K and of V each) keeps the streams less than eight segments with tiles apart.
+    int odd[2][8];
+    alignas(16) Seg seg[kSegs];
+    float2 stats[2][kRows];           // {1 / sum, log2-sum-exp} of the segment's rows
+    int redone[2];                    // the row warps have written the stream's results themselves
+};
+static_assert(sizeof(Meta) <= 3072, "meta block too large");
+
+struct TileParams {
+    PagedCall a;
+    Plan plan;
+    Parts parts;
+    const bf16 *q;
+    bf16 *out;
+    float *lse;
+    int TS;                           // tokens of a stream
+    int t_inner;                      // row i is token i % TS, head i / TS (else token i / G, head i % G), as Q's strides nest
+    int slot_t, slot_h, slot_p;       // (token, head, page) among the tensor-map coordinates 1..3 of K and V
+    int box_rows;                     // keys of a box: the smaller of a page and a tile
+};
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long pack2(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(unsigned long long r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ unsigned long long ffma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long fadd2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+    uint32_t y;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+    return y;
+}
+__device__ __forceinline__ uint64_t desc_advance(uint64_t desc, uint32_t bytes) {   // the address field, units of 16 bytes
+    uint32_t lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(desc));
+    lo += bytes >> 4;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(desc) : "r"(lo), "r"(hi));
+    return desc;
+}
+
+// One row of a segment by itself: keys [k0, k1), fp32 from global memory, values entering only with the keys the row sees.
+template <int D>
+__device__ __noinline__ void redo_row(const TileParams &p, const Seg &s, int x, int canon, int t, int g, int k0, int k1) {
+    const int h = s.head * p.a.G + g;
+    const long long row = s.row0 + t;
+    const bf16 *q = p.q + row * p.a.q_st + (long long)h * p.a.q_sh;
+    const int *table = p.a.c.table + (long long)max(s.slot, 0) * p.a.c.width;
+    auto at = [&](int j) {
+        return valid_page(p.a.c, table[j >> p.a.c.shift]) * p.a.c.s_page + s.head * p.a.c.s_h + (long long)(j & (p.a.c.P - 1)) * p.a.c.s_t;
+    };
+    auto logit = [&](int j) {
+        const bf16 *k = reinterpret_cast<const bf16 *>(p.a.c.k) + at(j);
+        float sum = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 8) {
+            float a[8], b[8];
+            Vec16<bf16>::load(q + d, a);
+            Vec16<bf16>::load(k + d, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(a[e], b[e], sum);
+        }
+        return sum * p.a.scale * kLog2e;
+    };
+    float m = -CUDART_INF_F, l = 0.f;
+#pragma unroll 1
+    for (int j = k0; j < k1; ++j) m = fmaxf(m, logit(j));
+    const float base = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll 1
+    for (int j = k0; j < k1; ++j) l += ex2_approx(logit(j) - base);
+    const bool none = l == 0.f && m == -CUDART_INF_F;
+    const float inv = none ? 0.f : 1.f / l, lse2 = none ? -CUDART_INF_F : m + log2f(l);
+#pragma unroll 1
+    for (int d0 = 0; d0 < D; d0 += 32) {
+        float acc[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) acc[e] = 0.f;
+#pragma unroll 1
+        for (int j = k0; j < k1; ++j) {
+            const float w = ex2_approx(logit(j) - base);
+            const bf16 *v = reinterpret_cast<const bf16 *>(p.a.c.v) + at(j) + d0;
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+                float b[8];
+                Vec16<bf16>::load(v + e, b);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) acc[e + u] = fmaf(w, b[u], acc[e + u]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float o = none ? 0.f : acc[e] * inv;
+            if (s.part < 0) p.out[row * p.a.q_st + (long long)h * p.a.q_sh + d0 + e] = __float2bfloat16_rn(o);
+            else p.parts.o[((long long)s.part * 256 + canon) * D + d0 + e] = o;
+        }
+    }
+    if (s.part < 0) p.lse[row * p.a.Hq + h] = lse2 * kLn2;
+    else p.parts.lse2[(long long)s.part * 256 + canon] = lse2;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+            const __grid_constant__ TileParams p) {
+    using L = Layout<D>;
+    constexpr int kStages = L::kStages, kHalves = L::kHalves;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t base = ptx::smem_u32(smem);
+    Meta *meta = reinterpret_cast<Meta *>(smem + L::kOffMeta);
+    volatile int *abort_flag = &meta->abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (base & 1023u) {   // the swizzled tiles need a 1024-byte aligned window: refuse rather than corrupt
+        if (tid == 0) atomicOr(p.a.c.status, kStatusTimeout);
+        return;
+    }
+    const uint32_t mbase = base + L::kOffMeta;
+    const uint32_t bar_q_full = mbase + offsetof(Meta, q_full), bar_q_empty = mbase + offsetof(Meta, q_empty);
+    const uint32_t bar_kv_full = mbase + offsetof(Meta, kv_full), bar_kv_empty = mbase + offsetof(Meta, kv_empty);
+    const uint32_t bar_s_full = mbase + offsetof(Meta, s_full), bar_p_ready = mbase + offsetof(Meta, p_ready);
+    const uint32_t bar_l_full = mbase + offsetof(Meta, l_full), bar_o_full = mbase + offsetof(Meta, o_full);
+    const uint32_t bar_o_empty = mbase + offsetof(Meta, o_empty), bar_checked = mbase + offsetof(Meta, checked);
+    const uint32_t bar_seg_full = mbase + offsetof(Meta, seg_full), bar_seg_empty = mbase + offsetof(Meta, seg_empty);
+
+    if (tid == 0) {
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+            ptx::mbar_init(bar_q_full + 8 * x, 1);
+            ptx::mbar_init(bar_q_empty + 8 * x, 1);
+            ptx::mbar_init(bar_s_full + 8 * x, 1);
+            ptx::mbar_init(bar_p_ready + 16 * x, 4);       // a row warp each
+            ptx::mbar_init(bar_p_ready + 16 * x + 8, 4);
+            ptx::mbar_init(bar_l_full + 8 * x, 4);
+            ptx::mbar_init(bar_checked + 8 * x, 4);
+            ptx::mbar_init(bar_o_full + 8 * x, 1);
+            ptx::mbar_init(bar_o_empty + 8 * x, 4);        // an epilogue warp each
+        }
+#pragma unroll 1
+        for (int s = 0; s < kStages; ++s) {
+            ptx::mbar_init(bar_kv_full + 8 * s, 1);
+            ptx::mbar_init(bar_kv_empty + 8 * s, 1);
+            ptx::mbar_init(bar_kv_empty + 80 + 8 * s, 1);
+        }
+#pragma unroll 1
+        for (int s = 0; s < kSegs; ++s) {
+            ptx::mbar_init(bar_seg_full + 8 * s, 1);
+            ptx::mbar_init(bar_seg_empty + 8 * s, 13 + 2 * 32);   // rows, epilogue, K/V: a warp each; the issuers a lane each
+        }
+        meta->abort_flag = 0;
+        for (int s = 0; s < 8; ++s) meta->odd[0][s] = meta->odd[1][s] = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 12) {
+        ptx::tmem_alloc(mbase + offsetof(Meta, tmem_base), kTmemCols);
+        ptx::tmem_relinquish();
+    }
+    chain_wait();      // the set-up above runs beside the kernel before this one
+    chain_release();
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = meta->tmem_base;
+    const int G = p.a.G, TS = p.TS;
+
+    // the CTA's k-th segment, for a whole warp
+    auto take_seg = [&](uint32_t k, Seg &s) {
+        if (!ptx::mbar_wait_warp(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag)) return false;
+        s = meta->seg[k % kSegs];
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
+        return s.valid != 0;
+    };
+
+    if (warp >= 12) {
+        ptx::setmaxnreg_dec<kRegsRest>();
+        if (warp < 14) {
+            // ---------------- MMA issuer of stream x: a whole warp, its elected lane issues.  S of the next tile goes right behind
+            // the PV of this one, which reads the P that lies over it (the tensor pipe keeps a thread's order).
+            const bool leader = ptx::elect_one();
+            const int x = warp - 12;
+            constexpr uint32_t kIdescS = ptx::idesc_bf16_f32(kRows, kKeys, false, false);   // both K-major
+            constexpr uint32_t kIdescO = ptx::idesc_bf16_f32(kRows, D, false, true);        // V is N-major
+            const uint32_t s_col = tmem + kColS + x * 128, o_col = tmem + kColO + x * 128;
+            const uint64_t dq = ptx::smem_desc_sw128(base + L::kOffQ + x * L::kTileBytes, 16, 1024);
+            const uint64_t dk0 = ptx::smem_desc_sw128(base + L::kOffKV, 16, 1024);
+            const uint64_t dv0 = ptx::smem_desc_sw128(base + L::kOffKV, L::kHalfBytes, 1024);
+            uint32_t i = 0, nt = 0, ns = 0;   // ring position; tiles and segments of the stream so far
+            bool ok = true;
+#pragma unroll 1
+            for (uint32_t k = 0; ok; ++k) {
+                if (!ptx::mbar_wait(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag)) break;
+                const Seg &s = meta->seg[k % kSegs];
+                const int lo = s.lo, hi = s.hi, lx = s.lo_x[x], hx = s.hi_x[x], valid = s.valid;
+                ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
+                if (!valid) break;
+#pragma unroll 1
+                for (int j = lo; j < hi; ++j) {
+                    const bool on = j >= lx && j < hx;
+                    uint32_t st = i % kStages;
+                    if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
+                    if (on) {
+                        if (j == lx && !(ok = ptx::mbar_wait(bar_q_full + 8 * x, ns & 1u, abort_flag))) break;
+                        ptx::tc_fence_after();
+                        const uint64_t dk = desc_advance(dk0, st * L::kTileBytes);
+                        if (leader) {
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const uint32_t off = (kk >> 2) * L::kHalfBytes + (kk & 3) * 32;
+                                ptx::mma_ss(s_col, desc_advance(dq, off), desc_advance(dk, off), kIdescS, kk > 0);
+                            }
+                            ptx::mma_commit(bar_s_full + 8 * x);
+                            ptx::mma_commit(bar_kv_empty + 80 * x + 8 * st);
+                            if (j == hx - 1) ptx::mma_commit(bar_q_empty + 8 * x);
+                        }
+                    } else if (leader) {
+                        ptx::mbar_arrive(bar_kv_empty + 80 * x + 8 * st);
+                    }
+                    ++i;
+                    st = i % kStages;
+                    if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
+                    if (on) {
+                        // the first PV of a segment overwrites O: the results of the segment before have been read
+                        if (j == lx && ns > 0 && !(ok = ptx::mbar_wait(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
+                        const uint64_t dv = desc_advance(dv0, st * L::kTileBytes);
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (!(ok = ptx::mbar_wait(bar_p_ready + 16 * x + 8 * half, nt & 1u, abort_flag))) break;
+                            ptx::tc_fence_after();
+                            if (leader) {
+#pragma unroll
+                                for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+                                    ptx::mma_ts(o_col, s_col + kk * 8, desc_advance(dv, kk * 2048), kIdescO, (j > lx || kk > 0) ? 1u : 0u);
+                            }
+                        }
+                        if (!ok) break;
+                        if (leader) {
+                            ptx::mma_commit(bar_kv_empty + 80 * x + 8 * st);
+                            if (j == hx - 1) ptx::mma_commit(bar_o_full + 8 * x);
+                        }
+                        ++nt;
+                    } else if (leader) {
+                        ptx::mbar_arrive(bar_kv_empty + 80 * x + 8 * st);
+                    }
+                    ++i;
+                }
+                ns += hx > lx;
+            }
+        } else if (warp == 14) {
+            // ---------------- K and V: a lane per box, as many as the tile has pages with tokens
+            ptx::prefetch_tensormap(&tm_k);
+            ptx::prefetch_tensormap(&tm_v);
+            const bool leader = ptx::elect_one();
+            const int boxes = kKeys / p.box_rows, shift = p.a.c.shift;
+            const uint32_t box_bytes = p.box_rows * 128;
+            uint32_t i = 0;
+            bool ok = true;
+            Seg s;
+#pragma unroll 1
+            for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
+                const int *table = p.a.c.table + (long long)max(s.slot, 0) * p.a.c.width;
+                auto key_of = [&](int j) { return j * kKeys + lane * p.box_rows; };
+                auto page_of = [&](int j) {   // -1: no box
+                    const int key = key_of(j);
+                    return j < s.hi && lane < boxes && key < s.n ? valid_page(p.a.c, __ldg(table + (key >> shift))) : -1;
+                };
+                int next = page_of(s.lo);
+#pragma unroll 1
+                for (int j = s.lo; j < s.hi && ok; ++j) {
+                    const int page = next;
+                    next = page_of(j + 1);
+                    int c[4];
+                    c[1 + p.slot_t] = key_of(j) & (p.a.c.P - 1);
+                    c[1 + p.slot_h] = s.head;
+                    c[1 + p.slot_p] = page;
+                    const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * box_bytes * kHalves;
+#pragma unroll 1
+                    for (int kv = 0; kv < 2; ++kv, ++i) {
+                        const uint32_t st = i % kStages, ph = ((i / kStages) & 1u) ^ 1u, full = bar_kv_full + 8 * st;
+                        ok = ptx::mbar_wait_warp(bar_kv_empty + 8 * st, ph, abort_flag) && ptx::mbar_wait_warp(bar_kv_empty + 80 + 8 * st, ph, abort_flag);
+                        if (!ok) break;
+                        if (leader) ptx::mbar_arrive_expect_tx(full, bytes);
+                        __syncwarp();
+                        if (page >= 0) {
+                            const uint32_t dst = base + L::kOffKV + st * L::kTileBytes + lane * box_bytes;
+                            const CUtensorMap *tm = kv ? &tm_v : &tm_k;
+                            ptx::tma_load_4d(dst, tm, full, 0, c[1], c[2], c[3]);
+                            if (kHalves == 2) ptx::tma_load_4d(dst + L::kHalfBytes, tm, full, 64, c[1], c[2], c[3]);
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+        } else {
+            // ---------------- the CTA's ranges, segment after segment, and their Q
+            ptx::prefetch_tensormap(&tm_q);
+            const bool leader = ptx::elect_one();
+            uint32_t k = 0, nq[2] = {0, 0};
+            bool ok = true;
+            auto put = [&](const Seg &s) {
+                ok = ptx::mbar_wait_warp(bar_seg_empty + 8 * (k % kSegs), ((k / kSegs) & 1u) ^ 1u, abort_flag);
+                if (ok && leader) {
+                    meta->seg[k % kSegs] = s;
+                    ptx::mbar_arrive(bar_seg_full + 8 * (k % kSegs));
+                }
+                __syncwarp();
+                ++k;
+            };
+            Seg s;
+            for (int range = blockIdx.x; ok; range += gridDim.x) {
+                Cursor cur;
+                Segment g;
+                int last_range;
+                int4 cut = make_int4(0, 0, 0, -1);
+                if (!cur.start(p.a, p.plan, range)) break;
+                while (ok && cur.next(p.a, p.plan, 2 * TS, kTileShift, g, last_range)) {
+                    if (last_range >= 0) cut = make_int4(g.x, g.head, g.unit, last_range);
+                    s.lo = g.lo; s.hi = g.hi; s.n = g.n; s.q = g.q;
+                    s.t0 = g.t0; s.t1 = g.t1; s.row0 = g.row0; s.head = g.head;
+                    s.part = g.part; s.slot = g.slot; s.valid = 1; s.pad = 0;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int a0 = min(g.t0 + x * TS, g.t1), a1 = min(a0 + TS, g.t1);
+                        int lo = 0, hi = 0;
+                        if (a1 > a0) unit_tiles(g.n, g.q, a0, a1, p.a.window, kTileShift, lo, hi);
+                        lo = max(lo, g.lo);
+                        hi = min(hi, g.hi);
+                        s.lo_x[x] = lo;
+                        s.hi_x[x] = max(lo, hi);
+                    }
+                    put(s);
+#pragma unroll 1
+                    for (int x = 0; x < 2 && ok; ++x) {
+                        if (s.hi_x[x] <= s.lo_x[x]) continue;
+                        ok = ptx::mbar_wait_warp(bar_q_empty + 8 * x, (nq[x] & 1u) ^ 1u, abort_flag);
+                        ++nq[x];
+                        if (!ok) break;
+                        if (leader) {
+                            const uint32_t full = bar_q_full + 8 * x, dst = base + L::kOffQ + x * L::kTileBytes;
+                            ptx::mbar_arrive_expect_tx(full, TS * G * 128 * kHalves);
+                            const int tok = g.row0 + g.t0 + x * TS, c1 = p.t_inner ? tok : g.head * G, c2 = p.t_inner ? g.head * G : tok;
+#pragma unroll
+                            for (int h = 0; h < kHalves; ++h) ptx::tma_load_4d(dst + h * L::kHalfBytes, &tm_q, full, 64 * h, c1, c2, 0);
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (leader) p.parts.cut[range] = cut;
+            }
+            s = Seg{};
+            if (ok) put(s);
+        }
+    } else if (warp >= 8) {
+        // ---------------- results: a thread a row
+        ptx::setmaxnreg_dec<kRegsRest>();
+        const int row = tid & 127;
+        const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G, canon = t * G + g;
+        const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        uint32_t ns[2] = {0, 0};
+        bool ok = true;
+        Seg s;
+#pragma unroll 1
+        for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
+#pragma unroll 1
+            for (int x = 0; x < 2 && ok; ++x) {
+                const int tok = s.t0 + x * TS + t;
+                const bool valid = t < TS && g < G && tok < s.t1, has = s.hi_x[x] > s.lo_x[x];
+                const int h = s.head * G + g;
+                const long long r = s.row0 + tok;
+                bf16 *dst = p.out + r * p.a.q_st + (long long)h * p.a.q_sh;
+                float *pdst = p.parts.o + ((long long)s.part * 256 + x * kRows + canon) * D;
+                float2 stat = make_float2(0.f, -CUDART_INF_F);
+                bool write = valid;
+                if (has) {
+                    ok = ptx::mbar_wait_warp(bar_l_full + 8 * x, ns[x] & 1u, abort_flag) && ptx::mbar_wait_warp(bar_o_full + 8 * x, ns[x] & 1u, abort_flag);
+                    if (!ok) break;
+                    ++ns[x];
+                    ptx::tc_fence_after();
+                    stat = meta->stats[x][row];
+                    write = valid && !meta->redone[x];
+                }
+                const bool none = stat.y == -CUDART_INF_F;
+                if (has) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        uint32_t o[32];
+                        ptx::tmem_ld32(lane_addr + kColO + x * 128 + c0, o);
+                        ptx::tmem_wait_ld();
+                        if (c0 == D - 32) {   // O is in registers: the next segment's first PV may overwrite it
+                            ptx::tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(bar_o_empty + 8 * x);
+                        }
+                        if (!write) continue;
+                        if (s.part < 0) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int u = 0; u < 4; ++u)
+                                    w[u] = none ? 0u : bf16x2(__uint_as_float(o[e + 2 * u]) * stat.x, __uint_as_float(o[e + 2 * u + 1]) * stat.x);
+                                *reinterpret_cast<uint4 *>(dst + c0 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                        } else if (!none) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<float4 *>(pdst + c0 + e) = make_float4(__uint_as_float(o[e]) * stat.x, __uint_as_float(o[e + 1]) * stat.x,
+                                                                                          __uint_as_float(o[e + 2]) * stat.x, __uint_as_float(o[e + 3]) * stat.x);
+                        }
+                    }
+                } else if (write && s.part < 0) {
+#pragma unroll 1
+                    for (int e = 0; e < D; e += 8) *reinterpret_cast<uint4 *>(dst + e) = make_uint4(0, 0, 0, 0);
+                }
+                if (write) {
+                    if (s.part < 0) p.lse[r * p.a.Hq + h] = stat.y * kLn2;
+                    else p.parts.lse2[(long long)s.part * 256 + x * kRows + canon] = stat.y;
+                }
+            }
+        }
+    } else {
+        // ---------------- rows of stream x: a thread a row
+        ptx::setmaxnreg_inc<kRegsRow>();
+        const int x = warp >> 2, row = tid & 127;
+        const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G, canon = t * G + g;
+        const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        const uint32_t o_addr = lane_addr + kColO + x * 128, s_col = lane_addr + kColS + x * 128;
+        const float scale2 = p.a.scale * kLog2e;
+        uint32_t nt = 0, ns = 0, tiles = 0;   // tiles and segments of the stream, tiles of the CTA so far
+        bool ok = true;
+        Seg s;
+#pragma unroll 1
+        for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
+            const int tok = s.t0 + x * TS + t;
+            const bool valid = t < TS && g < G && tok < s.t1;
+            const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 ? max(last - p.a.window + 1, 0) : 0;   // keys seen
+            // keys that not every row of the unit sees lie outside [all_lo, all_hi]
+            const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? s.n - s.q + s.t1 - p.a.window : 0;
+            const int lx = s.lo_x[x], hx = s.hi_x[x];
+            if (hx > lx) {
+                float m_ref = -CUDART_INF_F, l = 0.f;
+                bool fresh = true;   // no logit above -inf so far
+#pragma unroll 1
+                for (int j = lx; j < hx; ++j, ++nt) {
+                    const int k0 = j * kKeys;
+                    if (!(ok = ptx::mbar_wait_warp(bar_s_full + 8 * x, nt & 1u, abort_flag))) break;
+                    ptx::tc_fence_after();
+                    uint32_t sr[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) ptx::tmem_ld32(s_col + c * 32, sr[c]);
+                    ptx::tmem_wait_ld();
+                    if (k0 < first || k0 + kKeys - 1 > last) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int a = k0 + c * 32;   // bits [first - a, last - a] of the 32 columns
+                            const int lo = max(first - a, 0), hi = min(last - a, 31);
+                            const uint32_t inside = lo <= hi ? (0xffffffffu >> (31 - (hi - lo))) << lo : 0u;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(inside & (1u << e))) sr[c][e] = 0xff800000u;   // -inf
+                        }
+                    }
+                    float bm;   // (scale > 0)
+                    {
+                        float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8)
+#pragma unroll
+                                for (int u = 0; u < 4; ++u)
+                                    mx[u] = max3(mx[u], __uint_as_float(sr[c][e + 2 * u]), __uint_as_float(sr[c][e + 2 * u + 1]));
+                        bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale2;
+                    }
+                    const bool need = !fresh && bm > m_ref + kRescaleThreshold;
+                    if (__any_sync(0xffffffffu, need)) {
+                        // the PV of the tile before must have landed before O is touched
+                        const uint32_t v = 2 * (tiles + (j - s.lo) - 1u) + 1u;
+                        if (!(ok = ptx::mbar_wait_warp(bar_kv_empty + 80 * x + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
+                        ptx::tc_fence_after();
+                        const float f = need ? ex2_approx(m_ref - bm) : 1.f;
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            ptx::tmem_ld16(o_addr + c * 16, o);
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            ptx::tmem_st16(o_addr + c * 16, o);
+                        }
+                        if (need) {
+                            l *= f;
+                            m_ref = bm;
+                        }
+                    }
+                    if (fresh && bm > -CUDART_INF_F) {
+                        m_ref = bm;
+                        fresh = false;
+                    }
+                    const float neg_m = fresh ? 0.f : -m_ref;   // a row with no key so far: -inf stays -inf
+                    const unsigned long long sc2 = pack2(scale2, scale2), nm2 = pack2(neg_m, neg_m);
+                    unsigned long long acc2[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) acc2[u] = pack2(0.f, 0.f);
+                    const bool edge = k0 + kKeys - 1 > all_hi || k0 < all_lo;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int c = 2 * half + (e >> 4), c2 = (e & 15) * 2;
+                            float y0, y1;
+                            unpack2(ffma2(pack2(__uint_as_float(sr[c][c2]), __uint_as_float(sr[c][c2 + 1])), sc2, nm2), y0, y1);
+                            const float p0 = ex2_approx(y0), p1 = ex2_approx(y1);
+                            acc2[e & 3] = fadd2(acc2[e & 3], pack2(p0, p1));
+                            pk[e] = bf16x2(p0, p1);
+                        }
+                        ptx::tmem_st32(s_col + half * 32, pk);
+                        if (half == 0 && edge) {
+                            // this thread's key of the tile: beyond the sequence it is cleared, else looked at
+                            const uint32_t v = 2 * (tiles + (j - s.lo)) + 1u;
+                            if (!(ok = ptx::mbar_wait_warp(bar_kv_full + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
+                            const int key = k0 + row;
+                            uint4 *vr = reinterpret_cast<uint4 *>(smem + L::kOffKV + (v % kStages) * L::kTileBytes + row * 128);
+                            bool clear = key >= s.n;
+                            if (!clear && (key > all_hi || key < all_lo)) {
+                                uint32_t bad = 0;
+#pragma unroll
+                                for (int h = 0; h < kHalves; ++h)
+#pragma unroll 4
+                                    for (int c = 0; c < 8; ++c) {
+                                        const uint4 w = vr[h * (L::kHalfBytes / 16) + (c ^ (row & 7))];
+                                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                                        for (int u = 0; u < 4; ++u) bad |= ((ws[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // exponent all ones
+                                    }
+                                if (bad) {
+                                    clear = true;
+                                    *(volatile int *)&meta->odd[0][k & 7] = *(volatile int *)&meta->odd[1][k & 7] = (int)k + 1;
+                                    __threadfence_block();
+                                }
+                            }
+                            if (clear) {
+#pragma unroll
+                                for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                                    for (int c = 0; c < 8; ++c) vr[h * (L::kHalfBytes / 16) + c] = make_uint4(0, 0, 0, 0);
+                            }
+                            ptx::fence_proxy_async_smem();
+                        }
+                        ptx::tmem_wait_st();
+                        ptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(bar_p_ready + 16 * x + 8 * half);
+                    }
+                    if (!ok) break;
+                    float s0, s1, s2, s3;
+                    unpack2(fadd2(acc2[0], acc2[1]), s0, s1);
+                    unpack2(fadd2(acc2[2], acc2[3]), s2, s3);
+                    l += (s0 + s1) + (s2 + s3);
+                }
+                if (!ok) break;
+                // all four warps have looked at their keys
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
+                if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
+                const bool odd = *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1;
+                if (odd && valid)
+                    redo_row<D>(p, s, x, x * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
+                // the epilogue has read the statistics (and O) of the segment before
+                if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
+                ++ns;
+                const bool none = l == 0.f && fresh;   // (a row of NaN logits has a sum that is NaN)
+                meta->stats[x][row] = make_float2(none ? 0.f : 1.f / l, none ? -CUDART_INF_F : (fresh ? 0.f : m_ref) + log2f(l));
+                if ((warp & 3) == 0 && lane == 0) meta->redone[x] = odd;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar_l_full + 8 * x);
+            }
+            tiles += s.hi - s.lo;
+        }
+    }
+
+    // ---- teardown
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) atomicOr(p.a.c.status, kStatusTimeout);
+        __nanosleep(200000);   // let copies and MMAs that may still be in flight land
+        __syncthreads();
+    }
+    if (warp == 12) {
+        __syncwarp();
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    if (!fn) {
+        void *ptr = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+    }
+    return fn;
+}
+
+// The outer dimensions of a tensor in the order of their strides (bytes), those of size 1 last.  False when two overlap in memory:
+// such a layout is not a tiled tensor.
+struct Dim { unsigned long long size, stride; int which; };
+bool order_dims(Dim *d, int n, unsigned long long inner_bytes) {
+    for (int a = 0; a < n; ++a)
+        for (int b = a + 1; b < n; ++b) {
+            const bool swap = (d[b].size > 1 && d[a].size == 1) ? true : (d[a].size > 1 && d[b].size == 1) ? false : d[b].stride < d[a].stride;
+            if (swap) { const Dim t = d[a]; d[a] = d[b]; d[b] = t; }
+        }
+    unsigned long long extent = inner_bytes;
+    for (int a = 0; a < n; ++a) {
+        if (d[a].size == 1) d[a].stride = extent;
+        else if (d[a].stride < extent || d[a].stride >= (1ull << 40)) return false;
+        extent = d[a].stride * d[a].size;
+        if (extent >= (1ull << 46)) return false;
+    }
+    return true;
+}
+
+bool kv_dims(const PagedCall &a, Dim (&d)[3]) {
+    d[0] = {(unsigned long long)a.c.P, (unsigned long long)a.c.s_t * 2, 0};
+    d[1] = {(unsigned long long)a.c.Hkv, (unsigned long long)a.c.s_h * 2, 1};
+    d[2] = {(unsigned long long)a.c.n_pages, (unsigned long long)a.c.s_page * 2, 2};
+    return order_dims(d, 3, (unsigned long long)a.c.D * 2);
+}
+bool q_dims(const PagedCall &a, Dim (&d)[2]) {
+    d[0] = {(unsigned long long)a.Hq, (unsigned long long)a.q_sh * 2, 0};
+    d[1] = {(unsigned long long)a.b.n_new, (unsigned long long)a.q_st * 2, 1};
+    return order_dims(d, 2, (unsigned long long)a.c.D * 2);
+}
+
+bool make_map(CUtensorMap *tm, const void *ptr, int D, const Dim *d, int n, const cuuint32_t *box_outer) {
+    auto fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t gdim[4] = {(cuuint64_t)D, 1, 1, 1}, gstr[3];
+    cuuint32_t box[4] = {64, 1, 1, 1}, estr[4] = {1, 1, 1, 1};
+    for (int a = 0; a < 3; ++a) {
+        gdim[1 + a] = a < n ? d[a].size : 1;
+        gstr[a] = a < n ? d[a].stride : d[n - 1].stride * d[n - 1].size;
+        box[1 + a] = a < n ? box_outer[a] : 1;
+    }
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(ptr), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, char *scratch, void *out, float *lse, cudaStream_t st) {
+    static bool allowed[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev]) {
+        e = cudaFuncSetAttribute(paged_tiles<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev] = true;
+    }
+    TileParams p;
+    p.a = a;
+    p.plan = plan_at(pl, scratch);
+    p.parts = parts_at(pl, scratch);
+    p.q = (const bf16 *)q;
+    p.out = (bf16 *)out;
+    p.lse = lse;
+    p.TS = pl.TS;
+    p.box_rows = a.c.P < kKeys ? a.c.P : kKeys;
+    Dim kd[3], qd[2];
+    if (!kv_dims(a, kd) || !q_dims(a, qd)) return cudaErrorInvalidValue;
+    int *slot[3] = {&p.slot_t, &p.slot_h, &p.slot_p};
+    cuuint32_t kbox[3] = {1, 1, 1}, qbox[2];
+    for (int i = 0; i < 3; ++i) {
+        *slot[kd[i].which] = i;
+        if (kd[i].which == 0) kbox[i] = p.box_rows;
+    }
+    p.t_inner = qd[0].which == 1;
+    for (int i = 0; i < 2; ++i) qbox[i] = qd[i].which == 1 ? pl.TS : a.G;
+    CUtensorMap tq, tk, tv;
+    if (!make_map(&tq, q, D, qd, 2, qbox) || !make_map(&tk, a.c.k, D, kd, 3, kbox) || !make_map(&tv, a.c.v, D, kd, 3, kbox))
+        return cudaErrorInvalidValue;
+    return launch_chained(paged_tiles<D>, dim3(pl.n_ctas), dim3(kThreads), Layout<D>::kSmem, st, tq, tk, tv, p);
+}
+
+}  // namespace
+
+// bf16, strides that nest in memory (no broadcast views), a scale that keeps the order of the logits and -inf what it is
+bool paged_tiles_supported(const PagedCall &a, int dtype) {
+    Dim kd[3], qd[2];
+    return dtype == SLA_BF16 && a.scale > 0.f && kv_dims(a, kd) && q_dims(a, qd);
+}
+
+void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
+    p.R = 2 * kRows;
+    p.RS = kRows;
+    p.TS = kRows / a.G;
+    p.TQ = 2 * p.TS;
+    p.kt_shift = kTileShift;
+    p.n_ctas = sm_count;
+    // more ranges than CTAs only where the keys that several units read may not fit L2 (see build_plan)
+    const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * a.c.D * a.c.es * 2, groups = (bytes + kGroupBytes - 1) / kGroupBytes;
+    p.max_groups = groups < 8 ? (int)groups : 8;
+    p.min_weight = 6;
+}
+
+cudaError_t launch_paged_tiles(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
+    return a.c.D == 64 ? tiles_of<64>(q, a, p, scratch, out, lse, st) : tiles_of<128>(q, a, p, scratch, out, lse, st);
+}
+
+}  // namespace sla
