@@ -211,7 +211,8 @@ def make_layout(q: torch.Tensor, k: torch.Tensor, decode: bool = False) -> sla_l
 
 def _stream_ptr(stream) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the raw handle of torch.cuda.current_stream(), without the object around it (0.3 us a call instead of 3.3)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(stream.cuda_stream)
 
 

@@ -80,6 +80,11 @@ struct Plan {
     int max_units;        // room in unit_end
 };
 constexpr int kUnitWeight = 2;
+// How a kernel cuts a call up: TQ new tokens a unit, tiles of 1 << kt_shift keys.  Units of at most `small` tokens go through two tiles at
+// a time (sla_paged_tiles.cu): their tiles weigh half.
+struct Shape {
+    int TQ, kt_shift, small;
+};
 constexpr long long kGroupBytes = 48ll << 20;   // of keys and values that the CTAs go through at one time
 
 // Keys of the new tokens [t0, t1) of a sequence of n tokens, q of them new: tiles [lo, hi) of KT keys.
@@ -90,12 +95,17 @@ __device__ __forceinline__ void unit_tiles(int n, int q, int t0, int t1, int win
     hi = end > 0 ? (end + (1 << kt_shift) - 1) >> kt_shift : lo;
     if (hi < lo) hi = lo;
 }
+__device__ __forceinline__ int unit_weight(int n, int q, int t0, int t1, int window, const Shape &f) {
+    int lo, hi;
+    unit_tiles(n, q, t0, t1, window, f.kt_shift, lo, hi);
+    return (t1 - t0 <= f.small ? (hi - lo + 1) >> 1 : hi - lo) + kUnitWeight;
+}
 
-// A CTA builds the plan (all threads call it; the arrays are visible to the CTA on return).  TQ: tokens of a unit.
+// A CTA builds the plan (all threads call it; the arrays are visible to the CTA on return).
 // `groups`: the ranges are a multiple of n_ctas when the list is long, so that CTAs work on neighbouring units at any time
 // and share what they read in L2.
 template <int kThreads>
-__device__ inline void build_plan(const PagedCall &a, int TQ, int kt_shift, int n_ctas, int max_groups, int min_weight, const Plan &plan,
+__device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas, int max_groups, int min_weight, const Plan &plan,
                                   long long *s_sum) {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -109,7 +119,7 @@ __device__ inline void build_plan(const PagedCall &a, int TQ, int kt_shift, int 
             if (x < a.b.n_seqs) {
                 int lo, hi;
                 new_rows(a.b, x, lo, hi);
-                units = (hi - lo + TQ - 1) / TQ;
+                units = (hi - lo + f.TQ - 1) / f.TQ;
             }
             long long all = units;
 #pragma unroll
@@ -146,9 +156,7 @@ __device__ inline void build_plan(const PagedCall &a, int TQ, int kt_shift, int 
         }
         long long total = 0;
         if (units == 1) {
-            int lo, hi;
-            unit_tiles(n, q, 0, q, a.window, kt_shift, lo, hi);
-            total = hi - lo + kUnitWeight;
+            total = unit_weight(n, q, 0, q, a.window, f);
             plan.unit_end[plan.unit_at[x]] = total;
         }
         for (unsigned many = __ballot_sync(full, units > 1); many; many &= many - 1) {
@@ -158,9 +166,7 @@ __device__ inline void build_plan(const PagedCall &a, int TQ, int kt_shift, int 
             long long sum = 0;
             for (int u0 = 0; u0 < u_n; u0 += 32) {
                 const int u = u0 + lane;
-                int lo, hi;
-                unit_tiles(ns, qs, u * TQ, min((u + 1) * TQ, qs), a.window, kt_shift, lo, hi);
-                long long v = u < u_n ? hi - lo + kUnitWeight : 0;
+                long long v = u < u_n ? unit_weight(ns, qs, u * f.TQ, min((u + 1) * f.TQ, qs), a.window, f) : 0;
 #pragma unroll
                 for (int off = 1; off < 32; off <<= 1) {
                     const long long y = __shfl_up_sync(full, v, off);
@@ -260,7 +266,7 @@ struct Cursor {
     }
     // the segment at the cursor; false when the range is done.  *last_range: for a unit that starts in this range and does not
     // end in it, the range it ends in, else -1.
-    __device__ __forceinline__ bool next(const PagedCall &a, const Plan &plan, int TQ, int kt_shift, Segment &s, int &last_range) {
+    __device__ __forceinline__ bool next(const PagedCall &a, const Plan &plan, const Shape &f, Segment &s, int &last_range) {
         last_range = -1;
         if (w >= end) return false;
         if (unit == units) {
@@ -282,13 +288,14 @@ struct Cursor {
         int r1;
         new_rows(a.b, x, s.row0, r1);
         s.q = r1 - s.row0;
-        s.t0 = unit * TQ;
-        s.t1 = min(s.t0 + TQ, s.q);
+        s.t0 = unit * f.TQ;
+        s.t1 = min(s.t0 + f.TQ, s.q);
         int lo, hi;
-        unit_tiles(s.n, s.q, s.t0, s.t1, a.window, kt_shift, lo, hi);
+        unit_tiles(s.n, s.q, s.t0, s.t1, a.window, f.kt_shift, lo, hi);
+        const int per = s.t1 - s.t0 <= f.small ? 2 : 1;   // tiles of a weight
         const int from = (int)(w - start), to = (int)((end < stop ? end : stop) - start);   // weights of the unit in this range
-        s.lo = lo + max(from - kUnitWeight, 0);
-        s.hi = lo + max(to - kUnitWeight, 0);
+        s.lo = min(lo + per * max(from - kUnitWeight, 0), hi);
+        s.hi = min(lo + per * max(to - kUnitWeight, 0), hi);
         const bool begins = from == 0, ends = end >= stop;
         s.part = begins && ends ? -1 : begins ? 2 * r + 1 : 2 * r;
         if (begins && !ends) {
@@ -304,11 +311,15 @@ struct Cursor {
     }
 };
 
+// The unit that starts in a range and ends in the range `last` (-1 where none does): its first row, tokens and KV head.
+struct alignas(16) Cut {
+    int row0, tokens, head, last;
+};
 // Partial results: part p of a unit of R rows has its normalised sums at o + p * R * D and its log2-sum-exp at lse2 + p * R (-inf: no
-// keys; the sums are then not written).  cut[r]: the unit that starts in range r and ends in range cut[r].w, -1 where none does.
+// keys; the sums are then not written).
 struct Parts {
     float *o, *lse2;
-    int4 *cut;            // {sequence, head, unit, last range}
+    Cut *cut;             // [ranges]
 };
 
 }  // namespace sla

@@ -18,12 +18,11 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 
-__global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, int TQ, int kt_shift, int n_ctas, int max_groups, int min_weight,
-                                                           Plan plan) {
+__global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f, int n_ctas, int max_groups, int min_weight, Plan plan) {
     __shared__ long long s_sum[kPlanThreads / 32];
     chain_wait();
     chain_release();
-    build_plan<kPlanThreads>(a, TQ, kt_shift, n_ctas, max_groups, min_weight, plan, s_sum);
+    build_plan<kPlanThreads>(a, f, n_ctas, max_groups, min_weight, plan, s_sum);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -52,10 +51,10 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
         Cursor cur;
         Segment s;
         int last_range;
-        int4 cut = make_int4(0, 0, 0, -1);
+        Cut cut = {0, 0, 0, -1};
         if (!cur.start(a, plan, range)) break;
-        while (cur.next(a, plan, TQ, kShift, s, last_range)) {
-            if (last_range >= 0) cut = make_int4(s.x, s.head, s.unit, last_range);
+        while (cur.next(a, plan, Shape{TQ, kShift, 0}, s, last_range)) {
+            if (last_range >= 0) cut = {s.row0 + s.t0, s.t1 - s.t0, s.head, last_range};
             const int rows = (s.t1 - s.t0) * G;
             __syncthreads();   // the tiles of the segment before have been read
             constexpr int E = Vec16<T>::kElems;
@@ -219,83 +218,91 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
 }
 
 // ------------------------------------------------------------------------------------------------
-// blockIdx.x: the range a cut unit starts in; the CTA's 8 warps take blockIdx.y * (8 / WPR) rows at a time, WPR warps a row (few
-// rows with many parts: several).  RS rows of TS tokens make a sub-tile of the unit.
-template <typename T, int D, int WPR>
-__global__ void __launch_bounds__(256) paged_merge(PagedCall a, int R, int RS, int TS, int TQ, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
-    constexpr int N = D / 32;
-    __shared__ float s_sum[8], s_o[8][D];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % WPR;
+// blockIdx.x: the range a cut unit starts in.  A warp takes kMergeRows rows at a time, blockIdx.y and the warp saying which, and requests
+// two parts of each together: bound by the latency of two dependent loads where units have few parts.  Row i of a unit is token
+// i / G of sub-tile i / RS (TS tokens each).
+constexpr int kMergeRows = 4;
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 2) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
+    constexpr int N = D / 32, kParts = 2;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     chain_wait();
     const int n_ranges = *plan.n_ranges;
-    for (int r = blockIdx.x; r < n_ranges; r += gridDim.x) {
-        const int4 cut = parts.cut[r];
-        if (cut.w < 0) continue;
-        int row0, row1;
-        new_rows(a.b, cut.x, row0, row1);
-        const int t0 = cut.z * TQ, t1 = min(t0 + TQ, row1 - row0), n_parts = cut.w - r + 1;
-        for (int i0 = blockIdx.y * (8 / WPR); i0 < R; i0 += gridDim.y * (8 / WPR)) {
-            const int i = i0 + warp / WPR, in = i % RS, t = t0 + i / RS * TS + in / a.G, g = in % a.G;
-            const bool on = in < TS * a.G && t < t1;
-            auto part_at = [&](int e) { return (long long)(e == 0 ? 2 * r + 1 : 2 * (r + e)) * R + i; };
-            float mx = -CUDART_INF_F, sum = 0.f, acc[N];
+    Cut cut = parts.cut[blockIdx.x];   // (beyond n_ranges: not looked at)
+    for (int r = blockIdx.x; r < n_ranges;) {
+        const int n_parts = cut.last - r + 1;
+        const int rows = cut.last < 0 ? 0 : R;
+        for (int i0 = (blockIdx.y * 8 + warp) * kMergeRows; i0 < rows; i0 += gridDim.y * 8 * kMergeRows) {
+            int t[kMergeRows], h[kMergeRows];
+            bool on[kMergeRows], any = false;
+            float mx[kMergeRows], sum[kMergeRows], acc[kMergeRows][N];
 #pragma unroll
-            for (int d = 0; d < N; ++d) acc[d] = 0.f;
-            if (on) {
-                for (int e = lane; e < n_parts; e += 32) {
-                    const float z = __ldcg(parts.lse2 + part_at(e));
-                    mx = fmaxf(mx, z);   // a NaN reaches the result through its weight
-                }
+            for (int u = 0; u < kMergeRows; ++u) {
+                const int i = i0 + u, in = i % RS;
+                t[u] = i / RS * TS + in / a.G;
+                h[u] = cut.head * a.G + in % a.G;
+                on[u] = in < TS * a.G && t[u] < cut.tokens;
+                any |= on[u];
+                mx[u] = -CUDART_INF_F;
+                sum[u] = 0.f;
 #pragma unroll
-                for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-                for (int e0 = sub; e0 < n_parts; e0 += 4 * WPR) {
-                    float z[4], v[4][N];
+                for (int d = 0; d < N; ++d) acc[u][d] = 0.f;
+            }
+            if (!any) continue;
+            for (int e0 = 0; e0 < n_parts; e0 += kParts) {
+                float z[kMergeRows][kParts], v[kMergeRows][kParts][N];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int e = e0 + u * WPR;
-                        z[u] = e < n_parts ? __ldcg(parts.lse2 + part_at(e)) : -CUDART_INF_F;
+                for (int u = 0; u < kMergeRows; ++u)
 #pragma unroll
-                        for (int d = 0; d < N; ++d) v[u][d] = 0.f;
-                        if (z[u] != -CUDART_INF_F) {
-                            const float *src = parts.o + part_at(e) * D + lane * N;
-                            if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldcg(reinterpret_cast<const float4 *>(src));
-                            else *reinterpret_cast<float2 *>(v[u]) = __ldcg(reinterpret_cast<const float2 *>(src));
-                        }
+                    for (int e = 0; e < kParts; ++e) {
+                        // (a part that is not there: the first one's place, without a weight; of a part without keys the sums
+                        // were not written, and are not used)
+                        const int part = e0 + e == 0 || e0 + e >= n_parts ? 2 * r + 1 : 2 * (r + e0 + e);
+                        const long long at = (long long)part * R + i0 + u;
+                        z[u][e] = __ldcg(parts.lse2 + at);
+                        const float *src = parts.o + at * D + lane * N;
+                        if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u][e]) = __ldcg(reinterpret_cast<const float4 *>(src));
+                        else *reinterpret_cast<float2 *>(v[u][e]) = __ldcg(reinterpret_cast<const float2 *>(src));
+                        if (e0 + e >= n_parts) z[u][e] = -CUDART_INF_F;
                     }
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if (z[u] == -CUDART_INF_F) continue;
-                        const float w = exp2f(z[u] - mx);
-                        sum += w;
+                for (int u = 0; u < kMergeRows; ++u) {
+                    float top = mx[u];   // a NaN reaches the result through its weight
 #pragma unroll
-                        for (int d = 0; d < N; ++d) acc[d] = fmaf(w, v[u][d], acc[d]);
+                    for (int e = 0; e < kParts; ++e) top = fmaxf(top, z[u][e]);
+                    const float keep = mx[u] == top ? 1.f : exp2f(mx[u] - top);
+                    mx[u] = top;
+                    sum[u] *= keep;
+#pragma unroll
+                    for (int d = 0; d < N; ++d) acc[u][d] *= keep;
+#pragma unroll
+                    for (int e = 0; e < kParts; ++e) {
+                        if (z[u][e] == -CUDART_INF_F) continue;
+                        const float w = exp2f(z[u][e] - top);
+                        sum[u] += w;
+#pragma unroll
+                        for (int d = 0; d < N; ++d) acc[u][d] = fmaf(w, v[u][e][d], acc[u][d]);
                     }
                 }
             }
-            if constexpr (WPR > 1) {
-                __syncthreads();
-                if (lane == 0) s_sum[warp] = sum;
 #pragma unroll
-                for (int d = 0; d < N; ++d) s_o[warp][lane * N + d] = acc[d];
-                __syncthreads();
-                if (sub != 0) continue;
-#pragma unroll 1
-                for (int w = 1; w < WPR; ++w) {
-                    sum += s_sum[warp + w];
+            for (int u = 0; u < kMergeRows; ++u) {
+                if (!on[u]) continue;
+                const bool none = mx[u] == -CUDART_INF_F && sum[u] == 0.f;
+                const float inv = none ? 0.f : 1.f / sum[u];
+                const long long row = cut.row0 + t[u];
+                T *o = out + row * a.q_st + (long long)h[u] * a.q_sh + lane * N;
+                alignas(16) T w[N];
 #pragma unroll
-                    for (int d = 0; d < N; ++d) acc[d] += s_o[warp + w][lane * N + d];
-                }
+                for (int d = 0; d < N; ++d) w[d] = from_float<T>(acc[u][d] * inv);
+                if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<const uint4 *>(w);
+                else if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<const uint2 *>(w);
+                else *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<const uint32_t *>(w);
+                if (lane == 0) lse[row * a.Hq + h[u]] = none ? -CUDART_INF_F : (mx[u] + log2f(sum[u])) * kLn2;
             }
-            if (!on) continue;
-            const bool none = mx == -CUDART_INF_F && sum == 0.f;
-            const float inv = none ? 0.f : 1.f / sum;
-            const long long row = row0 + t;
-            const int h = cut.y * a.G + g;
-            T *o = out + row * a.q_st + (long long)h * a.q_sh + lane * N;
-#pragma unroll
-            for (int d = 0; d < N; ++d) o[d] = from_float<T>(acc[d] * inv);
-            if (lane == 0) lse[row * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
         }
+        r += gridDim.x;
+        if (r < n_ranges) cut = parts.cut[r];
     }
 }
 
@@ -317,17 +324,14 @@ cudaError_t run_rows(const void *q, const PagedCall &a, const PagedPlan &p, char
 }  // namespace
 
 cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scratch, cudaStream_t st) {
-    return launch_chained(paged_plan, dim3(1), dim3(kPlanThreads), 0, st, a, p.TQ, p.kt_shift, p.n_ctas, p.max_groups, p.min_weight,
+    return launch_chained(paged_plan, dim3(1), dim3(kPlanThreads), 0, st, a, Shape{p.TQ, p.kt_shift, p.small}, p.n_ctas, p.max_groups, p.min_weight,
                           plan_at(p, scratch));
 }
 
 template <typename T, int D>
 static cudaError_t merge_of(const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
-    // one row of eight warps, or rows of one
-    if (p.R <= 16)
-        return launch_chained(paged_merge<T, D, 8>, dim3(p.n_ctas, p.R), dim3(256), 0, st, a, p.R, p.RS, p.TS, p.TQ, plan_at(p, scratch),
-                              parts_at(p, scratch), (T *)out, lse);
-    return launch_chained(paged_merge<T, D, 1>, dim3(p.n_ctas, p.R / 32), dim3(256), 0, st, a, p.R, p.RS, p.TS, p.TQ, plan_at(p, scratch),
+    const int per = 8 * kMergeRows;
+    return launch_chained(paged_merge<T, D>, dim3(p.n_ctas, (p.R + per - 1) / per), dim3(256), 0, st, a, p.R, p.RS, p.TS, plan_at(p, scratch),
                           parts_at(p, scratch), (T *)out, lse);
 }
 
@@ -347,6 +351,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.n_ctas = 2 * sm_count;
     p.max_groups = 1;
     p.min_weight = 4;
+    p.small = 0;
     if (paged_decode_supported(a, dtype)) {
         p.kind = PagedPlan::kDecode;
         plan_paged_decode(a, p, sm_count);
@@ -366,7 +371,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.off_unit_at = take((size_t)(a.b.n_seqs + 1) * 4);
     p.off_unit_end = take(units * 8);
     p.off_n_ranges = take(4);
-    p.off_cut = take(ranges * sizeof(int4));
+    p.off_cut = take(ranges * sizeof(Cut));
     p.off_lse2 = take(2 * ranges * p.R * 4);
     p.off_o = take(2 * ranges * p.R * a.c.D * 4);
     p.bytes = off;

@@ -10,6 +10,7 @@ struct PagedPlan {
     enum Kind { kRows, kDecode, kTiles } kind;
     int R, RS, TS, TQ;      // rows of a unit, rows and tokens of its sub-tiles, tokens of the unit
     int kt_shift;           // log2 of the keys of a tile
+    int small;              // tokens of a unit whose tiles weigh half
     int n_ctas, max_groups, min_weight, max_units;
     size_t off_seq_at, off_unit_at, off_unit_end, off_n_ranges, off_cut, off_lse2, off_o, bytes;
 };
@@ -20,7 +21,7 @@ inline Plan plan_at(const PagedPlan &p, char *scratch) {
 }
 inline Parts parts_at(const PagedPlan &p, char *scratch) {
     return {reinterpret_cast<float *>(scratch + p.off_o), reinterpret_cast<float *>(scratch + p.off_lse2),
-            reinterpret_cast<int4 *>(scratch + p.off_cut)};
+            reinterpret_cast<Cut *>(scratch + p.off_cut)};
 }
 
 PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count);

@@ -28,7 +28,7 @@ constexpr int kThreads = 128, kWarps = kThreads / 32;
 __host__ __device__ constexpr int ctas_per_sm(int D, int NT) { return D == 128 && NT == 2 ? 2 : 3; }
 constexpr int kMaxSeqs = 1024;        // of a launch
 constexpr int kTileShift = 6;         // weights count 64 keys
-constexpr int kMinWeight = 4;         // of a range
+constexpr int kMinWeight = 2;         // of a range
 
 __device__ __forceinline__ uint4 load_stream(const void *p) {
     uint4 v;
@@ -333,25 +333,26 @@ paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n
             if (s_last) {
                 __threadfence();
                 auto part_at = [&](int e) { return (long long)(e == 0 ? 2 * r0 + 1 : 2 * (r0 + e)) * R; };
-                constexpr int kLanes = D / 4, kSplit = kThreads / kLanes;   // threads of a row; rows, or shares of a row's parts, at a time
-                // every group of kLanes threads takes a share of each row's parts, then the groups' sums are added up in order
-                const int grp = tid / kLanes, d = (tid % kLanes) * 4;
-                float *s_sum = &s_m[0][0];
-                for (int qi = 0; qi < G; ++qi) {
-                    float mx = -CUDART_INF_F;
-                    for (int e = lane; e < n_parts; e += 32) mx = fmaxf(mx, __ldcg(parts.lse2 + part_at(e) + qi));
-#pragma unroll
-                    for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-                    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (int e0 = grp; e0 < n_parts; e0 += 8 * kSplit) {
-                        float z[8];
+                for (int it = tid; it < G * (D / 4); it += kThreads) {
+                    const int qi = it / (D / 4), d = (it % (D / 4)) * 4;
+                    float mx = -CUDART_INF_F, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int e0 = 0; e0 < n_parts; e0 += 8) {
+                        float z[8], top = mx;
                         float4 v[8];
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
-                            const int e = e0 + u * kSplit;
-                            z[u] = e < n_parts ? __ldcg(parts.lse2 + part_at(e) + qi) : -CUDART_INF_F;
-                            v[u] = e < n_parts ? __ldcg(reinterpret_cast<const float4 *>(parts.o + (part_at(e) + qi) * D + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            z[u] = -CUDART_INF_F;
+                            if (e0 + u < n_parts) {
+                                z[u] = __ldcg(parts.lse2 + part_at(e0 + u) + qi);
+                                v[u] = __ldcg(reinterpret_cast<const float4 *>(parts.o + (part_at(e0 + u) + qi) * D + d));
+                            }
+                            top = fmaxf(top, z[u]);
                         }
+                        const float keep = mx == top ? 1.f : exp2_fast(mx - top);
+                        mx = top;
+                        sum *= keep;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] *= keep;
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
                             if (z[u] == -CUDART_INF_F) continue;   // nothing was written
@@ -360,24 +361,12 @@ paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n
                             o[0] = fmaf(wt, v[u].x, o[0]); o[1] = fmaf(wt, v[u].y, o[1]); o[2] = fmaf(wt, v[u].z, o[2]); o[3] = fmaf(wt, v[u].w, o[3]);
                         }
                     }
-                    __syncthreads();
-                    if (d == 0) s_sum[grp] = sum;
-                    *reinterpret_cast<float4 *>(&s_o[0][0][0] + grp * D + d) = make_float4(o[0], o[1], o[2], o[3]);
-                    __syncthreads();
-                    if (grp == 0) {
-#pragma unroll
-                        for (int v = 1; v < kSplit; ++v) {
-                            const float4 ov = *reinterpret_cast<const float4 *>(&s_o[0][0][0] + v * D + d);
-                            sum += s_sum[v];
-                            o[0] += ov.x; o[1] += ov.y; o[2] += ov.z; o[3] += ov.w;
-                        }
-                        const bool none = mx == -CUDART_INF_F && sum == 0.f;
-                        const float inv = none ? 0.f : 1.f / sum;
-                        const int h = head * G + qi;
-                        *reinterpret_cast<uint2 *>(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d) =
-                            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-                        if (d == 0) lse[(long long)row_q * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
-                    }
+                    const bool none = mx == -CUDART_INF_F && sum == 0.f;
+                    const float inv = none ? 0.f : 1.f / sum;
+                    const int h = head * G + qi;
+                    *reinterpret_cast<uint2 *>(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d) =
+                        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+                    if (d == 0) lse[(long long)row_q * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
                 }
             }
         }

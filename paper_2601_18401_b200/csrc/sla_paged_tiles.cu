@@ -11,6 +11,9 @@
 // CTA's ranges of the plan (sla_paged.cuh), hands the segments on through a ring in shared memory and fetches their Q.
 // Shared memory: Q 2 x 32 KB, ring 5 x 32 KB (K and V tiles in turn).  TMEM: O of the streams in columns 0 and 128, S in 256 and 384.
 //
+// A unit of one stream's rows or fewer -- the end of a chunk, a few tokens of a batch -- goes through both streams all the same, every
+// second tile each, and the two sums are joined where the results are written: its tiles take half the time.
+//
 // Values in masked places: a masked weight is 0, and 0 times NaN is NaN, so a value that some row must not see may not enter the
 // product unless it is finite.  Only the tiles at the edges of the mask hold such keys; there the row warps clear the values
 // beyond the sequence's end (a page's stale rest) and look at the others, and if one is not finite all rows of the segment are
@@ -39,6 +42,7 @@ constexpr int kTmemCols = 512;
 constexpr uint32_t kColO = 0, kColS = 256;   // + 128 per stream
 constexpr int kSegs = 2;            // entries of the ring of segments
 constexpr float kRescaleThreshold = 8.f;     // log2 units
+constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns, those whose exponentials go to the FMA pipe
 constexpr int kRegsRow = 184, kRegsRest = 72;
 static_assert(2 * kRegsRow + 2 * kRegsRest <= 4 * 128, "more registers than the block is launched with");
 
@@ -55,7 +59,8 @@ struct Seg {
     int lo, hi, n, q;                 // tiles; tokens and new tokens of the sequence
     int lo_x[2], hi_x[2];             // tiles of the streams
     int t0, t1, row0, head;
-    int part, slot, valid, pad;
+    int part, slot, valid;
+    int step;                         // 2: both streams have the unit's rows, of at most one stream, and every second tile each
 };
 static_assert(sizeof(Seg) == 64, "four 16-byte words");
 
@@ -86,9 +91,9 @@ struct TileParams {
     int box_rows;                     // keys of a box: the smaller of a page and a tile
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
+__device__ __forceinline__ float max3(float a, float b, float c) {   // NaN where one of them is
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 __device__ __forceinline__ unsigned long long pack2(float a, float b) {
@@ -112,6 +117,24 @@ __device__ __forceinline__ float ex2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// 2^x of two arguments at most 128, on the FMA pipe: 2^n p(r) with n the nearest whole number, |r| <= 1/2, and p the polynomial
+// 1 + r (c1 + ..) of degree 4 with the smallest relative error (2.8e-6, fitted on Chebyshev nodes).  Arguments below -127, -inf among
+// them, give 0 exactly: n = -127, r = 0, and the exponent field of p(0) = 1 less 127 is that of zero.
+__device__ __forceinline__ void ex2_poly(unsigned long long x, float &p0, float &p1) {
+    float x0, x1, t0, t1;
+    unpack2(x, x0, x1);
+    x = pack2(fmaxf(x0, -127.f), fmaxf(x1, -127.f));
+    const unsigned long long round = pack2(12582912.f, 12582912.f);   // 1.5 2^23: the sum's low bits are n
+    const unsigned long long t = fadd2(x, round), n = fadd2(t, pack2(-12582912.f, -12582912.f)), r = ffma2(n, pack2(-1.f, -1.f), x);
+    unsigned long long p = ffma2(r, pack2(0.00958285294f, 0.00958285294f), pack2(0.0559064262f, 0.0559064262f));
+    p = ffma2(r, p, pack2(0.240240991f, 0.240240991f));
+    p = ffma2(r, p, pack2(0.693124175f, 0.693124175f));
+    p = ffma2(r, p, pack2(1.f, 1.f));
+    unpack2(p, p0, p1);
+    unpack2(t, t0, t1);
+    p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+}
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
     uint32_t y;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
@@ -127,7 +150,7 @@ __device__ __forceinline__ uint64_t desc_advance(uint64_t desc, uint32_t bytes) 
 
 // One row of a segment by itself: keys [k0, k1), fp32 from global memory, values entering only with the keys the row sees.
 template <int D>
-__device__ __noinline__ void redo_row(const TileParams &p, const Seg &s, int x, int canon, int t, int g, int k0, int k1) {
+__device__ __noinline__ void redo_row(const TileParams &p, const Seg &s, int canon, int t, int g, int k0, int k1) {
     const int h = s.head * p.a.G + g;
     const long long row = s.row0 + t;
     const bf16 *q = p.q + row * p.a.q_st + (long long)h * p.a.q_sh;
@@ -275,12 +298,12 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             for (uint32_t k = 0; ok; ++k) {
                 if (!ptx::mbar_wait(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag)) break;
                 const Seg &s = meta->seg[k % kSegs];
-                const int lo = s.lo, hi = s.hi, lx = s.lo_x[x], hx = s.hi_x[x], valid = s.valid;
+                const int lo = s.lo, hi = s.hi, lx = s.lo_x[x], hx = s.hi_x[x], valid = s.valid, odd = s.step - 1;
                 ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
                 if (!valid) break;
 #pragma unroll 1
                 for (int j = lo; j < hi; ++j) {
-                    const bool on = j >= lx && j < hx;
+                    const bool on = j >= lx && j < hx && !((j - lx) & odd);
                     uint32_t st = i % kStages;
                     if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
                     if (on) {
@@ -395,15 +418,21 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 Cursor cur;
                 Segment g;
                 int last_range;
-                int4 cut = make_int4(0, 0, 0, -1);
+                Cut cut = {0, 0, 0, -1};
                 if (!cur.start(p.a, p.plan, range)) break;
-                while (ok && cur.next(p.a, p.plan, 2 * TS, kTileShift, g, last_range)) {
-                    if (last_range >= 0) cut = make_int4(g.x, g.head, g.unit, last_range);
+                while (ok && cur.next(p.a, p.plan, Shape{2 * TS, kTileShift, TS}, g, last_range)) {
+                    if (last_range >= 0) cut = {g.row0 + g.t0, g.t1 - g.t0, g.head, last_range};
                     s.lo = g.lo; s.hi = g.hi; s.n = g.n; s.q = g.q;
                     s.t0 = g.t0; s.t1 = g.t1; s.row0 = g.row0; s.head = g.head;
-                    s.part = g.part; s.slot = g.slot; s.valid = 1; s.pad = 0;
+                    s.part = g.part; s.slot = g.slot; s.valid = 1;
+                    s.step = g.t1 - g.t0 <= TS ? 2 : 1;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
+                        if (s.step == 2) {
+                            s.lo_x[x] = g.lo + x;
+                            s.hi_x[x] = max(g.hi - ((g.hi - g.lo - 1 - x) & 1), g.lo + x);   // behind the stream's last tile
+                            continue;
+                        }
                         const int a0 = min(g.t0 + x * TS, g.t1), a1 = min(a0 + TS, g.t1);
                         int lo = 0, hi = 0;
                         if (a1 > a0) unit_tiles(g.n, g.q, a0, a1, p.a.window, kTileShift, lo, hi);
@@ -422,7 +451,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         if (leader) {
                             const uint32_t full = bar_q_full + 8 * x, dst = base + L::kOffQ + x * L::kTileBytes;
                             ptx::mbar_arrive_expect_tx(full, TS * G * 128 * kHalves);
-                            const int tok = g.row0 + g.t0 + x * TS, c1 = p.t_inner ? tok : g.head * G, c2 = p.t_inner ? g.head * G : tok;
+                            const int tok = g.row0 + g.t0 + (s.step == 2 ? 0 : x * TS), c1 = p.t_inner ? tok : g.head * G, c2 = p.t_inner ? g.head * G : tok;
 #pragma unroll
                             for (int h = 0; h < kHalves; ++h) ptx::tma_load_4d(dst + h * L::kHalfBytes, &tm_q, full, 64 * h, c1, c2, 0);
                         }
@@ -448,20 +477,35 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
             for (int x = 0; x < 2 && ok; ++x) {
                 const int tok = s.t0 + x * TS + t;
-                const bool valid = t < TS && g < G && tok < s.t1, has = s.hi_x[x] > s.lo_x[x];
+                const bool both = s.step == 2, has = s.hi_x[x] > s.lo_x[x], second = both && s.hi_x[1] > s.lo_x[1];
+                bool write = t < TS && g < G && tok < s.t1;
                 const int h = s.head * G + g;
                 const long long r = s.row0 + tok;
                 bf16 *dst = p.out + r * p.a.q_st + (long long)h * p.a.q_sh;
                 float *pdst = p.parts.o + ((long long)s.part * 256 + x * kRows + canon) * D;
-                float2 stat = make_float2(0.f, -CUDART_INF_F);
-                bool write = valid;
+                float2 stat = make_float2(0.f, -CUDART_INF_F);   // factor of O, log2-sum-exp
+                float f1 = 0.f;                                  // factor of the other stream's O
                 if (has) {
                     ok = ptx::mbar_wait_warp(bar_l_full + 8 * x, ns[x] & 1u, abort_flag) && ptx::mbar_wait_warp(bar_o_full + 8 * x, ns[x] & 1u, abort_flag);
                     if (!ok) break;
                     ++ns[x];
                     ptx::tc_fence_after();
                     stat = meta->stats[x][row];
-                    write = valid && !meta->redone[x];
+                    write = write && !meta->redone[x];
+                }
+                if (second) {   // two sums over every second tile each
+                    ok = ptx::mbar_wait_warp(bar_l_full + 8, ns[1] & 1u, abort_flag) && ptx::mbar_wait_warp(bar_o_full + 8, ns[1] & 1u, abort_flag);
+                    if (!ok) break;
+                    ++ns[1];
+                    ptx::tc_fence_after();
+                    const float2 other = meta->stats[1][row];
+                    write = write && !meta->redone[1];
+                    const float top = fmaxf(stat.y, other.y), ref = top == -CUDART_INF_F ? 0.f : top;
+                    const float w0 = ex2_approx(stat.y - ref), w1 = ex2_approx(other.y - ref), sum = w0 + w1;
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    stat.x *= w0 * inv;
+                    f1 = other.x * w1 * inv;
+                    stat.y = sum == 0.f ? -CUDART_INF_F : ref + log2f(sum);
                 }
                 const bool none = stat.y == -CUDART_INF_F;
                 if (has) {
@@ -470,10 +514,25 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         uint32_t o[32];
                         ptx::tmem_ld32(lane_addr + kColO + x * 128 + c0, o);
                         ptx::tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * stat.x);
+                        if (second) {
+#pragma unroll
+                            for (int e0 = 0; e0 < 32; e0 += 16) {
+                                uint32_t o1[16];
+                                ptx::tmem_ld16(lane_addr + kColO + 128 + c0 + e0, o1);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e0 + e] = none ? 0u : __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e0 + e])));
+                            }
+                        }
                         if (c0 == D - 32) {   // O is in registers: the next segment's first PV may overwrite it
                             ptx::tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) ptx::mbar_arrive(bar_o_empty + 8 * x);
+                            if (lane == 0) {
+                                ptx::mbar_arrive(bar_o_empty + 8 * x);
+                                if (second) ptx::mbar_arrive(bar_o_empty + 8);
+                            }
                         }
                         if (!write) continue;
                         if (s.part < 0) {
@@ -481,15 +540,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                             for (int e = 0; e < 32; e += 8) {
                                 uint32_t w[4];
 #pragma unroll
-                                for (int u = 0; u < 4; ++u)
-                                    w[u] = none ? 0u : bf16x2(__uint_as_float(o[e + 2 * u]) * stat.x, __uint_as_float(o[e + 2 * u + 1]) * stat.x);
+                                for (int u = 0; u < 4; ++u) w[u] = bf16x2(__uint_as_float(o[e + 2 * u]), __uint_as_float(o[e + 2 * u + 1]));
                                 *reinterpret_cast<uint4 *>(dst + c0 + e) = make_uint4(w[0], w[1], w[2], w[3]);
                             }
                         } else if (!none) {
 #pragma unroll
                             for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<float4 *>(pdst + c0 + e) = make_float4(__uint_as_float(o[e]) * stat.x, __uint_as_float(o[e + 1]) * stat.x,
-                                                                                          __uint_as_float(o[e + 2]) * stat.x, __uint_as_float(o[e + 3]) * stat.x);
+                                *reinterpret_cast<float4 *>(pdst + c0 + e) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
                         }
                     }
                 } else if (write && s.part < 0) {
@@ -500,6 +557,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (s.part < 0) p.lse[r * p.a.Hq + h] = stat.y * kLn2;
                     else p.parts.lse2[(long long)s.part * 256 + x * kRows + canon] = stat.y;
                 }
+                if (both) break;
             }
         }
     } else {
@@ -515,7 +573,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         Seg s;
 #pragma unroll 1
         for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
-            const int tok = s.t0 + x * TS + t;
+            const int tok = s.t0 + (s.step == 2 ? 0 : x * TS) + t;
             const bool valid = t < TS && g < G && tok < s.t1;
             const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 ? max(last - p.a.window + 1, 0) : 0;   // keys seen
             // keys that not every row of the unit sees lie outside [all_lo, all_hi]
@@ -525,7 +583,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 float m_ref = -CUDART_INF_F, l = 0.f;
                 bool fresh = true;   // no logit above -inf so far
 #pragma unroll 1
-                for (int j = lx; j < hx; ++j, ++nt) {
+                for (int j = lx; j < hx; j += s.step, ++nt) {
                     const int k0 = j * kKeys;
                     if (!(ok = ptx::mbar_wait_warp(bar_s_full + 8 * x, nt & 1u, abort_flag))) break;
                     ptx::tc_fence_after();
@@ -554,12 +612,17 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll
                                 for (int u = 0; u < 4; ++u)
                                     mx[u] = max3(mx[u], __uint_as_float(sr[c][e + 2 * u]), __uint_as_float(sr[c][e + 2 * u + 1]));
-                        bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale2;
+                        bm = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * scale2;
+                    }
+                    // a logit that is NaN or +inf makes the row NaN: the sum says so, whatever the weights below become
+                    if (!(bm < CUDART_INF_F)) {
+                        l = CUDART_NAN_F;
+                        bm = m_ref;
                     }
                     const bool need = !fresh && bm > m_ref + kRescaleThreshold;
                     if (__any_sync(0xffffffffu, need)) {
-                        // the PV of the tile before must have landed before O is touched
-                        const uint32_t v = 2 * (tiles + (j - s.lo) - 1u) + 1u;
+                        // the PV of the stream's tile before must have landed before O is touched
+                        const uint32_t v = 2 * (tiles + (j - s.lo) - s.step) + 1u;
                         if (!(ok = ptx::mbar_wait_warp(bar_kv_empty + 80 * x + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
                         ptx::tc_fence_after();
                         const float f = need ? ex2_approx(m_ref - bm) : 1.f;
@@ -582,20 +645,28 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         fresh = false;
                     }
                     const float neg_m = fresh ? 0.f : -m_ref;   // a row with no key so far: -inf stays -inf
-                    const unsigned long long sc2 = pack2(scale2, scale2), nm2 = pack2(neg_m, neg_m);
+                    unsigned long long sc2 = pack2(scale2, scale2), nm2 = pack2(neg_m, neg_m);
                     unsigned long long acc2[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) acc2[u] = pack2(0.f, 0.f);
                     const bool edge = k0 + kKeys - 1 > all_hi || k0 < all_lo;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
+                        // keeps the compiler from working on the second half before the first is handed over
+                        asm volatile("" : "+l"(sc2), "+l"(nm2));
                         uint32_t pk[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
                             const int c = 2 * half + (e >> 4), c2 = (e & 15) * 2;
-                            float y0, y1;
-                            unpack2(ffma2(pack2(__uint_as_float(sr[c][c2]), __uint_as_float(sr[c][c2 + 1])), sc2, nm2), y0, y1);
-                            const float p0 = ex2_approx(y0), p1 = ex2_approx(y1);
+                            const unsigned long long y = ffma2(pack2(__uint_as_float(sr[c][c2]), __uint_as_float(sr[c][c2 + 1])), sc2, nm2);
+                            float p0, p1;
+                            if (kPolyPairs >> (e & 7) & 1) {
+                                ex2_poly(y, p0, p1);
+                            } else {
+                                unpack2(y, p0, p1);
+                                p0 = ex2_approx(p0);
+                                p1 = ex2_approx(p1);
+                            }
                             acc2[e & 3] = fadd2(acc2[e & 3], pack2(p0, p1));
                             pk[e] = bf16x2(p0, p1);
                         }
@@ -649,8 +720,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
                 if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
                 const bool odd = *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1;
-                if (odd && valid)
-                    redo_row<D>(p, s, x, x * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
+                if (odd && valid && (s.step == 1 || x == 0))
+                    redo_row<D>(p, s, x * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
                 ++ns;
@@ -784,6 +855,7 @@ void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.TS = kRows / a.G;
     p.TQ = 2 * p.TS;
     p.kt_shift = kTileShift;
+    p.small = p.TS;
     p.n_ctas = sm_count;
     // more ranges than CTAs only where the keys that several units read may not fit L2 (see build_plan)
     const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * a.c.D * a.c.es * 2, groups = (bytes + kGroupBytes - 1) / kGroupBytes;
