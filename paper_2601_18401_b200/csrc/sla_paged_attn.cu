@@ -2,12 +2,10 @@
 // map can follow), and the join of partial results.
 //
 //   paged_plan     one CTA: units, their weights, the cut into equal ranges (sla_paged.cuh)
-//   paged_rows     a range per CTA: tiles of KT keys against R rows (tokens x heads of a group) in fp32; running maximum and sum
+//   paged_rows     a range per CTA: tiles of 64 keys against R rows (tokens x heads of a group) in fp32; running maximum and sum
 //   paged_merge    per row of a cut unit: the partial results weighted by their log-sum-exp
 //
-// paged_rows: a tile's 2 R KT D multiply-adds run on the FMA pipe out of shared memory, each of 16 x 16 threads holding a
-// (R/16) x (KT/16) piece of S and a (R/16) x (D/16) piece of O; bound by the FMA pipe and the shared-memory reads that feed it at
-// R = 64, by the reads of K and V at R = 16 (one token of few heads).
+// paged_rows: a tile's 2 R 64 D multiply-adds run on the FMA pipe out of shared memory; bound by that pipe.
 #include <math_constants.h>
 
 #include "sla_paged_attn.h"
@@ -26,22 +24,43 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f,
 }
 
 // ------------------------------------------------------------------------------------------------
-constexpr int kRowThreads = 256;
-template <int D> constexpr int row_keys = D == 64 ? 64 : 32;
-template <int D, int R> constexpr size_t row_smem() {
-    constexpr int KT = row_keys<D>;
-    return (size_t)(R * (D + 4) + KT * (D + 4) + KT * D + R * (KT + 4)) * sizeof(float);
+// Tiles of KT = 64 keys against R = 16 RT rows, 16 x 16 threads: thread (ty, tx) has rows RT ty .. of S and O, keys tx + 16 k of S and
+// dimensions 64 (d / 4) + 4 tx + d % 4 of O.  Two neighbouring rows share an fma.f32x2: Q and P lie in shared memory by dimension and by
+// key, rows next to each other, so that pairs of rows come out of a 16-byte load; the key's (the value's) number is doubled in registers.
+constexpr int kRowThreads = 256, kRowKeys = 64;
+template <int D, int R> constexpr size_t kRowSmem = (size_t)(D * R + kRowKeys * (D + 4) + kRowKeys * D + kRowKeys * (R + 4)) * sizeof(float);
+// two CTAs an SM where their shared memory fits
+template <int D, int R> constexpr int kRowCtas = kRowSmem<D, R> <= 112 * 1024 ? 2 : 1;
+
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void of_pair(unsigned long long r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ unsigned long long fma_pair(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
 }
 
 template <typename T, int D, int R>
-__global__ void __launch_bounds__(kRowThreads, 2)
+__global__ void __launch_bounds__(kRowThreads, (kRowCtas<D, R>))
 paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
-    constexpr int KT = row_keys<D>, kShift = KT == 64 ? 6 : 5;
-    constexpr int RT = R / 16, CT = KT / 16, DT = D / 16;   // rows, keys, dimensions of a thread
-    constexpr int QS = D + 4, PS = KT + 4;
+    constexpr int KT = kRowKeys, kShift = 6;
+    constexpr int RT = R / 16, RP = RT / 2, CT = KT / 16, DT = D / 16;   // rows, pairs of rows, keys, dimensions of a thread
+    constexpr int KS = D + 4, PS = R + 4;   // (padded against bank conflicts)
+    constexpr int E = Vec16<T>::kElems, kLoads = KT * D / E / kRowThreads;   // 16-byte pieces of a tile per thread
+    static_assert(RT % 4 == 0, "rows of a thread come in 16-byte loads");
     extern __shared__ float4 row_sm[];
-    float *sq = reinterpret_cast<float *>(row_sm), *sk = sq + R * QS, *sv = sk + KT * QS, *sp = sv + KT * D;
-    __shared__ int s_odd;   // a value of the tile is not finite
+    float *sq = reinterpret_cast<float *>(row_sm), *sk = sq + D * R, *sv = sk + KT * KS, *sp = sv + KT * D;   // [D][R], [KT][KS], [KT][D], [KT][PS]
+    __shared__ int s_odd;      // a value of the tile is not finite
+    __shared__ int s_pos[R];   // positions of the rows, -1 for rows that do not exist
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int G = a.G;
     const float scale2 = a.scale * kLog2e;
@@ -56,123 +75,181 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
         while (cur.next(a, plan, Shape{TQ, kShift, 0}, s, last_range)) {
             if (last_range >= 0) cut = {s.row0 + s.t0, s.t1 - s.t0, s.head, last_range};
             const int rows = (s.t1 - s.t0) * G;
-            __syncthreads();   // the tiles of the segment before have been read
-            constexpr int E = Vec16<T>::kElems;
+            const int keys_end = min(s.n, s.n - s.q + s.t1);
+            const int *table = a.c.table + (long long)max(s.slot, 0) * a.c.width;
+            const long long head_at = s.head * a.c.s_h;
+            // pieces of a tile: piece c is 16 bytes of key c / (D / E)
+            uint4 raw[kLoads];
+            auto fetch = [&](const char *pool, int tile) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int c = tid + i * kRowThreads, j = tile * KT + c / (D / E), d = (c % (D / E)) * E;
+                    raw[i] = make_uint4(0, 0, 0, 0);
+                    if (j < keys_end) {
+                        const long long at = valid_page(a.c, __ldg(table + (j >> a.c.shift))) * a.c.s_page + head_at + (j & (a.c.P - 1)) * a.c.s_t + d;
+                        raw[i] = __ldg(reinterpret_cast<const uint4 *>(pool + at * sizeof(T)));
+                    }
+                }
+            };
+            auto widen = [&](const uint4 &v, float (&f)[E]) {
+                if constexpr (sizeof(T) == 2) {
+                    Vec16<__nv_bfloat16>::unpack(v, f);
+                } else {
+                    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+                }
+            };
+            if (s.lo < s.hi) fetch(a.c.k, s.lo);
+            __syncthreads();   // shared memory of the segment before has been read
             for (int c = tid; c < R * (D / E); c += kRowThreads) {
-                const int i = c / (D / E), d = (c % (D / E)) * E, t = i / G, g = i - t * G;
+                const int i = c % R, d = (c / R) * E, t = i / G, g = i - t * G;   // neighbouring threads, neighbouring rows: no conflicts
                 float f[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) f[e] = 0.f;
                 if (i < rows) Vec16<T>::load(q + (long long)(s.row0 + s.t0 + t) * a.q_st + (long long)(s.head * G + g) * a.q_sh + d, f);
 #pragma unroll
-                for (int e = 0; e < E; ++e) sq[i * QS + d + e] = f[e] * scale2;
+                for (int e = 0; e < E; ++e) sq[(d + e) * R + i] = f[e] * scale2;
             }
-            int last[RT], first[RT];   // keys [first, last] of this thread's rows
-            float m[RT], l[RT], acc[RT][DT];
+            if (tid < R) s_pos[tid] = tid < rows ? s.n - s.q + s.t0 + tid / G : -1;
+            // keys that every row of the unit sees; a row sees [position - window + 1, position]
+            const int all_hi = rows == R ? s.n - s.q + s.t0 : -1, all_lo = a.window > 0 ? s.n - s.q + s.t1 - a.window : 0;
+            const int reach = a.window > 0 ? a.window : 0x7fffffff;
+            float m[RT], l[RT];
+            unsigned long long acc[RP][DT];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const int i = ty * RT + r;
-                last[r] = i < rows ? s.n - s.q + s.t0 + i / G : -1;
-                first[r] = a.window > 0 ? last[r] - a.window + 1 : 0;
                 m[r] = -CUDART_INF_F;
                 l[r] = 0.f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) acc[r][d] = 0.f;
             }
-            const int keys_end = min(s.n, s.n - s.q + s.t1);
-            const int *table = a.c.table + (long long)max(s.slot, 0) * a.c.width;
-            const long long head_at = s.head * a.c.s_h;
+#pragma unroll
+            for (int r = 0; r < RP; ++r)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[r][d] = 0ull;
             for (int tile = s.lo; tile < s.hi; ++tile) {
                 const int j0 = tile * KT;
+                // K of this tile is on its way; its V is requested before S, the next tile's K before O
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int c = tid + i * kRowThreads;
+                    float f[E];
+                    widen(raw[i], f);
+#pragma unroll
+                    for (int e = 0; e < E; e += 4)
+                        *reinterpret_cast<float4 *>(sk + (c / (D / E)) * KS + (c % (D / E)) * E + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                }
                 if (tid == 0) s_odd = 0;
                 __syncthreads();
-                for (int c = tid; c < KT * (D / E); c += kRowThreads) {
-                    const int jj = c / (D / E), d = (c % (D / E)) * E, j = j0 + jj;
-                    float fk[E], fv[E];
+                fetch(a.c.v, tile);
+                unsigned long long x[RP][CT];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) fk[e] = fv[e] = 0.f;
-                    if (j < keys_end) {
-                        const long long at = valid_page(a.c, table[j >> a.c.shift]) * a.c.s_page + head_at + (j & (a.c.P - 1)) * a.c.s_t + d;
-                        Vec16<T>::load(reinterpret_cast<const T *>(a.c.k) + at, fk);
-                        Vec16<T>::load(reinterpret_cast<const T *>(a.c.v) + at, fv);
-                    }
-                    bool odd = false;
+                for (int r = 0; r < RP; ++r)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        sk[jj * QS + d + e] = fk[e];
-                        const bool fin = fabsf(fv[e]) <= 3.4028235e38f;
-                        odd |= !fin;
-                        sv[jj * D + d + e] = fin ? fv[e] : 0.f;   // reaches only the rows that see its key, below
-                    }
-                    if (odd) s_odd = 1;
-                }
-                __syncthreads();
-                float x[RT][CT];
+                    for (int k = 0; k < CT; ++k) x[r][k] = 0ull;
+#pragma unroll 8
+                for (int d0 = 0; d0 < D; d0 += 4) {
+                    float4 kv[CT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int k = 0; k < CT; ++k) x[r][k] = 0.f;
-#pragma unroll 4
-                for (int d = 0; d < D; d += 4) {
-                    float4 qv[RT], kv[CT];
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) qv[r] = *reinterpret_cast<const float4 *>(sq + (ty * RT + r) * QS + d);
-#pragma unroll
-                    for (int k = 0; k < CT; ++k) kv[k] = *reinterpret_cast<const float4 *>(sk + (tx + 16 * k) * QS + d);
-#pragma unroll
-                    for (int r = 0; r < RT; ++r)
-#pragma unroll
-                        for (int k = 0; k < CT; ++k) {
-                            x[r][k] = fmaf(qv[r].x, kv[k].x, x[r][k]);
-                            x[r][k] = fmaf(qv[r].y, kv[k].y, x[r][k]);
-                            x[r][k] = fmaf(qv[r].z, kv[k].z, x[r][k]);
-                            x[r][k] = fmaf(qv[r].w, kv[k].w, x[r][k]);
-                        }
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    float mx = -CUDART_INF_F;
-#pragma unroll
-                    for (int k = 0; k < CT; ++k) {
-                        const int j = j0 + tx + 16 * k;
-                        if (j > last[r] || j < first[r]) x[r][k] = -CUDART_INF_F;
-                        mx = fmaxf(mx, x[r][k]);
-                    }
-#pragma unroll
-                    for (int off = 8; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-                    const float mn = fmaxf(m[r], mx), base = mn == -CUDART_INF_F ? 0.f : mn;
-                    const float keep = exp2f(m[r] - base);   // 0 for the first tile: m is -inf
-                    m[r] = mn;
-                    l[r] *= keep;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) acc[r][d] *= keep;
-#pragma unroll
-                    for (int k = 0; k < CT; ++k) {
-                        const float p = exp2f(x[r][k] - base);
-                        l[r] += p;
-                        sp[(ty * RT + r) * PS + tx + 16 * k] = p;
-                    }
-                }
-                __syncwarp();   // a row's 16 threads are of one warp
-#pragma unroll 4
-                for (int jj = 0; jj < KT; jj += 4) {
-                    float4 pv[RT];
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) pv[r] = *reinterpret_cast<const float4 *>(sp + (ty * RT + r) * PS + jj);
+                    for (int k = 0; k < CT; ++k) kv[k] = *reinterpret_cast<const float4 *>(sk + (tx + 16 * k) * KS + d0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float vv[DT];
+                        unsigned long long qv[RP];
 #pragma unroll
-                        for (int d = 0; d < DT; d += 4) *reinterpret_cast<float4 *>(vv + d) = *reinterpret_cast<const float4 *>(sv + (jj + e) * D + (d / 4) * 64 + tx * 4);
+                        for (int r = 0; r < RP; r += 2) {
+                            const ulonglong2 w = *reinterpret_cast<const ulonglong2 *>(sq + (d0 + e) * R + ty * RT + 2 * r);
+                            qv[r] = w.x;
+                            qv[r + 1] = w.y;
+                        }
 #pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            const float p = e == 0 ? pv[r].x : e == 1 ? pv[r].y : e == 2 ? pv[r].z : pv[r].w;
+                        for (int k = 0; k < CT; ++k) {
+                            const float kk = e == 0 ? kv[k].x : e == 1 ? kv[k].y : e == 2 ? kv[k].z : kv[k].w;
+                            const unsigned long long k2 = pair_of(kk, kk);
 #pragma unroll
-                            for (int d = 0; d < DT; ++d) acc[r][d] = fmaf(p, vv[d], acc[r][d]);
+                            for (int r = 0; r < RP; ++r) x[r][k] = fma_pair(qv[r], k2, x[r][k]);
+                        }
+                    }
+                }
+                const bool edge = j0 + KT - 1 > all_hi || j0 < all_lo;
+#pragma unroll
+                for (int r = 0; r < RT; r += 2) {
+                    float keep[2];
+                    float y[2][CT];
+#pragma unroll
+                    for (int k = 0; k < CT; ++k) of_pair(x[r / 2][k], y[0][k], y[1][k]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (edge) {
+                            const int back = s_pos[ty * RT + r + h] - j0 - tx;   // how far a key lies before the row's position
+#pragma unroll
+                            for (int k = 0; k < CT; ++k)
+                                if (back - 16 * k < 0 || back - 16 * k >= reach) y[h][k] = -CUDART_INF_F;
+                        }
+                        float mx = y[h][0];
+#pragma unroll
+                        for (int k = 1; k < CT; ++k) mx = fmaxf(mx, y[h][k]);
+#pragma unroll
+                        for (int off = 8; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                        const float mn = fmaxf(m[r + h], mx), base = mn == -CUDART_INF_F ? 0.f : mn;
+                        keep[h] = ex2(m[r + h] - base);   // 0 for the first tile: m is -inf
+                        m[r + h] = mn;
+                        l[r + h] *= keep[h];
+#pragma unroll
+                        for (int k = 0; k < CT; ++k) {
+                            y[h][k] = ex2(y[h][k] - base);
+                            l[r + h] += y[h][k];
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < CT; ++k) x[r / 2][k] = pair_of(y[0][k], y[1][k]);
+                    const unsigned long long kp = pair_of(keep[0], keep[1]);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) acc[r / 2][d] = fma_pair(acc[r / 2][d], kp, 0ull);
+                }
+#pragma unroll
+                for (int k = 0; k < CT; ++k)
+#pragma unroll
+                    for (int r = 0; r < RP; r += 2)
+                        *reinterpret_cast<ulonglong2 *>(sp + (tx + 16 * k) * PS + ty * RT + 2 * r) = make_ulonglong2(x[r][k], x[r + 1][k]);
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int c = tid + i * kRowThreads;
+                    float f[E];
+                    widen(raw[i], f);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const bool fin = fabsf(f[e]) <= 3.4028235e38f;
+                        odd |= !fin;
+                        f[e] = fin ? f[e] : 0.f;   // reaches only the rows that see its key, below
+                    }
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(sv + c * E + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                }
+                if (odd) s_odd = 1;
+                __syncthreads();
+                if (tile + 1 < s.hi) fetch(a.c.k, tile + 1);
+#pragma unroll 8
+                for (int jj = 0; jj < KT; ++jj) {
+                    unsigned long long pv[RP];
+#pragma unroll
+                    for (int r = 0; r < RP; r += 2) {
+                        const ulonglong2 w = *reinterpret_cast<const ulonglong2 *>(sp + jj * PS + ty * RT + 2 * r);
+                        pv[r] = w.x;
+                        pv[r + 1] = w.y;
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; d += 4) {
+                        const float4 v = *reinterpret_cast<const float4 *>(sv + jj * D + (d / 4) * 64 + tx * 4);
+                        const unsigned long long v0 = pair_of(v.x, v.x), v1 = pair_of(v.y, v.y), v2 = pair_of(v.z, v.z), v3 = pair_of(v.w, v.w);
+#pragma unroll
+                        for (int r = 0; r < RP; ++r) {
+                            acc[r][d] = fma_pair(pv[r], v0, acc[r][d]);
+                            acc[r][d + 1] = fma_pair(pv[r], v1, acc[r][d + 1]);
+                            acc[r][d + 2] = fma_pair(pv[r], v2, acc[r][d + 2]);
+                            acc[r][d + 3] = fma_pair(pv[r], v3, acc[r][d + 3]);
                         }
                     }
                 }
                 if (s_odd) {   // values that are not finite, for the rows that see their keys
+#pragma unroll 1
                     for (int jj = 0; jj < KT && j0 + jj < keys_end; ++jj) {
                         const int j = j0 + jj;
                         const long long at = valid_page(a.c, table[j >> a.c.shift]) * a.c.s_page + head_at + (j & (a.c.P - 1)) * a.c.s_t;
@@ -181,8 +258,14 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
                             const float v = (float)(reinterpret_cast<const T *>(a.c.v) + at)[(d / 4) * 64 + tx * 4 + d % 4];
                             if (fabsf(v) <= 3.4028235e38f) continue;
 #pragma unroll
-                            for (int r = 0; r < RT; ++r)
-                                if (j <= last[r] && j >= first[r]) acc[r][d] = fmaf(sp[(ty * RT + r) * PS + jj], v, acc[r][d]);
+                            for (int r = 0; r < RP; ++r) {
+                                float o0, o1;
+                                of_pair(acc[r][d], o0, o1);
+                                const int b0 = s_pos[ty * RT + 2 * r] - j, b1 = s_pos[ty * RT + 2 * r + 1] - j;
+                                if (b0 >= 0 && b0 < reach) o0 = fmaf(sp[jj * PS + ty * RT + 2 * r], v, o0);
+                                if (b1 >= 0 && b1 < reach) o1 = fmaf(sp[jj * PS + ty * RT + 2 * r + 1], v, o1);
+                                acc[r][d] = pair_of(o0, o1);
+                            }
                         }
                     }
                 }
@@ -197,18 +280,25 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
                 if (i >= rows) continue;
                 const bool none = total == 0.f && m[r] == -CUDART_INF_F;
                 const float inv = none ? 0.f : 1.f / total, lse2 = none ? -CUDART_INF_F : m[r] + log2f(total);
+                float o[DT];
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    float o0, o1;
+                    of_pair(acc[r / 2][d], o0, o1);
+                    o[d] = none ? 0.f : (r & 1 ? o1 : o0) * inv;
+                }
                 if (s.part < 0) {
                     const int t = i / G, g = i - t * G;
                     const long long row = s.row0 + s.t0 + t;
-                    T *o = out + row * a.q_st + (long long)(s.head * G + g) * a.q_sh;
+                    T *dst = out + row * a.q_st + (long long)(s.head * G + g) * a.q_sh;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) o[(d / 4) * 64 + tx * 4 + d % 4] = from_float<T>(none ? 0.f : acc[r][d] * inv);
+                    for (int d = 0; d < DT; ++d) dst[(d / 4) * 64 + tx * 4 + d % 4] = from_float<T>(o[d]);
                     if (tx == 0) lse[row * a.Hq + s.head * G + g] = lse2 * kLn2;
                 } else {
-                    float *o = parts.o + ((long long)s.part * R + i) * D;
+                    float *dst = parts.o + ((long long)s.part * R + i) * D;
 #pragma unroll
                     for (int d = 0; d < DT; d += 4)
-                        if (!none) *reinterpret_cast<float4 *>(o + (d / 4) * 64 + tx * 4) = make_float4(acc[r][d] * inv, acc[r][d + 1] * inv, acc[r][d + 2] * inv, acc[r][d + 3] * inv);
+                        if (!none) *reinterpret_cast<float4 *>(dst + (d / 4) * 64 + tx * 4) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
                     if (tx == 0) parts.lse2[(long long)s.part * R + i] = lse2;
                 }
             }
@@ -313,11 +403,11 @@ cudaError_t run_rows(const void *q, const PagedCall &a, const PagedPlan &p, char
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !allowed[dev]) {
-        e = cudaFuncSetAttribute(paged_rows<T, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)row_smem<D, R>());
+        e = cudaFuncSetAttribute(paged_rows<T, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem<D, R>);
         if (e != cudaSuccess) return e;
         if (dev < 64) allowed[dev] = true;
     }
-    return launch_chained(paged_rows<T, D, R>, dim3(p.n_ctas), dim3(kRowThreads), (row_smem<D, R>()), st, (const T *)q, a, p.TQ,
+    return launch_chained(paged_rows<T, D, R>, dim3(p.n_ctas), dim3(kRowThreads), (kRowSmem<D, R>), st, (const T *)q, a, p.TQ,
                           plan_at(p, scratch), parts_at(p, scratch), (T *)out, lse);
 }
 
@@ -344,15 +434,15 @@ cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p
 PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     PagedPlan p;
     p.kind = PagedPlan::kRows;
-    p.R = a.b.max_new * (long long)a.G <= 16 ? 16 : 64;
+    p.R = a.b.max_new * (long long)a.G <= 64 ? 64 : 128;
     p.RS = p.R;
     p.TS = p.TQ = p.R / a.G;
-    p.kt_shift = a.c.D == 64 ? 6 : 5;
-    p.n_ctas = 2 * sm_count;
+    p.kt_shift = 6;
+    p.n_ctas = (a.c.D == 128 ? 1 : 2) * sm_count;
     p.max_groups = 1;
     p.min_weight = 4;
     p.small = 0;
-    if (paged_decode_supported(a, dtype)) {
+    if (paged_decode_supported(a)) {
         p.kind = PagedPlan::kDecode;
         plan_paged_decode(a, p, sm_count);
     } else if (paged_tiles_supported(a, dtype)) {
@@ -380,17 +470,17 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
 
 cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                    float *lse, cudaStream_t st, long long *launches) {
-    if (p.kind == PagedPlan::kDecode) return launch_paged_decode_attention(q, a, p, scratch, counters, out, lse, st, launches);
+    if (p.kind == PagedPlan::kDecode) return launch_paged_decode_attention(q, a, dtype, p, scratch, counters, out, lse, st, launches);
     cudaError_t e = launch_paged_plan(a, p, scratch, st);
     if (e == cudaSuccess && p.kind == PagedPlan::kTiles) {
         e = launch_paged_tiles(q, a, p, scratch, out, lse, st);
     } else if (e == cudaSuccess) {
         if (dtype == SLA_F32) {
-            if (a.c.D == 64) e = p.R == 16 ? run_rows<float, 64, 16>(q, a, p, scratch, out, lse, st) : run_rows<float, 64, 64>(q, a, p, scratch, out, lse, st);
-            else e = p.R == 16 ? run_rows<float, 128, 16>(q, a, p, scratch, out, lse, st) : run_rows<float, 128, 64>(q, a, p, scratch, out, lse, st);
+            if (a.c.D == 64) e = p.R == 64 ? run_rows<float, 64, 64>(q, a, p, scratch, out, lse, st) : run_rows<float, 64, 128>(q, a, p, scratch, out, lse, st);
+            else e = p.R == 64 ? run_rows<float, 128, 64>(q, a, p, scratch, out, lse, st) : run_rows<float, 128, 128>(q, a, p, scratch, out, lse, st);
         } else {
-            if (a.c.D == 64) e = p.R == 16 ? run_rows<__nv_bfloat16, 64, 16>(q, a, p, scratch, out, lse, st) : run_rows<__nv_bfloat16, 64, 64>(q, a, p, scratch, out, lse, st);
-            else e = p.R == 16 ? run_rows<__nv_bfloat16, 128, 16>(q, a, p, scratch, out, lse, st) : run_rows<__nv_bfloat16, 128, 64>(q, a, p, scratch, out, lse, st);
+            if (a.c.D == 64) e = p.R == 64 ? run_rows<__nv_bfloat16, 64, 64>(q, a, p, scratch, out, lse, st) : run_rows<__nv_bfloat16, 64, 128>(q, a, p, scratch, out, lse, st);
+            else e = p.R == 64 ? run_rows<__nv_bfloat16, 128, 64>(q, a, p, scratch, out, lse, st) : run_rows<__nv_bfloat16, 128, 128>(q, a, p, scratch, out, lse, st);
         }
     }
     if (e == cudaSuccess) e = launch_paged_merge(a, dtype, p, scratch, out, lse, st);

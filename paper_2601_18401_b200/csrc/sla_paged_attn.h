@@ -31,10 +31,10 @@ cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p
 cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                    float *lse, cudaStream_t st, long long *launches);
 
-// ---- one new token a sequence, bf16 (sla_paged_decode.cu)
-bool paged_decode_supported(const PagedCall &a, int dtype);
+// ---- one new token a sequence (sla_paged_decode.cu)
+bool paged_decode_supported(const PagedCall &a);
 void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count);
-cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out,
+cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches);
 
 // ---- chunks of new tokens, bf16 (sla_paged_tiles.cu)

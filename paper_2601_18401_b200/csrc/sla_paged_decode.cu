@@ -1,6 +1,8 @@
-// Attention of one new token a sequence over a paged cache, bf16.  One launch.
+// Attention of one new token a sequence over a paged cache.  One launch.
 //
-// All G query heads of a KV head share its keys, so that K and V are read once: bound by HBM.  The products run on the tensor
+// All G query heads of a KV head share its keys, so that K and V are read once: bound by HBM.
+//
+// bf16 (attend_bf16): the products run on the tensor
 // cores by mma.sync with the keys as the 16 rows of A and the heads as the 8 columns of B,
 //     S^T [16 keys, 8 heads] = K Q^T,      O^T [D, 8 heads] += V^T P^T,
 // which wastes nothing for groups of 8 and needs no shared memory on the way: a thread fetches pieces of 16 bytes of its rows
@@ -9,9 +11,13 @@
 // permutation, P^T is the 8 x 8 transpose of P (movmatrix).  A warp goes through 16 keys at a time -- they lie in one page -- with
 // the keys of the next step fetched as soon as these are used up, and the values after them.
 //
+// fp32 (attend_f32): on the FMA pipe, 32 keys a step and warp.  For S a lane has a key of its own and goes along its row, the heads' queries
+// broadcast from shared memory; for O a lane has dimensions of its own and the warp goes along the keys, the weights
+// broadcast: no sum crosses lanes.
+//
 // The running maximum of a head moves only when a logit passes it by 2^8 (a factor that neither the fp32 sums nor the bf16 weights
-// notice), decided by one vote of the warp.  Sums are fp32; a weight is rounded to bf16 before it meets its value, as the tensor
-// cores want it, the denominator adds the unrounded weights.
+// notice), decided by one vote of the warp.  Sums are fp32; in bf16 a weight is rounded before it meets its value, as the tensor
+// cores want it, and the denominator adds the unrounded weights.
 //
 // The units (sequence, KV head) of the call lie end to end, weighted by their keys, and are cut into as many equal ranges as there
 // are CTAs.  The CTA that finishes a cut unit last joins the partial results, in the order of the ranges.
@@ -55,25 +61,297 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float a, float b, float c, float d) { *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d)); }
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) { *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// What one warp does of a segment: the keys key, key + stride, .. below key_end in steps of the path's own, of which those in [first, n) count,
+// for the G heads of KV head `head`.  Its maxima, sums and weighted values go to w_m, w_l [heads] and w_o [heads][D].
+struct Walk {
+    int key, key_end, first, n, head, row_q;
+    const int *table;
+};
+
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT))
-paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
-             __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
+__device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q, const PagedCall &a, const Walk &wk, float *w_m, float *w_l, float *w_o) {
     constexpr int kChunks = D / 32;       // 16-byte pieces of a key row per thread
     constexpr int kVChunks = D / 64;      // of a value row
     constexpr int kMt = D / 16;           // m-tiles of O^T
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int G = a.G, first = wk.first, n = wk.n, head = wk.head, row_q = wk.row_q, key_end = wk.key_end;
+    const int *table = wk.table;
+    const float scale2 = a.scale * kLog2e;
+    int key = wk.key;
+    float m[NT][2], l[NT][2], acc[NT][kMt][4];
+    uint32_t qf[NT][kChunks][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const bool on = 8 * t + g < G;
+        const __nv_bfloat16 *src = q + (long long)row_q * a.q_st + (long long)(head * G + (on ? 8 * t + g : 0)) * a.q_sh + c * 8;
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const uint4 v = on ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * j)) : make_uint4(0, 0, 0, 0);
+            qf[t][j][0] = v.x; qf[t][j][1] = v.y; qf[t][j][2] = v.z; qf[t][j][3] = v.w;
+        }
+        m[t][0] = m[t][1] = -CUDART_INF_F;
+        l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMt; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][i][e] = 0.f;
+    }
+
+    const __nv_bfloat16 *kb = reinterpret_cast<const __nv_bfloat16 *>(a.c.k) + head * a.c.s_h;
+    const __nv_bfloat16 *vb = reinterpret_cast<const __nv_bfloat16 *>(a.c.v) + head * a.c.s_h;
+    uint4 kr[2][kChunks], vr[4][kVChunks];
+    long long at = 0;   // of the step's first row
+    auto find = [&](int k0) { return valid_page(a.c, __ldg(table + (k0 >> a.c.shift))) * a.c.s_page + (long long)(k0 & (a.c.P - 1)) * a.c.s_t; };
+    auto load_k = [&](long long to_) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) kr[e][j] = load_stream(kb + to_ + (long long)(g + 8 * e) * a.c.s_t + c * 8 + 32 * j);
+    };
+    auto load_v = [&](long long to_, int k0) {   // values of keys outside [first, n) may be anything: they are not read
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int kk = 2 * c + (e & 1) + 8 * (e >> 1);
+            const bool on = k0 + kk >= first && k0 + kk < n;
+#pragma unroll
+            for (int j = 0; j < kVChunks; ++j)
+                vr[e][j] = on ? load_stream(vb + to_ + (long long)kk * a.c.s_t + g * 8 + 64 * j) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    long long at_next = 0;
+    if (key < key_end) {
+        at = find(key);
+        load_k(at);
+        load_v(at, key);
+        if (key + 16 * kWarps < key_end) at_next = find(key + 16 * kWarps);
+    }
+    for (; key < key_end; key += 16 * kWarps) {
+        const int next = key + 16 * kWarps;
+        float s[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                mma16816(s[t], kr[0][j].x, kr[1][j].x, kr[0][j].y, kr[1][j].y, qf[t][j][0], qf[t][j][1]);
+                mma16816(s[t], kr[0][j].z, kr[1][j].z, kr[0][j].w, kr[1][j].w, qf[t][j][2], qf[t][j][3]);
+            }
+        }
+        if (next < key_end) load_k(at_next);
+        bool over = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][e] *= scale2;
+        if (key < first || key + 16 > n) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int kk = key + g + 8 * (e >> 1);
+                    if (kk < first || kk >= n) s[t][e] = -CUDART_INF_F;
+                }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) over |= fmaxf(s[t][e], s[t][e + 2]) > m[t][e] + 8.f;
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(m[t][e], fmaxf(s[t][e], s[t][e + 2]));
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                    const float keep = m[t][e] == mx ? 1.f : exp2_fast(m[t][e] - mx);
+                    m[t][e] = mx;
+                    l[t][e] *= keep;
+#pragma unroll
+                    for (int i = 0; i < kMt; ++i) {
+                        acc[t][i][e] *= keep;
+                        acc[t][i][e + 2] *= keep;
+                    }
+                }
+        }
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float base = m[t][e & 1] == -CUDART_INF_F ? 0.f : m[t][e & 1];
+                s[t][e] = exp2_fast(s[t][e] - base);
+                l[t][e & 1] += s[t][e];
+            }
+            pf[t][0] = transpose8x8(pack_bf16(s[t][0], s[t][1]));
+            pf[t][1] = transpose8x8(pack_bf16(s[t][2], s[t][3]));
+        }
+        // row g of m-tile i: dimension 8 g + i; row g + 8: 64 + 8 g + i (D = 64: 8 g + 4 + i)
+#pragma unroll
+        for (int i = 0; i < kMt; ++i) {
+            const int i1 = D == 128 ? i : i + 4, j1 = D == 128 ? kVChunks - 1 : 0;
+            const uint32_t sel = i & 1 ? 0x7632u : 0x5410u, sel1 = i1 & 1 ? 0x7632u : 0x5410u;
+            const uint32_t a0 = __byte_perm(word(vr[0][0], i / 2), word(vr[1][0], i / 2), sel);
+            const uint32_t a2 = __byte_perm(word(vr[2][0], i / 2), word(vr[3][0], i / 2), sel);
+            const uint32_t a1 = __byte_perm(word(vr[0][j1], i1 / 2), word(vr[1][j1], i1 / 2), sel1);
+            const uint32_t a3 = __byte_perm(word(vr[2][j1], i1 / 2), word(vr[3][j1], i1 / 2), sel1);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(acc[t][i], a0, a1, a2, a3, pf[t][0], pf[t][1]);
+        }
+        if (next < key_end) {
+            load_v(at_next, next);
+            if (next + 16 * kWarps < key_end) at_next = find(next + 16 * kWarps);
+        }
+    }
+
+    // ---- the warp's sums
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float v = l[t][e];
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+            const int qi = 8 * t + 2 * c + e;
+            if (g == 0) { w_m[qi] = m[t][e]; w_l[qi] = v; }
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+                w_o[qi * D + 8 * g + i] = acc[t][i][e];
+                w_o[qi * D + (D == 128 ? 64 + 8 * g + i : 8 * g + 4 + i)] = acc[t][i][e + 2];
+            }
+        }
+}
+
+// fp32: S by lanes of a key each, O by lanes of D / 32 dimensions each.  s_q: the queries [D][8 NT], scaled.
+template <int D, int NT>
+__device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, const float *s_q, float *w_m, float *w_l, float *w_o) {
+    float *s_p = w_o;   // a step's weights, until the sums are written
+    constexpr int H = 8 * NT, N = D / 32, kDeep = 8;   // heads, dimensions of a lane, loads in flight
+    const int lane = threadIdx.x & 31, first = wk.first, n = wk.n;
+    const float *kb = reinterpret_cast<const float *>(a.c.k) + wk.head * a.c.s_h;
+    const float *vb = reinterpret_cast<const float *>(a.c.v) + wk.head * a.c.s_h + lane * N;
+    auto row_of = [&](int j) { return valid_page(a.c, __ldg(wk.table + (j >> a.c.shift))) * a.c.s_page + (long long)(j & (a.c.P - 1)) * a.c.s_t; };
+    float m[H], l[H], acc[H][N];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        m[h] = -CUDART_INF_F;
+        l[h] = 0.f;
+#pragma unroll
+        for (int d = 0; d < N; ++d) acc[h][d] = 0.f;
+    }
+    for (int key = wk.key; key < wk.key_end; key += 32 * kWarps) {
+        const int j = key + lane;
+        const bool on = j >= first && j < n && j < wk.key_end;
+        const long long at = row_of(on ? j : min(max(first, 0), n - 1));
+        const float *kr = kb + at;
+        float s[H];
+#pragma unroll
+        for (int h = 0; h < H; ++h) s[h] = 0.f;
+#pragma unroll 1
+        for (int d0 = 0; d0 < D; d0 += 4 * kDeep) {
+            float4 k4[kDeep];
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) k4[u] = __ldg(reinterpret_cast<const float4 *>(kr + d0 + 4 * u));
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float kk = e == 0 ? k4[u].x : e == 1 ? k4[u].y : e == 2 ? k4[u].z : k4[u].w;
+#pragma unroll
+                    for (int h = 0; h < H; h += 4) {
+                        const float4 q4 = *reinterpret_cast<const float4 *>(s_q + (d0 + 4 * u + e) * H + h);
+                        s[h] = fmaf(q4.x, kk, s[h]); s[h + 1] = fmaf(q4.y, kk, s[h + 1]);
+                        s[h + 2] = fmaf(q4.z, kk, s[h + 2]); s[h + 3] = fmaf(q4.w, kk, s[h + 3]);
+                    }
+                }
+        }
+        bool over = false;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            if (!on) s[h] = -CUDART_INF_F;
+            over |= s[h] > m[h] + 8.f;
+        }
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                float mx = fmaxf(m[h], s[h]);
+#pragma unroll
+                for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                const float keep = m[h] == mx ? 1.f : exp2_fast(m[h] - mx);
+                m[h] = mx;
+                l[h] *= keep;
+#pragma unroll
+                for (int d = 0; d < N; ++d) acc[h][d] *= keep;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            s[h] = exp2_fast(s[h] - (m[h] == -CUDART_INF_F ? 0.f : m[h]));
+            l[h] += s[h];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < H; h += 4) *reinterpret_cast<float4 *>(s_p + lane * H + h) = make_float4(s[h], s[h + 1], s[h + 2], s[h + 3]);
+        __syncwarp();
+        const unsigned seen = __ballot_sync(0xffffffffu, on);   // values of other keys may be anything: they are not read
+#pragma unroll 1
+        for (int i0 = 0; i0 < 32; i0 += kDeep) {
+            float v[kDeep][N];
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
+                const long long to = __shfl_sync(0xffffffffu, at, i0 + u);
+#pragma unroll
+                for (int d = 0; d < N; ++d) v[u][d] = 0.f;
+                if (seen >> (i0 + u) & 1) {
+                    if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
+                    else *reinterpret_cast<float2 *>(v[u]) = __ldg(reinterpret_cast<const float2 *>(vb + to));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+                for (int h = 0; h < H; h += 4) {
+                    const float4 p4 = *reinterpret_cast<const float4 *>(s_p + (i0 + u) * H + h);
+                    const float pp[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int d = 0; d < N; ++d) acc[h + e][d] = fmaf(pp[e], v[u][d], acc[h + e][d]);
+                }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        float sum = l[h];
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (lane == 0) { w_m[h] = m[h]; w_l[h] = sum; }
+        if (h == 0) __syncwarp();   // the weights have been read
+#pragma unroll
+        for (int d = 0; d < N; ++d) w_o[h * D + lane * N + d] = acc[h][d];
+    }
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT))
+paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
+             T *__restrict__ out, float *__restrict__ lse) {
     constexpr int R = 16;                 // rows of a partial result
-    __shared__ float s_o[kWarps][8 * NT][D];
+    __shared__ alignas(16) float s_o[kWarps][8 * NT][D];
     __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
     __shared__ long long s_scan[kWarps];
     __shared__ int s_last;
     extern __shared__ long long s_seq_at[];   // [n_seqs + 1] weight before a sequence; then its tokens and its slot
     int *s_n = reinterpret_cast<int *>(s_seq_at + n_seqs + 1), *s_slot = s_n + n_seqs;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    constexpr bool kF32 = sizeof(T) == 4;
+    constexpr int kStep = kF32 ? 32 : 16;   // keys of a warp's step
+    __shared__ alignas(16) float s_q[kF32 ? D * 8 * NT : 4];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.G;
-    const float scale2 = a.scale * kLog2e;
     chain_wait();
     chain_release();
 
@@ -135,153 +413,20 @@ paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n
         unit_tiles(n, 1, 0, 1, a.window, kTileShift, lo, hi);
         const int from = (int)(w - start), to = (int)((w_end < stop ? w_end : stop) - start);
         const int first = a.window > 0 && n > a.window ? n - a.window : 0;
-        int key = max((lo + max(from - kUnitWeight, 0)) << kTileShift, first & ~15);
+        const int key = max((lo + max(from - kUnitWeight, 0)) << kTileShift, first & ~(kStep - 1));
         const int key_end = min((lo + max(to - kUnitWeight, 0)) << kTileShift, n);
-        key += 16 * warp;
-
-        float m[NT][2], l[NT][2], acc[NT][kMt][4];
-        uint32_t qf[NT][kChunks][4];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const bool on = 8 * t + g < G;
-            const __nv_bfloat16 *src = q + (long long)row_q * a.q_st + (long long)(head * G + (on ? 8 * t + g : 0)) * a.q_sh + c * 8;
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                const uint4 v = on ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * j)) : make_uint4(0, 0, 0, 0);
-                qf[t][j][0] = v.x; qf[t][j][1] = v.y; qf[t][j][2] = v.z; qf[t][j][3] = v.w;
+        const Walk walk = {key + kStep * warp, key_end, first, n, head, row_q, a.c.table + (long long)max(s_slot[x], 0) * a.c.width};
+        if constexpr (kF32) {
+            // (s_q: the segment before has been joined)
+            for (int c = tid; c < D * 8 * NT; c += kThreads) {
+                const int h = c / D, d = c % D;   // neighbouring threads, neighbouring dimensions
+                s_q[d * 8 * NT + h] = h < G ? q[(long long)row_q * a.q_st + (long long)(head * G + h) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
             }
-            m[t][0] = m[t][1] = -CUDART_INF_F;
-            l[t][0] = l[t][1] = 0.f;
-#pragma unroll
-            for (int i = 0; i < kMt; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t][i][e] = 0.f;
+            __syncthreads();
+            attend_f32<D, NT>(a, walk, s_q, s_m[warp], s_l[warp], &s_o[warp][0][0]);
+        } else {
+            attend_bf16<D, NT>(q, a, walk, s_m[warp], s_l[warp], &s_o[warp][0][0]);
         }
-
-        const int *table = a.c.table + (long long)max(s_slot[x], 0) * a.c.width;
-        const __nv_bfloat16 *kb = reinterpret_cast<const __nv_bfloat16 *>(a.c.k) + head * a.c.s_h;
-        const __nv_bfloat16 *vb = reinterpret_cast<const __nv_bfloat16 *>(a.c.v) + head * a.c.s_h;
-        uint4 kr[2][kChunks], vr[4][kVChunks];
-        long long at = 0;   // of the step's first row
-        auto find = [&](int k0) { return valid_page(a.c, __ldg(table + (k0 >> a.c.shift))) * a.c.s_page + (long long)(k0 & (a.c.P - 1)) * a.c.s_t; };
-        auto load_k = [&](long long to_) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int j = 0; j < kChunks; ++j) kr[e][j] = load_stream(kb + to_ + (long long)(g + 8 * e) * a.c.s_t + c * 8 + 32 * j);
-        };
-        auto load_v = [&](long long to_, int k0) {   // values of keys outside [first, n) may be anything: they are not read
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int kk = 2 * c + (e & 1) + 8 * (e >> 1);
-                const bool on = k0 + kk >= first && k0 + kk < n;
-#pragma unroll
-                for (int j = 0; j < kVChunks; ++j)
-                    vr[e][j] = on ? load_stream(vb + to_ + (long long)kk * a.c.s_t + g * 8 + 64 * j) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        long long at_next = 0;
-        if (key < key_end) {
-            at = find(key);
-            load_k(at);
-            load_v(at, key);
-            if (key + 16 * kWarps < key_end) at_next = find(key + 16 * kWarps);
-        }
-        for (; key < key_end; key += 16 * kWarps) {
-            const int next = key + 16 * kWarps;
-            float s[NT][4];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
-#pragma unroll
-                for (int j = 0; j < kChunks; ++j) {
-                    mma16816(s[t], kr[0][j].x, kr[1][j].x, kr[0][j].y, kr[1][j].y, qf[t][j][0], qf[t][j][1]);
-                    mma16816(s[t], kr[0][j].z, kr[1][j].z, kr[0][j].w, kr[1][j].w, qf[t][j][2], qf[t][j][3]);
-                }
-            }
-            if (next < key_end) load_k(at_next);
-            bool over = false;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[t][e] *= scale2;
-            if (key < first || key + 16 > n) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int kk = key + g + 8 * (e >> 1);
-                        if (kk < first || kk >= n) s[t][e] = -CUDART_INF_F;
-                    }
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) over |= fmaxf(s[t][e], s[t][e + 2]) > m[t][e] + 8.f;
-            if (__any_sync(0xffffffffu, over)) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(m[t][e], fmaxf(s[t][e], s[t][e + 2]));
-#pragma unroll
-                        for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-                        const float keep = m[t][e] == mx ? 1.f : exp2_fast(m[t][e] - mx);
-                        m[t][e] = mx;
-                        l[t][e] *= keep;
-#pragma unroll
-                        for (int i = 0; i < kMt; ++i) {
-                            acc[t][i][e] *= keep;
-                            acc[t][i][e + 2] *= keep;
-                        }
-                    }
-            }
-            uint32_t pf[NT][2];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float base = m[t][e & 1] == -CUDART_INF_F ? 0.f : m[t][e & 1];
-                    s[t][e] = exp2_fast(s[t][e] - base);
-                    l[t][e & 1] += s[t][e];
-                }
-                pf[t][0] = transpose8x8(pack_bf16(s[t][0], s[t][1]));
-                pf[t][1] = transpose8x8(pack_bf16(s[t][2], s[t][3]));
-            }
-            // row g of m-tile i: dimension 8 g + i; row g + 8: 64 + 8 g + i (D = 64: 8 g + 4 + i)
-#pragma unroll
-            for (int i = 0; i < kMt; ++i) {
-                const int i1 = D == 128 ? i : i + 4, j1 = D == 128 ? kVChunks - 1 : 0;
-                const uint32_t sel = i & 1 ? 0x7632u : 0x5410u, sel1 = i1 & 1 ? 0x7632u : 0x5410u;
-                const uint32_t a0 = __byte_perm(word(vr[0][0], i / 2), word(vr[1][0], i / 2), sel);
-                const uint32_t a2 = __byte_perm(word(vr[2][0], i / 2), word(vr[3][0], i / 2), sel);
-                const uint32_t a1 = __byte_perm(word(vr[0][j1], i1 / 2), word(vr[1][j1], i1 / 2), sel1);
-                const uint32_t a3 = __byte_perm(word(vr[2][j1], i1 / 2), word(vr[3][j1], i1 / 2), sel1);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) mma16816(acc[t][i], a0, a1, a2, a3, pf[t][0], pf[t][1]);
-            }
-            if (next < key_end) {
-                load_v(at_next, next);
-                if (next + 16 * kWarps < key_end) at_next = find(next + 16 * kWarps);
-            }
-        }
-
-        // ---- join the warps
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float v = l[t][e];
-#pragma unroll
-                for (int off = 4; off < 32; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-                const int qi = 8 * t + 2 * c + e;
-                if (g == 0) { s_m[warp][qi] = m[t][e]; s_l[warp][qi] = v; }
-#pragma unroll
-                for (int i = 0; i < kMt; ++i) {
-                    s_o[warp][qi][8 * g + i] = acc[t][i][e];
-                    s_o[warp][qi][D == 128 ? 64 + 8 * g + i : 8 * g + 4 + i] = acc[t][i][e + 2];
-                }
-            }
         __syncthreads();
         const bool begins = from == 0, ends = w_end >= stop;
         const int part = begins && ends ? -1 : begins ? 2 * r + 1 : 2 * r;
@@ -306,7 +451,7 @@ paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n
             for (int e = 0; e < 4; ++e) o[e] *= inv;
             if (part < 0) {
                 const int h = head * G + qi;
-                *reinterpret_cast<uint2 *>(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d) = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+                store4(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d, o[0], o[1], o[2], o[3]);
                 if (d == 0) lse[(long long)row_q * a.Hq + h] = z * kLn2;
             } else {
                 if (!none) __stcg(reinterpret_cast<float4 *>(parts.o + ((long long)part * R + qi) * D + d), make_float4(o[0], o[1], o[2], o[3]));
@@ -364,8 +509,7 @@ paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n
                     const bool none = mx == -CUDART_INF_F && sum == 0.f;
                     const float inv = none ? 0.f : 1.f / sum;
                     const int h = head * G + qi;
-                    *reinterpret_cast<uint2 *>(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d) =
-                        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+                    store4(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
                     if (d == 0) lse[(long long)row_q * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
                 }
             }
@@ -383,7 +527,7 @@ paged_decode(const __nv_bfloat16 *__restrict__ q, PagedCall a, int x_base, int n
 
 }  // namespace
 
-bool paged_decode_supported(const PagedCall &a, int dtype) { return dtype == SLA_BF16 && a.b.max_new == 1; }
+bool paged_decode_supported(const PagedCall &a) { return a.b.max_new == 1; }
 
 void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.R = p.RS = 16;
@@ -391,23 +535,30 @@ void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.n_ctas = ctas_per_sm(a.c.D, a.G <= 8 ? 1 : 2) * sm_count;
 }
 
-template <int D, int NT>
+template <typename T, int D, int NT>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
     for (int x0 = 0; x0 < a.b.n_seqs && e == cudaSuccess; x0 += kMaxSeqs) {
         const int n = a.b.n_seqs - x0 < kMaxSeqs ? a.b.n_seqs - x0 : kMaxSeqs;
-        e = launch_chained(paged_decode<D, NT>, dim3(p.n_ctas), dim3(kThreads), (size_t)(n + 1) * 8 + (size_t)n * 8, st,
-                           (const __nv_bfloat16 *)q, a, x0, n, parts_at(p, scratch), counters, (__nv_bfloat16 *)out, lse);
+        e = launch_chained(paged_decode<T, D, NT>, dim3(p.n_ctas), dim3(kThreads), (size_t)(n + 1) * 8 + (size_t)n * 8, st,
+                           (const T *)q, a, x0, n, parts_at(p, scratch), counters, (T *)out, lse);
         ++*launches;
     }
     return e;
 }
 
-cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out,
+template <typename T>
+static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
+                              cudaStream_t st, long long *launches) {
+    if (a.c.D == 64) return a.G <= 8 ? decode_of<T, 64, 1>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, 64, 2>(q, a, p, scratch, counters, out, lse, st, launches);
+    return a.G <= 8 ? decode_of<T, 128, 1>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, 128, 2>(q, a, p, scratch, counters, out, lse, st, launches);
+}
+
+cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches) {
-    if (a.c.D == 64) return a.G <= 8 ? decode_of<64, 1>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<64, 2>(q, a, p, scratch, counters, out, lse, st, launches);
-    return a.G <= 8 ? decode_of<128, 1>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<128, 2>(q, a, p, scratch, counters, out, lse, st, launches);
+    return dtype == SLA_F32 ? decode_for<float>(q, a, p, scratch, counters, out, lse, st, launches)
+                            : decode_for<__nv_bfloat16>(q, a, p, scratch, counters, out, lse, st, launches);
 }
 
 }  // namespace sla
