@@ -802,6 +802,7 @@ const char *check_cache(const sla_cache_t *c) {
     if (c->n_pages <= 0 || c->n_kv_heads <= 0 || c->n_slots <= 0 || c->table_width <= 0) return "n_pages, n_kv_heads, n_slots and table_width must be positive";
     if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens must be a power of two in 16..256";
     if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+    if ((int64_t)c->n_pages * c->page_tokens > 4294967295LL) return "n_pages * page_tokens above 2^32 - 1";
     if (c->n_kv_heads > 65536) return "n_kv_heads above 65536";
     if ((int64_t)c->table_width * c->page_tokens > 2147483647LL - 1024) return "table_width * page_tokens above 2^31 - 1025";
     if (c->dtype != SLA_F32 && c->dtype != SLA_BF16) return "dtype must be SLA_F32 or SLA_BF16";

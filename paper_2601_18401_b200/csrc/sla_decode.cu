@@ -73,6 +73,14 @@ template <class Cache> __device__ __forceinline__ long long row_at(const Cache &
         return pos * c.kv_st;
     }
 }
+// The same in two steps: the row's number in the pool (a page's rows one after another; below 2^32), and its offset.
+__device__ __forceinline__ unsigned row_number(const PagedCache &cache, const int *row, int pos) {
+    const int page = valid_page(cache.pages, __ldg(row + (pos >> cache.pages.shift)));
+    return ((unsigned)page << cache.pages.shift) + (unsigned)(pos & (cache.pages.P - 1));
+}
+__device__ __forceinline__ long long row_offset(const PagedCache &cache, const Call &c, unsigned number) {
+    return (number >> cache.pages.shift) * cache.pages.s_page + (number & (unsigned)(cache.pages.P - 1)) * c.kv_st;
+}
 
 template <typename T, int D, int GT, class Cache = FlatCache>
 __global__ void __launch_bounds__(kScoreThreads)
@@ -540,6 +548,20 @@ decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restr
     int piece = 0;
     const int slot = warp * RPI + rsel;
 
+    // Paged cache: the rows of a step are looked up while the one before it is worked on (16 sequences of 40000 tokens, 32/8 heads:
+    // 146 us a step with the look-up before the loads, 132 us over flat caches).
+    unsigned ahead[Cache::kPaged ? U : 1];
+    auto look_up = [&](long long f0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long f = f0 + u * kSlots + slot;
+            if (f < f_end) {
+                while (f >= s_cum[piece + 1]) ++piece;
+                if constexpr (Cache::kPaged) ahead[u] = row_number(cache, row, s_start[piece] + (int)(f - s_cum[piece]));
+            }
+        }
+    };
+    if constexpr (Cache::kPaged) look_up(f_begin);
     for (long long f0 = f_begin; f0 < f_end; f0 += kSlots * U) {
         uint4 kraw[U][C], vraw[U][C];
         bool ok[U];
@@ -548,8 +570,13 @@ decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restr
             const long long f = f0 + u * kSlots + slot;
             ok[u] = f < f_end;
             if (ok[u]) {
-                while (f >= s_cum[piece + 1]) ++piece;
-                const long long at = row_at(cache, c, row, s_start[piece] + (f - s_cum[piece]));
+                long long at;
+                if constexpr (Cache::kPaged) {
+                    at = row_offset(cache, c, ahead[u]);
+                } else {
+                    while (f >= s_cum[piece + 1]) ++piece;
+                    at = row_at(cache, c, row, s_start[piece] + (f - s_cum[piece]));
+                }
 #pragma unroll
                 for (int ch = 0; ch < C; ++ch) {
                     kraw[u][ch] = __ldg(reinterpret_cast<const uint4 *>(kbase + at + (ch * LPR + sub) * E));
@@ -563,6 +590,7 @@ decode_attn(const T *__restrict__ q_s, const T *__restrict__ q, const T *__restr
                 }
             }
         }
+        if constexpr (Cache::kPaged) look_up(f0 + kSlots * U);
         float x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
