@@ -134,25 +134,26 @@ def load_library():
     lib.sla_probe_l2_read.argtypes = [vp, vp, sz, C.c_int32, vp, vp]
     lib.sla_selftest_wait_expiry.restype = i32
     lib.sla_selftest_wait_expiry.argtypes = [vp, C.c_int32, vp, vp]
-    CP, BP, f32 = C.POINTER(sla_cache_t), C.POINTER(sla_batch_t), C.c_float
+    # (the structs of the paged calls go by address: a serving step is a handful of calls of a few microseconds each)
+    f32 = C.c_float
     lib.sla_paged_workspace_bytes.restype = sz
-    lib.sla_paged_workspace_bytes.argtypes = [CP, i32, i32, i32, PP]
+    lib.sla_paged_workspace_bytes.argtypes = [vp, i32, i32, i32, PP]
     lib.sla_cache_extend.restype = i32
-    lib.sla_cache_extend.argtypes = [vp, CP, BP, vp, vp]
+    lib.sla_cache_extend.argtypes = [vp, vp, vp, vp, vp]
     lib.sla_cache_append.restype = i32
-    lib.sla_cache_append.argtypes = [vp, CP, BP, vp, vp, vp, i64, i64, vp]
+    lib.sla_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp]
     lib.sla_cache_release.restype = i32
-    lib.sla_cache_release.argtypes = [vp, CP, vp, i32, vp]
+    lib.sla_cache_release.argtypes = [vp, vp, vp, i32, vp]
     lib.sla_cache_fork.restype = i32
-    lib.sla_cache_fork.argtypes = [vp, CP, vp, vp, i32, vp, vp]
+    lib.sla_cache_fork.argtypes = [vp, vp, vp, vp, i32, vp, vp]
     lib.sla_cache_compact.restype = i32
-    lib.sla_cache_compact.argtypes = [vp, CP, vp, vp]
+    lib.sla_cache_compact.argtypes = [vp, vp, vp, vp]
     lib.sla_cache_copy.restype = i32
-    lib.sla_cache_copy.argtypes = [vp, CP, vp, i32, vp]
+    lib.sla_cache_copy.argtypes = [vp, vp, vp, i32, vp]
     lib.sla_paged_attention.restype = i32
-    lib.sla_paged_attention.argtypes = [vp, vp, CP, BP, i32, i64, i64, i32, f32, vp, vp, vp]
+    lib.sla_paged_attention.argtypes = [vp, vp, vp, vp, i32, i64, i64, i32, f32, vp, vp, vp]
     lib.sla_paged_decode_step.restype = i32
-    lib.sla_paged_decode_step.argtypes = [vp, vp, vp, CP, BP, i64, i32, i64, i64, PP, vp, vp, vp, vp, vp]
+    lib.sla_paged_decode_step.argtypes = [vp, vp, vp, vp, vp, i64, i32, i64, i64, PP, vp, vp, vp, vp, vp]
     lib.sla_pattern_offsets.restype = C.c_int32
     lib.sla_pattern_offsets.argtypes = [C.c_double, i64, vp, C.c_int32]
     lib.sla_pattern_len_steps.restype = C.c_int32
@@ -487,7 +488,7 @@ def sla_decode_shard_merge(handle: Handle, all_partial: torch.Tensor, q_like: to
 
 
 def _int32(t: torch.Tensor, what: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or not t.is_contiguous():
+    if t.dtype is not torch.int32 or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor")
     return t
 
@@ -508,6 +509,7 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: 
     c = sla_cache_t(n_pages, page, hkv, d, _dtype_code(k), 0, table.shape[0], table.shape[1], k.stride(0), k.stride(1),
                     k.stride(2), k.data_ptr(), v.data_ptr(), table.data_ptr(), n_tokens.data_ptr(), ref.data_ptr())
     c.tensors = (k, v, table, n_tokens, ref)
+    c.address = C.addressof(c)
     return c
 
 
@@ -534,7 +536,7 @@ def sla_paged_workspace_bytes(cache: sla_cache_t, n_q_heads: int, n_seqs: int, n
                               params: Optional[sla_params_t] = None) -> int:
     """Workspace that the paged calls need for batches of up to n_seqs sequences and n_new tokens; params: of
     sla_paged_decode_step, None when it is not called."""
-    return int(load_library().sla_paged_workspace_bytes(C.byref(cache), int(n_q_heads), int(n_seqs), int(n_new),
+    return int(load_library().sla_paged_workspace_bytes(cache.address, int(n_q_heads), int(n_seqs), int(n_new),
                                                         None if params is None else C.byref(params)))
 
 
@@ -548,7 +550,7 @@ def sla_cache_extend(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     rows = n if cu_new is None or n == 0 else 0x7FFFFFFF if n_new is None else int(n_new)
     b = sla_batch_t(n, rows, 1 if cu_new is None else rows, 0, None if seq is None else _int32(seq, "seq").data_ptr(),
                     None if cu_new is None else _int32(cu_new, "cu_new").data_ptr())
-    handle.check(handle._lib.sla_cache_extend(handle.ptr, C.byref(cache), C.byref(b), first.data_ptr(), _stream_ptr(stream)),
+    handle.check(handle._lib.sla_cache_extend(handle.ptr, cache.address, C.addressof(b), first.data_ptr(), _stream_ptr(stream)),
                  "sla_cache_extend")
     return first
 
@@ -563,14 +565,14 @@ def sla_cache_append(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     b = _batch(cu_new, k_new.shape[0], None, seq)
     if _int32(first, "first").numel() != b.n_seqs:
         raise ValueError("first must have one entry per sequence")
-    handle.check(handle._lib.sla_cache_append(handle.ptr, C.byref(cache), C.byref(b), first.data_ptr(), k_new.data_ptr(),
+    handle.check(handle._lib.sla_cache_append(handle.ptr, cache.address, C.addressof(b), first.data_ptr(), k_new.data_ptr(),
                                               v_new.data_ptr(), k_new.stride(0), k_new.stride(1), _stream_ptr(stream)),
                  "sla_cache_append")
 
 
 def sla_cache_release(handle: Handle, cache: sla_cache_t, seq: torch.Tensor, *, stream=None) -> None:
     """Ends the sequences in the slots `seq` (int32, device)."""
-    handle.check(handle._lib.sla_cache_release(handle.ptr, C.byref(cache), _int32(seq, "seq").data_ptr(), seq.numel(),
+    handle.check(handle._lib.sla_cache_release(handle.ptr, cache.address, _int32(seq, "seq").data_ptr(), seq.numel(),
                                                _stream_ptr(stream)), "sla_cache_release")
 
 
@@ -581,7 +583,7 @@ def sla_cache_fork(handle: Handle, cache: sla_cache_t, src: torch.Tensor, dst: t
         raise ValueError("src and dst must have the same length")
     if pairs is None:
         pairs = torch.empty(2, n, dtype=torch.int32, device=_device_of(cache))
-    handle.check(handle._lib.sla_cache_fork(handle.ptr, C.byref(cache), src.data_ptr(), dst.data_ptr(), n, pairs.data_ptr(),
+    handle.check(handle._lib.sla_cache_fork(handle.ptr, cache.address, src.data_ptr(), dst.data_ptr(), n, pairs.data_ptr(),
                                             _stream_ptr(stream)), "sla_cache_fork")
     return pairs
 
@@ -590,7 +592,7 @@ def sla_cache_compact(handle: Handle, cache: sla_cache_t, *, pairs=None, stream=
     """Moves the pages in use to the front of the pool -> pairs int32 [2, n_pages] of the moves, then -1."""
     if pairs is None:
         pairs = torch.empty(2, cache.n_pages, dtype=torch.int32, device=_device_of(cache))
-    handle.check(handle._lib.sla_cache_compact(handle.ptr, C.byref(cache), pairs.data_ptr(), _stream_ptr(stream)),
+    handle.check(handle._lib.sla_cache_compact(handle.ptr, cache.address, pairs.data_ptr(), _stream_ptr(stream)),
                  "sla_cache_compact")
     return pairs
 
@@ -599,7 +601,7 @@ def sla_cache_copy(handle: Handle, cache: sla_cache_t, pairs: torch.Tensor, *, s
     """Copies pages pairs[0] to pages pairs[1] (int32 [2, n]; pairs with a negative entry are skipped)."""
     if _int32(pairs, "pairs").dim() != 2 or pairs.shape[0] != 2:
         raise ValueError("pairs must be [2, n]")
-    handle.check(handle._lib.sla_cache_copy(handle.ptr, C.byref(cache), pairs.data_ptr(), pairs.shape[1], _stream_ptr(stream)),
+    handle.check(handle._lib.sla_cache_copy(handle.ptr, cache.address, pairs.data_ptr(), pairs.shape[1], _stream_ptr(stream)),
                  "sla_cache_copy")
 
 
@@ -618,7 +620,7 @@ def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_
     if lse is None:
         lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
     b = _batch(cu_new, T, max_new, seq)
-    rc = handle._lib.sla_paged_attention(handle.ptr, q.data_ptr(), C.byref(cache), C.byref(b), Hq, q.stride(0), q.stride(1),
+    rc = handle._lib.sla_paged_attention(handle.ptr, q.data_ptr(), cache.address, C.addressof(b), Hq, q.stride(0), q.stride(1),
                                          int(window), 1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale,
                                          out.data_ptr(), lse.data_ptr(), _stream_ptr(stream))
     if rc != SLA_OK:
@@ -643,7 +645,7 @@ def sla_paged_decode_step(handle: Handle, q_s: torch.Tensor, q: torch.Tensor, ca
     out_score = torch.empty(B, Hq, params.top_k, dtype=torch.float32, device=dev) if out_score is None else out_score
     b = _batch(None, B, 1, seq)
     most = cache.table_width * cache.page_tokens if max_tokens is None else int(max_tokens)
-    rc = handle._lib.sla_paged_decode_step(handle.ptr, q_s.data_ptr(), q.data_ptr(), C.byref(cache), C.byref(b), most, Hq,
+    rc = handle._lib.sla_paged_decode_step(handle.ptr, q_s.data_ptr(), q.data_ptr(), cache.address, C.addressof(b), most, Hq,
                                            q.stride(0), q.stride(1), C.byref(params), out.data_ptr(), lse.data_ptr(),
                                            out_anchor.data_ptr(), out_score.data_ptr(), _stream_ptr(stream))
     if rc != SLA_OK:

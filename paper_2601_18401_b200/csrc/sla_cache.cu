@@ -351,6 +351,7 @@ __host__ __device__ inline int chunk_pages(int n_pages) {
 
 __device__ inline int count_live(const int *ref, int lo, int hi, int *s_warp) {
     int mine = 0;
+#pragma unroll 4
     for (int q = lo + threadIdx.x; q < hi; q += kPlanThreads) mine += ref[q] > 0;
     int total;
     cta_scan(mine, s_warp, total);
@@ -387,17 +388,26 @@ __global__ void __launch_bounds__(kPlanThreads) compact_rank(Pages p, int per, i
     const int n_moves = live - below;   // pages in use at or above `live`: as many as are free below it
     if (blockIdx.x == 0 && c == 0) *n_moves_out = n_moves;
     int upto = s_before;
-    for (int p0 = blockIdx.x * per; p0 < min((int)(blockIdx.x + 1) * per, p.n_pages); p0 += kPlanThreads) {
-        const int q = p0 + c;
-        const int on = q < p.n_pages && p.ref[q] > 0;
+    for (int p0 = blockIdx.x * per; p0 < min((int)(blockIdx.x + 1) * per, p.n_pages); p0 += 4 * kPlanThreads) {
+        const int q0 = p0 + 4 * c;   // four pages a thread
+        int on = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (q0 + e < p.n_pages && p.ref[q0 + e] > 0) on |= 1 << e;
         int total;
-        const int before = upto + cta_scan(on, s_warp, total) - on;   // pages in use below q
+        int before = upto + cta_scan(__popc(on), s_warp, total) - __popc(on);   // pages in use below q
         upto += total;
-        if (q >= p.n_pages) continue;
-        if (q >= n_moves) pairs[q] = pairs[p.n_pages + q] = -1;
-        rank[q] = on && q >= live ? before - below : -1;
-        if (on && q >= live) pairs[before - below] = q;
-        if (!on && q < live) pairs[p.n_pages + q - before] = q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int q = q0 + e, is = on >> e & 1;
+            if (q < p.n_pages) {
+                if (q >= n_moves) pairs[q] = pairs[p.n_pages + q] = -1;
+                rank[q] = is && q >= live ? before - below : -1;
+                if (is && q >= live) pairs[before - below] = q;
+                if (!is && q < live) pairs[p.n_pages + q - before] = q;
+            }
+            before += is;
+        }
     }
 }
 

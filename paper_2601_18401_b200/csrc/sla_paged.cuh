@@ -70,8 +70,12 @@ struct PagedCall {
 
 // The work of a call is a list of units -- (sequence, KV head, TQ consecutive new tokens with all G heads of the group) -- each
 // with the tiles of KT keys that its tokens see, written down as a running sum of weights (tiles + kUnitWeight, what a unit costs
-// beyond its tiles).  The list is cut into n_ranges equal ranges, wherever that falls: every CTA gets the same share of
-// the keys whatever the lengths are.  A unit that is cut leaves partial results, joined by paged_merge.
+// beyond its tiles).  The list is cut into equal ranges, wherever that falls: every CTA gets the same share of the keys whatever the
+// lengths are.  A unit that is cut leaves partial results, joined by paged_merge.  Where several units read the same keys and these
+// are too many for L2, the ranges are a multiple of the CTAs, who go through the list together: each multiple reads kGroupBytes.
+// (Not below kGroupWeight a range, where the cuts cost more: 1999 tokens at 30011, three multiples 980 us and one 925 us; 8192 tokens
+// that end at 65536, six multiples 6670 us and one 7180 us.  Claimed ranges of falling sizes for CTAs that are done early gave nothing:
+// 945 us and 7100 us.)
 struct Plan {
     long long *seq_at;    // [n_seqs + 1] weight before sequence x
     int *unit_at;         // [n_seqs + 1] units of one head before sequence x
@@ -80,12 +84,12 @@ struct Plan {
     int max_units;        // room in unit_end
 };
 constexpr int kUnitWeight = 2;
+constexpr long long kGroupBytes = 48ll << 20, kGroupWeight = 400;
 // How a kernel cuts a call up: TQ new tokens a unit, tiles of 1 << kt_shift keys.  Units of at most `small` tokens go through two tiles at
 // a time (sla_paged_tiles.cu): their tiles weigh half.
 struct Shape {
     int TQ, kt_shift, small;
 };
-constexpr long long kGroupBytes = 48ll << 20;   // of keys and values that the CTAs go through at one time
 
 // Keys of the new tokens [t0, t1) of a sequence of n tokens, q of them new: tiles [lo, hi) of KT keys.
 __device__ __forceinline__ void unit_tiles(int n, int q, int t0, int t1, int window, int kt_shift, int &lo, int &hi) {
@@ -102,8 +106,6 @@ __device__ __forceinline__ int unit_weight(int n, int q, int t0, int t1, int win
 }
 
 // A CTA builds the plan (all threads call it; the arrays are visible to the CTA on return).
-// `groups`: the ranges are a multiple of n_ctas when the list is long, so that CTAs work on neighbouring units at any time
-// and share what they read in L2.
 template <int kThreads>
 __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas, int max_groups, int min_weight, const Plan &plan,
                                   long long *s_sum) {
@@ -207,6 +209,7 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
         for (int w = 0; w < kWarps; ++w) bytes += s_sum[w];
         const long long total = plan.seq_at[a.b.n_seqs];
         long long groups = (bytes + kGroupBytes - 1) / kGroupBytes;
+        if (groups > total / (n_ctas * kGroupWeight)) groups = total / (n_ctas * kGroupWeight);
         groups = groups < 1 ? 1 : groups > max_groups ? max_groups : groups;
         long long n = groups * n_ctas;
         if (n > total / min_weight) n = total / min_weight;   // a range of a few tiles at least
@@ -230,7 +233,18 @@ __device__ __forceinline__ int warp_last_le(const long long *a, int n, long long
     return lo;
 }
 
-__device__ __forceinline__ long long range_at(long long total, int n_ranges, int r) { return total * r / n_ranges; }
+// The ranges of a list of `total` weight.
+struct Ranges {
+    long long total;
+    int count;
+    __device__ __forceinline__ long long at(int r) const { return total * r / count; }   // where range r begins
+    __device__ __forceinline__ int holding(long long p) const {                          // the range of position p
+        int r = min(max((int)((double)p * count / (double)total), 0), count - 1);
+        while (r > 0 && at(r) > p) --r;
+        while (at(r + 1) <= p) ++r;
+        return r;
+    }
+};
 
 // What one CTA does of one unit.
 struct Segment {
@@ -243,17 +257,16 @@ struct Segment {
 
 // Goes through the segments of range r.  All warps that need a segment run a cursor of their own, converged, and see the same.
 struct Cursor {
-    long long w, end, total;
-    int x, head, unit, units, r, n_ranges;
-    bool first;
+    Ranges ranges;
+    long long w, end;
+    int x, head, unit, units, r;
 
     __device__ __forceinline__ bool start(const PagedCall &a, const Plan &plan, int range) {
-        n_ranges = *plan.n_ranges;
+        ranges = {plan.seq_at[a.b.n_seqs], *plan.n_ranges};
         r = range;
-        if (r >= n_ranges) return false;
-        total = plan.seq_at[a.b.n_seqs];
-        w = range_at(total, n_ranges, r);
-        end = range_at(total, n_ranges, r + 1);
+        if (r >= ranges.count) return false;
+        w = ranges.at(r);
+        end = ranges.at(r + 1);
         x = warp_last_le(plan.seq_at, a.b.n_seqs, w);
         units = plan.unit_at[x + 1] - plan.unit_at[x];
         const long long *ue = plan.unit_end + plan.unit_at[x];
@@ -261,7 +274,6 @@ struct Cursor {
         head = (int)(rem / per_head);
         const long long in = rem - head * per_head;
         unit = ue[0] > in ? 0 : warp_last_le(ue, units, in) + 1;
-        first = true;
         return w < end;
     }
     // the segment at the cursor; false when the range is done.  *last_range: for a unit that starts in this range and does not
@@ -298,13 +310,7 @@ struct Cursor {
         s.hi = min(lo + per * max(to - kUnitWeight, 0), hi);
         const bool begins = from == 0, ends = end >= stop;
         s.part = begins && ends ? -1 : begins ? 2 * r + 1 : 2 * r;
-        if (begins && !ends) {
-            int z = (int)(((double)stop * n_ranges) / (double)total);
-            z = min(max(z, r), n_ranges - 1);
-            while (z > r && range_at(total, n_ranges, z) >= stop) --z;
-            while (range_at(total, n_ranges, z + 1) < stop) ++z;
-            last_range = z;
-        }
+        if (begins && !ends) last_range = ranges.holding(stop - 1);
         w = end < stop ? end : stop;
         ++unit;
         return true;

@@ -308,91 +308,86 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
 }
 
 // ------------------------------------------------------------------------------------------------
-// blockIdx.x: the range a cut unit starts in.  A warp takes kMergeRows rows at a time, blockIdx.y and the warp saying which, and requests
+// blockIdx.x: the range a cut unit starts in.  A warp takes kMergeRows rows, blockIdx.y and the warp saying which, and requests
 // two parts of each together: bound by the latency of two dependent loads where units have few parts.  Row i of a unit is token
 // i / G of sub-tile i / RS (TS tokens each).
 constexpr int kMergeRows = 4;
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 2) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
+__global__ void __launch_bounds__(256, 3) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int N = D / 32, kParts = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     chain_wait();
-    const int n_ranges = *plan.n_ranges;
-    Cut cut = parts.cut[blockIdx.x];   // (beyond n_ranges: not looked at)
-    for (int r = blockIdx.x; r < n_ranges;) {
-        const int n_parts = cut.last - r + 1;
-        const int rows = cut.last < 0 ? 0 : R;
-        for (int i0 = (blockIdx.y * 8 + warp) * kMergeRows; i0 < rows; i0 += gridDim.y * 8 * kMergeRows) {
-            int t[kMergeRows], h[kMergeRows];
-            bool on[kMergeRows], any = false;
-            float mx[kMergeRows], sum[kMergeRows], acc[kMergeRows][N];
+    const int r = blockIdx.x, n_ranges = *plan.n_ranges;
+    const Cut cut = parts.cut[r];   // (beyond n_ranges: not looked at)
+    if (r >= n_ranges || cut.last < 0) return;
+    const int n_parts = cut.last - r + 1;
+    const int i0 = (blockIdx.y * 8 + warp) * kMergeRows;
+    int t[kMergeRows], h[kMergeRows];
+    bool on[kMergeRows], any = false;
+    float mx[kMergeRows], sum[kMergeRows], acc[kMergeRows][N];
 #pragma unroll
-            for (int u = 0; u < kMergeRows; ++u) {
-                const int i = i0 + u, in = i % RS;
-                t[u] = i / RS * TS + in / a.G;
-                h[u] = cut.head * a.G + in % a.G;
-                on[u] = in < TS * a.G && t[u] < cut.tokens;
-                any |= on[u];
-                mx[u] = -CUDART_INF_F;
-                sum[u] = 0.f;
+    for (int u = 0; u < kMergeRows; ++u) {
+        const int i = i0 + u, in = i % RS;
+        t[u] = i / RS * TS + in / a.G;
+        h[u] = cut.head * a.G + in % a.G;
+        on[u] = in < TS * a.G && t[u] < cut.tokens;
+        any |= on[u];
+        mx[u] = -CUDART_INF_F;
+        sum[u] = 0.f;
 #pragma unroll
-                for (int d = 0; d < N; ++d) acc[u][d] = 0.f;
-            }
-            if (!any) continue;
-            for (int e0 = 0; e0 < n_parts; e0 += kParts) {
-                float z[kMergeRows][kParts], v[kMergeRows][kParts][N];
+        for (int d = 0; d < N; ++d) acc[u][d] = 0.f;
+    }
+    if (!any) return;
+    for (int e0 = 0; e0 < n_parts; e0 += kParts) {
+        float z[kMergeRows][kParts], v[kMergeRows][kParts][N];
 #pragma unroll
-                for (int u = 0; u < kMergeRows; ++u)
+        for (int u = 0; u < kMergeRows; ++u)
 #pragma unroll
-                    for (int e = 0; e < kParts; ++e) {
-                        // (a part that is not there: the first one's place, without a weight; of a part without keys the sums
-                        // were not written, and are not used)
-                        const int part = e0 + e == 0 || e0 + e >= n_parts ? 2 * r + 1 : 2 * (r + e0 + e);
-                        const long long at = (long long)part * R + i0 + u;
-                        z[u][e] = __ldcg(parts.lse2 + at);
-                        const float *src = parts.o + at * D + lane * N;
-                        if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u][e]) = __ldcg(reinterpret_cast<const float4 *>(src));
-                        else *reinterpret_cast<float2 *>(v[u][e]) = __ldcg(reinterpret_cast<const float2 *>(src));
-                        if (e0 + e >= n_parts) z[u][e] = -CUDART_INF_F;
-                    }
-#pragma unroll
-                for (int u = 0; u < kMergeRows; ++u) {
-                    float top = mx[u];   // a NaN reaches the result through its weight
-#pragma unroll
-                    for (int e = 0; e < kParts; ++e) top = fmaxf(top, z[u][e]);
-                    const float keep = mx[u] == top ? 1.f : exp2f(mx[u] - top);
-                    mx[u] = top;
-                    sum[u] *= keep;
-#pragma unroll
-                    for (int d = 0; d < N; ++d) acc[u][d] *= keep;
-#pragma unroll
-                    for (int e = 0; e < kParts; ++e) {
-                        if (z[u][e] == -CUDART_INF_F) continue;
-                        const float w = exp2f(z[u][e] - top);
-                        sum[u] += w;
-#pragma unroll
-                        for (int d = 0; d < N; ++d) acc[u][d] = fmaf(w, v[u][e][d], acc[u][d]);
-                    }
-                }
+            for (int e = 0; e < kParts; ++e) {
+                // (a part that is not there: the first one's place, without a weight; of a part without keys the sums
+                // were not written, and are not used)
+                const int part = e0 + e == 0 || e0 + e >= n_parts ? 2 * r + 1 : 2 * (r + e0 + e);
+                const long long at = (long long)part * R + i0 + u;
+                z[u][e] = __ldcg(parts.lse2 + at);
+                const float *src = parts.o + at * D + lane * N;
+                if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u][e]) = __ldcg(reinterpret_cast<const float4 *>(src));
+                else *reinterpret_cast<float2 *>(v[u][e]) = __ldcg(reinterpret_cast<const float2 *>(src));
+                if (e0 + e >= n_parts) z[u][e] = -CUDART_INF_F;
             }
 #pragma unroll
-            for (int u = 0; u < kMergeRows; ++u) {
-                if (!on[u]) continue;
-                const bool none = mx[u] == -CUDART_INF_F && sum[u] == 0.f;
-                const float inv = none ? 0.f : 1.f / sum[u];
-                const long long row = cut.row0 + t[u];
-                T *o = out + row * a.q_st + (long long)h[u] * a.q_sh + lane * N;
-                alignas(16) T w[N];
+        for (int u = 0; u < kMergeRows; ++u) {
+            float top = mx[u];   // a NaN reaches the result through its weight
 #pragma unroll
-                for (int d = 0; d < N; ++d) w[d] = from_float<T>(acc[u][d] * inv);
-                if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<const uint4 *>(w);
-                else if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<const uint2 *>(w);
-                else *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<const uint32_t *>(w);
-                if (lane == 0) lse[row * a.Hq + h[u]] = none ? -CUDART_INF_F : (mx[u] + log2f(sum[u])) * kLn2;
+            for (int e = 0; e < kParts; ++e) top = fmaxf(top, z[u][e]);
+            const float keep = mx[u] == top ? 1.f : exp2f(mx[u] - top);
+            mx[u] = top;
+            sum[u] *= keep;
+#pragma unroll
+            for (int d = 0; d < N; ++d) acc[u][d] *= keep;
+#pragma unroll
+            for (int e = 0; e < kParts; ++e) {
+                if (z[u][e] == -CUDART_INF_F) continue;
+                const float w = exp2f(z[u][e] - top);
+                sum[u] += w;
+#pragma unroll
+                for (int d = 0; d < N; ++d) acc[u][d] = fmaf(w, v[u][e][d], acc[u][d]);
             }
         }
-        r += gridDim.x;
-        if (r < n_ranges) cut = parts.cut[r];
+    }
+#pragma unroll
+    for (int u = 0; u < kMergeRows; ++u) {
+        if (!on[u]) continue;
+        const bool none = mx[u] == -CUDART_INF_F && sum[u] == 0.f;
+        const float inv = none ? 0.f : 1.f / sum[u];
+        const long long row = cut.row0 + t[u];
+        T *o = out + row * a.q_st + (long long)h[u] * a.q_sh + lane * N;
+        alignas(16) T w[N];
+#pragma unroll
+        for (int d = 0; d < N; ++d) w[d] = from_float<T>(acc[u][d] * inv);
+        if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<const uint4 *>(w);
+        else if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<const uint2 *>(w);
+        else *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<const uint32_t *>(w);
+        if (lane == 0) lse[row * a.Hq + h[u]] = none ? -CUDART_INF_F : (mx[u] + log2f(sum[u])) * kLn2;
     }
 }
 
@@ -421,7 +416,7 @@ cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scra
 template <typename T, int D>
 static cudaError_t merge_of(const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
     const int per = 8 * kMergeRows;
-    return launch_chained(paged_merge<T, D>, dim3(p.n_ctas, (p.R + per - 1) / per), dim3(256), 0, st, a, p.R, p.RS, p.TS, plan_at(p, scratch),
+    return launch_chained(paged_merge<T, D>, dim3(p.n_ctas * p.max_groups, p.R / per), dim3(256), 0, st, a, p.R, p.RS, p.TS, plan_at(p, scratch),
                           parts_at(p, scratch), (T *)out, lse);
 }
 

@@ -398,8 +398,9 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
     if (n_ranges < 1) n_ranges = 1;
     const int r = blockIdx.x;
     if (r >= n_ranges || total == 0) return;
-    long long w = range_at(total, n_ranges, r);
-    const long long w_end = range_at(total, n_ranges, r + 1);
+    const Ranges ranges = {total, n_ranges};
+    long long w = ranges.at(r);
+    const long long w_end = ranges.at(r + 1);
     if (w >= w_end) return;
     int x = warp_last_le(s_seq_at, n_seqs, w);
     long long per_head = (s_seq_at[x + 1] - s_seq_at[x]) / a.c.Hkv;
@@ -460,14 +461,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
         }
         if (part >= 0) {
             // ranges [r0, r1] hold this unit
-            auto range_of = [&](long long p) {   // the range of position p
-                int z = (int)((double)p * n_ranges / (double)total);
-                z = min(max(z, 0), n_ranges - 1);
-                while (z > 0 && range_at(total, n_ranges, z) > p) --z;
-                while (range_at(total, n_ranges, z + 1) <= p) ++z;
-                return z;
-            };
-            const int r0 = begins ? r : range_of(start), r1 = ends ? r : range_of(stop - 1), n_parts = r1 - r0 + 1;
+            const int r0 = begins ? r : ranges.holding(start), r1 = ends ? r : ranges.holding(stop - 1), n_parts = r1 - r0 + 1;
             __threadfence();
             __syncthreads();
             if (tid == 0) {

@@ -857,9 +857,11 @@ void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.kt_shift = kTileShift;
     p.small = p.TS;
     p.n_ctas = sm_count;
-    // more ranges than CTAs only where the keys that several units read may not fit L2 (see build_plan)
-    const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * a.c.D * a.c.es * 2, groups = (bytes + kGroupBytes - 1) / kGroupBytes;
-    p.max_groups = groups < 8 ? (int)groups : 8;
+    // (a bound that does not ask the number of SMs, so that the workspace can be sized without a device)
+    const long long units = a.b.n_new / p.TQ + a.b.n_seqs, weight = units * a.c.Hkv * (((long long)a.c.width << a.c.shift) / kKeys + 1 + kUnitWeight);
+    const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * a.c.D * a.c.es * 2, groups = bytes / kGroupBytes + 1;
+    const long long most = groups < weight / (128 * kGroupWeight) ? groups : weight / (128 * kGroupWeight);
+    p.max_groups = most < 1 ? 1 : most < 8 ? (int)most : 8;
     p.min_weight = 6;
 }
 
