@@ -301,11 +301,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 const int lo = s.lo, hi = s.hi, lx = s.lo_x[x], hx = s.hi_x[x], valid = s.valid, odd = s.step - 1;
                 ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
                 if (!valid) break;
+                bool k_there = false;   // K of the tile has been waited for
 #pragma unroll 1
                 for (int j = lo; j < hi; ++j) {
                     const bool on = j >= lx && j < hx && !((j - lx) & odd);
                     uint32_t st = i % kStages;
-                    if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
+                    if (!k_there && !(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
+                    k_there = false;
                     if (on) {
                         if (j == lx && !(ok = ptx::mbar_wait(bar_q_full + 8 * x, ns & 1u, abort_flag))) break;
                         ptx::tc_fence_after();
@@ -329,6 +331,10 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (on) {
                         // the first PV of a segment overwrites O: the results of the segment before have been read
                         if (j == lx && ns > 0 && !(ok = ptx::mbar_wait(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
+                        if (j + 1 < hi) {   // off the way from P to the next S
+                            k_there = true;
+                            if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1u, abort_flag))) break;
+                        }
                         const uint64_t dv = desc_advance(dv0, st * L::kTileBytes);
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
@@ -645,15 +651,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         fresh = false;
                     }
                     const float neg_m = fresh ? 0.f : -m_ref;   // a row with no key so far: -inf stays -inf
-                    unsigned long long sc2 = pack2(scale2, scale2), nm2 = pack2(neg_m, neg_m);
+                    const unsigned long long sc2 = pack2(scale2, scale2), nm2 = pack2(neg_m, neg_m);
                     unsigned long long acc2[4];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) acc2[u] = pack2(0.f, 0.f);
                     const bool edge = k0 + kKeys - 1 > all_hi || k0 < all_lo;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        // keeps the compiler from working on the second half before the first is handed over
-                        asm volatile("" : "+l"(sc2), "+l"(nm2));
                         uint32_t pk[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
