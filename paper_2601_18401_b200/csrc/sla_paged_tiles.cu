@@ -42,6 +42,9 @@ constexpr int kTmemCols = 512;
 constexpr uint32_t kColO = 0, kColS = 256;   // + 128 per stream
 constexpr int kSegs = 2;            // entries of the ring of segments
 constexpr float kRescaleThreshold = 8.f;     // log2 units
+// The streams' products are kept at least this many cycles apart.  A stream's tile takes about 3400 cycles of which 1000 are products and 1200
+// exponentials; where both streams come to the same pipe at the same time it takes 4000, and nothing moves them apart again.
+constexpr uint32_t kApart = 1300;
 constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns, those whose exponentials go to the FMA pipe
 constexpr int kRegsRow = 184, kRegsRest = 72;
 static_assert(2 * kRegsRow + 2 * kRegsRest <= 4 * 128, "more registers than the block is launched with");
@@ -69,6 +72,7 @@ struct Meta {
         seg_full[kSegs], seg_empty[kSegs], checked[2];
     uint32_t tmem_base;
     int abort_flag;
+    uint32_t s_time[2];               // clock at the stream's last S
     // [stream][segment & 7]: the segment (counted from 1) if it has a value that is not finite.  Whoever finds one says so to both
     // streams before it clears the value; the ring of ten stages at most (a tile of K and of V each) keeps the streams less than eight segments with tiles apart.
     int odd[2][8];
@@ -255,6 +259,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             ptx::mbar_init(bar_seg_empty + 8 * s, 13 + 2 * 32);   // rows, epilogue, K/V: a warp each; the issuers a lane each
         }
         meta->abort_flag = 0;
+        meta->s_time[0] = meta->s_time[1] = clock();
         for (int s = 0; s < 8; ++s) meta->odd[0][s] = meta->odd[1][s] = 0;
         ptx::fence_barrier_init();
     }
@@ -311,6 +316,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (on) {
                         if (j == lx && !(ok = ptx::mbar_wait(bar_q_full + 8 * x, ns & 1u, abort_flag))) break;
                         ptx::tc_fence_after();
+                        {
+                            volatile uint32_t *s_time = meta->s_time;
+                            const uint32_t other = s_time[1 - x];
+                            uint32_t now;
+                            do now = clock(); while (now - other < kApart);
+                            s_time[x] = now;
+                        }
                         const uint64_t dk = desc_advance(dk0, st * L::kTileBytes);
                         if (leader) {
 #pragma unroll
