@@ -170,6 +170,97 @@ def test_strided_queries_slots_and_shared_pages(sla, handle, dtype):
     assert (out[:, 0] == 7).all() and (out[:, 2] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("G", [1, 3, 4, 8, 12])
+def test_queries_with_tokens_inside_heads(sla, handle, dtype, G):
+    """Queries stored head by head: [Hq, n_new, D] seen as [n_new, Hq, D]."""
+    for n, new in (SINGLE, CHUNKS, ([300, 41], [300, 41])):
+        cache, k, v, table, q, cu = build(sla, n, new, dtype=dtype, G=G)
+        q = q.transpose(0, 1).contiguous().transpose(0, 1)
+        out, lse = sla.sla_paged_attention(handle, q, cache, cu, max_new=max(new))
+        assert out.stride() == q.stride()
+        U.check_attention(out, lse, U.attention_reference(q, k, v, table, n, new, G, 0, 128 ** -0.5, 16), dtype)
+
+
+@pytest.mark.parametrize("dtype,n_seqs,new", [(BF16, 1100, 1), (F32, 1030, 1), (BF16, 1500, 3), (F32, 300, 2)])
+def test_many_sequences(sla, handle, dtype, n_seqs, new):
+    """More sequences than one launch, one warp or one CTA takes at a time."""
+    rs = np.random.RandomState(n_seqs)
+    n = rs.randint(0, 70, n_seqs)
+    c = np.minimum(n, rs.randint(0, new + 1, n_seqs)) if new > 1 else np.minimum(n, 1)
+    run(sla, handle, n.tolist(), c.tolist(), dtype=dtype, hkv=1, G=2, d=64, max_new=new)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_above_2_to_31(sla, handle, dtype):
+    """A pool of more than 2^31 elements: the pages of the sequences lie behind them."""
+    free = torch.cuda.mem_get_info()[0]
+    n_pages, hkv, page, d = 33000, 8, 64, 128
+    if free < 2.5 * n_pages * hkv * page * d * (2 if dtype == BF16 else 4):
+        pytest.skip("not enough device memory")
+    k, v = (torch.empty(n_pages, hkv, page, d, dtype=dtype, device="cuda:0") for _ in range(2))
+    table = np.full((2, 4), -1, dtype=np.int32)
+    table[0, :3], table[1, :1] = [32999, 32800, 40], [32900]
+    for p in (32999, 32800, 40, 32900):
+        k[p].normal_(), v[p].normal_()
+    n = [150, 40]
+    ref = np.zeros(n_pages, dtype=np.int32)
+    cache = sla.make_cache(k, v, U.device_ints(table), U.device_ints(n), U.device_ints(ref))
+    for new in ([1, 1], [100, 40]):
+        q = torch.empty(sum(new), 16, d, dtype=dtype, device="cuda:0").normal_()
+        out, lse = sla.sla_paged_attention(handle, q, cache, U.device_ints(np.concatenate([[0], np.cumsum(new)])), max_new=max(new))
+        U.check_attention(out, lse, U.attention_reference(q, k, v, table, n, new, 2, 0, d ** -0.5, page), dtype)
+    kn, vn = (torch.empty(2, hkv, d, dtype=dtype, device="cuda:0").normal_() for _ in range(2))
+    sla.sla_cache_append(handle, cache, None, U.device_ints([127, 39]), kn, vn)
+    assert torch.equal(k[32800, :, 63], kn[0]) and torch.equal(v[32900, :, 39], vn[1])
+    sla.sla_cache_copy(handle, cache, U.device_ints([[32999], [32998]]))
+    assert torch.equal(k[32998], k[32999]) and torch.equal(v[32998], v[32999])
+    del k, v, cache
+    torch.cuda.empty_cache()
+
+
+def test_calls_can_be_captured(sla):
+    """A step -- room, tokens, attention, the span step -- in a graph, replayed as the sequences grow."""
+    from paper_2601_18401_b200.paged import PagedCache
+    c = PagedCache(40, 3, 640, n_q_heads=8, n_kv_heads=2, page_tokens=32, max_new=512, params=sla.make_params(4, 0))
+    g = torch.Generator(device="cuda:0")
+    rand = lambda *s: torch.empty(*s, dtype=BF16, device="cuda:0").normal_(generator=g)  # noqa: E731
+    cu = U.device_ints([0, 90, 120, 311])
+    c.append(cu, c.extend(cu), rand(311, 2, 128), rand(311, 2, 128))
+    kn, vn, q, q_s = rand(3, 2, 128), rand(3, 2, 128), rand(3, 8, 128), rand(3, 8, 128)
+
+    def step():
+        first = c.extend()
+        c.append(None, first, kn, vn)
+        return c.attend(q), c.step(q_s, q, max_tokens=640)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(40):
+        graph.replay()
+    torch.cuda.synchronize()
+    n = [131, 71, 232]
+    assert c.n_tokens.tolist() == n and c.poll() == sla.SLA_OK
+    table = c.table.cpu().numpy()
+    U.check_attention(*got[0], U.attention_reference(q, c.k, c.v, table, n, [1, 1, 1], 4, 0, 128 ** -0.5, 32), BF16)
+    again = c.step(q_s, q, max_tokens=640)
+    assert all(torch.equal(a, b) for a, b in zip(got[1], again))
+
+
+def test_the_example_runs(sla):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_serving.py")
+    spec = importlib.util.spec_from_file_location("paged_serving", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    r = m.run(prompts=4, chunk=300, steps=6, span_from=1500)
+    assert r["status"] == sla.SLA_OK and r["worst"] < 2e-2
+    assert r["tokens"] == sum(200 + 777 * i for i in range(4)) + 3 * 7 + 3 * 6
+
+
 def test_chunk_bound_may_be_loose(sla, handle):
     """max_new is a bound: single tokens with a bound of many give the same results."""
     a, la, _ = run(sla, handle, *SINGLE)

@@ -1,0 +1,113 @@
+"""Host-only checks of the paged calls: workspace sizes, refusals before anything is launched, and the model the GPU tests use."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paged_util as U
+
+
+@pytest.fixture(scope="module")
+def sla():
+    from paper_2601_18401_b200 import build
+    build.build_library()
+    import paper_2601_18401_b200 as sla_pkg
+    return sla_pkg
+
+
+def cache_of(sla, n_pages=64, hkv=8, page=64, d=128, slots=4, width=32, dtype=torch.bfloat16):
+    k = torch.empty(n_pages, hkv, page, d, dtype=dtype)
+    ints = [torch.zeros(slots, width, dtype=torch.int32), torch.zeros(slots, dtype=torch.int32), torch.zeros(n_pages, dtype=torch.int32)]
+    return sla.make_cache(k, k.clone(), *ints)
+
+
+def test_workspace_sizes(sla):
+    c = cache_of(sla)
+    step, chunk = sla.sla_paged_workspace_bytes(c, 32, 4, 4), sla.sla_paged_workspace_bytes(c, 32, 4, 4096)
+    assert 0 < step <= chunk < 1 << 30
+    assert sla.sla_paged_workspace_bytes(c, 32, 4, 4, params=sla.make_params(8, 0)) >= step
+    assert sla.sla_paged_workspace_bytes(cache_of(sla, dtype=torch.float32, d=64), 8, 4, 100) > 0
+
+
+@pytest.mark.parametrize("change", [dict(page=8), dict(page=48), dict(page=512), dict(d=96)])
+def test_unsupported_shapes_have_no_workspace(sla, change):
+    assert sla.sla_paged_workspace_bytes(cache_of(sla, **change), 8, 1, 1) == 0
+
+
+def test_invalid_arguments_have_no_workspace(sla):
+    c = cache_of(sla)
+    assert sla.sla_paged_workspace_bytes(c, 12, 1, 1) == 0           # not a multiple of the KV heads
+    assert sla.sla_paged_workspace_bytes(c, 8 * 17, 1, 1) == 0       # groups of 17
+    assert sla.sla_paged_workspace_bytes(c, 32, -1, 1) == 0
+    assert sla.sla_paged_workspace_bytes(c, 32, 1, 1, params=sla.make_params(65, 0)) == 0
+    c.reserved = 1
+    assert sla.sla_paged_workspace_bytes(c, 32, 1, 1) == 0
+    c.reserved, c.stride_t = 0, 60
+    assert sla.sla_paged_workspace_bytes(c, 32, 1, 1) == 0
+    c.stride_t, c.table_width = 128, 1 << 30
+    assert sla.sla_paged_workspace_bytes(c, 32, 1, 1) == 0
+    c.table_width, c.n_pages = 32, 1 << 30
+    assert sla.sla_paged_workspace_bytes(c, 32, 1, 1) == 0
+
+
+def test_a_missing_handle_is_refused(sla):
+    lib, c = sla.load_library(), cache_of(sla)
+    b = sla.sla_batch_t(1, 1, 1, 0, None, None)
+    ca, ba = C.addressof(c), C.addressof(b)
+    assert lib.sla_cache_extend(None, ca, ba, 16, None) == -1
+    assert lib.sla_cache_append(None, ca, ba, 16, 16, 16, 128, 128, None) == -1
+    assert lib.sla_cache_release(None, ca, 16, 1, None) == -1
+    assert lib.sla_cache_fork(None, ca, 16, 16, 1, 16, None) == -1
+    assert lib.sla_cache_compact(None, ca, 16, None) == -1
+    assert lib.sla_cache_copy(None, ca, 16, 1, None) == -1
+    assert lib.sla_paged_attention(None, 16, ca, ba, 8, 128, 128, 0, 1.0, 16, 16, None) == -1
+    p = sla.make_params(4, 0)
+    assert lib.sla_paged_decode_step(None, 16, 16, ca, ba, 64, 8, 128, 128, C.byref(p), 16, 16, 16, 16, None) == -1
+    assert lib.sla_status_string(-8) == b"SLA_ERR_CACHE_FULL"
+
+
+def test_make_cache_checks_its_tensors(sla):
+    k = torch.empty(4, 2, 16, 64, dtype=torch.bfloat16)
+    t, n, r = torch.zeros(3, 5, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    sla.make_cache(k, k.clone(), t, n, r)
+    for bad in ((k, k.float(), t, n, r), (k, k[:, :, :8], t, n, r), (k, k.transpose(1, 2).contiguous().transpose(1, 2), t, n, r),
+                (k, k.clone(), t[:, ::2], n, r), (k, k.clone(), t, n[:2], r), (k, k.clone(), t, n, r.float()),
+                (k.half(), k.half(), t, n, r)):
+        with pytest.raises((ValueError, TypeError)):
+            sla.make_cache(*bad)
+
+
+def test_model_of_the_bookkeeping():
+    """The model by hand: pages of two tokens."""
+    m = U.Model(6, 2, 4, 4)
+    assert list(m.extend([0, 1], [3, 2])) == [0, 0]
+    assert m.table[0].tolist() == [0, 1, -1, -1] and m.table[1].tolist() == [2, -1, -1, -1]
+    assert m.fork([0, 1], [2, 3]).tolist() == [[1, -1], [3, -1]]
+    assert m.table[2].tolist() == [0, 3, -1, -1] and m.table[3].tolist() == [2, -1, -1, -1]
+    assert m.ref.tolist() == [2, 1, 2, 1, 0, 0] and m.n.tolist() == [3, 2, 3, 2]
+    m.release([0])
+    assert m.ref.tolist() == [1, 0, 2, 1, 0, 0]
+    assert m.compact()[:, :2].tolist() == [[3, -1], [1, -1]]
+    assert m.table[2].tolist() == [0, 1, -1, -1] and m.ref.tolist() == [1, 1, 2, 0, 0, 0]
+    assert list(m.extend([2, 3, 0], [4, 9, 3])) == [3, -1, -1]       # 2 takes two of the three pages; 3's row is too short; 0 wants two
+    assert m.n.tolist() == [0, 2, 7, 2]
+
+
+def test_reference_against_dense_attention():
+    """The row-by-row reference equals softmax over the whole sequence with a mask."""
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn(5, 2, 16, 8, generator=g) for _ in range(2))
+    q = torch.randn(20, 4, 8, generator=g)
+    table = np.array([[3, 0, -1], [4, 1, -1]], dtype=np.int32)
+    n, new = [30, 17], [12, 8]
+    out, lse, *_ = U.attention_reference(q, k, v, table, n, new, 2, 5, 0.3, 16)
+    r = 0
+    for x in range(2):
+        kk, vv = (p[torch.from_numpy(table[x, :2].astype(np.int64))].transpose(1, 2).reshape(-1, 2, 8)[:n[x]].double().repeat_interleave(2, 1) for p in (k, v))
+        z = torch.einsum("thd,jhd->htj", q[r:r + new[x]].double(), kk) * 0.3
+        p, j = torch.arange(n[x] - new[x], n[x])[:, None], torch.arange(n[x])
+        z = z.masked_fill(~((j <= p) & (j > p - 5)), -np.inf)
+        assert torch.allclose(out[r:r + new[x]], torch.einsum("htj,jhd->thd", z.softmax(-1), vv))
+        assert torch.allclose(lse[r:r + new[x]], z.logsumexp(-1).T)
+        r += new[x]
