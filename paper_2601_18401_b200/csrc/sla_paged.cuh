@@ -68,6 +68,26 @@ struct PagedCall {
     float scale;
 };
 
+// Whole part of a / b for 0 <= a < 2^53, b > 0: an estimate put right, where a 64-bit division is a hundred instructions, each
+// fetched for the first time at the start of a launch.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    long long q = (long long)((float)a / (float)b);
+    long long r = a - q * b;
+    while (r < 0) { const long long d = max((long long)((float)-r / (float)b), 1ll); q -= d; r += d * b; }
+    while (r >= b) { const long long d = max((long long)((float)r / (float)b), 1ll); q += d; r -= d * b; }
+    return q;
+}
+// The ranges of a list: the first `longer` of them have a weight more than `each`.
+struct Ranges {
+    long long each;
+    int count, longer;
+    __device__ __forceinline__ long long at(int r) const { return each * r + min(r, longer); }   // where range r begins
+    __device__ __forceinline__ int holding(long long p) const {                                 // the range of position p
+        const long long head = (each + 1) * longer;
+        return (int)(p < head ? quotient(p, each + 1) : longer + quotient(p - head, each));
+    }
+};
+
 // The work of a call is a list of units -- (sequence, KV head, TQ consecutive new tokens with all G heads of the group) -- each
 // with the tiles of KT keys that its tokens see, written down as a running sum of weights (tiles + kUnitWeight, what a unit costs
 // beyond its tiles).  The list is cut into equal ranges, wherever that falls: every CTA gets the same share of the keys whatever the
@@ -80,7 +100,7 @@ struct Plan {
     long long *seq_at;    // [n_seqs + 1] weight before sequence x
     int *unit_at;         // [n_seqs + 1] units of one head before sequence x
     long long *unit_end;  // [units] weight up to and with the unit, from the start of its (sequence, head)
-    int *n_ranges;
+    Ranges *ranges;
     int max_units;        // room in unit_end
 };
 constexpr int kUnitWeight = 2;
@@ -214,7 +234,8 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
         long long n = groups * n_ctas;
         if (n > total / min_weight) n = total / min_weight;   // a range of a few tiles at least
         if (n < 1) n = total > 0 ? 1 : 0;
-        *plan.n_ranges = (int)n;
+        const long long each = n ? total / n : 0;
+        *plan.ranges = {each, (int)n, (int)(total - each * n)};
     }
     __syncthreads();
 }
@@ -233,22 +254,9 @@ __device__ __forceinline__ int warp_last_le(const long long *a, int n, long long
     return lo;
 }
 
-// The ranges of a list of `total` weight.
-struct Ranges {
-    long long total;
-    int count;
-    __device__ __forceinline__ long long at(int r) const { return total * r / count; }   // where range r begins
-    __device__ __forceinline__ int holding(long long p) const {                          // the range of position p
-        int r = min(max((int)((double)p * count / (double)total), 0), count - 1);
-        while (r > 0 && at(r) > p) --r;
-        while (at(r + 1) <= p) ++r;
-        return r;
-    }
-};
-
 // What one CTA does of one unit.
 struct Segment {
-    int x, head, unit;        // sequence, KV head, unit within the (sequence, head)
+    int head;                 // KV head
     int slot, n, q;           // cache slot (-1: none), tokens, new tokens
     int t0, t1, row0;         // new tokens of the unit; row of the sequence's first new token
     int lo, hi;               // tiles to attend to
@@ -262,7 +270,7 @@ struct Cursor {
     int x, head, unit, units, r;
 
     __device__ __forceinline__ bool start(const PagedCall &a, const Plan &plan, int range) {
-        ranges = {plan.seq_at[a.b.n_seqs], *plan.n_ranges};
+        ranges = *plan.ranges;
         r = range;
         if (r >= ranges.count) return false;
         w = ranges.at(r);
@@ -271,7 +279,7 @@ struct Cursor {
         units = plan.unit_at[x + 1] - plan.unit_at[x];
         const long long *ue = plan.unit_end + plan.unit_at[x];
         const long long rem = w - plan.seq_at[x], per_head = ue[units - 1];
-        head = (int)(rem / per_head);
+        head = (int)quotient(rem, per_head);
         const long long in = rem - head * per_head;
         unit = ue[0] > in ? 0 : warp_last_le(ue, units, in) + 1;
         return w < end;
@@ -292,9 +300,7 @@ struct Cursor {
         const long long *ue = plan.unit_end + plan.unit_at[x];
         const long long u1 = ue[unit], u0 = unit ? ue[unit - 1] : 0;
         const long long start = plan.seq_at[x] + head * ue[units - 1] + u0, stop = start + (u1 - u0);
-        s.x = x;
         s.head = head;
-        s.unit = unit;
         s.slot = slot_of(a.c, a.b, x);
         s.n = s.slot < 0 ? 0 : tokens_of(a.c, s.slot);
         int r1;

@@ -311,13 +311,13 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
 // blockIdx.x: the range a cut unit starts in.  A warp takes kMergeRows rows, blockIdx.y and the warp saying which, and requests
 // two parts of each together: bound by the latency of two dependent loads where units have few parts.  Row i of a unit is token
 // i / G of sub-tile i / RS (TS tokens each).
-constexpr int kMergeRows = 4;
+constexpr int kMergeRows = 2;
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 3) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
+__global__ void __launch_bounds__(256, 4) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int N = D / 32, kParts = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     chain_wait();
-    const int r = blockIdx.x, n_ranges = *plan.n_ranges;
+    const int r = blockIdx.x, n_ranges = plan.ranges->count;
     const Cut cut = parts.cut[r];   // (beyond n_ranges: not looked at)
     if (r >= n_ranges || cut.last < 0) return;
     const int n_parts = cut.last - r + 1;
@@ -435,7 +435,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.kt_shift = 6;
     p.n_ctas = (a.c.D == 128 ? 1 : 2) * sm_count;
     p.max_groups = 1;
-    p.min_weight = 4;
+    p.min_weight = 2;
     p.small = 0;
     if (paged_decode_supported(a)) {
         p.kind = PagedPlan::kDecode;
@@ -455,7 +455,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.off_seq_at = take((size_t)(a.b.n_seqs + 1) * 8);
     p.off_unit_at = take((size_t)(a.b.n_seqs + 1) * 4);
     p.off_unit_end = take(units * 8);
-    p.off_n_ranges = take(4);
+    p.off_ranges = take(sizeof(Ranges));
     p.off_cut = take(ranges * sizeof(Cut));
     p.off_lse2 = take(2 * ranges * p.R * 4);
     p.off_o = take(2 * ranges * p.R * a.c.D * 4);

@@ -12,12 +12,12 @@ struct PagedPlan {
     int kt_shift;           // log2 of the keys of a tile
     int small;              // tokens of a unit whose tiles weigh half
     int n_ctas, max_groups, min_weight, max_units;
-    size_t off_seq_at, off_unit_at, off_unit_end, off_n_ranges, off_cut, off_lse2, off_o, bytes;
+    size_t off_seq_at, off_unit_at, off_unit_end, off_ranges, off_cut, off_lse2, off_o, bytes;
 };
 
 inline Plan plan_at(const PagedPlan &p, char *scratch) {
     return {reinterpret_cast<long long *>(scratch + p.off_seq_at), reinterpret_cast<int *>(scratch + p.off_unit_at),
-            reinterpret_cast<long long *>(scratch + p.off_unit_end), reinterpret_cast<int *>(scratch + p.off_n_ranges), p.max_units};
+            reinterpret_cast<long long *>(scratch + p.off_unit_end), reinterpret_cast<Ranges *>(scratch + p.off_ranges), p.max_units};
 }
 inline Parts parts_at(const PagedPlan &p, char *scratch) {
     return {reinterpret_cast<float *>(scratch + p.off_o), reinterpret_cast<float *>(scratch + p.off_lse2),

@@ -398,13 +398,14 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
     if (n_ranges < 1) n_ranges = 1;
     const int r = blockIdx.x;
     if (r >= n_ranges || total == 0) return;
-    const Ranges ranges = {total, n_ranges};
+    const long long each = total / n_ranges;
+    const Ranges ranges = {each, n_ranges, (int)(total - each * n_ranges)};
     long long w = ranges.at(r);
     const long long w_end = ranges.at(r + 1);
     if (w >= w_end) return;
     int x = warp_last_le(s_seq_at, n_seqs, w);
     long long per_head = (s_seq_at[x + 1] - s_seq_at[x]) / a.c.Hkv;
-    int head = (int)((w - s_seq_at[x]) / per_head);
+    int head = (int)quotient(w - s_seq_at[x], per_head);
 
     while (true) {
         const long long start = s_seq_at[x] + head * per_head, stop = start + per_head;

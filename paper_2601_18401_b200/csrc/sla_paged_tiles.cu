@@ -93,6 +93,7 @@ struct TileParams {
     int t_inner;                      // row i is token i % TS, head i / TS (else token i / G, head i % G), as Q's strides nest
     int slot_t, slot_h, slot_p;       // (token, head, page) among the tensor-map coordinates 1..3 of K and V
     int box_rows;                     // keys of a box: the smaller of a page and a tile
+    int out32;                        // every row of the output starts at a multiple of 32 bytes
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {   // NaN where one of them is
@@ -555,16 +556,23 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         if (!write) continue;
                         if (s.part < 0) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
-                                uint32_t w[4];
+                            for (int e = 0; e < 32; e += 16) {   // (rows may start at any 16 bytes)
+                                uint32_t w[8];
 #pragma unroll
-                                for (int u = 0; u < 4; ++u) w[u] = bf16x2(__uint_as_float(o[e + 2 * u]), __uint_as_float(o[e + 2 * u + 1]));
-                                *reinterpret_cast<uint4 *>(dst + c0 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                                for (int u = 0; u < 8; ++u) w[u] = bf16x2(__uint_as_float(o[e + 2 * u]), __uint_as_float(o[e + 2 * u + 1]));
+                                if (p.out32) {
+                                    ptx::st_global_v8(dst + c0 + e, w);
+                                } else {
+                                    *reinterpret_cast<uint4 *>(dst + c0 + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                                    *reinterpret_cast<uint4 *>(dst + c0 + e + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                                }
                             }
                         } else if (!none) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<float4 *>(pdst + c0 + e) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+                            for (int e = 0; e < 32; e += 8) {
+                                const uint32_t w[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
+                                ptx::st_global_v8(pdst + c0 + e, w);
+                            }
                         }
                     }
                 } else if (write && s.part < 0) {
@@ -840,6 +848,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
     p.out = (bf16 *)out;
     p.lse = lse;
     p.TS = pl.TS;
+    p.out32 = (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && a.q_st % 16 == 0 && a.q_sh % 16 == 0;
     p.box_rows = a.c.P < kKeys ? a.c.P : kKeys;
     Dim kd[3], qd[2];
     if (!kv_dims(a, kd) || !q_dims(a, qd)) return cudaErrorInvalidValue;
@@ -878,7 +887,7 @@ void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
     const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * a.c.D * a.c.es * 2, groups = bytes / kGroupBytes + 1;
     const long long most = groups < weight / (128 * kGroupWeight) ? groups : weight / (128 * kGroupWeight);
     p.max_groups = most < 1 ? 1 : most < 8 ? (int)most : 8;
-    p.min_weight = 6;
+    p.min_weight = 3;
 }
 
 cudaError_t launch_paged_tiles(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
