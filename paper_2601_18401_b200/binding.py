@@ -493,6 +493,20 @@ def _int32(t: torch.Tensor, what: str) -> torch.Tensor:
     return t
 
 
+def _on_gpu(*tensors) -> None:
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("tensors of the paged calls must be in device memory")
+
+
+def _output(t: Optional[torch.Tensor], shape, device, dtype=torch.float32) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.dtype is not dtype or not t.is_contiguous() or tuple(t.shape) != shape or not t.is_cuda:
+        raise ValueError(f"output must be a contiguous {dtype} tensor of shape {shape} in device memory")
+    return t
+
+
 def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: torch.Tensor, ref: torch.Tensor) -> sla_cache_t:
     """A paged cache from its tensors: k, v [n_pages, Hkv, page_tokens, D] (any strides with D contiguous; the two share them),
     table int32 [n_slots, table_width], n_tokens int32 [n_slots], ref int32 [n_pages], all on one device."""
@@ -545,8 +559,8 @@ def sla_cache_extend(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     """Room for cu_new[x+1] - cu_new[x] tokens (None: one) of every sequence -> first int32 [n_seqs], the position of its
     first new token, -1 where it was refused.  n_new: rows of the call, when cu_new's last entry does not bound them yet."""
     n = _slots(cache, cu_new, seq)
-    if first is None:
-        first = torch.empty(n, dtype=torch.int32, device=_device_of(cache))
+    _on_gpu(cache.tensors[0], cu_new, seq)
+    first = _output(first, (n,), _device_of(cache), torch.int32)
     rows = n if cu_new is None or n == 0 else 0x7FFFFFFF if n_new is None else int(n_new)
     b = sla_batch_t(n, rows, 1 if cu_new is None else rows, 0, None if seq is None else _int32(seq, "seq").data_ptr(),
                     None if cu_new is None else _int32(cu_new, "cu_new").data_ptr())
@@ -558,20 +572,23 @@ def sla_cache_extend(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
 def sla_cache_append(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.Tensor], first: torch.Tensor,
                      k_new: torch.Tensor, v_new: torch.Tensor, *, seq: Optional[torch.Tensor] = None, stream=None) -> None:
     """k_new, v_new [n_new, Hkv, D] to the positions first[x] + r of their sequences."""
-    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.dtype != v_new.dtype or k_new.stride(-1) != 1:
+    shape, strides, dtype = k_new.shape, k_new.stride(), k_new.dtype
+    if shape != v_new.shape or strides != v_new.stride() or dtype is not v_new.dtype or strides[-1] != 1:
         raise ValueError("k_new and v_new must share shape, strides and dtype, head_dim contiguous")
-    if k_new.shape[1:] != (cache.n_kv_heads, cache.head_dim) or _dtype_code(k_new) != cache.dtype:
+    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or dtype is not cache.tensors[0].dtype:
         raise ValueError("k_new must be [n_new, Hkv, D] in the cache's dtype")
-    b = _batch(cu_new, k_new.shape[0], None, seq)
+    _on_gpu(cache.tensors[0], k_new, v_new, first, cu_new, seq)
+    b = _batch(cu_new, shape[0], None, seq)
     if _int32(first, "first").numel() != b.n_seqs:
         raise ValueError("first must have one entry per sequence")
     handle.check(handle._lib.sla_cache_append(handle.ptr, cache.address, C.addressof(b), first.data_ptr(), k_new.data_ptr(),
-                                              v_new.data_ptr(), k_new.stride(0), k_new.stride(1), _stream_ptr(stream)),
+                                              v_new.data_ptr(), strides[0], strides[1], _stream_ptr(stream)),
                  "sla_cache_append")
 
 
 def sla_cache_release(handle: Handle, cache: sla_cache_t, seq: torch.Tensor, *, stream=None) -> None:
     """Ends the sequences in the slots `seq` (int32, device)."""
+    _on_gpu(cache.tensors[0], seq)
     handle.check(handle._lib.sla_cache_release(handle.ptr, cache.address, _int32(seq, "seq").data_ptr(), seq.numel(),
                                                _stream_ptr(stream)), "sla_cache_release")
 
@@ -581,8 +598,8 @@ def sla_cache_fork(handle: Handle, cache: sla_cache_t, src: torch.Tensor, dst: t
     n = _int32(src, "src").numel()
     if _int32(dst, "dst").numel() != n:
         raise ValueError("src and dst must have the same length")
-    if pairs is None:
-        pairs = torch.empty(2, n, dtype=torch.int32, device=_device_of(cache))
+    _on_gpu(cache.tensors[0], src, dst)
+    pairs = _output(pairs, (2, n), _device_of(cache), torch.int32)
     handle.check(handle._lib.sla_cache_fork(handle.ptr, cache.address, src.data_ptr(), dst.data_ptr(), n, pairs.data_ptr(),
                                             _stream_ptr(stream)), "sla_cache_fork")
     return pairs
@@ -590,8 +607,8 @@ def sla_cache_fork(handle: Handle, cache: sla_cache_t, src: torch.Tensor, dst: t
 
 def sla_cache_compact(handle: Handle, cache: sla_cache_t, *, pairs=None, stream=None):
     """Moves the pages in use to the front of the pool -> pairs int32 [2, n_pages] of the moves, then -1."""
-    if pairs is None:
-        pairs = torch.empty(2, cache.n_pages, dtype=torch.int32, device=_device_of(cache))
+    _on_gpu(cache.tensors[0])
+    pairs = _output(pairs, (2, cache.n_pages), _device_of(cache), torch.int32)
     handle.check(handle._lib.sla_cache_compact(handle.ptr, cache.address, pairs.data_ptr(), _stream_ptr(stream)),
                  "sla_cache_compact")
     return pairs
@@ -601,6 +618,7 @@ def sla_cache_copy(handle: Handle, cache: sla_cache_t, pairs: torch.Tensor, *, s
     """Copies pages pairs[0] to pages pairs[1] (int32 [2, n]; pairs with a negative entry are skipped)."""
     if _int32(pairs, "pairs").dim() != 2 or pairs.shape[0] != 2:
         raise ValueError("pairs must be [2, n]")
+    _on_gpu(cache.tensors[0], pairs)
     handle.check(handle._lib.sla_cache_copy(handle.ptr, cache.address, pairs.data_ptr(), pairs.shape[1], _stream_ptr(stream)),
                  "sla_cache_copy")
 
@@ -610,17 +628,17 @@ def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_
                         softmax_scale: Optional[float] = None, out=None, lse=None, stream=None):
     """q [n_new, Hq, D], the new tokens of the sequences (cu_new None: one each) -> out (q's dtype and strides), lse fp32
     [n_new, Hq].  max_new: the longest chunk (default n_new); it decides the tiles."""
-    T, Hq, D = q.shape
-    if q.stride(-1) != 1 or D != cache.head_dim or _dtype_code(q) != cache.dtype:
+    (T, Hq, D), strides, dtype = q.shape, q.stride(), q.dtype
+    if strides[-1] != 1 or D != cache.head_dim or _dtype_code(q) != cache.dtype:
         raise ValueError("q must be [n_new, Hq, D] in the cache's dtype and head_dim, head_dim contiguous")
     if out is None:
-        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device)
-    elif out.stride() != q.stride() or out.shape != q.shape or out.dtype != q.dtype:
+        out = torch.empty_strided(q.shape, strides, dtype=dtype, device=q.device)
+    elif out.stride() != strides or out.shape != q.shape or out.dtype is not dtype:
         raise ValueError("out must have q's shape, strides and dtype")
-    if lse is None:
-        lse = torch.empty(T, Hq, dtype=torch.float32, device=q.device)
+    _on_gpu(cache.tensors[0], q, out, cu_new, seq)
+    lse = _output(lse, (T, Hq), q.device)
     b = _batch(cu_new, T, max_new, seq)
-    rc = handle._lib.sla_paged_attention(handle.ptr, q.data_ptr(), cache.address, C.addressof(b), Hq, q.stride(0), q.stride(1),
+    rc = handle._lib.sla_paged_attention(handle.ptr, q.data_ptr(), cache.address, C.addressof(b), Hq, strides[0], strides[1],
                                          int(window), 1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale,
                                          out.data_ptr(), lse.data_ptr(), _stream_ptr(stream))
     if rc != SLA_OK:
@@ -639,10 +657,14 @@ def sla_paged_decode_step(handle: Handle, q_s: torch.Tensor, q: torch.Tensor, ca
     if D != cache.head_dim or _dtype_code(q) != cache.dtype or _dtype_code(q_s) != cache.dtype:
         raise ValueError("q_s and q must have the cache's dtype and head_dim")
     dev = q.device
-    out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev) if out is None else out
-    lse = torch.empty(B, Hq, dtype=torch.float32, device=dev) if lse is None else lse
-    out_anchor = torch.empty(B, Hq, params.top_k, dtype=torch.int32, device=dev) if out_anchor is None else out_anchor
-    out_score = torch.empty(B, Hq, params.top_k, dtype=torch.float32, device=dev) if out_score is None else out_score
+    if out is None:
+        out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)
+    elif out.stride() != q.stride() or out.shape != q.shape or out.dtype is not q.dtype:
+        raise ValueError("out must have q's shape, strides and dtype")
+    _on_gpu(cache.tensors[0], q_s, q, out, seq)
+    lse = _output(lse, (B, Hq), dev)
+    out_anchor = _output(out_anchor, (B, Hq, params.top_k), dev, torch.int32)
+    out_score = _output(out_score, (B, Hq, params.top_k), dev)
     b = _batch(None, B, 1, seq)
     most = cache.table_width * cache.page_tokens if max_tokens is None else int(max_tokens)
     rc = handle._lib.sla_paged_decode_step(handle.ptr, q_s.data_ptr(), q.data_ptr(), cache.address, C.addressof(b), most, Hq,

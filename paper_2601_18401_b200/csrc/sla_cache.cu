@@ -66,6 +66,7 @@ __device__ __forceinline__ int pages_for(const Pages &p, long long tokens) { ret
 __global__ void __launch_bounds__(kPlanThreads) cache_extend(Pages p, Batch b, int *__restrict__ first, int *__restrict__ scratch) {
     __shared__ int s_warp[32];
     chain_wait();
+    chain_release();
     int *free_list = scratch, *upto = scratch + p.n_pages;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int sum = 0;
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_extend(Pages p, Batch b, i
 __global__ void __launch_bounds__(256) cache_append(Pages p, Batch b, const int *__restrict__ first, const char *__restrict__ k_new,
                                                     const char *__restrict__ v_new, long long s_t, long long s_h, int parts) {
     chain_wait();
+    chain_release();
     const int lane = threadIdx.x & 31;
     const int per_head = p.D * p.es / 16, chunks = p.Hkv * per_head, part_len = (chunks + parts - 1) / parts;   // 16-byte chunks
     const long long items = (long long)b.n_new * parts;
@@ -186,6 +188,7 @@ __global__ void __launch_bounds__(256) cache_append(Pages p, Batch b, const int 
 
 __global__ void __launch_bounds__(256) cache_release(Pages p, const int *__restrict__ seq) {
     chain_wait();
+    chain_release();
     const int s = seq[blockIdx.x];
     if ((unsigned)s >= (unsigned)p.n_slots) {
         if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, kStatusBadIndex);
@@ -257,6 +260,7 @@ __device__ inline void copy_page_part(const Pages &p, const PageShape &f, int fr
 
 __global__ void __launch_bounds__(kCopyThreads) cache_copy(Pages p, PageShape f, const int *__restrict__ pairs, int n) {
     chain_wait();
+    chain_release();
     const int from = pairs[blockIdx.x], to = pairs[n + blockIdx.x];
     if (from < 0 || to < 0) return;
     if (from >= p.n_pages || to >= p.n_pages) {
@@ -322,6 +326,7 @@ __global__ void __launch_bounds__(kCopyThreads) fork_share(Pages p, PageShape f,
                                                            int n, const int *__restrict__ pairs, const int *__restrict__ full,
                                                            int share_ctas) {
     chain_wait();
+    chain_release();
     const int x = blockIdx.x;
     if ((int)blockIdx.y >= share_ctas) {
         const int from = pairs[x], to = pairs[n + x];
@@ -414,6 +419,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_rank(Pages p, int per, i
 __global__ void __launch_bounds__(kCopyThreads) compact_move(Pages p, PageShape f, const int *__restrict__ scratch, const int *__restrict__ pairs,
                                                              int table_ctas) {
     chain_wait();
+    chain_release();
     const int n_moves = scratch[kMaxChunks];
     const int *rank = scratch + kMaxChunks + 1;
     if ((int)blockIdx.x < table_ctas) {

@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(256, 4) paged_merge(PagedCall a, int R, int RS
     constexpr int N = D / 32, kParts = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     chain_wait();
+    chain_release();
     const int r = blockIdx.x, n_ranges = plan.ranges->count;
     const Cut cut = parts.cut[r];   // (beyond n_ranges: not looked at)
     if (r >= n_ranges || cut.last < 0) return;

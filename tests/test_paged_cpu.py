@@ -78,6 +78,19 @@ def test_make_cache_checks_its_tensors(sla):
             sla.make_cache(*bad)
 
 
+def test_host_tensors_are_refused(sla):
+    """A cache or an argument in host memory is refused by the binding: no kernel ever gets its address."""
+    c = cache_of(sla)
+    i = torch.zeros(4, dtype=torch.int32)
+    new, q = torch.zeros(4, 8, 128, dtype=torch.bfloat16), torch.zeros(4, 32, 128, dtype=torch.bfloat16)
+    for call in (lambda: sla.sla_cache_extend(None, c), lambda: sla.sla_cache_append(None, c, None, i, new, new),
+                 lambda: sla.sla_cache_release(None, c, i), lambda: sla.sla_cache_fork(None, c, i, i),
+                 lambda: sla.sla_cache_compact(None, c), lambda: sla.sla_cache_copy(None, c, torch.zeros(2, 3, dtype=torch.int32)),
+                 lambda: sla.sla_paged_attention(None, q, c), lambda: sla.sla_paged_decode_step(None, q, q, c, sla.make_params(4, 0))):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_model_of_the_bookkeeping():
     """The model by hand: pages of two tokens."""
     m = U.Model(6, 2, 4, 4)
