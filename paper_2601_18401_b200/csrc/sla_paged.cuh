@@ -260,6 +260,7 @@ struct Segment {
     int slot, n, q;           // cache slot (-1: none), tokens, new tokens
     int t0, t1, row0;         // new tokens of the unit; row of the sequence's first new token
     int lo, hi;               // tiles to attend to
+    int all;                  // tiles of the whole unit
     int part;                 // -1: the whole unit; else the partial result's number
 };
 
@@ -314,6 +315,7 @@ struct Cursor {
         const int from = (int)(w - start), to = (int)((end < stop ? end : stop) - start);   // weights of the unit in this range
         s.lo = min(lo + per * max(from - kUnitWeight, 0), hi);
         s.hi = min(lo + per * max(to - kUnitWeight, 0), hi);
+        s.all = hi - lo;
         const bool begins = from == 0, ends = end >= stop;
         s.part = begins && ends ? -1 : begins ? 2 * r + 1 : 2 * r;
         if (begins && !ends) last_range = ranges.holding(stop - 1);

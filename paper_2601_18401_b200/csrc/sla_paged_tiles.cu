@@ -40,6 +40,7 @@ constexpr int kKeys = 128;          // of a tile
 constexpr int kTileShift = 7;
 constexpr int kTmemCols = 512;
 constexpr uint32_t kColO = 0, kColS = 256;   // + 128 per stream
+constexpr int kTurnTiles = 128;      // units of as many tiles are begun at a tile that depends on the time
 constexpr int kSegs = 2;            // entries of the ring of segments
 constexpr float kRescaleThreshold = 8.f;     // log2 units
 // The streams' products are kept at least this many cycles apart.  A stream's tile takes about 3400 cycles of which 1000 are products and 1200
@@ -60,12 +61,19 @@ template <int D> struct Layout {
 // What a segment is to the warps of the CTA.
 struct Seg {
     int lo, hi, n, q;                 // tiles; tokens and new tokens of the sequence
-    int lo_x[2], hi_x[2];             // tiles of the streams
+    int lo_x[2], hi_x[2];             // tiles that the streams take theirs from: at hi_x a stream goes on at lo_x
     int t0, t1, row0, head;
     int part, slot, valid;
-    int step;                         // 2: both streams have the unit's rows, of at most one stream, and every second tile each
+    int both;                         // both streams have the unit's rows, of at most one stream, and every second tile each
+    int begin;                        // the tile to begin with: at hi the order goes on at lo
+    int begin_x[2], own[2];           // the same of the streams, and how many tiles they take
+    int pad[3];
+    // the tile behind j; its place in the order; whether stream x takes the i-th tile, j
+    __device__ __forceinline__ int next(int j) const { return j + 1 < hi ? j + 1 : lo; }
+    __device__ __forceinline__ int place(int j) const { return j >= begin ? j - begin : j - begin + hi - lo; }
+    __device__ __forceinline__ bool has(int x, int i, int j) const { return both ? (i & 1) == x : j >= lo_x[x] && j < hi_x[x]; }
 };
-static_assert(sizeof(Seg) == 64, "four 16-byte words");
+static_assert(sizeof(Seg) == 96, "six 16-byte words");
 
 struct Meta {
     unsigned long long q_full[2], q_empty[2], kv_full[10], kv_empty[2][10], s_full[2], p_ready[2][2], l_full[2], o_full[2], o_empty[2],
@@ -276,13 +284,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
     const uint32_t tmem = meta->tmem_base;
     const int G = p.a.G, TS = p.TS;
 
-    // the CTA's k-th segment, for a whole warp
-    auto take_seg = [&](uint32_t k, Seg &s) {
-        if (!ptx::mbar_wait_warp(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag)) return false;
-        s = meta->seg[k % kSegs];
+    // the CTA's k-th segment is there, for a whole warp; the warp has done with it
+    auto take_seg = [&](uint32_t k) {
+        return ptx::mbar_wait_warp(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag) && meta->seg[k % kSegs].valid != 0;
+    };
+    auto free_seg = [&](uint32_t k) {
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
-        return s.valid != 0;
     };
 
     if (warp >= 12) {
@@ -303,19 +311,21 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
             for (uint32_t k = 0; ok; ++k) {
                 if (!ptx::mbar_wait(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag)) break;
-                const Seg &s = meta->seg[k % kSegs];
-                const int lo = s.lo, hi = s.hi, lx = s.lo_x[x], hx = s.hi_x[x], valid = s.valid, odd = s.step - 1;
+                const Seg s = meta->seg[k % kSegs];
                 ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
-                if (!valid) break;
+                if (!s.valid) break;
+                const int tiles = s.hi - s.lo, own = s.own[x];
+                int done = 0, j = s.begin;   // done: of the stream's own
                 bool k_there = false;   // K of the tile has been waited for
 #pragma unroll 1
-                for (int j = lo; j < hi; ++j) {
-                    const bool on = j >= lx && j < hx && !((j - lx) & odd);
+                for (int t = 0; t < tiles; ++t) {
+                    const bool on = s.has(x, t, j);
+                    j = s.next(j);
                     uint32_t st = i % kStages;
                     if (!k_there && !(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
                     k_there = false;
                     if (on) {
-                        if (j == lx && !(ok = ptx::mbar_wait(bar_q_full + 8 * x, ns & 1u, abort_flag))) break;
+                        if (done == 0 && !(ok = ptx::mbar_wait(bar_q_full + 8 * x, ns & 1u, abort_flag))) break;
                         ptx::tc_fence_after();
                         {
                             volatile uint32_t *s_time = meta->s_time;
@@ -333,7 +343,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                             }
                             ptx::mma_commit(bar_s_full + 8 * x);
                             ptx::mma_commit(bar_kv_empty + 80 * x + 8 * st);
-                            if (j == hx - 1) ptx::mma_commit(bar_q_empty + 8 * x);
+                            if (done == own - 1) ptx::mma_commit(bar_q_empty + 8 * x);
                         }
                     } else if (leader) {
                         ptx::mbar_arrive(bar_kv_empty + 80 * x + 8 * st);
@@ -343,8 +353,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * st, (i / kStages) & 1u, abort_flag))) break;
                     if (on) {
                         // the first PV of a segment overwrites O: the results of the segment before have been read
-                        if (j == lx && ns > 0 && !(ok = ptx::mbar_wait(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
-                        if (j + 1 < hi) {   // off the way from P to the next S
+                        if (done == 0 && ns > 0 && !(ok = ptx::mbar_wait(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
+                        if (t + 1 < tiles) {   // off the way from P to the next S
                             k_there = true;
                             if (!(ok = ptx::mbar_wait(bar_kv_full + 8 * ((i + 1) % kStages), ((i + 1) / kStages) & 1u, abort_flag))) break;
                         }
@@ -356,21 +366,22 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                             if (leader) {
 #pragma unroll
                                 for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
-                                    ptx::mma_ts(o_col, s_col + kk * 8, desc_advance(dv, kk * 2048), kIdescO, (j > lx || kk > 0) ? 1u : 0u);
+                                    ptx::mma_ts(o_col, s_col + kk * 8, desc_advance(dv, kk * 2048), kIdescO, (done > 0 || kk > 0) ? 1u : 0u);
                             }
                         }
                         if (!ok) break;
                         if (leader) {
                             ptx::mma_commit(bar_kv_empty + 80 * x + 8 * st);
-                            if (j == hx - 1) ptx::mma_commit(bar_o_full + 8 * x);
+                            if (done == own - 1) ptx::mma_commit(bar_o_full + 8 * x);
                         }
                         ++nt;
+                        ++done;
                     } else if (leader) {
                         ptx::mbar_arrive(bar_kv_empty + 80 * x + 8 * st);
                     }
                     ++i;
                 }
-                ns += hx > lx;
+                ns += own > 0;
             }
         } else if (warp == 14) {
             // ---------------- K and V: a lane per box, as many as the tile has pages with tokens
@@ -381,23 +392,25 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             const uint32_t box_bytes = p.box_rows * 128;
             uint32_t i = 0;
             bool ok = true;
-            Seg s;
 #pragma unroll 1
-            for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
+            for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) {
+                const Seg &s = meta->seg[k % kSegs];
+                const int tiles = s.hi - s.lo, n = s.n, head = s.head;
                 const int *table = p.a.c.table + (long long)max(s.slot, 0) * p.a.c.width;
                 auto key_of = [&](int j) { return j * kKeys + lane * p.box_rows; };
                 auto page_of = [&](int j) {   // -1: no box
                     const int key = key_of(j);
-                    return j < s.hi && lane < boxes && key < s.n ? valid_page(p.a.c, __ldg(table + (key >> shift))) : -1;
+                    return lane < boxes && key < n ? valid_page(p.a.c, __ldg(table + (key >> shift))) : -1;
                 };
-                int next = page_of(s.lo);
+                int next = tiles > 0 ? page_of(s.begin) : -1, j_next = s.begin;
 #pragma unroll 1
-                for (int j = s.lo; j < s.hi && ok; ++j) {
-                    const int page = next;
-                    next = page_of(j + 1);
+                for (int t = 0; t < tiles && ok; ++t) {
+                    const int page = next, j = j_next;
+                    j_next = s.next(j);
+                    next = page_of(j_next);
                     int c[4];
                     c[1 + p.slot_t] = key_of(j) & (p.a.c.P - 1);
-                    c[1 + p.slot_h] = s.head;
+                    c[1 + p.slot_h] = head;
                     c[1 + p.slot_p] = page;
                     const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, page >= 0)) * box_bytes * kHalves;
 #pragma unroll 1
@@ -422,6 +435,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             ptx::prefetch_tensormap(&tm_q);
             const bool leader = ptx::elect_one();
             uint32_t k = 0, nq[2] = {0, 0};
+            int at = 0;   // tiles so far
             bool ok = true;
             auto put = [&](const Seg &s) {
                 ok = ptx::mbar_wait_warp(bar_seg_empty + 8 * (k % kSegs), ((k / kSegs) & 1u) ^ 1u, abort_flag);
@@ -444,33 +458,45 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     s.lo = g.lo; s.hi = g.hi; s.n = g.n; s.q = g.q;
                     s.t0 = g.t0; s.t1 = g.t1; s.row0 = g.row0; s.head = g.head;
                     s.part = g.part; s.slot = g.slot; s.valid = 1;
-                    s.step = g.t1 - g.t0 <= TS ? 2 : 1;
+                    s.both = g.t1 - g.t0 <= TS;
+                    const int tiles = g.hi - g.lo;
+                    // CTAs that read the same keys read them at about the same time, so that they find them in L2: after t tiles each is at
+                    // the tile t of its unit, or, where a unit is shared by several, at one that is t modulo their share.  512 tokens at
+                    // 65536 (64 units over 148 CTAs): 540 us instead of 620, which read 1.86 GB out of DRAM for 0.27 GB of keys; 2048 at
+                    // 30720: 920 instead of 985.  Short units keep their order: their keys stay in L2 in any order, and four prompts of
+                    // 2048 tokens (D 64) took 162 us instead of 154 with turns.
+                    int turn = 0;
+                    if (g.all >= kTurnTiles) {
+                        const int period = max(1, min(g.all, (int)min(cur.ranges.each, (long long)0x3fffffff)));
+                        turn = (at - g.lo) % period;
+                        turn += turn < 0 ? period : 0;
+                    }
+                    s.begin = turn < tiles ? g.lo + turn : g.lo;
+                    at = (at + tiles) & 0x3fffffff;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        if (s.step == 2) {
-                            s.lo_x[x] = g.lo + x;
-                            s.hi_x[x] = max(g.hi - ((g.hi - g.lo - 1 - x) & 1), g.lo + x);   // behind the stream's last tile
-                            continue;
-                        }
                         const int a0 = min(g.t0 + x * TS, g.t1), a1 = min(a0 + TS, g.t1);
-                        int lo = 0, hi = 0;
-                        if (a1 > a0) unit_tiles(g.n, g.q, a0, a1, p.a.window, kTileShift, lo, hi);
+                        int lo = g.lo, hi = g.hi;
+                        if (!s.both) unit_tiles(g.n, g.q, a0, a1, p.a.window, kTileShift, lo, hi);
                         lo = max(lo, g.lo);
                         hi = min(hi, g.hi);
+                        const int at_x = s.begin + (s.both ? x : 0);
                         s.lo_x[x] = lo;
-                        s.hi_x[x] = max(lo, hi);
+                        s.hi_x[x] = hi;
+                        s.own[x] = s.both ? (tiles + 1 - x) >> 1 : max(hi - lo, 0);
+                        s.begin_x[x] = s.both ? (at_x < hi ? at_x : at_x - tiles) : at_x >= lo && at_x < hi ? at_x : lo;
                     }
                     put(s);
 #pragma unroll 1
                     for (int x = 0; x < 2 && ok; ++x) {
-                        if (s.hi_x[x] <= s.lo_x[x]) continue;
+                        if (s.own[x] == 0) continue;
                         ok = ptx::mbar_wait_warp(bar_q_empty + 8 * x, (nq[x] & 1u) ^ 1u, abort_flag);
                         ++nq[x];
                         if (!ok) break;
                         if (leader) {
                             const uint32_t full = bar_q_full + 8 * x, dst = base + L::kOffQ + x * L::kTileBytes;
                             ptx::mbar_arrive_expect_tx(full, TS * G * 128 * kHalves);
-                            const int tok = g.row0 + g.t0 + (s.step == 2 ? 0 : x * TS), c1 = p.t_inner ? tok : g.head * G, c2 = p.t_inner ? g.head * G : tok;
+                            const int tok = g.row0 + g.t0 + (s.both ? 0 : x * TS), c1 = p.t_inner ? tok : g.head * G, c2 = p.t_inner ? g.head * G : tok;
 #pragma unroll
                             for (int h = 0; h < kHalves; ++h) ptx::tma_load_4d(dst + h * L::kHalfBytes, &tm_q, full, 64 * h, c1, c2, 0);
                         }
@@ -490,13 +516,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         uint32_t ns[2] = {0, 0};
         bool ok = true;
-        Seg s;
 #pragma unroll 1
-        for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
+        for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) {
+            const Seg &s = meta->seg[k % kSegs];
 #pragma unroll 1
             for (int x = 0; x < 2 && ok; ++x) {
                 const int tok = s.t0 + x * TS + t;
-                const bool both = s.step == 2, has = s.hi_x[x] > s.lo_x[x], second = both && s.hi_x[1] > s.lo_x[1];
+                const bool has = s.own[x] > 0, second = s.both && s.own[1] > 0;
                 bool write = t < TS && g < G && tok < s.t1;
                 const int h = s.head * G + g;
                 const long long r = s.row0 + tok;
@@ -583,7 +609,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (s.part < 0) p.lse[r * p.a.Hq + h] = stat.y * kLn2;
                     else p.parts.lse2[(long long)s.part * 256 + x * kRows + canon] = stat.y;
                 }
-                if (both) break;
+                if (s.both) break;
             }
         }
     } else {
@@ -596,20 +622,21 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         const float scale2 = p.a.scale * kLog2e;
         uint32_t nt = 0, ns = 0, tiles = 0;   // tiles and segments of the stream, tiles of the CTA so far
         bool ok = true;
-        Seg s;
 #pragma unroll 1
-        for (uint32_t k = 0; ok && take_seg(k, s); ++k) {
-            const int tok = s.t0 + (s.step == 2 ? 0 : x * TS) + t;
+        for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) {
+            const Seg &s = meta->seg[k % kSegs];
+            const int tok = s.t0 + (s.both ? 0 : x * TS) + t;
             const bool valid = t < TS && g < G && tok < s.t1;
             const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 ? max(last - p.a.window + 1, 0) : 0;   // keys seen
             // keys that not every row of the unit sees lie outside [all_lo, all_hi]
             const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? s.n - s.q + s.t1 - p.a.window : 0;
-            const int lx = s.lo_x[x], hx = s.hi_x[x];
-            if (hx > lx) {
+            if (s.own[x] > 0) {
+                const int lx = s.lo_x[x], hx = s.hi_x[x], step = s.both ? 2 : 1;
+                int j = s.begin_x[x];
                 float m_ref = -CUDART_INF_F, l = 0.f;
                 bool fresh = true;   // no logit above -inf so far
 #pragma unroll 1
-                for (int j = lx; j < hx; j += s.step, ++nt) {
+                for (int left = s.own[x]; left > 0; --left, ++nt) {
                     const int k0 = j * kKeys;
                     if (!(ok = ptx::mbar_wait_warp(bar_s_full + 8 * x, nt & 1u, abort_flag))) break;
                     ptx::tc_fence_after();
@@ -648,7 +675,9 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     const bool need = !fresh && bm > m_ref + kRescaleThreshold;
                     if (__any_sync(0xffffffffu, need)) {
                         // the PV of the stream's tile before must have landed before O is touched
-                        const uint32_t v = 2 * (tiles + (j - s.lo) - s.step) + 1u;
+                        // (no two tiles that the stream skips lie between, so that its stage has not been used again)
+                        const int before = j - step;
+                        const uint32_t v = 2 * (tiles + s.place(before < lx ? before + hx - lx : before)) + 1u;
                         if (!(ok = ptx::mbar_wait_warp(bar_kv_empty + 80 * x + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
                         ptx::tc_fence_after();
                         const float f = need ? ex2_approx(m_ref - bm) : 1.f;
@@ -697,7 +726,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         ptx::tmem_st32(s_col + half * 32, pk);
                         if (half == 0 && edge) {
                             // this thread's key of the tile: beyond the sequence it is cleared, else looked at
-                            const uint32_t v = 2 * (tiles + (j - s.lo)) + 1u;
+                            const uint32_t v = 2 * (tiles + s.place(j)) + 1u;
                             if (!(ok = ptx::mbar_wait_warp(bar_kv_full + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
                             const int key = k0 + row;
                             uint4 *vr = reinterpret_cast<uint4 *>(smem + L::kOffKV + (v % kStages) * L::kTileBytes + row * 128);
@@ -737,6 +766,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     unpack2(fadd2(acc2[0], acc2[1]), s0, s1);
                     unpack2(fadd2(acc2[2], acc2[3]), s2, s3);
                     l += (s0 + s1) + (s2 + s3);
+                    j += step;
+                    if (j >= hx) j -= hx - lx;
                 }
                 if (!ok) break;
                 // all four warps have looked at their keys
@@ -744,7 +775,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
                 if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
                 const bool odd = *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1;
-                if (odd && valid && (s.step == 1 || x == 0))
+                if (odd && valid && (!s.both || x == 0))
                     redo_row<D>(p, s, x * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
