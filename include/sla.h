@@ -51,7 +51,10 @@
  * leaves the one by rows, also where the other is faster.  Both sum in fp32, in different orders: the last
  * bits of a result can depend on which one ran, hence on the workspace.  In the same way the workspace, and
  * the rows of a call, decide which touching spans the tensor-core span-attention attends as one piece; every
- * result stays within the rounding of its type.
+ * result stays within the rounding of its type.  sla_paged_attention runs one new token a sequence on a kernel of
+ * its own, chunks of bf16 tokens on the tensor cores, and chunks of fp32 tokens -- and of bf16 ones whose strides
+ * do not nest or whose softmax_scale is not positive -- on a kernel that computes in fp32; sizes, strides and
+ * scale decide, never lengths, and no workspace changes a result.
  *
  * Errors: every call returns an sla_status_t; 0 is success, negative values are errors.  When
  * argument validation fails nothing is launched.  No exception or abort crosses this interface.
@@ -354,8 +357,8 @@ sla_status_t sla_prefill_host(sla_handle_t handle, const void *q_s_host, const v
 /* ---- paged key/value cache ---------------------------------------------------------------------
  *
  * (The paper has no counterpart: its cache is one contiguous sequence.  A serving program holds many
- * sequences of different lengths that grow, share their beginnings and end.)  The cache is a pool of pages of page_tokens tokens, a table that says which page holds which
- * part of which sequence, and counts:
+ * sequences of different lengths that grow, share their beginnings and end.)  The cache is a pool of pages
+ * of page_tokens tokens, a table that says which page holds which part of which sequence, and counts:
  *
  *   k, v      [n_pages, n_kv_heads, page_tokens, head_dim]  strides stride_{page,h,t}, head_dim contiguous
  *   table     int32 [n_slots, table_width]  page of positions [c * page_tokens, (c+1) * page_tokens) of the

@@ -7,7 +7,10 @@
 //   fork_plan, fork_share   one CTA hands out the pages for the partly filled ones; the grid shares the full ones and copies
 //   compact_count, compact_rank, compact_move   pages in use per chunk; ranks of movers and holes; data, tables, ref
 //
-// All are bound by the latency of a few dependent loads except the copies of pages, which are bound by HBM.
+// All are bound by the latency of a few dependent loads except the copies of tokens and pages, which are bound by HBM.  Measured (8 KV
+// heads, D 128, bf16): extend and append of a token to each of 48 sequences 7.4 us, of 18.7 thousand tokens to 3 sequences 33 us (153 MB
+// moved, 23 us at the rate of a copy); 6 sequences forked to 48 9.4 us; a pool of 1 GB whose holes take 304 MB compacted in 114 us, 94 of
+// them the copies at 6.5 TB/s.
 #include "sla_paged.cuh"
 
 namespace sla {

