@@ -51,8 +51,8 @@
  * leaves the one by rows, also where the other is faster.  Both sum in fp32, in different orders: the last
  * bits of a result can depend on which one ran, hence on the workspace.  In the same way the workspace, and
  * the rows of a call, decide which touching spans the tensor-core span-attention attends as one piece; every
- * result stays within the rounding of its type.  sla_paged_attention runs one new token a sequence on a kernel of
- * its own, chunks of bf16 tokens on the tensor cores, and chunks of fp32 tokens -- and of bf16 ones whose strides
+ * result stays within the rounding of its type.  sla_paged_attention runs few new tokens a sequence (max_new times
+ * the heads of a group at most 16) on a kernel of their own, chunks of bf16 tokens on the tensor cores, and chunks of fp32 tokens -- and of bf16 ones whose strides
  * do not nest or whose softmax_scale is not positive -- on a kernel that computes in fp32; sizes, strides and
  * scale decide, never lengths, and no workspace changes a result.
  *

@@ -1,6 +1,10 @@
-// Attention of one new token a sequence over a paged cache.  One launch.
+// Attention of one new token a sequence over a paged cache, or of so few that tokens x heads of a group are at most 16 rows (a step that
+// checks guessed tokens).  One launch.
 //
-// All G query heads of a KV head share its keys, so that K and V are read once: bound by HBM.
+// All rows of a KV head share its keys, so that K and V are read once: bound by HBM.  (The heads below are rows.)  The bound of 16 is
+// what the registers hold.  Against the kernels of chunks, D 128: 32 sequences of 198 tokens with 1 to 3 new ones, 8/2 heads, 11.5 us
+// here and 22 there; 28 of 14 to 583, 32/8 heads, 17 and 27; 32 of 1000 to 65536 with 4, 272 and 268; fp32, 16 of 1000 to 20000 with 4,
+// 259 and 581.
 //
 // bf16 (attend_bf16): the products run on the tensor
 // cores by mma.sync with the keys as the 16 rows of A and the heads as the 8 columns of B,
@@ -37,7 +41,11 @@ namespace {
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 // resident CTAs an SM: two where 16 heads of 128 dimensions fill the registers
 __host__ __device__ constexpr int ctas_per_sm(int D, int NT) { return D == 128 && NT == 2 ? 2 : 3; }
-constexpr int kMaxSeqs = 1024;        // of a launch
+// sequences of a launch: as many as there is room for (16 bytes each) beside the kernel's arrays in 48 KB
+template <typename T> constexpr int max_seqs(int D, int NT) {
+    const int arrays = kWarps * 8 * NT * (D + 2) * 4 + (sizeof(T) == 4 ? D * 8 * NT * 4 : 16) + 128, room = (48 * 1024 - arrays) / 16 - 1;
+    return room < 1024 ? room : 1024;
+}
 constexpr int kTileShift = 6;         // weights count 64 keys
 constexpr int kMinWeight = 2;         // of a range
 
@@ -72,12 +80,22 @@ __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 
 
 // What one warp does of a segment: the keys key, key + stride, .. below key_end in steps of the path's own, of which those in [first, n) count,
 // for the G heads of KV head `head`.  Its maxima, sums and weighted values go to w_m, w_l [heads] and w_o [heads][D].
+// With several new tokens (kTok) the rows are tokens x heads: row r is head r % G of token r / G.
 struct Walk {
     int key, key_end, first, n, head, row_q;
     const int *table;
+    int q, rows, window;   // tokens; rows; 0: no window
+    // all rows see the keys [all_first, all_n)
+    int all_first, all_n;
+    // the rows that see key k of [first, n)
+    __device__ __forceinline__ void rows_of(int k, int G, int &lo, int &hi) const {
+        const int t = k - (n - q);   // the token at k
+        lo = max(t, 0) * G;
+        hi = window > 0 && t + window < q ? (t + window) * G : rows;
+    }
 };
 
-template <int D, int NT>
+template <int D, int NT, bool kTok>
 __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q, const PagedCall &a, const Walk &wk, float *w_m, float *w_l, float *w_o) {
     constexpr int kChunks = D / 32;       // 16-byte pieces of a key row per thread
     constexpr int kVChunks = D / 64;      // of a value row
@@ -91,8 +109,9 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
     uint32_t qf[NT][kChunks][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const bool on = 8 * t + g < G;
-        const __nv_bfloat16 *src = q + (long long)row_q * a.q_st + (long long)(head * G + (on ? 8 * t + g : 0)) * a.q_sh + c * 8;
+        const bool on = 8 * t + g < (kTok ? wk.rows : G);
+        const int r = on ? 8 * t + g : 0, tok = kTok ? r / G : 0;
+        const __nv_bfloat16 *src = q + (long long)(row_q + tok) * a.q_st + (long long)(head * G + r - tok * G) * a.q_sh + c * 8;
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const uint4 v = on ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * j)) : make_uint4(0, 0, 0, 0);
@@ -152,14 +171,20 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[t][e] *= scale2;
-        if (key < first || key + 16 > n) {
+        const bool edge = kTok ? key < wk.all_first || key + 16 > wk.all_n : key < first || key + 16 > n;
+        if (edge) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int e2 = 0; e2 < 2; ++e2) {
+                const int kk = key + g + 8 * e2;
+                int lo = 0, hi = 8 * NT;
+                if constexpr (kTok) wk.rows_of(kk, G, lo, hi);
+                if (kk < first || kk >= n) hi = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int kk = key + g + 8 * (e >> 1);
-                    if (kk < first || kk >= n) s[t][e] = -CUDART_INF_F;
-                }
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (8 * t + 2 * c + e < lo || 8 * t + 2 * c + e >= hi) s[t][2 * e2 + e] = -CUDART_INF_F;
+            }
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -194,6 +219,52 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
             }
             pf[t][0] = transpose8x8(pack_bf16(s[t][0], s[t][1]));
             pf[t][1] = transpose8x8(pack_bf16(s[t][2], s[t][3]));
+        }
+        if constexpr (kTok) {
+            // keys that some rows see and others do not: 0 times a value that is not finite is NaN.  Where there is one, the products of these
+            // keys are left out of the MMA and added row by row.
+            if (edge) {
+                bool part[4];
+                uint32_t bad = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = key + 2 * c + (e & 1) + 8 * (e >> 1);
+                    part[e] = k < wk.all_first || k >= wk.all_n;
+#pragma unroll
+                    for (int j = 0; j < kVChunks; ++j)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            if (part[e]) bad |= ((word(vr[e][j], u) & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // exponent all ones
+                }
+                if (__any_sync(0xffffffffu, bad != 0)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < kVChunks; ++j)
+                            if (part[e]) vr[e][j] = make_uint4(0, 0, 0, 0);
+                    const __nv_bfloat16 *vs = vb + find(key);
+#pragma unroll 1
+                    for (int kk = 0; kk < 16; ++kk) {
+                        const int k = key + kk;
+                        if (k < first || k >= n || (k >= wk.all_first && k < wk.all_n)) continue;
+                        int lo, hi;
+                        wk.rows_of(k, G, lo, hi);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float wt = __shfl_sync(0xffffffffu, kk < 8 ? s[t][e] : s[t][e + 2], (kk & 7) * 4 + c);
+                                const int r = 8 * t + 2 * c + e;
+                                if (r < lo || r >= hi) continue;
+#pragma unroll
+                                for (int i = 0; i < kMt; ++i) {
+                                    acc[t][i][e] = fmaf(wt, __bfloat162float(vs[(long long)kk * a.c.s_t + 8 * g + i]), acc[t][i][e]);
+                                    acc[t][i][e + 2] = fmaf(wt, __bfloat162float(vs[(long long)kk * a.c.s_t + (D == 128 ? 64 + 8 * g + i : 8 * g + 4 + i)]), acc[t][i][e + 2]);
+                                }
+                            }
+                    }
+                }
+            }
         }
         // row g of m-tile i: dimension 8 g + i; row g + 8: 64 + 8 g + i (D = 64: 8 g + 4 + i)
 #pragma unroll
@@ -232,7 +303,7 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
 }
 
 // fp32: S by lanes of a key each, O by lanes of D / 32 dimensions each.  s_q: the queries [D][8 NT], scaled.
-template <int D, int NT>
+template <int D, int NT, bool kTok>
 __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, const float *s_q, float *w_m, float *w_l, float *w_o) {
     float *s_p = w_o;   // a step's weights, until the sums are written
     constexpr int H = 8 * NT, N = D / 32, kDeep = 8;   // heads, dimensions of a lane, loads in flight
@@ -275,9 +346,14 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
                 }
         }
         bool over = false;
+        int lo = 0, hi = H;   // rows that see the lane's key
+        if constexpr (kTok) {
+            wk.rows_of(j, a.G, lo, hi);
+            if (!on) hi = 0;
+        }
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-            if (!on) s[h] = -CUDART_INF_F;
+            if (kTok ? h < lo || h >= hi : !on) s[h] = -CUDART_INF_F;
             over |= s[h] > m[h] + 8.f;
         }
         if (__any_sync(0xffffffffu, over)) {
@@ -303,6 +379,7 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
         for (int h = 0; h < H; h += 4) *reinterpret_cast<float4 *>(s_p + lane * H + h) = make_float4(s[h], s[h + 1], s[h + 2], s[h + 3]);
         __syncwarp();
         const unsigned seen = __ballot_sync(0xffffffffu, on);   // values of other keys may be anything: they are not read
+        const unsigned part = kTok ? __ballot_sync(0xffffffffu, on && (j < wk.all_first || j >= wk.all_n)) : 0u;   // not every row sees them
 #pragma unroll 1
         for (int i0 = 0; i0 < 32; i0 += kDeep) {
             float v[kDeep][N];
@@ -317,7 +394,9 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u)
+            for (int u = 0; u < kDeep; ++u) {
+                int lo_u = 0, hi_u = H;
+                if (kTok && (part >> (i0 + u) & 1)) wk.rows_of(j - lane + i0 + u, a.G, lo_u, hi_u);
 #pragma unroll
                 for (int h = 0; h < H; h += 4) {
                     const float4 p4 = *reinterpret_cast<const float4 *>(s_p + (i0 + u) * H + h);
@@ -325,8 +404,10 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int d = 0; d < N; ++d) acc[h + e][d] = fmaf(pp[e], v[u][d], acc[h + e][d]);
+                        for (int d = 0; d < N; ++d)
+                            if (!kTok || (h + e >= lo_u && h + e < hi_u)) acc[h + e][d] = fmaf(pp[e], v[u][d], acc[h + e][d]);
                 }
+            }
         }
     }
 #pragma unroll
@@ -341,7 +422,7 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
     }
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool kTok>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT))
 paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
              T *__restrict__ out, float *__restrict__ lse) {
@@ -375,7 +456,9 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                 s_n[x] = n;
                 s_slot[x] = slot;
                 if (hi > lo) {
-                    unit_tiles(n, 1, 0, 1, a.window, kTileShift, lo, hi);
+                    const int q_x = kTok ? hi - lo : 1;
+                    if (q_x > a.b.max_new) atomicOr(a.c.status, kStatusBadIndex);
+                    unit_tiles(n, q_x, 0, q_x, a.window, kTileShift, lo, hi);
                     w = (long long)(hi - lo + kUnitWeight) * a.c.Hkv;
                 }
             }
@@ -417,27 +500,31 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
         const int n = s_n[x];
         int lo, hi, row_q;
         new_rows(a.b, x_base + x, row_q, hi);
-        unit_tiles(n, 1, 0, 1, a.window, kTileShift, lo, hi);
+        const int q_x = kTok ? hi - row_q : 1, rows = kTok ? min(q_x, a.b.max_new) * G : G;
+        unit_tiles(n, q_x, 0, q_x, a.window, kTileShift, lo, hi);
         const int from = (int)(w - start), to = (int)((w_end < stop ? w_end : stop) - start);
-        const int first = a.window > 0 && n > a.window ? n - a.window : 0;
+        // keys seen by any row [first, n), by all rows [all_first, all_n)
+        const int window = a.window > 0 && a.window < n ? a.window : 0;
+        const int all_first = window > 0 ? n - window : 0, all_n = n - q_x + 1, first = max(all_first - q_x + 1, 0);
         const int key = max((lo + max(from - kUnitWeight, 0)) << kTileShift, first & ~(kStep - 1));
         const int key_end = min((lo + max(to - kUnitWeight, 0)) << kTileShift, n);
-        const Walk walk = {key + kStep * warp, key_end, first, n, head, row_q, a.c.table + (long long)max(s_slot[x], 0) * a.c.width};
+        const Walk walk = {key + kStep * warp, key_end, first, n, head, row_q, a.c.table + (long long)max(s_slot[x], 0) * a.c.width, q_x, rows, window, all_first, all_n};
         if constexpr (kF32) {
             // (s_q: the segment before has been joined)
             for (int c = tid; c < D * 8 * NT; c += kThreads) {
                 const int h = c / D, d = c % D;   // neighbouring threads, neighbouring dimensions
-                s_q[d * 8 * NT + h] = h < G ? q[(long long)row_q * a.q_st + (long long)(head * G + h) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
+                const int tok = kTok ? h / G : 0;
+                s_q[d * 8 * NT + h] = h < rows ? q[(long long)(row_q + tok) * a.q_st + (long long)(head * G + h - tok * G) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
             }
             __syncthreads();
-            attend_f32<D, NT>(a, walk, s_q, s_m[warp], s_l[warp], &s_o[warp][0][0]);
+            attend_f32<D, NT, kTok>(a, walk, s_q, s_m[warp], s_l[warp], &s_o[warp][0][0]);
         } else {
-            attend_bf16<D, NT>(q, a, walk, s_m[warp], s_l[warp], &s_o[warp][0][0]);
+            attend_bf16<D, NT, kTok>(q, a, walk, s_m[warp], s_l[warp], &s_o[warp][0][0]);
         }
         __syncthreads();
         const bool begins = from == 0, ends = w_end >= stop;
         const int part = begins && ends ? -1 : begins ? 2 * r + 1 : 2 * r;
-        for (int it = tid; it < G * (D / 4); it += kThreads) {
+        for (int it = tid; it < rows * (D / 4); it += kThreads) {
             const int qi = it / (D / 4), d = (it % (D / 4)) * 4;
             float mx = s_m[0][qi];
 #pragma unroll
@@ -457,9 +544,9 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] *= inv;
             if (part < 0) {
-                const int h = head * G + qi;
-                store4(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d, o[0], o[1], o[2], o[3]);
-                if (d == 0) lse[(long long)row_q * a.Hq + h] = z * kLn2;
+                const int tok = kTok ? qi / G : 0, h = head * G + qi - tok * G;
+                store4(out + (long long)(row_q + tok) * a.q_st + (long long)h * a.q_sh + d, o[0], o[1], o[2], o[3]);
+                if (d == 0) lse[(long long)(row_q + tok) * a.Hq + h] = z * kLn2;
             } else {
                 if (!none) __stcg(reinterpret_cast<float4 *>(parts.o + ((long long)part * R + qi) * D + d), make_float4(o[0], o[1], o[2], o[3]));
                 if (d == 0) __stcg(parts.lse2 + (long long)part * R + qi, z);
@@ -478,7 +565,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
             if (s_last) {
                 __threadfence();
                 auto part_at = [&](int e) { return (long long)(e == 0 ? 2 * r0 + 1 : 2 * (r0 + e)) * R; };
-                for (int it = tid; it < G * (D / 4); it += kThreads) {
+                for (int it = tid; it < rows * (D / 4); it += kThreads) {
                     const int qi = it / (D / 4), d = (it % (D / 4)) * 4;
                     float mx = -CUDART_INF_F, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
                     for (int e0 = 0; e0 < n_parts; e0 += 8) {
@@ -508,9 +595,9 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                     }
                     const bool none = mx == -CUDART_INF_F && sum == 0.f;
                     const float inv = none ? 0.f : 1.f / sum;
-                    const int h = head * G + qi;
-                    store4(out + (long long)row_q * a.q_st + (long long)h * a.q_sh + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-                    if (d == 0) lse[(long long)row_q * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
+                    const int tok = kTok ? qi / G : 0, h = head * G + qi - tok * G;
+                    store4(out + (long long)(row_q + tok) * a.q_st + (long long)h * a.q_sh + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+                    if (d == 0) lse[(long long)(row_q + tok) * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
                 }
             }
         }
@@ -527,38 +614,43 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
 
 }  // namespace
 
-bool paged_decode_supported(const PagedCall &a) { return a.b.max_new == 1; }
+bool paged_decode_supported(const PagedCall &a) { return (long long)a.b.max_new * a.G <= 16; }
 
 void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.R = p.RS = 16;
     p.TS = p.TQ = 1;
-    p.n_ctas = ctas_per_sm(a.c.D, a.G <= 8 ? 1 : 2) * sm_count;
+    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2) * sm_count;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool kTok>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
-    for (int x0 = 0; x0 < a.b.n_seqs && e == cudaSuccess; x0 += kMaxSeqs) {
-        const int n = a.b.n_seqs - x0 < kMaxSeqs ? a.b.n_seqs - x0 : kMaxSeqs;
-        e = launch_chained(paged_decode<T, D, NT>, dim3(p.n_ctas), dim3(kThreads), (size_t)(n + 1) * 8 + (size_t)n * 8, st,
+    constexpr int kMost = max_seqs<T>(D, NT);
+    for (int x0 = 0; x0 < a.b.n_seqs && e == cudaSuccess; x0 += kMost) {
+        const int n = a.b.n_seqs - x0 < kMost ? a.b.n_seqs - x0 : kMost;
+        e = launch_chained(paged_decode<T, D, NT, kTok>, dim3(p.n_ctas), dim3(kThreads), (size_t)(n + 1) * 8 + (size_t)n * 8, st,
                            (const T *)q, a, x0, n, parts_at(p, scratch), counters, (T *)out, lse);
         ++*launches;
     }
     return e;
 }
 
-template <typename T>
+template <typename T, int D>
 static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                               cudaStream_t st, long long *launches) {
-    if (a.c.D == 64) return a.G <= 8 ? decode_of<T, 64, 1>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, 64, 2>(q, a, p, scratch, counters, out, lse, st, launches);
-    return a.G <= 8 ? decode_of<T, 128, 1>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, 128, 2>(q, a, p, scratch, counters, out, lse, st, launches);
+    const bool small = a.b.max_new * a.G <= 8;
+    if (a.b.max_new == 1)
+        return small ? decode_of<T, D, 1, false>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, false>(q, a, p, scratch, counters, out, lse, st, launches);
+    return small ? decode_of<T, D, 1, true>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, true>(q, a, p, scratch, counters, out, lse, st, launches);
 }
 
 cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches) {
-    return dtype == SLA_F32 ? decode_for<float>(q, a, p, scratch, counters, out, lse, st, launches)
-                            : decode_for<__nv_bfloat16>(q, a, p, scratch, counters, out, lse, st, launches);
+    if (dtype == SLA_F32)
+        return a.c.D == 64 ? decode_for<float, 64>(q, a, p, scratch, counters, out, lse, st, launches) : decode_for<float, 128>(q, a, p, scratch, counters, out, lse, st, launches);
+    return a.c.D == 64 ? decode_for<__nv_bfloat16, 64>(q, a, p, scratch, counters, out, lse, st, launches)
+                       : decode_for<__nv_bfloat16, 128>(q, a, p, scratch, counters, out, lse, st, launches);
 }
 
 }  // namespace sla

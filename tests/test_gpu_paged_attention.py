@@ -182,6 +182,49 @@ def test_queries_with_tokens_inside_heads(sla, handle, dtype, G):
         U.check_attention(out, lse, U.attention_reference(q, k, v, table, n, new, G, 0, 128 ** -0.5, 16), dtype)
 
 
+FEW = [(1, 16), (1, 9), (2, 8), (2, 3), (3, 5), (4, 4), (4, 2), (5, 3), (7, 2), (8, 2)]   # heads of a group x new tokens <= 16
+
+
+@pytest.mark.parametrize("G,new", FEW)
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+def test_few_new_tokens(sla, handle, G, new, dtype, d):
+    """As many rows as the kernel of single tokens takes: ragged counts, none, fewer keys than tokens, a long sequence."""
+    n = [1, 2, 15, 16, 17, 0, 63, 64, 65, 700, 3, 40, 9001]
+    c = [(i * 5 + 2) % (new + 1) for i in range(len(n))]
+    c[2] = c[5] = c[10] = c[-1] = new
+    for window in (0, 1, 7, 100):
+        out, lse, _ = run(sla, handle, n, c, dtype=dtype, d=d, G=G, window=window, max_new=new)
+    one, one_lse, _ = run(sla, handle, n, c, dtype=dtype, d=d, G=G, window=100, max_new=400)   # the kernel of chunks
+    assert torch.allclose(out.float(), one.float(), atol=0.02) and torch.equal(lse.isinf(), one_lse.isinf())
+
+
+@pytest.mark.parametrize("G,new", [(1, 16), (2, 3), (4, 4), (8, 2)])
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_few_new_tokens_and_values_that_are_not_finite(sla, handle, G, new, dtype, d, bad):
+    """At every position that only some of the new tokens see, at either end of the window."""
+    n = [400, 300]
+    for window in (0, 40):
+        for back in range(new):
+            for at in (n[0] - 1 - back, n[0] - window - back):
+                if at >= n[0]:
+                    continue
+
+                def prep(k, v, table, q):
+                    v[int(table[0, at // 16]), 1, at % 16, 5] = bad
+                    v[int(table[0, at // 16]), 0, at % 16, d - 1] = bad
+                run(sla, handle, n, [new, new], dtype=dtype, d=d, G=G, window=window, prep=prep)
+
+
+@pytest.mark.parametrize("dtype,n_seqs,new,G,d", [(F32, 1030, 1, 16, 128), (F32, 600, 2, 8, 128), (BF16, 1010, 1, 16, 128), (BF16, 1030, 4, 4, 64)])
+def test_many_sequences_of_many_rows(sla, handle, dtype, n_seqs, new, G, d):
+    """More sequences than fit beside the sums of 16 rows in the shared memory of one launch."""
+    rs = np.random.RandomState(n_seqs)
+    n = rs.randint(0, 40, n_seqs)
+    c = np.minimum(n, rs.randint(0, new + 1, n_seqs)) if new > 1 else np.ones(n_seqs, dtype=int)
+    run(sla, handle, n.tolist(), c.tolist(), dtype=dtype, hkv=1, G=G, d=d, max_new=new)
+
+
 @pytest.mark.parametrize("dtype,n_seqs,new", [(BF16, 1100, 1), (F32, 1030, 1), (BF16, 1500, 3), (F32, 300, 2)])
 def test_many_sequences(sla, handle, dtype, n_seqs, new):
     """More sequences than one launch, one warp or one CTA takes at a time."""
