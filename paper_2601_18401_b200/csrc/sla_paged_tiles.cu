@@ -319,8 +319,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
             for (uint32_t k = 0; ok; ++k) {
                 if (!ptx::mbar_wait(bar_seg_full + 8 * (k % kSegs), (k / kSegs) & 1u, abort_flag)) break;
-                const Seg s = meta->seg[k % kSegs];
-                ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
+                const Seg &s = meta->seg[k % kSegs];
                 if (!s.valid) break;
                 const int tiles = s.hi - s.lo, own = s.own[x];
                 int done = 0, j = s.begin;   // done: of the stream's own
@@ -390,6 +389,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     ++i;
                 }
                 ns += own > 0;
+                ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
             }
         } else if (warp == 14) {
             // ---------------- K and V: a lane per box, as many as the tile has pages with tokens
@@ -563,23 +563,21 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 const bool none = stat.y == -CUDART_INF_F;
                 if (has) {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
-                        uint32_t o[32];
-                        ptx::tmem_ld32(lane_addr + kColO + x * 128 + c0, o);
-                        ptx::tmem_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = none ? 0u : __float_as_uint(__uint_as_float(o[e]) * stat.x);
+                    for (int c0 = 0; c0 < D; c0 += 16) {   // (32 columns at a time spill)
+                        uint32_t o[16];
+                        ptx::tmem_ld16(lane_addr + kColO + x * 128 + c0, o);
                         if (second) {
+                            uint32_t o1[16];
+                            ptx::tmem_ld16(lane_addr + kColO + 128 + c0, o1);
+                            ptx::tmem_wait_ld();
 #pragma unroll
-                            for (int e0 = 0; e0 < 32; e0 += 16) {
-                                uint32_t o1[16];
-                                ptx::tmem_ld16(lane_addr + kColO + 128 + c0 + e0, o1);
-                                ptx::tmem_wait_ld();
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e]) * stat.x));
+                        } else {
+                            ptx::tmem_wait_ld();
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e0 + e] = none ? 0u : __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e0 + e])));
-                            }
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * stat.x);
                         }
-                        if (c0 == D - 32) {   // O is in registers: the next segment's first PV may overwrite it
+                        if (c0 == D - 16) {   // O is in registers: the next segment's first PV may overwrite it
                             ptx::tc_fence_before();
                             __syncwarp();
                             if (lane == 0) {
@@ -588,22 +586,19 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                             }
                         }
                         if (!write) continue;
-                        if (s.part < 0) {
+                        if (s.part < 0) {   // (rows may start at any 16 bytes)
+                            uint32_t w[8];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 16) {   // (rows may start at any 16 bytes)
-                                uint32_t w[8];
-#pragma unroll
-                                for (int u = 0; u < 8; ++u) w[u] = bf16x2(__uint_as_float(o[e + 2 * u]), __uint_as_float(o[e + 2 * u + 1]));
-                                if (p.out32) {
-                                    ptx::st_global_v8(dst + c0 + e, w);
-                                } else {
-                                    *reinterpret_cast<uint4 *>(dst + c0 + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                                    *reinterpret_cast<uint4 *>(dst + c0 + e + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-                                }
+                            for (int u = 0; u < 8; ++u) w[u] = none ? 0u : bf16x2(__uint_as_float(o[2 * u]), __uint_as_float(o[2 * u + 1]));
+                            if (p.out32) {
+                                ptx::st_global_v8(dst + c0, w);
+                            } else {
+                                *reinterpret_cast<uint4 *>(dst + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+                                *reinterpret_cast<uint4 *>(dst + c0 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
                             }
                         } else if (!none) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
+                            for (int e = 0; e < 16; e += 8) {
                                 const uint32_t w[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
                                 ptx::st_global_v8(pdst + c0 + e, w);
                             }
