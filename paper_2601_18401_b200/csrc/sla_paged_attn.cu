@@ -297,10 +297,9 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
                     for (int d = 0; d < DT; ++d) dst[(d / 4) * 64 + tx * 4 + d % 4] = from_float<T>(o[d]);
                     if (tx == 0) lse[row * a.Hq + s.head * G + g] = lse2 * kLn2;
                 } else {
-                    float *dst = parts.o + ((long long)s.part * R + i) * D;
 #pragma unroll
                     for (int d = 0; d < DT; d += 4)
-                        if (!none) *reinterpret_cast<float4 *>(dst + (d / 4) * 64 + tx * 4) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+                        if (!none) *reinterpret_cast<float4 *>(parts.at(s.part, R, D, i, (d / 4) * 64 + tx * 4)) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
                     if (tx == 0) parts.lse2[(long long)s.part * R + i] = lse2;
                 }
             }
@@ -310,88 +309,72 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
 }
 
 // ------------------------------------------------------------------------------------------------
-// blockIdx.x: the range a cut unit starts in.  A warp takes kMergeRows rows, blockIdx.y and the warp saying which, and requests
-// two parts of each together: bound by the latency of two dependent loads where units have few parts (8 to 13 us).  Row i of a unit is token
+// blockIdx.x: the range a cut unit starts in.  A thread takes 16 columns of a row, neighbouring threads neighbouring rows, and requests
+// two parts together: bound by the latency of dependent loads where units have few parts.  Row i of a unit is token
 // i / G of sub-tile i / RS (TS tokens each).
-constexpr int kMergeRows = 2;
+constexpr int kMergeThreads = 256, kMergeCols = 16;
+__device__ __forceinline__ void load8(const float *p, float *v) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "l"(p));
+}
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 4) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
-    constexpr int N = D / 32, kParts = 2;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__global__ void __launch_bounds__(kMergeThreads, 4) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
+    constexpr int kParts = 2;
     chain_wait();
     chain_release();
     const int r = blockIdx.x, n_ranges = plan.ranges->count;
     const Cut cut = parts.cut[r];   // (beyond n_ranges: not looked at)
     if (r >= n_ranges || cut.last < 0) return;
     const int n_parts = cut.last - r + 1;
-    const int i0 = (blockIdx.y * 8 + warp) * kMergeRows;
-    int t[kMergeRows], h[kMergeRows];
-    bool on[kMergeRows], any = false;
-    float mx[kMergeRows], sum[kMergeRows], acc[kMergeRows][N];
+    const int i = threadIdx.x & (R - 1), d0 = kMergeCols * (blockIdx.y * (kMergeThreads / R) + threadIdx.x / R);
+    const int in = i % RS, t = i / RS * TS + in / a.G, h = cut.head * a.G + in % a.G;
+    if (in >= TS * a.G || t >= cut.tokens) return;
+    float mx = -CUDART_INF_F, sum = 0.f, acc[kMergeCols];
 #pragma unroll
-    for (int u = 0; u < kMergeRows; ++u) {
-        const int i = i0 + u, in = i % RS;
-        t[u] = i / RS * TS + in / a.G;
-        h[u] = cut.head * a.G + in % a.G;
-        on[u] = in < TS * a.G && t[u] < cut.tokens;
-        any |= on[u];
-        mx[u] = -CUDART_INF_F;
-        sum[u] = 0.f;
-#pragma unroll
-        for (int d = 0; d < N; ++d) acc[u][d] = 0.f;
-    }
-    if (!any) return;
+    for (int d = 0; d < kMergeCols; ++d) acc[d] = 0.f;
     for (int e0 = 0; e0 < n_parts; e0 += kParts) {
-        float z[kMergeRows][kParts], v[kMergeRows][kParts][N];
+        float z[kParts], v[kParts][kMergeCols];
 #pragma unroll
-        for (int u = 0; u < kMergeRows; ++u)
+        for (int e = 0; e < kParts; ++e) {
+            z[e] = -CUDART_INF_F;
+            if (e0 + e >= n_parts) continue;
+            // (of a part without keys the sums were not written, and are not used)
+            const int part = e0 + e == 0 ? 2 * r + 1 : 2 * (r + e0 + e);
+            z[e] = parts.lse2[(long long)part * R + i];
 #pragma unroll
-            for (int e = 0; e < kParts; ++e) {
-                // (a part that is not there: the first one's place, without a weight; of a part without keys the sums
-                // were not written, and are not used)
-                const int part = e0 + e == 0 || e0 + e >= n_parts ? 2 * r + 1 : 2 * (r + e0 + e);
-                const long long at = (long long)part * R + i0 + u;
-                z[u][e] = __ldcg(parts.lse2 + at);
-                const float *src = parts.o + at * D + lane * N;
-                if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u][e]) = __ldcg(reinterpret_cast<const float4 *>(src));
-                else *reinterpret_cast<float2 *>(v[u][e]) = __ldcg(reinterpret_cast<const float2 *>(src));
-                if (e0 + e >= n_parts) z[u][e] = -CUDART_INF_F;
-            }
+            for (int d = 0; d < kMergeCols; d += 8) load8(parts.at(part, R, D, i, d0 + d), v[e] + d);
+        }
+        float top = mx;   // a NaN reaches the result through its weight
 #pragma unroll
-        for (int u = 0; u < kMergeRows; ++u) {
-            float top = mx[u];   // a NaN reaches the result through its weight
+        for (int e = 0; e < kParts; ++e) top = fmaxf(top, z[e]);
+        const float keep = mx == top ? 1.f : exp2f(mx - top);
+        mx = top;
+        sum *= keep;
 #pragma unroll
-            for (int e = 0; e < kParts; ++e) top = fmaxf(top, z[u][e]);
-            const float keep = mx[u] == top ? 1.f : exp2f(mx[u] - top);
-            mx[u] = top;
-            sum[u] *= keep;
+        for (int d = 0; d < kMergeCols; ++d) acc[d] *= keep;
 #pragma unroll
-            for (int d = 0; d < N; ++d) acc[u][d] *= keep;
+        for (int e = 0; e < kParts; ++e) {
+            if (z[e] == -CUDART_INF_F) continue;
+            const float w = exp2f(z[e] - top);
+            sum += w;
 #pragma unroll
-            for (int e = 0; e < kParts; ++e) {
-                if (z[u][e] == -CUDART_INF_F) continue;
-                const float w = exp2f(z[u][e] - top);
-                sum[u] += w;
-#pragma unroll
-                for (int d = 0; d < N; ++d) acc[u][d] = fmaf(w, v[u][e][d], acc[u][d]);
-            }
+            for (int d = 0; d < kMergeCols; ++d) acc[d] = fmaf(w, v[e][d], acc[d]);
         }
     }
+    const bool none = mx == -CUDART_INF_F && sum == 0.f;
+    const float inv = none ? 0.f : 1.f / sum;
+    const long long row = cut.row0 + t;
+    T *o = out + row * a.q_st + (long long)h * a.q_sh + d0;
+    constexpr int E = Vec16<T>::kElems;
 #pragma unroll
-    for (int u = 0; u < kMergeRows; ++u) {
-        if (!on[u]) continue;
-        const bool none = mx[u] == -CUDART_INF_F && sum[u] == 0.f;
-        const float inv = none ? 0.f : 1.f / sum[u];
-        const long long row = cut.row0 + t[u];
-        T *o = out + row * a.q_st + (long long)h[u] * a.q_sh + lane * N;
-        alignas(16) T w[N];
+    for (int d = 0; d < kMergeCols; d += E) {
+        alignas(16) T w[E];
 #pragma unroll
-        for (int d = 0; d < N; ++d) w[d] = from_float<T>(acc[u][d] * inv);
-        if constexpr (N * sizeof(T) == 16) *reinterpret_cast<uint4 *>(o) = *reinterpret_cast<const uint4 *>(w);
-        else if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<const uint2 *>(w);
-        else *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<const uint32_t *>(w);
-        if (lane == 0) lse[row * a.Hq + h[u]] = none ? -CUDART_INF_F : (mx[u] + log2f(sum[u])) * kLn2;
+        for (int e = 0; e < E; ++e) w[e] = from_float<T>(acc[d + e] * inv);
+        *reinterpret_cast<uint4 *>(o + d) = *reinterpret_cast<const uint4 *>(w);
     }
+    if (d0 == 0) lse[row * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
 }
 
 template <typename T, int D, int R>
@@ -418,9 +401,8 @@ cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scra
 
 template <typename T, int D>
 static cudaError_t merge_of(const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
-    const int per = 8 * kMergeRows;
-    return launch_chained(paged_merge<T, D>, dim3(p.n_ctas * p.max_groups, p.R / per), dim3(256), 0, st, a, p.R, p.RS, p.TS, plan_at(p, scratch),
-                          parts_at(p, scratch), (T *)out, lse);
+    return launch_chained(paged_merge<T, D>, dim3(p.n_ctas * p.max_groups, D / kMergeCols * p.R / kMergeThreads), dim3(kMergeThreads), 0, st, a, p.R,
+                          p.RS, p.TS, plan_at(p, scratch), parts_at(p, scratch), (T *)out, lse);
 }
 
 cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {

@@ -221,7 +221,7 @@ __device__ __noinline__ void redo_row(const TileParams &p, const Seg &s, int can
         for (int e = 0; e < 32; ++e) {
             const float o = none ? 0.f : acc[e] * inv;
             if (s.part < 0) p.out[row * p.a.q_st + (long long)h * p.a.q_sh + d0 + e] = __float2bfloat16_rn(o);
-            else p.parts.o[((long long)s.part * 256 + canon) * D + d0 + e] = o;
+            else *p.parts.at(s.part, 256, D, canon, d0 + e) = o;
         }
     }
     if (s.part < 0) p.lse[row * p.a.Hq + h] = lse2 * kLn2;
@@ -535,7 +535,6 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 const int h = s.head * G + g;
                 const long long r = s.row0 + tok;
                 bf16 *dst = p.out + r * p.a.q_st + (long long)h * p.a.q_sh;
-                float *pdst = p.parts.o + ((long long)s.part * 256 + x * kRows + canon) * D;
                 float2 stat = make_float2(0.f, -CUDART_INF_F);   // factor of O, log2-sum-exp
                 float f1 = 0.f;                                  // factor of the other stream's O
                 if (has) {
@@ -600,7 +599,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll
                             for (int e = 0; e < 16; e += 8) {
                                 const uint32_t w[8] = {o[e], o[e + 1], o[e + 2], o[e + 3], o[e + 4], o[e + 5], o[e + 6], o[e + 7]};
-                                ptx::st_global_v8(pdst + c0 + e, w);
+                                ptx::st_global_v8(p.parts.at(s.part, 256, D, x * kRows + canon, c0 + e), w);
                             }
                         }
                     }
