@@ -309,10 +309,12 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
 }
 
 // ------------------------------------------------------------------------------------------------
-// blockIdx.x: the range a cut unit starts in.  A thread takes 16 columns of a row, neighbouring threads neighbouring rows, and requests
-// two parts together: bound by the latency of dependent loads where units have few parts.  Row i of a unit is token
-// i / G of sub-tile i / RS (TS tokens each).
-constexpr int kMergeThreads = 256, kMergeCols = 16;
+// blockIdx.x: the range a cut unit starts in.  A thread takes kMergeCols columns of a row, neighbouring threads neighbouring rows, and requests
+// kParts parts together: bound by the latency of dependent loads (8 us).  22 tokens at 23199, 32/4 heads, D 64, 37 parts a unit, whole call:
+// 30.7 us, 34.7 with 16 columns and two parts at a time; four threads a row that take every fourth part, 28.0, but then calls of few parts
+// a unit take longer for the number of CTAs (1 to 600 tokens of 16 sequences: 66 us instead of 59.6).  Row i of a unit is token i / G of
+// sub-tile i / RS (TS tokens each).
+constexpr int kMergeThreads = 256, kMergeCols = 8;
 __device__ __forceinline__ void load8(const float *p, float *v) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
@@ -320,7 +322,7 @@ __device__ __forceinline__ void load8(const float *p, float *v) {
 }
 template <typename T, int D>
 __global__ void __launch_bounds__(kMergeThreads, 4) paged_merge(PagedCall a, int R, int RS, int TS, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
-    constexpr int kParts = 2;
+    constexpr int kParts = 4;
     chain_wait();
     chain_release();
     const int r = blockIdx.x, n_ranges = plan.ranges->count;
