@@ -96,12 +96,15 @@ struct Ranges {
 // (Not below kGroupWeight a range, where the cuts cost more: 1999 tokens at 30011, three multiples 980 us and one 925 us; 8192 tokens
 // that end at 65536, six multiples 6670 us and one 7180 us.  Claimed ranges of falling sizes for CTAs that are done early gave nothing:
 // 945 us and 7100 us.)
+struct Start;
 struct Plan {
     long long *seq_at;    // [n_seqs + 1] weight before sequence x
     int *unit_at;         // [n_seqs + 1] units of one head before sequence x
     long long *unit_end;  // [units] weight up to and with the unit, from the start of its (sequence, head)
+    int4 *seqs;           // [n_seqs] slot (-1: none), tokens, new tokens, first row
     Ranges *ranges;
-    int max_units;        // room in unit_end
+    Start *starts;        // [ranges]
+    int max_units, max_ranges;   // room in unit_end and starts
 };
 constexpr int kUnitWeight = 2;
 constexpr long long kGroupBytes = 48ll << 20, kGroupWeight = 400;
@@ -175,6 +178,7 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
             const int slot = slot_of(a.c, a.b, x);
             if (slot < 0) atomicOr(a.c.status, kStatusBadIndex);
             else n = tokens_of(a.c, slot);
+            plan.seqs[x] = make_int4(slot, n, q, r0);
         }
         long long total = 0;
         if (units == 1) {
@@ -254,6 +258,18 @@ __device__ __forceinline__ int warp_last_le(const long long *a, int n, long long
     return lo;
 }
 
+// The same by a thread alone.
+__device__ __forceinline__ int last_le(const long long *a, int n, long long v) {
+    int lo = 0;
+    while (n > 1) {
+        const int half = n / 2;
+        const bool le = a[lo + half] <= v;
+        lo += le ? half : 0;
+        n = le ? n - half : half;
+    }
+    return lo;
+}
+
 // What one CTA does of one unit.
 struct Segment {
     int head;                 // KV head
@@ -264,26 +280,45 @@ struct Segment {
     int part;                 // -1: the whole unit; else the partial result's number
 };
 
-// Goes through the segments of range r.  All warps that need a segment run a cursor of their own, converged, and see the same.
+// The first segment of a range and where its cursor stands behind it.  The plan has them for every range: to find them takes half a dozen
+// loads that wait for one another, which the plan has in shared memory.  (Four prompts of 2048 tokens, D 64: 146 us with the search at
+// the start of every CTA, 135 so; 1 to 600 tokens of 16 sequences 59.7 and 59.2; calls of 25 to 40 us the same within 2 %.)
+struct alignas(16) Start {
+    long long w;
+    Segment s;
+    int last_range, x, unit, units;
+};
+
+// Goes through the segments of range r.
 struct Cursor {
     Ranges ranges;
     long long w, end;
     int x, head, unit, units, r;
 
-    __device__ __forceinline__ bool start(const PagedCall &a, const Plan &plan, int range) {
+    // the first segment of range r (in w < end); false beyond the last range
+    __device__ __forceinline__ bool open(const Plan &plan, int range, Segment &s, int &last_range) {
         ranges = *plan.ranges;
         r = range;
+        const Start b = plan.starts[min(r, plan.max_ranges - 1)];   // (both loads at once)
         if (r >= ranges.count) return false;
+        end = ranges.at(r + 1);
+        w = b.w; s = b.s; last_range = b.last_range;
+        x = b.x; unit = b.unit; units = b.units; head = b.s.head;
+        return true;
+    }
+    // puts the cursor in front of it
+    __device__ __forceinline__ void seek(const PagedCall &a, const Plan &plan, const Ranges &of, int range) {
+        ranges = of;
+        r = range;
         w = ranges.at(r);
         end = ranges.at(r + 1);
-        x = warp_last_le(plan.seq_at, a.b.n_seqs, w);
+        x = last_le(plan.seq_at, a.b.n_seqs, w);
         units = plan.unit_at[x + 1] - plan.unit_at[x];
         const long long *ue = plan.unit_end + plan.unit_at[x];
         const long long rem = w - plan.seq_at[x], per_head = ue[units - 1];
         head = (int)quotient(rem, per_head);
         const long long in = rem - head * per_head;
-        unit = ue[0] > in ? 0 : warp_last_le(ue, units, in) + 1;
-        return w < end;
+        unit = ue[0] > in ? 0 : last_le(ue, units, in) + 1;
     }
     // the segment at the cursor; false when the range is done.  *last_range: for a unit that starts in this range and does not
     // end in it, the range it ends in, else -1.
@@ -302,11 +337,8 @@ struct Cursor {
         const long long u1 = ue[unit], u0 = unit ? ue[unit - 1] : 0;
         const long long start = plan.seq_at[x] + head * ue[units - 1] + u0, stop = start + (u1 - u0);
         s.head = head;
-        s.slot = slot_of(a.c, a.b, x);
-        s.n = s.slot < 0 ? 0 : tokens_of(a.c, s.slot);
-        int r1;
-        new_rows(a.b, x, s.row0, r1);
-        s.q = r1 - s.row0;
+        const int4 of = plan.seqs[x];
+        s.slot = of.x; s.n = of.y; s.q = of.z; s.row0 = of.w;
         s.t0 = unit * f.TQ;
         s.t1 = min(s.t0 + f.TQ, s.q);
         int lo, hi;

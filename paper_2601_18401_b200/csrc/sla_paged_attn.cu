@@ -18,11 +18,43 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 
+// The plan is built in shared memory where it fits (4 to 6 us), else where it goes.
+constexpr int kPlanSeqs = 512, kPlanUnits = 2048;
 __global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f, int n_ctas, int max_groups, int min_weight, Plan plan) {
-    __shared__ long long s_sum[kPlanThreads / 32];
+    __shared__ long long s_sum[kPlanThreads / 32], s_seq_at[kPlanSeqs + 1], s_unit_end[kPlanUnits];
+    __shared__ int s_unit_at[kPlanSeqs + 1];
+    __shared__ int4 s_seqs[kPlanSeqs];
+    __shared__ Ranges s_ranges;
+    const bool fits = a.b.n_seqs <= kPlanSeqs && plan.max_units <= kPlanUnits;
+    Plan own = plan;
+    own.ranges = &s_ranges;
+    if (fits) {
+        own.seq_at = s_seq_at;
+        own.unit_at = s_unit_at;
+        own.unit_end = s_unit_end;
+        own.seqs = s_seqs;
+    }
     chain_wait();
     chain_release();
-    build_plan<kPlanThreads>(a, f, n_ctas, max_groups, min_weight, plan, s_sum);
+    build_plan<kPlanThreads>(a, f, n_ctas, max_groups, min_weight, own, s_sum);
+    const Ranges ranges = s_ranges;
+    for (int r = threadIdx.x; r < ranges.count; r += kPlanThreads) {
+        Cursor c;
+        Start b;
+        c.seek(a, own, ranges, r);
+        c.next(a, own, f, b.s, b.last_range);
+        b.w = c.w; b.x = c.x; b.unit = c.unit; b.units = c.units;
+        plan.starts[r] = b;
+    }
+    if (fits) {
+        for (int x = threadIdx.x; x <= a.b.n_seqs; x += kPlanThreads) {
+            plan.seq_at[x] = s_seq_at[x];
+            plan.unit_at[x] = s_unit_at[x];
+            if (x < a.b.n_seqs) plan.seqs[x] = s_seqs[x];
+        }
+        for (int u = threadIdx.x; u < s_unit_at[a.b.n_seqs]; u += kPlanThreads) plan.unit_end[u] = s_unit_end[u];
+    }
+    if (threadIdx.x == 0) *plan.ranges = ranges;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -73,8 +105,8 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
         Segment s;
         int last_range;
         Cut cut = {0, 0, 0, -1};
-        if (!cur.start(a, plan, range)) break;
-        while (cur.next(a, plan, Shape{TQ, kShift, 0}, s, last_range)) {
+        if (!cur.open(plan, range, s, last_range)) break;
+        do {
             if (last_range >= 0) cut = {s.row0 + s.t0, s.t1 - s.t0, s.head, last_range};
             const int rows = (s.t1 - s.t0) * G;
             const int keys_end = min(s.n, s.n - s.q + s.t1);
@@ -303,7 +335,7 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
                     if (tx == 0) parts.lse2[(long long)s.part * R + i] = lse2;
                 }
             }
-        }
+        } while (cur.next(a, plan, Shape{TQ, kShift, 0}, s, last_range));
         if (tid == 0) parts.cut[range] = cut;
     }
 }
@@ -443,6 +475,9 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.off_unit_at = take((size_t)(a.b.n_seqs + 1) * 4);
     p.off_unit_end = take(units * 8);
     p.off_ranges = take(sizeof(Ranges));
+    p.max_ranges = (int)ranges;
+    p.off_seqs = take((size_t)a.b.n_seqs * sizeof(int4));
+    p.off_starts = take(ranges * sizeof(Start));
     p.off_cut = take(ranges * sizeof(Cut));
     p.off_lse2 = take(2 * ranges * p.R * 4);
     p.off_o = take(2 * ranges * p.R * a.c.D * 4);

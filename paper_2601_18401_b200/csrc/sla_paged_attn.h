@@ -11,13 +11,14 @@ struct PagedPlan {
     int R, RS, TS, TQ;      // rows of a unit, rows and tokens of its sub-tiles, tokens of the unit
     int kt_shift;           // log2 of the keys of a tile
     int small;              // tokens of a unit whose tiles weigh half
-    int n_ctas, max_groups, min_weight, max_units;
-    size_t off_seq_at, off_unit_at, off_unit_end, off_ranges, off_cut, off_lse2, off_o, bytes;
+    int n_ctas, max_groups, min_weight, max_units, max_ranges;
+    size_t off_seq_at, off_unit_at, off_unit_end, off_ranges, off_seqs, off_starts, off_cut, off_lse2, off_o, bytes;
 };
 
 inline Plan plan_at(const PagedPlan &p, char *scratch) {
     return {reinterpret_cast<long long *>(scratch + p.off_seq_at), reinterpret_cast<int *>(scratch + p.off_unit_at),
-            reinterpret_cast<long long *>(scratch + p.off_unit_end), reinterpret_cast<Ranges *>(scratch + p.off_ranges), p.max_units};
+            reinterpret_cast<long long *>(scratch + p.off_unit_end), reinterpret_cast<int4 *>(scratch + p.off_seqs),
+            reinterpret_cast<Ranges *>(scratch + p.off_ranges), reinterpret_cast<Start *>(scratch + p.off_starts), p.max_units, p.max_ranges};
 }
 inline Parts parts_at(const PagedPlan &p, char *scratch) {
     return {reinterpret_cast<float *>(scratch + p.off_o), reinterpret_cast<float *>(scratch + p.off_lse2),

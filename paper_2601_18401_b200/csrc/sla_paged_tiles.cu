@@ -460,8 +460,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 Segment g;
                 int last_range;
                 Cut cut = {0, 0, 0, -1};
-                if (!cur.start(p.a, p.plan, range)) break;
-                while (ok && cur.next(p.a, p.plan, Shape{2 * TS, kTileShift, TS}, g, last_range)) {
+                if (!cur.open(p.plan, range, g, last_range)) break;
+                do {
                     if (last_range >= 0) cut = {g.row0 + g.t0, g.t1 - g.t0, g.head, last_range};
                     s.lo = g.lo; s.hi = g.hi; s.n = g.n; s.q = g.q;
                     s.t0 = g.t0; s.t1 = g.t1; s.row0 = g.row0; s.head = g.head;
@@ -510,7 +510,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         }
                         __syncwarp();
                     }
-                }
+                } while (ok && cur.next(p.a, p.plan, Shape{2 * TS, kTileShift, TS}, g, last_range));
                 if (leader) p.parts.cut[range] = cut;
             }
             s = Seg{};
