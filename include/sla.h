@@ -395,7 +395,8 @@ typedef struct {
 typedef struct {
     int32_t n_seqs;
     int32_t n_new;            /* rows of the tensors: cu_new[n_seqs]                                  */
-    int32_t max_new;          /* no sequence has more new tokens than this                           */
+    int32_t max_new;          /* no sequence has more new tokens than this (SLA_ERR_DEVICE_INDEX where
+                               * the kernel that it chose depends on it; results are then undefined)  */
     int32_t reserved;         /* must be 0                                                           */
     const int32_t *seq;       /* device [n_seqs]: slots, all different; NULL = 0 .. n_seqs-1         */
     const int32_t *cu_new;    /* device [n_seqs + 1], ascending from 0; NULL = one token a sequence   */

@@ -457,7 +457,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                 s_slot[x] = slot;
                 if (hi > lo) {
                     const int q_x = kTok ? hi - lo : 1;
-                    if (q_x > a.b.max_new) atomicOr(a.c.status, kStatusBadIndex);
+                    if (hi - lo > a.b.max_new) atomicOr(a.c.status, kStatusBadIndex);   // (no more than max_new of its rows are computed)
                     unit_tiles(n, q_x, 0, q_x, a.window, kTileShift, lo, hi);
                     w = (long long)(hi - lo + kUnitWeight) * a.c.Hkv;
                 }

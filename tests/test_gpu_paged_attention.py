@@ -391,3 +391,22 @@ def test_refusals(sla, handle):
         sla.sla_paged_attention(small, q, cache, cu)
     assert e.value.status == -3
     small.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("max_new", [1, 2, 3])
+def test_more_new_tokens_than_max_new_are_flagged(sla, dtype, max_new):
+    """Where the rows of a sequence were to fit into one pass: the status word, nothing written outside the call's rows."""
+    h = sla.Handle(0, 1 << 28)
+    new = [2 * max_new, 0]
+    cache, k, v, table, q, cu = build(sla, [100, 60], new, dtype=dtype)
+    out = torch.full((q.shape[0] + 8, *q.shape[1:]), 7.0, dtype=dtype, device="cuda:0")
+    sla.sla_paged_attention(h, q, cache, cu, max_new=max_new, out=out[:q.shape[0]])
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    assert (out[q.shape[0]:] == 7).all()
+    sla.sla_paged_attention(h, q, cache, U.device_ints([0, 10 ** 6, -5]), max_new=max_new, out=out[:q.shape[0]])
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    assert (out[q.shape[0]:] == 7).all()
+    sla.sla_paged_attention(h, q, cache, cu, max_new=2 * max_new, out=out[:q.shape[0]])
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    h.close()
