@@ -135,6 +135,21 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned full = 0xffffffffu;
+    // a warp has as few sequences at a time as it can, so that few of them wait for one another; its first ones are on their way at once
+    const int per = min(32, (a.b.n_seqs + kWarps - 1) / kWarps);
+    auto sequence = [&](int x) {
+        int4 s = make_int4(-1, 0, 0, 0);
+        if (lane < per && x < a.b.n_seqs) {
+            int r1;
+            new_rows(a.b, x, s.w, r1);
+            s.z = r1 - s.w;
+            s.x = slot_of(a.c, a.b, x);
+            if (s.x < 0) atomicOr(a.c.status, kStatusBadIndex);
+            else s.y = tokens_of(a.c, s.x);
+        }
+        return s;
+    };
+    int4 of = sequence(warp * per + lane);
     // units of every sequence (a cu_new that does not ascend could name more than there is room for: those are left out)
     if (warp == 0) {
         int at = 0;
@@ -167,19 +182,12 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
     __syncthreads();
     // weights of a sequence's units: by a lane where one unit is all there is, else by a warp
     long long reread = 0;   // bytes of keys and values that several units read
-    for (int x0 = warp * 32; x0 < a.b.n_seqs; x0 += kWarps * 32) {
+    for (int x0 = warp * per; x0 < a.b.n_seqs; x0 += kWarps * per) {
         const int x = x0 + lane;
-        int units = 0, q = 0, n = 0;
-        if (x < a.b.n_seqs) {
-            int r0, r1;
-            new_rows(a.b, x, r0, r1);
-            q = r1 - r0;
-            units = plan.unit_at[x + 1] - plan.unit_at[x];
-            const int slot = slot_of(a.c, a.b, x);
-            if (slot < 0) atomicOr(a.c.status, kStatusBadIndex);
-            else n = tokens_of(a.c, slot);
-            plan.seqs[x] = make_int4(slot, n, q, r0);
-        }
+        const bool on = lane < per && x < a.b.n_seqs;
+        if (x0 != warp * per) of = sequence(x);
+        const int n = of.y, q = of.z, units = on ? plan.unit_at[x + 1] - plan.unit_at[x] : 0;
+        if (on) plan.seqs[x] = of;
         long long total = 0;
         if (units == 1) {
             total = unit_weight(n, q, 0, q, a.window, f);
@@ -206,7 +214,7 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
                 reread += (long long)n * a.c.Hkv * a.c.D * a.c.es * 2;
             }
         }
-        if (x < a.b.n_seqs) plan.seq_at[x + 1] = total * a.c.Hkv;
+        if (on) plan.seq_at[x + 1] = total * a.c.Hkv;
     }
     __syncthreads();
     if (warp == 0) {
@@ -232,13 +240,17 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
         long long bytes = 0;
         for (int w = 0; w < kWarps; ++w) bytes += s_sum[w];
         const long long total = plan.seq_at[a.b.n_seqs];
-        long long groups = (bytes + kGroupBytes - 1) / kGroupBytes;
-        if (groups > total / (n_ctas * kGroupWeight)) groups = total / (n_ctas * kGroupWeight);
-        groups = groups < 1 ? 1 : groups > max_groups ? max_groups : groups;
+        long long groups = 1;
+        if (max_groups > 1) {
+            const long long most = quotient(total, n_ctas * kGroupWeight);
+            groups = quotient(bytes + kGroupBytes - 1, kGroupBytes);
+            groups = groups > most ? most : groups;
+            groups = groups < 1 ? 1 : groups > max_groups ? max_groups : groups;
+        }
         long long n = groups * n_ctas;
-        if (n > total / min_weight) n = total / min_weight;   // a range of a few tiles at least
+        if (n * min_weight > total) n = quotient(total, min_weight);   // a range of a few tiles at least
         if (n < 1) n = total > 0 ? 1 : 0;
-        const long long each = n ? total / n : 0;
+        const long long each = n ? quotient(total, n) : 0;
         *plan.ranges = {each, (int)n, (int)(total - each * n)};
     }
     __syncthreads();

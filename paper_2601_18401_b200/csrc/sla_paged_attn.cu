@@ -38,6 +38,16 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f,
     chain_release();
     build_plan<kPlanThreads>(a, f, n_ctas, max_groups, min_weight, own, s_sum);
     const Ranges ranges = s_ranges;
+    if (fits) {   // (by the threads that have no range, if there are such)
+        const int last = kPlanThreads - 1 - threadIdx.x;
+        for (int x = last; x <= a.b.n_seqs; x += kPlanThreads) {
+            plan.seq_at[x] = s_seq_at[x];
+            plan.unit_at[x] = s_unit_at[x];
+            if (x < a.b.n_seqs) plan.seqs[x] = s_seqs[x];
+        }
+        for (int u = last; u < s_unit_at[a.b.n_seqs]; u += kPlanThreads) plan.unit_end[u] = s_unit_end[u];
+    }
+    if (threadIdx.x == kPlanThreads - 1) *plan.ranges = ranges;
     for (int r = threadIdx.x; r < ranges.count; r += kPlanThreads) {
         Cursor c;
         Start b;
@@ -46,15 +56,6 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f,
         b.w = c.w; b.x = c.x; b.unit = c.unit; b.units = c.units;
         plan.starts[r] = b;
     }
-    if (fits) {
-        for (int x = threadIdx.x; x <= a.b.n_seqs; x += kPlanThreads) {
-            plan.seq_at[x] = s_seq_at[x];
-            plan.unit_at[x] = s_unit_at[x];
-            if (x < a.b.n_seqs) plan.seqs[x] = s_seqs[x];
-        }
-        for (int u = threadIdx.x; u < s_unit_at[a.b.n_seqs]; u += kPlanThreads) plan.unit_end[u] = s_unit_end[u];
-    }
-    if (threadIdx.x == 0) *plan.ranges = ranges;
 }
 
 // ------------------------------------------------------------------------------------------------
