@@ -778,8 +778,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
                 if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
                 const bool odd = *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1;
-                if (odd && valid && (!s.both || x == 0))
-                    redo_row<D>(p, s, x * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
+                // (both streams with the same rows: either may be the one that knows, and both write the same)
+                if (odd && valid) redo_row<D>(p, s, (s.both ? 0 : x) * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
                 ++ns;

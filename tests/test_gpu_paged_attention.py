@@ -410,3 +410,20 @@ def test_more_new_tokens_than_max_new_are_flagged(sla, dtype, max_new):
     sla.sla_paged_attention(h, q, cache, cu, max_new=2 * max_new, out=out[:q.shape[0]])
     assert sla.sla_poll_status(h) == sla.SLA_OK
     h.close()
+
+
+@pytest.mark.parametrize("n", [300, 400, 520, 650])
+@pytest.mark.parametrize("G,new", [(4, 5), (4, 20), (4, 32), (1, 40), (1, 128), (8, 16), (16, 8)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_small_units_and_values_that_are_not_finite(sla, handle, n, G, new, bad):
+    """Units of few tokens, whose tiles two groups of warps take in turn: whichever of them meets the value, all rows that see it
+    have it and the others do not, at either end of a window."""
+    for window in (0, 200):
+        for back in {0, new // 2, new - 1}:
+            for at in (n - 1 - back, n - window - back):
+                if at >= n:
+                    continue
+
+                def prep(k, v, table, q):
+                    v[int(table[0, at // 16]), 1, at % 16, 5] = bad
+                run(sla, handle, [n], [new], G=G, window=window, prep=prep)
