@@ -427,3 +427,53 @@ def test_small_units_and_values_that_are_not_finite(sla, handle, n, G, new, bad)
                 def prep(k, v, table, q):
                     v[int(table[0, at // 16]), 1, at % 16, 5] = bad
                 run(sla, handle, [n], [new], G=G, window=window, prep=prep)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("new", [3, 20, 70, 200])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_cut_units_and_values_that_are_not_finite(sla, handle, dtype, d, new, bad):
+    """The same where a sequence is cut into parts that several CTAs attend to: near its end, at a window's beginning, in every tile."""
+    n = 4000 + 37 * new
+    for window in (0, 2500):
+        for at in (n - 1, n - new, n - 1 - new // 2, n - window - new // 2, n - 130):
+            if at >= n:
+                continue
+
+            def prep(k, v, table, q):
+                v[int(table[0, at // 16]), 1, at % 16, d - 3] = bad
+                v[int(table[1, 10]), 0, 3, 2] = bad
+            run(sla, handle, [n, 350], [new, new], dtype=dtype, d=d, window=window, prep=prep)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("tokens_inside", [False, True])
+@pytest.mark.parametrize("G,n,new", [(4, [6000, 90], [3, 4]), (4, [6000, 90], [70, 90]), (3, [300, 41], [300, 41]), (1, [5000], [130]), (16, [2000, 7], [1, 1])])
+def test_queries_of_any_16_bytes(sla, handle, dtype, d, tokens_inside, G, n, new):
+    """Rows of q and out that begin at any multiple of 16 bytes, tokens inside or outside heads, whole and cut units."""
+    cache, k, v, table, q, cu = build(sla, n, new, dtype=dtype, d=d, G=G)
+    T, H = q.shape[:2]
+    a, b = (H, T) if tokens_inside else (T, H)
+
+    def wide(x):
+        big = torch.full((a, b, d + 8), 7.0, dtype=dtype, device="cuda:0")
+        view = big[:, :, 8:]
+        view.copy_(x.transpose(0, 1) if tokens_inside else x)
+        return big, view.transpose(0, 1) if tokens_inside else view
+    _, q2 = wide(q)
+    big, out = wide(torch.zeros_like(q))
+    o, lse = sla.sla_paged_attention(handle, q2, cache, cu, max_new=max(new), out=out)
+    U.check_attention(o, lse, U.attention_reference(q, k, v, table, n, new, G, 0, d ** -0.5, 16), dtype)
+    assert (big[:, :, :8] == 7).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,new,G,window", [([20011], [300], 4, 0), ([20011, 17000], [150, 40], 4, 16900), ([33000], [20], 4, 0), ([18000, 19000], [260, 129], 1, 0)])
+@pytest.mark.parametrize("bad", [None, math.nan])
+def test_long_units_in_turns(sla, handle, d, n, new, G, window, bad):
+    """Units of so many keys that CTAs begin them at different ones."""
+    def prep(k, v, table, q):
+        if bad is not None:
+            at = n[0] - 1 - new[0] // 2
+            v[int(table[0, at // 64]), 1, at % 64, 7] = bad
+    run(sla, handle, n, new, d=d, G=G, window=window, page=64, prep=prep)
