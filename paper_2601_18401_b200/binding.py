@@ -507,6 +507,11 @@ def _output(t: Optional[torch.Tensor], shape, device, dtype=torch.float32) -> to
     return t
 
 
+def _int32_output(t: Optional[torch.Tensor], cache: sla_cache_t, *shape: int) -> torch.Tensor:
+    # (new_empty of plain numbers takes half the time of torch.empty)
+    return cache.tensors[3].new_empty(*shape) if t is None else _output(t, shape, None, torch.int32)
+
+
 def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: torch.Tensor, ref: torch.Tensor) -> sla_cache_t:
     """A paged cache from its tensors: k, v [n_pages, Hkv, page_tokens, D] (any strides with D contiguous; the two share them),
     table int32 [n_slots, table_width], n_tokens int32 [n_slots], ref int32 [n_pages], all on one device."""
@@ -542,10 +547,6 @@ def _slots(cache: sla_cache_t, cu_new: Optional[torch.Tensor], seq: Optional[tor
     return cu_new.numel() - 1 if cu_new is not None else seq.numel() if seq is not None else cache.n_slots
 
 
-def _device_of(cache: sla_cache_t) -> torch.device:
-    return cache.tensors[2].device
-
-
 def sla_paged_workspace_bytes(cache: sla_cache_t, n_q_heads: int, n_seqs: int, n_new: int,
                               params: Optional[sla_params_t] = None) -> int:
     """Workspace that the paged calls need for batches of up to n_seqs sequences and n_new tokens; params: of
@@ -560,7 +561,7 @@ def sla_cache_extend(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     first new token, -1 where it was refused.  n_new: rows of the call, when cu_new's last entry does not bound them yet."""
     n = _slots(cache, cu_new, seq)
     _on_gpu(cache.tensors[0], cu_new, seq)
-    first = _output(first, (n,), _device_of(cache), torch.int32)
+    first = _int32_output(first, cache, n)
     rows = n if cu_new is None or n == 0 else 0x7FFFFFFF if n_new is None else int(n_new)
     b = sla_batch_t(n, rows, 1 if cu_new is None else rows, 0, None if seq is None else _int32(seq, "seq").data_ptr(),
                     None if cu_new is None else _int32(cu_new, "cu_new").data_ptr())
@@ -599,7 +600,7 @@ def sla_cache_fork(handle: Handle, cache: sla_cache_t, src: torch.Tensor, dst: t
     if _int32(dst, "dst").numel() != n:
         raise ValueError("src and dst must have the same length")
     _on_gpu(cache.tensors[0], src, dst)
-    pairs = _output(pairs, (2, n), _device_of(cache), torch.int32)
+    pairs = _int32_output(pairs, cache, 2, n)
     handle.check(handle._lib.sla_cache_fork(handle.ptr, cache.address, src.data_ptr(), dst.data_ptr(), n, pairs.data_ptr(),
                                             _stream_ptr(stream)), "sla_cache_fork")
     return pairs
@@ -608,7 +609,7 @@ def sla_cache_fork(handle: Handle, cache: sla_cache_t, src: torch.Tensor, dst: t
 def sla_cache_compact(handle: Handle, cache: sla_cache_t, *, pairs=None, stream=None):
     """Moves the pages in use to the front of the pool -> pairs int32 [2, n_pages] of the moves, then -1."""
     _on_gpu(cache.tensors[0])
-    pairs = _output(pairs, (2, cache.n_pages), _device_of(cache), torch.int32)
+    pairs = _int32_output(pairs, cache, 2, cache.n_pages)
     handle.check(handle._lib.sla_cache_compact(handle.ptr, cache.address, pairs.data_ptr(), _stream_ptr(stream)),
                  "sla_cache_compact")
     return pairs
