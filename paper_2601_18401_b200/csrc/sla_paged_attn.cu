@@ -1,7 +1,7 @@
 // Attention of new tokens over a paged cache: the plan of a call, the kernel for fp32 (and for bf16 pools whose strides no tensor
 // map can follow), and the join of partial results.
 //
-//   paged_plan     one CTA: units, their weights, the cut into equal ranges (sla_paged.cuh)
+//   paged_plan     one CTA: units, their weights, the cut into equal ranges, where each begins (sla_paged.cuh)
 //   paged_rows     a range per CTA: tiles of 64 keys against R rows (tokens x heads of a group) in fp32; running maximum and sum
 //   paged_merge    per row of a cut unit: the partial results weighted by their log-sum-exp
 //
@@ -449,6 +449,8 @@ cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p
 PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     PagedPlan p;
     p.kind = PagedPlan::kRows;
+    // 64 rows where no sequence has more, else 128: fp32, 2 sequences of 4000 to 9000 tokens, 12 to 16 new, 8/2 heads, D 64, 40 us against 53
+    // with 128; 1000 new at 4000, D 128, 374 us with 128 against 468.
     p.R = a.b.max_new * (long long)a.G <= 64 ? 64 : 128;
     p.RS = p.R;
     p.TS = p.TQ = p.R / a.G;

@@ -20,7 +20,8 @@
 // before that rounding, whose errors (2^-9 each) are independent and average out over the keys.  The result is rounded once.
 //
 // A unit of one stream's rows or fewer -- the end of a chunk, a few tokens of a batch -- goes through both streams all the same, every
-// second tile each, and the two sums are joined where the results are written: its tiles take half the time.
+// second tile each, and the two sums are joined where the results are written: its tiles take half the time.  (24 sequences of 100 to 4000
+// tokens, 1 to 300 new: 60 us, 69 where such a unit keeps to one stream.)
 //
 // Values in masked places: a masked weight is 0, and 0 times NaN is NaN, so a value that some row must not see may not enter the
 // product unless it is finite.  Only the tiles at the edges of the mask hold such keys; there the row warps clear the values
