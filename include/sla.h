@@ -196,6 +196,11 @@ sla_status_t sla_probe_l2_read(sla_handle_t handle, const void *buf, size_t byte
 sla_status_t sla_selftest_wait_expiry(sla_handle_t handle, int32_t max_polls, int32_t *polls_done_device,
                                       void *stream);
 
+/* The same for the tensor-core kernel of sla_paged_attention: while enabled, its thread blocks leave as if their
+ * first wait had run out, before any copy or MMA is issued.  The call then writes no row of out and lse, and the next
+ * sla_poll_status reports SLA_ERR_DEVICE_TIMEOUT.  Calls that run on other kernels are not affected. */
+sla_status_t sla_selftest_paged_expiry(sla_handle_t handle, int enable);
+
 /* The two integer tables the library derives from exponents other than 1/2 (host-only diagnostics, so
  * that the rounding rule stated at sla_params_t can be checked without a device; Section "Span
  * attention", anchors at i - (s+1)^(1/p) + 1, and l(i) proportional to i^p):

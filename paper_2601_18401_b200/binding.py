@@ -22,6 +22,7 @@ SLA_UNION, SLA_PER_SPAN = 0, 1
 SLA_ERR_INVALID_ARG = -1
 SLA_ERR_UNSUPPORTED = -2
 SLA_ERR_WORKSPACE = -3
+SLA_ERR_DEVICE_TIMEOUT = -5
 SLA_ERR_DEVICE_INDEX = -6
 SLA_ERR_CACHE_FULL = -8
 
@@ -32,6 +33,7 @@ EXPORTS = [
     "sla_kernel_time_ms", "sla_decode_step_static", "sla_span_attention_gated",
     "sla_decode_shard_search", "sla_decode_shard_attend", "sla_decode_shard_merge",
     "sla_pattern_offsets", "sla_pattern_len_steps", "sla_probe_l2_read", "sla_selftest_wait_expiry",
+    "sla_selftest_paged_expiry",
     "sla_set_debug_canaries", "sla_selftest_canary_trip", "sla_attention_tile_stats",
     "sla_paged_workspace_bytes", "sla_cache_extend", "sla_cache_append", "sla_cache_release", "sla_cache_fork",
     "sla_cache_compact", "sla_cache_copy", "sla_paged_attention", "sla_paged_decode_step",
@@ -134,6 +136,8 @@ def load_library():
     lib.sla_probe_l2_read.argtypes = [vp, vp, sz, C.c_int32, vp, vp]
     lib.sla_selftest_wait_expiry.restype = i32
     lib.sla_selftest_wait_expiry.argtypes = [vp, C.c_int32, vp, vp]
+    lib.sla_selftest_paged_expiry.restype = i32
+    lib.sla_selftest_paged_expiry.argtypes = [vp, i32]
     # (the structs of the paged calls go by address: a serving step is a handful of calls of a few microseconds each)
     f32 = C.c_float
     lib.sla_paged_workspace_bytes.restype = sz
@@ -304,6 +308,11 @@ def sla_selftest_wait_expiry(handle: Handle, max_polls: int = 2000, polls_done: 
     handle.check(handle._lib.sla_selftest_wait_expiry(handle.ptr, int(max_polls),
                                                      None if polls_done is None else polls_done.data_ptr(),
                                                      _stream_ptr(stream)), "sla_selftest_wait_expiry")
+
+
+def sla_selftest_paged_expiry(handle: Handle, enable: bool) -> None:
+    """While enabled, the tensor-core kernel of sla_paged_attention leaves as if its first wait had run out."""
+    handle.check(handle._lib.sla_selftest_paged_expiry(handle.ptr, int(bool(enable))), "sla_selftest_paged_expiry")
 
 
 def sla_poll_status(handle: Handle, stream=None) -> int:

@@ -21,6 +21,7 @@ struct sla_handle_s {
     sla::KernelTimer timer;   // sla_set_kernel_timing / sla_kernel_time_ms
     sla::TcLast tc_last;      // tile table of the most recent tensor-core attention chunk
     bool canaries = false;    // sla_set_debug_canaries
+    bool paged_expiry = false;   // sla_selftest_paged_expiry
     sla::Canaries last_canaries;   // of the most recent call that laid any, and where its scratch began
     char *last_canary_base = nullptr;
     // stride-offset and span-length tables for exponents other than 1/2 (host copies; the device
@@ -348,6 +349,12 @@ sla_status_t sla_selftest_wait_expiry(sla_handle_t h, int32_t max_polls, int32_t
                                                      static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_selftest_wait_expiry");
     h->launches += 1;
+    return SLA_OK;
+}
+
+sla_status_t sla_selftest_paged_expiry(sla_handle_t h, int enable) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    h->paged_expiry = enable != 0;
     return SLA_OK;
 }
 
@@ -982,6 +989,7 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     a.q_st = q_stride_t;
     a.q_sh = q_stride_h;
     a.scale = softmax_scale;
+    a.expire = h->paged_expiry;
     const sla::PagedPlan plan = sla::plan_paged(a, c->dtype, h->sm_count);
     if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
     cudaError_t e = sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, static_cast<cudaStream_t>(stream), &h->launches);

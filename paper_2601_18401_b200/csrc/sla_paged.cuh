@@ -66,6 +66,7 @@ struct PagedCall {
     int Hq, G, window;
     long long q_st, q_sh;      // strides of q and out, in elements
     float scale;
+    int expire;                // self-test: the CTAs of paged_tiles leave as if their first wait had run out
 };
 
 // Whole part of a / b for 0 <= a < 2^53, b > 0: an estimate put right, where a 64-bit division is a hundred instructions, each

@@ -20,7 +20,7 @@ constexpr int kPlanThreads = 1024;
 
 // The plan is built in shared memory where it fits (4 to 6 us), else where it goes.
 constexpr int kPlanSeqs = 512, kPlanUnits = 2048;
-__global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f, int n_ctas, int max_groups, int min_weight, Plan plan) {
+__global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f, int n_ctas, int max_groups, int min_weight, Plan plan, Cut *__restrict__ cut) {
     __shared__ long long s_sum[kPlanThreads / 32], s_seq_at[kPlanSeqs + 1], s_unit_end[kPlanUnits];
     __shared__ int s_unit_at[kPlanSeqs + 1];
     __shared__ int4 s_seqs[kPlanSeqs];
@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan(PagedCall a, Shape f,
         c.next(a, own, f, b.s, b.last_range);
         b.w = c.w; b.x = c.x; b.unit = c.unit; b.units = c.units;
         plan.starts[r] = b;
+        cut[r] = {0, 0, 0, -1};   // a CTA that leaves early (a wait that ran out) leaves its ranges so, and paged_merge writes nothing for them
     }
 }
 
@@ -431,7 +432,7 @@ cudaError_t run_rows(const void *q, const PagedCall &a, const PagedPlan &p, char
 
 cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scratch, cudaStream_t st) {
     return launch_chained(paged_plan, dim3(1), dim3(kPlanThreads), 0, st, a, Shape{p.TQ, p.kt_shift, p.small}, p.n_ctas, p.max_groups, p.min_weight,
-                          plan_at(p, scratch));
+                          plan_at(p, scratch), parts_at(p, scratch).cut);
 }
 
 template <typename T, int D>

@@ -28,7 +28,8 @@
 // beyond the sequence's end (a page's stale rest) and look at the others, and if one is not finite all rows of the segment are
 // computed again by themselves, each over the keys it sees (redo_row).
 //
-// Every wait on an mbarrier is bounded; when one runs out the CTA sets a status bit, drains and leaves.
+// Every wait on an mbarrier is bounded; when one runs out the CTA sets a status bit, drains and leaves.  The ranges that it had not
+// finished handing out stay without a cut (paged_plan has set them so): no unit that begins in them is joined.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -445,7 +446,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             const bool leader = ptx::elect_one();
             uint32_t k = 0, nq[2] = {0, 0};
             int at = 0;   // tiles so far
-            bool ok = true;
+            bool ok = !p.a.expire;
+            if (!ok) *abort_flag = 1;
             auto put = [&](const Seg &s) {
                 ok = ptx::mbar_wait_warp(bar_seg_empty + 8 * (k % kSegs), ((k / kSegs) & 1u) ^ 1u, abort_flag);
                 if (ok && leader) {
@@ -512,7 +514,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         __syncwarp();
                     }
                 } while (ok && cur.next(p.a, p.plan, Shape{2 * TS, kTileShift, TS}, g, last_range));
-                if (leader) p.parts.cut[range] = cut;
+                if (leader && ok) p.parts.cut[range] = cut;
             }
             s = Seg{};
             if (ok) put(s);

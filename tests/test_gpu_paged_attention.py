@@ -477,3 +477,29 @@ def test_long_units_in_turns(sla, handle, d, n, new, G, window, bad):
             at = n[0] - 1 - new[0] // 2
             v[int(table[0, at // 64]), 1, at % 64, 7] = bad
     run(sla, handle, n, new, d=d, G=G, window=window, page=64, prep=prep)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_after_a_wait_that_ran_out_no_row_is_written(sla, d):
+    """CTAs that leave early leave their ranges without a cut: the join writes nothing from what an earlier call of the same
+    layout, or of another, has left in the scratch memory."""
+    h = sla.Handle(0, 1 << 28)
+    n, new = [9000, 4000, 2500], [70, 300, 129]
+    cache, k, v, table, q, cu = build(sla, n, new, d=d, page=64)
+    big = build(sla, [6000] * 9, [700] * 9, d=d, page=64, seed=8)
+    want = sla.sla_paged_attention(h, q, cache, cu, max_new=300)
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    rows, guard = q.shape[0], 512
+    for before in (lambda: None, lambda: sla.sla_paged_attention(h, big[4], big[0], big[5], max_new=700)):
+        before()
+        out = torch.full((rows + 2 * guard, *q.shape[1:]), 7.0, dtype=q.dtype, device=q.device)
+        lse = torch.full((rows + 2 * guard, q.shape[1]), 7.0, device=q.device)
+        sla.sla_selftest_paged_expiry(h, True)
+        sla.sla_paged_attention(h, q, cache, cu, max_new=300, out=out[guard:guard + rows], lse=lse[guard:guard + rows])
+        sla.sla_selftest_paged_expiry(h, False)
+        assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_TIMEOUT
+        assert (out == 7).all() and (lse == 7).all()
+    again = sla.sla_paged_attention(h, q, cache, cu, max_new=300)
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+    h.close()
