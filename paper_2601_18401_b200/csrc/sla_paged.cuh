@@ -115,10 +115,11 @@ struct Shape {
     int TQ, kt_shift, small;
 };
 
-// Keys of the new tokens [t0, t1) of a sequence of n tokens, q of them new: tiles [lo, hi) of KT keys.
-__device__ __forceinline__ void unit_tiles(int n, int q, int t0, int t1, int window, int kt_shift, int &lo, int &hi) {
+// Keys of the new tokens [t0, t1) of a sequence of n tokens, q of them new: tiles [lo, hi) of KT keys.  (A position is negative where the
+// sequence is shorter than its new tokens, and the window may be the largest int: their difference is formed only where it is positive.)
+__host__ __device__ __forceinline__ void unit_tiles(int n, int q, int t0, int t1, int window, int kt_shift, int &lo, int &hi) {
     const int p0 = n - q + t0, end = n - q + t1;   // first position, one past the last
-    const int first = window > 0 && p0 - window + 1 > 0 ? p0 - window + 1 : 0;
+    const int first = window > 0 && p0 >= window ? p0 - window + 1 : 0;
     lo = first >> kt_shift;
     hi = end > 0 ? (end + (1 << kt_shift) - 1) >> kt_shift : lo;
     if (hi < lo) hi = lo;

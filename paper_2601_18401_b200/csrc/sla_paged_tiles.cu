@@ -632,9 +632,9 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             const Seg &s = meta->seg[k % kSegs];
             const int tok = s.t0 + (s.both ? 0 : x * TS) + t;
             const bool valid = t < TS && g < G && tok < s.t1;
-            const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 ? max(last - p.a.window + 1, 0) : 0;   // keys seen
+            const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 && last >= p.a.window ? last - p.a.window + 1 : 0;   // keys seen
             // keys that not every row of the unit sees lie outside [all_lo, all_hi]
-            const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? s.n - s.q + s.t1 - p.a.window : 0;
+            const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? max(s.n - s.q + s.t1, 0) - p.a.window : 0;
             if (s.own[x] > 0) {
                 const int lx = s.lo_x[x], hx = s.hi_x[x], step = s.both ? 2 : 1;
                 int j = s.begin_x[x];

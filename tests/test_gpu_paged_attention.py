@@ -503,3 +503,14 @@ def test_after_a_wait_that_ran_out_no_row_is_written(sla, d):
     assert sla.sla_poll_status(h) == sla.SLA_OK
     assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
     h.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("window", [2 ** 30, 2 ** 31 - 5, 2 ** 31 - 1])
+@pytest.mark.parametrize("n,new", [([1], [4]), ([10], [20]), ([3, 0, 20, 1], [5, 4, 20, 3]), ([130, 40], [200, 300])])
+def test_a_window_beyond_any_length_is_none(sla, handle, dtype, window, n, new):
+    """Sequences shorter than their new tokens, whose first positions are negative, under windows up to the largest int."""
+    for bound in (max(new), 400):
+        a, la, _ = run(sla, handle, n, new, window=window, dtype=dtype, max_new=bound)
+        b, lb, _ = run(sla, handle, n, new, dtype=dtype, max_new=bound)
+        assert torch.equal(a, b) and torch.equal(la, lb)

@@ -124,3 +124,34 @@ def test_reference_against_dense_attention():
         assert torch.allclose(out[r:r + new[x]], torch.einsum("htj,jhd->thd", z.softmax(-1), vv))
         assert torch.allclose(lse[r:r + new[x]], z.logsumexp(-1).T)
         r += new[x]
+
+
+def test_tiles_of_a_unit_do_not_overflow(tmp_path):
+    """unit_tiles, compiled for the host with signed overflow as an error, against plain Python: positions from below zero to the
+    longest sequence, windows up to the largest int."""
+    import os
+    import subprocess
+    from paper_2601_18401_b200 import build
+    src, exe = tmp_path / "t.cu", tmp_path / "t"
+    src.write_text("""
+#include <stdio.h>
+#include "sla_paged.cuh"
+int main() {
+    int n, q, t0, t1, window, shift, lo, hi;
+    while (scanf("%d %d %d %d %d %d", &n, &q, &t0, &t1, &window, &shift) == 6) {
+        sla::unit_tiles(n, q, t0, t1, window, shift, lo, hi);
+        printf("%d %d\\n", lo, hi);
+    }
+}
+""")
+    subprocess.run([build._nvcc(), "-std=c++17", "-Xcompiler", "-fsanitize=signed-integer-overflow,-fno-sanitize-recover=all", "-I", build.CSRC,
+                    "-I", os.path.join(build.ROOT, "include"), str(src), "-o", str(exe)], check=True, capture_output=True)
+    top = 2 ** 31 - 1025
+    cases = [(n, q, t0, min(t0 + 32, q), w, s) for n in (0, 1, 10, 129, 5000, top) for q in (1, 4, 20, 5000) for t0 in (0, 3, 64, 4990) if t0 < q
+             for w in (0, 1, 7, 128, 5000, 2 ** 30, 2 ** 31 - 2, 2 ** 31 - 1) for s in (6, 7)]
+    r = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in cases), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    for (n, q, t0, t1, w, s), line in zip(cases, r.stdout.splitlines(), strict=True):
+        p0, end = n - q + t0, n - q + t1
+        lo = (max(p0 - w + 1, 0) if w else 0) >> s
+        assert line == f"{lo} {max(-(-end >> s) if end > 0 else lo, lo)}", (n, q, t0, t1, w, s)
