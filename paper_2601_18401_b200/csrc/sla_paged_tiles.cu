@@ -25,8 +25,8 @@
 //
 // Values in masked places: a masked weight is 0, and 0 times NaN is NaN, so a value that some row must not see may not enter the
 // product unless it is finite.  Only the tiles at the edges of the mask hold such keys; there the row warps clear the values
-// beyond the sequence's end (a page's stale rest) and look at the others, and if one is not finite all rows of the segment are
-// computed again by themselves, each over the keys it sees (redo_row).
+// beyond the sequence's end (a page's stale rest) and look at the others; what is not finite is cleared too, and added to O of the
+// rows that see its key when the segment's products are done (add_not_finite).
 //
 // Every wait on an mbarrier is bounded; when one runs out the CTA sets a status bit, drains and leaves.  The ranges that it had not
 // finished handing out stay without a cut (paged_plan has set them so): no unit that begins in them is joined.
@@ -91,12 +91,11 @@ struct Meta {
     uint32_t tmem_base;
     int abort_flag;
     uint32_t s_time[2];               // clock at the stream's last S
-    // [stream][segment & 7]: the segment (counted from 1) if it has a value that is not finite.  Whoever finds one says so to both
-    // streams before it clears the value; the ring of ten stages at most (a tile of K and of V each) keeps the streams less than eight segments with tiles apart.
+    // [stream][segment & 7]: the segment (counted from 1) if values that are not finite were cleared in it.  Whoever finds one says so
+    // to both streams before it clears it; the ring of ten stages at most (a tile of K and of V each) keeps the streams less than eight segments with tiles apart.
     int odd[2][8];
     alignas(16) Seg seg[kSegs];
     float2 stats[2][kRows];           // {1 / sum, log2-sum-exp} of the segment's rows
-    int redone[2];                    // the row warps have written the stream's results themselves
 };
 static_assert(sizeof(Meta) <= 3072, "meta block too large");
 
@@ -171,63 +170,88 @@ __device__ __forceinline__ uint64_t desc_advance(uint64_t desc, uint32_t bytes) 
     return desc;
 }
 
-// One row of a segment by itself: keys [k0, k1), fp32 from global memory, values entering only with the keys the row sees.
+// Of every bf16 of a pair of two: all bits of the half where the exponent is all ones, an infinity or a NaN.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((((w & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu; }
+
+// Clears what is not finite in the row of 128 bytes at v (and in the next half's).
 template <int D>
-__device__ __noinline__ void redo_row(const TileParams &p, const Seg &s, int canon, int t, int g, int k0, int k1) {
-    const int h = s.head * p.a.G + g;
-    const long long row = s.row0 + t;
-    const bf16 *q = p.q + row * p.a.q_st + (long long)h * p.a.q_sh;
+__device__ __noinline__ void clear_not_finite(uint4 *v) {
+#pragma unroll 1
+    for (int h = 0; h < D / 64; ++h)
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c) {
+            uint4 &w = v[h * (Layout<D>::kHalfBytes / 16) + c];
+            w = make_uint4(w.x & ~not_finite(w.x), w.y & ~not_finite(w.y), w.z & ~not_finite(w.z), w.w & ~not_finite(w.w));
+        }
+}
+
+// Adds the values that the row warps have cleared to the rows of O that see them: those that are not finite, of the keys of stream x
+// that not every row of the unit sees.  Whatever a row's sums and maxima are, such a value makes the result infinite or NaN, so that
+// its weight counts only as positive or (a logit of -inf) zero.  A converged warp with a row of O a lane; a lane looks at one of 32
+// keys.  The keys lie at the two ends of the mask, at most the unit's tokens and a tile at each, however long the segment is.
+template <int D>
+__device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, int x, const bf16 *q, int first, int last, int all_lo, int all_hi, uint32_t o_addr) {
+    const int lane = threadIdx.x & 31, end = min(s.hi * kKeys, s.n);
     const int *table = p.a.c.table + (long long)max(s.slot, 0) * p.a.c.width;
     auto at = [&](int j) {
-        return valid_page(p.a.c, table[j >> p.a.c.shift]) * p.a.c.s_page + s.head * p.a.c.s_h + (long long)(j & (p.a.c.P - 1)) * p.a.c.s_t;
+        return valid_page(p.a.c, __ldg(table + (j >> p.a.c.shift))) * p.a.c.s_page + s.head * p.a.c.s_h + (long long)(j & (p.a.c.P - 1)) * p.a.c.s_t;
     };
-    auto logit = [&](int j) {
-        const bf16 *k = reinterpret_cast<const bf16 *>(p.a.c.k) + at(j);
-        float sum = 0.f;
 #pragma unroll 1
-        for (int d = 0; d < D; d += 8) {
-            float a[8], b[8];
-            Vec16<bf16>::load(q + d, a);
-            Vec16<bf16>::load(k + d, b);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(a[e], b[e], sum);
+    for (int j0 = s.lo * kKeys; j0 < end; j0 += 32) {
+        if (j0 >= all_lo && j0 + 31 <= all_hi) {   // every row sees these 32 keys, and all up to all_hi: the product has them
+            j0 += (all_hi + 1 - j0) / 32 * 32 - 32;
+            continue;
         }
-        return sum * p.a.scale * kLog2e;
-    };
-    float m = -CUDART_INF_F, l = 0.f;
-#pragma unroll 1
-    for (int j = k0; j < k1; ++j) m = fmaxf(m, logit(j));
-    const float base = m == -CUDART_INF_F ? 0.f : m;
-#pragma unroll 1
-    for (int j = k0; j < k1; ++j) l += ex2_approx(logit(j) - base);
-    const bool none = l == 0.f && m == -CUDART_INF_F;
-    const float inv = none ? 0.f : 1.f / l, lse2 = none ? -CUDART_INF_F : m + log2f(l);
-#pragma unroll 1
-    for (int d0 = 0; d0 < D; d0 += 32) {
-        float acc[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) acc[e] = 0.f;
-#pragma unroll 1
-        for (int j = k0; j < k1; ++j) {
-            const float w = ex2_approx(logit(j) - base);
-            const bf16 *v = reinterpret_cast<const bf16 *>(p.a.c.v) + at(j) + d0;
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-                float b[8];
-                Vec16<bf16>::load(v + e, b);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) acc[e + u] = fmaf(w, b[u], acc[e + u]);
+        const int j = j0 + lane;
+        uint32_t bad = 0;
+        if (j < end && (j < all_lo || j > all_hi) && (!s.both || (s.place(j / kKeys) & 1) == x)) {
+            const uint4 *v = reinterpret_cast<const uint4 *>(reinterpret_cast<const bf16 *>(p.a.c.v) + at(j));
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+                const uint4 w = __ldg(v + c);
+                bad |= not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w);
             }
         }
+#pragma unroll 1
+        for (unsigned left = __ballot_sync(0xffffffffu, bad != 0); left; left &= left - 1) {
+            const int key = j0 + __ffs(left) - 1;
+            const long long off = at(key);
+            const bool sees = key >= first && key <= last;
+            float weight = 1.f;
+            if (sees) {
+                const bf16 *k = reinterpret_cast<const bf16 *>(p.a.c.k) + off;
+                float dot = 0.f;
+#pragma unroll 2
+                for (int d = 0; d < D; d += 8) {
+                    float a[8], b[8];
+                    Vec16<bf16>::load(q + d, a);
+                    Vec16<bf16>::load(k + d, b);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            const float o = none ? 0.f : acc[e] * inv;
-            if (s.part < 0) p.out[row * p.a.q_st + (long long)h * p.a.q_sh + d0 + e] = __float2bfloat16_rn(o);
-            else *p.parts.at(s.part, 256, D, canon, d0 + e) = o;
+                    for (int e = 0; e < 8; ++e) dot = fmaf(a[e], b[e], dot);
+                }
+                if (dot == -CUDART_INF_F) weight = 0.f;   // (a NaN, or +inf, is in the row's sum)
+            }
+            __syncwarp();
+            const bf16 *v = reinterpret_cast<const bf16 *>(p.a.c.v) + off;
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {
+                float f[2][8];
+                Vec16<bf16>::load(v + c, f[0]);
+                Vec16<bf16>::load(v + c + 8, f[1]);
+                uint32_t o[16];
+                ptx::tmem_ld16(o_addr + c, o);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float u = f[e >> 3][e & 7];
+                    if (sees && !(fabsf(u) < CUDART_INF_F)) o[e] = __float_as_uint(fmaf(weight, u, __uint_as_float(o[e])));
+                }
+                ptx::tmem_st16(o_addr + c, o);
+                ptx::tmem_wait_st();
+            }
         }
     }
-    if (s.part < 0) p.lse[row * p.a.Hq + h] = lse2 * kLn2;
-    else p.parts.lse2[(long long)s.part * 256 + canon] = lse2;
+    ptx::tc_fence_before();
 }
 
 template <int D>
@@ -534,7 +558,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             for (int x = 0; x < 2 && ok; ++x) {
                 const int tok = s.t0 + x * TS + t;
                 const bool has = s.own[x] > 0, second = s.both && s.own[1] > 0;
-                bool write = t < TS && g < G && tok < s.t1;
+                const bool write = t < TS && g < G && tok < s.t1;
                 const int h = s.head * G + g;
                 const long long r = s.row0 + tok;
                 bf16 *dst = p.out + r * p.a.q_st + (long long)h * p.a.q_sh;
@@ -546,7 +570,6 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     ++ns[x];
                     ptx::tc_fence_after();
                     stat = meta->stats[x][row];
-                    write = write && !meta->redone[x];
                 }
                 if (second) {   // two sums over every second tile each
                     ok = ptx::mbar_wait_warp(bar_l_full + 8, ns[1] & 1u, abort_flag) && ptx::mbar_wait_warp(bar_o_full + 8, ns[1] & 1u, abort_flag);
@@ -554,7 +577,6 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     ++ns[1];
                     ptx::tc_fence_after();
                     const float2 other = meta->stats[1][row];
-                    write = write && !meta->redone[1];
                     const float top = fmaxf(stat.y, other.y), ref = top == -CUDART_INF_F ? 0.f : top;
                     const float w0 = ex2_approx(stat.y - ref), w1 = ex2_approx(other.y - ref), sum = w0 + w1;
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -621,7 +643,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         // ---------------- rows of stream x: a thread a row
         ptx::setmaxnreg_inc<kRegsRow>();
         const int x = warp >> 2, row = tid & 127;
-        const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G, canon = t * G + g;
+        const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G;
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const uint32_t o_addr = lane_addr + kColO + x * 128, s_col = lane_addr + kColS + x * 128;
         const float scale2 = p.a.scale * kLog2e;
@@ -736,7 +758,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                             if (!(ok = ptx::mbar_wait_warp(bar_kv_full + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
                             const int key = k0 + row;
                             uint4 *vr = reinterpret_cast<uint4 *>(smem + L::kOffKV + (v % kStages) * L::kTileBytes + row * 128);
-                            bool clear = key >= s.n;
+                            const bool clear = key >= s.n;
                             if (!clear && (key > all_hi || key < all_lo)) {
                                 uint32_t bad = 0;
 #pragma unroll
@@ -749,9 +771,9 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                                         for (int u = 0; u < 4; ++u) bad |= ((ws[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // exponent all ones
                                     }
                                 if (bad) {
-                                    clear = true;
                                     *(volatile int *)&meta->odd[0][k & 7] = *(volatile int *)&meta->odd[1][k & 7] = (int)k + 1;
                                     __threadfence_block();
+                                    clear_not_finite<D>(vr);
                                 }
                             }
                             if (clear) {
@@ -780,15 +802,16 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
                 if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
-                const bool odd = *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1;
-                // (both streams with the same rows: either may be the one that knows, and both write the same)
-                if (odd && valid) redo_row<D>(p, s, (s.both ? 0 : x) * kRows + canon, tok, g, max(first, s.lo * kKeys), min(last + 1, s.hi * kKeys));
+                if (__any_sync(0xffffffffu, *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1)) {   // (O is complete, and the next segment's first PV waits for the epilogue, which waits for this warp)
+                    if (!(ok = ptx::mbar_wait_warp(bar_o_full + 8 * x, ns & 1u, abort_flag))) break;
+                    ptx::tc_fence_after();
+                    add_not_finite<D>(p, s, x, p.q + (s.row0 + tok) * p.a.q_st + (long long)(s.head * G + g) * p.a.q_sh, first, last, all_lo, all_hi, o_addr);
+                }
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
                 ++ns;
                 const bool none = l == 0.f && fresh;   // (a row of NaN logits has a sum that is NaN)
                 meta->stats[x][row] = make_float2(none ? 0.f : 1.f / l, none ? -CUDART_INF_F : (fresh ? 0.f : m_ref) + log2f(l));
-                if ((warp & 3) == 0 && lane == 0) meta->redone[x] = odd;
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar_l_full + 8 * x);
             }

@@ -514,3 +514,58 @@ def test_a_window_beyond_any_length_is_none(sla, handle, dtype, window, n, new):
         a, la, _ = run(sla, handle, n, new, window=window, dtype=dtype, max_new=bound)
         b, lb, _ = run(sla, handle, n, new, dtype=dtype, max_new=bound)
         assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+@pytest.mark.parametrize("d,window", [(128, 0), (64, 0), (128, 700000)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_that_are_not_finite_in_long_ranges(sla, d, window, bad):
+    """8192 new tokens that end at 2^20: a CTA's ranges are some 900 thousand keys long, and a value in one of the last rows' own keys
+    (or at the window's beginning) reaches the rows that see it, in its column, without a wait that runs out."""
+    N, T, hkv, G, page = 1 << 20, 8192, 2, 16, 64
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("not enough device memory")
+    k, v = U.make_pools(N // page, hkv, page, d, BF16)
+    table = np.random.RandomState(1).permutation(N // page).astype(np.int32)[None]
+    cache = sla.make_cache(k, v, U.device_ints(table), U.device_ints([N]), U.device_ints(np.ones(N // page)))
+    q = torch.empty(T, hkv * G, d, dtype=BF16, device="cuda:0").normal_()
+    cu = U.device_ints([0, T])
+    h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, hkv * G, 1, T))
+    clean, clean_lse = sla.sla_paged_attention(h, q, cache, cu, window=window)
+    pos = torch.arange(N - T, N, device="cuda:0")
+    for at in (N - 70, N - window - 70 if window else N - T + 3):
+        for g, col in ((0, 5), (1, d - 1)):
+            v[int(table[0, at // page]), g, at % page, col] = bad
+        out, lse = sla.sla_paged_attention(h, q, cache, cu, window=window)
+        assert sla.sla_poll_status(h) == sla.SLA_OK
+        sees = (pos >= at) & ((pos - at < window) if window else True)
+        assert 0 < sees.sum() < T
+        want = clean.clone()
+        want[sees, :G, 5] = bad
+        want[sees, G:, d - 1] = bad
+        assert torch.equal(out.nan_to_num(123.0), want.nan_to_num(123.0)) and torch.equal(out.isnan(), want.isnan())
+        assert torch.equal(lse, clean_lse)
+        for g, col in ((0, 5), (1, d - 1)):
+            v[int(table[0, at // page]), g, at % page, col] = 0.5
+        clean, clean_lse = sla.sla_paged_attention(h, q, cache, cu, window=window)
+    # a few rows against 64 bits
+    scale = d ** -0.5
+    pages = torch.from_numpy(table[0].astype(np.int64)).cuda()
+    rows = [0, 17, 5000, T - 1]
+    ref = [torch.zeros(len(rows), hkv * G, d, dtype=torch.float64, device="cuda:0"), torch.zeros(len(rows), hkv * G, dtype=torch.float64, device="cuda:0")]
+    ref += [torch.zeros_like(ref[0]), torch.zeros_like(ref[1]), torch.zeros(len(rows), dtype=torch.float64, device="cuda:0")]
+    for g in range(hkv):
+        kk, vv = (t[pages, g].reshape(N, d).double() for t in (k, v))
+        hs = slice(g * G, (g + 1) * G)
+        for x, r in enumerate(rows):
+            p = N - T + r
+            lo = max(0, p - window + 1) if window else 0
+            z = q[r, hs].double() @ kk[lo:p + 1].T * scale
+            ref[1][x, hs] = torch.logsumexp(z, -1)
+            w = torch.exp(z - ref[1][x, hs, None])
+            ref[0][x, hs], ref[2][x, hs] = w @ vv[lo:p + 1], w @ vv[lo:p + 1].abs()
+            ref[3][x, hs] = (q[r, hs].double().abs() @ kk[lo:p + 1].abs().T).amax(-1) * scale
+            ref[4][x] = p + 1 - lo
+    U.check_attention(clean[rows], clean_lse[rows], ref, BF16)
+    h.close()
+    del k, v, cache
+    torch.cuda.empty_cache()
