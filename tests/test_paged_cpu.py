@@ -155,3 +155,25 @@ int main() {
         p0, end = n - q + t0, n - q + t1
         lo = (max(p0 - w + 1, 0) if w else 0) >> s
         assert line == f"{lo} {max(-(-end >> s) if end > 0 else lo, lo)}", (n, q, t0, t1, w, s)
+
+
+def test_every_call_wants_a_slot_per_sequence(sla):
+    """seq shorter or longer than the sequences of cu_new: refused before its address goes anywhere."""
+    c = cache_of(sla)
+    cu = torch.tensor([0, 1, 2, 3], dtype=torch.int32)
+    new, q = torch.zeros(3, 8, 128, dtype=torch.bfloat16), torch.zeros(3, 32, 128, dtype=torch.bfloat16)
+    from paper_2601_18401_b200 import binding as B
+    for n in (2, 4):
+        seq = torch.arange(n, dtype=torch.int32)
+        with pytest.raises(ValueError, match="one slot per sequence"):
+            sla.sla_cache_extend(None, c, cu, seq=seq)
+        with pytest.raises(ValueError, match="one slot per sequence"):
+            B._batch(cu, 3, None, seq)
+        with pytest.raises(ValueError, match="one slot per sequence"):
+            B._batch(None, 3, 1, seq)
+    with pytest.raises(ValueError, match="contiguous int32"):
+        sla.sla_cache_extend(None, c, cu, seq=torch.arange(3))
+    for call in (lambda s: sla.sla_cache_append(None, c, cu, torch.zeros(3, dtype=torch.int32), new, new, seq=s),
+                 lambda s: sla.sla_paged_attention(None, q, c, cu, seq=s), lambda s: sla.sla_paged_decode_step(None, q, q, c, sla.make_params(4, 0), seq=s)):
+        with pytest.raises(ValueError):
+            call(torch.arange(2, dtype=torch.int32))
