@@ -401,14 +401,15 @@ typedef struct {
     int32_t n_seqs;
     int32_t n_new;            /* rows of the tensors: cu_new[n_seqs]                                  */
     int32_t max_new;          /* no sequence has more new tokens than this (SLA_ERR_DEVICE_INDEX where
-                               * the kernel that it chose depends on it; results are then undefined)  */
+                               * the kernel that it chose depends on it; results are then undefined);
+                               * a bound above n_new says no more than n_new does                     */
     int32_t reserved;         /* must be 0                                                           */
     const int32_t *seq;       /* device [n_seqs]: slots, all different; NULL = 0 .. n_seqs-1         */
     const int32_t *cu_new;    /* device [n_seqs + 1], ascending from 0; NULL = one token a sequence   */
 } sla_batch_t;
 
 /* Workspace bytes that every call below needs at most, for batches of up to n_seqs sequences and n_new
- * tokens and n_q_heads query heads.  params: of sla_paged_decode_step, NULL when it is not called.  0 when the
+ * tokens, whatever their max_new, and n_q_heads query heads.  params: of sla_paged_decode_step, NULL when it is not called.  0 when the
  * arguments are invalid.  Host-only. */
 size_t sla_paged_workspace_bytes(const sla_cache_t *cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_new,
                                  const sla_params_t *params);

@@ -849,6 +849,9 @@ sla::Pages make_pages(sla_handle_t h, const sla_cache_t *c) {
 
 sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, b->seq, b->cu_new}; }
 
+// Rows that a sequence can have at most, given a bound that may be loose.
+int32_t longest_chunk(int32_t n_new, int32_t max_new) { return max_new > n_new ? n_new : max_new > 0 ? max_new : 1; }
+
 // The handle, the cache and the scratch a bookkeeping call needs.  SLA_OK when the call may go on.
 sla_status_t cache_call(sla_handle_t h, const sla_cache_t *c, size_t n_seqs) {
     if (!h) return SLA_ERR_INVALID_ARG;
@@ -876,9 +879,10 @@ size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_
     a.G = n_q_heads / c->n_kv_heads;
     a.q_sh = c->head_dim;
     a.q_st = (int64_t)n_q_heads * c->head_dim;
-    for (int32_t most : {1, n_new})         // the tiles go by the longest chunk,
-        for (float scale : {1.f, -1.f}) {   // and by the sign of the scale
-            a.b = {n_seqs, n_new, most, nullptr, nullptr};
+    // the kernel and its tiles go by the rows of the longest chunk (up to 8, 16 or 64, or more) and by the sign of the scale
+    for (int32_t most : {1, 8 / a.G, 16 / a.G, 64 / a.G, n_new})
+        for (float scale : {1.f, -1.f}) {
+            a.b = {n_seqs, n_new, longest_chunk(n_new, most), nullptr, nullptr};
             a.scale = scale;
             const size_t bytes = sla::plan_paged(a, c->dtype, 160).bytes;
             if (bytes > need) need = bytes;
@@ -983,6 +987,7 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     sla::PagedCall a;
     a.c = make_pages(h, c);
     a.b = make_batch(b);
+    a.b.max_new = longest_chunk(b->n_new, b->max_new);
     a.Hq = n_q_heads;
     a.G = n_q_heads / c->n_kv_heads;
     a.window = window;

@@ -569,3 +569,25 @@ def test_values_that_are_not_finite_in_long_ranges(sla, d, window, bad):
     h.close()
     del k, v, cache
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,d,hkv,G", [(BF16, 128, 8, 4), (BF16, 64, 2, 16), (BF16, 128, 2, 1), (F32, 128, 2, 4), (F32, 64, 1, 16)])
+@pytest.mark.parametrize("n_seqs,n_new", [(4, 4), (3, 40), (40, 300)])
+def test_a_workspace_of_the_size_asked_for_is_enough(sla, dtype, d, hkv, G, n_seqs, n_new):
+    """Every bound of the new tokens, loose ones included, batches below the size asked for, either sign of the scale."""
+    new = [n_new // n_seqs] * n_seqs
+    new[0] += n_new - sum(new)
+    n = [30 + x for x in new]
+    cache, k, v, table, q, cu = build(sla, n, new, dtype=dtype, d=d, hkv=hkv, G=G)
+    h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, hkv * G, n_seqs, n_new))
+    for scale in (None, -0.1):
+        ref = U.attention_reference(q, k, v, table, n, new, G, 0, d ** -0.5 if scale is None else scale, 16)
+        for bound in sorted({max(new), max(new) + 1, 16, 17, 64, 65, n_new, n_new + 1, 2 ** 31 - 1}):
+            if bound >= max(new):
+                U.check_attention(*sla.sla_paged_attention(h, q, cache, cu, max_new=bound, softmax_scale=scale), ref, dtype)
+        for less in range(1, n_seqs, 7):   # the first sequences alone
+            rows = sum(new[:less])
+            out, lse = sla.sla_paged_attention(h, q[:rows], cache, cu[:less + 1].contiguous(), max_new=2 ** 31 - 1, softmax_scale=scale)
+            U.check_attention(out, lse, [t[:rows] for t in ref], dtype)
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    h.close()
