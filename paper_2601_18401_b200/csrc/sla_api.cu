@@ -1018,23 +1018,30 @@ sla_status_t sla_paged_decode_step(sla_handle_t h, const void *q_s, const void *
     if (!aligned16(q_s) || !aligned16(q) || !aligned16(out)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (sla_status_t ps = prepare_pattern(h, p, max_tokens, st)) return ps;
-    const sla::Call call = make_call(h, &l, p, 1, max_tokens - 1, max_tokens);
+    // Sequences of a launch: as many as the counters and the grid's second dimension hold, all launches about the same.
+    const long long units = p->mode == SLA_PER_SPAN ? p->top_k : 1;
+    const long long by_counters = (long long)((kCounterEnd - kCounterOffset) / sizeof(int)) / (c->n_kv_heads + n_q_heads * (units + 1));
+    const long long by_grid = 65535 / (n_q_heads * units), most = by_counters < by_grid ? by_counters : by_grid;
+    if (most < 1) return fail(h, SLA_ERR_UNSUPPORTED, "too many heads for the decode step%s");
+    const int n_launches = (int)((b->n_seqs + most - 1) / most), per = (b->n_seqs + n_launches - 1) / n_launches;
+    sla::Call call = make_call(h, &l, p, 1, max_tokens - 1, max_tokens);
+    call.B = per;
     const sla::DecodePlan plan = sla::plan_decode(call, max_tokens, h->sm_count * sla::decode_attn_blocks_per_sm(c->dtype, c->head_dim),
                                                   h->canaries ? sla::Canaries::kBytes : 0);
     if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
     if ((size_t)plan.n_anchor * sizeof(float) * 8 > 180 * 1024) return fail(h, SLA_ERR_UNSUPPORTED, "context too long for the decode top-k stage%s");
-    const size_t units = p->mode == SLA_PER_SPAN ? (size_t)p->top_k : 1;
-    if ((size_t)b->n_seqs * (c->n_kv_heads + n_q_heads * (units + 1)) * sizeof(int) > kCounterEnd - kCounterOffset ||
-        (size_t)b->n_seqs * n_q_heads * units > 65535)
-        return fail(h, SLA_ERR_UNSUPPORTED, "too many (sequence, head) pairs for the decode step%s");
-    sla::Batch batch = {b->n_seqs, b->n_seqs, 1, b->seq, nullptr};
     cudaError_t e = sla::launch_canary_fill(h->ws + kHeaderBytes, plan.canaries, st);
-    if (e == cudaSuccess)
-        e = sla::launch_paged_decode(q_s, q, make_pages(h, c), batch, call, c->dtype, plan, h->ws + kHeaderBytes,
-                                     reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, out_anchor, out_score, st);
+    for (int x = 0; x < b->n_seqs && e == cudaSuccess; x += per) {
+        call.B = b->n_seqs - x < per ? b->n_seqs - x : per;   // (fewer than the plan has room for in the last launch)
+        const sla::Batch batch = {call.B, call.B, 1, b->seq ? b->seq + x : nullptr, nullptr, x};
+        const size_t at = (size_t)x * q_stride_b * elem_size(c->dtype), row = (size_t)x * n_q_heads;
+        e = sla::launch_paged_decode(static_cast<const char *>(q_s) + at, static_cast<const char *>(q) + at, make_pages(h, c), batch, call,
+                                     c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset),
+                                     static_cast<char *>(out) + at, lse + row, out_anchor + row * p->top_k, out_score + row * p->top_k, st);
+        h->launches += plan.score_first ? 2 : 1;
+    }
     if (e == cudaSuccess) e = sla::launch_canary_check(h->ws + kHeaderBytes, plan.canaries, call.status, st);
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_paged_decode_step");
-    h->launches += plan.score_first ? 2 : 1;
     if (plan.canaries.n) { h->last_canaries = plan.canaries; h->last_canary_base = h->ws + kHeaderBytes; }
     return SLA_OK;
 }

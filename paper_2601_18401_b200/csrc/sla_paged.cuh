@@ -19,7 +19,8 @@ struct Pages {
 // The sequences of a call.
 struct Batch {
     int n_seqs, n_new, max_new;
-    const int *seq, *cu;            // either may be NULL (slots 0 .. n_seqs-1; one token a sequence)
+    const int *seq, *cu;            // either may be NULL (slots slot0 .. slot0 + n_seqs - 1; one token a sequence)
+    int slot0 = 0;
 };
 
 // Rows [lo, hi) of sequence x in the call's tensors, kept inside them whatever cu_new holds.
@@ -29,7 +30,7 @@ __device__ __forceinline__ void new_rows(const Batch &b, int x, int &lo, int &hi
 }
 // The slot of sequence x, or -1 (the caller flags it).
 __device__ __forceinline__ int slot_of(const Pages &p, const Batch &b, int x) {
-    const int s = b.seq ? b.seq[x] : x;
+    const int s = b.seq ? b.seq[x] : b.slot0 + x;
     return (unsigned)s < (unsigned)p.n_slots ? s : -1;
 }
 // Tokens of a slot, kept inside its table row.

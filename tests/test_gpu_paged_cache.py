@@ -303,3 +303,30 @@ def test_span_step_refusals(sla):
     with pytest.raises(ValueError):
         sla.sla_paged_decode_step(h, q.float(), q, cache, params)
     h.close()
+
+
+@pytest.mark.parametrize("mode,n_seqs,hkv,G", [("union", 500, 8, 4), ("gated", 130, 8, 4), ("union", 300, 3, 16)])
+def test_span_step_of_more_sequences_than_one_launch_takes(sla, mode, n_seqs, hkv, G):
+    """The same anchors and scores as by parts of 20 sequences, outputs within rounding; slots in order and by name."""
+    import test_gpu_paged_attention as A
+    rs = np.random.RandomState(n_seqs)
+    n = rs.randint(0, 300, n_seqs).tolist()
+    cache, k, v, table, _, _ = A.build(sla, n, [0] * n_seqs, d=64, hkv=hkv, G=G, page=32)
+    params = sla.make_params(8, 0, head_dim=64, **(dict(window=9, mode=sla.SLA_PER_SPAN) if mode == "gated" else {}))
+    g = torch.Generator(device="cuda:0")
+    q_s, q = (torch.empty(n_seqs, hkv * G, 64, dtype=torch.bfloat16, device="cuda:0").normal_(generator=g) for _ in range(2))
+    h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, hkv * G, n_seqs, n_seqs, params=params))
+    for order in (None, rs.permutation(n_seqs)):
+        slots = np.arange(n_seqs) if order is None else order
+        out, lse, anchor, score = sla.sla_paged_decode_step(h, q_s, q, cache, params, max_tokens=400,
+                                                            seq=None if order is None else U.device_ints(order))
+        assert sla.sla_poll_status(h) == sla.SLA_OK
+        for x in range(0, n_seqs, 20):
+            part = sla.sla_paged_decode_step(h, q_s[x:x + 20], q[x:x + 20], cache, params, max_tokens=400, seq=U.device_ints(slots[x:x + 20]))
+            assert torch.equal(part[2], anchor[x:x + 20]) and torch.equal(part[3], score[x:x + 20])
+            # sums of at most 300 terms in another order, one rounding of the result each
+            big = v.float().nan_to_num().abs().max()
+            assert ((part[0].float() - out[x:x + 20].float()).abs() <= 2.0 ** -7 * part[0].float().abs() + 1e-5 * big).all()
+            a, b = part[1], lse[x:x + 20]
+            assert torch.equal(torch.isfinite(a), torch.isfinite(b)) and ((a - b).abs().nan_to_num() <= 4e-6 * (1 + a.abs().nan_to_num(posinf=0, neginf=0))).all()
+    h.close()
