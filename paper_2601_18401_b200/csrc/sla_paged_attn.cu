@@ -147,7 +147,7 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
             }
             if (tid < R) s_pos[tid] = tid < rows ? s.n - s.q + s.t0 + tid / G : -1;
             // keys that every row of the unit sees; a row sees [position - window + 1, position]
-            const int all_hi = rows == R ? s.n - s.q + s.t0 : -1, all_lo = a.window > 0 ? max(s.n - s.q + s.t1, 0) - a.window : 0;
+            const int all_hi = rows == R ? s.n - s.q + s.t0 : -1, all_lo = a.window > 0 ? minus(s.n - s.q + s.t1, a.window) : 0;
             const int reach = a.window > 0 ? a.window : 0x7fffffff;
             float m[RT], l[RT];
             unsigned long long acc[RP][DT];

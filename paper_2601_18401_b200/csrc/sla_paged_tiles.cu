@@ -189,9 +189,17 @@ __device__ __noinline__ void clear_not_finite(uint4 *v) {
 // that not every row of the unit sees.  Whatever a row's sums and maxima are, such a value makes the result infinite or NaN, so that
 // its weight counts only as positive or (a logit of -inf) zero.  A converged warp with a row of O a lane; a lane looks at one of 32
 // keys.  The keys lie at the two ends of the mask, at most the unit's tokens and a tile at each, however long the segment is.
+// (The row's address and bounds are worked out again in here, off the way of the segments that have no such value: 1 to 600 tokens of
+// 16 sequences take 60.5 us so, 61.2 with them as arguments.)
 template <int D>
-__device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, int x, const bf16 *q, int first, int last, int all_lo, int all_hi, uint32_t o_addr) {
-    const int lane = threadIdx.x & 31, end = min(s.hi * kKeys, s.n);
+__device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, int x, uint32_t tmem) {
+    const int lane = threadIdx.x & 31, row = threadIdx.x & 127, TS = p.TS, G = p.a.G, end = min(s.hi * kKeys, s.n);
+    const uint32_t o_addr = tmem + (static_cast<uint32_t>(row & 96) << 16) + kColO + x * 128;
+    // the row, as the row warps have it
+    const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G, tok = s.t0 + (s.both ? 0 : x * TS) + t;
+    const int last = t < TS && g < G && tok < s.t1 ? s.n - s.q + tok : -1, first = p.a.window > 0 ? max(minus(last, p.a.window - 1), 0) : 0;
+    const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? minus(s.n - s.q + s.t1, p.a.window) : 0;   // keys that every row sees
+    const bf16 *q = p.q + (s.row0 + tok) * p.a.q_st + (long long)(s.head * G + g) * p.a.q_sh;
     const int *table = p.a.c.table + (long long)max(s.slot, 0) * p.a.c.width;
     auto at = [&](int j) {
         return valid_page(p.a.c, __ldg(table + (j >> p.a.c.shift))) * p.a.c.s_page + s.head * p.a.c.s_h + (long long)(j & (p.a.c.P - 1)) * p.a.c.s_t;
@@ -654,9 +662,9 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             const Seg &s = meta->seg[k % kSegs];
             const int tok = s.t0 + (s.both ? 0 : x * TS) + t;
             const bool valid = t < TS && g < G && tok < s.t1;
-            const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 && last >= p.a.window ? last - p.a.window + 1 : 0;   // keys seen
+            const int last = valid ? s.n - s.q + tok : -1, first = p.a.window > 0 ? max(minus(last, p.a.window - 1), 0) : 0;   // keys seen
             // keys that not every row of the unit sees lie outside [all_lo, all_hi]
-            const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? max(s.n - s.q + s.t1, 0) - p.a.window : 0;
+            const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? minus(s.n - s.q + s.t1, p.a.window) : 0;
             if (s.own[x] > 0) {
                 const int lx = s.lo_x[x], hx = s.hi_x[x], step = s.both ? 2 : 1;
                 int j = s.begin_x[x];
@@ -802,10 +810,11 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
                 if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
-                if (__any_sync(0xffffffffu, *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1)) {   // (O is complete, and the next segment's first PV waits for the epilogue, which waits for this warp)
+                if (__any_sync(0xffffffffu, *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1)) {
+                    // O is complete, and stays: the next segment's first PV waits for the epilogue, which waits for this warp
                     if (!(ok = ptx::mbar_wait_warp(bar_o_full + 8 * x, ns & 1u, abort_flag))) break;
                     ptx::tc_fence_after();
-                    add_not_finite<D>(p, s, x, p.q + (s.row0 + tok) * p.a.q_st + (long long)(s.head * G + g) * p.a.q_sh, first, last, all_lo, all_hi, o_addr);
+                    add_not_finite<D>(p, s, x, tmem);
                 }
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
