@@ -145,7 +145,8 @@ const char *sla_status_string(sla_status_t status); /* static string, never NULL
 const char *sla_last_error(sla_handle_t handle);    /* text of the last failure on this handle     */
 
 /* Waits for `stream` and reads the device status word: SLA_OK, SLA_ERR_DEVICE_OVERRUN,
- * SLA_ERR_DEVICE_TIMEOUT, SLA_ERR_DEVICE_INDEX or SLA_ERR_CACHE_FULL; the word is cleared. */
+ * SLA_ERR_DEVICE_TIMEOUT, SLA_ERR_DEVICE_INDEX or SLA_ERR_CACHE_FULL, the first of these that applies; the word is
+ * cleared.  A refusal of pages beside another error is not lost: the next call reports it. */
 sla_status_t sla_poll_status(sla_handle_t handle, void *stream);
 
 /* Number of kernels this handle has launched since sla_create (a diagnostic for benchmarks; the

@@ -22,6 +22,7 @@ struct sla_handle_s {
     sla::TcLast tc_last;      // tile table of the most recent tensor-core attention chunk
     bool canaries = false;    // sla_set_debug_canaries
     bool paged_expiry = false;   // sla_selftest_paged_expiry
+    int pending = 0;          // a refusal of pages that sla_poll_status has read beside another error and not reported yet
     sla::Canaries last_canaries;   // of the most recent call that laid any, and where its scratch began
     char *last_canary_base = nullptr;
     // stride-offset and span-length tables for exponents other than 1/2 (host copies; the device
@@ -440,6 +441,8 @@ sla_status_t sla_poll_status(sla_handle_t h, void *stream) {
     if (e == cudaSuccess) e = cudaMemsetAsync(h->ws, 0, sizeof word, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_poll_status");
+    word |= h->pending;
+    h->pending = word != sla::kStatusCacheFull ? word & sla::kStatusCacheFull : 0;
     if (word & sla::kStatusOverrun) return fail(h, SLA_ERR_DEVICE_OVERRUN, "a kernel wrote outside its scratch region%s");
     if (word & sla::kStatusTimeout) return fail(h, SLA_ERR_DEVICE_TIMEOUT, "a bounded device-side wait expired%s");
     if (word & sla::kStatusBadIndex) return fail(h, SLA_ERR_DEVICE_INDEX, "an anchor outside [0, i], or a slot, length or page outside a paged cache, was skipped%s");

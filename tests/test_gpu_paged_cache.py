@@ -330,3 +330,18 @@ def test_span_step_of_more_sequences_than_one_launch_takes(sla, mode, n_seqs, hk
             a, b = part[1], lse[x:x + 20]
             assert torch.equal(torch.isfinite(a), torch.isfinite(b)) and ((a - b).abs().nan_to_num() <= 4e-6 * (1 + a.abs().nan_to_num(posinf=0, neginf=0))).all()
     h.close()
+
+
+def test_a_refusal_beside_another_error_is_reported_too(sla):
+    h = sla.Handle(0, 1 << 26)
+    c = Pair(sla, h, n_pages=2, width=4)
+    for _ in range(2):
+        first = sla.sla_cache_extend(h, c.cache, U.device_ints([0, 40, 41]), seq=U.device_ints([0, 9]))   # three pages; no such slot
+        assert list(first.cpu()) == [-1, -1]
+        assert [sla.sla_poll_status(h) for _ in range(3)] == [sla.SLA_ERR_DEVICE_INDEX, sla.SLA_ERR_CACHE_FULL, sla.SLA_OK]
+    # one refused while the other waits to be reported: once more, not twice
+    sla.sla_cache_extend(h, c.cache, U.device_ints([0, 40, 41]), seq=U.device_ints([0, 9]))
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    sla.sla_cache_extend(h, c.cache, U.device_ints([0, 40]), seq=U.device_ints([0]))
+    assert [sla.sla_poll_status(h) for _ in range(2)] == [sla.SLA_ERR_CACHE_FULL, sla.SLA_OK]
+    h.close()
