@@ -45,7 +45,7 @@ def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8,
         cu = ints([0] + torch.tensor(new).cumsum(0).tolist())
         first = c.extend(cu, seq=ints(seq))
         c.append(cu, first, rand(sum(new), kv_heads, head_dim), rand(sum(new), kv_heads, head_dim), seq=ints(seq))
-        c.attend(rand(sum(new), q_heads, head_dim), cu, seq=ints(seq), max_new=max(new))
+        c.attend(rand(sum(new), q_heads, head_dim), cu, seq=ints(seq), max_new=max(new), first=first)
         for s, n in zip(seq, new):
             done[s] += n
         tokens += sum(new)
@@ -69,9 +69,9 @@ def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8,
             c.append(None, first, rand(len(group), kv_heads, head_dim), rand(len(group), kv_heads, head_dim), seq=seq)
             q = rand(len(group), q_heads, head_dim)
             if spans:
-                c.step(rand(len(group), q_heads, head_dim), q, seq=seq, max_tokens=most)
+                c.step(rand(len(group), q_heads, head_dim), q, seq=seq, max_tokens=most, first=first)
             else:
-                out, _ = c.attend(q, seq=seq)
+                out, _ = c.attend(q, seq=seq, first=first)
                 last = (group, q, out)
             for s in group:
                 live[s] += 1

@@ -407,6 +407,11 @@ typedef struct {
     int32_t reserved;         /* must be 0                                                           */
     const int32_t *seq;       /* device [n_seqs]: slots, all different; NULL = 0 .. n_seqs-1         */
     const int32_t *cu_new;    /* device [n_seqs + 1], ascending from 0; NULL = one token a sequence   */
+    const int32_t *first;     /* device [n_seqs], out of sla_cache_extend, or NULL.  sla_paged_attention and
+                               * sla_paged_decode_step take a sequence whose entry is negative as one without
+                               * tokens: extend has refused it, and the tokens it has are not the call's
+                               * (with NULL its rows are attended as the last ones it has).  The other calls
+                               * do not read it                                                      */
 } sla_batch_t;
 
 /* Workspace bytes that every call below needs at most, for batches of up to n_seqs sequences and n_new

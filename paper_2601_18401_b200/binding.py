@@ -63,7 +63,7 @@ class sla_cache_t(C.Structure):
 
 class sla_batch_t(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("n_new", C.c_int32), ("max_new", C.c_int32), ("reserved", C.c_int32),
-                ("seq", C.c_void_p), ("cu_new", C.c_void_p)]
+                ("seq", C.c_void_p), ("cu_new", C.c_void_p), ("first", C.c_void_p)]
 
 
 class sla_params_t(C.Structure):
@@ -549,13 +549,17 @@ def _seq(seq: Optional[torch.Tensor], n: int) -> Optional[int]:
     return seq.data_ptr()
 
 
-def _batch(cu_new: Optional[torch.Tensor], n_new: int, max_new: Optional[int], seq: Optional[torch.Tensor]) -> sla_batch_t:
+def _batch(cu_new: Optional[torch.Tensor], n_new: int, max_new: Optional[int], seq: Optional[torch.Tensor],
+           first: Optional[torch.Tensor] = None) -> sla_batch_t:
     if cu_new is None:
         n, max_new = n_new, 1
     else:
         n = _int32(cu_new, "cu_new").numel() - 1
         max_new = n_new if max_new is None else int(max_new)
-    return sla_batch_t(n, n_new, max_new, 0, _seq(seq, n), None if cu_new is None else cu_new.data_ptr())
+    if first is not None and _int32(first, "first").numel() != n:
+        raise ValueError("first must have one entry per sequence")
+    return sla_batch_t(n, n_new, max_new, 0, _seq(seq, n), None if cu_new is None else cu_new.data_ptr(),
+                       None if first is None else first.data_ptr())
 
 
 def _slots(cache: sla_cache_t, cu_new: Optional[torch.Tensor], seq: Optional[torch.Tensor]) -> int:
@@ -642,9 +646,10 @@ def sla_cache_copy(handle: Handle, cache: sla_cache_t, pairs: torch.Tensor, *, s
 
 def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_new: Optional[torch.Tensor] = None, *,
                         seq: Optional[torch.Tensor] = None, max_new: Optional[int] = None, window: int = 0,
-                        softmax_scale: Optional[float] = None, out=None, lse=None, stream=None):
+                        softmax_scale: Optional[float] = None, first: Optional[torch.Tensor] = None, out=None, lse=None, stream=None):
     """q [n_new, Hq, D], the new tokens of the sequences (cu_new None: one each) -> out (q's dtype and strides), lse fp32
-    [n_new, Hq].  max_new: the longest chunk (default n_new); it decides the tiles."""
+    [n_new, Hq].  max_new: the longest chunk (default n_new); it decides the tiles.  first: what sla_cache_extend returned; the
+    rows of a sequence that it refused are then 0 and -inf (without it, those of the tokens the sequence has)."""
     (T, Hq, D), strides, dtype = q.shape, q.stride(), q.dtype
     if strides[-1] != 1 or D != cache.head_dim or _dtype_code(q) != cache.dtype:
         raise ValueError("q must be [n_new, Hq, D] in the cache's dtype and head_dim, head_dim contiguous")
@@ -652,9 +657,9 @@ def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_
         out = torch.empty_strided(q.shape, strides, dtype=dtype, device=q.device)
     elif out.stride() != strides or out.shape != q.shape or out.dtype is not dtype:
         raise ValueError("out must have q's shape, strides and dtype")
-    _on_gpu(cache.tensors[0], q, out, cu_new, seq)
+    _on_gpu(cache.tensors[0], q, out, cu_new, seq, first)
     lse = _output(lse, (T, Hq), q.device)
-    b = _batch(cu_new, T, max_new, seq)
+    b = _batch(cu_new, T, max_new, seq, first)
     rc = handle._lib.sla_paged_attention(handle.ptr, q.data_ptr(), cache.address, C.addressof(b), Hq, strides[0], strides[1],
                                          int(window), 1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale,
                                          out.data_ptr(), lse.data_ptr(), _stream_ptr(stream))
@@ -664,10 +669,11 @@ def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_
 
 
 def sla_paged_decode_step(handle: Handle, q_s: torch.Tensor, q: torch.Tensor, cache: sla_cache_t, params: sla_params_t, *,
-                          seq: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None, out=None, lse=None,
-                          out_anchor=None, out_score=None, stream=None):
+                          seq: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None,
+                          first: Optional[torch.Tensor] = None, out=None, lse=None, out_anchor=None, out_score=None, stream=None):
     """sla_decode_step over the paged cache: q_s, q [n_seqs, Hq, D], the last token of every sequence -> out, lse, anchors
-    (positions), scores.  max_tokens: a bound of the lengths (default: what the table can hold); it sizes the grids."""
+    (positions), scores.  max_tokens: a bound of the lengths (default: what the table can hold); it sizes the grids.  first: as
+    for sla_paged_attention."""
     B, Hq, D = q.shape
     if q_s.stride() != q.stride() or q.stride(-1) != 1 or q_s.shape != q.shape:
         raise ValueError("q_s and q must share shape and strides, head_dim contiguous")
@@ -678,11 +684,11 @@ def sla_paged_decode_step(handle: Handle, q_s: torch.Tensor, q: torch.Tensor, ca
         out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)
     elif out.stride() != q.stride() or out.shape != q.shape or out.dtype is not q.dtype:
         raise ValueError("out must have q's shape, strides and dtype")
-    _on_gpu(cache.tensors[0], q_s, q, out, seq)
+    _on_gpu(cache.tensors[0], q_s, q, out, seq, first)
     lse = _output(lse, (B, Hq), dev)
     out_anchor = _output(out_anchor, (B, Hq, params.top_k), dev, torch.int32)
     out_score = _output(out_score, (B, Hq, params.top_k), dev)
-    b = _batch(None, B, 1, seq)
+    b = _batch(None, B, 1, seq, first)
     most = cache.table_width * cache.page_tokens if max_tokens is None else int(max_tokens)
     rc = handle._lib.sla_paged_decode_step(handle.ptr, q_s.data_ptr(), q.data_ptr(), cache.address, C.addressof(b), most, Hq,
                                            q.stride(0), q.stride(1), C.byref(params), out.data_ptr(), lse.data_ptr(),

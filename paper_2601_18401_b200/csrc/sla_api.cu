@@ -850,7 +850,7 @@ sla::Pages make_pages(sla_handle_t h, const sla_cache_t *c) {
     return p;
 }
 
-sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, b->seq, b->cu_new}; }
+sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, b->seq, b->cu_new, 0, b->first}; }
 
 // Rows that a sequence can have at most, given a bound that may be loose.
 int32_t longest_chunk(int32_t n_new, int32_t max_new) { return max_new > n_new ? n_new : max_new > 0 ? max_new : 1; }
@@ -1036,7 +1036,7 @@ sla_status_t sla_paged_decode_step(sla_handle_t h, const void *q_s, const void *
     cudaError_t e = sla::launch_canary_fill(h->ws + kHeaderBytes, plan.canaries, st);
     for (int x = 0; x < b->n_seqs && e == cudaSuccess; x += per) {
         call.B = b->n_seqs - x < per ? b->n_seqs - x : per;   // (fewer than the plan has room for in the last launch)
-        const sla::Batch batch = {call.B, call.B, 1, b->seq ? b->seq + x : nullptr, nullptr, x};
+        const sla::Batch batch = {call.B, call.B, 1, b->seq ? b->seq + x : nullptr, nullptr, x, b->first ? b->first + x : nullptr};
         const size_t at = (size_t)x * q_stride_b * elem_size(c->dtype), row = (size_t)x * n_q_heads;
         e = sla::launch_paged_decode(static_cast<const char *>(q_s) + at, static_cast<const char *>(q) + at, make_pages(h, c), batch, call,
                                      c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset),

@@ -52,12 +52,12 @@ struct PagedCache {
     static constexpr bool kPaged = true;
     Pages pages;
     Batch batch;
-    // query position of sequence x, -1 when it has no tokens (or a slot or length out of bounds, which is flagged)
+    // query position of sequence x, -1 when it has no tokens or was refused its last one (or a slot or length out of bounds, which is flagged)
     __device__ __forceinline__ long long position(int x, long long most, const int *&row) const {
         const int s = slot_of(pages, batch, x);
         row = pages.table + (long long)max(s, 0) * pages.width;
         if (s >= 0) {
-            const int n = tokens_of(pages, s);
+            const int n = tokens_of(pages, batch, x, s);
             if (n <= most) return n - 1;
         }
         atomicOr(pages.status, kStatusBadIndex);

@@ -21,6 +21,7 @@ struct Batch {
     int n_seqs, n_new, max_new;
     const int *seq, *cu;            // either may be NULL (slots slot0 .. slot0 + n_seqs - 1; one token a sequence)
     int slot0 = 0;
+    const int *first = nullptr;     // of cache_extend: a sequence whose entry is negative was refused; may be NULL
 };
 
 // Rows [lo, hi) of sequence x in the call's tensors, kept inside them whatever cu_new holds.
@@ -41,6 +42,12 @@ __device__ __forceinline__ int tokens_of(const Pages &p, int slot) {
         return n < 0 ? 0 : most;
     }
     return n;
+}
+// Tokens of sequence x in its slot, for the calls that attend to them: none of one that was refused.
+__device__ __forceinline__ int tokens_of(const Pages &p, const Batch &b, int x, int slot) {
+    const bool refused = b.first && b.first[x] < 0;
+    const int n = tokens_of(p, slot);
+    return refused ? 0 : n;
 }
 // A page number from the table: one outside the pool is flagged and read as page 0, so that no address leaves it.
 __device__ __forceinline__ int valid_page(const Pages &p, int page) {
@@ -152,7 +159,7 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
             s.z = r1 - s.w;
             s.x = slot_of(a.c, a.b, x);
             if (s.x < 0) atomicOr(a.c.status, kStatusBadIndex);
-            else s.y = tokens_of(a.c, s.x);
+            else s.y = tokens_of(a.c, a.b, x, s.x);
         }
         return s;
     };

@@ -47,14 +47,14 @@ class PagedCache:
     def append(self, cu_new, first, k_new, v_new, *, seq=None):
         B.sla_cache_append(self.handle, self.cache, cu_new, first, k_new, v_new, seq=seq)
 
-    def attend(self, q, cu_new=None, *, seq=None, max_new=None, window=0, softmax_scale=None):
-        """Dense causal attention of the new tokens -> out, lse."""
+    def attend(self, q, cu_new=None, *, seq=None, max_new=None, window=0, softmax_scale=None, first=None):
+        """Dense causal attention of the new tokens -> out, lse.  first: of `extend`; refused sequences then give 0 and -inf."""
         return B.sla_paged_attention(self.handle, q, self.cache, cu_new, seq=seq, max_new=max_new, window=window,
-                                     softmax_scale=softmax_scale)
+                                     softmax_scale=softmax_scale, first=first)
 
-    def step(self, q_s, q, *, seq=None, max_tokens=None):
-        """The span decode step of each sequence's last token -> out, lse, anchors, scores."""
-        return B.sla_paged_decode_step(self.handle, q_s, q, self.cache, self.params, seq=seq, max_tokens=max_tokens)
+    def step(self, q_s, q, *, seq=None, max_tokens=None, first=None):
+        """The span decode step of each sequence's last token -> out, lse, anchors, scores.  first: as for `attend`."""
+        return B.sla_paged_decode_step(self.handle, q_s, q, self.cache, self.params, seq=seq, max_tokens=max_tokens, first=first)
 
     def fork(self, src, dst):
         return B.sla_cache_fork(self.handle, self.cache, src, dst)

@@ -345,3 +345,42 @@ def test_a_refusal_beside_another_error_is_reported_too(sla):
     sla.sla_cache_extend(h, c.cache, U.device_ints([0, 40]), seq=U.device_ints([0]))
     assert [sla.sla_poll_status(h) for _ in range(2)] == [sla.SLA_ERR_CACHE_FULL, sla.SLA_OK]
     h.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [3, 2, 1, 4], [90, 40, 17, 33]])
+def test_a_refused_sequence_is_not_attended(sla, dtype, new):
+    """With what extend returned: the rows of a refused sequence are 0 and -inf, the others as in a call without it."""
+    from paper_2601_18401_b200.paged import PagedCache
+    c = PagedCache(12, 6, 16 * 8, n_q_heads=8, n_kv_heads=2, page_tokens=16, dtype=dtype, max_new=400, params=sla.make_params(4, 0))
+    g = torch.Generator(device="cuda:0")
+    rand = lambda n, h: torch.empty(n, h, 128, dtype=dtype, device="cuda:0").normal_(generator=g)  # noqa: E731
+    start, slots = [16, 32, 15, 16], [4, 0, 2, 5]
+    cu = U.device_ints(np.concatenate([[0], np.cumsum(start)]))
+    c.append(cu, c.extend(cu, seq=U.device_ints(slots)), rand(sum(start), 2), rand(sum(start), 2), seq=U.device_ints(slots))
+    c.ref[5:] = 1                                            # two free pages are left
+    c.ref[6:8] = 0
+    if new[0] == 1:
+        c.ref[7] = 1                                         # or one
+    cu = U.device_ints(np.concatenate([[0], np.cumsum(new)]))
+    first = c.extend(cu, seq=U.device_ints(slots))
+    ok = [f >= 0 for f in first.tolist()]
+    assert c.poll() == sla.SLA_ERR_CACHE_FULL and 0 < sum(ok) + (new[0] == 90) and not all(ok)
+    kn, vn, q, q_s = rand(sum(new), 2), rand(sum(new), 2), rand(sum(new), 8), rand(sum(new), 8)
+    c.append(cu, first, kn, vn, seq=U.device_ints(slots))
+    n = [int(x) for x in c.n_tokens[torch.tensor(slots).cuda()]]
+    seen = [x if o else 0 for x, o in zip(n, ok)]
+    table = c.table.cpu().numpy()[slots]
+    for bound in (max(new), sum(new)):
+        out, lse = c.attend(q, cu, seq=U.device_ints(slots), max_new=bound, first=first)
+        U.check_attention(out, lse, U.attention_reference(q, c.k, c.v, table, seen, new, 4, 0, 128 ** -0.5, 16), dtype)
+    out, lse, anchor, score = c.step(q_s[:4], q[:4], seq=U.device_ints(slots), max_tokens=128, first=first)
+    whole = c.step(q_s[:4], q[:4], seq=U.device_ints(slots), max_tokens=128)
+    for x in range(4):
+        if ok[x]:
+            assert all(torch.equal(a[x], b[x]) for a, b in zip((out, lse, anchor, score), whole))
+        else:
+            assert (out[x] == 0).all() and (lse[x] == -math.inf).all() and (anchor[x] == -1).all() and (score[x] == -math.inf).all()
+    assert c.poll() == sla.SLA_OK
+    with pytest.raises(ValueError):
+        c.attend(q, cu, seq=U.device_ints(slots), first=first[:3])
