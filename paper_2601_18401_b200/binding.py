@@ -216,8 +216,11 @@ def make_layout(q: torch.Tensor, k: torch.Tensor, decode: bool = False) -> sla_l
 
 def _stream_ptr(stream) -> int:
     if stream is None:
-        # the raw handle of torch.cuda.current_stream(), without the object around it (0.3 us a call instead of 3.3)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        try:
+            # the raw handle of torch.cuda.current_stream(), without the object around it (0.3 us a call instead of 3.3)
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:   # (private names: a torch without them has the public one)
+            stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
 
 

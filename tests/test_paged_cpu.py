@@ -177,3 +177,16 @@ def test_every_call_wants_a_slot_per_sequence(sla):
                  lambda s: sla.sla_paged_attention(None, q, c, cu, seq=s), lambda s: sla.sla_paged_decode_step(None, q, q, c, sla.make_params(4, 0), seq=s)):
         with pytest.raises(ValueError):
             call(torch.arange(2, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("missing", ["_cuda_getCurrentRawStream", "_cuda_getDevice"])
+def test_the_current_stream_without_torchs_private_names(monkeypatch, missing):
+    from types import SimpleNamespace
+
+    from paper_2601_18401_b200 import binding as B
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: SimpleNamespace(cuda_stream=4711))
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.setattr(torch._C, name, lambda *a: 0, raising=False)
+    monkeypatch.delattr(torch._C, missing)
+    assert B._stream_ptr(None) == 4711
+    assert B._stream_ptr(SimpleNamespace(cuda_stream=12)) == 12
