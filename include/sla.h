@@ -170,11 +170,12 @@ sla_status_t sla_kernel_time_ms(sla_handle_t handle, float *ms, int32_t *n_launc
 sla_status_t sla_attention_tile_stats(sla_handle_t handle, int64_t *out4_host, void *stream);
 
 /* Debug canaries (the paper has no counterpart; they stand in for a memory checker).  When enabled,
- * sla_span_attention, sla_span_attention_gated and sla_decode_step separate the regions of their scratch
- * memory by 256-byte gaps, fill the gaps with a pattern before their kernels run and check them
- * afterwards; a damaged gap shows as SLA_ERR_DEVICE_OVERRUN at the next sla_poll_status.  Costs two
- * small launches per call (per chunk of a chunked call); off by default.
- * sla_selftest_canary_trip damages one gap of the most recent sla_decode_step of this handle itself (a
+ * sla_span_attention, sla_span_attention_gated, sla_decode_step and those calls on a paged cache that use scratch
+ * memory (extend, fork, compact, attention, the decode step) separate the regions of that memory by
+ * 256-byte gaps, fill the gaps with a pattern before their kernels run and check them afterwards; a damaged
+ * gap shows as SLA_ERR_DEVICE_OVERRUN at the next sla_poll_status.  Costs two small launches per call (per
+ * chunk of a chunked call); off by default.
+ * sla_selftest_canary_trip damages one gap of the most recent sla_decode_step or paged call of this handle itself (a
  * 4-byte memset, nothing out of bounds) and runs the check again, to show that the check reports. */
 sla_status_t sla_set_debug_canaries(sla_handle_t handle, int enable);
 sla_status_t sla_selftest_canary_trip(sla_handle_t handle, void *stream);

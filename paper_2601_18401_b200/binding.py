@@ -24,6 +24,7 @@ SLA_ERR_UNSUPPORTED = -2
 SLA_ERR_WORKSPACE = -3
 SLA_ERR_DEVICE_TIMEOUT = -5
 SLA_ERR_DEVICE_INDEX = -6
+SLA_ERR_DEVICE_OVERRUN = -7
 SLA_ERR_CACHE_FULL = -8
 
 EXPORTS = [

@@ -208,6 +208,16 @@ const char *check_prefill_range(int64_t Lq, int64_t q_pos0, int64_t Lkv) {
 
 size_t elem_size(int dtype) { return dtype == SLA_F32 ? 4 : 2; }
 
+// Launches a call that uses scratch memory between the fill of its canaries and their check.
+template <class F>
+cudaError_t with_canaries(sla_handle_t h, const sla::Canaries &cn, cudaStream_t st, F launch) {
+    cudaError_t e = sla::launch_canary_fill(h->ws + kHeaderBytes, cn, st);
+    if (e == cudaSuccess) e = launch();
+    if (e == cudaSuccess) e = sla::launch_canary_check(h->ws + kHeaderBytes, cn, reinterpret_cast<int *>(h->ws), st);
+    if (e == cudaSuccess && cn.n) { h->last_canaries = cn; h->last_canary_base = h->ws + kHeaderBytes; }
+    return e;
+}
+
 }  // namespace
 
 namespace sla {
@@ -318,7 +328,7 @@ sla_status_t sla_set_debug_canaries(sla_handle_t h, int enable) {
 sla_status_t sla_selftest_canary_trip(sla_handle_t h, void *stream) {
     if (!h) return SLA_ERR_INVALID_ARG;
     if (!h->last_canary_base || h->last_canaries.n == 0)
-        return fail(h, SLA_ERR_INVALID_ARG, "no decode step with canaries has run on this handle%s");
+        return fail(h, SLA_ERR_INVALID_ARG, "no decode step or paged call with canaries has run on this handle%s");
     if (const char *why = check_device(h)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // what an overrun of the first scratch region by one word would leave behind
@@ -855,12 +865,16 @@ sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->ma
 // Rows that a sequence can have at most, given a bound that may be loose.
 int32_t longest_chunk(int32_t n_new, int32_t max_new) { return max_new > n_new ? n_new : max_new > 0 ? max_new : 1; }
 
+sla::CacheScratch cache_scratch(sla_handle_t h, const sla_cache_t *c, size_t n_seqs) {
+    return sla::plan_cache(make_pages(h, c), (int)n_seqs, h->canaries ? sla::Canaries::kBytes : 0);
+}
+
 // The handle, the cache and the scratch a bookkeeping call needs.  SLA_OK when the call may go on.
 sla_status_t cache_call(sla_handle_t h, const sla_cache_t *c, size_t n_seqs) {
     if (!h) return SLA_ERR_INVALID_ARG;
     if (const char *why = check_cache(c)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
     if (const char *why = check_device(h)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
-    if (sla::cache_scratch_bytes(make_pages(h, c), (int)n_seqs) > h->scratch_avail)
+    if (cache_scratch(h, c, n_seqs).bytes > h->scratch_avail)
         return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this cache: ask sla_paged_workspace_bytes%s");
     return SLA_OK;
 }
@@ -875,7 +889,7 @@ sla_layout_t layout_of(const sla_cache_t *c, int32_t n_q_heads, int32_t n_seqs, 
 size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_t n_seqs, int32_t n_new, const sla_params_t *p) {
     if (check_cache(c) || n_q_heads <= 0 || n_q_heads % c->n_kv_heads || n_q_heads / c->n_kv_heads > sla::kMaxGroup || n_seqs < 0 || n_new < 0)
         return 0;
-    size_t need = sla::cache_scratch_bytes(make_pages(nullptr, c), n_seqs > c->n_slots ? n_seqs : c->n_slots);
+    size_t need = sla::plan_cache(make_pages(nullptr, c), n_seqs > c->n_slots ? n_seqs : c->n_slots).bytes;
     sla::PagedCall a = {};
     a.c = make_pages(nullptr, c);
     a.Hq = n_q_heads;
@@ -905,7 +919,9 @@ sla_status_t sla_cache_extend(sla_handle_t h, const sla_cache_t *c, const sla_ba
     if (sla_status_t s = cache_call(h, c, b->n_seqs)) return s;
     if (b->n_seqs == 0) return SLA_OK;
     if (!first) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
-    cudaError_t e = sla::launch_cache_extend(make_pages(h, c), make_batch(b), first, reinterpret_cast<int *>(h->ws + kHeaderBytes), static_cast<cudaStream_t>(stream));
+    const sla::CacheScratch s = cache_scratch(h, c, b->n_seqs);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = with_canaries(h, s.canaries, st, [&] { return sla::launch_cache_extend(make_pages(h, c), make_batch(b), first, s, h->ws + kHeaderBytes, st); });
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_extend");
     h->launches += 1;
     return SLA_OK;
@@ -944,7 +960,9 @@ sla_status_t sla_cache_fork(sla_handle_t h, const sla_cache_t *c, const int32_t 
     if (n < 0 || (n > 0 && (!src || !dst || !pairs))) return fail(h, SLA_ERR_INVALID_ARG, "n must be >= 0 and src, dst and pairs not NULL%s");
     if (sla_status_t s = cache_call(h, c, n)) return s;
     if (n == 0) return SLA_OK;
-    cudaError_t e = sla::launch_cache_fork(make_pages(h, c), src, dst, n, pairs, reinterpret_cast<int *>(h->ws + kHeaderBytes), static_cast<cudaStream_t>(stream));
+    const sla::CacheScratch s = cache_scratch(h, c, n);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = with_canaries(h, s.canaries, st, [&] { return sla::launch_cache_fork(make_pages(h, c), src, dst, n, pairs, s, h->ws + kHeaderBytes, st); });
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_fork");
     h->launches += 2;
     return SLA_OK;
@@ -953,7 +971,9 @@ sla_status_t sla_cache_fork(sla_handle_t h, const sla_cache_t *c, const int32_t 
 sla_status_t sla_cache_compact(sla_handle_t h, const sla_cache_t *c, int32_t *pairs, void *stream) {
     if (sla_status_t s = cache_call(h, c, 0)) return s;
     if (!pairs) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
-    cudaError_t e = sla::launch_cache_compact(make_pages(h, c), pairs, reinterpret_cast<int *>(h->ws + kHeaderBytes), h->sm_count, static_cast<cudaStream_t>(stream));
+    const sla::CacheScratch s = cache_scratch(h, c, 0);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = with_canaries(h, s.canaries, st, [&] { return sla::launch_cache_compact(make_pages(h, c), pairs, s, h->ws + kHeaderBytes, h->sm_count, st); });
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_compact");
     h->launches += 3;
     return SLA_OK;
@@ -998,9 +1018,12 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     a.q_sh = q_stride_h;
     a.scale = softmax_scale;
     a.expire = h->paged_expiry;
-    const sla::PagedPlan plan = sla::plan_paged(a, c->dtype, h->sm_count);
+    const sla::PagedPlan plan = sla::plan_paged(a, c->dtype, h->sm_count, h->canaries ? sla::Canaries::kBytes : 0);
     if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
-    cudaError_t e = sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, static_cast<cudaStream_t>(stream), &h->launches);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = with_canaries(h, plan.canaries, st, [&] {
+        return sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, st, &h->launches);
+    });
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_paged_attention");
     return SLA_OK;
 }

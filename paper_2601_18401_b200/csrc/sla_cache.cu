@@ -65,12 +65,12 @@ __device__ inline int find_free(const int *ref, int n_pages, int want, int *free
 
 __device__ __forceinline__ int pages_for(const Pages &p, long long tokens) { return (int)((tokens + p.P - 1) >> p.shift); }
 
-// scratch: free_list[n_pages], need[n_seqs] (inclusive prefix sums of the pages wanted)
-__global__ void __launch_bounds__(kPlanThreads) cache_extend(Pages p, Batch b, int *__restrict__ first, int *__restrict__ scratch) {
+// free_list [n_pages], upto [n_seqs]: inclusive prefix sums of the pages wanted
+__global__ void __launch_bounds__(kPlanThreads) cache_extend(Pages p, Batch b, int *__restrict__ first, int *__restrict__ free_list,
+                                                             int *__restrict__ upto) {
     __shared__ int s_warp[32];
     chain_wait();
     chain_release();
-    int *free_list = scratch, *upto = scratch + p.n_pages;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int sum = 0;
     for (int x0 = 0; x0 < b.n_seqs; x0 += kPlanThreads) {
@@ -274,13 +274,12 @@ __global__ void __launch_bounds__(kCopyThreads) cache_copy(Pages p, PageShape f,
 }
 
 // ---- fork -------------------------------------------------------------------------------------------
-// scratch: free_list[n_pages], upto[n], full[n] (pages to share; 0 for a refused pair)
+// free_list [n_pages], upto [n], full [n]: pages to share, 0 for a refused pair
 __global__ void __launch_bounds__(kPlanThreads) fork_plan(Pages p, const int *__restrict__ src, const int *__restrict__ dst, int n,
-                                                          int *__restrict__ pairs, int *__restrict__ scratch) {
+                                                          int *__restrict__ pairs, int *__restrict__ free_list, int *__restrict__ upto, int *__restrict__ full) {
     __shared__ int s_warp[32];
     chain_wait();
     chain_release();
-    int *free_list = scratch, *upto = scratch + p.n_pages, *full = upto + n;
     int sum = 0;
     for (int x0 = 0; x0 < n; x0 += kPlanThreads) {
         const int x = x0 + threadIdx.x;
@@ -349,9 +348,8 @@ __global__ void __launch_bounds__(kCopyThreads) fork_share(Pages p, PageShape f,
 }
 
 // ---- compact ----------------------------------------------------------------------------------------
-// The pool in at most 1024 chunks of a multiple of 4096 pages.  scratch: count[1024], n_moves, rank[n_pages] (of a mover among the
-// movers, -1 otherwise)
-constexpr int kMaxChunks = 1024;
+// The pool in at most 1024 chunks of a multiple of 4096 pages.  count [kMaxChunks], behind it the number of moves; rank [n_pages]: of a
+// mover among the movers, -1 otherwise
 __host__ __device__ inline int chunk_pages(int n_pages) {
     const long long quantum = 4ll * kPlanThreads;
     return (int)(quantum * ((n_pages + quantum * kMaxChunks - 1) / (quantum * kMaxChunks)));
@@ -375,12 +373,10 @@ __global__ void __launch_bounds__(kPlanThreads) compact_count(Pages p, int per, 
     if (threadIdx.x == 0) count[blockIdx.x] = total;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) compact_rank(Pages p, int per, int *__restrict__ scratch, int *__restrict__ pairs) {
+__global__ void __launch_bounds__(kPlanThreads) compact_rank(Pages p, int per, int *__restrict__ count, int *__restrict__ rank, int *__restrict__ pairs) {
     __shared__ int s_warp[32], s_before, s_below;
     chain_wait();
     chain_release();
-    const int *count = scratch;
-    int *n_moves_out = scratch + kMaxChunks, *rank = n_moves_out + 1;
     const int n_chunks = gridDim.x, c = threadIdx.x;
     // pages in use in all; before this chunk; in the whole chunks below page `live`
     const int mine = c < n_chunks ? count[c] : 0;
@@ -394,7 +390,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_rank(Pages p, int per, i
     __syncthreads();
     const int below = s_below + (edge < n_chunks ? count_live(p.ref, edge * per, live, s_warp) : 0);
     const int n_moves = live - below;   // pages in use at or above `live`: as many as are free below it
-    if (blockIdx.x == 0 && c == 0) *n_moves_out = n_moves;
+    if (blockIdx.x == 0 && c == 0) count[kMaxChunks] = n_moves;
     int upto = s_before;
     for (int p0 = blockIdx.x * per; p0 < min((int)(blockIdx.x + 1) * per, p.n_pages); p0 += 4 * kPlanThreads) {
         const int q0 = p0 + 4 * c;   // four pages a thread
@@ -419,12 +415,11 @@ __global__ void __launch_bounds__(kPlanThreads) compact_rank(Pages p, int per, i
     }
 }
 
-__global__ void __launch_bounds__(kCopyThreads) compact_move(Pages p, PageShape f, const int *__restrict__ scratch, const int *__restrict__ pairs,
-                                                             int table_ctas) {
+__global__ void __launch_bounds__(kCopyThreads) compact_move(Pages p, PageShape f, const int *__restrict__ count, const int *__restrict__ rank,
+                                                             const int *__restrict__ pairs, int table_ctas) {
     chain_wait();
     chain_release();
-    const int n_moves = scratch[kMaxChunks];
-    const int *rank = scratch + kMaxChunks + 1;
+    const int n_moves = count[kMaxChunks];
     if ((int)blockIdx.x < table_ctas) {
         if (n_moves == 0) return;
         const long long entries = (long long)p.n_slots * p.width;
@@ -456,12 +451,28 @@ int parts_of(const PageShape &f) { return (f.chunks + kCopyChunks - 1) / kCopyCh
 
 }  // namespace
 
-size_t cache_scratch_bytes(const Pages &p, int n_seqs) {
-    return ((size_t)p.n_pages + 2 * (size_t)(n_seqs > 0 ? n_seqs : 0) + kMaxChunks + 64) * sizeof(int);
+CacheScratch plan_cache(const Pages &p, int n_seqs, size_t gap) {
+    CacheScratch s;
+    size_t off = 0;
+    auto take = [&](size_t ints) {
+        if (gap) { s.canaries.add(off); off += gap; }
+        const size_t at = off;
+        off = (off + ints * sizeof(int) + 255) & ~(size_t)255;
+        return at;
+    };
+    const size_t n = n_seqs > 0 ? n_seqs : 0;
+    s.off_pages = take(p.n_pages);
+    s.off_seqs = take(n);
+    s.off_seqs2 = take(n);
+    s.off_chunks = take(kMaxChunks + 1);
+    if (gap) { s.canaries.add(off); off += gap; }
+    s.bytes = off;
+    return s;
 }
 
-cudaError_t launch_cache_extend(const Pages &p, const Batch &b, int *first, int *scratch, cudaStream_t st) {
-    return launch_chained(cache_extend, dim3(1), dim3(kPlanThreads), 0, st, p, b, first, scratch);
+cudaError_t launch_cache_extend(const Pages &p, const Batch &b, int *first, const CacheScratch &s, char *scratch, cudaStream_t st) {
+    return launch_chained(cache_extend, dim3(1), dim3(kPlanThreads), 0, st, p, b, first, reinterpret_cast<int *>(scratch + s.off_pages),
+                          reinterpret_cast<int *>(scratch + s.off_seqs));
 }
 
 cudaError_t launch_cache_append(const Pages &p, const Batch &b, const int *first, const void *k_new, const void *v_new,
@@ -485,26 +496,30 @@ cudaError_t launch_cache_copy(const Pages &p, const int *pairs, int n, cudaStrea
     return launch_chained(cache_copy, dim3(n, parts_of(f)), dim3(kCopyThreads), 0, st, p, f, pairs, n);
 }
 
-cudaError_t launch_cache_fork(const Pages &p, const int *src, const int *dst, int n, int *pairs, int *scratch, cudaStream_t st) {
+cudaError_t launch_cache_fork(const Pages &p, const int *src, const int *dst, int n, int *pairs, const CacheScratch &s, char *scratch, cudaStream_t st) {
     if (n == 0) return cudaSuccess;
     const PageShape f = page_shape(p);
-    cudaError_t e = launch_chained(fork_plan, dim3(1), dim3(kPlanThreads), 0, st, p, src, dst, n, pairs, scratch);
+    int *full = reinterpret_cast<int *>(scratch + s.off_seqs2);
+    cudaError_t e = launch_chained(fork_plan, dim3(1), dim3(kPlanThreads), 0, st, p, src, dst, n, pairs, reinterpret_cast<int *>(scratch + s.off_pages),
+                                   reinterpret_cast<int *>(scratch + s.off_seqs), full);
     const int share = p.width < 16 * kCopyThreads ? (p.width + kCopyThreads - 1) / kCopyThreads : 16;
     if (e == cudaSuccess)
         e = launch_chained(fork_share, dim3(n, share + parts_of(f)), dim3(kCopyThreads), 0, st, p, f, src, dst, n, (const int *)pairs,
-                           (const int *)(scratch + p.n_pages + n), share);
+                           (const int *)full, share);
     return e;
 }
 
-cudaError_t launch_cache_compact(const Pages &p, int *pairs, int *scratch, int sm_count, cudaStream_t st) {
+cudaError_t launch_cache_compact(const Pages &p, int *pairs, const CacheScratch &s, char *scratch, int sm_count, cudaStream_t st) {
     const PageShape f = page_shape(p);
+    int *count = reinterpret_cast<int *>(scratch + s.off_chunks), *rank = reinterpret_cast<int *>(scratch + s.off_pages);
     const int per = chunk_pages(p.n_pages), chunks = (p.n_pages + per - 1) / per;
-    cudaError_t e = launch_chained(compact_count, dim3(chunks), dim3(kPlanThreads), 0, st, p, per, scratch);
-    if (e == cudaSuccess) e = launch_chained(compact_rank, dim3(chunks), dim3(kPlanThreads), 0, st, p, per, scratch, pairs);
+    cudaError_t e = launch_chained(compact_count, dim3(chunks), dim3(kPlanThreads), 0, st, p, per, count);
+    if (e == cudaSuccess) e = launch_chained(compact_rank, dim3(chunks), dim3(kPlanThreads), 0, st, p, per, count, rank, pairs);
     const long long entries = (long long)p.n_slots * p.width;
     const int table_ctas = (int)(entries < 64ll * 4 * kCopyThreads ? (entries + 4 * kCopyThreads - 1) / (4 * kCopyThreads) : 64);
     if (e == cudaSuccess)
-        e = launch_chained(compact_move, dim3(table_ctas + sm_count * 8), dim3(kCopyThreads), 0, st, p, f, (const int *)scratch, (const int *)pairs, table_ctas);
+        e = launch_chained(compact_move, dim3(table_ctas + sm_count * 8), dim3(kCopyThreads), 0, st, p, f, (const int *)count, (const int *)rank,
+                           (const int *)pairs, table_ctas);
     return e;
 }
 

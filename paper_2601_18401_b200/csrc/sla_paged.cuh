@@ -2,6 +2,7 @@
 #pragma once
 
 #include "sla_common.cuh"
+#include "sla_kernels.h"
 
 namespace sla {
 
@@ -57,14 +58,20 @@ __device__ __forceinline__ int valid_page(const Pages &p, int page) {
 }
 
 // ---- launchers (sla_cache.cu)
-cudaError_t launch_cache_extend(const Pages &p, const Batch &b, int *first, int *scratch, cudaStream_t st);
+// Scratch of extend, fork and compact, in bytes from the scratch base: ints [n_pages], twice [n_seqs], [kMaxChunks + 1]
+constexpr int kMaxChunks = 1024;   // of a pool, to compact
+struct CacheScratch {
+    size_t off_pages, off_seqs, off_seqs2, off_chunks, bytes;
+    Canaries canaries;
+};
+CacheScratch plan_cache(const Pages &p, int n_seqs, size_t gap = 0);   // gap: bytes of canary between regions
+cudaError_t launch_cache_extend(const Pages &p, const Batch &b, int *first, const CacheScratch &s, char *scratch, cudaStream_t st);
 cudaError_t launch_cache_append(const Pages &p, const Batch &b, const int *first, const void *k_new, const void *v_new,
                                 long long s_t, long long s_h, int sm_count, cudaStream_t st);
 cudaError_t launch_cache_release(const Pages &p, const int *seq, int n, cudaStream_t st);
-cudaError_t launch_cache_fork(const Pages &p, const int *src, const int *dst, int n, int *pairs, int *scratch, cudaStream_t st);
-cudaError_t launch_cache_compact(const Pages &p, int *pairs, int *scratch, int sm_count, cudaStream_t st);
+cudaError_t launch_cache_fork(const Pages &p, const int *src, const int *dst, int n, int *pairs, const CacheScratch &s, char *scratch, cudaStream_t st);
+cudaError_t launch_cache_compact(const Pages &p, int *pairs, const CacheScratch &s, char *scratch, int sm_count, cudaStream_t st);
 cudaError_t launch_cache_copy(const Pages &p, const int *pairs, int n, cudaStream_t st);
-size_t cache_scratch_bytes(const Pages &p, int n_seqs);   // of extend, fork and compact
 
 // ---- attention over the cache ---------------------------------------------------------------------
 // One call of sla_paged_attention.

@@ -447,7 +447,7 @@ cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p
 }
 
 // Which kernel and with what tiles.
-PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
+PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap) {
     PagedPlan p;
     p.kind = PagedPlan::kRows;
     // 64 rows where no sequence has more, else 128: fp32, 2 sequences of 4000 to 9000 tokens, 12 to 16 new, 8/2 heads, D 64, 40 us against 53
@@ -471,6 +471,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.max_units = (int)units;
     size_t off = 0;
     auto take = [&](size_t bytes) {
+        if (gap) { p.canaries.add(off); off += gap; }
         const size_t at = off;
         off = (off + bytes + 255) & ~(size_t)255;
         return at;
@@ -485,6 +486,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count) {
     p.off_cut = take(ranges * sizeof(Cut));
     p.off_lse2 = take(2 * ranges * p.R * 4);
     p.off_o = take(2 * ranges * p.R * a.c.D * 4);
+    if (gap) { p.canaries.add(off); off += gap; }
     p.bytes = off;
     return p;
 }

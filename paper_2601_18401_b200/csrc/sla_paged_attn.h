@@ -1,6 +1,7 @@
 // Internal launcher declarations of the attention over a paged cache.
 #pragma once
 
+#include "sla_kernels.h"
 #include "sla_paged.cuh"
 
 namespace sla {
@@ -13,6 +14,7 @@ struct PagedPlan {
     int small;              // tokens of a unit whose tiles weigh half
     int n_ctas, max_groups, min_weight, max_units, max_ranges;
     size_t off_seq_at, off_unit_at, off_unit_end, off_ranges, off_seqs, off_starts, off_cut, off_lse2, off_o, bytes;
+    Canaries canaries;
 };
 
 inline Plan plan_at(const PagedPlan &p, char *scratch) {
@@ -25,7 +27,7 @@ inline Parts parts_at(const PagedPlan &p, char *scratch) {
             reinterpret_cast<Cut *>(scratch + p.off_cut)};
 }
 
-PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count);
+PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap = 0);   // gap: bytes of canary between regions
 cudaError_t launch_paged_plan(const PagedCall &a, const PagedPlan &p, char *scratch, cudaStream_t st);
 cudaError_t launch_paged_merge(const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st);
 // counters: p.n_ctas ints, zero on entry and again on exit

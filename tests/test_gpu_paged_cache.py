@@ -384,3 +384,44 @@ def test_a_refused_sequence_is_not_attended(sla, dtype, new):
     assert c.poll() == sla.SLA_OK
     with pytest.raises(ValueError):
         c.attend(q, cu, seq=U.device_ints(slots), first=first[:3])
+
+
+def test_canaries_of_the_paged_calls(sla):
+    """Gaps between the scratch regions of every call that has some: intact after it, the same results as without, and a damaged one
+    is reported.  Handles of exactly the size asked for."""
+    import test_gpu_paged_attention as A
+    params = sla.make_params(4, 0)
+    results = []
+    for on in (False, True):
+        got = []
+        for dtype, lens in ((torch.bfloat16, A.SINGLE), (torch.bfloat16, A.CHUNKS), (torch.bfloat16, ([9000, 40], [70, 33])), (torch.float32, A.CHUNKS), (torch.float32, ([6000], [70]))):
+            cache, k, v, table, q, cu = A.build(sla, *lens, dtype=dtype)
+            h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, 8, len(lens[0]), q.shape[0], params=params))
+            sla.sla_set_debug_canaries(h, on)
+            got += sla.sla_paged_attention(h, q, cache, cu, max_new=max(lens[1]))
+            if on:
+                assert sla.sla_poll_status(h) == sla.SLA_OK
+                sla.sla_selftest_canary_trip(h)
+                assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_OVERRUN
+            got += sla.sla_paged_decode_step(h, q[:len(lens[0])], q[:len(lens[0])], cache, params)
+            assert sla.sla_poll_status(h) == sla.SLA_OK
+            h.close()
+        c = Pair(sla, sla.Handle(0, sla.sla_paged_workspace_bytes(Pair(sla, None).cache, 2, 8, 100)))
+        sla.sla_set_debug_canaries(c.h, on)
+
+        def checked():
+            if on:
+                assert sla.sla_poll_status(c.h) == sla.SLA_OK
+                sla.sla_selftest_canary_trip(c.h)
+                assert sla.sla_poll_status(c.h) == sla.SLA_ERR_DEVICE_OVERRUN
+        c.add([0, 2, 5], [40, 0, 33])
+        checked()
+        c.fork([0, 5, 0], [1, 3, 4])
+        checked()
+        c.release([0])
+        c.compact()
+        checked()
+        assert sla.sla_poll_status(c.h) == sla.SLA_OK
+        c.h.close()
+        results.append(got)
+    assert all(torch.equal(a, b) for a, b in zip(*results, strict=True))
