@@ -545,9 +545,7 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: 
     return c
 
 
-def _seq(seq: Optional[torch.Tensor], n: int) -> Optional[int]:
-    if seq is None:
-        return None
+def _seq(seq: torch.Tensor, n: int) -> int:
     if _int32(seq, "seq").numel() != n:
         raise ValueError("seq must name one slot per sequence")
     return seq.data_ptr()
@@ -562,7 +560,7 @@ def _batch(cu_new: Optional[torch.Tensor], n_new: int, max_new: Optional[int], s
         max_new = n_new if max_new is None else int(max_new)
     if first is not None and _int32(first, "first").numel() != n:
         raise ValueError("first must have one entry per sequence")
-    return sla_batch_t(n, n_new, max_new, 0, _seq(seq, n), None if cu_new is None else cu_new.data_ptr(),
+    return sla_batch_t(n, n_new, max_new, 0, None if seq is None else _seq(seq, n), None if cu_new is None else cu_new.data_ptr(),
                        None if first is None else first.data_ptr())
 
 
@@ -583,7 +581,7 @@ def sla_cache_extend(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     """Room for cu_new[x+1] - cu_new[x] tokens (None: one) of every sequence -> first int32 [n_seqs], the position of its
     first new token, -1 where it was refused.  n_new: rows of the call, when cu_new's last entry does not bound them yet."""
     n = _slots(cache, cu_new, seq)
-    slots = _seq(seq, n)
+    slots = None if seq is None else _seq(seq, n)
     _on_gpu(cache.tensors[0], cu_new, seq)
     first = _int32_output(first, cache, n)
     rows = n if cu_new is None or n == 0 else 0x7FFFFFFF if n_new is None else int(n_new)
