@@ -19,9 +19,12 @@ class PagedCache:
                  page_tokens: int = 64, dtype: torch.dtype = torch.bfloat16, device: int = 0, max_batch: Optional[int] = None,
                  max_new: int = 8192, params: Optional[B.sla_params_t] = None, share: Optional["PagedCache"] = None):
         """max_batch, max_new: the most sequences and new tokens of one call (they size the workspace); params: of the span decode
-        step, when it is used.  share: the cache of another layer, whose table, lengths, counts and handle this one uses."""
+        step, when it is used.  share: the cache of another layer, whose table, lengths, counts, handle (a workspace for that layer's
+        heads) and, where they are not given, params this one uses; pages, slots and lengths have to be the same."""
         dev = torch.device("cuda", device)
         width = -(-max_tokens // page_tokens)
+        if share is not None and (share.k.shape[0], share.k.shape[2], *share.table.shape) != (n_pages, page_tokens, n_slots, width):
+            raise ValueError("layers that share a table must have the same pages, page_tokens, slots and max_tokens")
         self.k = torch.empty(n_pages, n_kv_heads, page_tokens, head_dim, dtype=dtype, device=dev)
         self.v = torch.empty_like(self.k)
         if share is None:
@@ -31,7 +34,7 @@ class PagedCache:
         else:
             self.table, self.n_tokens, self.ref = share.table, share.n_tokens, share.ref
         self.cache = B.make_cache(self.k, self.v, self.table, self.n_tokens, self.ref)
-        self.params = params
+        self.params = share.params if params is None and share is not None else params
         if share is None:
             need = B.sla_paged_workspace_bytes(self.cache, n_q_heads, max_batch or n_slots, max_new, params=params)
             if need == 0:

@@ -425,3 +425,62 @@ def test_canaries_of_the_paged_calls(sla):
         c.h.close()
         results.append(got)
     assert all(torch.equal(a, b) for a, b in zip(*results, strict=True))
+
+
+def test_layers_that_share_a_table(sla):
+    """Three layers of one model: table, lengths and counts in common, room, forks, ends and compaction once, copies, appends,
+    attention and span steps for every layer."""
+    from paper_2601_18401_b200.paged import PagedCache
+    kw = dict(n_q_heads=8, n_kv_heads=2, page_tokens=16, max_new=400)
+    first_layer = PagedCache(60, 6, 300, params=sla.make_params(4, 0), **kw)
+    layers = [first_layer] + [PagedCache(60, 6, 300, share=first_layer, **kw) for _ in range(2)]
+    assert all(c.table is first_layer.table and c.handle is first_layer.handle and c.params is first_layer.params for c in layers)
+    g = torch.Generator(device="cuda:0")
+    rand = lambda n, h: torch.empty(n, h, 128, dtype=torch.bfloat16, device="cuda:0").normal_(generator=g)  # noqa: E731
+    rows = [{s: [] for s in range(6)} for _ in layers]       # (k, v) of every position, by layer and slot
+
+    def add(slots, new):
+        cu = U.device_ints(np.concatenate([[0], np.cumsum(new)]))
+        first = layers[0].extend(cu, seq=U.device_ints(slots))
+        assert (first >= 0).all()
+        for c, mine in zip(layers, rows):
+            kn, vn, q = rand(sum(new), 2), rand(sum(new), 2), rand(sum(new), 8)
+            c.append(cu, first, kn, vn, seq=U.device_ints(slots))
+            at = 0
+            for s, x in zip(slots, new):
+                mine[s] += [(kn[at + r], vn[at + r]) for r in range(x)]
+                at += x
+            out, lse = c.attend(q, cu, seq=U.device_ints(slots), max_new=max(new), first=first)
+            n = [len(mine[s]) for s in slots]
+            k, v = (torch.zeros(len(slots), 2, 320, 128, dtype=torch.bfloat16, device="cuda:0") for _ in range(2))   # a page each
+            for x, s in enumerate(slots):
+                k[x, :, :n[x]] = torch.stack([a for a, _ in mine[s]], 1)
+                v[x, :, :n[x]] = torch.stack([b for _, b in mine[s]], 1)
+            U.check_attention(out, lse, U.attention_reference(q, k, v, np.arange(len(slots))[:, None], n, new, 4, 0, 128 ** -0.5, 320), torch.bfloat16)
+            if max(new) == 1:
+                got = c.step(q, q, seq=U.device_ints(slots), max_tokens=300, first=first)
+                for x in range(len(slots)):
+                    one = sla.sla_decode_step(c.handle, q[x:x + 1], q[x:x + 1], k[x:x + 1, :, :n[x]].contiguous(), v[x:x + 1, :, :n[x]].contiguous(), n[x], c.params)
+                    assert torch.equal(one[2][0], got[2][x]) and torch.equal(one[3][0], got[3][x])
+                    assert ((one[0][0].float() - got[0][x].float()).abs() <= 2.0 ** -8 * one[0][0].float().abs() + 1e-5).all()
+
+    add([0, 3], [100, 37])
+    pairs = layers[0].fork(U.device_ints([0, 3, 0]), U.device_ints([1, 2, 5]))
+    for c, mine in zip(layers, rows):
+        if c is not layers[0]:
+            c.copy(pairs)
+        mine[1], mine[2], mine[5] = list(mine[0]), list(mine[3]), list(mine[0])
+    add([1, 2, 5, 0], [1, 1, 1, 1])
+    layers[0].release(U.device_ints([0, 3]))
+    for mine in rows:
+        mine[0], mine[3] = [], []
+    pairs = layers[0].compact()
+    for c in layers[1:]:
+        c.copy(pairs)
+    add([5, 2, 1], [1, 1, 1])
+    add([3, 1], [60, 20])
+    assert layers[0].poll() == sla.SLA_OK
+    for bad in (dict(page_tokens=32), dict(n_slots=5), dict(max_tokens=400), dict(n_pages=61)):
+        a = dict(n_pages=60, n_slots=6, max_tokens=300, share=first_layer) | kw | bad
+        with pytest.raises(ValueError):
+            PagedCache(**a)
