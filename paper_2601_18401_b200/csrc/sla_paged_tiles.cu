@@ -170,6 +170,10 @@ __device__ __forceinline__ uint64_t desc_advance(uint64_t desc, uint32_t bytes) 
     return desc;
 }
 
+// Polls of a wait that lasts as long as a segment: its tiles take some 2 us each (a poll at most 1.4 us), and the plain limit is the time of
+// half a million of them, 70 million keys.
+__device__ __forceinline__ uint32_t segment_polls(int tiles) { return ptx::kSpinLimit + 16u * (uint32_t)tiles; }
+
 // Of every bf16 of a pair of two: all bits of the half where the exponent is all ones, an infinity or a NaN.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((((w & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu; }
 
@@ -478,10 +482,11 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
             const bool leader = ptx::elect_one();
             uint32_t k = 0, nq[2] = {0, 0};
             int at = 0;   // tiles so far
+            uint32_t polls = ptx::kSpinLimit;   // of a wait for the segments before
             bool ok = !p.a.expire;
             if (!ok) *abort_flag = 1;
             auto put = [&](const Seg &s) {
-                ok = ptx::mbar_wait_warp(bar_seg_empty + 8 * (k % kSegs), ((k / kSegs) & 1u) ^ 1u, abort_flag);
+                ok = ptx::mbar_wait_warp(bar_seg_empty + 8 * (k % kSegs), ((k / kSegs) & 1u) ^ 1u, abort_flag, polls);
                 if (ok && leader) {
                     meta->seg[k % kSegs] = s;
                     ptx::mbar_arrive(bar_seg_full + 8 * (k % kSegs));
@@ -533,7 +538,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
                     for (int x = 0; x < 2 && ok; ++x) {
                         if (s.own[x] == 0) continue;
-                        ok = ptx::mbar_wait_warp(bar_q_empty + 8 * x, (nq[x] & 1u) ^ 1u, abort_flag);
+                        ok = ptx::mbar_wait_warp(bar_q_empty + 8 * x, (nq[x] & 1u) ^ 1u, abort_flag, polls);
                         ++nq[x];
                         if (!ok) break;
                         if (leader) {
@@ -545,6 +550,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         }
                         __syncwarp();
                     }
+                    polls = max(polls, segment_polls(tiles));
                 } while (ok && cur.next(p.a, p.plan, Shape{2 * TS, kTileShift, TS}, g, last_range));
                 if (leader && ok) p.parts.cut[range] = cut;
             }
@@ -573,7 +579,8 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 float2 stat = make_float2(0.f, -CUDART_INF_F);   // factor of O, log2-sum-exp
                 float f1 = 0.f;                                  // factor of the other stream's O
                 if (has) {
-                    ok = ptx::mbar_wait_warp(bar_l_full + 8 * x, ns[x] & 1u, abort_flag) && ptx::mbar_wait_warp(bar_o_full + 8 * x, ns[x] & 1u, abort_flag);
+                    ok = ptx::mbar_wait_warp(bar_l_full + 8 * x, ns[x] & 1u, abort_flag, segment_polls(s.hi - s.lo)) &&
+                         ptx::mbar_wait_warp(bar_o_full + 8 * x, ns[x] & 1u, abort_flag);
                     if (!ok) break;
                     ++ns[x];
                     ptx::tc_fence_after();

@@ -47,10 +47,11 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
 // for up to 1.4 us).  The first poll stands outside the loop: a wait for a phase that is already complete costs
 // 68 cycles instead of 121.
 constexpr uint32_t kSpinLimit = 1u << 20;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+// A wait for work whose length the caller knows may be given a limit of its own.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t limit = kSpinLimit) {
     if (mbar_try_wait(bar, parity)) return true;
 #pragma unroll 1
-    for (uint32_t it = 0; it < kSpinLimit; ++it) {
+    for (uint32_t it = 0; it < limit; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((it & 31u) == 31u && *abort_flag) return false;
     }
@@ -69,8 +70,8 @@ __device__ __forceinline__ bool mbar_wait_short(uint32_t bar, uint32_t parity, v
 }
 // Warp-collective form: every lane of a converged warp waits on the same barrier and all lanes
 // return the same answer, so that the .sync.aligned TMEM instructions that follow stay convergent.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t limit = kSpinLimit) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
 // One lane of a converged warp.  Issuing threads are whole warps that run their loop converged and issue under
 // this predicate: the operands then stay in uniform registers (eight MMAs 352 cycles instead of 461, a commit 10

@@ -591,3 +591,32 @@ def test_a_workspace_of_the_size_asked_for_is_enough(sla, dtype, d, hkv, G, n_se
             U.check_attention(out, lse, [t[:rows] for t in ref], dtype)
     assert sla.sla_poll_status(h) == sla.SLA_OK
     h.close()
+
+
+def test_ranges_of_more_than_a_second(sla):
+    """2^28 tokens, in pages that are the same one again and again but for forty: a CTA's range takes some three seconds, and the warps
+    that wait for its end wait so long.  The keys of the one page have logits of -200 and weights that are 0 in fp32, so that the result is
+    that over the forty."""
+    N, T, G, page, d = 1 << 28, 1600, 16, 256, 64
+    k, v = U.make_pools(8, 1, page, d, BF16)
+    k[..., 0] = 0
+    k[0] = 0
+    k[0, ..., 0] = -200
+    table = np.zeros((1, N // page), dtype=np.int32)
+    at = np.random.RandomState(4).choice(N // page - T // page - 1, 40, replace=False)
+    table[0, at] = 1 + np.arange(40) % 7
+    cache = sla.make_cache(k, v, U.device_ints(table), U.device_ints([N]), U.device_ints(np.bincount(table[0], minlength=8)))
+    q = torch.empty(T, G, d, dtype=BF16, device="cuda:0").normal_()
+    q[..., 0] = 8
+    h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, G, 1, T))
+    out, lse = sla.sla_paged_attention(h, q, cache, U.device_ints([0, T]))
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    rows = list(range(0, T, 37)) + [T - 1]
+    pages = torch.from_numpy(table[0, np.sort(at)].astype(np.int64)).cuda()
+    kk, vv = (t[pages, 0].reshape(-1, d).double() for t in (k, v))
+    z = torch.einsum("thd,jd->thj", q[rows].double(), kk) * d ** -0.5
+    w = z.softmax(-1)
+    ref = (torch.einsum("thj,jd->thd", w, vv), z.logsumexp(-1), torch.einsum("thj,jd->thd", w, vv.abs()),
+           torch.einsum("thd,jd->thj", q[rows].double().abs(), kk.abs()).amax(-1) * d ** -0.5, torch.full((len(rows),), float(len(kk)), dtype=torch.float64, device="cuda:0"))
+    U.check_attention(out[rows], lse[rows], ref, BF16)
+    h.close()
