@@ -860,7 +860,7 @@ sla::Pages make_pages(sla_handle_t h, const sla_cache_t *c) {
     return p;
 }
 
-sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, b->seq, b->cu_new, 0, b->first}; }
+sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, 0, b->seq, b->cu_new}; }
 
 // Rows that a sequence can have at most, given a bound that may be loose.
 int32_t longest_chunk(int32_t n_new, int32_t max_new) { return max_new > n_new ? n_new : max_new > 0 ? max_new : 1; }
@@ -899,7 +899,7 @@ size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_
     // the kernel and its tiles go by the rows of the longest chunk (up to 8, 16 or 64, or more) and by the sign of the scale
     for (int32_t most : {1, 8 / a.G, 16 / a.G, 64 / a.G, n_new})
         for (float scale : {1.f, -1.f}) {
-            a.b = {n_seqs, n_new, longest_chunk(n_new, most), nullptr, nullptr};
+            a.b = {n_seqs, n_new, longest_chunk(n_new, most), 0, nullptr, nullptr};
             a.scale = scale;
             const size_t bytes = sla::plan_paged(a, c->dtype, 160).bytes;
             if (bytes > need) need = bytes;
@@ -1010,6 +1010,7 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     sla::PagedCall a;
     a.c = make_pages(h, c);
     a.b = make_batch(b);
+    a.first = b->first;
     a.b.max_new = longest_chunk(b->n_new, b->max_new);
     a.Hq = n_q_heads;
     a.G = n_q_heads / c->n_kv_heads;
@@ -1059,9 +1060,9 @@ sla_status_t sla_paged_decode_step(sla_handle_t h, const void *q_s, const void *
     cudaError_t e = sla::launch_canary_fill(h->ws + kHeaderBytes, plan.canaries, st);
     for (int x = 0; x < b->n_seqs && e == cudaSuccess; x += per) {
         call.B = b->n_seqs - x < per ? b->n_seqs - x : per;   // (fewer than the plan has room for in the last launch)
-        const sla::Batch batch = {call.B, call.B, 1, b->seq ? b->seq + x : nullptr, nullptr, x, b->first ? b->first + x : nullptr};
+        const sla::Batch batch = {call.B, call.B, 1, b->seq ? 0 : x, b->seq ? b->seq + x : nullptr, nullptr};
         const size_t at = (size_t)x * q_stride_b * elem_size(c->dtype), row = (size_t)x * n_q_heads;
-        e = sla::launch_paged_decode(static_cast<const char *>(q_s) + at, static_cast<const char *>(q) + at, make_pages(h, c), batch, call,
+        e = sla::launch_paged_decode(static_cast<const char *>(q_s) + at, static_cast<const char *>(q) + at, make_pages(h, c), batch, b->first ? b->first + x : nullptr, call,
                                      c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset),
                                      static_cast<char *>(out) + at, lse + row, out_anchor + row * p->top_k, out_score + row * p->top_k, st);
         h->launches += plan.score_first ? 2 : 1;

@@ -52,12 +52,13 @@ struct PagedCache {
     static constexpr bool kPaged = true;
     Pages pages;
     Batch batch;
+    const int *first;   // of cache_extend, or NULL
     // query position of sequence x, -1 when it has no tokens or was refused its last one (or a slot or length out of bounds, which is flagged)
     __device__ __forceinline__ long long position(int x, long long most, const int *&row) const {
         const int s = slot_of(pages, batch, x);
         row = pages.table + (long long)max(s, 0) * pages.width;
         if (s >= 0) {
-            const int n = tokens_of(pages, batch, x, s);
+            const int n = tokens_of(pages, first, x, s);
             if (n <= most) return n - 1;
         }
         atomicOr(pages.status, kStatusBadIndex);
@@ -1149,10 +1150,10 @@ cudaError_t launch_decode(const void *q_s, const void *q, const void *k, const v
 }
 
 // The step for the sequences of a paged cache (c: B = sequences, Lkv = the bound of their lengths, kv strides those of a page).
-cudaError_t launch_paged_decode(const void *q_s, const void *q, const Pages &pages, const Batch &batch, const Call &c, int dtype,
+cudaError_t launch_paged_decode(const void *q_s, const void *q, const Pages &pages, const Batch &batch, const int *first, const Call &c, int dtype,
                                 const DecodePlan &plan, void *scratch, int *counters, void *out, float *lse, int32_t *out_anchor,
                                 float *out_score, cudaStream_t st) {
-    const PagedCache cache{pages, batch};
+    const PagedCache cache{pages, batch, first};
     const void *k = pages.k, *v = pages.v;
     const long long n = c.Lkv;
     if (dtype == SLA_F32) {

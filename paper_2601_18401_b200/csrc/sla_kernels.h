@@ -105,7 +105,7 @@ cudaError_t launch_decode(const void *q_s, const void *q, const void *k, const v
 
 struct Pages;   // sla_paged.cuh
 struct Batch;
-cudaError_t launch_paged_decode(const void *q_s, const void *q, const Pages &pages, const Batch &batch, const Call &c, int dtype,
+cudaError_t launch_paged_decode(const void *q_s, const void *q, const Pages &pages, const Batch &batch, const int *first, const Call &c, int dtype,
                                 const DecodePlan &plan, void *scratch, int *counters, void *out, float *lse, int32_t *out_anchor,
                                 float *out_score, cudaStream_t st);
 

@@ -452,7 +452,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                 new_rows(a.b, x_base + x, lo, hi);
                 const int slot = slot_of(a.c, a.b, x_base + x);
                 if (slot < 0) atomicOr(a.c.status, kStatusBadIndex);
-                else n = tokens_of(a.c, a.b, x_base + x, slot);
+                else n = tokens_of(a.c, a.first, x_base + x, slot);
                 s_n[x] = n;
                 s_slot[x] = slot;
                 if (hi > lo) {
