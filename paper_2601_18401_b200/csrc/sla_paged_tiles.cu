@@ -54,7 +54,8 @@ constexpr int kTurnTiles = 128;      // units of as many tiles are begun at a ti
 constexpr int kSegs = 2;            // entries of the ring of segments
 constexpr float kRescaleThreshold = 8.f;     // log2 units
 // The streams' products are kept at least this many cycles apart.  A stream's tile takes about 3400 cycles of which 1000 are products and 1200
-// exponentials; where both streams come to the same pipe at the same time it takes 4000, and nothing moves them apart again.
+// exponentials; where both streams come to the same pipe at the same time it takes 4000, and nothing moves them apart again.  (Found at D 128; at
+// D 64, whose products take half, 700 to 1700 were tried and none was better.)
 constexpr uint32_t kApart = 1300;
 constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns, those whose exponentials go to the FMA pipe
 constexpr int kRegsRow = 184, kRegsRest = 72;
