@@ -460,6 +460,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap) {
     p.max_groups = 1;
     p.min_weight = 2;
     p.small = 0;
+    p.fold_bytes = 0;
     if (paged_decode_supported(a)) {
         p.kind = PagedPlan::kDecode;
         plan_paged_decode(a, p, sm_count);
@@ -486,6 +487,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap) {
     p.off_cut = take(ranges * sizeof(Cut));
     p.off_lse2 = take(2 * ranges * p.R * 4);
     p.off_o = take(2 * ranges * p.R * a.c.D * 4);
+    p.off_fold = take(p.fold_bytes);
     if (gap) { p.canaries.add(off); off += gap; }
     p.bytes = off;
     return p;

@@ -13,7 +13,8 @@ struct PagedPlan {
     int kt_shift;           // log2 of the keys of a tile
     int small;              // tokens of a unit whose tiles weigh half
     int n_ctas, max_groups, min_weight, max_units, max_ranges;
-    size_t off_seq_at, off_unit_at, off_unit_end, off_ranges, off_seqs, off_starts, off_cut, off_lse2, off_o, bytes;
+    size_t off_seq_at, off_unit_at, off_unit_end, off_ranges, off_seqs, off_starts, off_cut, off_lse2, off_o, off_fold, bytes;
+    size_t fold_bytes;      // sums of O beside TMEM (sla_paged_tiles.cu)
     Canaries canaries;
 };
 

@@ -58,6 +58,12 @@ constexpr float kRescaleThreshold = 8.f;     // log2 units
 // D 64, whose products take half, 700 to 1700 were tried and none was better.)
 constexpr uint32_t kApart = 1300;
 constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns, those whose exponentials go to the FMA pipe
+// Tiles whose products a stream adds up in TMEM before O is moved to a sum in memory: the tensor cores cut what does not fit into 24 bits, always
+// towards zero, so that values of one sign come out too small by about 2^-24 for every 16 keys.  Over 2^20, 2^22 and 2^24 keys of like weight
+// that was 0.6, 2.6 and 5 % where a range went on so long; it is 0.03 % after 65536 keys, below the rounding of the result to bf16.  Only calls
+// whose tables and windows reach further take the kernel that does so (kLong): its loop costs 1 to 3 % (1 to 600 tokens of 16 sequences 61.9 us
+// instead of 60.2, 1999 at 30011 988 instead of 980, 2400 at 2^20 nothing that can be told from noise).
+constexpr int kFoldTiles = 512;
 constexpr int kRegsRow = 184, kRegsRest = 72;
 static_assert(2 * kRegsRow + 2 * kRegsRest <= 4 * 128, "more registers than the block is launched with");
 
@@ -107,6 +113,7 @@ struct TileParams {
     const bf16 *q;
     bf16 *out;
     float *lse;
+    float *fold;                      // [CTAs][8 warps] sums of O, for segments of more than kFoldTiles tiles (kLong)
     int TS;                           // tokens of a stream
     int t_inner;                      // row i is token i % TS, head i / TS (else token i / G, head i % G), as Q's strides nest
     int slot_t, slot_h, slot_p;       // (token, head, page) among the tensor-map coordinates 1..3 of K and V
@@ -190,6 +197,42 @@ __device__ __noinline__ void clear_not_finite(uint4 *v) {
         }
 }
 
+// O of a warp's rows and its sum in memory, [D / 4] pieces of 16 bytes a lane and the maximum that they refer to, by a converged warp
+// when the products so far are complete.  first: the sum is O; else the sum and O together, by the present maximum.  last: into O, which stays;
+// otherwise into memory, and O is zero again.
+template <int D>
+__device__ __noinline__ void fold_rows(float *fold, uint32_t o_addr, float m, bool first, bool last) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;   // (rows of stream warp / 4)
+    float4 *sum = reinterpret_cast<float4 *>(fold + ((long long)blockIdx.x * 8 + warp) * 32 * (D + 4)) + lane;
+    float4 *m_at = sum + 32 * (D / 4);
+    float f = 0.f;
+    if (!first) {
+        const float m_sum = m_at->x;
+        f = m_sum == m ? 1.f : ex2_approx(m_sum - m);
+    }
+#pragma unroll 1
+    for (int c = 0; c < D; c += 16) {
+        uint32_t o[16];
+        float4 w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[u] = first ? make_float4(0.f, 0.f, 0.f, 0.f) : sum[32 * (c / 4 + u)];
+        ptx::tmem_ld16(o_addr + c, o);
+        ptx::tmem_wait_ld();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            w[u].x = fmaf(w[u].x, f, __uint_as_float(o[4 * u])); w[u].y = fmaf(w[u].y, f, __uint_as_float(o[4 * u + 1]));
+            w[u].z = fmaf(w[u].z, f, __uint_as_float(o[4 * u + 2])); w[u].w = fmaf(w[u].w, f, __uint_as_float(o[4 * u + 3]));
+            if (!last) sum[32 * (c / 4 + u)] = w[u];
+            o[4 * u] = last ? __float_as_uint(w[u].x) : 0u; o[4 * u + 1] = last ? __float_as_uint(w[u].y) : 0u;
+            o[4 * u + 2] = last ? __float_as_uint(w[u].z) : 0u; o[4 * u + 3] = last ? __float_as_uint(w[u].w) : 0u;
+        }
+        ptx::tmem_st16(o_addr + c, o);
+    }
+    if (!last) m_at->x = m;
+    ptx::tmem_wait_st();
+    ptx::tc_fence_before();
+}
+
 // Adds the values that the row warps have cleared to the rows of O that see them: those that are not finite, of the keys of stream x
 // that not every row of the unit sees.  Whatever a row's sums and maxima are, such a value makes the result infinite or NaN, so that
 // its weight counts only as positive or (a logit of -inf) zero.  A converged warp with a row of O a lane; a lane looks at one of 32
@@ -267,7 +310,7 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
     ptx::tc_fence_before();
 }
 
-template <int D>
+template <int D, bool kLong>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
             const __grid_constant__ TileParams p) {
@@ -681,6 +724,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
                 for (int left = s.own[x]; left > 0; --left, ++nt) {
                     const int k0 = j * kKeys;
+                    if (kLong && s.own[x] > kFoldTiles && left != s.own[x] && (s.own[x] - left) % kFoldTiles == 0) {   // (the wait as before a rescale, below)
+                        const int before = j - step;
+                        const uint32_t v = 2 * (tiles + s.place(before < lx ? before + hx - lx : before)) + 1u;
+                        if (!(ok = ptx::mbar_wait_warp(bar_kv_empty + 80 * x + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
+                        ptx::tc_fence_after();
+                        fold_rows<D>(p.fold, o_addr, fresh ? -CUDART_INF_F : m_ref, s.own[x] - left == kFoldTiles, false);
+                    }
                     if (!(ok = ptx::mbar_wait_warp(bar_s_full + 8 * x, nt & 1u, abort_flag))) break;
                     ptx::tc_fence_after();
                     uint32_t sr[4][32];
@@ -818,11 +868,13 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar_checked + 8 * x);
                 if (!(ok = ptx::mbar_wait_warp(bar_checked + 8 * x, ns & 1u, abort_flag))) break;
-                if (__any_sync(0xffffffffu, *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1)) {
+                const bool odd = __any_sync(0xffffffffu, *(volatile int *)&meta->odd[x][k & 7] == (int)k + 1);
+                if (odd || (kLong && s.own[x] > kFoldTiles)) {
                     // O is complete, and stays: the next segment's first PV waits for the epilogue, which waits for this warp
                     if (!(ok = ptx::mbar_wait_warp(bar_o_full + 8 * x, ns & 1u, abort_flag))) break;
                     ptx::tc_fence_after();
-                    add_not_finite<D>(p, s, x, tmem);
+                    if (kLong && s.own[x] > kFoldTiles) fold_rows<D>(p.fold, o_addr, fresh ? -CUDART_INF_F : m_ref, false, true);
+                    if (odd) add_not_finite<D>(p, s, x, tmem);
                 }
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
@@ -906,14 +958,14 @@ bool make_map(CUtensorMap *tm, const void *ptr, int D, const Dim *d, int n, cons
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, bool kLong>
 cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, char *scratch, void *out, float *lse, cudaStream_t st) {
     static bool allowed[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !allowed[dev]) {
-        e = cudaFuncSetAttribute(paged_tiles<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
+        e = cudaFuncSetAttribute(paged_tiles<D, kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
         if (e != cudaSuccess) return e;
         if (dev < 64) allowed[dev] = true;
     }
@@ -924,6 +976,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
     p.q = (const bf16 *)q;
     p.out = (bf16 *)out;
     p.lse = lse;
+    p.fold = pl.fold_bytes ? reinterpret_cast<float *>(scratch + pl.off_fold) : nullptr;
     p.TS = pl.TS;
     p.out32 = (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && a.q_st % 16 == 0 && a.q_sh % 16 == 0;
     p.box_rows = a.c.P < kKeys ? a.c.P : kKeys;
@@ -940,7 +993,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
     CUtensorMap tq, tk, tv;
     if (!make_map(&tq, q, D, qd, 2, qbox) || !make_map(&tk, a.c.k, D, kd, 3, kbox) || !make_map(&tv, a.c.v, D, kd, 3, kbox))
         return cudaErrorInvalidValue;
-    return launch_chained(paged_tiles<D>, dim3(pl.n_ctas), dim3(kThreads), Layout<D>::kSmem, st, tq, tk, tv, p);
+    return launch_chained(paged_tiles<D, kLong>, dim3(pl.n_ctas), dim3(kThreads), Layout<D>::kSmem, st, tq, tk, tv, p);
 }
 
 }  // namespace
@@ -965,10 +1018,15 @@ void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
     const long long most = groups < weight / (128 * kGroupWeight) ? groups : weight / (128 * kGroupWeight);
     p.max_groups = most < 1 ? 1 : most < 8 ? (int)most : 8;
     p.min_weight = 3;
+    // A unit's keys at most: of a table row, or of its tokens' windows, with the tiles at either end.  (A warp's 32 rows of O and a maximum each, in
+    // 16-byte pieces.)
+    const long long row = (long long)a.c.width << a.c.shift, keys = a.window > 0 && a.window < row ? (long long)a.window + p.TQ + 2 * kKeys : row;
+    p.fold_bytes = keys > (long long)kFoldTiles * kKeys ? (size_t)sm_count * 8 * 32 * (a.c.D + 4) * sizeof(float) : 0;
 }
 
 cudaError_t launch_paged_tiles(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
-    return a.c.D == 64 ? tiles_of<64>(q, a, p, scratch, out, lse, st) : tiles_of<128>(q, a, p, scratch, out, lse, st);
+    if (p.fold_bytes) return a.c.D == 64 ? tiles_of<64, true>(q, a, p, scratch, out, lse, st) : tiles_of<128, true>(q, a, p, scratch, out, lse, st);
+    return a.c.D == 64 ? tiles_of<64, false>(q, a, p, scratch, out, lse, st) : tiles_of<128, false>(q, a, p, scratch, out, lse, st);
 }
 
 }  // namespace sla

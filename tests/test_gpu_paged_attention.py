@@ -620,3 +620,40 @@ def test_ranges_of_more_than_a_second(sla):
            torch.einsum("thd,jd->thj", q[rows].double().abs(), kk.abs()).amax(-1) * d ** -0.5, torch.full((len(rows),), float(len(kk)), dtype=torch.float64, device="cuda:0"))
     U.check_attention(out[rows], lse[rows], ref, BF16)
     h.close()
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("n,T,G", [(1 << 20, 2400, 16), ((1 << 22) + 777, 2400, 16), (1 << 22, 1, 16), (600000, 700, 1)])
+def test_long_sums_of_values_of_one_sign(sla, dtype, d, n, T, G):
+    """Hundreds of thousands of keys of like weight in a range: the sums lose nothing at their lower end, where the tensor cores cut
+    what does not fit.  Pages that are the same 64 again and again, so that a key's weight counts as often as a row sees its page.
+
+    Bounds, relative, values positive: bf16 rounds each weight and the result to 2^-9; a sum of 65536 keys in TMEM is cut 4096 times by at
+    most 2^-23; the 8192 or so tiles' sums in fp32 (of O, of the weights) are off by 2^-24 each.  fp32 instead: 2^-24 for every 64 keys'
+    sums and within them, and the logits' 2^-19."""
+    if dtype == F32 and n > 1 << 20 and T > 1:
+        n = (1 << 18) + 777   # (0.2 s)
+    page, n_pages = 256, 64
+    k, v = U.make_pools(n_pages, 1, page, d, dtype)
+    v.abs_()
+    width = -(-n // page)
+    table = (np.arange(width) % n_pages).astype(np.int32)[None]
+    cache = sla.make_cache(k, v, U.device_ints(table), U.device_ints([n]), U.device_ints(np.bincount(table[0], minlength=n_pages)))
+    q = torch.empty(T, G, d, dtype=dtype, device="cuda:0").normal_()
+    h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, G, 1, T))
+    sla.sla_set_debug_canaries(h, True)
+    out, lse = sla.sla_paged_attention(h, q, cache, None if T == 1 else U.device_ints([0, T]))
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    kk, vv = (t[:, 0].reshape(-1, d).double() for t in (k, v))
+    at = torch.arange(len(kk), device="cuda:0")
+    tiles = n / 128
+    tol = 2.0 ** -8 + 4096 * 2.0 ** -23 + 2 * tiles * 2.0 ** -24 if dtype == BF16 else 4 * tiles * 2.0 ** -24 + 2.0 ** -18
+    for r in {0, T // 2, T - 1}:
+        seen = n - T + r + 1
+        times = (seen // len(kk) + (at < seen % len(kk))).double()
+        z = q[r].double() @ kk.T * d ** -0.5
+        w = torch.exp(z) * times
+        want = (w @ vv) / w.sum(-1, keepdim=True)
+        assert ((out[r].double() / want - 1).abs() <= tol).all()
+        assert ((lse[r].double() - w.sum(-1).log()).abs() <= tol).all()
+    h.close()
