@@ -1039,6 +1039,8 @@ sla_status_t sla_paged_decode_step(sla_handle_t h, const void *q_s, const void *
     if (n_q_heads <= 0 || n_q_heads % c->n_kv_heads) return fail(h, SLA_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of n_kv_heads%s");
     const sla_layout_t l = layout_of(c, n_q_heads, b->n_seqs, q_stride_b, q_stride_h);
     if (const char *why = check_layout_params(&l, p, true)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if ((b->n_seqs > 1 && q_stride_b < c->head_dim) || (n_q_heads > 1 && q_stride_h < c->head_dim))   // rows of out would lie over one another
+        return fail(h, SLA_ERR_INVALID_ARG, "sequence or head stride below head_dim%s");
     if (max_tokens <= 0 || max_tokens > 2147483647LL) return fail(h, SLA_ERR_INVALID_ARG, "max_tokens must be in 1..2^31-1%s");
     if (const char *why = check_device(h)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
     if (!q_s || !q || !out || !lse || !out_anchor || !out_score) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");

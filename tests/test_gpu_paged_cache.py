@@ -484,3 +484,22 @@ def test_layers_that_share_a_table(sla):
         a = dict(n_pages=60, n_slots=6, max_tokens=300, share=first_layer) | kw | bad
         with pytest.raises(ValueError):
             PagedCache(**a)
+
+
+def test_queries_that_lie_over_one_another_are_refused(sla):
+    """Broadcast queries: the output has their strides, and its rows would be written by several sequences or heads."""
+    import test_gpu_paged_attention as A
+    h = sla.Handle(0, 1 << 26)
+    cache, k, v, table, _, _ = A.build(sla, [100, 60], [0, 0])
+    params = sla.make_params(4, 0)
+    one = torch.ones(1, 8, 128, dtype=torch.bfloat16, device="cuda:0")
+    for q in (one.expand(2, 8, 128), one[:, :1].repeat(2, 1, 1).expand(2, 8, 128), one[:, :1].expand(2, 8, 128)):
+        with pytest.raises(sla.SlaError) as e:
+            sla.sla_paged_decode_step(h, q, q, cache, params)
+        assert e.value.status == -1
+        with pytest.raises(sla.SlaError) as e:
+            sla.sla_paged_attention(h, q, cache)
+        assert e.value.status == -1
+    sla.sla_paged_decode_step(h, one.expand(1, 8, 128), one, cache, params, seq=U.device_ints([1]))   # a single sequence has no such stride
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    h.close()
