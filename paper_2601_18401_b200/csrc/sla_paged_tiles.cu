@@ -11,8 +11,8 @@
 // CTA's ranges of the plan (sla_paged.cuh), hands the segments on through a ring in shared memory and fetches their Q.
 // Shared memory: Q 2 x 32 KB, ring 5 x 32 KB (K and V tiles in turn).  TMEM: O of the streams in columns 0 and 128, S in 256 and 384.
 //
-// Measured (32/8 heads, D 128, pages of 64 tokens): 8192 tokens that end at 65536 in 7.4 ms = 1110 TFLOP/s at the power cap (1.59 GHz),
-// 6.7 ms and 1230 in a single call; 1999 at 30011 in 0.95 ms, 1000; 512 at 65536 in 0.53 ms, 1020; 64 at 65536 in 83 us, 3.2 TB/s.  D 64:
+// Measured (32/8 heads, D 128, pages of 64 tokens): 8192 tokens that end at 65536 in 7.5 to 7.7 ms = 1070 to 1100 TFLOP/s at the power cap
+// (1.59 GHz), 6.7 ms and 1230 in a single call; 1999 at 30011 in 0.95 to 0.98 ms, 990; 512 at 65536 in 0.54 ms, 1010; 64 at 65536 in 83 us, 3.2 TB/s.  D 64:
 // four prompts of 2048 tokens in 135 us, 510 TFLOP/s.  Bound by the chain of a row warp: a tile takes a stream about 3400 cycles, of which its products take the tensor pipe
 // 1000, so that two streams leave that pipe idle for two fifths of the time.
 //
