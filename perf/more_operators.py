@@ -2,7 +2,7 @@
 tensors, and attention of new tokens over the cache (one token a sequence, a few, chunks of a prefill, mixed batches).
 
 A value x of a key or value is held as c s: s per token, KV head and group of 32 dimensions is the smallest number of five significant
-bits (and at least 2^-40) with 7.5 s >= max |x|, c = x / s rounded to a whole number, -7 .. 7.  A page's plane of one head has the
+bits (and at least 2^-40) with 7.5 s >= max |x|, c = x / s rounded to a whole number (halves away from zero), -7 .. 7.  A page's plane of one head has the
 codes of its tokens, head_dim / 2 bytes each, and behind them their scales, head_dim / 32 bf16 each.
 
 A case gives ranges; which length each sequence of a case has, and which page each part of it lies in, follows from the case's
@@ -170,7 +170,7 @@ def _quantise(x):
     s = torch.where(7.5 * (s - quantum) >= a, s - quantum, s)          # (2 / 15 is rounded)
     s = torch.where(7.5 * s < a, s + quantum, s)
     s = s.clamp(min=2.0 ** -40)
-    return torch.round(g / s[..., None]).clamp(-7, 7).flatten(-2), s
+    return (torch.floor(g.abs() / s[..., None] + 0.5).clamp(max=7) * torch.sign(g)).flatten(-2), s
 
 
 def _pack(codes, s, values):
@@ -371,8 +371,8 @@ def _held(x):
     g = x.double().unflatten(-1, (-1, 32))
     s = numbers[torch.searchsorted(7.5 * numbers, g.abs().amax(-1))][..., None]
     code = torch.zeros_like(g)
-    for j in range(7):      # a value half way between two codes goes to the even one
-        code += (g.abs() > (j + 0.5) * s) if j % 2 == 0 else (g.abs() >= (j + 0.5) * s)
+    for j in range(7):
+        code += g.abs() >= (j + 0.5) * s
     return (torch.sign(g) * code * s).flatten(-2)
 
 
