@@ -85,7 +85,9 @@ typedef enum {
     SLA_ERR_CACHE_FULL = -8      /* a sequence was refused pages: none free, or its table row full */
 } sla_status_t;
 
-typedef enum { SLA_F32 = 0, SLA_BF16 = 1 } sla_dtype_t;
+/* SLA_Q4, SLA_Q4_F32: a paged cache in four bits; the other tensors of its calls are bf16, or fp32 (the cache is the
+ * same). */
+typedef enum { SLA_F32 = 0, SLA_BF16 = 1, SLA_Q4 = 2, SLA_Q4_F32 = 3 } sla_dtype_t;
 
 /* SLA_UNION: one softmax over the de-duplicated union of the selected spans and the local window
  * (reduces to dense causal attention when the selection covers every key); sla_span_attention and
@@ -384,15 +386,28 @@ sla_status_t sla_prefill_host(sla_handle_t handle, const void *q_s_host, const v
  * only, so that appending never writes into another's tokens.  Pages are handed out in ascending order of
  * their index, in the order of the call's sequences: results do not depend on timing.
  *
+ * In four bits (dtype SLA_Q4 or SLA_Q4_F32): a row of head_dim values is held in groups of 32 consecutive ones, each as
+ * a scale s of its group times a whole number c, -7 .. 7:
+ *   a = max |x| of the group;  s = the smallest number of five significant bits with 7.5 s >= a, at least 2^-40;
+ *   c = x / s rounded to a whole number, halves away from zero, at most 7 in magnitude
+ * so that |x - c s| <= s / 2.  c s has eight significant bits: it is a bf16 number, and what the calls read.  A group with
+ * an infinity or a NaN, or whose s would be 2^40 or more, reads as NaN.  A row takes head_dim / 2 + head_dim / 16 bytes (72
+ * for 128 values).  k and v are [n_pages, n_kv_heads] planes of SLA_Q4_PLANE_BYTES contiguous bytes each, stride_{page,h} in
+ * BYTES and multiples of 16, stride_t 0.  A plane has its tokens' codes, head_dim / 2 bytes each, and then their scales,
+ * head_dim / 32 bf16 each.  Four codes make a 16-bit word: code i of word (g, c, h) is dimension 32 g + 8 c + 2 i + h, its sign
+ * bit 15, 14, 7, 6 and its magnitude bits 0-2, 3-5, 8-10, 11-13 for i = 0, 1, 2, 3; a row's words lie in the order (c, g, h)
+ * in k and (c, h, g) in v.  Every call below takes such a cache except sla_paged_decode_step (SLA_ERR_UNSUPPORTED).
+ *
  * What the device finds wrong -- a slot outside [0, n_slots), a table entry outside [0, n_pages) where
  * the sequence has tokens, lengths that do not fit the table -- sets the status word
  * (SLA_ERR_DEVICE_INDEX at the next sla_poll_status); nothing outside the cache is read or written. */
+#define SLA_Q4_PLANE_BYTES(page_tokens, head_dim) ((page_tokens) * ((head_dim) / 2 + (head_dim) / 16))
 typedef struct {
     int32_t n_pages, page_tokens;   /* page_tokens: a power of two, 16 .. 256                     */
     int32_t n_kv_heads, head_dim;   /* head_dim 64 or 128                                          */
     int32_t dtype, reserved;        /* sla_dtype_t of k and v; reserved must be 0                   */
     int32_t n_slots, table_width;   /* table_width * page_tokens at most 2^31 - 1025                */
-    int64_t stride_page, stride_h, stride_t; /* of k and v, in elements                            */
+    int64_t stride_page, stride_h, stride_t; /* of k and v, in elements (four bits: in bytes)      */
     void *k, *v;
     int32_t *table, *n_tokens, *ref;
 } sla_cache_t;
@@ -430,10 +445,19 @@ sla_status_t sla_cache_extend(sla_handle_t handle, const sla_cache_t *cache, con
                               int32_t *first, void *stream);
 
 /* Writes the new tokens' keys and values: row r of sequence x goes to position first[x] + r.  k_new, v_new
- * [n_new, n_kv_heads, head_dim], strides new_stride_{t,h} in elements.  Sequences with first < 0 are left out. */
+ * [n_new, n_kv_heads, head_dim], strides new_stride_{t,h} in elements.  Sequences with first < 0 are left out.
+ * Into a cache in four bits they are rounded as they are written. */
 sla_status_t sla_cache_append(sla_handle_t handle, const sla_cache_t *cache, const sla_batch_t *batch,
                               const int32_t *first, const void *k_new, const void *v_new, int64_t new_stride_t,
                               int64_t new_stride_h, void *stream);
+
+/* Reads rows back: row r of sequence x is position first[x] + r, for r < cu_new[x+1] - cu_new[x] (first NULL: position r).
+ * k_out, v_out [n_new, n_kv_heads, head_dim], strides out_stride_{t,h} in elements: the cache's values, of one in four bits
+ * c s in bf16 or fp32, both exact.  Sequences with first < 0 are left out; so is a position that the sequence does not have,
+ * which sets SLA_ERR_DEVICE_INDEX.  The rows of k_out and v_out left out keep what they hold. */
+sla_status_t sla_cache_read(sla_handle_t handle, const sla_cache_t *cache, const sla_batch_t *batch,
+                            const int32_t *first, void *k_out, void *v_out, int64_t out_stride_t,
+                            int64_t out_stride_h, void *stream);
 
 /* Ends the sequences in the n slots seq (device): their pages lose a reference each, and the slots are empty. */
 sla_status_t sla_cache_release(sla_handle_t handle, const sla_cache_t *cache, const int32_t *seq, int32_t n,
@@ -461,7 +485,8 @@ sla_status_t sla_cache_copy(sla_handle_t handle, const sla_cache_t *cache, const
  * is position i = n_tokens - (its new tokens) + r and attends to positions [0, i], or with a local window w
  * (the W of Algorithm 1) to [max(0, i-w+1), i].  The form for contexts too short for spans to pay (the paper
  * puts that at about 60K tokens), for chunks of a prefill and single tokens alike.
- *   q     in   [n_new, n_q_heads, head_dim]  strides q_stride_{t,h}, cache dtype; group size <= 16
+ *   q     in   [n_new, n_q_heads, head_dim]  strides q_stride_{t,h}, cache dtype (bf16 or fp32 for a cache in four bits);
+ *              group size <= 16
  *   out   out  as q;  lse out [n_new, n_q_heads] fp32 contiguous (natural log); a row without keys (a
  *              sequence that is shorter than its new tokens) is 0 and -inf
  * bf16 runs on the tensor cores with fp32 sums (weights are rounded to bf16 before they meet the values),

@@ -10,5 +10,5 @@ from .binding import (  # noqa: F401
     sla_pattern_len_steps, sla_pattern_offsets, sla_probe_l2_read, sla_selftest_canary_trip, sla_selftest_wait_expiry, sla_selftest_paged_expiry, sla_set_debug_canaries, sla_prefill_host, sla_span_attention, sla_span_attention_gated, sla_span_search, sla_workspace_bytes,
     SLA_ERR_CACHE_FULL, SLA_ERR_DEVICE_INDEX, SLA_ERR_DEVICE_OVERRUN, SLA_ERR_DEVICE_TIMEOUT, make_cache, sla_batch_t, sla_cache_append, sla_cache_compact, sla_cache_copy,
     sla_cache_extend, sla_cache_fork, sla_cache_release, sla_cache_t, sla_paged_attention, sla_paged_decode_step,
-    sla_paged_workspace_bytes,
+    sla_paged_workspace_bytes, SLA_Q4, SLA_Q4_F32, make_cache_q4, q4_plane_bytes, sla_cache_read,
 )

@@ -17,7 +17,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libsla.so")
 
 SLA_OK = 0
-SLA_F32, SLA_BF16 = 0, 1
+SLA_F32, SLA_BF16, SLA_Q4, SLA_Q4_F32 = 0, 1, 2, 3
 SLA_UNION, SLA_PER_SPAN = 0, 1
 SLA_ERR_INVALID_ARG = -1
 SLA_ERR_UNSUPPORTED = -2
@@ -36,7 +36,7 @@ EXPORTS = [
     "sla_pattern_offsets", "sla_pattern_len_steps", "sla_probe_l2_read", "sla_selftest_wait_expiry",
     "sla_selftest_paged_expiry",
     "sla_set_debug_canaries", "sla_selftest_canary_trip", "sla_attention_tile_stats",
-    "sla_paged_workspace_bytes", "sla_cache_extend", "sla_cache_append", "sla_cache_release", "sla_cache_fork",
+    "sla_paged_workspace_bytes", "sla_cache_extend", "sla_cache_append", "sla_cache_read", "sla_cache_release", "sla_cache_fork",
     "sla_cache_compact", "sla_cache_copy", "sla_paged_attention", "sla_paged_decode_step",
 ]
 
@@ -147,6 +147,8 @@ def load_library():
     lib.sla_cache_extend.argtypes = [vp, vp, vp, vp, vp]
     lib.sla_cache_append.restype = i32
     lib.sla_cache_append.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp]
+    lib.sla_cache_read.restype = i32
+    lib.sla_cache_read.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp]
     lib.sla_cache_release.restype = i32
     lib.sla_cache_release.argtypes = [vp, vp, vp, i32, vp]
     lib.sla_cache_fork.restype = i32
@@ -541,6 +543,37 @@ def make_cache(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: 
     c = sla_cache_t(n_pages, page, hkv, d, _dtype_code(k), 0, table.shape[0], table.shape[1], k.stride(0), k.stride(1),
                     k.stride(2), k.data_ptr(), v.data_ptr(), table.data_ptr(), n_tokens.data_ptr(), ref.data_ptr())
     c.tensors = (k, v, table, n_tokens, ref)
+    c.tensor_dtype, c.tensor_code = k.dtype, c.dtype   # of the keys, values, queries and results of its calls
+    c.address = C.addressof(c)
+    return c
+
+
+def q4_plane_bytes(page_tokens: int, head_dim: int) -> int:
+    """Bytes of a plane (the rows of a page and head) of a cache in four bits."""
+    return page_tokens * (head_dim // 2 + head_dim // 16)
+
+
+def make_cache_q4(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, n_tokens: torch.Tensor, ref: torch.Tensor, *,
+                  page_tokens: int, head_dim: int, dtype: torch.dtype = torch.bfloat16) -> sla_cache_t:
+    """A paged cache in four bits from its tensors: k, v uint8 [n_pages, Hkv, q4_plane_bytes(page_tokens, head_dim)] (any strides
+    with the bytes of a plane contiguous; the two share them), the others as for :func:`make_cache`.  dtype: of the keys, values, queries and
+    results of its calls, bf16 or fp32."""
+    if k.dim() != 3 or k.shape != v.shape or k.stride() != v.stride() or k.dtype is not torch.uint8 or v.dtype is not torch.uint8:
+        raise ValueError("k and v must be uint8 [n_pages, Hkv, bytes of a plane] and share their shape and strides")
+    if k.stride(-1) != 1 or k.shape[2] != q4_plane_bytes(page_tokens, head_dim):
+        raise ValueError("a plane must have q4_plane_bytes(page_tokens, head_dim) contiguous bytes")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}")
+    _int32(table, "table"), _int32(n_tokens, "n_tokens"), _int32(ref, "ref")
+    if table.dim() != 2 or n_tokens.shape != table.shape[:1] or ref.shape != k.shape[:1]:
+        raise ValueError("table must be [n_slots, table_width], n_tokens [n_slots] and ref [n_pages]")
+    if len({t.device for t in (k, v, table, n_tokens, ref)}) != 1:
+        raise ValueError("the tensors of a cache must be on one device")
+    c = sla_cache_t(k.shape[0], page_tokens, k.shape[1], head_dim, SLA_Q4 if dtype is torch.bfloat16 else SLA_Q4_F32, 0,
+                    table.shape[0], table.shape[1], k.stride(0), k.stride(1), 0, k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                    n_tokens.data_ptr(), ref.data_ptr())
+    c.tensors = (k, v, table, n_tokens, ref)
+    c.tensor_dtype, c.tensor_code = dtype, SLA_BF16 if dtype is torch.bfloat16 else SLA_F32
     c.address = C.addressof(c)
     return c
 
@@ -598,7 +631,7 @@ def sla_cache_append(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     shape, strides, dtype = k_new.shape, k_new.stride(), k_new.dtype
     if shape != v_new.shape or strides != v_new.stride() or dtype is not v_new.dtype or strides[-1] != 1:
         raise ValueError("k_new and v_new must share shape, strides and dtype, head_dim contiguous")
-    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or dtype is not cache.tensors[0].dtype:
+    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or dtype is not cache.tensor_dtype:
         raise ValueError("k_new must be [n_new, Hkv, D] in the cache's dtype")
     _on_gpu(cache.tensors[0], k_new, v_new, first, cu_new, seq)
     b = _batch(cu_new, shape[0], None, seq)
@@ -607,6 +640,36 @@ def sla_cache_append(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.
     handle.check(handle._lib.sla_cache_append(handle.ptr, cache.address, C.addressof(b), first.data_ptr(), k_new.data_ptr(),
                                               v_new.data_ptr(), strides[0], strides[1], _stream_ptr(stream)),
                  "sla_cache_append")
+
+
+def sla_cache_read(handle: Handle, cache: sla_cache_t, cu_new: Optional[torch.Tensor], first: Optional[torch.Tensor] = None, *,
+                   n_new: Optional[int] = None, seq: Optional[torch.Tensor] = None, k_out=None, v_out=None, stream=None):
+    """Positions first[x] .. (None: 0 ..) of the sequences, cu_new[x+1] - cu_new[x] of each (None: one), back into k_out, v_out
+    [n_new, Hkv, D] in the dtype of the cache's calls -> k_out, v_out.  n_new: their rows, where they are not given."""
+    if (k_out is None) != (v_out is None):
+        raise ValueError("k_out and v_out go together")
+    if k_out is None:
+        if n_new is None:
+            if cu_new is not None:
+                raise ValueError("give n_new, the rows of the call, or k_out and v_out")
+            n_new = _slots(cache, None, seq)
+        k_out = torch.empty(int(n_new), cache.n_kv_heads, cache.head_dim, dtype=cache.tensor_dtype, device=cache.tensors[0].device)
+        v_out = torch.empty_like(k_out)
+    shape, strides = k_out.shape, k_out.stride()
+    if shape != v_out.shape or strides != v_out.stride() or k_out.dtype is not cache.tensor_dtype or v_out.dtype is not cache.tensor_dtype:
+        raise ValueError("k_out and v_out must share shape and strides, in the dtype of the cache's calls")
+    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or strides[-1] != 1:
+        raise ValueError("k_out must be [n_new, Hkv, D], head_dim contiguous")
+    if n_new is not None and int(n_new) != shape[0]:
+        raise ValueError("n_new must be the rows of k_out")
+    _on_gpu(cache.tensors[0], k_out, v_out, first, cu_new, seq)
+    b = _batch(cu_new, shape[0], None, seq)
+    if first is not None and _int32(first, "first").numel() != b.n_seqs:
+        raise ValueError("first must have one entry per sequence")
+    handle.check(handle._lib.sla_cache_read(handle.ptr, cache.address, C.addressof(b), None if first is None else first.data_ptr(),
+                                            k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1], _stream_ptr(stream)),
+                 "sla_cache_read")
+    return k_out, v_out
 
 
 def sla_cache_release(handle: Handle, cache: sla_cache_t, seq: torch.Tensor, *, stream=None) -> None:
@@ -653,7 +716,7 @@ def sla_paged_attention(handle: Handle, q: torch.Tensor, cache: sla_cache_t, cu_
     [n_new, Hq].  max_new: the longest chunk (default n_new); it decides the tiles.  first: what sla_cache_extend returned; the
     rows of a sequence that it refused are then 0 and -inf (without it, those of the tokens the sequence has)."""
     (T, Hq, D), strides, dtype = q.shape, q.stride(), q.dtype
-    if strides[-1] != 1 or D != cache.head_dim or _dtype_code(q) != cache.dtype:
+    if strides[-1] != 1 or D != cache.head_dim or _dtype_code(q) != cache.tensor_code:
         raise ValueError("q must be [n_new, Hq, D] in the cache's dtype and head_dim, head_dim contiguous")
     if out is None:
         out = torch.empty_strided(q.shape, strides, dtype=dtype, device=q.device)
@@ -679,7 +742,7 @@ def sla_paged_decode_step(handle: Handle, q_s: torch.Tensor, q: torch.Tensor, ca
     B, Hq, D = q.shape
     if q_s.stride() != q.stride() or q.stride(-1) != 1 or q_s.shape != q.shape:
         raise ValueError("q_s and q must share shape and strides, head_dim contiguous")
-    if D != cache.head_dim or _dtype_code(q) != cache.dtype or _dtype_code(q_s) != cache.dtype:
+    if D != cache.head_dim or _dtype_code(q) != cache.tensor_code or _dtype_code(q_s) != cache.tensor_code:
         raise ValueError("q_s and q must have the cache's dtype and head_dim")
     dev = q.device
     if out is None:

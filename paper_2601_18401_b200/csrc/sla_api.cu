@@ -10,6 +10,7 @@
 
 #include "sla_kernels.h"
 #include "sla_paged_attn.h"
+#include "sla_q4.cuh"
 
 struct sla_handle_s {
     int device = 0;
@@ -817,6 +818,10 @@ sla_status_t sla_prefill_host(sla_handle_t h, const void *q_s_host, const void *
 // ---- paged cache ------------------------------------------------------------------------------------
 namespace {
 
+bool four_bits(const sla_cache_t *c) { return c->dtype == SLA_Q4 || c->dtype == SLA_Q4_F32; }
+// The type of the tensors of a cache's calls.
+int tensor_type(const sla_cache_t *c) { return c->dtype == SLA_Q4 ? SLA_BF16 : c->dtype == SLA_Q4_F32 ? SLA_F32 : c->dtype; }
+
 const char *check_cache(const sla_cache_t *c) {
     if (!c) return "cache is NULL";
     if (c->n_pages <= 0 || c->n_kv_heads <= 0 || c->n_slots <= 0 || c->table_width <= 0) return "n_pages, n_kv_heads, n_slots and table_width must be positive";
@@ -825,11 +830,17 @@ const char *check_cache(const sla_cache_t *c) {
     if ((int64_t)c->n_pages * c->page_tokens > 4294967295LL) return "n_pages * page_tokens above 2^32 - 1";
     if (c->n_kv_heads > 65536) return "n_kv_heads above 65536";
     if ((int64_t)c->table_width * c->page_tokens > 2147483647LL - 1024) return "table_width * page_tokens above 2^31 - 1025";
-    if (c->dtype != SLA_F32 && c->dtype != SLA_BF16) return "dtype must be SLA_F32 or SLA_BF16";
+    if (c->dtype != SLA_F32 && c->dtype != SLA_BF16 && !four_bits(c)) return "dtype must be SLA_F32, SLA_BF16, SLA_Q4 or SLA_Q4_F32";
     if (c->reserved != 0) return "reserved must be 0";
-    for (int64_t s : {c->stride_page, c->stride_h, c->stride_t})
+    if (four_bits(c)) {
+        const int64_t plane = sla::q4::plane_bytes(c->page_tokens, c->head_dim);
+        for (int64_t s : {c->stride_page, c->stride_h})
+            if (s < 0 || s % 16 || s > ((int64_t)1 << 41)) return "strides of a cache in four bits must be non-negative multiples of 16 bytes";
+        if ((c->n_kv_heads > 1 && c->stride_h < plane) || (c->n_pages > 1 && c->stride_page < plane)) return "a cache stride is below a plane's bytes";
+        if (c->stride_t != 0) return "stride_t of a cache in four bits must be 0";
+    } else for (int64_t s : {c->stride_page, c->stride_h, c->stride_t})
         if (s < 0 || s % 8 || s > ((int64_t)1 << 40)) return "cache strides must be non-negative multiples of 8 elements";
-    if (c->stride_t < c->head_dim || (c->n_kv_heads > 1 && c->stride_h < c->head_dim) || (c->n_pages > 1 && c->stride_page < c->head_dim))
+    if (!four_bits(c) && (c->stride_t < c->head_dim || (c->n_kv_heads > 1 && c->stride_h < c->head_dim) || (c->n_pages > 1 && c->stride_page < c->head_dim)))
         return "a cache stride is below head_dim";
     if (!c->k || !c->v || !c->table || !c->n_tokens || !c->ref) return "NULL pointer in the cache";
     if (!aligned16(c->k) || !aligned16(c->v)) return "k and v must be 16-byte aligned";
@@ -853,7 +864,7 @@ sla::Pages make_pages(sla_handle_t h, const sla_cache_t *c) {
     p.n_pages = c->n_pages; p.P = c->page_tokens;
     p.shift = 0;
     while ((1 << p.shift) < p.P) ++p.shift;
-    p.Hkv = c->n_kv_heads; p.D = c->head_dim; p.es = (int)elem_size(c->dtype);
+    p.Hkv = c->n_kv_heads; p.D = c->head_dim; p.es = four_bits(c) ? 1 : (int)elem_size(c->dtype);
     p.n_slots = c->n_slots; p.width = c->table_width;
     p.s_page = c->stride_page; p.s_h = c->stride_h; p.s_t = c->stride_t;
     p.status = h ? reinterpret_cast<int *>(h->ws) : nullptr;
@@ -901,9 +912,10 @@ size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_
         for (float scale : {1.f, -1.f}) {
             a.b = {n_seqs, n_new, longest_chunk(n_new, most), 0, nullptr, nullptr};
             a.scale = scale;
-            const size_t bytes = sla::plan_paged(a, c->dtype, 160).bytes;
+            const size_t bytes = sla::plan_paged(a, tensor_type(c), 160).bytes;
             if (bytes > need) need = bytes;
         }
+    if (p && four_bits(c)) return 0;   // no span decode step over it
     if (p && n_seqs > 0) {
         const sla_layout_t l = layout_of(c, n_q_heads, n_seqs, c->head_dim * (int64_t)n_q_heads, c->head_dim);
         const size_t bytes = sla_workspace_bytes(&l, p, 1, (int64_t)c->table_width * c->page_tokens);
@@ -937,9 +949,30 @@ sla_status_t sla_cache_append(sla_handle_t h, const sla_cache_t *c, const sla_ba
     if (!aligned16(k_new) || !aligned16(v_new)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");
     if (new_stride_t < 0 || new_stride_t % 8 || new_stride_h < 0 || new_stride_h % 8)
         return fail(h, SLA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements%s");
-    cudaError_t e = sla::launch_cache_append(make_pages(h, c), make_batch(b), first, k_new, v_new, new_stride_t, new_stride_h, h->sm_count,
-                                             static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const sla::Pages p = make_pages(h, c);
+    cudaError_t e = four_bits(c) ? sla::launch_append_q4(p, make_batch(b), first, tensor_type(c) == SLA_F32, k_new, v_new, new_stride_t, new_stride_h, h->sm_count, st)
+                                 : sla::launch_cache_append(p, make_batch(b), first, k_new, v_new, new_stride_t, new_stride_h, h->sm_count, st);
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_append");
+    h->launches += 1;
+    return SLA_OK;
+}
+
+sla_status_t sla_cache_read(sla_handle_t h, const sla_cache_t *c, const sla_batch_t *b, const int32_t *first, void *k_out,
+                            void *v_out, int64_t out_stride_t, int64_t out_stride_h, void *stream) {
+    if (!h) return SLA_ERR_INVALID_ARG;
+    if (const char *why = check_batch(b)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (sla_status_t s = cache_call(h, c, 0)) return s;
+    if (b->n_new == 0) return SLA_OK;
+    if (!k_out || !v_out) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
+    if (!aligned16(k_out) || !aligned16(v_out)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");
+    if (out_stride_t < 0 || out_stride_t % 8 || out_stride_h < 0 || out_stride_h % 8)
+        return fail(h, SLA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements%s");
+    if ((b->n_new > 1 && out_stride_t < c->head_dim) || (c->n_kv_heads > 1 && out_stride_h < c->head_dim))
+        return fail(h, SLA_ERR_INVALID_ARG, "token or head stride below head_dim%s");
+    cudaError_t e = sla::launch_cache_read(make_pages(h, c), make_batch(b), first, tensor_type(c) == SLA_F32, k_out, v_out, out_stride_t, out_stride_h,
+                                           h->sm_count, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_read");
     h->launches += 1;
     return SLA_OK;
 }
@@ -1019,11 +1052,11 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     a.q_sh = q_stride_h;
     a.scale = softmax_scale;
     a.expire = h->paged_expiry;
-    const sla::PagedPlan plan = sla::plan_paged(a, c->dtype, h->sm_count, h->canaries ? sla::Canaries::kBytes : 0);
+    const sla::PagedPlan plan = sla::plan_paged(a, tensor_type(c), h->sm_count, h->canaries ? sla::Canaries::kBytes : 0);
     if (plan.bytes > h->scratch_avail) return fail(h, SLA_ERR_WORKSPACE, "workspace too small for this call: ask sla_paged_workspace_bytes%s");
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = with_canaries(h, plan.canaries, st, [&] {
-        return sla::launch_paged_attention(q, a, c->dtype, plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, st, &h->launches);
+        return sla::launch_paged_attention(q, a, tensor_type(c), plan, h->ws + kHeaderBytes, reinterpret_cast<int *>(h->ws + kCounterOffset), out, lse, st, &h->launches);
     });
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_paged_attention");
     return SLA_OK;
@@ -1034,6 +1067,7 @@ sla_status_t sla_paged_decode_step(sla_handle_t h, const void *q_s, const void *
                                    void *out, float *lse, int32_t *out_anchor, float *out_score, void *stream) {
     if (!h) return SLA_ERR_INVALID_ARG;
     if (const char *why = check_cache(c)) return fail(h, SLA_ERR_INVALID_ARG, "%s", why);
+    if (four_bits(c)) return fail(h, SLA_ERR_UNSUPPORTED, "no span decode step over a cache in four bits: sla_paged_attention, or sla_cache_read and sla_decode_step%s");
     if (!b || b->n_seqs < 0 || b->reserved != 0) return fail(h, SLA_ERR_INVALID_ARG, "batch is NULL, or n_seqs < 0, or reserved not 0%s");
     if (b->n_seqs == 0) return SLA_OK;
     if (n_q_heads <= 0 || n_q_heads % c->n_kv_heads) return fail(h, SLA_ERR_INVALID_ARG, "n_q_heads must be a positive multiple of n_kv_heads%s");

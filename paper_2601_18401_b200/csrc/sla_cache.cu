@@ -11,7 +11,7 @@
 // heads, D 128, bf16): extend and append of a token to each of 48 sequences 7.4 us, of 18.7 thousand tokens to 3 sequences 33 us (153 MB
 // moved, 23 us at the rate of a copy); 6 sequences forked to 48 9.4 us; a pool of 1 GB whose holes take 304 MB compacted in 114 us, 94 of
 // them the copies at 6.5 TB/s.
-#include "sla_paged.cuh"
+#include "sla_q4.cuh"
 
 namespace sla {
 
@@ -222,6 +222,15 @@ struct PageShape {
 };
 __host__ __device__ inline PageShape page_shape(const Pages &p) {
     PageShape f;
+    if (q4::is(p)) {   // a plane of each head
+        f.per_row = q4::plane_bytes(p.P, p.D) / 16;
+        f.chunks = p.Hkv * f.per_row;
+        f.inner = p.Hkv;
+        f.s_inner = p.s_h;
+        f.s_outer = 0;
+        f.dense = p.s_h == f.per_row * 16ll || p.Hkv == 1;
+        return f;
+    }
     f.per_row = p.D * p.es / 16;
     f.chunks = p.Hkv * p.P * f.per_row;
     const bool head_inner = p.Hkv > 1 && p.s_h < p.s_t;

@@ -11,9 +11,9 @@ struct Pages {
     char *k, *v;
     int *table, *n_tokens, *ref;
     int n_pages, P, shift;          // page_tokens = P = 1 << shift
-    int Hkv, D, es;                 // es: bytes of an element
+    int Hkv, D, es;                 // es: bytes of an element; 1: a cache in four bits (sla_q4.cuh), s_t unused
     int n_slots, width;
-    long long s_page, s_h, s_t;     // in elements
+    long long s_page, s_h, s_t;     // in elements (four bits: in bytes)
     int *status;
 };
 
@@ -23,6 +23,9 @@ struct Batch {
     int slot0;                      // 0 where seq is not NULL
     const int *seq, *cu;            // either may be NULL (slots slot0 .. slot0 + n_seqs - 1; one token a sequence)
 };
+
+// Bytes of a row of k or v, with its scales where it has some.
+__host__ __device__ __forceinline__ int row_bytes(const Pages &p) { return p.es == 1 ? p.D / 2 + p.D / 16 : p.D * p.es; }
 
 // Rows [lo, hi) of sequence x in the call's tensors, kept inside them whatever cu_new holds.
 __device__ __forceinline__ void new_rows(const Batch &b, int x, int &lo, int &hi) {
@@ -68,6 +71,10 @@ CacheScratch plan_cache(const Pages &p, int n_seqs, size_t gap = 0);   // gap: b
 cudaError_t launch_cache_extend(const Pages &p, const Batch &b, int *first, const CacheScratch &s, char *scratch, cudaStream_t st);
 cudaError_t launch_cache_append(const Pages &p, const Batch &b, const int *first, const void *k_new, const void *v_new,
                                 long long s_t, long long s_h, int sm_count, cudaStream_t st);
+cudaError_t launch_append_q4(const Pages &p, const Batch &b, const int *first, bool f32, const void *k_new, const void *v_new,
+                             long long s_t, long long s_h, int sm_count, cudaStream_t st);   // (sla_q4.cu)
+cudaError_t launch_cache_read(const Pages &p, const Batch &b, const int *first, bool f32, void *k_out, void *v_out, long long s_t,
+                              long long s_h, int sm_count, cudaStream_t st);
 cudaError_t launch_cache_release(const Pages &p, const int *seq, int n, cudaStream_t st);
 cudaError_t launch_cache_fork(const Pages &p, const int *src, const int *dst, int n, int *pairs, const CacheScratch &s, char *scratch, cudaStream_t st);
 cudaError_t launch_cache_compact(const Pages &p, int *pairs, const CacheScratch &s, char *scratch, int sm_count, cudaStream_t st);
@@ -233,7 +240,7 @@ __device__ inline void build_plan(const PagedCall &a, const Shape &f, int n_ctas
             }
             if (lane == src) {
                 total = sum;
-                reread += (long long)n * a.c.Hkv * a.c.D * a.c.es * 2;
+                reread += (long long)n * a.c.Hkv * row_bytes(a.c) * 2;
             }
         }
         if (on) plan.seq_at[x + 1] = total * a.c.Hkv;

@@ -10,7 +10,10 @@
 // 883 us.  Single rows of fp32 FMA reach 75 TFLOP/s; tf32 tensor products were not taken: they round the inputs to 11 bits.
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "sla_paged_attn.h"
+#include "sla_q4.cuh"
 
 namespace sla {
 
@@ -85,13 +88,14 @@ __device__ __forceinline__ unsigned long long fma_pair(unsigned long long a, uns
     return d;
 }
 
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool kQ4>
 __global__ void __launch_bounds__(kRowThreads, (kRowCtas<D, R>))
 paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts, T *__restrict__ out, float *__restrict__ lse) {
     constexpr int KT = kRowKeys, kShift = 6;
     constexpr int RT = R / 16, RP = RT / 2, CT = KT / 16, DT = D / 16;   // rows, pairs of rows, keys, dimensions of a thread
     constexpr int KS = D + 4, PS = R + 4;   // (padded against bank conflicts)
-    constexpr int E = Vec16<T>::kElems, kLoads = KT * D / E / kRowThreads;   // 16-byte pieces of a tile per thread
+    constexpr int E = kQ4 ? 8 : Vec16<T>::kElems, kLoads = KT * D / E / kRowThreads;   // pieces of a tile per thread: 16 bytes, or 8 codes and their scale
+    constexpr int QE = Vec16<T>::kElems;
     static_assert(RT % 4 == 0, "rows of a thread come in 16-byte loads");
     extern __shared__ float4 row_sm[];
     float *sq = reinterpret_cast<float *>(row_sm), *sk = sq + D * R, *sv = sk + KT * KS, *sp = sv + KT * D;   // [D][R], [KT][KS], [KT][D], [KT][PS]
@@ -114,21 +118,31 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
             const int keys_end = min(s.n, s.n - s.q + s.t1);
             const int *table = a.c.table + (long long)max(s.slot, 0) * a.c.width;
             const long long head_at = s.head * a.c.s_h;
-            // pieces of a tile: piece c is 16 bytes of key c / (D / E)
-            uint4 raw[kLoads];
+            // pieces of a tile: piece c is E values of key c / (D / E)
+            using Raw = typename std::conditional<kQ4, uint2, uint4>::type;
+            Raw raw[kLoads];
             auto fetch = [&](const char *pool, int tile) {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int c = tid + i * kRowThreads, j = tile * KT + c / (D / E), d = (c % (D / E)) * E;
-                    raw[i] = make_uint4(0, 0, 0, 0);
-                    if (j < keys_end) {
+                    raw[i] = Raw{};
+                    if (j >= keys_end) continue;
+                    if constexpr (kQ4) {
+                        const char *plane = pool + valid_page(a.c, __ldg(table + (j >> a.c.shift))) * a.c.s_page + head_at;
+                        if (pool == a.c.k) q4::load_piece<false>(plane, a.c.P, D, j & (a.c.P - 1), d / 8, raw[i].x, raw[i].y);
+                        else q4::load_piece<true>(plane, a.c.P, D, j & (a.c.P - 1), d / 8, raw[i].x, raw[i].y);
+                    } else {
                         const long long at = valid_page(a.c, __ldg(table + (j >> a.c.shift))) * a.c.s_page + head_at + (j & (a.c.P - 1)) * a.c.s_t + d;
                         raw[i] = __ldg(reinterpret_cast<const uint4 *>(pool + at * sizeof(T)));
                     }
                 }
             };
-            auto widen = [&](const uint4 &v, float (&f)[E]) {
-                if constexpr (sizeof(T) == 2) {
+            auto widen = [&](const Raw &v, float (&f)[E]) {
+                if constexpr (kQ4) {
+                    uint32_t w[4];
+                    q4::values(v.x, q4::factor(v.y), w);
+                    Vec16<__nv_bfloat16>::unpack(make_uint4(w[0], w[1], w[2], w[3]), f);
+                } else if constexpr (sizeof(T) == 2) {
                     Vec16<__nv_bfloat16>::unpack(v, f);
                 } else {
                     f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
@@ -136,14 +150,14 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
             };
             if (s.lo < s.hi) fetch(a.c.k, s.lo);
             __syncthreads();   // shared memory of the segment before has been read
-            for (int c = tid; c < R * (D / E); c += kRowThreads) {
-                const int i = c % R, d = (c / R) * E, t = i / G, g = i - t * G;   // neighbouring threads, neighbouring rows: no conflicts
-                float f[E];
+            for (int c = tid; c < R * (D / QE); c += kRowThreads) {
+                const int i = c % R, d = (c / R) * QE, t = i / G, g = i - t * G;   // neighbouring threads, neighbouring rows: no conflicts
+                float f[QE];
 #pragma unroll
-                for (int e = 0; e < E; ++e) f[e] = 0.f;
+                for (int e = 0; e < QE; ++e) f[e] = 0.f;
                 if (i < rows) Vec16<T>::load(q + (long long)(s.row0 + s.t0 + t) * a.q_st + (long long)(s.head * G + g) * a.q_sh + d, f);
 #pragma unroll
-                for (int e = 0; e < E; ++e) sq[(d + e) * R + i] = f[e] * scale2;
+                for (int e = 0; e < QE; ++e) sq[(d + e) * R + i] = f[e] * scale2;
             }
             if (tid < R) s_pos[tid] = tid < rows ? s.n - s.q + s.t0 + tid / G : -1;
             // keys that every row of the unit sees; a row sees [position - window + 1, position]
@@ -288,10 +302,13 @@ paged_rows(const T *__restrict__ q, PagedCall a, int TQ, Plan plan, Parts parts,
 #pragma unroll 1
                     for (int jj = 0; jj < KT && j0 + jj < keys_end; ++jj) {
                         const int j = j0 + jj;
-                        const long long at = valid_page(a.c, table[j >> a.c.shift]) * a.c.s_page + head_at + (j & (a.c.P - 1)) * a.c.s_t;
+                        const long long plane = valid_page(a.c, table[j >> a.c.shift]) * a.c.s_page + head_at, at = plane + (j & (a.c.P - 1)) * a.c.s_t;
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
-                            const float v = (float)(reinterpret_cast<const T *>(a.c.v) + at)[(d / 4) * 64 + tx * 4 + d % 4];
+                            const int dim = (d / 4) * 64 + tx * 4 + d % 4;
+                            float v;   // (of a four-bit cache: whether it is finite, which its scale says)
+                            if constexpr (kQ4) v = __uint_as_float(q4::scale_of(a.c.v + plane, a.c.P, D, j & (a.c.P - 1), dim) << 16);
+                            else v = (float)(reinterpret_cast<const T *>(a.c.v) + at)[dim];
                             if (fabsf(v) <= 3.4028235e38f) continue;
 #pragma unroll
                             for (int r = 0; r < RP; ++r) {
@@ -413,18 +430,18 @@ __global__ void __launch_bounds__(kMergeThreads, 4) paged_merge(PagedCall a, int
     if (d0 == 0) lse[row * a.Hq + h] = none ? -CUDART_INF_F : (mx + log2f(sum)) * kLn2;
 }
 
-template <typename T, int D, int R>
+template <typename T, int D, int R, bool kQ4>
 cudaError_t run_rows(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
     static bool allowed[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !allowed[dev]) {
-        e = cudaFuncSetAttribute(paged_rows<T, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem<D, R>);
+        e = cudaFuncSetAttribute(paged_rows<T, D, R, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem<D, R>);
         if (e != cudaSuccess) return e;
         if (dev < 64) allowed[dev] = true;
     }
-    return launch_chained(paged_rows<T, D, R>, dim3(p.n_ctas), dim3(kRowThreads), (kRowSmem<D, R>), st, (const T *)q, a, p.TQ,
+    return launch_chained(paged_rows<T, D, R, kQ4>, dim3(p.n_ctas), dim3(kRowThreads), (kRowSmem<D, R>), st, (const T *)q, a, p.TQ,
                           plan_at(p, scratch), parts_at(p, scratch), (T *)out, lse);
 }
 
@@ -493,6 +510,16 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap) {
     return p;
 }
 
+template <typename T, int D, bool kQ4>
+static cudaError_t rows_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
+    return p.R == 64 ? run_rows<T, D, 64, kQ4>(q, a, p, scratch, out, lse, st) : run_rows<T, D, 128, kQ4>(q, a, p, scratch, out, lse, st);
+}
+template <bool kQ4>
+static cudaError_t rows_for(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
+    if (dtype == SLA_F32) return a.c.D == 64 ? rows_of<float, 64, kQ4>(q, a, p, scratch, out, lse, st) : rows_of<float, 128, kQ4>(q, a, p, scratch, out, lse, st);
+    return a.c.D == 64 ? rows_of<__nv_bfloat16, 64, kQ4>(q, a, p, scratch, out, lse, st) : rows_of<__nv_bfloat16, 128, kQ4>(q, a, p, scratch, out, lse, st);
+}
+
 cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                    float *lse, cudaStream_t st, long long *launches) {
     if (p.kind == PagedPlan::kDecode) return launch_paged_decode_attention(q, a, dtype, p, scratch, counters, out, lse, st, launches);
@@ -500,13 +527,7 @@ cudaError_t launch_paged_attention(const void *q, const PagedCall &a, int dtype,
     if (e == cudaSuccess && p.kind == PagedPlan::kTiles) {
         e = launch_paged_tiles(q, a, p, scratch, out, lse, st);
     } else if (e == cudaSuccess) {
-        if (dtype == SLA_F32) {
-            if (a.c.D == 64) e = p.R == 64 ? run_rows<float, 64, 64>(q, a, p, scratch, out, lse, st) : run_rows<float, 64, 128>(q, a, p, scratch, out, lse, st);
-            else e = p.R == 64 ? run_rows<float, 128, 64>(q, a, p, scratch, out, lse, st) : run_rows<float, 128, 128>(q, a, p, scratch, out, lse, st);
-        } else {
-            if (a.c.D == 64) e = p.R == 64 ? run_rows<__nv_bfloat16, 64, 64>(q, a, p, scratch, out, lse, st) : run_rows<__nv_bfloat16, 64, 128>(q, a, p, scratch, out, lse, st);
-            else e = p.R == 64 ? run_rows<__nv_bfloat16, 128, 64>(q, a, p, scratch, out, lse, st) : run_rows<__nv_bfloat16, 128, 128>(q, a, p, scratch, out, lse, st);
-        }
+        e = q4::is(a.c) ? rows_for<true>(q, a, dtype, p, scratch, out, lse, st) : rows_for<false>(q, a, dtype, p, scratch, out, lse, st);
     }
     if (e == cudaSuccess) e = launch_paged_merge(a, dtype, p, scratch, out, lse, st);
     if (e == cudaSuccess) *launches += 3;

@@ -614,7 +614,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
 
 }  // namespace
 
-bool paged_decode_supported(const PagedCall &a) { return (long long)a.b.max_new * a.G <= 16; }
+bool paged_decode_supported(const PagedCall &a) { return a.c.es != 1 && (long long)a.b.max_new * a.G <= 16; }
 
 void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.R = p.RS = 16;

@@ -1001,7 +1001,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
 // bf16, strides that nest in memory (no broadcast views), a scale that keeps the order of the logits and -inf what it is
 bool paged_tiles_supported(const PagedCall &a, int dtype) {
     Dim kd[3], qd[2];
-    return dtype == SLA_BF16 && a.scale > 0.f && kv_dims(a, kd) && q_dims(a, qd);
+    return a.c.es != 1 && dtype == SLA_BF16 && a.scale > 0.f && kv_dims(a, kd) && q_dims(a, qd);
 }
 
 void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
@@ -1014,7 +1014,7 @@ void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.n_ctas = sm_count;
     // (a bound that does not ask the number of SMs, so that the workspace can be sized without a device)
     const long long units = a.b.n_new / p.TQ + a.b.n_seqs, weight = units * a.c.Hkv * (((long long)a.c.width << a.c.shift) / kKeys + 1 + kUnitWeight);
-    const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * a.c.D * a.c.es * 2, groups = bytes / kGroupBytes + 1;
+    const long long bytes = (long long)a.c.n_pages * a.c.P * a.c.Hkv * row_bytes(a.c) * 2, groups = bytes / kGroupBytes + 1;
     const long long most = groups < weight / (128 * kGroupWeight) ? groups : weight / (128 * kGroupWeight);
     p.max_groups = most < 1 ? 1 : most < 8 ? (int)most : 8;
     p.min_weight = 3;

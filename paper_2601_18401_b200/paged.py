@@ -17,15 +17,22 @@ class PagedCache:
 
     def __init__(self, n_pages: int, n_slots: int, max_tokens: int, *, n_q_heads: int, n_kv_heads: int, head_dim: int = 128,
                  page_tokens: int = 64, dtype: torch.dtype = torch.bfloat16, device: int = 0, max_batch: Optional[int] = None,
-                 max_new: int = 8192, params: Optional[B.sla_params_t] = None, share: Optional["PagedCache"] = None):
-        """max_batch, max_new: the most sequences and new tokens of one call (they size the workspace); params: of the span decode
+                 max_new: int = 8192, params: Optional[B.sla_params_t] = None, share: Optional["PagedCache"] = None,
+                 four_bits: bool = False):
+        """four_bits: keys and values are rounded to four bits as they are appended (dtype is then that of the calls' tensors), and there is
+        no span decode step.  max_batch, max_new: the most sequences and new tokens of one call (they size the workspace); params: of the span decode
         step, when it is used.  share: the cache of another layer, whose table, lengths, counts, handle (a workspace for that layer's
         heads) and, where they are not given, params this one uses; pages, slots and lengths have to be the same."""
         dev = torch.device("cuda", device)
         width = -(-max_tokens // page_tokens)
-        if share is not None and (share.k.shape[0], share.k.shape[2], *share.table.shape) != (n_pages, page_tokens, n_slots, width):
+        if share is not None and (share.k.shape[0], share.cache.page_tokens, *share.table.shape) != (n_pages, page_tokens, n_slots, width):
             raise ValueError("layers that share a table must have the same pages, page_tokens, slots and max_tokens")
-        self.k = torch.empty(n_pages, n_kv_heads, page_tokens, head_dim, dtype=dtype, device=dev)
+        if four_bits and params is not None:
+            raise ValueError("no span decode step over a cache in four bits: params must be None")
+        if four_bits:
+            self.k = torch.empty(n_pages, n_kv_heads, B.q4_plane_bytes(page_tokens, head_dim), dtype=torch.uint8, device=dev)
+        else:
+            self.k = torch.empty(n_pages, n_kv_heads, page_tokens, head_dim, dtype=dtype, device=dev)
         self.v = torch.empty_like(self.k)
         if share is None:
             self.table = torch.full((n_slots, width), -1, dtype=torch.int32, device=dev)
@@ -33,7 +40,11 @@ class PagedCache:
             self.ref = torch.zeros(n_pages, dtype=torch.int32, device=dev)
         else:
             self.table, self.n_tokens, self.ref = share.table, share.n_tokens, share.ref
-        self.cache = B.make_cache(self.k, self.v, self.table, self.n_tokens, self.ref)
+        if four_bits:
+            self.cache = B.make_cache_q4(self.k, self.v, self.table, self.n_tokens, self.ref, page_tokens=page_tokens, head_dim=head_dim,
+                                         dtype=dtype)
+        else:
+            self.cache = B.make_cache(self.k, self.v, self.table, self.n_tokens, self.ref)
         self.params = share.params if params is None and share is not None else params
         if share is None:
             need = B.sla_paged_workspace_bytes(self.cache, n_q_heads, max_batch or n_slots, max_new, params=params)
@@ -49,6 +60,10 @@ class PagedCache:
 
     def append(self, cu_new, first, k_new, v_new, *, seq=None):
         B.sla_cache_append(self.handle, self.cache, cu_new, first, k_new, v_new, seq=seq)
+
+    def read(self, cu_new=None, first=None, *, n_new=None, seq=None, k_out=None, v_out=None):
+        """Keys and values of the positions first[x] .. (None: 0 ..) of the sequences -> k, v [n_new, Hkv, D]."""
+        return B.sla_cache_read(self.handle, self.cache, cu_new, first, n_new=n_new, seq=seq, k_out=k_out, v_out=v_out)
 
     def attend(self, q, cu_new=None, *, seq=None, max_new=None, window=0, softmax_scale=None, first=None):
         """Dense causal attention of the new tokens -> out, lse.  first: of `extend`; refused sequences then give 0 and -inf."""
