@@ -478,7 +478,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap) {
     p.min_weight = 2;
     p.small = 0;
     p.fold_bytes = 0;
-    if (paged_decode_supported(a)) {
+    if (paged_decode_supported(a, dtype)) {
         p.kind = PagedPlan::kDecode;
         plan_paged_decode(a, p, sm_count);
     } else if (paged_tiles_supported(a, dtype)) {

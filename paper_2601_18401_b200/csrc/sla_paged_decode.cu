@@ -33,16 +33,22 @@
 #include <math_constants.h>
 
 #include "sla_paged_attn.h"
+#include "sla_q4_decode.cuh"
 
 namespace sla {
 
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-// resident CTAs an SM: two where 16 heads of 128 dimensions fill the registers
-__host__ __device__ constexpr int ctas_per_sm(int D, int NT) { return D == 128 && NT == 2 ? 2 : 3; }
+// resident CTAs an SM: two where 16 heads of 128 dimensions fill the registers; over a cache in four bits
+#ifndef Q4C1
+#define Q4C1 3
+#define Q4C2 2
+#endif
+__host__ __device__ constexpr int ctas_per_sm(int D, int NT, bool q4) { return q4 ? (NT == 2 ? Q4C2 : Q4C1) : D == 128 && NT == 2 ? 2 : 3; }
 // sequences of a launch: as many as there is room for (16 bytes each) beside the kernel's arrays in 48 KB
-template <typename T> constexpr int max_seqs(int D, int NT) {
+template <typename T, bool kQ4> constexpr int max_seqs(int D, int NT) {
+    if (kQ4) return 1024;   // (its arrays are dynamic too)
     const int arrays = kWarps * 8 * NT * (D + 2) * 4 + (sizeof(T) == 4 ? D * 8 * NT * 4 : 16) + 128, room = (48 * 1024 - arrays) / 16 - 1;
     return room < 1024 ? room : 1024;
 }
@@ -422,19 +428,24 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
     }
 }
 
-template <typename T, int D, int NT, bool kTok>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT))
+template <typename T, int D, int NT, bool kTok, bool kQ4>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kQ4))
 paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
              T *__restrict__ out, float *__restrict__ lse) {
     constexpr int R = 16;                 // rows of a partial result
-    __shared__ alignas(16) float s_o[kWarps][8 * NT][D];
+    // a warp's sums [8 NT][D]; over a cache in four bits they lie over its ring of stages
+    extern __shared__ __align__(128) char dyn_sm[];
+    constexpr int kRing = kQ4 ? q4::ring_bytes(D) : 0, kSums = kQ4 ? kRing / 4 : 8 * NT * D;
+    static_assert(kSums >= 8 * NT * D, "the sums fit into the ring");
+    __shared__ alignas(16) float s_sums[kQ4 ? 4 : kWarps * kSums];
+    float *s_o = kQ4 ? reinterpret_cast<float *>(dyn_sm) : s_sums;
     __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
     __shared__ long long s_scan[kWarps];
     __shared__ int s_last;
-    extern __shared__ long long s_seq_at[];   // [n_seqs + 1] weight before a sequence; then its tokens and its slot
+    long long *s_seq_at = reinterpret_cast<long long *>(dyn_sm + kWarps * kRing);   // [n_seqs + 1] weight before a sequence; then its tokens and its slot
     int *s_n = reinterpret_cast<int *>(s_seq_at + n_seqs + 1), *s_slot = s_n + n_seqs;
     constexpr bool kF32 = sizeof(T) == 4;
-    constexpr int kStep = kF32 ? 32 : 16;   // keys of a warp's step
+    constexpr int kStep = kF32 || kQ4 ? 32 : 16;   // keys of a warp's step
     __shared__ alignas(16) float s_q[kF32 ? D * 8 * NT : 4];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.G;
@@ -509,7 +520,9 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
         const int key = max((lo + max(from - kUnitWeight, 0)) << kTileShift, first & ~(kStep - 1));
         const int key_end = min((lo + max(to - kUnitWeight, 0)) << kTileShift, n);
         const Walk walk = {key + kStep * warp, key_end, first, n, head, row_q, a.c.table + (long long)max(s_slot[x], 0) * a.c.width, q_x, rows, window, all_first, all_n};
-        if constexpr (kF32) {
+        if constexpr (kQ4) {
+            q4::attend<D, NT, kTok, kWarps>(q, a, walk, ptx::smem_u32(dyn_sm) + warp * kRing, s_m[warp], s_l[warp], s_o + warp * kSums);
+        } else if constexpr (kF32) {
             // (s_q: the segment before has been joined)
             for (int c = tid; c < D * 8 * NT; c += kThreads) {
                 const int h = c / D, d = c % D;   // neighbouring threads, neighbouring dimensions
@@ -517,9 +530,9 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                 s_q[d * 8 * NT + h] = h < rows ? q[(long long)(row_q + tok) * a.q_st + (long long)(head * G + h - tok * G) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
             }
             __syncthreads();
-            attend_f32<D, NT, kTok>(a, walk, s_q, s_m[warp], s_l[warp], &s_o[warp][0][0]);
+            attend_f32<D, NT, kTok>(a, walk, s_q, s_m[warp], s_l[warp], s_o + warp * kSums);
         } else {
-            attend_bf16<D, NT, kTok>(q, a, walk, s_m[warp], s_l[warp], &s_o[warp][0][0]);
+            attend_bf16<D, NT, kTok>(q, a, walk, s_m[warp], s_l[warp], s_o + warp * kSums);
         }
         __syncthreads();
         const bool begins = from == 0, ends = w_end >= stop;
@@ -535,7 +548,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                 const float wt = s_m[v][qi] == -CUDART_INF_F && s_l[v][qi] == 0.f ? 0.f : exp2_fast(s_m[v][qi] - (mx == -CUDART_INF_F ? 0.f : mx));
                 // a warp without a key has no weight; one whose only logits are NaN carries them in its sum
                 const float wv = s_m[v][qi] == -CUDART_INF_F && !(s_l[v][qi] == 0.f) ? 1.f : wt;
-                const float4 ov = *reinterpret_cast<const float4 *>(&s_o[v][qi][d]);
+                const float4 ov = *reinterpret_cast<const float4 *>(s_o + v * kSums + qi * D + d);
                 sum = fmaf(wv, s_l[v][qi], sum);
                 o[0] = fmaf(wv, ov.x, o[0]); o[1] = fmaf(wv, ov.y, o[1]); o[2] = fmaf(wv, ov.z, o[2]); o[3] = fmaf(wv, ov.w, o[3]);
             }
@@ -614,43 +627,56 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
 
 }  // namespace
 
-bool paged_decode_supported(const PagedCall &a) { return a.c.es != 1 && (long long)a.b.max_new * a.G <= 16; }
+bool paged_decode_supported(const PagedCall &a, int dtype) { return (long long)a.b.max_new * a.G <= 16 && !(q4::is(a.c) && dtype == SLA_F32); }
 
 void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.R = p.RS = 16;
     p.TS = p.TQ = 1;
-    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2) * sm_count;
+    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2, q4::is(a.c)) * sm_count;
 }
 
-template <typename T, int D, int NT, bool kTok>
+template <typename T, int D, int NT, bool kTok, bool kQ4>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
-    constexpr int kMost = max_seqs<T>(D, NT);
+    constexpr size_t kRing = kQ4 ? kWarps * q4::ring_bytes(D) : 0;
+    if (kQ4) {
+        static bool allowed[64] = {};
+        int dev = 0;
+        e = cudaGetDevice(&dev);
+        if (e == cudaSuccess && (dev >= 64 || !allowed[dev])) {
+            e = cudaFuncSetAttribute(paged_decode<T, D, NT, kTok, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRing + 1025 * 16);
+            if (e == cudaSuccess && dev < 64) allowed[dev] = true;
+        }
+    }
+    constexpr int kMost = max_seqs<T, kQ4>(D, NT);
     for (int x0 = 0; x0 < a.b.n_seqs && e == cudaSuccess; x0 += kMost) {
         const int n = a.b.n_seqs - x0 < kMost ? a.b.n_seqs - x0 : kMost;
-        e = launch_chained(paged_decode<T, D, NT, kTok>, dim3(p.n_ctas), dim3(kThreads), (size_t)(n + 1) * 8 + (size_t)n * 8, st,
+        e = launch_chained(paged_decode<T, D, NT, kTok, kQ4>, dim3(p.n_ctas), dim3(kThreads), kRing + (size_t)(n + 1) * 8 + (size_t)n * 8, st,
                            (const T *)q, a, x0, n, parts_at(p, scratch), counters, (T *)out, lse);
         ++*launches;
     }
     return e;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kQ4>
 static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                               cudaStream_t st, long long *launches) {
     const bool small = a.b.max_new * a.G <= 8;
     if (a.b.max_new == 1)
-        return small ? decode_of<T, D, 1, false>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, false>(q, a, p, scratch, counters, out, lse, st, launches);
-    return small ? decode_of<T, D, 1, true>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, true>(q, a, p, scratch, counters, out, lse, st, launches);
+        return small ? decode_of<T, D, 1, false, kQ4>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, false, kQ4>(q, a, p, scratch, counters, out, lse, st, launches);
+    return small ? decode_of<T, D, 1, true, kQ4>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, true, kQ4>(q, a, p, scratch, counters, out, lse, st, launches);
 }
 
 cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches) {
     if (dtype == SLA_F32)
-        return a.c.D == 64 ? decode_for<float, 64>(q, a, p, scratch, counters, out, lse, st, launches) : decode_for<float, 128>(q, a, p, scratch, counters, out, lse, st, launches);
-    return a.c.D == 64 ? decode_for<__nv_bfloat16, 64>(q, a, p, scratch, counters, out, lse, st, launches)
-                       : decode_for<__nv_bfloat16, 128>(q, a, p, scratch, counters, out, lse, st, launches);
+        return a.c.D == 64 ? decode_for<float, 64, false>(q, a, p, scratch, counters, out, lse, st, launches) : decode_for<float, 128, false>(q, a, p, scratch, counters, out, lse, st, launches);
+    if (q4::is(a.c))
+        return a.c.D == 64 ? decode_for<__nv_bfloat16, 64, true>(q, a, p, scratch, counters, out, lse, st, launches)
+                           : decode_for<__nv_bfloat16, 128, true>(q, a, p, scratch, counters, out, lse, st, launches);
+    return a.c.D == 64 ? decode_for<__nv_bfloat16, 64, false>(q, a, p, scratch, counters, out, lse, st, launches)
+                       : decode_for<__nv_bfloat16, 128, false>(q, a, p, scratch, counters, out, lse, st, launches);
 }
 
 }  // namespace sla

@@ -1,0 +1,359 @@
+// Attention of a few rows over a range of keys of a cache in four bits, by a warp: what paged_decode (sla_paged_decode.cu) calls in the place of
+// attend_bf16.
+//
+// The codes go into mma.sync as the bf16 subnormals that q4::pairs makes of them, without their scales:
+//     S^T [16 keys, 8 rows] = sum over groups of (C_g Q_g^T) s,      O^T [16 dimensions of a group, 8 rows] += C^T (P s)^T.
+// A logit is the sum of four products of 32 dimensions, each times the scale of its group and key; a weight is multiplied by the scale of the
+// value's group and rounded to bf16 once, which is what rounding the weight alone costs.  So no value is ever formed, and eight
+// codes cost seven instructions.  P s goes through the 8 x 8 transpose (movmatrix) on its way into the second product.  (With the rows as
+// A, so that P stays where it is, half of A is empty for groups of 8 and less: twice the instructions of the first product, and 168 registers
+// instead of 128.)
+//
+// A cache in four bits brings a quarter of the bytes for the same work: what matters is how many instructions a key takes, and that no warp ever
+// waits for memory.  Every warp has a ring of stages of 32 keys in shared memory, which its lanes fill by asynchronous copies of 16
+// bytes: nine instructions a stage, since a plane's rows lie on end.  (With the pieces in registers, requested a step of 16 keys ahead, as
+// attend_bf16 has them, 32 sequences of 1000 to 65536 took 164 us.  Bulk copies take 40 instructions more a stage: their operands are
+// those of a warp, and each lane's copy goes on its own.)
+//
+// Powers of two: Q is multiplied by F, a power of two that brings its row's largest magnitude next to 2^100 (a sixteenth of it where codes
+// carry a factor of 16); logits are divided by F 2^-133.  Weights are 2^78 times what they are: 2^78 2^40 2^8 (the largest scale, the slack of
+// the running maximum) stays in the range of bf16, and products with subnormals down to 2^-133 2^78 2^-40 in that of fp32.
+#pragma once
+
+#include <math_constants.h>
+
+#include "sla_q4.cuh"
+#include "sla_tc_ptx.cuh"
+
+namespace sla {
+namespace q4 {
+
+// N words of shared memory, as wide as they are
+template <int N> __device__ __forceinline__ void load_shared(uint32_t at, uint32_t (&w)[N]) {
+    if constexpr (N == 1) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+    } else if constexpr (N == 2) {
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4 * i));
+    }
+}
+// d += A B, and d = A B
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma0(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ float half_of(uint32_t w, int i) { return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t y;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+    return y;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t transpose(uint32_t x) {   // of an 8 x 8 matrix of 16-bit numbers
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+constexpr float kLift = 78.f;    // log2 of what the weights are multiplied by
+constexpr int kKeys = 32;        // of a stage
+#ifndef Q4ST
+#define Q4ST 2
+#endif
+constexpr int kStages = Q4ST;
+__host__ __device__ constexpr int stage_bytes(int D) { return 2 * kKeys * (D / 2 + D / 16); }   // K codes, K scales, V codes, V scales
+__host__ __device__ constexpr int ring_bytes(int D) { return kStages * stage_bytes(D); }
+
+// 8 NT rows at most; Walk, w_m, w_l and w_o as for attend_bf16, w_o over the ring, but the warp takes 32 keys at a time.  A thread (g, c) = (lane / 4,
+// lane % 4) has of the products' operands (16 keys a step) the keys ka = 4 (g / 2) + g % 2 and kb = ka + 2 of K, S and P, row g of Q (and g + 8) and
+// the values of keys 4 c .. 4 c + 3.
+template <int D, int NT, bool kTok, int kWarps, typename Walk>
+__device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, const PagedCall &a, const Walk &wk, uint32_t ring, float *w_m, float *w_l, float *w_o) {
+    constexpr int N = D / 32, kStride = kKeys * kWarps, S = kKeys / 16, kHalf = 8 * D;   // kHalf: bytes of the codes of 16 rows
+    constexpr unsigned kAll = 0xffffffffu;
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int G = a.G, first = wk.first, n = wk.n, key_end = wk.key_end;
+
+    // A stage's keys lie in one page, or in two of 16 tokens: where the rows begin in k and in v, looked up a stage ahead of the copies.
+    const bool small = a.c.P < kKeys;
+    const int sl = lane % (D / 8);   // of the scales: 16 bytes a lane, K and then V
+    const char *const s_pool = (lane < D / 8 ? a.c.k : a.c.v) + wk.head * a.c.s_h + a.c.P * (D / 2) + sl * 16 - (small && sl >= D / 16 ? D : 0);
+    const char *const k_pool = a.c.k + wk.head * a.c.s_h + lane * 16, *const v_pool = a.c.v + wk.head * a.c.s_h + lane * 16;
+    const uint32_t s_to = ring + (lane < D / 8 ? 0 : stage_bytes(D) / 2) + kKeys * (D / 2) + sl * 16;
+    auto page_at = [&](int k) { return valid_page(a.c, __ldg(wk.table + (k >> a.c.shift))) * a.c.s_page; };
+    long long at0 = 0, at1 = 0;
+    auto find = [&](int k0) {
+        if (k0 >= key_end) return;
+        at0 = page_at(k0);
+        if (small) at1 = page_at(min(k0 + 16, n - 1));
+    };
+    auto fill = [&](int k0, uint32_t st) {
+        if (k0 < key_end) {
+            const int t0 = k0 & (a.c.P - 1);
+            const long long c0 = at0 + t0 * (D / 2), c1 = small ? at1 : c0 + kHalf;
+            const uint32_t to = ring + st * stage_bytes(D) + lane * 16;
+            const bool two = !small || k0 + 16 < n;   // what lies beyond n is not copied where it has a page of its own
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) {
+                ptx::cp_async16(to + j * 512, k_pool + c0 + j * 512);
+                ptx::cp_async16(to + stage_bytes(D) / 2 + j * 512, v_pool + c0 + j * 512);
+            }
+            if (two) {
+#pragma unroll
+                for (int j = 0; j < N / 2; ++j) {
+                    ptx::cp_async16(to + kHalf + j * 512, k_pool + c1 + j * 512);
+                    ptx::cp_async16(to + stage_bytes(D) / 2 + kHalf + j * 512, v_pool + c1 + j * 512);
+                }
+            }
+            if (lane < D / 4 && (two || sl < D / 16)) ptx::cp_async16(s_to + st * stage_bytes(D), s_pool + (small && sl >= D / 16 ? at1 : at0 + t0 * (D / 16)));
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int key = wk.key;
+#pragma unroll
+    for (int st = 0; st < kStages; ++st) {
+        find(key + st * kStride);
+        fill(key + st * kStride, st);
+    }
+    find(key + kStages * kStride);
+    // [t][e]: row 8 t + 2 c + e
+    float m[NT][2], l[NT][2], lim[NT][2], mult[NT][2], acc[NT][2 * N][4];
+    uint32_t qf[NT][N][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const bool on = 8 * t + g < (kTok ? wk.rows : G);
+        const int r = on ? 8 * t + g : 0, tok = kTok ? r / G : 0;
+        const __nv_bfloat16 *src = q + (long long)(wk.row_q + tok) * a.q_st + (long long)(wk.head * G + r - tok * G) * a.q_sh + c * 8;
+        uint32_t top = 0;
+#pragma unroll
+        for (int w = 0; w < N; ++w) {
+            const uint4 v = on ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * w)) : make_uint4(0, 0, 0, 0);
+            qf[t][w][0] = v.x; qf[t][w][1] = v.y; qf[t][w][2] = v.z; qf[t][w][3] = v.w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = __vmaxu2(top, qf[t][w][i] & 0x7fff7fffu);
+        }
+        top = max(top & 0xffffu, top >> 16);
+        top = max(top, __shfl_xor_sync(kAll, top, 1));
+        top = max(top, __shfl_xor_sync(kAll, top, 2));
+        // exponent of the row's largest magnitude, kept where F and 2^133 / F are numbers; F = 2^(100 - e)
+        const int e = min(max((int)(top >> 7) - 127, -27), 85);
+        const float f0 = __uint_as_float((uint32_t)(227 - e) << 23), f1 = __uint_as_float((uint32_t)(223 - e) << 23);
+#pragma unroll
+        for (int w = 0; w < N; ++w)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) qf[t][w][i] = pack(half_of(qf[t][w][i], 0) * (i & 1 ? f1 : f0), half_of(qf[t][w][i], 1) * (i & 1 ? f1 : f0));
+        const float back = a.scale * kLog2e * __uint_as_float((uint32_t)(160 + e) << 23);   // 2^(33 + e)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            mult[t][u] = __shfl_sync(kAll, back, 4 * (2 * c + u));
+            m[t][u] = lim[t][u] = -CUDART_INF_F;
+            l[t][u] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc[t][i][u] = 0.f;
+    }
+
+    const uint32_t ka = 4 * (g >> 1) + (g & 1);
+    const uint32_t k_at = ring + ka * (D / 2) + c * 4 * N;
+    const uint32_t v_at = ring + stage_bytes(D) / 2 + 4 * c * (D / 2) + g * 2 * N;
+    const uint32_t s_at = ring + kKeys * (D / 2) + ka * (D / 16);
+    uint32_t st = 0;
+#pragma unroll 1
+    for (; key < key_end; key += kStride) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();   // every lane's copies are there
+        const uint32_t of = st * stage_bytes(D);
+        float y[S][NT][4];   // [s][t][2 h + e]: key 16 s + ka + 2 h, row 8 t + 2 c + e
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            uint32_t kw[2][N], ks[2][N / 2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                load_shared(k_at + of + (16 * s + 2 * h) * (D / 2), kw[h]);
+                load_shared(s_at + of + (16 * s + 2 * h) * (D / 16), ks[h]);
+            }
+#pragma unroll
+            for (int w = 0; w < N; ++w) {
+                uint32_t ra[4], rb[4];
+                pairs(kw[0][w], ra);
+                pairs(kw[1][w], rb);
+                const float sa = half_of(ks[0][w >> 1], w), sb = half_of(ks[1][w >> 1], w);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float d[4];
+                    mma0(d, ra[0], rb[0], ra[1], rb[1], qf[t][w][0], qf[t][w][1]);
+                    mma(d, ra[2], rb[2], ra[3], rb[3], qf[t][w][2], qf[t][w][3]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) y[s][t][u] = w == 0 ? d[u] * (u < 2 ? sa : sb) : fmaf(d[u], u < 2 ? sa : sb, y[s][t][u]);
+                }
+            }
+        }
+        // a logit less what the row's weights are taken from, m - 78 (m: not below the largest so far but by 8; 0 for none)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float base = kLift - (m[t][u] == -CUDART_INF_F ? 0.f : m[t][u]);
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    y[s][t][u] = fmaf(y[s][t][u], mult[t][u], base);
+                    y[s][t][u + 2] = fmaf(y[s][t][u + 2], mult[t][u], base);
+                }
+            }
+        uint32_t vs[S][2][N / 2];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) load_shared(s_at + of + stage_bytes(D) / 2 + (16 * s + 2 * h) * (D / 16), vs[s][h]);
+        const bool edge = kTok ? key < wk.all_first || key + kKeys > wk.all_n : key < first || key + kKeys > n;
+        if (edge) {
+            uint32_t nan = 0;   // of the keys that some rows see and others do not: bit 8 s + 4 h + group
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int k = key + 16 * s + (int)ka + 2 * h;
+                    int lo = 0, hi = 8 * NT;
+                    if constexpr (kTok) wk.rows_of(k, G, lo, hi);
+                    if (k < first || k >= n) hi = 0;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            if (8 * t + 2 * c + u < lo || 8 * t + 2 * c + u >= hi) y[s][t][2 * h + u] = -CUDART_INF_F;
+                    const bool part = kTok && hi > 0 && (k < wk.all_first || k >= wk.all_n);
+#pragma unroll
+                    for (int w = 0; w < N; ++w) {
+                        const uint32_t mask = w & 1 ? 0xffff0000u : 0xffffu;
+                        const bool out = part && is_nan((w & 1 ? vs[s][h][w >> 1] >> 16 : vs[s][h][w >> 1]) & 0xffffu);
+                        if (out) nan |= 1u << (8 * s + 4 * h + w);
+                        if (hi == 0 || out) vs[s][h][w >> 1] &= ~mask;   // what no row sees may be anything
+                    }
+                }
+            if (kTok && __any_sync(kAll, nan != 0)) {
+                // 0 times NaN is NaN: such a group is left out of the product and put into the rows that see its key
+#pragma unroll 1
+                for (int i = 0; i < kKeys; ++i) {
+                    const uint32_t groups = __shfl_sync(kAll, nan, 8 * (i >> 2 & 3) + 4 * (i & 1)) >> (8 * (i >> 4) + 2 * (i & 2));
+                    int lo, hi;
+                    wk.rows_of(key + i, G, lo, hi);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int w = 0; w < N; ++w)
+                                if ((groups >> w & 1) && 8 * t + 2 * c + u >= lo && 8 * t + 2 * c + u < hi)
+                                    acc[t][2 * w][u] = acc[t][2 * w][u + 2] = acc[t][2 * w + 1][u] = acc[t][2 * w + 1][u + 2] = CUDART_NAN_F;
+                }
+            }
+        }
+        bool over = false;
+        float up[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                up[t][u] = fmaxf(y[0][t][u], y[0][t][u + 2]);
+#pragma unroll
+                for (int s = 1; s < S; ++s) up[t][u] = fmaxf(up[t][u], fmaxf(y[s][t][u], y[s][t][u + 2]));
+                over |= up[t][u] > lim[t][u];
+            }
+        if (__any_sync(kAll, over)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float was = m[t][u] == -CUDART_INF_F ? 0.f : m[t][u];
+                    float top = up[t][u];
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, off));
+                    const float mx = fmaxf(m[t][u], top - kLift + was);
+                    const float keep = m[t][u] == mx ? 1.f : ex2(m[t][u] - mx), by = mx == -CUDART_INF_F ? 0.f : was - mx;
+                    m[t][u] = mx;
+                    lim[t][u] = mx == -CUDART_INF_F ? mx : kLift + 8.f;
+                    l[t][u] *= keep;
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        y[s][t][u] += by;
+                        y[s][t][u + 2] += by;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2 * N; ++i) {
+                        acc[t][i][u] *= keep;
+                        acc[t][i][u + 2] *= keep;
+                    }
+                }
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    y[s][t][u] = ex2(y[s][t][u]);
+                    l[t][u & 1] += y[s][t][u];
+                }
+            uint32_t vw[4][N / 2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_shared(v_at + of + (16 * s + i) * (D / 2), vw[i]);
+#pragma unroll
+            for (int w = 0; w < N; ++w) {
+                uint32_t ra[4], rb[4];   // codes of keys 4 c, 4 c + 1; of 4 c + 2, 4 c + 3
+                const uint32_t sel = w & 1 ? 0x7632u : 0x5410u;
+                pairs(__byte_perm(vw[0][w >> 1], vw[1][w >> 1], sel), ra);
+                pairs(__byte_perm(vw[2][w >> 1], vw[3][w >> 1], sel), rb);
+                const float sa = half_of(vs[s][0][w >> 1], w), sb = half_of(vs[s][1][w >> 1], w);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const uint32_t b0 = transpose(pack(y[s][t][0] * sa, y[s][t][1] * sa)), b1 = transpose(pack(y[s][t][2] * sb, y[s][t][3] * sb));
+                    mma(acc[t][2 * w], ra[0], ra[1], rb[0], rb[1], b0, b1);
+                    mma(acc[t][2 * w + 1], ra[2], ra[3], rb[2], rb[3], b0, b1);
+                }
+            }
+        }
+        __syncwarp();   // the stage has been read
+        fill(key + kStages * kStride, st);
+        find(key + (kStages + 1) * kStride);
+        st = st + 1 == kStages ? 0 : st + 1;
+    }
+
+    // ---- the warp's sums: row g of tile 2 w + i is dimension 32 w + 8 (g / 2) + g % 2 + 4 i, row g + 8 that + 2
+    __syncwarp();
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = 8 * t + 2 * c + u;
+            float v = l[t][u];
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) v += __shfl_xor_sync(kAll, v, off);
+            if (g == 0) { w_m[r] = m[t][u]; w_l[r] = v * 0x1p-78f; }
+#pragma unroll
+            for (int w = 0; w < N; ++w)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float *o = w_o + r * D + 32 * w + 8 * (g >> 1) + (g & 1) + 4 * i;
+                    o[0] = acc[t][2 * w + i][u] * 0x1p55f;
+                    o[2] = acc[t][2 * w + i][u + 2] * 0x1p51f;
+                }
+        }
+}
+
+}  // namespace q4
+}  // namespace sla

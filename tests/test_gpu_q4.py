@@ -254,10 +254,15 @@ def build(sla, n, new, *, hkv=2, G=4, d=128, dtype=BF16, page=16, gap=0, seed=3,
 
 
 def reference(q, k, v, table, n, new, G, window, scale, page):
-    """attention_reference over the values that the planes stand for."""
+    """attention_reference over the values that the planes stand for.
+
+    A bound beside U.tolerances: codes of bf16 calls are 2^-133 as large as they are in their products and weights 2^78 times as large, so that
+    a sum in fp32, which is cut at 2^-149 with each of its 16 keys or fewer, is off by 2^-149 2^(133 - 78) = 2^-94 each time.  (Where the keys of
+    large weight have codes of zero in a dimension, the result there is as small.)  The weights' rounding, 2^-8 of sum p |v|, makes 2^-94 of 2^-86."""
     d = q.shape[-1]
     kk, vv = Q.unpack(k, page, d, False), Q.unpack(v, page, d, True)
-    return U.attention_reference(q, kk, vv, table, n, new, G, window, scale, page)
+    out, lse, mag, dot, keys = U.attention_reference(q, kk, vv, table, n, new, G, window, scale, page)
+    return out, lse, mag + keys[:, None, None] * 2.0 ** -86 if q.dtype == BF16 else mag, dot, keys
 
 
 def run(sla, handle, n, new, window=0, scale=None, max_new=None, prep=None, **kw):
