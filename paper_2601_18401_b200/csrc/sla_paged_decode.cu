@@ -435,7 +435,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
     constexpr int R = 16;                 // rows of a partial result
     // a warp's sums [8 NT][D]; over a cache in four bits they lie over its ring of stages
     extern __shared__ __align__(128) char dyn_sm[];
-    constexpr int kRing = kQ4 ? q4::ring_bytes(D) : 0, kSums = kQ4 ? kRing / 4 : 8 * NT * D;
+    constexpr int kRing = kQ4 ? q4::ring_bytes(D, NT) : 0, kSums = kQ4 ? kRing / 4 : 8 * NT * D;
     static_assert(kSums >= 8 * NT * D, "the sums fit into the ring");
     __shared__ alignas(16) float s_sums[kQ4 ? 4 : kWarps * kSums];
     float *s_o = kQ4 ? reinterpret_cast<float *>(dyn_sm) : s_sums;
@@ -639,7 +639,7 @@ template <typename T, int D, int NT, bool kTok, bool kQ4>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
-    constexpr size_t kRing = kQ4 ? kWarps * q4::ring_bytes(D) : 0;
+    constexpr size_t kRing = kQ4 ? kWarps * q4::ring_bytes(D, NT) : 0;
     if (kQ4) {
         static bool allowed[64] = {};
         int dev = 0;

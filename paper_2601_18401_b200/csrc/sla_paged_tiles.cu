@@ -35,7 +35,10 @@
 #include <math_constants.h>
 #include <stddef.h>
 
+#include <type_traits>
+
 #include "sla_paged_attn.h"
+#include "sla_q4.cuh"
 #include "sla_tc_ptx.cuh"
 
 namespace sla {
@@ -239,7 +242,7 @@ __device__ __noinline__ void fold_rows(float *fold, uint32_t o_addr, float m, bo
 // keys.  The keys lie at the two ends of the mask, at most the unit's tokens and a tile at each, however long the segment is.
 // (The row's address and bounds are worked out again in here, off the way of the segments that have no such value: 1 to 600 tokens of
 // 16 sequences take 60.5 us so, 61.2 with them as arguments.)
-template <int D>
+template <int D, bool kQ4>
 __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, int x, uint32_t tmem) {
     const int lane = threadIdx.x & 31, row = threadIdx.x & 127, TS = p.TS, G = p.a.G, end = min(s.hi * kKeys, s.n);
     const uint32_t o_addr = tmem + (static_cast<uint32_t>(row & 96) << 16) + kColO + x * 128;
@@ -249,8 +252,17 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
     const int all_hi = s.n - s.q + s.t0, all_lo = p.a.window > 0 ? minus(s.n - s.q + s.t1, p.a.window) : 0;   // keys that every row sees
     const bf16 *q = p.q + (s.row0 + tok) * p.a.q_st + (long long)(s.head * G + g) * p.a.q_sh;
     const int *table = p.a.c.table + (long long)max(s.slot, 0) * p.a.c.width;
-    auto at = [&](int j) {
-        return valid_page(p.a.c, __ldg(table + (j >> p.a.c.shift))) * p.a.c.s_page + s.head * p.a.c.s_h + (long long)(j & (p.a.c.P - 1)) * p.a.c.s_t;
+    auto at = [&](int j) {   // of its row; in four bits of its plane
+        return valid_page(p.a.c, __ldg(table + (j >> p.a.c.shift))) * p.a.c.s_page + s.head * p.a.c.s_h + (kQ4 ? 0 : (long long)(j & (p.a.c.P - 1)) * p.a.c.s_t);
+    };
+    // eight values from dimension d on of the key j, whose row or plane lies at `off`
+    auto k_piece = [&](long long off, int j, int d, float (&f)[8]) {
+        if constexpr (kQ4) q4::load_values<false>(p.a.c.k + off, p.a.c.P, D, j & (p.a.c.P - 1), d / 8, f);
+        else Vec16<bf16>::load(reinterpret_cast<const bf16 *>(p.a.c.k) + off + d, f);
+    };
+    auto v_piece = [&](long long off, int j, int d, float (&f)[8]) {
+        if constexpr (kQ4) q4::load_values<true>(p.a.c.v + off, p.a.c.P, D, j & (p.a.c.P - 1), d / 8, f);
+        else Vec16<bf16>::load(reinterpret_cast<const bf16 *>(p.a.c.v) + off + d, f);
     };
 #pragma unroll 1
     for (int j0 = s.lo * kKeys; j0 < end; j0 += 32) {
@@ -261,11 +273,15 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
         const int j = j0 + lane;
         uint32_t bad = 0;
         if (j < end && (j < all_lo || j > all_hi) && (!s.both || (s.place(j / kKeys) & 1) == x)) {
-            const uint4 *v = reinterpret_cast<const uint4 *>(reinterpret_cast<const bf16 *>(p.a.c.v) + at(j));
+            if constexpr (kQ4) {
+                for (int d = 0; d < D; d += 32) bad |= q4::is_nan(q4::scale_of(p.a.c.v + at(j), p.a.c.P, D, j & (p.a.c.P - 1), d));
+            } else {
+                const uint4 *v = reinterpret_cast<const uint4 *>(reinterpret_cast<const bf16 *>(p.a.c.v) + at(j));
 #pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-                const uint4 w = __ldg(v + c);
-                bad |= not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w);
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 w = __ldg(v + c);
+                    bad |= not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w);
+                }
             }
         }
 #pragma unroll 1
@@ -275,25 +291,23 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
             const bool sees = key >= first && key <= last;
             float weight = 1.f;
             if (sees) {
-                const bf16 *k = reinterpret_cast<const bf16 *>(p.a.c.k) + off;
                 float dot = 0.f;
 #pragma unroll 2
                 for (int d = 0; d < D; d += 8) {
                     float a[8], b[8];
                     Vec16<bf16>::load(q + d, a);
-                    Vec16<bf16>::load(k + d, b);
+                    k_piece(off, key, d, b);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) dot = fmaf(a[e], b[e], dot);
                 }
                 if (dot == -CUDART_INF_F) weight = 0.f;   // (a NaN, or +inf, is in the row's sum)
             }
             __syncwarp();
-            const bf16 *v = reinterpret_cast<const bf16 *>(p.a.c.v) + off;
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
                 float f[2][8];
-                Vec16<bf16>::load(v + c, f[0]);
-                Vec16<bf16>::load(v + c + 8, f[1]);
+                v_piece(off, key, c, f[0]);
+                v_piece(off, key, c + 8, f[1]);
                 uint32_t o[16];
                 ptx::tmem_ld16(o_addr + c, o);
                 ptx::tmem_wait_ld();
@@ -310,7 +324,51 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
     ptx::tc_fence_before();
 }
 
-template <int D, bool kLong>
+// A cache in four bits: the warps that write results make K and V of it in the ring.  A warp has 32 rows of a tile, which lie in one page or in two of
+// 16 tokens; a lane takes 16 bytes of codes of kItems of them, neighbouring lanes a row's pieces, and requests them a tile of K (or V) ahead.  The
+// rows of eight neighbouring lanes differ where the swizzle of the tiles wants it: their 16-byte stores meet all banks.
+template <int D> struct Codes {
+    static constexpr int kItems = D / 32, kLanes = D / 32, kRows = 32 / kLanes;   // of a lane; lanes of a row; rows of an item
+    uint4 w[kItems];
+    uint2 s[kItems];   // scales
+    // The rows of a warp whose first key is k0 (of pages `at`, in bytes from pool, by halves of 16) and of which those below n count.
+    __device__ __forceinline__ void load(const char *pool, const long long (&at)[2], const Pages &c, int k0, int n, int row) {
+        const int t0 = c.P < 32 ? 0 : k0 & (c.P - 1);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int r = i * kRows + row, half = 2 * i / kItems, t = t0 + (c.P < 32 ? r - 16 * half : r);
+            const char *plane = pool + at[half];
+            w[i] = make_uint4(0, 0, 0, 0);
+            s[i] = make_uint2(0, 0);
+            if (k0 + r < n) {   // what lies behind the sequence may be anything
+                w[i] = __ldg(reinterpret_cast<const uint4 *>(plane + q4::codes_at(D, t)) + threadIdx.x % kLanes);
+                const char *sc = plane + q4::scales_at(c.P, D, t);
+                if constexpr (D == 128) s[i] = __ldg(reinterpret_cast<const uint2 *>(sc));
+                else s[i].x = __ldg(reinterpret_cast<const uint32_t *>(sc));
+            }
+        }
+    }
+    // to: where the lane's first piece goes in its first row
+    template <bool kValues> __device__ __forceinline__ void store(uint32_t to) const {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const uint32_t word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                // the piece of eight dimensions: group, and which of the group's four
+                const int g = D == 128 ? x : x & 1, up = D == 128 ? 0 : x >> 1;
+                const uint32_t sel = x & 1 ? 0x7632u : 0x5410u;
+                const uint32_t codes = !kValues ? word[x] : D == 128 ? __byte_perm(word[x >> 1], word[2 + (x >> 1)], sel) : __byte_perm(word[2 * (x >> 1)], word[2 * (x >> 1) + 1], sel);
+                const uint32_t sc = g & 2 ? s[i].y : s[i].x;
+                uint32_t v[4];
+                q4::values(codes, q4::factor(g & 1 ? sc >> 16 : sc & 0xffffu), v);
+                ptx::st_shared_v4((to ^ ((g & 1) * 64 + up * 16)) + (g >> 1) * Layout<D>::kHalfBytes + i * kRows * 128, v);
+            }
+        }
+    }
+};
+
+template <int D, bool kLong, bool kQ4>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
             const __grid_constant__ TileParams p) {
@@ -348,14 +406,14 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         }
 #pragma unroll 1
         for (int s = 0; s < kStages; ++s) {
-            ptx::mbar_init(bar_kv_full + 8 * s, 1);
+            ptx::mbar_init(bar_kv_full + 8 * s, kQ4 ? 4 : 1);   // four bits: a filling warp each
             ptx::mbar_init(bar_kv_empty + 8 * s, 1);
             ptx::mbar_init(bar_kv_empty + 80 + 8 * s, 1);
         }
 #pragma unroll 1
         for (int s = 0; s < kSegs; ++s) {
             ptx::mbar_init(bar_seg_full + 8 * s, 1);
-            ptx::mbar_init(bar_seg_empty + 8 * s, 13 + 2 * 32);   // rows, epilogue, K/V: a warp each; the issuers a lane each
+            ptx::mbar_init(bar_seg_empty + 8 * s, (kQ4 ? 12 : 13) + 2 * 32);   // rows, epilogue, K/V: a warp each; the issuers a lane each
         }
         meta->abort_flag = 0;
         meta->s_time[0] = meta->s_time[1] = clock();
@@ -474,6 +532,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
             }
         } else if (warp == 14) {
+            if constexpr (!kQ4) {
             // ---------------- K and V: a lane per box, as many as the tile has pages with tokens
             ptx::prefetch_tensormap(&tm_k);
             ptx::prefetch_tensormap(&tm_v);
@@ -519,6 +578,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                         __syncwarp();
                     }
                 }
+            }
             }
         } else {
             // ---------------- the CTA's ranges, segment after segment, and their Q
@@ -609,8 +669,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         uint32_t ns[2] = {0, 0};
         bool ok = true;
-#pragma unroll 1
-        for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) {
+        auto results = [&](uint32_t k) {
             const Seg &s = meta->seg[k % kSegs];
 #pragma unroll 1
             for (int x = 0; x < 2 && ok; ++x) {
@@ -696,6 +755,81 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     else p.parts.lse2[(long long)s.part * 256 + x * kRows + canon] = stat.y;
                 }
                 if (s.both) break;
+            }
+        };
+        if constexpr (!kQ4) {
+#pragma unroll 1
+            for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) results(k);
+        } else {
+            // Two tiles of the next segment go into the ring before the results of this one are written: they wait for nothing but this segment's
+            // products.
+            using F = Codes<D>;
+            const int idx = lane / F::kLanes;   // row of an item, mixed so that its low bits differ where the swizzle does
+            const int row0 = D == 128 ? (idx & 1) << 2 | idx >> 1 : (idx & 9) | (idx & 2) << 1 | (idx & 4) >> 1;
+            const uint32_t to = (warp - 8) * 32 * 128 + row0 * 128 + ((D == 128 ? lane % 4 : 2 * (lane % 2)) ^ (row0 & 7)) * 16;
+            const Pages &c = p.a.c;
+            uint32_t i = 0;   // ring position
+            auto fill = [&](uint32_t k, int from, int until) {
+                if (from >= until) return;
+                const Seg &s = meta->seg[k % kSegs];
+                const int n = s.n, lo = s.lo, hi = s.hi;
+                const int *table = c.table + (long long)max(s.slot, 0) * c.width;
+                const char *kp = c.k + s.head * c.s_h, *vp = c.v + s.head * c.s_h;
+                auto after = [&](int j) { return j + 1 < hi ? j + 1 : lo; };
+                auto first_key = [&](int j) { return j * kKeys + (warp - 8) * 32; };
+                // the pages of a tile's rows; those behind the sequence are not asked for
+                auto look = [&](int j, int (&page)[2]) {
+                    const int key = first_key(j);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) page[h] = key + 16 * h < n ? __ldg(table + ((key + 16 * h) >> c.shift)) : 0;
+                };
+                auto place = [&](const int (&page)[2], long long (&at)[2]) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) at[h] = valid_page(c, page[h]) * c.s_page;
+                };
+                auto put = [&](auto values, const F &f) {
+                    const uint32_t st = i % kStages, ph = ((i / kStages) & 1u) ^ 1u;
+                    ok = ptx::mbar_wait_warp(bar_kv_empty + 8 * st, ph, abort_flag) && ptx::mbar_wait_warp(bar_kv_empty + 80 + 8 * st, ph, abort_flag);
+                    if (!ok) return;
+                    f.template store<decltype(values)::value>(base + L::kOffKV + st * L::kTileBytes + to);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar_kv_full + 8 * st);
+                    ++i;
+                };
+                int j = s.begin + from;
+                if (j >= hi) j -= hi - lo;
+                int page[2];
+                long long at[2];
+                F kf, vf;
+                look(j, page);
+                place(page, at);
+                kf.load(kp, at, c, first_key(j), n, row0);
+                look(after(j), page);
+#pragma unroll 1
+                for (int t = from; t < until && ok; ++t) {
+                    vf.load(vp, at, c, first_key(j), n, row0);
+                    put(std::false_type{}, kf);
+                    j = after(j);
+                    if (t + 1 < until) {
+                        place(page, at);
+                        kf.load(kp, at, c, first_key(j), n, row0);
+                        look(after(j), page);
+                    }
+                    if (ok) put(std::true_type{}, vf);
+                }
+            };
+            auto tiles_of = [&](uint32_t k) { return meta->seg[k % kSegs].hi - meta->seg[k % kSegs].lo; };
+            int done = 0;
+            bool more = take_seg(0);
+#pragma unroll 1
+            for (uint32_t k = 0; ok && more; ++k) {
+                fill(k, done, tiles_of(k));
+                more = ok && take_seg(k + 1);
+                done = more ? min(2, tiles_of(k + 1)) : 0;
+                if (more) fill(k + 1, 0, done);
+                if (ok) results(k);
+                free_seg(k);
             }
         }
     } else {
@@ -874,7 +1008,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     if (!(ok = ptx::mbar_wait_warp(bar_o_full + 8 * x, ns & 1u, abort_flag))) break;
                     ptx::tc_fence_after();
                     if (kLong && s.own[x] > kFoldTiles) fold_rows<D>(p.fold, o_addr, fresh ? -CUDART_INF_F : m_ref, false, true);
-                    if (odd) add_not_finite<D>(p, s, x, tmem);
+                    if (odd) add_not_finite<D, kQ4>(p, s, x, tmem);
                 }
                 // the epilogue has read the statistics (and O) of the segment before
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
@@ -958,14 +1092,14 @@ bool make_map(CUtensorMap *tm, const void *ptr, int D, const Dim *d, int n, cons
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kLong>
+template <int D, bool kLong, bool kQ4>
 cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, char *scratch, void *out, float *lse, cudaStream_t st) {
     static bool allowed[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !allowed[dev]) {
-        e = cudaFuncSetAttribute(paged_tiles<D, kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
+        e = cudaFuncSetAttribute(paged_tiles<D, kLong, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
         if (e != cudaSuccess) return e;
         if (dev < 64) allowed[dev] = true;
     }
@@ -980,20 +1114,22 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
     p.TS = pl.TS;
     p.out32 = (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && a.q_st % 16 == 0 && a.q_sh % 16 == 0;
     p.box_rows = a.c.P < kKeys ? a.c.P : kKeys;
-    Dim kd[3], qd[2];
-    if (!kv_dims(a, kd) || !q_dims(a, qd)) return cudaErrorInvalidValue;
+    Dim kd[3] = {}, qd[2];
+    if ((!kQ4 && !kv_dims(a, kd)) || !q_dims(a, qd)) return cudaErrorInvalidValue;
     int *slot[3] = {&p.slot_t, &p.slot_h, &p.slot_p};
     cuuint32_t kbox[3] = {1, 1, 1}, qbox[2];
-    for (int i = 0; i < 3; ++i) {
+    p.slot_t = p.slot_h = p.slot_p = 0;
+    for (int i = 0; i < 3 && !kQ4; ++i) {
         *slot[kd[i].which] = i;
         if (kd[i].which == 0) kbox[i] = p.box_rows;
     }
     p.t_inner = qd[0].which == 1;
     for (int i = 0; i < 2; ++i) qbox[i] = qd[i].which == 1 ? pl.TS : a.G;
     CUtensorMap tq, tk, tv;
-    if (!make_map(&tq, q, D, qd, 2, qbox) || !make_map(&tk, a.c.k, D, kd, 3, kbox) || !make_map(&tv, a.c.v, D, kd, 3, kbox))
-        return cudaErrorInvalidValue;
-    return launch_chained(paged_tiles<D, kLong>, dim3(pl.n_ctas), dim3(kThreads), Layout<D>::kSmem, st, tq, tk, tv, p);
+    if (!make_map(&tq, q, D, qd, 2, qbox)) return cudaErrorInvalidValue;
+    tk = tv = tq;   // (four bits: not looked at)
+    if (!kQ4 && (!make_map(&tk, a.c.k, D, kd, 3, kbox) || !make_map(&tv, a.c.v, D, kd, 3, kbox))) return cudaErrorInvalidValue;
+    return launch_chained(paged_tiles<D, kLong, kQ4>, dim3(pl.n_ctas), dim3(kThreads), Layout<D>::kSmem, st, tq, tk, tv, p);
 }
 
 }  // namespace
@@ -1001,7 +1137,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
 // bf16, strides that nest in memory (no broadcast views), a scale that keeps the order of the logits and -inf what it is
 bool paged_tiles_supported(const PagedCall &a, int dtype) {
     Dim kd[3], qd[2];
-    return a.c.es != 1 && dtype == SLA_BF16 && a.scale > 0.f && kv_dims(a, kd) && q_dims(a, qd);
+    return dtype == SLA_BF16 && a.scale > 0.f && (q4::is(a.c) || kv_dims(a, kd)) && q_dims(a, qd);
 }
 
 void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
@@ -1024,9 +1160,14 @@ void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.fold_bytes = keys > (long long)kFoldTiles * kKeys ? (size_t)sm_count * 8 * 32 * (a.c.D + 4) * sizeof(float) : 0;
 }
 
+template <bool kQ4>
+static cudaError_t tiles_for(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
+    if (p.fold_bytes) return a.c.D == 64 ? tiles_of<64, true, kQ4>(q, a, p, scratch, out, lse, st) : tiles_of<128, true, kQ4>(q, a, p, scratch, out, lse, st);
+    return a.c.D == 64 ? tiles_of<64, false, kQ4>(q, a, p, scratch, out, lse, st) : tiles_of<128, false, kQ4>(q, a, p, scratch, out, lse, st);
+}
+
 cudaError_t launch_paged_tiles(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, void *out, float *lse, cudaStream_t st) {
-    if (p.fold_bytes) return a.c.D == 64 ? tiles_of<64, true>(q, a, p, scratch, out, lse, st) : tiles_of<128, true>(q, a, p, scratch, out, lse, st);
-    return a.c.D == 64 ? tiles_of<64, false>(q, a, p, scratch, out, lse, st) : tiles_of<128, false>(q, a, p, scratch, out, lse, st);
+    return q4::is(a.c) ? tiles_for<true>(q, a, p, scratch, out, lse, st) : tiles_for<false>(q, a, p, scratch, out, lse, st);
 }
 
 }  // namespace sla

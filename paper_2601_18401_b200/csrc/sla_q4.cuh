@@ -69,6 +69,14 @@ __device__ __forceinline__ void load_piece(const char *plane, int P, int D, int 
         w = __ldg(reinterpret_cast<const uint32_t *>(row) + c * n + g);
     }
 }
+// Its values in fp32.
+template <bool kValues>
+__device__ __forceinline__ void load_values(const char *plane, int P, int D, int t, int j, float (&f)[8]) {
+    uint32_t w, s, r[4];
+    load_piece<kValues>(plane, P, D, t, j, w, s);
+    values(w, factor(s), r);
+    Vec16<__nv_bfloat16>::unpack(make_uint4(r[0], r[1], r[2], r[3]), f);
+}
 // The 16 bits of the scale of dimension d.
 __device__ __forceinline__ uint32_t scale_of(const char *plane, int P, int D, int t, int d) {
     return __ldg(reinterpret_cast<const unsigned short *>(plane + scales_at(P, D, t)) + d / 32);

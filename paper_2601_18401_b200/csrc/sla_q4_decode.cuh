@@ -75,7 +75,8 @@ constexpr int kKeys = 32;        // of a stage
 #endif
 constexpr int kStages = Q4ST;
 __host__ __device__ constexpr int stage_bytes(int D) { return 2 * kKeys * (D / 2 + D / 16); }   // K codes, K scales, V codes, V scales
-__host__ __device__ constexpr int ring_bytes(int D) { return kStages * stage_bytes(D); }
+// of a warp: its stages, and behind them Q as the products take it
+__host__ __device__ constexpr int ring_bytes(int D, int NT) { return kStages * stage_bytes(D) + NT * D * 16; }
 
 // 8 NT rows at most; Walk, w_m, w_l and w_o as for attend_bf16, w_o over the ring, but the warp takes 32 keys at a time.  A thread (g, c) = (lane / 4,
 // lane % 4) has of the products' operands (16 keys a step) the keys ka = 4 (g / 2) + g % 2 and kb = ka + 2 of K, S and P, row g of Q (and g + 8) and
@@ -129,11 +130,12 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         fill(key + st * kStride, st);
     }
     find(key + kStages * kStride);
+    const uint32_t q_at = ring + kStages * stage_bytes(D) + lane * 16;   // (a lane reads what it wrote)
     // [t][e]: row 8 t + 2 c + e
     float m[NT][2], l[NT][2], lim[NT][2], mult[NT][2], acc[NT][2 * N][4];
-    uint32_t qf[NT][N][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+        uint32_t qf[N][4];
         const bool on = 8 * t + g < (kTok ? wk.rows : G);
         const int r = on ? 8 * t + g : 0, tok = kTok ? r / G : 0;
         const __nv_bfloat16 *src = q + (long long)(wk.row_q + tok) * a.q_st + (long long)(wk.head * G + r - tok * G) * a.q_sh + c * 8;
@@ -141,9 +143,9 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
 #pragma unroll
         for (int w = 0; w < N; ++w) {
             const uint4 v = on ? __ldg(reinterpret_cast<const uint4 *>(src + 32 * w)) : make_uint4(0, 0, 0, 0);
-            qf[t][w][0] = v.x; qf[t][w][1] = v.y; qf[t][w][2] = v.z; qf[t][w][3] = v.w;
+            qf[w][0] = v.x; qf[w][1] = v.y; qf[w][2] = v.z; qf[w][3] = v.w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = __vmaxu2(top, qf[t][w][i] & 0x7fff7fffu);
+            for (int i = 0; i < 4; ++i) top = __vmaxu2(top, qf[w][i] & 0x7fff7fffu);
         }
         top = max(top & 0xffffu, top >> 16);
         top = max(top, __shfl_xor_sync(kAll, top, 1));
@@ -152,9 +154,11 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         const int e = min(max((int)(top >> 7) - 127, -27), 85);
         const float f0 = __uint_as_float((uint32_t)(227 - e) << 23), f1 = __uint_as_float((uint32_t)(223 - e) << 23);
 #pragma unroll
-        for (int w = 0; w < N; ++w)
+        for (int w = 0; w < N; ++w) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qf[t][w][i] = pack(half_of(qf[t][w][i], 0) * (i & 1 ? f1 : f0), half_of(qf[t][w][i], 1) * (i & 1 ? f1 : f0));
+            for (int i = 0; i < 4; ++i) qf[w][i] = pack(half_of(qf[w][i], 0) * (i & 1 ? f1 : f0), half_of(qf[w][i], 1) * (i & 1 ? f1 : f0));
+            ptx::st_shared_v4(q_at + (t * N + w) * 512, qf[w]);
+        }
         const float back = a.scale * kLog2e * __uint_as_float((uint32_t)(160 + e) << 23);   // 2^(33 + e)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -179,25 +183,30 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         __syncwarp();   // every lane's copies are there
         const uint32_t of = st * stage_bytes(D);
         float y[S][NT][4];   // [s][t][2 h + e]: key 16 s + ka + 2 h, row 8 t + 2 c + e
+        uint32_t kw[S][2][N], ks[S][2][N / 2];
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            uint32_t kw[2][N], ks[2][N / 2];
+        for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                load_shared(k_at + of + (16 * s + 2 * h) * (D / 2), kw[h]);
-                load_shared(s_at + of + (16 * s + 2 * h) * (D / 16), ks[h]);
+                load_shared(k_at + of + (16 * s + 2 * h) * (D / 2), kw[s][h]);
+                load_shared(s_at + of + (16 * s + 2 * h) * (D / 16), ks[s][h]);
             }
 #pragma unroll
-            for (int w = 0; w < N; ++w) {
+        for (int w = 0; w < N; ++w) {
+            uint32_t qf[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) load_shared(q_at + (t * N + w) * 512, qf[t]);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
                 uint32_t ra[4], rb[4];
-                pairs(kw[0][w], ra);
-                pairs(kw[1][w], rb);
-                const float sa = half_of(ks[0][w >> 1], w), sb = half_of(ks[1][w >> 1], w);
+                pairs(kw[s][0][w], ra);
+                pairs(kw[s][1][w], rb);
+                const float sa = half_of(ks[s][0][w >> 1], w), sb = half_of(ks[s][1][w >> 1], w);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     float d[4];
-                    mma0(d, ra[0], rb[0], ra[1], rb[1], qf[t][w][0], qf[t][w][1]);
-                    mma(d, ra[2], rb[2], ra[3], rb[3], qf[t][w][2], qf[t][w][3]);
+                    mma0(d, ra[0], rb[0], ra[1], rb[1], qf[t][0], qf[t][1]);
+                    mma(d, ra[2], rb[2], ra[3], rb[3], qf[t][2], qf[t][3]);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) y[s][t][u] = w == 0 ? d[u] * (u < 2 ? sa : sb) : fmaf(d[u], u < 2 ? sa : sb, y[s][t][u]);
                 }
