@@ -67,8 +67,11 @@ constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns,
 // whose tables and windows reach further take the kernel that does so (kLong): its loop costs 1 to 3 % (1 to 600 tokens of 16 sequences 61.9 us
 // instead of 60.2, 1999 at 30011 988 instead of 980, 2400 at 2^20 nothing that can be told from noise).
 constexpr int kFoldTiles = 512;
-constexpr int kRegsRow = 184, kRegsRest = 72;
-static_assert(2 * kRegsRow + 2 * kRegsRest <= 4 * 128, "more registers than the block is launched with");
+// (four bits: the warps that make K and V hold the codes of a tile of both; 8192 tokens that end at 65536 8.65 ms so, 8.75 with 176 and 80, 8.97 with
+// 184 and 72)
+template <bool kQ4> constexpr int kRegsRow = kQ4 ? 168 : 184;
+template <bool kQ4> constexpr int kRegsRest = kQ4 ? 88 : 72;
+static_assert(kRegsRow<false> + kRegsRest<false> <= 2 * 128 && kRegsRow<true> + kRegsRest<true> <= 2 * 128, "more registers than the block is launched with");
 
 template <int D> struct Layout {
     static constexpr int kHalves = D / 64;                  // 64-column halves of a tile, 128 rows x 128 B each
@@ -328,24 +331,23 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
 // 16 tokens; a lane takes 16 bytes of codes of kItems of them, neighbouring lanes a row's pieces, and requests them a tile of K (or V) ahead.  The
 // rows of eight neighbouring lanes differ where the swizzle of the tiles wants it: their 16-byte stores meet all banks.
 template <int D> struct Codes {
-    static constexpr int kItems = D / 32, kLanes = D / 32, kRows = 32 / kLanes;   // of a lane; lanes of a row; rows of an item
+    static constexpr int kItems = D / 32, kLanes = D / 32, kRows = 32 / kLanes, kHalf = kItems / 2;   // of a lane; lanes of a row; rows of an item; items of 16 rows
     uint4 w[kItems];
     uint2 s[kItems];   // scales
-    // The rows of a warp whose first key is k0 (of pages `at`, in bytes from pool, by halves of 16) and of which those below n count.
-    __device__ __forceinline__ void load(const char *pool, const long long (&at)[2], const Pages &c, int k0, int n, int row) {
-        const int t0 = c.P < 32 ? 0 : k0 & (c.P - 1);
+    // codes, scales: where the lane's first row of either half of 16 has them, from pool.  left: of the lane's rows those below it count, what lies
+    // behind them may be anything.
+    __device__ __forceinline__ void load(const char *pool, const long long (&codes)[2], const long long (&scales)[2], int left) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int r = i * kRows + row, half = 2 * i / kItems, t = t0 + (c.P < 32 ? r - 16 * half : r);
-            const char *plane = pool + at[half];
-            w[i] = make_uint4(0, 0, 0, 0);
-            s[i] = make_uint2(0, 0);
-            if (k0 + r < n) {   // what lies behind the sequence may be anything
-                w[i] = __ldg(reinterpret_cast<const uint4 *>(plane + q4::codes_at(D, t)) + threadIdx.x % kLanes);
-                const char *sc = plane + q4::scales_at(c.P, D, t);
-                if constexpr (D == 128) s[i] = __ldg(reinterpret_cast<const uint2 *>(sc));
-                else s[i].x = __ldg(reinterpret_cast<const uint32_t *>(sc));
-            }
+            const int h = i / kHalf, e = i % kHalf * kRows;
+            w[i] = __ldg(reinterpret_cast<const uint4 *>(pool + codes[h] + e * (D / 2)));
+            if constexpr (D == 128) s[i] = __ldg(reinterpret_cast<const uint2 *>(pool + scales[h] + e * (D / 16)));
+            else s[i].x = __ldg(reinterpret_cast<const uint32_t *>(pool + scales[h] + e * (D / 16)));
+        }
+        if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i)
+                if (i * kRows >= left) s[i] = make_uint2(0, 0);
         }
     }
     // to: where the lane's first piece goes in its first row
@@ -361,7 +363,7 @@ template <int D> struct Codes {
                 const uint32_t codes = !kValues ? word[x] : D == 128 ? __byte_perm(word[x >> 1], word[2 + (x >> 1)], sel) : __byte_perm(word[2 * (x >> 1)], word[2 * (x >> 1) + 1], sel);
                 const uint32_t sc = g & 2 ? s[i].y : s[i].x;
                 uint32_t v[4];
-                q4::values(codes, q4::factor(g & 1 ? sc >> 16 : sc & 0xffffu), v);
+                q4::small_values(codes, g & 1 ? __byte_perm(sc, 0, 0x3232) : __byte_perm(sc, 0, 0x1010), v);
                 ptx::st_shared_v4((to ^ ((g & 1) * 64 + up * 16)) + (g >> 1) * Layout<D>::kHalfBytes + i * kRows * 128, v);
             }
         }
@@ -442,7 +444,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
     };
 
     if (warp >= 12) {
-        ptx::setmaxnreg_dec<kRegsRest>();
+        ptx::setmaxnreg_dec<kRegsRest<kQ4>>();
         if (warp < 14) {
             // ---------------- MMA issuer of stream x: a whole warp, its elected lane issues.  S of the next tile goes right behind
             // the PV of this one, which reads the P that lies over it (the tensor pipe keeps a thread's order).
@@ -663,7 +665,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         }
     } else if (warp >= 8) {
         // ---------------- results: a thread a row
-        ptx::setmaxnreg_dec<kRegsRest>();
+        ptx::setmaxnreg_dec<kRegsRest<kQ4>>();
         const int row = tid & 127;
         const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G, canon = t * G + g;
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -777,15 +779,23 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 const char *kp = c.k + s.head * c.s_h, *vp = c.v + s.head * c.s_h;
                 auto after = [&](int j) { return j + 1 < hi ? j + 1 : lo; };
                 auto first_key = [&](int j) { return j * kKeys + (warp - 8) * 32; };
-                // the pages of a tile's rows; those behind the sequence are not asked for
+                // the pages of a tile's rows (behind the sequence page 0, which nobody asks for)
                 auto look = [&](int j, int (&page)[2]) {
                     const int key = first_key(j);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) page[h] = key + 16 * h < n ? __ldg(table + ((key + 16 * h) >> c.shift)) : 0;
                 };
-                auto place = [&](const int (&page)[2], long long (&at)[2]) {
+                long long codes[2], scales[2];
+                auto place = [&](int j, const int (&page)[2]) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) at[h] = valid_page(c, page[h]) * c.s_page;
+                    for (int h = 0; h < 2; ++h) {
+                        const int t = c.P < 32 ? row0 : (first_key(j) & (c.P - 1)) + 16 * h + row0;
+                        const bool there = (unsigned)page[h] < (unsigned)c.n_pages;
+                        if (!there) atomicOr(c.status, kStatusBadIndex);
+                        const long long plane = (there ? page[h] : 0) * c.s_page;
+                        codes[h] = plane + q4::codes_at(D, t) + lane % F::kLanes * 16;
+                        scales[h] = plane + q4::scales_at(c.P, D, t);
+                    }
                 };
                 auto put = [&](auto values, const F &f) {
                     const uint32_t st = i % kStages, ph = ((i / kStages) & 1u) ^ 1u;
@@ -800,23 +810,21 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 int j = s.begin + from;
                 if (j >= hi) j -= hi - lo;
                 int page[2];
-                long long at[2];
                 F kf, vf;
                 look(j, page);
-                place(page, at);
-                kf.load(kp, at, c, first_key(j), n, row0);
+                place(j, page);
+                kf.load(kp, codes, scales, n - first_key(j) - row0);
                 look(after(j), page);
 #pragma unroll 1
                 for (int t = from; t < until && ok; ++t) {
-                    vf.load(vp, at, c, first_key(j), n, row0);
+                    vf.load(vp, codes, scales, n - first_key(j) - row0);
                     put(std::false_type{}, kf);
+                    if (!ok) break;
                     j = after(j);
-                    if (t + 1 < until) {
-                        place(page, at);
-                        kf.load(kp, at, c, first_key(j), n, row0);
-                        look(after(j), page);
-                    }
-                    if (ok) put(std::true_type{}, vf);
+                    place(j, page);
+                    kf.load(kp, codes, scales, n - first_key(j) - row0);   // (behind the last tile another one, for nothing)
+                    look(after(j), page);
+                    put(std::true_type{}, vf);
                 }
             };
             auto tiles_of = [&](uint32_t k) { return meta->seg[k % kSegs].hi - meta->seg[k % kSegs].lo; };
@@ -834,12 +842,12 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         }
     } else {
         // ---------------- rows of stream x: a thread a row
-        ptx::setmaxnreg_inc<kRegsRow>();
+        ptx::setmaxnreg_inc<kRegsRow<kQ4>>();
         const int x = warp >> 2, row = tid & 127;
         const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G;
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const uint32_t o_addr = lane_addr + kColO + x * 128, s_col = lane_addr + kColS + x * 128;
-        const float scale2 = p.a.scale * kLog2e;
+        const float scale2 = p.a.scale * kLog2e * (kQ4 ? q4::kSmall : 1.f);   // (K and V of codes are 2^-48 of what they are)
         uint32_t nt = 0, ns = 0, tiles = 0;   // tiles and segments of the stream, tiles of the CTA so far
         bool ok = true;
 #pragma unroll 1
@@ -1014,7 +1022,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 if (ns > 0 && !(ok = ptx::mbar_wait_warp(bar_o_empty + 8 * x, (ns - 1u) & 1u, abort_flag))) break;
                 ++ns;
                 const bool none = l == 0.f && fresh;   // (a row of NaN logits has a sum that is NaN)
-                meta->stats[x][row] = make_float2(none ? 0.f : 1.f / l, none ? -CUDART_INF_F : (fresh ? 0.f : m_ref) + log2f(l));
+                meta->stats[x][row] = make_float2(none ? 0.f : (kQ4 ? q4::kSmall : 1.f) / l, none ? -CUDART_INF_F : (fresh ? 0.f : m_ref) + log2f(l));
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar_l_full + 8 * x);
             }

@@ -52,6 +52,16 @@ __device__ __forceinline__ void values(uint32_t w, uint32_t f, uint32_t (&r)[4])
     r[2] = mul_bf16x2(mul_bf16x2(r[2], 0x7b807b80u), f);
     r[3] = mul_bf16x2(mul_bf16x2(r[3], 0x79807980u), f);
 }
+// The values times 2^-48, from the scale in both halves of s: one product a pair, with 2^85 s or 2^81 s (which are bf16 numbers, s being below 2^40).
+constexpr float kSmall = 0x1p48f;
+__device__ __forceinline__ void small_values(uint32_t w, uint32_t s, uint32_t (&r)[4]) {
+    const uint32_t f0 = mul_bf16x2(s, 0x6a006a00u), f1 = mul_bf16x2(s, 0x68006800u);   // 2^85, 2^81
+    pairs(w, r);
+    r[0] = mul_bf16x2(r[0], f0);
+    r[1] = mul_bf16x2(r[1], f1);
+    r[2] = mul_bf16x2(r[2], f0);
+    r[3] = mul_bf16x2(r[3], f1);
+}
 
 // Where a row of a plane has what: bytes from the plane's start.
 __device__ __forceinline__ int codes_at(int D, int t) { return t * (D / 2); }
