@@ -428,11 +428,13 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
     }
 }
 
-template <typename T, int D, int NT, bool kTok, bool kQ4>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kQ4))
+// kBits: 0; over a cache in four bits 1, or 2 where there are four rows at most
+template <typename T, int D, int NT, bool kTok, int kBits>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kBits != 0))
 paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
              T *__restrict__ out, float *__restrict__ lse) {
     constexpr int R = 16;                 // rows of a partial result
+    constexpr bool kQ4 = kBits != 0;
     // a warp's sums [8 NT][D]; over a cache in four bits they lie over its ring of stages
     extern __shared__ __align__(128) char dyn_sm[];
     constexpr int kRing = kQ4 ? q4::ring_bytes(D, NT) : 0, kSums = kQ4 ? kRing / 4 : 8 * NT * D;
@@ -521,7 +523,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
         const int key_end = min((lo + max(to - kUnitWeight, 0)) << kTileShift, n);
         const Walk walk = {key + kStep * warp, key_end, first, n, head, row_q, a.c.table + (long long)max(s_slot[x], 0) * a.c.width, q_x, rows, window, all_first, all_n};
         if constexpr (kQ4) {
-            q4::attend<D, NT, kTok, kWarps>(q, a, walk, ptx::smem_u32(dyn_sm) + warp * kRing, s_m[warp], s_l[warp], s_o + warp * kSums);
+            q4::attend<D, NT, kTok, kBits == 2, kWarps>(q, a, walk, ptx::smem_u32(dyn_sm) + warp * kRing, s_m[warp], s_l[warp], s_o + warp * kSums);
         } else if constexpr (kF32) {
             // (s_q: the segment before has been joined)
             for (int c = tid; c < D * 8 * NT; c += kThreads) {
@@ -635,24 +637,25 @@ void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2, q4::is(a.c)) * sm_count;
 }
 
-template <typename T, int D, int NT, bool kTok, bool kQ4>
+template <typename T, int D, int NT, bool kTok, int kBits>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
+    constexpr bool kQ4 = kBits != 0;
     constexpr size_t kRing = kQ4 ? kWarps * q4::ring_bytes(D, NT) : 0;
     if (kQ4) {
         static bool allowed[64] = {};
         int dev = 0;
         e = cudaGetDevice(&dev);
         if (e == cudaSuccess && (dev >= 64 || !allowed[dev])) {
-            e = cudaFuncSetAttribute(paged_decode<T, D, NT, kTok, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRing + 1025 * 16);
+            e = cudaFuncSetAttribute(paged_decode<T, D, NT, kTok, kBits>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRing + 1025 * 16);
             if (e == cudaSuccess && dev < 64) allowed[dev] = true;
         }
     }
     constexpr int kMost = max_seqs<T, kQ4>(D, NT);
     for (int x0 = 0; x0 < a.b.n_seqs && e == cudaSuccess; x0 += kMost) {
         const int n = a.b.n_seqs - x0 < kMost ? a.b.n_seqs - x0 : kMost;
-        e = launch_chained(paged_decode<T, D, NT, kTok, kQ4>, dim3(p.n_ctas), dim3(kThreads), kRing + (size_t)(n + 1) * 8 + (size_t)n * 8, st,
+        e = launch_chained(paged_decode<T, D, NT, kTok, kBits>, dim3(p.n_ctas), dim3(kThreads), kRing + (size_t)(n + 1) * 8 + (size_t)n * 8, st,
                            (const T *)q, a, x0, n, parts_at(p, scratch), counters, (T *)out, lse);
         ++*launches;
     }
@@ -662,7 +665,13 @@ static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan 
 template <typename T, int D, bool kQ4>
 static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                               cudaStream_t st, long long *launches) {
-    const bool small = a.b.max_new * a.G <= 8;
+    const int rows = a.b.max_new * a.G;
+    const bool small = rows <= 8;
+    if constexpr (kQ4) {
+        if (rows <= 4)
+            return a.b.max_new == 1 ? decode_of<T, D, 1, false, 2>(q, a, p, scratch, counters, out, lse, st, launches)
+                                    : decode_of<T, D, 1, true, 2>(q, a, p, scratch, counters, out, lse, st, launches);
+    }
     if (a.b.max_new == 1)
         return small ? decode_of<T, D, 1, false, kQ4>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, false, kQ4>(q, a, p, scratch, counters, out, lse, st, launches);
     return small ? decode_of<T, D, 1, true, kQ4>(q, a, p, scratch, counters, out, lse, st, launches) : decode_of<T, D, 2, true, kQ4>(q, a, p, scratch, counters, out, lse, st, launches);

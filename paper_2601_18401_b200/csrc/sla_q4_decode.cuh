@@ -78,10 +78,18 @@ __host__ __device__ constexpr int stage_bytes(int D) { return 2 * kKeys * (D / 2
 // of a warp: its stages, and behind them Q as the products take it
 __host__ __device__ constexpr int ring_bytes(int D, int NT) { return kStages * stage_bytes(D) + NT * D * 16; }
 
-// 8 NT rows at most; Walk, w_m, w_l and w_o as for attend_bf16, w_o over the ring, but the warp takes 32 keys at a time.  A thread (g, c) = (lane / 4,
+// The codes of a stage lie in lines of 128 bytes (two rows, or four of 64 dimensions) of eight pieces of 16 bytes; piece x of line y has the place x ^ mix(y).
+// A warp's loads then meet all banks: those of K have a row's pieces in neighbouring lanes, those of V the rows of four keys in four.
+template <int D> __device__ __forceinline__ uint32_t mix(uint32_t line) { return D == 128 ? 2 * (line >> 1 & 3) : 4 * (line & 1) + (line & 2); }
+
+// 8 NT rows at most, four where kFour; Walk, w_m, w_l and w_o as for attend_bf16, w_o over the ring, but the warp takes 32 keys at a time.  A thread (g, c) = (lane / 4,
 // lane % 4) has of the products' operands (16 keys a step) the keys ka = 4 (g / 2) + g % 2 and kb = ka + 2 of K, S and P, row g of Q (and g + 8) and
 // the values of keys 4 c .. 4 c + 3.
-template <int D, int NT, bool kTok, int kWarps, typename Walk>
+//
+// kFour: the products' eight columns have the four rows twice.  The weights of the first four are scaled for a group, those of the others for the next
+// group, so that one operand P s serves the products of both: of the first group's, columns 0 to 3 are results, of the second's 4 to 7.  Twenty
+// instructions less of the 320 of 16 keys.
+template <int D, int NT, bool kTok, bool kFour, int kWarps, typename Walk>
 __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, const PagedCall &a, const Walk &wk, uint32_t ring, float *w_m, float *w_l, float *w_o) {
     constexpr int N = D / 32, kStride = kKeys * kWarps, S = kKeys / 16, kHalf = 8 * D;   // kHalf: bytes of the codes of 16 rows
     constexpr unsigned kAll = 0xffffffffu;
@@ -93,7 +101,11 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
     const int sl = lane % (D / 8);   // of the scales: 16 bytes a lane, K and then V
     const char *const s_pool = (lane < D / 8 ? a.c.k : a.c.v) + wk.head * a.c.s_h + a.c.P * (D / 2) + sl * 16 - (small && sl >= D / 16 ? D : 0);
     const char *const k_pool = a.c.k + wk.head * a.c.s_h + lane * 16, *const v_pool = a.c.v + wk.head * a.c.s_h + lane * 16;
+    // where a lane's pieces go: of the lines lane / 8 and that + 4, whose places differ
+    const uint32_t code_to[2] = {(lane >> 3) * 128 + ((lane & 7) ^ mix<D>(lane >> 3)) * 16, (lane >> 3) * 128 + ((lane & 7) ^ mix<D>((lane >> 3) + 4)) * 16};
     const uint32_t s_to = ring + (lane < D / 8 ? 0 : stage_bytes(D) / 2) + kKeys * (D / 2) + sl * 16;
+    // the row in column 8 t + x of the products, and those in a thread's columns of their results
+    auto row_of = [&](int t, int x) { return kFour ? x & 3 : 8 * t + x; };
     auto page_at = [&](int k) { return valid_page(a.c, __ldg(wk.table + (k >> a.c.shift))) * a.c.s_page; };
     long long at0 = 0, at1 = 0;
     auto find = [&](int k0) {
@@ -105,18 +117,18 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         if (k0 < key_end) {
             const int t0 = k0 & (a.c.P - 1);
             const long long c0 = at0 + t0 * (D / 2), c1 = small ? at1 : c0 + kHalf;
-            const uint32_t to = ring + st * stage_bytes(D) + lane * 16;
+            const uint32_t to = ring + st * stage_bytes(D);
             const bool two = !small || k0 + 16 < n;   // what lies beyond n is not copied where it has a page of its own
 #pragma unroll
             for (int j = 0; j < N / 2; ++j) {
-                ptx::cp_async16(to + j * 512, k_pool + c0 + j * 512);
-                ptx::cp_async16(to + stage_bytes(D) / 2 + j * 512, v_pool + c0 + j * 512);
+                ptx::cp_async16(to + code_to[j & 1] + j * 512, k_pool + c0 + j * 512);
+                ptx::cp_async16(to + stage_bytes(D) / 2 + code_to[j & 1] + j * 512, v_pool + c0 + j * 512);
             }
             if (two) {
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) {
-                    ptx::cp_async16(to + kHalf + j * 512, k_pool + c1 + j * 512);
-                    ptx::cp_async16(to + stage_bytes(D) / 2 + kHalf + j * 512, v_pool + c1 + j * 512);
+                    ptx::cp_async16(to + code_to[j & 1] + kHalf + j * 512, k_pool + c1 + j * 512);
+                    ptx::cp_async16(to + stage_bytes(D) / 2 + code_to[j & 1] + kHalf + j * 512, v_pool + c1 + j * 512);
                 }
             }
             if (lane < D / 4 && (two || sl < D / 16)) ptx::cp_async16(s_to + st * stage_bytes(D), s_pool + (small && sl >= D / 16 ? at1 : at0 + t0 * (D / 16)));
@@ -136,8 +148,8 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         uint32_t qf[N][4];
-        const bool on = 8 * t + g < (kTok ? wk.rows : G);
-        const int r = on ? 8 * t + g : 0, tok = kTok ? r / G : 0;
+        const bool on = row_of(t, g) < (kTok ? wk.rows : G);
+        const int r = on ? row_of(t, g) : 0, tok = kTok ? r / G : 0;
         const __nv_bfloat16 *src = q + (long long)(wk.row_q + tok) * a.q_st + (long long)(wk.head * G + r - tok * G) * a.q_sh + c * 8;
         uint32_t top = 0;
 #pragma unroll
@@ -173,9 +185,13 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
     }
 
     const uint32_t ka = 4 * (g >> 1) + (g & 1);
-    const uint32_t k_at = ring + ka * (D / 2) + c * 4 * N;
-    const uint32_t v_at = ring + stage_bytes(D) / 2 + 4 * c * (D / 2) + g * 2 * N;
+    // (of 16 s + row, where the rows' numbers add up without carries into what mix() looks at: a line is row * D / 256)
+    constexpr int kLine = 256 / D;   // rows of a line
+    auto code_at = [&](int row, int byte) { return row / kLine * 128u + (((row % kLine * (D / 2) + byte) / 16) ^ mix<D>(row / kLine)) * 16 + byte % 16; };
+    const uint32_t k_at[2] = {ring + code_at(ka, c * 4 * N), ring + code_at(ka + 2, c * 4 * N)};
+    const uint32_t v_at[2] = {ring + stage_bytes(D) / 2 + code_at(4 * c, g * 2 * N), ring + stage_bytes(D) / 2 + code_at(4 * c + 1, g * 2 * N)};
     const uint32_t s_at = ring + kKeys * (D / 2) + ka * (D / 16);
+    const uint32_t four = c < 2 ? 0x1044u : 0x3244u;   // kFour: the columns' scale of a word of two, as a float
     uint32_t st = 0;
 #pragma unroll 1
     for (; key < key_end; key += kStride) {
@@ -188,7 +204,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                load_shared(k_at + of + (16 * s + 2 * h) * (D / 2), kw[s][h]);
+                load_shared(k_at[h] + of + 16 * s * (D / 2), kw[s][h]);
                 load_shared(s_at + of + (16 * s + 2 * h) * (D / 16), ks[s][h]);
             }
 #pragma unroll
@@ -244,7 +260,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int u = 0; u < 2; ++u)
-                            if (8 * t + 2 * c + u < lo || 8 * t + 2 * c + u >= hi) y[s][t][2 * h + u] = -CUDART_INF_F;
+                            if (row_of(t, 2 * c + u) < lo || row_of(t, 2 * c + u) >= hi) y[s][t][2 * h + u] = -CUDART_INF_F;
                     const bool part = kTok && hi > 0 && (k < wk.all_first || k >= wk.all_n);
 #pragma unroll
                     for (int w = 0; w < N; ++w) {
@@ -267,7 +283,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
                         for (int u = 0; u < 2; ++u)
 #pragma unroll
                             for (int w = 0; w < N; ++w)
-                                if ((groups >> w & 1) && 8 * t + 2 * c + u >= lo && 8 * t + 2 * c + u < hi)
+                                if ((groups >> w & 1) && row_of(t, 2 * c + u) >= lo && row_of(t, 2 * c + u) < hi)
                                     acc[t][2 * w][u] = acc[t][2 * w][u + 2] = acc[t][2 * w + 1][u] = acc[t][2 * w + 1][u + 2] = CUDART_NAN_F;
                 }
             }
@@ -320,19 +336,27 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
                 }
             uint32_t vw[4][N / 2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_shared(v_at + of + (16 * s + i) * (D / 2), vw[i]);
+            for (int i = 0; i < 4; ++i) load_shared(D == 128 ? v_at[i & 1] + of + (16 * s + (i & 2)) * (D / 2) : (v_at[i & 1] ^ (i & 2) * 32) + of + 16 * s * (D / 2), vw[i]);
+            uint32_t b0[NT], b1[NT];   // P s
 #pragma unroll
             for (int w = 0; w < N; ++w) {
                 uint32_t ra[4], rb[4];   // codes of keys 4 c, 4 c + 1; of 4 c + 2, 4 c + 3
                 const uint32_t sel = w & 1 ? 0x7632u : 0x5410u;
                 pairs(__byte_perm(vw[0][w >> 1], vw[1][w >> 1], sel), ra);
                 pairs(__byte_perm(vw[2][w >> 1], vw[3][w >> 1], sel), rb);
-                const float sa = half_of(vs[s][0][w >> 1], w), sb = half_of(vs[s][1][w >> 1], w);
+                if (!kFour || w % 2 == 0) {
+                    const float sa = kFour ? __uint_as_float(__byte_perm(vs[s][0][w >> 1], 0, four)) : half_of(vs[s][0][w >> 1], w);
+                    const float sb = kFour ? __uint_as_float(__byte_perm(vs[s][1][w >> 1], 0, four)) : half_of(vs[s][1][w >> 1], w);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        b0[t] = transpose(pack(y[s][t][0] * sa, y[s][t][1] * sa));
+                        b1[t] = transpose(pack(y[s][t][2] * sb, y[s][t][3] * sb));
+                    }
+                }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const uint32_t b0 = transpose(pack(y[s][t][0] * sa, y[s][t][1] * sa)), b1 = transpose(pack(y[s][t][2] * sb, y[s][t][3] * sb));
-                    mma(acc[t][2 * w], ra[0], ra[1], rb[0], rb[1], b0, b1);
-                    mma(acc[t][2 * w + 1], ra[2], ra[3], rb[2], rb[3], b0, b1);
+                    mma(acc[t][2 * w], ra[0], ra[1], rb[0], rb[1], b0[t], b1[t]);
+                    mma(acc[t][2 * w + 1], ra[2], ra[3], rb[2], rb[3], b0[t], b1[t]);
                 }
             }
         }
@@ -348,19 +372,21 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int r = 8 * t + 2 * c + u;
+            const int r = row_of(t, 2 * c + u);
             float v = l[t][u];
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) v += __shfl_xor_sync(kAll, v, off);
-            if (g == 0) { w_m[r] = m[t][u]; w_l[r] = v * 0x1p-78f; }
+            if (g == 0 && (!kFour || c < 2)) { w_m[r] = m[t][u]; w_l[r] = v * 0x1p-78f; }
 #pragma unroll
-            for (int w = 0; w < N; ++w)
+            for (int w = 0; w < N; ++w) {
+                if (kFour && (w & 1) != (c >> 1)) continue;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float *o = w_o + r * D + 32 * w + 8 * (g >> 1) + (g & 1) + 4 * i;
                     o[0] = acc[t][2 * w + i][u] * 0x1p55f;
                     o[2] = acc[t][2 * w + i][u + 2] * 0x1p51f;
                 }
+            }
         }
 }
 
