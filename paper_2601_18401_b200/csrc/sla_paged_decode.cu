@@ -40,12 +40,12 @@ namespace sla {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-// resident CTAs an SM: two where 16 heads of 128 dimensions fill the registers; over a cache in four bits
-#ifndef Q4C1
-#define Q4C1 3
-#define Q4C2 2
-#endif
-__host__ __device__ constexpr int ctas_per_sm(int D, int NT, bool q4) { return q4 ? (NT == 2 ? Q4C2 : Q4C1) : D == 128 && NT == 2 ? 2 : 3; }
+// resident CTAs an SM: two where 16 heads of 128 dimensions fill the registers (over a cache in four bits for 64 dimensions too; 16 warps of 128
+// registers there, or 12 where there are 16 rows, were not faster: 32 sequences of 1000 to 65536 102.4 us against 101.2, 4 new tokens each 168 and 168)
+__host__ __device__ constexpr int ctas_per_sm(int D, int NT, bool q4) { return NT == 2 && (D == 128 || q4) ? 2 : 3; }
+// What a unit costs beyond its tiles over a cache in four bits, in tiles: more than in bf16, since these take less time.  32 sequences of 1000 to 65536:
+// 101 us with 2, 97.2 with 4, 96.2 with 6, 97.1 with 9; with 4 new tokens each 168, 161, 153 and 148.
+__host__ __device__ constexpr int q4_unit_weight(int NT) { return NT == 2 ? 9 : 6; }
 // sequences of a launch: as many as there is room for (16 bytes each) beside the kernel's arrays in 48 KB
 template <typename T, bool kQ4> constexpr int max_seqs(int D, int NT) {
     if (kQ4) return 1024;   // (its arrays are dynamic too)
@@ -435,6 +435,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
              T *__restrict__ out, float *__restrict__ lse) {
     constexpr int R = 16;                 // rows of a partial result
     constexpr bool kQ4 = kBits != 0;
+    constexpr int kUnit = kQ4 ? q4_unit_weight(NT) : kUnitWeight;   // what a unit costs beyond its tiles
     // a warp's sums [8 NT][D]; over a cache in four bits they lie over its ring of stages
     extern __shared__ __align__(128) char dyn_sm[];
     constexpr int kRing = kQ4 ? q4::ring_bytes(D, NT) : 0, kSums = kQ4 ? kRing / 4 : 8 * NT * D;
@@ -472,7 +473,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                     const int q_x = kTok ? hi - lo : 1;
                     if (hi - lo > a.b.max_new) atomicOr(a.c.status, kStatusBadIndex);   // (no more than max_new of its rows are computed)
                     unit_tiles(n, q_x, 0, q_x, a.window, kTileShift, lo, hi);
-                    w = (long long)(hi - lo + kUnitWeight) * a.c.Hkv;
+                    w = (long long)(hi - lo + kUnit) * a.c.Hkv;
                 }
             }
 #pragma unroll
@@ -519,8 +520,8 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
         // keys seen by any row [first, n), by all rows [all_first, all_n)
         const int window = a.window > 0 && a.window < n ? a.window : 0;
         const int all_first = window > 0 ? n - window : 0, all_n = n - q_x + 1, first = max(all_first - q_x + 1, 0);
-        const int key = max((lo + max(from - kUnitWeight, 0)) << kTileShift, first & ~(kStep - 1));
-        const int key_end = min((lo + max(to - kUnitWeight, 0)) << kTileShift, n);
+        const int key = max((lo + max(from - kUnit, 0)) << kTileShift, first & ~(kStep - 1));
+        const int key_end = min((lo + max(to - kUnit, 0)) << kTileShift, n);
         const Walk walk = {key + kStep * warp, key_end, first, n, head, row_q, a.c.table + (long long)max(s_slot[x], 0) * a.c.width, q_x, rows, window, all_first, all_n};
         if constexpr (kQ4) {
             q4::attend<D, NT, kTok, kBits == 2, kWarps>(q, a, walk, ptx::smem_u32(dyn_sm) + warp * kRing, s_m[warp], s_l[warp], s_o + warp * kSums);

@@ -70,10 +70,7 @@ __device__ __forceinline__ uint32_t transpose(uint32_t x) {   // of an 8 x 8 mat
 
 constexpr float kLift = 78.f;    // log2 of what the weights are multiplied by
 constexpr int kKeys = 32;        // of a stage
-#ifndef Q4ST
-#define Q4ST 2
-#endif
-constexpr int kStages = Q4ST;
+constexpr int kStages = 2;       // (three: 32 sequences of 1000 to 65536 no faster)
 __host__ __device__ constexpr int stage_bytes(int D) { return 2 * kKeys * (D / 2 + D / 16); }   // K codes, K scales, V codes, V scales
 // of a warp: its stages, and behind them Q as the products take it
 __host__ __device__ constexpr int ring_bytes(int D, int NT) { return kStages * stage_bytes(D) + NT * D * 16; }
@@ -91,7 +88,7 @@ template <int D> __device__ __forceinline__ uint32_t mix(uint32_t line) { return
 // instructions less of the 320 of 16 keys.
 template <int D, int NT, bool kTok, bool kFour, int kWarps, typename Walk>
 __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, const PagedCall &a, const Walk &wk, uint32_t ring, float *w_m, float *w_l, float *w_o) {
-    constexpr int N = D / 32, kStride = kKeys * kWarps, S = kKeys / 16, kHalf = 8 * D;   // kHalf: bytes of the codes of 16 rows
+    constexpr int N = D / 32, kStride = kKeys * kWarps, S = kKeys / 16;
     constexpr unsigned kAll = 0xffffffffu;
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int G = a.G, first = wk.first, n = wk.n, key_end = wk.key_end;
@@ -115,23 +112,27 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
     };
     auto fill = [&](int k0, uint32_t st) {
         if (k0 < key_end) {
-            const int t0 = k0 & (a.c.P - 1);
-            const long long c0 = at0 + t0 * (D / 2), c1 = small ? at1 : c0 + kHalf;
-            const uint32_t to = ring + st * stage_bytes(D);
-            const bool two = !small || k0 + 16 < n;   // what lies beyond n is not copied where it has a page of its own
+            const uint32_t to = ring + st * stage_bytes(D), v_to = to + stage_bytes(D) / 2;
+            if (!small) {
+                const int t0 = k0 & (a.c.P - 1);
+                const char *const k_src = k_pool + at0 + t0 * (D / 2), *const v_src = v_pool + at0 + t0 * (D / 2);
 #pragma unroll
-            for (int j = 0; j < N / 2; ++j) {
-                ptx::cp_async16(to + code_to[j & 1] + j * 512, k_pool + c0 + j * 512);
-                ptx::cp_async16(to + stage_bytes(D) / 2 + code_to[j & 1] + j * 512, v_pool + c0 + j * 512);
-            }
-            if (two) {
-#pragma unroll
-                for (int j = 0; j < N / 2; ++j) {
-                    ptx::cp_async16(to + code_to[j & 1] + kHalf + j * 512, k_pool + c1 + j * 512);
-                    ptx::cp_async16(to + stage_bytes(D) / 2 + code_to[j & 1] + kHalf + j * 512, v_pool + c1 + j * 512);
+                for (int j = 0; j < N; ++j) {
+                    ptx::cp_async16(to + code_to[j & (N / 2 - 1)] + j * 512, k_src + j * 512);
+                    ptx::cp_async16(v_to + code_to[j & (N / 2 - 1)] + j * 512, v_src + j * 512);
                 }
+                if (D == 128 || lane < D / 4) ptx::cp_async16(s_to + st * stage_bytes(D), s_pool + at0 + t0 * (D / 16));
+            } else {
+                const bool two = k0 + 16 < n;   // what lies beyond n is not copied where it has a page of its own
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (j < N / 2 || two) {
+                        const long long from = (j < N / 2 ? at0 : at1) + (j & (N / 2 - 1)) * 512;
+                        ptx::cp_async16(to + code_to[j & (N / 2 - 1)] + j * 512, k_pool + from);
+                        ptx::cp_async16(v_to + code_to[j & (N / 2 - 1)] + j * 512, v_pool + from);
+                    }
+                if (lane < D / 4 && (sl < D / 16 || two)) ptx::cp_async16(s_to + st * stage_bytes(D), s_pool + (sl < D / 16 ? at0 : at1));
             }
-            if (lane < D / 4 && (two || sl < D / 16)) ptx::cp_async16(s_to + st * stage_bytes(D), s_pool + (small && sl >= D / 16 ? at1 : at0 + t0 * (D / 16)));
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -144,7 +145,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
     find(key + kStages * kStride);
     const uint32_t q_at = ring + kStages * stage_bytes(D) + lane * 16;   // (a lane reads what it wrote)
     // [t][e]: row 8 t + 2 c + e
-    float m[NT][2], l[NT][2], lim[NT][2], mult[NT][2], acc[NT][2 * N][4];
+    float m[NT][2], l[NT][2], lim[NT][2], base[NT][2], mult[NT][2], acc[NT][2 * N][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         uint32_t qf[N][4];
@@ -176,6 +177,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         for (int u = 0; u < 2; ++u) {
             mult[t][u] = __shfl_sync(kAll, back, 4 * (2 * c + u));
             m[t][u] = lim[t][u] = -CUDART_INF_F;
+            base[t][u] = kLift;
             l[t][u] = 0.f;
         }
 #pragma unroll
@@ -199,25 +201,23 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         __syncwarp();   // every lane's copies are there
         const uint32_t of = st * stage_bytes(D);
         float y[S][NT][4];   // [s][t][2 h + e]: key 16 s + ka + 2 h, row 8 t + 2 c + e
-        uint32_t kw[S][2][N], ks[S][2][N / 2];
 #pragma unroll
-        for (int s = 0; s < S; ++s)
+        for (int s = 0; s < S; ++s) {
+            uint32_t kw[2][N], ks[2][N / 2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                load_shared(k_at[h] + of + 16 * s * (D / 2), kw[s][h]);
-                load_shared(s_at + of + (16 * s + 2 * h) * (D / 16), ks[s][h]);
+                load_shared(k_at[h] + of + 16 * s * (D / 2), kw[h]);
+                load_shared(s_at + of + (16 * s + 2 * h) * (D / 16), ks[h]);
             }
 #pragma unroll
-        for (int w = 0; w < N; ++w) {
-            uint32_t qf[NT][4];
+            for (int w = 0; w < N; ++w) {
+                uint32_t qf[NT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) load_shared(q_at + (t * N + w) * 512, qf[t]);
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
+                for (int t = 0; t < NT; ++t) load_shared(q_at + (t * N + w) * 512, qf[t]);
                 uint32_t ra[4], rb[4];
-                pairs(kw[s][0][w], ra);
-                pairs(kw[s][1][w], rb);
-                const float sa = half_of(ks[s][0][w >> 1], w), sb = half_of(ks[s][1][w >> 1], w);
+                pairs(kw[0][w], ra);
+                pairs(kw[1][w], rb);
+                const float sa = half_of(ks[0][w >> 1], w), sb = half_of(ks[1][w >> 1], w);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     float d[4];
@@ -233,11 +233,10 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const float base = kLift - (m[t][u] == -CUDART_INF_F ? 0.f : m[t][u]);
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    y[s][t][u] = fmaf(y[s][t][u], mult[t][u], base);
-                    y[s][t][u + 2] = fmaf(y[s][t][u + 2], mult[t][u], base);
+                    y[s][t][u] = fmaf(y[s][t][u], mult[t][u], base[t][u]);
+                    y[s][t][u + 2] = fmaf(y[s][t][u + 2], mult[t][u], base[t][u]);
                 }
             }
         uint32_t vs[S][2][N / 2];
@@ -304,7 +303,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float was = m[t][u] == -CUDART_INF_F ? 0.f : m[t][u];
+                    const float was = kLift - base[t][u];
                     float top = up[t][u];
 #pragma unroll
                     for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, off));
@@ -312,6 +311,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
                     const float keep = m[t][u] == mx ? 1.f : ex2(m[t][u] - mx), by = mx == -CUDART_INF_F ? 0.f : was - mx;
                     m[t][u] = mx;
                     lim[t][u] = mx == -CUDART_INF_F ? mx : kLift + 8.f;
+                    base[t][u] = kLift - (mx == -CUDART_INF_F ? 0.f : mx);
                     l[t][u] *= keep;
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
