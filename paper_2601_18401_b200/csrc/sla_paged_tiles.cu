@@ -28,6 +28,13 @@
 // beyond the sequence's end (a page's stale rest) and look at the others; what is not finite is cleared too, and added to O of the
 // rows that see its key when the segment's products are done (add_not_finite).
 //
+// A cache in four bits (kQ4): warp 14 brings pages of codes and scales (bulk copies) into a ring of their own, and the warps that write results make
+// bf16 tiles of them, K and V in turn, where the copies would have put them: values times 2^-48, exact, one product a pair of codes (sla_q4.cuh).
+// The ring of tiles is shorter by one.  8192 tokens that end at 65536 in 8.9 ms, 930 TFLOP/s; 1999 at 30011 in 1.09 ms, 870; 64 at 65536 in 109 us; four
+// prompts of about 2000 tokens at D 64 in 180 us.  What costs the rest against bf16 are the issue slots and registers of those four warps: about 600
+// instructions a tile, which one warp on each scheduler takes about 3500 cycles for.  (Eight warps of 48 registers: 10.1 ms; codes read from
+// global memory into registers a tile ahead: 1999 at 30011 1.18 ms, 1 to 600 tokens of 16 sequences 91 us instead of 84.)
+//
 // Every wait on an mbarrier is bounded; when one runs out the CTA sets a status bit, drains and leaves.  The ranges that it had not
 // finished handing out stay without a cut (paged_plan has set them so): no unit that begins in them is joined.
 #include <cuda.h>
@@ -59,7 +66,10 @@ constexpr float kRescaleThreshold = 8.f;     // log2 units
 // The streams' products are kept at least this many cycles apart.  A stream's tile takes about 3400 cycles of which 1000 are products and 1200
 // exponentials; where both streams come to the same pipe at the same time it takes 4000, and nothing moves them apart again.  (Found at D 128; at
 // D 64, whose products take half, 700 to 1700 were tried and none was better.)
-constexpr uint32_t kApart = 1300;
+// Over a cache in four bits the warps that make K and V take a share of the issue slots, and less is better (D 128, 8192 tokens that end at 65536, 1999 at
+// 30011 and 512 at 65536: 8.92 ms, 1108 and 634 us with 1300; 8.87, 1093 and 622 with 1150; 8.96, 1078 and 616 with 1000; 9.23, 1069 and 644 with
+// 800.  D 64, one prompt of 8192: 549 us with 1300, 515 with 800, 513 with 600).
+template <int D, bool kQ4> constexpr uint32_t kApart = !kQ4 ? 1300 : D == 128 ? 1100 : 700;
 constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns, those whose exponentials go to the FMA pipe
 // Tiles whose products a stream adds up in TMEM before O is moved to a sum in memory: the tensor cores cut what does not fit into 24 bits, always
 // towards zero, so that values of one sign come out too small by about 2^-24 for every 16 keys.  Over 2^20, 2^22 and 2^24 keys of like weight
@@ -67,17 +77,16 @@ constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns,
 // whose tables and windows reach further take the kernel that does so (kLong): its loop costs 1 to 3 % (1 to 600 tokens of 16 sequences 61.9 us
 // instead of 60.2, 1999 at 30011 988 instead of 980, 2400 at 2^20 nothing that can be told from noise).
 constexpr int kFoldTiles = 512;
-// (four bits: the warps that make K and V hold the codes of a tile of both; 8192 tokens that end at 65536 8.65 ms so, 8.75 with 176 and 80, 8.97 with
-// 184 and 72)
-template <bool kQ4> constexpr int kRegsRow = kQ4 ? 168 : 184;
-template <bool kQ4> constexpr int kRegsRest = kQ4 ? 88 : 72;
-static_assert(kRegsRow<false> + kRegsRest<false> <= 2 * 128 && kRegsRow<true> + kRegsRest<true> <= 2 * 128, "more registers than the block is launched with");
+constexpr int kRegsRow = 184, kRegsRest = 72;
+static_assert(2 * kRegsRow + 2 * kRegsRest <= 4 * 128, "more registers than the block is launched with");
 
-template <int D> struct Layout {
+template <int D, bool kQ4> struct Layout {
     static constexpr int kHalves = D / 64;                  // 64-column halves of a tile, 128 rows x 128 B each
     static constexpr int kTileBytes = kKeys * D * 2, kHalfBytes = kKeys * 128;
-    static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int kOffQ = 0, kOffKV = 2 * kTileBytes, kOffMeta = kOffKV + kStages * kTileBytes;
+    static constexpr int kStages = D == 128 ? (kQ4 ? 4 : 5) : 10;
+    // four bits: codes and scales of a tile of K or V, as its pages have them
+    static constexpr int kSlots = D == 128 ? 3 : 6, kSlotBytes = kQ4 ? kKeys * (D / 2 + D / 16) : 0;
+    static constexpr int kOffQ = 0, kOffKV = 2 * kTileBytes, kOffCodes = kOffKV + kStages * kTileBytes, kOffMeta = kOffCodes + kSlots * kSlotBytes;
     static constexpr int kSmem = kOffMeta + 3072;
 };
 
@@ -100,7 +109,7 @@ static_assert(sizeof(Seg) == 96, "six 16-byte words");
 
 struct Meta {
     unsigned long long q_full[2], q_empty[2], kv_full[10], kv_empty[2][10], s_full[2], p_ready[2][2], l_full[2], o_full[2], o_empty[2],
-        seg_full[kSegs], seg_empty[kSegs], checked[2];
+        seg_full[kSegs], seg_empty[kSegs], checked[2], code_full[6], code_empty[6];
     uint32_t tmem_base;
     int abort_flag;
     uint32_t s_time[2];               // clock at the stream's last S
@@ -192,13 +201,13 @@ __device__ __forceinline__ uint32_t segment_polls(int tiles) { return ptx::kSpin
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((((w & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu; }
 
 // Clears what is not finite in the row of 128 bytes at v (and in the next half's).
-template <int D>
+template <int D, bool kQ4>
 __device__ __noinline__ void clear_not_finite(uint4 *v) {
 #pragma unroll 1
     for (int h = 0; h < D / 64; ++h)
 #pragma unroll 1
         for (int c = 0; c < 8; ++c) {
-            uint4 &w = v[h * (Layout<D>::kHalfBytes / 16) + c];
+            uint4 &w = v[h * (Layout<D, kQ4>::kHalfBytes / 16) + c];
             w = make_uint4(w.x & ~not_finite(w.x), w.y & ~not_finite(w.y), w.z & ~not_finite(w.z), w.w & ~not_finite(w.w));
         }
 }
@@ -327,46 +336,57 @@ __device__ __noinline__ void add_not_finite(const TileParams &p, const Seg &s, i
     ptx::tc_fence_before();
 }
 
-// A cache in four bits: the warps that write results make K and V of it in the ring.  A warp has 32 rows of a tile, which lie in one page or in two of
-// 16 tokens; a lane takes 16 bytes of codes of kItems of them, neighbouring lanes a row's pieces, and requests them a tile of K (or V) ahead.  The
-// rows of eight neighbouring lanes differ where the swizzle of the tiles wants it: their 16-byte stores meet all banks.
+// A cache in four bits: bulk copies bring a tile's codes and scales to shared memory, page after page; the warps that write results make K and V of them
+// in the ring.  A warp has 32 rows of a tile; a lane takes 16 bytes of codes of kItems of them, neighbouring lanes a row's pieces.  The
+// rows of eight neighbouring lanes are such that both their loads and, through the swizzle of the tiles, their 16-byte stores meet all banks.
 template <int D> struct Codes {
     static constexpr int kItems = D / 32, kLanes = D / 32, kRows = 32 / kLanes, kHalf = kItems / 2;   // of a lane; lanes of a row; rows of an item; items of 16 rows
-    uint4 w[kItems];
-    uint2 s[kItems];   // scales
-    // codes, scales: where the lane's first row of either half of 16 has them, from pool.  left: of the lane's rows those below it count, what lies
-    // behind them may be anything.
-    __device__ __forceinline__ void load(const char *pool, const long long (&codes)[2], const long long (&scales)[2], int left) {
+    uint32_t codes[2], scales[2];   // where the lane's first row of either half of its warp's 32 has them, from the slot's start
+    uint32_t to;                    // where its first piece goes, from the tile's start
+    int row0;
+
+    __device__ __forceinline__ Codes(int page, int warp) {   // (warp: of the four)
+        const int lane = threadIdx.x & 31, idx = lane / kLanes, chunk = min(page, kKeys), bytes = q4::plane_bytes(chunk, D);
+        row0 = D == 128 ? 5 * (idx & 1) ^ (idx & 2) ^ (idx >> 2 & 1) : 5 * (idx & 1) ^ 3 * (idx & 2) ^ (idx >> 2 & 1) ^ (idx & 8);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 32 * warp + 16 * h + row0, t = r & (chunk - 1);
+            codes[h] = r / chunk * bytes + q4::codes_at(D, t) + lane % kLanes * 16;
+            scales[h] = r / chunk * bytes + q4::scales_at(chunk, D, t);
+        }
+        to = (32 * warp + row0) * 128 + ((D == 128 ? lane % 4 : 2 * (lane % 2)) ^ (row0 & 7)) * 16;
+    }
+    uint32_t w[kItems][4], sc[kItems][D / 64];
+
+    // A tile's codes and scales out of the slot at `slot`.  left: rows of the warp that count; those behind them may be anything and become zero.
+    __device__ __forceinline__ void load(uint32_t slot, int left) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const int h = i / kHalf, e = i % kHalf * kRows;
-            w[i] = __ldg(reinterpret_cast<const uint4 *>(pool + codes[h] + e * (D / 2)));
-            if constexpr (D == 128) s[i] = __ldg(reinterpret_cast<const uint2 *>(pool + scales[h] + e * (D / 16)));
-            else s[i].x = __ldg(reinterpret_cast<const uint32_t *>(pool + scales[h] + e * (D / 16)));
+            q4::load_shared(slot + codes[h] + e * (D / 2), w[i]);
+            q4::load_shared(slot + scales[h] + e * (D / 16), sc[i]);
         }
         if (left < 32) {
 #pragma unroll
             for (int i = 0; i < kItems; ++i)
-                if (i * kRows >= left) s[i] = make_uint2(0, 0);
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) sc[i][x] = i * kRows + row0 < left ? sc[i][x] : 0;
         }
     }
-    // to: where the lane's first piece goes in its first row
-    template <bool kValues> __device__ __forceinline__ void store(uint32_t to) const {
+    // K or V of it to the tile at `tile`.
+    template <bool kValues> __device__ __forceinline__ void store(uint32_t tile) const {
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const uint32_t word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        for (int i = 0; i < kItems; ++i)
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
                 // the piece of eight dimensions: group, and which of the group's four
                 const int g = D == 128 ? x : x & 1, up = D == 128 ? 0 : x >> 1;
                 const uint32_t sel = x & 1 ? 0x7632u : 0x5410u;
-                const uint32_t codes = !kValues ? word[x] : D == 128 ? __byte_perm(word[x >> 1], word[2 + (x >> 1)], sel) : __byte_perm(word[2 * (x >> 1)], word[2 * (x >> 1) + 1], sel);
-                const uint32_t sc = g & 2 ? s[i].y : s[i].x;
+                const uint32_t word = !kValues ? w[i][x] : D == 128 ? __byte_perm(w[i][x >> 1], w[i][2 + (x >> 1)], sel) : __byte_perm(w[i][2 * (x >> 1)], w[i][2 * (x >> 1) + 1], sel);
                 uint32_t v[4];
-                q4::small_values(codes, g & 1 ? __byte_perm(sc, 0, 0x3232) : __byte_perm(sc, 0, 0x1010), v);
-                ptx::st_shared_v4((to ^ ((g & 1) * 64 + up * 16)) + (g >> 1) * Layout<D>::kHalfBytes + i * kRows * 128, v);
+                q4::small_values(word, __byte_perm(sc[i][g >> 1], 0, g & 1 ? 0x3232 : 0x1010), v);
+                ptx::st_shared_v4(((tile + to) ^ ((g & 1) * 64 + up * 16)) + (g >> 1) * Layout<D, true>::kHalfBytes + i * kRows * 128, v);
             }
-        }
     }
 };
 
@@ -374,7 +394,7 @@ template <int D, bool kLong, bool kQ4>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
             const __grid_constant__ TileParams p) {
-    using L = Layout<D>;
+    using L = Layout<D, kQ4>;
     constexpr int kStages = L::kStages, kHalves = L::kHalves;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = ptx::smem_u32(smem);
@@ -391,6 +411,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
     const uint32_t bar_s_full = mbase + offsetof(Meta, s_full), bar_p_ready = mbase + offsetof(Meta, p_ready);
     const uint32_t bar_l_full = mbase + offsetof(Meta, l_full), bar_o_full = mbase + offsetof(Meta, o_full);
     const uint32_t bar_o_empty = mbase + offsetof(Meta, o_empty), bar_checked = mbase + offsetof(Meta, checked);
+    const uint32_t bar_code_full = mbase + offsetof(Meta, code_full), bar_code_empty = mbase + offsetof(Meta, code_empty);
     const uint32_t bar_seg_full = mbase + offsetof(Meta, seg_full), bar_seg_empty = mbase + offsetof(Meta, seg_empty);
 
     if (tid == 0) {
@@ -415,7 +436,14 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
         for (int s = 0; s < kSegs; ++s) {
             ptx::mbar_init(bar_seg_full + 8 * s, 1);
-            ptx::mbar_init(bar_seg_empty + 8 * s, (kQ4 ? 12 : 13) + 2 * 32);   // rows, epilogue, K/V: a warp each; the issuers a lane each
+            ptx::mbar_init(bar_seg_empty + 8 * s, 13 + 2 * 32);   // rows, epilogue, K/V: a warp each; the issuers a lane each
+        }
+        if constexpr (kQ4) {
+#pragma unroll 1
+            for (int s = 0; s < L::kSlots; ++s) {
+                ptx::mbar_init(bar_code_full + 8 * s, 1);
+                ptx::mbar_init(bar_code_empty + 8 * s, 4);
+            }
         }
         meta->abort_flag = 0;
         meta->s_time[0] = meta->s_time[1] = clock();
@@ -444,7 +472,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
     };
 
     if (warp >= 12) {
-        ptx::setmaxnreg_dec<kRegsRest<kQ4>>();
+        ptx::setmaxnreg_dec<kRegsRest>();
         if (warp < 14) {
             // ---------------- MMA issuer of stream x: a whole warp, its elected lane issues.  S of the next tile goes right behind
             // the PV of this one, which reads the P that lies over it (the tensor pipe keeps a thread's order).
@@ -480,7 +508,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                             volatile uint32_t *s_time = meta->s_time;
                             const uint32_t other = s_time[1 - x];
                             uint32_t now;
-                            do now = clock(); while (now - other < kApart);
+                            do now = clock(); while (now - other < kApart<D, kQ4>);
                             s_time[x] = now;
                         }
                         const uint64_t dk = desc_advance(dk0, st * L::kTileBytes);
@@ -534,7 +562,49 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                 ptx::mbar_arrive(bar_seg_empty + 8 * (k % kSegs));
             }
         } else if (warp == 14) {
-            if constexpr (!kQ4) {
+            if constexpr (kQ4) {
+            // ---------------- codes and scales of K and V: a lane per page that the tile has
+            const Pages &c = p.a.c;
+            const int chunk = min(c.P, kKeys), bytes = q4::plane_bytes(chunk, D), chunks = kKeys / chunk;
+            uint32_t i = 0;
+            bool ok = true;
+#pragma unroll 1
+            for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) {
+                const Seg &s = meta->seg[k % kSegs];
+                const int tiles = s.hi - s.lo, n = s.n;
+                const int *table = c.table + (long long)max(s.slot, 0) * c.width;
+                auto page_of = [&](int j) {   // -1: no page
+                    const int key = j * kKeys + lane * chunk;
+                    return lane < chunks && key < n ? valid_page(c, __ldg(table + (key >> c.shift))) : -1;
+                };
+                int next = tiles > 0 ? page_of(s.begin) : -1, j_next = s.begin;
+#pragma unroll 1
+                for (int t = 0; t < tiles && ok; ++t) {
+                    const int page = next, t0 = j_next * kKeys & (c.P - 1);   // (pages of 256 tokens: the half)
+                    j_next = s.next(j_next);
+                    next = page_of(j_next);
+                    const uint32_t all = __popc(__ballot_sync(0xffffffffu, page >= 0)) * bytes;
+#pragma unroll 1
+                    for (int kv = 0; kv < 2; ++kv, ++i) {
+                        const uint32_t slot = i % L::kSlots, full = bar_code_full + 8 * slot;
+                        if (!(ok = ptx::mbar_wait_warp(bar_code_empty + 8 * slot, ((i / L::kSlots) & 1u) ^ 1u, abort_flag))) break;
+                        if (lane == 0) ptx::mbar_arrive_expect_tx(full, all);
+                        __syncwarp();
+                        if (page >= 0) {
+                            const char *plane = (kv ? c.v : c.k) + page * c.s_page + s.head * c.s_h;
+                            const uint32_t dst = base + L::kOffCodes + slot * L::kSlotBytes + lane * bytes;
+                            if (chunk == c.P) {
+                                ptx::bulk_load(dst, plane, bytes, full);
+                            } else {
+                                ptx::bulk_load(dst, plane + q4::codes_at(D, t0), chunk * (D / 2), full);
+                                ptx::bulk_load(dst + chunk * (D / 2), plane + q4::scales_at(c.P, D, t0), chunk * (D / 16), full);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+            } else {
             // ---------------- K and V: a lane per box, as many as the tile has pages with tokens
             ptx::prefetch_tensormap(&tm_k);
             ptx::prefetch_tensormap(&tm_v);
@@ -665,7 +735,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
         }
     } else if (warp >= 8) {
         // ---------------- results: a thread a row
-        ptx::setmaxnreg_dec<kRegsRest<kQ4>>();
+        ptx::setmaxnreg_dec<kRegsRest>();
         const int row = tid & 127;
         const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G, canon = t * G + g;
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -763,86 +833,66 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
 #pragma unroll 1
             for (uint32_t k = 0; ok && take_seg(k); free_seg(k++)) results(k);
         } else {
-            // Two tiles of the next segment go into the ring before the results of this one are written: they wait for nothing but this segment's
-            // products.
-            using F = Codes<D>;
-            const int idx = lane / F::kLanes;   // row of an item, mixed so that its low bits differ where the swizzle does
-            const int row0 = D == 128 ? (idx & 1) << 2 | idx >> 1 : (idx & 9) | (idx & 2) << 1 | (idx & 4) >> 1;
-            const uint32_t to = (warp - 8) * 32 * 128 + row0 * 128 + ((D == 128 ? lane % 4 : 2 * (lane % 2)) ^ (row0 & 7)) * 16;
-            const Pages &c = p.a.c;
-            uint32_t i = 0;   // ring position
-            auto fill = [&](uint32_t k, int from, int until) {
-                if (from >= until) return;
+            Codes<D> codes(p.a.c.P, warp - 8);
+            uint32_t i = 0;   // tiles of K and V so far
+            auto make = [&](auto values, int left) {
+                const uint32_t st = i % kStages, ph = ((i / kStages) & 1u) ^ 1u, slot = i % L::kSlots;
+                if (!ptx::mbar_wait_warp(bar_code_full + 8 * slot, (i / L::kSlots) & 1u, abort_flag)) return false;
+                codes.load(base + L::kOffCodes + slot * L::kSlotBytes, left);
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar_code_empty + 8 * slot);
+                if (!ptx::mbar_wait_warp(bar_kv_empty + 8 * st, ph, abort_flag) || !ptx::mbar_wait_warp(bar_kv_empty + 80 + 8 * st, ph, abort_flag)) return false;
+                codes.template store<decltype(values)::value>(base + L::kOffKV + st * L::kTileBytes);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar_kv_full + 8 * st);
+                ++i;
+                return true;
+            };
+            auto make_tiles = [&](uint32_t k, int from, int until) {
                 const Seg &s = meta->seg[k % kSegs];
                 const int n = s.n, lo = s.lo, hi = s.hi;
-                const int *table = c.table + (long long)max(s.slot, 0) * c.width;
-                const char *kp = c.k + s.head * c.s_h, *vp = c.v + s.head * c.s_h;
-                auto after = [&](int j) { return j + 1 < hi ? j + 1 : lo; };
-                auto first_key = [&](int j) { return j * kKeys + (warp - 8) * 32; };
-                // the pages of a tile's rows (behind the sequence page 0, which nobody asks for)
-                auto look = [&](int j, int (&page)[2]) {
-                    const int key = first_key(j);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) page[h] = key + 16 * h < n ? __ldg(table + ((key + 16 * h) >> c.shift)) : 0;
-                };
-                long long codes[2], scales[2];
-                auto place = [&](int j, const int (&page)[2]) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int t = c.P < 32 ? row0 : (first_key(j) & (c.P - 1)) + 16 * h + row0;
-                        const bool there = (unsigned)page[h] < (unsigned)c.n_pages;
-                        if (!there) atomicOr(c.status, kStatusBadIndex);
-                        const long long plane = (there ? page[h] : 0) * c.s_page;
-                        codes[h] = plane + q4::codes_at(D, t) + lane % F::kLanes * 16;
-                        scales[h] = plane + q4::scales_at(c.P, D, t);
-                    }
-                };
-                auto put = [&](auto values, const F &f) {
-                    const uint32_t st = i % kStages, ph = ((i / kStages) & 1u) ^ 1u;
-                    ok = ptx::mbar_wait_warp(bar_kv_empty + 8 * st, ph, abort_flag) && ptx::mbar_wait_warp(bar_kv_empty + 80 + 8 * st, ph, abort_flag);
-                    if (!ok) return;
-                    f.template store<decltype(values)::value>(base + L::kOffKV + st * L::kTileBytes + to);
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(bar_kv_full + 8 * st);
-                    ++i;
-                };
                 int j = s.begin + from;
                 if (j >= hi) j -= hi - lo;
-                int page[2];
-                F kf, vf;
-                look(j, page);
-                place(j, page);
-                kf.load(kp, codes, scales, n - first_key(j) - row0);
-                look(after(j), page);
 #pragma unroll 1
-                for (int t = from; t < until && ok; ++t) {
-                    vf.load(vp, codes, scales, n - first_key(j) - row0);
-                    put(std::false_type{}, kf);
-                    if (!ok) break;
-                    j = after(j);
-                    place(j, page);
-                    kf.load(kp, codes, scales, n - first_key(j) - row0);   // (behind the last tile another one, for nothing)
-                    look(after(j), page);
-                    put(std::true_type{}, vf);
+                for (int t = from; t < until; ++t) {
+                    const int left = n - j * kKeys - 32 * (warp - 8);
+                    if (!make(std::false_type{}, left) || !make(std::true_type{}, left)) return false;
+                    j = j + 1 < hi ? j + 1 : lo;
                 }
+                return true;
             };
             auto tiles_of = [&](uint32_t k) { return meta->seg[k % kSegs].hi - meta->seg[k % kSegs].lo; };
-            int done = 0;
-            bool more = take_seg(0);
+            // The first two tiles of the next segment are made before the results of this one are written: they wait for nothing but this segment's
+            // products.
+            uint32_t k = 0;
+            int from = 0;
+            bool first = true;   // in turn: what is left of segment k; the first tiles of the next k, and the results of the one before
 #pragma unroll 1
-            for (uint32_t k = 0; ok && more; ++k) {
-                fill(k, done, tiles_of(k));
-                more = ok && take_seg(k + 1);
-                done = more ? min(2, tiles_of(k + 1)) : 0;
-                if (more) fill(k + 1, 0, done);
-                if (ok) results(k);
-                free_seg(k);
+            for (bool more = take_seg(0); ok && more;) {   // (one call of make_tiles, which is long)
+                const int until = first ? tiles_of(k) : min(2, tiles_of(k));
+                ok = make_tiles(k, from, until);
+                from = until;
+                if (first) {
+                    more = ok && take_seg(k + 1);
+                    if (more) {
+                        ++k;
+                        from = 0;
+                        first = false;
+                        continue;
+                    }
+                    if (ok) results(k);
+                    free_seg(k);
+                } else {
+                    if (ok) results(k - 1);
+                    free_seg(k - 1);
+                    first = true;
+                }
             }
         }
     } else {
         // ---------------- rows of stream x: a thread a row
-        ptx::setmaxnreg_inc<kRegsRow<kQ4>>();
+        ptx::setmaxnreg_inc<kRegsRow>();
         const int x = warp >> 2, row = tid & 127;
         const int t = p.t_inner ? row % TS : row / G, g = p.t_inner ? row / TS : row % G;
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -981,7 +1031,7 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                                 if (bad) {
                                     *(volatile int *)&meta->odd[0][k & 7] = *(volatile int *)&meta->odd[1][k & 7] = (int)k + 1;
                                     __threadfence_block();
-                                    clear_not_finite<D>(vr);
+                                    clear_not_finite<D, kQ4>(vr);
                                 }
                             }
                             if (clear) {
@@ -1107,7 +1157,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !allowed[dev]) {
-        e = cudaFuncSetAttribute(paged_tiles<D, kLong, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
+        e = cudaFuncSetAttribute(paged_tiles<D, kLong, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D, kQ4>::kSmem);
         if (e != cudaSuccess) return e;
         if (dev < 64) allowed[dev] = true;
     }
@@ -1137,7 +1187,7 @@ cudaError_t tiles_of(const void *q, const PagedCall &a, const PagedPlan &pl, cha
     if (!make_map(&tq, q, D, qd, 2, qbox)) return cudaErrorInvalidValue;
     tk = tv = tq;   // (four bits: not looked at)
     if (!kQ4 && (!make_map(&tk, a.c.k, D, kd, 3, kbox) || !make_map(&tv, a.c.v, D, kd, 3, kbox))) return cudaErrorInvalidValue;
-    return launch_chained(paged_tiles<D, kLong, kQ4>, dim3(pl.n_ctas), dim3(kThreads), Layout<D>::kSmem, st, tq, tk, tv, p);
+    return launch_chained(paged_tiles<D, kLong, kQ4>, dim3(pl.n_ctas), dim3(kThreads), Layout<D, kQ4>::kSmem, st, tq, tk, tv, p);
 }
 
 }  // namespace

@@ -63,6 +63,18 @@ __device__ __forceinline__ void small_values(uint32_t w, uint32_t s, uint32_t (&
     r[3] = mul_bf16x2(r[3], f1);
 }
 
+// N words of shared memory, as wide as they are
+template <int N> __device__ __forceinline__ void load_shared(uint32_t at, uint32_t (&w)[N]) {
+    if constexpr (N == 1) {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+    } else if constexpr (N == 2) {
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4 * i));
+    }
+}
 // Where a row of a plane has what: bytes from the plane's start.
 __device__ __forceinline__ int codes_at(int D, int t) { return t * (D / 2); }
 __device__ __forceinline__ int scales_at(int P, int D, int t) { return P * (D / 2) + t * (D / 16); }

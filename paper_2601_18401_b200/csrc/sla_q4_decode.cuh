@@ -28,18 +28,6 @@
 namespace sla {
 namespace q4 {
 
-// N words of shared memory, as wide as they are
-template <int N> __device__ __forceinline__ void load_shared(uint32_t at, uint32_t (&w)[N]) {
-    if constexpr (N == 1) {
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
-    } else if constexpr (N == 2) {
-        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i += 4)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4 * i));
-    }
-}
 // d += A B, and d = A B
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
