@@ -1033,6 +1033,8 @@ sla_status_t sla_paged_attention(sla_handle_t h, const void *q, const sla_cache_
     if (n_q_heads / c->n_kv_heads > sla::kMaxGroup) return fail(h, SLA_ERR_INVALID_ARG, "group size above 16%s");
     if (window < 0) return fail(h, SLA_ERR_INVALID_ARG, "window must be >= 0%s");
     if (!(softmax_scale == softmax_scale)) return fail(h, SLA_ERR_INVALID_ARG, "scale is NaN%s");
+    // (the kernels multiply it by powers of two that keep the codes' products in range)
+    if (four_bits(c) && !(fabsf(softmax_scale) < 0x1p64f)) return fail(h, SLA_ERR_INVALID_ARG, "scale of 2^64 or more over a cache in four bits%s");
     if (b->n_new == 0) return SLA_OK;
     if (!q || !out || !lse) return fail(h, SLA_ERR_INVALID_ARG, "NULL tensor pointer%s");
     if (!aligned16(q) || !aligned16(out)) return fail(h, SLA_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned%s");

@@ -556,7 +556,7 @@ def test_refusals(sla, handle):
     with pytest.raises(sla.SlaError) as e:
         sla.sla_paged_decode_step(handle, q, q, cache, sla.make_params(4, 0))
     assert e.value.status == -2
-    for bad in (dict(window=-1), dict(softmax_scale=math.nan), dict(max_new=0)):
+    for bad in (dict(window=-1), dict(softmax_scale=math.nan), dict(max_new=0), dict(softmax_scale=2.0 ** 64), dict(softmax_scale=-math.inf)):
         with pytest.raises(sla.SlaError):
             sla.sla_paged_attention(handle, q, cache, cu, **bad)
     with pytest.raises(TypeError):
@@ -587,6 +587,117 @@ def test_refusals(sla, handle):
         PagedCache(8, 2, 64, n_q_heads=8, n_kv_heads=2, four_bits=True, params=sla.make_params(4, 0))
     none = sla.sla_cache_read(handle, cache, U.device_ints([0, 0, 0]), first, n_new=0)
     assert none[0].shape == (0, 2, 128)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,T,G", [((1 << 20) + 777, 2400, 16), (1 << 22, 1, 4), (1 << 21, 2, 8), (600000, 700, 1)])
+def test_long_sums_of_values_of_one_sign(sla, d, n, T, G):
+    """Hundreds of thousands of keys of like weight in a range.  Pages that are the same 64 again and again, so that a key's weight counts as
+    often as a row sees its page.  Bounds as for bf16: each weight and the result rounded to 2^-9 of the value and more, 4096 sums in
+    TMEM cut by 2^-23 each, the tiles' sums in fp32 2^-24 each."""
+    page, n_pages = 256, 64
+    k, v = planes(sla, n_pages, 1, page, d)
+    width = -(-n // page)
+    table = (np.arange(width) % n_pages).astype(np.int32)[None]
+    ints = [U.device_ints(table), U.device_ints([n_pages * page]), U.device_ints(np.zeros(n_pages))]
+    cache = sla.make_cache_q4(k, v, *ints, page_tokens=page, head_dim=d)
+    h = sla.Handle(0, sla.sla_paged_workspace_bytes(cache, G, 1, n_pages * page))
+    sla.sla_cache_append(h, cache, U.device_ints([0, n_pages * page]), U.device_ints([0]), normal((n_pages * page, 1, d), BF16, 1, 0.2),
+                         normal((n_pages * page, 1, d), BF16, 2, 0.2).abs())
+    ints[1].fill_(n)
+    q = normal((T, G, d), BF16, 3, 0.1)
+    sla.sla_set_debug_canaries(h, True)
+    out, lse = sla.sla_paged_attention(h, q, cache, None if T == 1 else U.device_ints([0, T]))
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    kk, vv = (Q.unpack(t[:, 0], page, d, values).reshape(-1, d) for t, values in ((k, False), (v, True)))
+    at = torch.arange(len(kk), device="cuda:0")
+    tol = 2.0 ** -8 + 4096 * 2.0 ** -23 + 2 * (n / 128) * 2.0 ** -24
+    for r in {0, T // 2, T - 1}:
+        seen = n - T + r + 1
+        times = (seen // len(kk) + (at < seen % len(kk))).double()
+        z = q[r].double() @ kk.T * d ** -0.5
+        w = torch.exp(z) * times
+        want = (w @ vv) / w.sum(-1, keepdim=True)
+        assert ((out[r].double() - want).abs() <= tol * want + 2.0 ** -40).all()
+        assert ((lse[r].double() - w.sum(-1).log()).abs() <= tol).all()
+    h.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window", [0, 70000])
+def test_groups_that_are_nan_in_long_ranges(sla, handle, d, window):
+    """Segments of more tiles than one sum in TMEM has, a group that is NaN near the rows' own keys and at the window's beginning."""
+    n, new = 300000, 300
+    for at in (n - 100, n - 400, n - window - 100 if window else 70001):
+        def prep(k, v, table, q):
+            spoil(v, int(table[0, at // 64]), 1, at % 64, 64, d, 5)
+        cache, k, v, table, q, cu = build(sla, [n], [new], d=d, page=64, G=2)
+        clean, clean_lse = sla.sla_paged_attention(handle, q, cache, cu, window=window)
+        prep(k, v, table, q)
+        out, lse = sla.sla_paged_attention(handle, q, cache, cu, window=window)
+        pos = torch.arange(n - new, n, device="cuda:0")
+        sees = (pos >= at) & ((pos - at < window) if window else True)
+        want = clean.clone()
+        want[sees, 2:, :32] = math.nan
+        assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.nan_to_num(9.0), want.nan_to_num(9.0)) and torch.equal(lse, clean_lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_after_a_wait_that_ran_out_no_row_is_written(sla, d):
+    h = sla.Handle(0, 1 << 28)
+    cache, k, v, table, q, cu = build(sla, [9000, 4000, 2500], [70, 300, 129], d=d, page=64)
+    want = sla.sla_paged_attention(h, q, cache, cu, max_new=300)
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda:0")
+    sla.sla_selftest_paged_expiry(h, True)
+    sla.sla_paged_attention(h, q, cache, cu, max_new=300, out=out, lse=lse)
+    sla.sla_selftest_paged_expiry(h, False)
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_TIMEOUT
+    assert (out == 7).all() and (lse == 7).all()
+    again = sla.sla_paged_attention(h, q, cache, cu, max_new=300)
+    assert sla.sla_poll_status(h) == sla.SLA_OK
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+    h.close()
+
+
+def test_two_streams_at_once(sla):
+    """Two handles over one cache, each on its own stream, at the same time."""
+    n, new = [9000, 100, 4000], [40, 50, 300]
+    cache, k, v, table, q, cu = build(sla, n, new, page=64)
+    q1, cu1 = q[:3].contiguous(), cu_of([1, 1, 1])
+    hs = [sla.Handle(0, sla.sla_paged_workspace_bytes(cache, 8, 3, 390)) for _ in range(2)]
+    want = [sla.sla_paged_attention(hs[0], q, cache, cu, max_new=300), sla.sla_paged_attention(hs[0], q1, cache, cu1, max_new=1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for x, (qq, cc, m) in enumerate(((q, cu, 300), (q1, cu1, 1))):
+            with torch.cuda.stream(streams[x]):
+                got[x].append(sla.sla_paged_attention(hs[x], qq, cache, cc, max_new=m))
+    torch.cuda.synchronize()
+    for x in range(2):
+        for o, l in got[x]:
+            assert torch.equal(o, want[x][0]) and torch.equal(l, want[x][1])
+        assert sla.sla_poll_status(hs[x]) == sla.SLA_OK
+        hs[x].close()
+
+
+def test_rows_that_no_sequence_has_stay_as_they_are(sla, handle):
+    """Tensors with more rows than cu_new names: attention, reading and appending leave the rest alone."""
+    cache, k, v, table, q, cu = build(sla, [300, 40], [70, 3])
+    for new, most in (([70, 3], 70), ([1, 1], 1), ([3, 2], 3)):
+        T = sum(new) + 9
+        qq = normal((T, 8, 128), BF16, 5, 0.1)
+        out, lse = torch.full_like(qq, 7.0), torch.full((T, 8), 7.0, device="cuda:0")
+        sla.sla_paged_attention(handle, qq, cache, cu_of(new), max_new=max(most, -(-T // 2)), out=out, lse=lse)
+        assert (out[T - 9:] == 7).all() and (lse[T - 9:] == 7).all() and not (out[: T - 9] == 7).all()
+        ko = torch.full((T, 2, 128), 7.0, dtype=BF16, device="cuda:0")
+        vo = ko.clone()
+        sla.sla_cache_read(handle, cache, cu_of(new), k_out=ko, v_out=vo)
+        assert (ko[T - 9:] == 7).all() and (vo[T - 9:] == 7).all()
+        before = k.clone(), v.clone()
+        sla.sla_cache_append(handle, cache, U.device_ints([0, 0, 0]), U.device_ints([5, 5]), ko, vo)
+        assert torch.equal(k, before[0]) and torch.equal(v, before[1])
 
 
 # ---- together -------------------------------------------------------------------------------------------------------------------------
