@@ -2,9 +2,10 @@
 continuations of a prompt, ends, compaction, and the span decode step for the sequences that have grown long.  The layers share
 the table, the lengths and the counts: room, forks, ends and compaction go once, copies and the rest for every layer.
 
-    python examples/paged_serving.py [--prompts 8] [--chunk 1024] [--steps 32] [--span-from 4096] [--layers 2]
+    python examples/paged_serving.py [--prompts 8] [--chunk 1024] [--steps 32] [--span-from 4096] [--layers 2] [--four-bits]
 
-Prints the tokens that went through and checks the last step against attention over a contiguous copy.
+With --four-bits the caches hold their keys and values in four bits, and there are no span steps.  Prints the tokens that went through and
+checks the last step against attention over what the cache gives back.
 """
 import argparse
 import os
@@ -22,7 +23,7 @@ def ints(values):
     return torch.tensor(values, dtype=torch.int32, device="cuda")
 
 
-def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8, head_dim=128, layers=2, seed=0):
+def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8, head_dim=128, layers=2, seed=0, four_bits=False):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
 
@@ -33,8 +34,8 @@ def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8,
     slots = prompts + 3
     most = max(lengths) + steps + 64
     pages = sum(-(-(n + steps) // 64) + 1 for n in lengths) + 3 * (-(-(lengths[0] + steps) // 64) + 2)
-    params = sla.make_params(8, 0, head_dim=head_dim)
-    shape = dict(n_q_heads=q_heads, n_kv_heads=kv_heads, head_dim=head_dim, max_new=prompts * chunk)
+    params = None if four_bits else sla.make_params(8, 0, head_dim=head_dim)
+    shape = dict(n_q_heads=q_heads, n_kv_heads=kv_heads, head_dim=head_dim, max_new=prompts * chunk, four_bits=four_bits)
     c = PagedCache(pages, slots, most, params=params, **shape)
     caches = [c] + [PagedCache(pages, slots, most, share=c, **shape) for _ in range(layers - 1)]
     done, tokens = [0] * prompts, 0
@@ -66,8 +67,8 @@ def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8,
             for layer in caches[1:]:
                 layer.copy(pairs)
             live[1] = 0
-        short = [s for s in range(slots) if live[s] and live[s] < span_from]
-        long_ = [s for s in range(slots) if live[s] >= span_from]
+        short = [s for s in range(slots) if live[s] and (four_bits or live[s] < span_from)]
+        long_ = [s for s in range(slots) if not four_bits and live[s] >= span_from]
         for group, spans in ((short, False), (long_, True)):
             if not group:
                 continue
@@ -91,9 +92,7 @@ def run(prompts=8, chunk=1024, steps=32, span_from=4096, q_heads=32, kv_heads=8,
     worst = 0.0
     for x, s in enumerate(last[0]):
         n = live[s]
-        rows = c.table[s, : -(-n // 64)].long()
-        k, v = (p[rows].transpose(1, 2).reshape(-1, kv_heads, head_dim)[:n].float().repeat_interleave(q_heads // kv_heads, 1)
-                for p in (caches[-1].k, caches[-1].v))
+        k, v = (t.float().repeat_interleave(q_heads // kv_heads, 1) for t in caches[-1].read(ints([0, n]), seq=ints([s]), n_new=n))
         w = torch.softmax(torch.einsum("hd,jhd->hj", last[1][x].float(), k) * head_dim ** -0.5, -1)
         worst = max(worst, (torch.einsum("hj,jhd->hd", w, v) - last[2][x].float()).abs().max().item())
     assert c.n_tokens.tolist() == live
@@ -107,7 +106,8 @@ if __name__ == "__main__":
     ap.add_argument("--steps", type=int, default=32)
     ap.add_argument("--span-from", type=int, default=4096)
     ap.add_argument("--layers", type=int, default=2)
+    ap.add_argument("--four-bits", action="store_true")
     a = ap.parse_args()
-    r = run(a.prompts, a.chunk, a.steps, a.span_from, layers=a.layers)
+    r = run(a.prompts, a.chunk, a.steps, a.span_from, layers=a.layers, four_bits=a.four_bits)
     assert r["status"] == sla.SLA_OK and r["worst"] < 2e-2, r
     print(f"{r['tokens']} tokens of {a.layers} layer(s) in {r['seconds'] * 1e3:.1f} ms; last step off by at most {r['worst']:.1e}")

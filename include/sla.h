@@ -54,7 +54,8 @@
  * result stays within the rounding of its type.  sla_paged_attention runs few new tokens a sequence (max_new times
  * the heads of a group at most 16) on a kernel of their own, chunks of bf16 tokens on the tensor cores, and chunks of fp32 tokens -- and of bf16 ones whose strides
  * do not nest or whose softmax_scale is not positive -- on a kernel that computes in fp32; sizes, strides and
- * scale decide, never lengths, and no workspace changes a result.
+ * scale decide, never lengths, and no workspace changes a result.  Over a cache in four bits the same three: few new bf16 tokens
+ * (a kernel that multiplies the codes), chunks of bf16 tokens with a positive softmax_scale on the tensor cores, the rest in fp32.
  *
  * Errors: every call returns an sla_status_t; 0 is success, negative values are errors.  When
  * argument validation fails nothing is launched.  No exception or abort crosses this interface.
@@ -490,7 +491,8 @@ sla_status_t sla_cache_copy(sla_handle_t handle, const sla_cache_t *cache, const
  *   out   out  as q;  lse out [n_new, n_q_heads] fp32 contiguous (natural log); a row without keys (a
  *              sequence that is shorter than its new tokens) is 0 and -inf
  * bf16 runs on the tensor cores with fp32 sums (weights are rounded to bf16 before they meet the values),
- * fp32 in fp32. */
+ * fp32 in fp32.  Over a cache in four bits the values are those that it holds, c s, and the weight that is rounded is p or p s;
+ * softmax_scale must be below 2^64 there. */
 sla_status_t sla_paged_attention(sla_handle_t handle, const void *q, const sla_cache_t *cache,
                                  const sla_batch_t *batch, int32_t n_q_heads, int64_t q_stride_t,
                                  int64_t q_stride_h, int32_t window, float softmax_scale, void *out, float *lse,

@@ -801,3 +801,15 @@ def test_a_step_can_be_captured(sla):
     U.check_attention(*got[0], reference(q, c.k, c.v, table, n, [1, 1, 1], 4, 0, 128 ** -0.5, 32), BF16)
     U.check_attention(*got2, reference(q2, c.k, c.v, table, n, [7, 4, 19], 4, 0, 128 ** -0.5, 32), BF16)
     assert torch.equal(got[1][0].double(), Q.held(kn)) and torch.equal(got[1][1].double(), Q.held(vn))
+
+
+def test_the_example_runs(sla):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_serving.py")
+    spec = importlib.util.spec_from_file_location("paged_serving", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    r = m.run(prompts=4, chunk=300, steps=6, four_bits=True)
+    assert r["status"] == sla.SLA_OK and r["worst"] < 2e-2
+    assert r["tokens"] == sum(200 + 777 * i for i in range(4)) + 3 * 7 + 3 * 6
