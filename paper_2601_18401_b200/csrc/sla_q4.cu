@@ -1,7 +1,12 @@
 // A paged cache in four bits (format: sla_q4.cuh): quantising new tokens as they are written, and reading rows of a cache back.
 //
-//   append_q4     a warp per new token (or 1024 values of it): loads its K and V, finds its place meanwhile, a scale per four lanes, codes
-//   cache_read    a warp per row (or 128 pieces of it): values of a four-bit cache in bf16 or fp32, or the rows of another cache as they are
+//   append_q4     a warp per new token, or several (and 1024 values of each): loads their K and V, finds their places meanwhile, a scale per four lanes, codes
+//   read_q4       a warp per row, or several (and 512 values of each): values of a cache in four bits, in bf16 or fp32
+//   read_rows     the same of other caches, whose rows are copied
+//
+// A lane has eight neighbouring dimensions, four lanes a group.  Appending is bound by instructions (245 for eight values of K and of V; ALU pipe
+// 61 %), reading by the latency of a row's loads behind its lookups.  Measured (8 heads, D 128, bf16): 18.7 thousand tokens appended in 28 us, 3.5 TB/s;
+// 65536 rows read in 65 us, 5.3 TB/s, the rate of a copy being 6.5.
 #include "sla_q4.cuh"
 
 namespace sla {

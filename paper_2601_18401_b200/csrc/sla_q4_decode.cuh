@@ -6,14 +6,17 @@
 // A logit is the sum of four products of 32 dimensions, each times the scale of its group and key; a weight is multiplied by the scale of the
 // value's group and rounded to bf16 once, which is what rounding the weight alone costs.  So no value is ever formed, and eight
 // codes cost seven instructions.  P s goes through the 8 x 8 transpose (movmatrix) on its way into the second product.  (With the rows as
-// A, so that P stays where it is, half of A is empty for groups of 8 and less: twice the instructions of the first product, and 168 registers
-// instead of 128.)
+// A, so that P stays where it is, half of A is empty for groups of 8 and less: 400 instructions for 16 keys where this form then took 366.)
 //
 // A cache in four bits brings a quarter of the bytes for the same work: what matters is how many instructions a key takes, and that no warp ever
 // waits for memory.  Every warp has a ring of stages of 32 keys in shared memory, which its lanes fill by asynchronous copies of 16
 // bytes: nine instructions a stage, since a plane's rows lie on end.  (With the pieces in registers, requested a step of 16 keys ahead, as
 // attend_bf16 has them, 32 sequences of 1000 to 65536 took 164 us.  Bulk copies take 40 instructions more a stage: their operands are
 // those of a warp, and each lane's copy goes on its own.)
+//
+// Measured (32/8 heads, D 128, pages of 64 tokens): 32 sequences of 1000 to 65536 in 96 us, 4.8 TB/s of the cache's bytes, 290 instructions for 16 keys of a
+// head; bound by these (ALU pipe 51 %, issue slots 54 % with 12 warps an SM), not by HBM (49 %).  D 64: 64 us; 16 sequences of 500 to 30000 with up to four
+// new tokens 37 us.
 //
 // Powers of two: Q is multiplied by F, a power of two that brings its row's largest magnitude next to 2^100 (a sixteenth of it where codes
 // carry a factor of 16); logits are divided by F 2^-133.  Weights are 2^78 times what they are: 2^78 2^40 2^8 (the largest scale, the slack of
@@ -67,13 +70,13 @@ __host__ __device__ constexpr int ring_bytes(int D, int NT) { return kStages * s
 // A warp's loads then meet all banks: those of K have a row's pieces in neighbouring lanes, those of V the rows of four keys in four.
 template <int D> __device__ __forceinline__ uint32_t mix(uint32_t line) { return D == 128 ? 2 * (line >> 1 & 3) : 4 * (line & 1) + (line & 2); }
 
-// 8 NT rows at most, four where kFour; Walk, w_m, w_l and w_o as for attend_bf16, w_o over the ring, but the warp takes 32 keys at a time.  A thread (g, c) = (lane / 4,
-// lane % 4) has of the products' operands (16 keys a step) the keys ka = 4 (g / 2) + g % 2 and kb = ka + 2 of K, S and P, row g of Q (and g + 8) and
+// 8 NT rows at most, four where kFour; Walk, w_m, w_l and w_o as for attend_bf16, w_o over the ring, but the warp takes 32 keys at a time.  A thread
+// (g, c) = (lane / 4, lane % 4) has of the products' operands (16 keys a step) the keys ka = 4 (g / 2) + g % 2 and kb = ka + 2 of K, S and P, row g of Q (and g + 8) and
 // the values of keys 4 c .. 4 c + 3.
 //
 // kFour: the products' eight columns have the four rows twice.  The weights of the first four are scaled for a group, those of the others for the next
-// group, so that one operand P s serves the products of both: of the first group's, columns 0 to 3 are results, of the second's 4 to 7.  Twenty
-// instructions less of the 320 of 16 keys.
+// group, so that one operand P s serves the products of both: of the first group's, columns 0 to 3 are results, of the second's 4 to 7.
+// (With the places of the codes mixed, 309 instructions for 16 keys instead of 319, 32 sequences of 1000 to 65536 104 us instead of 107.)
 template <int D, int NT, bool kTok, bool kFour, int kWarps, typename Walk>
 __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, const PagedCall &a, const Walk &wk, uint32_t ring, float *w_m, float *w_l, float *w_o) {
     constexpr int N = D / 32, kStride = kKeys * kWarps, S = kKeys / 16;
