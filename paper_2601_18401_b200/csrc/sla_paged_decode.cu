@@ -308,15 +308,18 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
         }
 }
 
-// fp32: S by lanes of a key each, O by lanes of D / 32 dimensions each.  s_q: the queries [D][8 NT], scaled.
-template <int D, int NT, bool kTok>
+// fp32: S by lanes of a key each, O by lanes of D / 32 dimensions each.  s_q: the queries [D][8 NT], scaled.  kQ4: over a cache in four bits, whose values
+// are formed where a row's would be loaded (16 sequences of 1000 to 20000 rows, 32 query and 8 KV heads of 128: 184 us; a block a tile of rows 576 us).
+template <int D, int NT, bool kTok, bool kQ4>
 __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, const float *s_q, float *w_m, float *w_l, float *w_o) {
     float *s_p = w_o;   // a step's weights, until the sums are written
     constexpr int H = 8 * NT, N = D / 32, kDeep = 8;   // heads, dimensions of a lane, loads in flight
     const int lane = threadIdx.x & 31, first = wk.first, n = wk.n;
     const float *kb = reinterpret_cast<const float *>(a.c.k) + wk.head * a.c.s_h;
     const float *vb = reinterpret_cast<const float *>(a.c.v) + wk.head * a.c.s_h + lane * N;
-    auto row_of = [&](int j) { return valid_page(a.c, __ldg(wk.table + (j >> a.c.shift))) * a.c.s_page + (long long)(j & (a.c.P - 1)) * a.c.s_t; };
+    // of a key's row, in elements; in four bits of its plane, in bytes
+    auto row_of = [&](int j) { return valid_page(a.c, __ldg(wk.table + (j >> a.c.shift))) * a.c.s_page + (kQ4 ? 0 : (long long)(j & (a.c.P - 1)) * a.c.s_t); };
+    const char *const k_planes = a.c.k + wk.head * a.c.s_h, *const v_planes = a.c.v + wk.head * a.c.s_h;   // (four bits)
     float m[H], l[H], acc[H][N];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -329,27 +332,45 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
         const int j = key + lane;
         const bool on = j >= first && j < n && j < wk.key_end;
         const long long at = row_of(on ? j : min(max(first, 0), n - 1));
-        const float *kr = kb + at;
         float s[H];
 #pragma unroll
         for (int h = 0; h < H; ++h) s[h] = 0.f;
+        if constexpr (kQ4) {
+            const char *plane = k_planes + at;
+            const int t = (on ? j : min(max(first, 0), n - 1)) & (a.c.P - 1);
 #pragma unroll 1
-        for (int d0 = 0; d0 < D; d0 += 4 * kDeep) {
-            float4 k4[kDeep];
+            for (int d0 = 0; d0 < D; d0 += 8) {
+                float f[8];
+                q4::load_values<false>(plane, a.c.P, D, t, d0 / 8, f);
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u) k4[u] = __ldg(reinterpret_cast<const float4 *>(kr + d0 + 4 * u));
-#pragma unroll
-            for (int u = 0; u < kDeep; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float kk = e == 0 ? k4[u].x : e == 1 ? k4[u].y : e == 2 ? k4[u].z : k4[u].w;
+                for (int e = 0; e < 8; ++e)
 #pragma unroll
                     for (int h = 0; h < H; h += 4) {
-                        const float4 q4 = *reinterpret_cast<const float4 *>(s_q + (d0 + 4 * u + e) * H + h);
-                        s[h] = fmaf(q4.x, kk, s[h]); s[h + 1] = fmaf(q4.y, kk, s[h + 1]);
-                        s[h + 2] = fmaf(q4.z, kk, s[h + 2]); s[h + 3] = fmaf(q4.w, kk, s[h + 3]);
+                        const float4 q4 = *reinterpret_cast<const float4 *>(s_q + (d0 + e) * H + h);
+                        s[h] = fmaf(q4.x, f[e], s[h]); s[h + 1] = fmaf(q4.y, f[e], s[h + 1]);
+                        s[h + 2] = fmaf(q4.z, f[e], s[h + 2]); s[h + 3] = fmaf(q4.w, f[e], s[h + 3]);
                     }
-                }
+            }
+        } else {
+            const float *kr = kb + at;
+#pragma unroll 1
+            for (int d0 = 0; d0 < D; d0 += 4 * kDeep) {
+                float4 k4[kDeep];
+#pragma unroll
+                for (int u = 0; u < kDeep; ++u) k4[u] = __ldg(reinterpret_cast<const float4 *>(kr + d0 + 4 * u));
+#pragma unroll
+                for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float kk = e == 0 ? k4[u].x : e == 1 ? k4[u].y : e == 2 ? k4[u].z : k4[u].w;
+#pragma unroll
+                        for (int h = 0; h < H; h += 4) {
+                            const float4 q4 = *reinterpret_cast<const float4 *>(s_q + (d0 + 4 * u + e) * H + h);
+                            s[h] = fmaf(q4.x, kk, s[h]); s[h + 1] = fmaf(q4.y, kk, s[h + 1]);
+                            s[h + 2] = fmaf(q4.z, kk, s[h + 2]); s[h + 3] = fmaf(q4.w, kk, s[h + 3]);
+                        }
+                    }
+            }
         }
         bool over = false;
         int lo = 0, hi = H;   // rows that see the lane's key
@@ -395,7 +416,16 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
 #pragma unroll
                 for (int d = 0; d < N; ++d) v[u][d] = 0.f;
                 if (seen >> (i0 + u) & 1) {
-                    if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
+                    if constexpr (kQ4) {
+                        float f[8];
+                        q4::load_values<true>(v_planes + to, a.c.P, D, (j - lane + i0 + u) & (a.c.P - 1), lane * N / 8, f);
+#pragma unroll
+                        for (int e = 0; e < 8; e += N)
+                            if (lane * N % 8 == e) {
+#pragma unroll
+                                for (int d = 0; d < N; ++d) v[u][d] = f[e + d];
+                            }
+                    } else if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
                     else *reinterpret_cast<float2 *>(v[u]) = __ldg(reinterpret_cast<const float2 *>(vb + to));
                 }
             }
@@ -430,11 +460,11 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
 
 // kBits: 0; over a cache in four bits 1, or 2 where there are four rows at most
 template <typename T, int D, int NT, bool kTok, int kBits>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kBits != 0))
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kBits != 0 && sizeof(T) == 2))
 paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
              T *__restrict__ out, float *__restrict__ lse) {
     constexpr int R = 16;                 // rows of a partial result
-    constexpr bool kQ4 = kBits != 0;
+    constexpr bool kF32 = sizeof(T) == 4, kQ4 = kBits != 0 && !kF32;   // (in fp32 the values of codes take the place of a row's)
     constexpr int kUnit = kQ4 ? q4_unit_weight(NT) : kUnitWeight;   // what a unit costs beyond its tiles
     // a warp's sums [8 NT][D]; over a cache in four bits they lie over its ring of stages
     extern __shared__ __align__(128) char dyn_sm[];
@@ -447,7 +477,6 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
     __shared__ int s_last;
     long long *s_seq_at = reinterpret_cast<long long *>(dyn_sm + kWarps * kRing);   // [n_seqs + 1] weight before a sequence; then its tokens and its slot
     int *s_n = reinterpret_cast<int *>(s_seq_at + n_seqs + 1), *s_slot = s_n + n_seqs;
-    constexpr bool kF32 = sizeof(T) == 4;
     constexpr int kStep = kF32 || kQ4 ? 32 : 16;   // keys of a warp's step
     __shared__ alignas(16) float s_q[kF32 ? D * 8 * NT : 4];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -533,7 +562,7 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
                 s_q[d * 8 * NT + h] = h < rows ? q[(long long)(row_q + tok) * a.q_st + (long long)(head * G + h - tok * G) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
             }
             __syncthreads();
-            attend_f32<D, NT, kTok>(a, walk, s_q, s_m[warp], s_l[warp], s_o + warp * kSums);
+            attend_f32<D, NT, kTok, kBits != 0>(a, walk, s_q, s_m[warp], s_l[warp], s_o + warp * kSums);
         } else {
             attend_bf16<D, NT, kTok>(q, a, walk, s_m[warp], s_l[warp], s_o + warp * kSums);
         }
@@ -630,19 +659,19 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
 
 }  // namespace
 
-bool paged_decode_supported(const PagedCall &a, int dtype) { return (long long)a.b.max_new * a.G <= 16 && !(q4::is(a.c) && dtype == SLA_F32); }
+bool paged_decode_supported(const PagedCall &a) { return (long long)a.b.max_new * a.G <= 16; }
 
-void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
+void plan_paged_decode(const PagedCall &a, int dtype, PagedPlan &p, int sm_count) {
     p.R = p.RS = 16;
     p.TS = p.TQ = 1;
-    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2, q4::is(a.c)) * sm_count;
+    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2, q4::is(a.c) && dtype == SLA_BF16) * sm_count;
 }
 
 template <typename T, int D, int NT, bool kTok, int kBits>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
-    constexpr bool kQ4 = kBits != 0;
+    constexpr bool kQ4 = kBits != 0 && sizeof(T) == 2;
     constexpr size_t kRing = kQ4 ? kWarps * q4::ring_bytes(D, NT) : 0;
     if (kQ4) {
         static bool allowed[64] = {};
@@ -668,7 +697,7 @@ static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan
                               cudaStream_t st, long long *launches) {
     const int rows = a.b.max_new * a.G;
     const bool small = rows <= 8;
-    if constexpr (kQ4) {
+    if constexpr (kQ4 && sizeof(T) == 2) {
         if (rows <= 4)
             return a.b.max_new == 1 ? decode_of<T, D, 1, false, 2>(q, a, p, scratch, counters, out, lse, st, launches)
                                     : decode_of<T, D, 1, true, 2>(q, a, p, scratch, counters, out, lse, st, launches);
@@ -680,6 +709,8 @@ static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan
 
 cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches) {
+    if (dtype == SLA_F32 && q4::is(a.c))
+        return a.c.D == 64 ? decode_for<float, 64, true>(q, a, p, scratch, counters, out, lse, st, launches) : decode_for<float, 128, true>(q, a, p, scratch, counters, out, lse, st, launches);
     if (dtype == SLA_F32)
         return a.c.D == 64 ? decode_for<float, 64, false>(q, a, p, scratch, counters, out, lse, st, launches) : decode_for<float, 128, false>(q, a, p, scratch, counters, out, lse, st, launches);
     if (q4::is(a.c))
