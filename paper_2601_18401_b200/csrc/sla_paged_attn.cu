@@ -480,7 +480,7 @@ PagedPlan plan_paged(const PagedCall &a, int dtype, int sm_count, size_t gap) {
     p.fold_bytes = 0;
     if (paged_decode_supported(a)) {
         p.kind = PagedPlan::kDecode;
-        plan_paged_decode(a, dtype, p, sm_count);
+        plan_paged_decode(a, p, sm_count);
     } else if (paged_tiles_supported(a, dtype)) {
         p.kind = PagedPlan::kTiles;
         plan_paged_tiles(a, p, sm_count);

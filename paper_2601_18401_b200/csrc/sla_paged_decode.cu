@@ -308,12 +308,15 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
         }
 }
 
-// fp32: S by lanes of a key each, O by lanes of D / 32 dimensions each.  s_q: the queries [D][8 NT], scaled.  kQ4: over a cache in four bits, whose values
-// are formed where a row's would be loaded (16 sequences of 1000 to 20000 rows, 32 query and 8 KV heads of 128: 184 us; a block a tile of rows 576 us).
-template <int D, int NT, bool kTok, bool kQ4>
+// fp32: S by lanes of a key each, O by lanes of N dimensions each.  s_q: the queries [D][H], scaled; H the rows computed.  kQ4: over a cache in
+// four bits, whose values are formed where a row's would be loaded.  A piece there is eight dimensions, so that a key takes 16 lanes (8 for
+// D 64) and the warp several keys at a time; with four dimensions a lane, two lanes formed each piece: 16 sequences of 1000 to 20000 rows, 32 query and
+// 8 KV heads of 128, 160 us against 108 here (and 8 rows where there are four: 184; paged_rows: 576).  Bound by the FMA pipe and the making of values.
+template <int D, int H, bool kTok, bool kQ4>
 __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, const float *s_q, float *w_m, float *w_l, float *w_o) {
     float *s_p = w_o;   // a step's weights, until the sums are written
-    constexpr int H = 8 * NT, N = D / 32, kDeep = 8;   // heads, dimensions of a lane, loads in flight
+    // dimensions of a lane, lanes that a key's values take, keys of the warp at a time, loads in flight
+    constexpr int N = kQ4 ? 8 : D / 32, L = D / N, K = 32 / L, kDeep = kQ4 ? 4 : 8;
     const int lane = threadIdx.x & 31, first = wk.first, n = wk.n;
     const float *kb = reinterpret_cast<const float *>(a.c.k) + wk.head * a.c.s_h;
     const float *vb = reinterpret_cast<const float *>(a.c.v) + wk.head * a.c.s_h + lane * N;
@@ -338,7 +341,7 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
         if constexpr (kQ4) {
             const char *plane = k_planes + at;
             const int t = (on ? j : min(max(first, 0), n - 1)) & (a.c.P - 1);
-#pragma unroll 1
+#pragma unroll 4
             for (int d0 = 0; d0 < D; d0 += 8) {
                 float f[8];
                 q4::load_values<false>(plane, a.c.P, D, t, d0 / 8, f);
@@ -408,34 +411,28 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
         const unsigned seen = __ballot_sync(0xffffffffu, on);   // values of other keys may be anything: they are not read
         const unsigned part = kTok ? __ballot_sync(0xffffffffu, on && (j < wk.all_first || j >= wk.all_n)) : 0u;   // not every row sees them
 #pragma unroll 1
-        for (int i0 = 0; i0 < 32; i0 += kDeep) {
+        for (int i0 = lane / L; i0 < 32; i0 += kDeep * K) {
             float v[kDeep][N];
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) {
-                const long long to = __shfl_sync(0xffffffffu, at, i0 + u);
+                const int i = i0 + u * K;
+                const long long to = __shfl_sync(0xffffffffu, at, i);
 #pragma unroll
                 for (int d = 0; d < N; ++d) v[u][d] = 0.f;
-                if (seen >> (i0 + u) & 1) {
-                    if constexpr (kQ4) {
-                        float f[8];
-                        q4::load_values<true>(v_planes + to, a.c.P, D, (j - lane + i0 + u) & (a.c.P - 1), lane * N / 8, f);
-#pragma unroll
-                        for (int e = 0; e < 8; e += N)
-                            if (lane * N % 8 == e) {
-#pragma unroll
-                                for (int d = 0; d < N; ++d) v[u][d] = f[e + d];
-                            }
-                    } else if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
+                if (seen >> i & 1) {
+                    if constexpr (kQ4) q4::load_values<true>(v_planes + to, a.c.P, D, (j - lane + i) & (a.c.P - 1), lane % L, v[u]);
+                    else if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
                     else *reinterpret_cast<float2 *>(v[u]) = __ldg(reinterpret_cast<const float2 *>(vb + to));
                 }
             }
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) {
+                const int i = i0 + u * K;
                 int lo_u = 0, hi_u = H;
-                if (kTok && (part >> (i0 + u) & 1)) wk.rows_of(j - lane + i0 + u, a.G, lo_u, hi_u);
+                if (kTok && (part >> i & 1)) wk.rows_of(j - lane + i, a.G, lo_u, hi_u);
 #pragma unroll
                 for (int h = 0; h < H; h += 4) {
-                    const float4 p4 = *reinterpret_cast<const float4 *>(s_p + (i0 + u) * H + h);
+                    const float4 p4 = *reinterpret_cast<const float4 *>(s_p + i * H + h);
                     const float pp[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -454,13 +451,17 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
         if (lane == 0) { w_m[h] = m[h]; w_l[h] = sum; }
         if (h == 0) __syncwarp();   // the weights have been read
 #pragma unroll
-        for (int d = 0; d < N; ++d) w_o[h * D + lane * N + d] = acc[h][d];
+        for (int d = 0; d < N; ++d) {
+#pragma unroll
+            for (int off = L; off < 32; off *= 2) acc[h][d] += __shfl_xor_sync(0xffffffffu, acc[h][d], off);
+            if (lane < L) w_o[h * D + lane * N + d] = acc[h][d];
+        }
     }
 }
 
 // kBits: 0; over a cache in four bits 1, or 2 where there are four rows at most
 template <typename T, int D, int NT, bool kTok, int kBits>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kBits != 0 && sizeof(T) == 2))
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(D, NT, kBits != 0))
 paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts parts, int *__restrict__ done,
              T *__restrict__ out, float *__restrict__ lse) {
     constexpr int R = 16;                 // rows of a partial result
@@ -478,7 +479,8 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
     long long *s_seq_at = reinterpret_cast<long long *>(dyn_sm + kWarps * kRing);   // [n_seqs + 1] weight before a sequence; then its tokens and its slot
     int *s_n = reinterpret_cast<int *>(s_seq_at + n_seqs + 1), *s_slot = s_n + n_seqs;
     constexpr int kStep = kF32 || kQ4 ? 32 : 16;   // keys of a warp's step
-    __shared__ alignas(16) float s_q[kF32 ? D * 8 * NT : 4];
+    constexpr int H = kF32 && kBits == 2 ? 4 : 8 * NT;
+    __shared__ alignas(16) float s_q[kF32 ? D * H : 4];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.G;
     chain_wait();
@@ -556,13 +558,13 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
             q4::attend<D, NT, kTok, kBits == 2, kWarps>(q, a, walk, ptx::smem_u32(dyn_sm) + warp * kRing, s_m[warp], s_l[warp], s_o + warp * kSums);
         } else if constexpr (kF32) {
             // (s_q: the segment before has been joined)
-            for (int c = tid; c < D * 8 * NT; c += kThreads) {
+            for (int c = tid; c < D * H; c += kThreads) {
                 const int h = c / D, d = c % D;   // neighbouring threads, neighbouring dimensions
                 const int tok = kTok ? h / G : 0;
-                s_q[d * 8 * NT + h] = h < rows ? q[(long long)(row_q + tok) * a.q_st + (long long)(head * G + h - tok * G) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
+                s_q[d * H + h] = h < rows ? q[(long long)(row_q + tok) * a.q_st + (long long)(head * G + h - tok * G) * a.q_sh + d] * (a.scale * kLog2e) : 0.f;
             }
             __syncthreads();
-            attend_f32<D, NT, kTok, kBits != 0>(a, walk, s_q, s_m[warp], s_l[warp], s_o + warp * kSums);
+            attend_f32<D, H, kTok, kBits != 0>(a, walk, s_q, s_m[warp], s_l[warp], s_o + warp * kSums);
         } else {
             attend_bf16<D, NT, kTok>(q, a, walk, s_m[warp], s_l[warp], s_o + warp * kSums);
         }
@@ -661,10 +663,10 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
 
 bool paged_decode_supported(const PagedCall &a) { return (long long)a.b.max_new * a.G <= 16; }
 
-void plan_paged_decode(const PagedCall &a, int dtype, PagedPlan &p, int sm_count) {
+void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count) {
     p.R = p.RS = 16;
     p.TS = p.TQ = 1;
-    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2, q4::is(a.c) && dtype == SLA_BF16) * sm_count;
+    p.n_ctas = ctas_per_sm(a.c.D, a.b.max_new * a.G <= 8 ? 1 : 2, q4::is(a.c)) * sm_count;
 }
 
 template <typename T, int D, int NT, bool kTok, int kBits>
@@ -697,7 +699,7 @@ static cudaError_t decode_for(const void *q, const PagedCall &a, const PagedPlan
                               cudaStream_t st, long long *launches) {
     const int rows = a.b.max_new * a.G;
     const bool small = rows <= 8;
-    if constexpr (kQ4 && sizeof(T) == 2) {
+    if constexpr (kQ4) {
         if (rows <= 4)
             return a.b.max_new == 1 ? decode_of<T, D, 1, false, 2>(q, a, p, scratch, counters, out, lse, st, launches)
                                     : decode_of<T, D, 1, true, 2>(q, a, p, scratch, counters, out, lse, st, launches);

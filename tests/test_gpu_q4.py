@@ -346,6 +346,22 @@ def test_few_new_tokens(sla, handle, G, new, dtype, d):
     assert torch.allclose(out.float(), one.float(), atol=0.02) and torch.equal(lse.isinf(), one_lse.isinf())
 
 
+@pytest.mark.parametrize("G,new", [(1, 2), (1, 3), (1, 4), (2, 2), (1, 7), (2, 4)])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_few_rows(sla, handle, G, new, dtype, d):
+    """Heads of a group x new tokens <= 8, four and fewer among them; with groups that are NaN where only some rows look."""
+    n = [1, 2, 31, 32, 33, 0, 64, 700, 9001]
+    c = [(i * 5 + 2) % (new + 1) for i in range(len(n))]
+    c[1] = c[2] = c[5] = c[-1] = new
+    for window in (0, 1, 31, 100):
+        def prep(k, v, table, q):
+            at = n[-1] - new // 2 - 1
+            spoil(v, int(table[-1, at // 16]), 1, at % 16, 16, d, 5)
+            spoil(v, int(table[7, 43]), 0, 8, 16, d, d - 1)
+        run(sla, handle, n, c, dtype=dtype, d=d, G=G, window=window, max_new=new)
+        run(sla, handle, n, c, dtype=dtype, d=d, G=G, window=window, max_new=new, prep=prep)
+
+
 def spoil(pool, page_of, g, t, page, d, dim):
     """The scale of dimension `dim` of row t of a plane becomes NaN."""
     at = page * d // 2 + t * (d // 16) + dim // 32 * 2
