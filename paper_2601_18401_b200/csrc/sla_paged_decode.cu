@@ -308,21 +308,32 @@ __device__ __forceinline__ void attend_bf16(const __nv_bfloat16 *__restrict__ q,
         }
 }
 
-// fp32: S by lanes of a key each, O by lanes of N dimensions each.  s_q: the queries [D][H], scaled; H the rows computed.  kQ4: over a cache in
-// four bits, whose values are formed where a row's would be loaded.  A piece there is eight dimensions, so that a key takes 16 lanes (8 for
-// D 64) and the warp several keys at a time; with four dimensions a lane, two lanes formed each piece: 16 sequences of 1000 to 20000 rows, 32 query and
-// 8 KV heads of 128, 160 us against 108 here (and 8 rows where there are four: 184; paged_rows: 576).  Bound by the FMA pipe and the making of values.
+// fp32 over a cache in four bits: of a warp, stages (32 rows of codes of K and of V, 16 bytes apart for the banks, and their scales), then the weights of a step
+constexpr int kF32Stages = 2;
+__host__ __device__ constexpr int f32_stage_bytes(int D) { return 2 * 32 * (D / 2 + 16 + D / 16); }
+__host__ __device__ constexpr int f32_ring_bytes(int D, int NT) { return kF32Stages * f32_stage_bytes(D) + 32 * 8 * NT * 4; }
+
+// fp32: S by lanes of a key each, O by lanes of N dimensions each.  s_q: the queries [D][H], scaled; H the rows computed.
+//
+// kQ4: over a cache in four bits.  Rows come by asynchronous copies two steps ahead, and a lane turns codes into values in its registers: for S those of
+// its key, for O a word of a key's, four dimensions of each of two groups (a key takes D / 8 lanes, the warp goes through several keys at a time).
+// 16 sequences of 1000 to 20000 rows, 32 query and 8 KV heads of 128, one new token each: 58 us (151 over the cache in fp32).  With the codes loaded
+// where they are used 102 us, of which warps waited for them two thirds of the time, and 96 with prefetches into L2 a step ahead; with two
+// lanes a piece of eight dimensions 160; with 8 rows computed where there are four 184; by paged_rows 573.
 template <int D, int H, bool kTok, bool kQ4>
 __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, const float *s_q, float *w_m, float *w_l, float *w_o) {
-    float *s_p = w_o;   // a step's weights, until the sums are written
+    // a step's weights, until the sums are written (four bits: behind the stages)
+    float *s_p = w_o + (kQ4 ? kF32Stages * f32_stage_bytes(D) / 4 : 0);
     // dimensions of a lane, lanes that a key's values take, keys of the warp at a time, loads in flight
-    constexpr int N = kQ4 ? 8 : D / 32, L = D / N, K = 32 / L, kDeep = kQ4 ? 4 : 8;
+    constexpr int N = kQ4 ? 8 : D / 32, L = D / N, K = 32 / L, kDeep = kQ4 ? 4 : 8, NG = D / 32;
     const int lane = threadIdx.x & 31, first = wk.first, n = wk.n;
     const float *kb = reinterpret_cast<const float *>(a.c.k) + wk.head * a.c.s_h;
     const float *vb = reinterpret_cast<const float *>(a.c.v) + wk.head * a.c.s_h + lane * N;
     // of a key's row, in elements; in four bits of its plane, in bytes
     auto row_of = [&](int j) { return valid_page(a.c, __ldg(wk.table + (j >> a.c.shift))) * a.c.s_page + (kQ4 ? 0 : (long long)(j & (a.c.P - 1)) * a.c.s_t); };
     const char *const k_planes = a.c.k + wk.head * a.c.s_h, *const v_planes = a.c.v + wk.head * a.c.s_h;   // (four bits)
+    // four bits: the first dimension of a lane's word of values, of two groups: own + 2 i and own + 32 + 2 i
+    const int ch = lane % L / (NG / 2), own = 64 * (lane % (NG / 2)) + 8 * (ch >> 1) + (ch & 1);
     float m[H], l[H], acc[H][N];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -331,28 +342,85 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
 #pragma unroll
         for (int d = 0; d < N; ++d) acc[h][d] = 0.f;
     }
-    for (int key = wk.key; key < wk.key_end; key += 32 * kWarps) {
+    auto seen_by_any = [&](int j) { return j >= first && j < n && j < wk.key_end; };
+    auto to_read = [&](int j) { return seen_by_any(j) ? j : min(max(first, 0), n - 1); };
+    constexpr int kAll = 32 * kWarps;
+    constexpr int kRow = D / 2 + 16, kVAt = 32 * kRow, kKScales = 2 * kVAt, kVScales = kKScales + 32 * (D / 16);   // of a stage
+    char *const ring = reinterpret_cast<char *>(w_o);
+    const uint32_t ring_at = kQ4 ? ptx::smem_u32(ring) : 0;
+    long long codes = 0, scales = 0;   // of a lane's key, kF32Stages steps ahead: bytes from the planes' base
+    auto find = [&](int key) {
+        if (key >= wk.key_end) return;
+        const int x = to_read(key + lane), t = x & (a.c.P - 1);
+        const long long plane = row_of(x);
+        codes = plane + q4::codes_at(D, t);
+        scales = plane + q4::scales_at(a.c.P, D, t);
+    };
+    auto fill = [&](int key, int st) {
+        if (key < wk.key_end) {
+            const uint32_t to = ring_at + st * f32_stage_bytes(D);
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {   // neighbouring lanes, neighbouring pieces of a row
+                const int x = (lane + 32 * i) / NG, at = lane % NG * 16;
+                const long long from = __shfl_sync(0xffffffffu, codes, x) + at;
+                ptx::cp_async16(to + x * kRow + at, k_planes + from);
+                ptx::cp_async16(to + kVAt + x * kRow + at, v_planes + from);
+            }
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + kKScales + lane * (D / 16)), "l"(k_planes + scales), "n"(D / 16) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + kVScales + lane * (D / 16)), "l"(v_planes + scales), "n"(D / 16) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int st = 0;
+    if constexpr (kQ4) {
+#pragma unroll
+        for (int i = 0; i < kF32Stages; ++i) {
+            find(wk.key + i * kAll);
+            fill(wk.key + i * kAll, i);
+        }
+        find(wk.key + kF32Stages * kAll);
+    }
+    for (int key = wk.key; key < wk.key_end; key += kAll) {
         const int j = key + lane;
-        const bool on = j >= first && j < n && j < wk.key_end;
-        const long long at = row_of(on ? j : min(max(first, 0), n - 1));
+        const bool on = seen_by_any(j);
+        const long long at = kQ4 ? 0 : row_of(to_read(j));
+        const char *const stage = ring + st * f32_stage_bytes(D);
+        if constexpr (kQ4) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kF32Stages - 1) : "memory");
+            __syncwarp();   // every lane's copies are there
+        }
         float s[H];
 #pragma unroll
         for (int h = 0; h < H; ++h) s[h] = 0.f;
         if constexpr (kQ4) {
-            const char *plane = k_planes + at;
-            const int t = (on ? j : min(max(first, 0), n - 1)) & (a.c.P - 1);
-#pragma unroll 4
-            for (int d0 = 0; d0 < D; d0 += 8) {
-                float f[8];
-                q4::load_values<false>(plane, a.c.P, D, t, d0 / 8, f);
+            uint32_t f[NG];   // the groups' scales
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+            for (int g = 0; g < NG; g += 2) {
+                const uint32_t two = reinterpret_cast<const uint32_t *>(stage + kKScales + lane * (D / 16))[g / 2];
+                f[g] = q4::factor(two & 0xffffu);
+                f[g + 1] = q4::factor(two >> 16);
+            }
+            const uint4 *row = reinterpret_cast<const uint4 *>(stage + lane * kRow);
+#pragma unroll 1
+            for (int c0 = 0; c0 < 4; c0 += 4 / NG) {
+                const uint4 piece = row[c0 * NG / 4];
+                const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};   // words (c0, 0), (c0, 1) ..
 #pragma unroll
-                    for (int h = 0; h < H; h += 4) {
-                        const float4 q4 = *reinterpret_cast<const float4 *>(s_q + (d0 + e) * H + h);
-                        s[h] = fmaf(q4.x, f[e], s[h]); s[h + 1] = fmaf(q4.y, f[e], s[h + 1]);
-                        s[h + 2] = fmaf(q4.z, f[e], s[h + 2]); s[h + 3] = fmaf(q4.w, f[e], s[h + 3]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const int d0 = 32 * (i % NG) + 8 * (c0 + i / NG);
+                    uint32_t v[4];
+                    float k8[8];
+                    q4::values(w[i], f[i % NG], v);
+                    Vec16<__nv_bfloat16>::unpack(make_uint4(v[0], v[1], v[2], v[3]), k8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+#pragma unroll
+                        for (int h = 0; h < H; h += 4) {
+                            const float4 q4 = *reinterpret_cast<const float4 *>(s_q + (d0 + e) * H + h);
+                            s[h] = fmaf(q4.x, k8[e], s[h]); s[h + 1] = fmaf(q4.y, k8[e], s[h + 1]);
+                            s[h + 2] = fmaf(q4.z, k8[e], s[h + 2]); s[h + 3] = fmaf(q4.w, k8[e], s[h + 3]);
+                        }
+                }
             }
         } else {
             const float *kr = kb + at;
@@ -416,12 +484,17 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) {
                 const int i = i0 + u * K;
-                const long long to = __shfl_sync(0xffffffffu, at, i);
+                const long long to = kQ4 ? 0 : __shfl_sync(0xffffffffu, at, i);
 #pragma unroll
                 for (int d = 0; d < N; ++d) v[u][d] = 0.f;
                 if (seen >> i & 1) {
-                    if constexpr (kQ4) q4::load_values<true>(v_planes + to, a.c.P, D, (j - lane + i) & (a.c.P - 1), lane % L, v[u]);
-                    else if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
+                    if constexpr (kQ4) {   // a word: four codes of each of two groups
+                        const uint32_t w = reinterpret_cast<const uint32_t *>(stage + kVAt + i * kRow)[lane % L];
+                        const uint32_t two = reinterpret_cast<const uint32_t *>(stage + kVScales + i * (D / 16))[lane % (NG / 2)];
+                        uint32_t x[4];
+                        q4::values(w, q4::mul_bf16x2(two, 0x46004600u), x);
+                        Vec16<__nv_bfloat16>::unpack(make_uint4(x[0], x[1], x[2], x[3]), v[u]);
+                    } else if constexpr (N == 4) *reinterpret_cast<float4 *>(v[u]) = __ldg(reinterpret_cast<const float4 *>(vb + to));
                     else *reinterpret_cast<float2 *>(v[u]) = __ldg(reinterpret_cast<const float2 *>(vb + to));
                 }
             }
@@ -442,6 +515,12 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
                 }
             }
         }
+        if constexpr (kQ4) {
+            __syncwarp();   // the stage has been read
+            fill(key + kF32Stages * kAll, st);
+            find(key + (kF32Stages + 1) * kAll);
+            st = st + 1 == kF32Stages ? 0 : st + 1;
+        }
     }
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -454,9 +533,14 @@ __device__ __forceinline__ void attend_f32(const PagedCall &a, const Walk &wk, c
         for (int d = 0; d < N; ++d) {
 #pragma unroll
             for (int off = L; off < 32; off *= 2) acc[h][d] += __shfl_xor_sync(0xffffffffu, acc[h][d], off);
-            if (lane < L) w_o[h * D + lane * N + d] = acc[h][d];
+            if (lane < L) w_o[h * D + (kQ4 ? own + 32 * (d & 1) + 2 * (d >> 1) : lane * N + d)] = acc[h][d];
         }
     }
+}
+
+// bytes of a warp's ring
+template <typename T> __host__ __device__ constexpr int ring_of(int D, int NT, int bits) {
+    return !bits ? 0 : sizeof(T) == 4 ? f32_ring_bytes(D, NT) : q4::ring_bytes(D, NT);
 }
 
 // kBits: 0; over a cache in four bits 1, or 2 where there are four rows at most
@@ -469,10 +553,10 @@ paged_decode(const T *__restrict__ q, PagedCall a, int x_base, int n_seqs, Parts
     constexpr int kUnit = kQ4 ? q4_unit_weight(NT) : kUnitWeight;   // what a unit costs beyond its tiles
     // a warp's sums [8 NT][D]; over a cache in four bits they lie over its ring of stages
     extern __shared__ __align__(128) char dyn_sm[];
-    constexpr int kRing = kQ4 ? q4::ring_bytes(D, NT) : 0, kSums = kQ4 ? kRing / 4 : 8 * NT * D;
+    constexpr int kRing = ring_of<T>(D, NT, kBits), kSums = kRing ? kRing / 4 : 8 * NT * D;
     static_assert(kSums >= 8 * NT * D, "the sums fit into the ring");
-    __shared__ alignas(16) float s_sums[kQ4 ? 4 : kWarps * kSums];
-    float *s_o = kQ4 ? reinterpret_cast<float *>(dyn_sm) : s_sums;
+    __shared__ alignas(16) float s_sums[kRing ? 4 : kWarps * kSums];
+    float *s_o = kRing ? reinterpret_cast<float *>(dyn_sm) : s_sums;
     __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
     __shared__ long long s_scan[kWarps];
     __shared__ int s_last;
@@ -673,8 +757,8 @@ template <typename T, int D, int NT, bool kTok, int kBits>
 static cudaError_t decode_of(const void *q, const PagedCall &a, const PagedPlan &p, char *scratch, int *counters, void *out, float *lse,
                              cudaStream_t st, long long *launches) {
     cudaError_t e = cudaSuccess;
-    constexpr bool kQ4 = kBits != 0 && sizeof(T) == 2;
-    constexpr size_t kRing = kQ4 ? kWarps * q4::ring_bytes(D, NT) : 0;
+    constexpr bool kQ4 = kBits != 0;
+    constexpr size_t kRing = kWarps * ring_of<T>(D, NT, kBits);
     if (kQ4) {
         static bool allowed[64] = {};
         int dev = 0;
