@@ -471,6 +471,11 @@ def test_many_sequences(sla, handle, dtype, n_seqs, new, G, d):
     run(sla, handle, n.tolist(), c.tolist(), dtype=dtype, hkv=1, G=G, d=d, max_new=new)
 
 
+@pytest.mark.parametrize("n_seqs,new,G,d", [(1030, 4, 4, 128), (2500, 1, 2, 64), (1025, 2, 2, 128)])
+def test_many_sequences_in_fp32(sla, handle, n_seqs, new, G, d):
+    test_many_sequences(sla, handle, F32, n_seqs, new, G, d)
+
+
 def test_offsets_above_2_to_32(sla, handle):
     """Pools of more than 2^32 bytes: the pages of the sequences lie behind them."""
     n_pages, hkv, page, d = 120000, 8, 64, 128
