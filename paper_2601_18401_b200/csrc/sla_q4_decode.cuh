@@ -18,9 +18,10 @@
 // head; bound by these (ALU pipe 51 %, issue slots 54 % with 12 warps an SM), not by HBM (49 %).  D 64: 64 us; 16 sequences of 500 to 30000 with up to four
 // new tokens 37 us.
 //
-// Powers of two: Q is multiplied by F, a power of two that brings its row's largest magnitude next to 2^100 (a sixteenth of it where codes
-// carry a factor of 16); logits are divided by F 2^-133.  Weights are 2^78 times what they are: 2^78 2^40 2^8 (the largest scale, the slack of
-// the running maximum) stays in the range of bf16, and products with subnormals down to 2^-133 2^78 2^-40 in that of fp32.
+// Powers of two: Q is multiplied by F, a power of two that brings its row's largest magnitude next to 2^125 (a sixteenth of it where codes
+// carry a factor of 16); logits are divided by F 2^-133, in two steps where that and the softmax's scale make no fp32 number.  Weights are
+// 2^78 times what they are: 2^78 2^40 2^8 (the largest scale, the slack of the running maximum) stays in the range of bf16, and products with
+// subnormals down to 2^-133 2^78 2^-40 in that of fp32.
 #pragma once
 
 #include <math_constants.h>
@@ -137,6 +138,7 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
     const uint32_t q_at = ring + kStages * stage_bytes(D) + lane * 16;   // (a lane reads what it wrote)
     // [t][e]: row 8 t + 2 c + e
     float m[NT][2], l[NT][2], lim[NT][2], base[NT][2], mult[NT][2], acc[NT][2 * N][4];
+    int top_e[NT], most_e = -2;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         uint32_t qf[N][4];
@@ -154,19 +156,19 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         top = max(top & 0xffffu, top >> 16);
         top = max(top, __shfl_xor_sync(kAll, top, 1));
         top = max(top, __shfl_xor_sync(kAll, top, 2));
-        // exponent of the row's largest magnitude, kept where F and 2^133 / F are numbers; F = 2^(100 - e)
-        const int e = min(max((int)(top >> 7) - 127, -27), 85);
-        const float f0 = __uint_as_float((uint32_t)(227 - e) << 23), f1 = __uint_as_float((uint32_t)(223 - e) << 23);
+        // exponent of the row's largest magnitude, kept where F is a number; F = 2^(125 - e)
+        const int e = min(max((int)(top >> 7) - 127, -2), 127);
+        const float f0 = __uint_as_float((uint32_t)(252 - e) << 23), f1 = __uint_as_float((uint32_t)(248 - e) << 23);
 #pragma unroll
         for (int w = 0; w < N; ++w) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) qf[w][i] = pack(half_of(qf[w][i], 0) * (i & 1 ? f1 : f0), half_of(qf[w][i], 1) * (i & 1 ? f1 : f0));
             ptx::st_shared_v4(q_at + (t * N + w) * 512, qf[w]);
         }
-        const float back = a.scale * kLog2e * __uint_as_float((uint32_t)(160 + e) << 23);   // 2^(33 + e)
+        top_e[t] = e;
+        most_e = max(most_e, e);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            mult[t][u] = __shfl_sync(kAll, back, 4 * (2 * c + u));
             m[t][u] = lim[t][u] = -CUDART_INF_F;
             base[t][u] = kLift;
             l[t][u] = 0.f;
@@ -175,6 +177,16 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
         for (int i = 0; i < 2 * N; ++i)
 #pragma unroll
             for (int u = 0; u < 4; ++u) acc[t][i][u] = 0.f;
+    }
+    // What a logit's products are multiplied by: scale 2^(8 + e), which is no fp32 number for queries of 2^125 and a scale of 2^-4, say.  Then the
+    // products, below 2^44, take 2^72 of it beforehand.  (scale is below 2^64.)
+    const float scale2 = a.scale * kLog2e;
+    const bool far = __any_sync(kAll, fabsf(scale2) * __uint_as_float((uint32_t)(63 + most_e) << 23) >= 0x1p55f);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float back = far ? scale2 * __uint_as_float((uint32_t)(63 + top_e[t]) << 23) : scale2 * __uint_as_float((uint32_t)(127 + top_e[t]) << 23) * 0x1p8f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) mult[t][u] = __shfl_sync(kAll, back, 4 * (2 * c + u));
     }
 
     const uint32_t ka = 4 * (g >> 1) + (g & 1);
@@ -218,6 +230,14 @@ __device__ __forceinline__ void attend(const __nv_bfloat16 *__restrict__ q, cons
                     for (int u = 0; u < 4; ++u) y[s][t][u] = w == 0 ? d[u] * (u < 2 ? sa : sb) : fmaf(d[u], u < 2 ? sa : sb, y[s][t][u]);
                 }
             }
+        }
+        if (far) {   // (a jump on its own: selecting the factor for each product took 96.6 us for 32 sequences of 1000 to 65536, this 95.9)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) y[s][t][u] *= 0x1p72f;
         }
         // a logit less what the row's weights are taken from, m - 78 (m: not below the largest so far but by 8; 0 for none)
 #pragma unroll

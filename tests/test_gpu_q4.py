@@ -434,6 +434,40 @@ def test_small_and_large_queries(sla, handle, power, new):
     run(sla, handle, [500, 31], new, scale=128 ** -0.5 * 2.0 ** -power, prep=prep)
 
 
+@pytest.mark.parametrize("power,scale", [(100, None), (113, None), (120, None), (124, None), (-110, 2.0 ** 63)])
+@pytest.mark.parametrize("new,G", [([1, 1], 2), ([1, 1], 4), ([1, 1], 8), ([3, 1], 4), ([60, 1], 4)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_next_to_the_ends_of_bf16(sla, handle, power, scale, new, G, d):
+    """Every finite query has its answer, whatever kernel the call runs on.  Powers of two move no rounding but at the small end: fp32 sums of
+    products, which may be 2^-48 as large as they are, end at 2^-149, 2^-38 of a logit under the largest scale, beside which 2^-20 is allowed."""
+    def prep(k, v, table, q):
+        q.clamp_(-7.5, 7.5).mul_(2.0 ** power)
+    run(sla, handle, [500, 31], new, G=G, d=d, scale=d ** -0.5 * 2.0 ** -power if scale is None else scale, prep=prep)
+
+
+@pytest.mark.parametrize("power,scale", [(60, 2.0 ** 63), (124, 1.0), (124, -1.0), (126, 2.0 ** 63), (0, 2.0 ** 63)])
+@pytest.mark.parametrize("new", [[1, 1], [3, 1], [60, 1]])
+def test_keys_of_zero_under_large_queries_and_scales(sla, handle, power, scale, new):
+    """Logits that are zero stay zero, whatever they are multiplied by: every key weighs the same."""
+    def prep(k, v, table, q):
+        k[:, :, : 16 * 64] = 0                                    # codes
+        q.clamp_(-2, 2).mul_(2.0 ** (power - 1))
+    run(sla, handle, [500, 31], new, scale=scale, prep=prep)
+
+
+@pytest.mark.parametrize("power", [20, 60, 100, 125])
+@pytest.mark.parametrize("new", [[1, 1], [3, 1], [60, 1]])
+def test_a_large_dimension_whose_codes_are_zero(sla, handle, power, new):
+    """The others decide, however much smaller they are.  (Sums of codes' products, 2^-133 as large as they are beside a query of 2^125, end at
+    2^-149: 2^-16 times a key's scale, here about 1/2, and the softmax's, 2^-3.5, each of the 6 to 24 times that something is added, 2^-16 in
+    all.  The bound allows 2^-16 of the sum of the products' magnitudes, which are about 100 2^-3.5 here.)"""
+    def prep(k, v, table, q):
+        b = k[:, :, : 16 * 64].unflatten(-1, (16, 4, 4, 4))       # row, piece of eight, group, bytes
+        b[:, :, :, :, 0] = 0
+        q[..., 5] = 2.0 ** power
+    run(sla, handle, [500, 31], new, prep=prep)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_strided_queries_slots_and_shared_pages(sla, handle, dtype):
     n, new = [100, 64, 250], [3, 1, 40]
