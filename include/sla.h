@@ -455,7 +455,8 @@ sla_status_t sla_cache_append(sla_handle_t handle, const sla_cache_t *cache, con
 /* Reads rows back: row r of sequence x is position first[x] + r, for r < cu_new[x+1] - cu_new[x] (first NULL: position r).
  * k_out, v_out [n_new, n_kv_heads, head_dim], strides out_stride_{t,h} in elements: the cache's values, of one in four bits
  * c s in bf16 or fp32, both exact.  Sequences with first < 0 are left out; so is a position that the sequence does not have,
- * which sets SLA_ERR_DEVICE_INDEX.  The rows of k_out and v_out left out keep what they hold. */
+ * which sets SLA_ERR_DEVICE_INDEX.  The rows of k_out and v_out left out keep what they hold.  No two rows of the call may share
+ * memory (SLA_ERR_INVALID_ARG). */
 sla_status_t sla_cache_read(sla_handle_t handle, const sla_cache_t *cache, const sla_batch_t *batch,
                             const int32_t *first, void *k_out, void *v_out, int64_t out_stride_t,
                             int64_t out_stride_h, void *stream);

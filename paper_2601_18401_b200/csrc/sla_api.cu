@@ -871,6 +871,22 @@ sla::Pages make_pages(sla_handle_t h, const sla_cache_t *c) {
     return p;
 }
 
+// Whether rows of D elements at t s_t + h s_h (t < T, h < H) and others that lie `apart` elements further share an element; with themselves for apart 0.
+// s_t and s_h are at least D where there is more than one.
+bool rows_meet(int64_t apart, int64_t T, int64_t stride_t, int64_t H, int64_t stride_h, int64_t D) {
+    using Wide = __int128;   // (strides may be any number)
+    const Wide s_t = stride_t, s_h = stride_h, reach_t = (T - 1) * s_t + D, reach_h = (H - 1) * s_h + D, reach = reach_t + reach_h - D;
+    if (apart >= reach || -apart >= reach) return false;
+    if (apart == 0 && (T == 1 || H == 1 || s_t >= reach_h || s_h >= reach_t)) return false;   // one inside the other
+    for (int64_t h = apart == 0 ? 1 : 1 - H; h < H; ++h) {   // (of two rows with themselves one has the larger h)
+        const Wide x = apart + h * s_h;                      // and t from -x / s_t, down or up
+        const Wide t = T == 1 ? 0 : x >= 0 ? -((x + s_t - 1) / s_t) : -x / s_t;
+        for (Wide u = t; u <= t + (T > 1); ++u)
+            if (u > -T && u < T && x + u * s_t < D && x + u * s_t > -D) return true;
+    }
+    return false;
+}
+
 sla::Batch make_batch(const sla_batch_t *b) { return {b->n_seqs, b->n_new, b->max_new, 0, b->seq, b->cu_new}; }
 
 // Rows that a sequence can have at most, given a bound that may be loose.
@@ -970,6 +986,10 @@ sla_status_t sla_cache_read(sla_handle_t h, const sla_cache_t *c, const sla_batc
         return fail(h, SLA_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements%s");
     if ((b->n_new > 1 && out_stride_t < c->head_dim) || (c->n_kv_heads > 1 && out_stride_h < c->head_dim))
         return fail(h, SLA_ERR_INVALID_ARG, "token or head stride below head_dim%s");
+    const int64_t apart = (int64_t)(reinterpret_cast<intptr_t>(v_out) - reinterpret_cast<intptr_t>(k_out)) / (int64_t)elem_size(tensor_type(c));
+    if (apart == 0 || rows_meet(0, b->n_new, out_stride_t, c->n_kv_heads, out_stride_h, c->head_dim) ||
+        rows_meet(apart, b->n_new, out_stride_t, c->n_kv_heads, out_stride_h, c->head_dim))
+        return fail(h, SLA_ERR_INVALID_ARG, "rows of k_out and v_out lie over one another%s");
     cudaError_t e = sla::launch_cache_read(make_pages(h, c), make_batch(b), first, tensor_type(c) == SLA_F32, k_out, v_out, out_stride_t, out_stride_h,
                                            h->sm_count, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(h, e, "sla_cache_read");

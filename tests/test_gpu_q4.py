@@ -644,6 +644,40 @@ def test_refusals(sla, handle):
     assert none[0].shape == (0, 2, 128)
 
 
+@pytest.mark.parametrize("four", [False, True])
+def test_rows_read_that_would_lie_over_one_another(sla, handle, four):
+    """Refused, and nothing is written; keys and values that share a tensor without meeting are read as any others."""
+    d = 64
+    if four:
+        c, *_ = empty_cache(sla, d=d)
+    else:
+        k, v = U.make_pools(40, 2, 16, d, BF16)
+        c = sla.make_cache(k, v, U.device_ints(np.full((6, 20), -1)), U.device_ints(np.zeros(6)), U.device_ints(np.zeros(40)))
+    cu, x, y = U.device_ints([0, 5, 5, 5, 5, 5, 5]), normal((5, 2, d), BF16, 1), normal((5, 2, d), BF16, 2)
+    sla.sla_cache_append(handle, c, cu, sla.sla_cache_extend(handle, c, cu), x, y)
+    want = [Q.held(t) if four else t.double() for t in (x, y)]
+    flat = torch.full((4000,), 7.0, dtype=BF16, device="cuda:0")
+
+    def rows(at, s_t, s_h, T=5, H=2):
+        return flat[at:].as_strided((T, H, d), (s_t, s_h, 1))
+    for ko, vo in ((rows(0, 64, 64), rows(2000, 64, 64)),            # the second head of a row is the first of the next
+                   (rows(0, 72, 136), rows(2000, 72, 136)),          # .. of the next but one, in part
+                   (rows(0, 128, 64), rows(0, 128, 64)),             # keys and values in one place
+                   (rows(0, 256, 64), rows(64, 256, 64)),            # values over the keys' second head
+                   (rows(568, 128, 64), rows(0, 128, 64))):          # keys behind the values' start
+        with pytest.raises(sla.SlaError) as e:
+            sla.sla_cache_read(handle, c, cu, k_out=ko, v_out=vo)
+        assert e.value.status == -1 and (flat == 7).all()
+    for ko, vo in ((rows(0, 256, 64), rows(128, 256, 64)),           # token by token: keys, then values
+                   (rows(0, 256, 128), rows(64, 256, 128)),          # head by head
+                   (rows(0, 192, 128), rows(1600, 192, 128)),        # heads of one token between the next token's: 0, 128, 192, 320, ..
+                   (rows(0, 64, 320), rows(640, 64, 320))):
+        flat.fill_(7.0)
+        for o, w in zip(sla.sla_cache_read(handle, c, cu, k_out=ko, v_out=vo), want):
+            assert torch.equal(o.double(), w)
+        assert (flat == 7).sum() == 4000 - 2 * 5 * 2 * d + sum((w == 7).sum() for w in want)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n,T,G", [((1 << 20) + 777, 2400, 16), (1 << 22, 1, 4), (1 << 21, 2, 8), (600000, 700, 1)])
 def test_long_sums_of_values_of_one_sign(sla, d, n, T, G):
