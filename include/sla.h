@@ -432,8 +432,8 @@ typedef struct {
 } sla_batch_t;
 
 /* Workspace bytes that every call below needs at most, for batches of up to n_seqs sequences and n_new
- * tokens, whatever their max_new, and n_q_heads query heads.  params: of sla_paged_decode_step, NULL when it is not called.  0 when the
- * arguments are invalid.  Host-only. */
+ * tokens, whatever their max_new, and n_q_heads query heads.  params: of sla_paged_decode_step, NULL when it is not called, as over a
+ * cache in four bits.  0 when the arguments are invalid, params for such a cache among them.  Host-only. */
 size_t sla_paged_workspace_bytes(const sla_cache_t *cache, int32_t n_q_heads, int32_t n_seqs, int32_t n_new,
                                  const sla_params_t *params);
 

@@ -604,7 +604,7 @@ def _slots(cache: sla_cache_t, cu_new: Optional[torch.Tensor], seq: Optional[tor
 def sla_paged_workspace_bytes(cache: sla_cache_t, n_q_heads: int, n_seqs: int, n_new: int,
                               params: Optional[sla_params_t] = None) -> int:
     """Workspace that the paged calls need for batches of up to n_seqs sequences and n_new tokens; params: of
-    sla_paged_decode_step, None when it is not called."""
+    sla_paged_decode_step, None when it is not called, as over a cache in four bits (0 otherwise)."""
     return int(load_library().sla_paged_workspace_bytes(cache.address, int(n_q_heads), int(n_seqs), int(n_new),
                                                         None if params is None else C.byref(params)))
 

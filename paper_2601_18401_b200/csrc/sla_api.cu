@@ -916,6 +916,7 @@ sla_layout_t layout_of(const sla_cache_t *c, int32_t n_q_heads, int32_t n_seqs, 
 size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_t n_seqs, int32_t n_new, const sla_params_t *p) {
     if (check_cache(c) || n_q_heads <= 0 || n_q_heads % c->n_kv_heads || n_q_heads / c->n_kv_heads > sla::kMaxGroup || n_seqs < 0 || n_new < 0)
         return 0;
+    if (p && four_bits(c)) return 0;   // no span decode step over it
     size_t need = sla::plan_cache(make_pages(nullptr, c), n_seqs > c->n_slots ? n_seqs : c->n_slots).bytes;
     sla::PagedCall a = {};
     a.c = make_pages(nullptr, c);
@@ -931,7 +932,6 @@ size_t sla_paged_workspace_bytes(const sla_cache_t *c, int32_t n_q_heads, int32_
             const size_t bytes = sla::plan_paged(a, tensor_type(c), 160).bytes;
             if (bytes > need) need = bytes;
         }
-    if (p && four_bits(c)) return 0;   // no span decode step over it
     if (p && n_seqs > 0) {
         const sla_layout_t l = layout_of(c, n_q_heads, n_seqs, c->head_dim * (int64_t)n_q_heads, c->head_dim);
         const size_t bytes = sla_workspace_bytes(&l, p, 1, (int64_t)c->table_width * c->page_tokens);

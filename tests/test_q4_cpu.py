@@ -72,6 +72,15 @@ def test_workspace_sizes(sla):
         assert sla.sla_paged_workspace_bytes(c, 16, 4, 4) == 0, name
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_no_workspace_for_span_steps_that_there_are_none_of(sla, dtype):
+    """Whatever the batch, no sequences among them."""
+    c, params = cache_of(sla, dtype=dtype), sla.make_params(8, 0)
+    for n_seqs, n_new in ((0, 0), (0, 5), (4, 4), (4, 4096)):
+        assert sla.sla_paged_workspace_bytes(c, 16, n_seqs, n_new) > 0
+        assert sla.sla_paged_workspace_bytes(c, 16, n_seqs, n_new, params=params) == 0
+
+
 def test_make_cache_checks_its_tensors(sla):
     k = torch.zeros(4, 2, sla.q4_plane_bytes(16, 64), dtype=torch.uint8)
     t, n, r = torch.zeros(3, 5, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
