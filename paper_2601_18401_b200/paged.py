@@ -17,12 +17,13 @@ class PagedCache:
 
     def __init__(self, n_pages: int, n_slots: int, max_tokens: int, *, n_q_heads: int, n_kv_heads: int, head_dim: int = 128,
                  page_tokens: int = 64, dtype: torch.dtype = torch.bfloat16, device: int = 0, max_batch: Optional[int] = None,
-                 max_new: int = 8192, params: Optional[B.sla_params_t] = None, share: Optional["PagedCache"] = None,
+                 max_new: Optional[int] = None, params: Optional[B.sla_params_t] = None, share: Optional["PagedCache"] = None,
                  four_bits: bool = False):
         """four_bits: keys and values are rounded to four bits as they are appended (dtype is then that of the calls' tensors), and there is
-        no span decode step.  max_batch, max_new: the most sequences and new tokens of one call (they size the workspace); params: of the span decode
-        step, when it is used.  share: the cache of another layer, whose table, lengths, counts, handle (a workspace for that layer's
-        heads) and, where they are not given, params this one uses; pages, slots and lengths have to be the same."""
+        no span decode step.  max_batch, max_new: the most sequences and new tokens of one call (they size the workspace; n_slots and 8192, or those of share, where
+        they are not given); params: of the span decode step, when it is used.  share: the cache of another layer, whose table, lengths,
+        counts and, where they are not given, params this one uses, and a handle of the layers that share it unless this layer's calls need
+        a larger workspace than they have; pages, slots and lengths have to be the same."""
         dev = torch.device("cuda", device)
         width = -(-max_tokens // page_tokens)
         if share is not None and (share.k.shape[0], share.cache.page_tokens, *share.table.shape) != (n_pages, page_tokens, n_slots, width):
@@ -46,13 +47,17 @@ class PagedCache:
         else:
             self.cache = B.make_cache(self.k, self.v, self.table, self.n_tokens, self.ref)
         self.params = share.params if params is None and share is not None else params
-        if share is None:
-            need = B.sla_paged_workspace_bytes(self.cache, n_q_heads, max_batch or n_slots, max_new, params=params)
-            if need == 0:
-                raise ValueError("shapes or parameters the library does not support")
-            self.handle = B.Handle(device, need)
-        else:
-            self.handle = share.handle
+        self.max_batch = max_batch or (n_slots if share is None else share.max_batch)
+        self.max_new = max_new if max_new is not None else 8192 if share is None else share.max_new
+        need = B.sla_paged_workspace_bytes(self.cache, n_q_heads, self.max_batch, self.max_new, params=None if four_bits else self.params)
+        if share is None and need == 0:
+            raise ValueError("shapes or parameters the library does not support")
+        self.handles = [] if share is None else share.handles   # of the layers that share the table
+        enough = [] if share is None else [h for h in (share.handle, *share.handles) if h.workspace_bytes >= need]
+        if not enough:
+            enough = [B.Handle(device, need)]
+            self.handles += enough
+        self.handle = enough[0]
 
     def extend(self, cu_new=None, *, seq=None):
         """Room for the new tokens of every sequence -> position of each one's first, -1 where refused."""
@@ -88,5 +93,10 @@ class PagedCache:
         B.sla_cache_copy(self.handle, self.cache, pairs)
 
     def poll(self) -> int:
-        """Waits and returns the status of the calls so far (SLA_OK, SLA_ERR_CACHE_FULL, ..)."""
-        return B.sla_poll_status(self.handle)
+        """Waits and returns the status of the calls so far (SLA_OK, SLA_ERR_CACHE_FULL, ..), those of the layers that share the table included;
+        where several have something to report, the next poll returns the next."""
+        for handle in self.handles:
+            status = B.sla_poll_status(handle)
+            if status != B.SLA_OK:
+                return status
+        return B.SLA_OK

@@ -856,6 +856,50 @@ def test_serving_from_two_layers(sla, dtype):
     assert a.poll() == sla.SLA_OK
 
 
+@pytest.mark.parametrize("order", [(True, False), (False, True), (True, False, True)])
+def test_layers_of_both_kinds_share_a_table(sla, order):
+    """Whichever is the first: each gives what it gives alone, in calls as large as its max_new, and a poll of either sees what went wrong."""
+    from paper_2601_18401_b200.paged import PagedCache
+    new = [6000, 2190, 1, 1]
+    cu, seq = cu_of(new), U.device_ints([2, 0, 1, 3])
+    T = sum(new)
+    kn, vn, q = (normal((T, h, 128), BF16, 40 + i, 0.3) for i, h in enumerate((8, 8, 32)))
+    shape = dict(n_q_heads=32, n_kv_heads=8, max_batch=4, max_new=8192)
+
+    def calls(c, first):
+        c.append(cu, first, kn, vn, seq=seq)
+        return [*c.attend(q, cu, seq=seq, max_new=6000, first=first), *c.attend(q[:4], seq=seq), *c.read(seq=seq, cu_new=U.device_ints([0, 9, 9, 9, 9]), n_new=9)]
+    layers = []
+    for four in order:
+        layers.append(PagedCache(1100, 4, 1100 * 64, four_bits=four, share=layers[0] if layers else None, **shape))
+    assert len({c.handle for c in layers}) == 1 + (order[0] and False in order)
+    more = PagedCache(1100, 4, 1100 * 64, share=layers[0], **shape)   # (a handle that is large enough is used again)
+    assert more.handle is layers[order.index(False)].handle and more.handles is layers[0].handles
+    del more
+    first = layers[0].extend(cu, seq=seq)
+    got = [calls(c, first) for c in layers]
+    for c in layers:
+        assert c.poll() == sla.SLA_OK
+    for four, outs in zip(order, got):
+        alone = PagedCache(1100, 4, 1100 * 64, four_bits=four, **shape)
+        for a, b in zip(outs, calls(alone, alone.extend(cu, seq=seq))):
+            assert torch.equal(a, b)
+        assert alone.poll() == sla.SLA_OK
+        del alone
+    for c in layers:                                   # what one layer's call finds is reported by any of them, once
+        c.read(U.device_ints([0, 1]), U.device_ints([10 ** 6]), n_new=1)
+        assert [x.poll() for x in layers[::-1]] == [sla.SLA_ERR_DEVICE_INDEX] + [sla.SLA_OK] * (len(layers) - 1)
+
+
+def test_a_layer_that_needs_no_more_shares_the_handle(sla):
+    from paper_2601_18401_b200.paged import PagedCache
+    shape = dict(n_q_heads=8, n_kv_heads=2, head_dim=64, page_tokens=32, max_new=300)
+    a = PagedCache(40, 6, 500, four_bits=True, **shape)
+    for four in (True, False):
+        b = PagedCache(40, 6, 500, share=a, four_bits=four, n_q_heads=8, n_kv_heads=2, head_dim=64, page_tokens=32)
+        assert b.handle is a.handle
+
+
 def test_a_step_can_be_captured(sla):
     """Room, tokens, attention and reading back in a graph, replayed as the sequences grow; a second graph of the same handle beside it."""
     from paper_2601_18401_b200.paged import PagedCache
