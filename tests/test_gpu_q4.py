@@ -586,6 +586,22 @@ def test_more_new_tokens_than_max_new_are_flagged(sla, max_new):
     h.close()
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("G,max_new", [(1, 1), (1, 4), (4, 1), (4, 2), (4, 4), (2, 3), (8, 2), (16, 1)])
+def test_more_few_new_tokens_than_max_new_are_always_flagged(sla, dtype, d, G, max_new):
+    """On the kernels of few rows, four, eight and sixteen of them; the sequence of max_new tokens beside it has its results."""
+    h = sla.Handle(0, 1 << 28)
+    n, new = [100, 60, 10], [2 * max_new, max_new, 0]
+    cache, k, v, table, q, cu = build(sla, n, new, G=G, dtype=dtype, d=d)
+    out = torch.full((q.shape[0] + 8, *q.shape[1:]), 7.0, dtype=dtype, device="cuda:0")
+    o, lse = sla.sla_paged_attention(h, q, cache, cu, max_new=max_new, out=out[:q.shape[0]])
+    assert sla.sla_poll_status(h) == sla.SLA_ERR_DEVICE_INDEX
+    assert (out[q.shape[0]:] == 7).all()
+    ref = reference(q, k, v, table, n, new, G, 0, d ** -0.5, 16)
+    U.check_attention(o[2 * max_new:], lse[2 * max_new:], [t[2 * max_new:] for t in ref], dtype)
+    h.close()
+
+
 @pytest.mark.parametrize("dtype,d,hkv,G", [(BF16, 128, 8, 4), (BF16, 64, 2, 16), (BF16, 128, 2, 1), (F32, 64, 1, 16)])
 @pytest.mark.parametrize("n_seqs,n_new", [(4, 4), (3, 40), (40, 300)])
 def test_a_workspace_of_the_size_asked_for_is_enough(sla, dtype, d, hkv, G, n_seqs, n_new):
