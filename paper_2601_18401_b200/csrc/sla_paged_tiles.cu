@@ -88,6 +88,7 @@ template <int D, bool kQ4> struct Layout {
     static constexpr int kSlots = D == 128 ? 3 : 6, kSlotBytes = kQ4 ? kKeys * (D / 2 + D / 16) : 0;
     static constexpr int kOffQ = 0, kOffKV = 2 * kTileBytes, kOffCodes = kOffKV + kStages * kTileBytes, kOffMeta = kOffCodes + kSlots * kSlotBytes;
     static constexpr int kSmem = kOffMeta + 3072;
+    static_assert(kStages >= 4, "the waits for a stream's tile before look up to four stages back");
 };
 
 // What a segment is to the warps of the CTA.
@@ -960,8 +961,9 @@ paged_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CU
                     const bool need = !fresh && bm > m_ref + kRescaleThreshold;
                     if (__any_sync(0xffffffffu, need)) {
                         // the PV of the stream's tile before must have landed before O is touched
-                        // (its stage has not been used again: a stream has every tile of the unit but at most one, or every second one,
-                        // so that the tile before lies at most two places back, and the ring is longer than that)
+                        // (a stream has every tile of the unit but at most one, or every second one, so that the tile before lies at most two
+                        // places, four stages, back.  Its stage may hold V of the present tile by now, but no later one: the stream
+                        // gives that up when P of the present tile, which this warp still owes, has met it.  So the parity is that of the tile before.)
                         const int before = j - step;
                         const uint32_t v = 2 * (tiles + s.place(before < lx ? before + hx - lx : before)) + 1u;
                         if (!(ok = ptx::mbar_wait_warp(bar_kv_empty + 80 * x + 8 * (v % kStages), (v / kStages) & 1u, abort_flag))) break;
