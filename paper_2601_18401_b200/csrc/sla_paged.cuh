@@ -404,7 +404,7 @@ struct alignas(16) Cut {
 };
 // Partial results: part p of a unit of R rows has its normalised sums at o + p * R * D and its log2-sum-exp at lse2 + p * R (-inf: no
 // keys; the sums are then not written).  Eight columns of all rows lie together, row by row: where a thread has a row, the threads of a
-// warp write and read 1 KB on end.  (sla_paged_decode.cu joins its own parts and has them as [R, D].)
+// warp write and read 1 KB on end.  (sla_paged_decode.cuh joins its own parts and has them as [R, D].)
 struct Parts {
     float *o, *lse2;
     Cut *cut;             // [ranges]

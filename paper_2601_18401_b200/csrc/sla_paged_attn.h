@@ -41,6 +41,9 @@ void plan_paged_decode(const PagedCall &a, PagedPlan &p, int sm_count);
 cudaError_t launch_paged_decode_attention(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
                                           float *lse, cudaStream_t st, long long *launches);
 
+cudaError_t launch_paged_decode_q4(const void *q, const PagedCall &a, int dtype, const PagedPlan &p, char *scratch, int *counters, void *out,
+                                   float *lse, cudaStream_t st, long long *launches);   // (sla_q4_decode.cu)
+
 // ---- chunks of new tokens, bf16 (sla_paged_tiles.cu)
 bool paged_tiles_supported(const PagedCall &a, int dtype);
 void plan_paged_tiles(const PagedCall &a, PagedPlan &p, int sm_count);

@@ -1,4 +1,4 @@
-// Attention of a few rows over a range of keys of a cache in four bits, by a warp: what paged_decode (sla_paged_decode.cu) calls in the place of
+// Attention of a few rows over a range of keys of a cache in four bits, by a warp: what paged_decode (sla_paged_decode.cuh) calls in the place of
 // attend_bf16.
 //
 // The codes go into mma.sync as the bf16 subnormals that q4::pairs makes of them, without their scales:
