@@ -493,8 +493,10 @@ sla_status_t sla_cache_copy(sla_handle_t handle, const sla_cache_t *cache, const
  *              sequence that is shorter than its new tokens) is 0 and -inf
  * bf16 runs on the tensor cores with fp32 sums (weights are rounded to bf16 before they meet the values),
  * fp32 in fp32.  Over a cache in four bits the values are those that it holds, c s, and the weight that is rounded is p or p s;
- * softmax_scale must be below 2^64 there, and every finite query will do as long as its logits are fp32 numbers (on the path that
- * computes in fp32, as long as the query times the scale is one too: it is formed first). */
+ * softmax_scale must be below 2^64 there.
+ * Any finite query will do as long as its logits do not pass 2^24 in magnitude, beyond which fp32 does not tell them apart
+ * and a row may become NaN; on the path that computes in fp32 the query times the scale, which is formed first, must be an
+ * fp32 number as well. */
 sla_status_t sla_paged_attention(sla_handle_t handle, const void *q, const sla_cache_t *cache,
                                  const sla_batch_t *batch, int32_t n_q_heads, int64_t q_stride_t,
                                  int64_t q_stride_h, int32_t window, float softmax_scale, void *out, float *lse,

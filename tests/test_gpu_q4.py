@@ -468,6 +468,23 @@ def test_a_large_dimension_whose_codes_are_zero(sla, handle, power, new):
     run(sla, handle, [500, 31], new, prep=prep)
 
 
+@pytest.mark.parametrize("dtype,new", [(BF16, [1, 1]), (BF16, [3, 1]), (BF16, [60, 1]), (F32, [1, 1]), (F32, [60, 1])])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 35])
+def test_logits_next_to_the_largest_allowed(sla, handle, dtype, new, size):
+    """Logits up to 2^23, of either sign: results lie among the values, whatever these are, and the sums' logarithms are right.  (D 2^-23 of the
+    sum of a logit's magnitudes, as everywhere; logits times log2 e are rounded to 2 each, a maximum, a weight's exponent and the logarithm
+    at the end: 8 in all.)"""
+    n = [500, 31]
+    cache, k, v, table, q, cu = build(sla, n, new, dtype=dtype, size=size)
+    ref = reference(q, k, v, table, n, new, 4, 0, 1.0, 16)
+    scale = 2.0 ** 23 / ref[3].max().item()                    # (no logit passes the sum of its products' magnitudes)
+    out, lse = sla.sla_paged_attention(handle, q, cache, cu, max_new=max(new), softmax_scale=scale)
+    ref = reference(q, k, v, table, n, new, 4, 0, scale, 16)
+    assert torch.isfinite(out).all()
+    assert out.double().abs().max() <= Q.unpack(v, 16, 128, True).nan_to_num(0).abs().max() * (1 + 2.0 ** -8)
+    assert ((lse.double() - ref[1]).abs() <= 128 * 2.0 ** -23 * ref[3] + 8).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_strided_queries_slots_and_shared_pages(sla, handle, dtype):
     n, new = [100, 64, 250], [3, 1, 40]
