@@ -30,9 +30,11 @@
 //
 // A cache in four bits (kQ4): warp 14 brings pages of codes and scales (bulk copies) into a ring of their own, and the warps that write results make
 // bf16 tiles of them, K and V in turn, where the copies would have put them: values times 2^-48, exact, one product a pair of codes (sla_q4.cuh).
-// The ring of tiles is shorter by one.  8192 tokens that end at 65536 in 8.9 ms, 930 TFLOP/s; 1999 at 30011 in 1.09 ms, 870; 64 at 65536 in 109 us; four
-// prompts of about 2000 tokens at D 64 in 180 us.  What costs the rest against bf16 are the issue slots and registers of those four warps: about 600
-// instructions a tile, which one warp on each scheduler takes about 3500 cycles for.  (Eight warps of 48 registers: 10.1 ms; codes read from
+// The ring of tiles is shorter by one.  8192 tokens that end at 65536 in 8.8 to 9.0 ms, 920 TFLOP/s (over bf16 7.4); 1999 at 30011 in 1.08 ms, 880 (0.93);
+// 64 at 65536 in 109 us (84); four prompts of about 2000 tokens at D 64 in 180 us (127); 1 to 600 tokens of 16 sequences in 84 us (58).  What costs the
+// rest against bf16 is the making: a chain of about 600 instructions a tile, which one warp on each scheduler takes about 3500 cycles for, as long as
+// the rows take for theirs, while issue slots are 44 % used; and every unit that reads the same keys makes them again.  A unit of one stream's rows
+// or fewer wants a tile every 1700 cycles and waits for it.  (Eight warps of 48 registers: 10.1 ms; codes read from
 // global memory into registers a tile ahead: 1999 at 30011 1.18 ms, 1 to 600 tokens of 16 sequences 91 us instead of 84.)
 //
 // Every wait on an mbarrier is bounded; when one runs out the CTA sets a status bit, drains and leaves.  The ranges that it had not
@@ -66,9 +68,9 @@ constexpr float kRescaleThreshold = 8.f;     // log2 units
 // The streams' products are kept at least this many cycles apart.  A stream's tile takes about 3400 cycles of which 1000 are products and 1200
 // exponentials; where both streams come to the same pipe at the same time it takes 4000, and nothing moves them apart again.  (Found at D 128; at
 // D 64, whose products take half, 700 to 1700 were tried and none was better.)
-// Over a cache in four bits the warps that make K and V take a share of the issue slots, and less is better (D 128, 8192 tokens that end at 65536, 1999 at
-// 30011 and 512 at 65536: 8.92 ms, 1108 and 634 us with 1300; 8.87, 1093 and 622 with 1150; 8.96, 1078 and 616 with 1000; 9.23, 1069 and 644 with
-// 800.  D 64, one prompt of 8192: 549 us with 1300, 515 with 800, 513 with 600).
+// Over a cache in four bits the making of K and V moves the streams too, and less is better (D 128, 8192 tokens that end at 65536, 1999 at
+// 30011 and 512 at 65536: 8.77 ms, 1097 and 629 us with 1300; 8.81, 1075 and 614 with 1100; 8.85, 1067 and 611 with 1000; 8.98, 1060 and 618 with
+// 900.  D 64, one prompt of 8192 and four of about 2000: 544 and 185 us with 1300; 510 and 180 with 900; 508 and 179 with 700; 509 and 179 with 500).
 template <int D, bool kQ4> constexpr uint32_t kApart = !kQ4 ? 1300 : D == 128 ? 1100 : 700;
 constexpr uint32_t kPolyPairs = 0x10;        // of every eight pairs of columns, those whose exponentials go to the FMA pipe
 // Tiles whose products a stream adds up in TMEM before O is moved to a sum in memory: the tensor cores cut what does not fit into 24 bits, always

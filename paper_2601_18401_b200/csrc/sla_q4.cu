@@ -4,9 +4,10 @@
 //   read_q4       a warp per row, or several (and 512 values of each): values of a cache in four bits, in bf16 or fp32
 //   read_rows     the same of other caches, whose rows are copied
 //
-// A lane has eight neighbouring dimensions, four lanes a group.  Appending is bound by instructions (245 for eight values of K and of V; ALU pipe
-// 61 %), reading by the latency of a row's loads behind its lookups.  Measured (8 heads, D 128, bf16): 18.7 thousand tokens appended in 28 us, 3.5 TB/s;
-// 65536 rows read in 65 us, 5.3 TB/s, the rate of a copy being 6.5.
+// A lane has eight neighbouring dimensions, four lanes a group.  What appending takes are instructions (245 for eight values of K and of V; issue slots
+// 70 %, ALU pipe 61 %), reading the latency of a row's loads behind its lookups.  Measured in a graph (8 heads, D 128, the rate of a copy being 6.5 TB/s):
+// 18.7 thousand tokens in bf16 appended in 24 us, 4.1 TB/s, in fp32 in 48 us, 3.6 TB/s; 65536 rows read into bf16 in 64 us, 5.4 TB/s, into fp32 in 127 to
+// 132 us, 4.7 TB/s; as many of a cache in bf16 in 88 us, 6.1 TB/s, in fp32 in 172 us, 6.2 TB/s.
 #include "sla_q4.cuh"
 
 namespace sla {
@@ -330,8 +331,8 @@ __global__ void __launch_bounds__(kThreads) read_rows(Pages p, Batch b, const in
 // serves them all.
 // Pieces of a lane: one where there are not enough of them for every warp that the chip holds (a token of each of 48 sequences appended and read
 // 9.9 us, 10.3 with two, 11.1 with four); else two to read and four to append, of which more are on their way together (18.7 thousand
-// tokens of 8 heads of 128: appended in 26.8 us, 29.1 with two, 30.5 with one; 65536 read in 65 us, 68 with four).  In fp32 one is as many bytes
-// as two in bf16: 74 us for three chunks of 4000 to 8192 tokens written and read, 77 with four.
+// tokens of 8 heads of 128: appended in 24.0 us, 24.1 with two, 26.9 with one; 65536 read head by head in 64.5 us, 68 with four or one).  Appending
+// in fp32 takes one, as many bytes as two in bf16: 74 us for three chunks of 4000 to 8192 tokens written and read, 77 with four.
 constexpr int kReadPieces = 2, kAppendPieces = 4;
 struct Grid {
     dim3 ctas;

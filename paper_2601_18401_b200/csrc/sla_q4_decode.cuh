@@ -14,9 +14,9 @@
 // attend_bf16 has them, 32 sequences of 1000 to 65536 took 164 us.  Bulk copies take 40 instructions more a stage: their operands are
 // those of a warp, and each lane's copy goes on its own.)
 //
-// Measured (32/8 heads, D 128, pages of 64 tokens): 32 sequences of 1000 to 65536 in 96 us, 4.8 TB/s of the cache's bytes, 290 instructions for 16 keys of a
-// head; bound by these (ALU pipe 51 %, issue slots 54 % with 12 warps an SM), not by HBM (49 %).  D 64: 64 us; 16 sequences of 500 to 30000 with up to four
-// new tokens 37 us.
+// Measured in a graph (32/8 heads, D 128, pages of 64 tokens): 32 sequences of 1000 to 65536 in 96 us, 4.8 TB/s of the cache's bytes (105 us call by call),
+// D 64 66 us; 16 sequences of 500 to 30000 with up to four new tokens 38 us; one of 2^20 245 us, 4.9 TB/s.  No pipe is full (ALU 51 %, issue slots
+// 54 %, DRAM 49 %): 290 instructions for 16 keys of a head, half of them on the ALU pipe, whose latencies three warps a scheduler do not cover.
 //
 // Powers of two: Q is multiplied by F, a power of two that brings its row's largest magnitude next to 2^125 (a sixteenth of it where codes
 // carry a factor of 16); logits are divided by F 2^-133, in two steps where that and the softmax's scale make no fp32 number.  Weights are
